@@ -10,3 +10,4 @@ from .binding import (  # noqa: F401
     PRED_LAZY, PRED_ABSOLUTE, PRED_RELATIVE, PRED_NEVER, PRED_ALWAYS,
 )
 from . import protocol  # noqa: F401,E402
+from .training import TrainingOps, TRAIN_SYMBOLS, load_training_library  # noqa: F401,E402

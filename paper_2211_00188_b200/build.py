@@ -11,7 +11,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libadacgd.so")
-SOURCES = ["adacgd_api.cu", "adacgd_compress.cu", "adacgd_small.cu", "adacgd_noalloc.cu", "adacgd_gradient.cu"]
+SOURCES = ["adacgd_api.cu", "adacgd_compress.cu", "adacgd_small.cu", "adacgd_noalloc.cu", "adacgd_gradient.cu",
+           "adacgd_train.cu", "adacgd_train_norm.cu", "adacgd_train_loss.cu"]
 
 
 def nvcc_path() -> str:
@@ -25,7 +26,8 @@ def needs_build() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "adacgd.h")]
+    include = os.path.join(ROOT, "include")
+    deps = [os.path.join(d, f) for d in (CSRC, include) for f in os.listdir(d)]
     return any(os.path.getmtime(p) > t for p in deps)
 
 
