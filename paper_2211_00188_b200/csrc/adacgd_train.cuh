@@ -47,6 +47,59 @@ template <> __device__ __forceinline__ float from_f<float>(float v) { return v; 
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// ---- eight consecutive elements, moved in 16-byte pieces ----
+template <typename T> struct Run { uint4 v[sizeof(T) / 2]; };
+
+template <typename T> __device__ __forceinline__ Run<T> load_run(const T* p) {
+  Run<T> r;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = *(reinterpret_cast<const uint4*>(p) + i);
+  return r;
+}
+__device__ __forceinline__ void unpack(const Run<float>& r, float (&o)[8]) {
+  o[0] = __uint_as_float(r.v[0].x); o[1] = __uint_as_float(r.v[0].y); o[2] = __uint_as_float(r.v[0].z); o[3] = __uint_as_float(r.v[0].w);
+  o[4] = __uint_as_float(r.v[1].x); o[5] = __uint_as_float(r.v[1].y); o[6] = __uint_as_float(r.v[1].z); o[7] = __uint_as_float(r.v[1].w);
+}
+__device__ __forceinline__ void unpack(const Run<__nv_bfloat16>& r, float (&o)[8]) {
+  const u32 w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[2 * i] = __uint_as_float(w[i] << 16);
+    o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack(const Run<__half>& r, float (&o)[8]) {
+  const u32 w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+    o[2 * i] = f.x;
+    o[2 * i + 1] = f.y;
+  }
+}
+__device__ __forceinline__ void store_run(float* p, const float (&v)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store_run(__nv_bfloat16* p, const float (&v)[8]) {
+  u32 w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<const u32*>(&b);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store_run(__half* p, const float (&v)[8]) {
+  u32 w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 b = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<const u32*>(&b);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // ---- dropout's random bits: Philox4x32-10 (Salmon et al., SC 2011) ----
 struct Drop {        // what the kernels need of adacgd_drop
   bool on;
@@ -113,20 +166,6 @@ __device__ __forceinline__ float ex2(float x) {
 }
 constexpr float LOG2E = 1.4426950408889634f;
 __device__ __forceinline__ float exp_fast(float x) { return ex2(x * LOG2E); }
-
-// Sum over the CTA (NT threads), the same bits in every thread; the order is fixed.  sh: NT / 32 floats per value.
-template <int NT>
-__device__ __forceinline__ float block_sum(float v, float* sh) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
-  __syncthreads();
-  float t = 0.f;
-#pragma unroll
-  for (int w = 0; w < NT / 32; ++w) t += sh[w];
-  return t;
-}
 
 // The first token of sequence q and the one behind its last, cut off at the ends of the batch.
 __device__ __forceinline__ void seq_bounds(const int32_t* start, long long q, long long tokens, long long each,

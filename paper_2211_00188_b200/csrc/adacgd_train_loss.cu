@@ -1,13 +1,28 @@
 // Token log-probabilities, the preference loss and the clipped policy loss with their gradients (adacgd_train.h).
+//
+// Everything here is passes over rows of logits, a few operations and one or two exponentials an element: memory sets the
+// time (the exponential unit, 16 a clock and SM, is at 70 % when 16-bit logits arrive at the copy rate).
+//   statistics   one pass with the running maximum and sum: sum_j exp(z_j) = s exp(m)
+//   gradient     c (1{j = label} - exp(z_j - m) / s); for the policy loss c is known as soon as the row's log-probability
+//                is, so the same kernel reads the row again, now from the cache, and writes it; the preference loss first
+//                needs the sums of both answers of the pair
+// m and s are kept apart to the end: in a row of the type's lowest values the logarithm of s is lost against m.
+#include <cooperative_groups.h>
+
 #include "adacgd_train.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace adacgd {
 
 namespace {
 
-constexpr int NT = 256;
+// Programmatic dependent launch: the kernels of a call may become resident early and wait for their predecessors' results
+// where they need them.
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Running maximum and sum of exponentials of a set of numbers: sum_j exp(x_j) = s exp(m).  m = -inf: nothing but -inf.
+// m: maximum; s: sum of exponentials relative to base_of(m).  m = -inf: nothing but -inf, s = 0.
 struct Soft { float m, s; };
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ Soft join(Soft a, Soft b) {
@@ -17,98 +32,290 @@ __device__ __forceinline__ Soft join(Soft a, Soft b) {
   r.s = a.s * exp_fast(a.m - base) + b.s * exp_fast(b.m - base);
   return r;
 }
-__device__ __forceinline__ void add(Soft& a, float x) {
-  if (x > a.m) {
-    a.s = a.s * exp_fast(a.m - x);
-    a.m = x;
-  }
-  a.s += exp_fast(x - base_of(a.m));
-}
 
 __device__ __forceinline__ long long label_at(const adacgd_token_rows& r, long long t) {
   return r.label_bytes == 8 ? (long long)((const int64_t*)r.labels)[t] : (long long)((const int32_t*)r.labels)[t];
 }
 
-__device__ Soft block_soft(Soft v, Soft* sh) {
+// A row, or a cluster part of it, cut at 16-byte boundaries: elements [first, first + 8 runs) in whole runs of eight,
+// [begin, first) and [first + 8 runs, end) one by one (at most seven each).
+struct Cut {
+  int begin, first, runs, end;
+};
+template <typename T>
+__device__ __forceinline__ Cut cut_row(const T* row, int vocab, int part, int parts) {
+  constexpr int ALIGN = 16 / sizeof(T);
+  const int head = min(vocab, (int)((ALIGN - ((uintptr_t)row / sizeof(T)) % ALIGN) % ALIGN));
+  const int runs = (vocab - head) >> 3;
+  const int r0 = (int)((long long)runs * part / parts), r1 = (int)((long long)runs * (part + 1) / parts);
+  Cut c;
+  c.first = head + 8 * r0;
+  c.runs = r1 - r0;
+  c.begin = part == 0 ? 0 : c.first;
+  c.end = part == parts - 1 ? vocab : head + 8 * r1;
+  return c;
+}
+// Element of the ragged ends that thread t handles, or -1.
+__device__ __forceinline__ int edge_of(const Cut& c, int t) {
+  const int head = c.first - c.begin, tail0 = c.first + 8 * c.runs;
+  if (t < head) return c.begin + t;
+  t -= head;
+  return t < c.end - tail0 ? tail0 + t : -1;
+}
+
+template <int N>
+__device__ __forceinline__ void absorb(Soft& a, const float (&x)[N]) {
+  float m = x[0];
+#pragma unroll
+  for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
+  if (m > a.m) {
+    a.s *= exp_fast(a.m - m);     // a.m = -inf: s is 0 and stays 0
+    a.m = m;
+  }
+  const float base = base_of(a.m);
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) s += exp_fast(x[j] - base);
+  a.s += s;
+}
+
+// This thread's share of the statistics.
+template <typename T, int NTH>
+__device__ __forceinline__ Soft thread_soft(const T* row, const Cut& c, int t) {
+  constexpr int U = sizeof(T) == 2 ? 4 : 2;   // runs under way at a time: 64 bytes
+  Soft a = {-INFINITY, 0.f};
+  const int e = edge_of(c, t);
+  if (e >= 0) {
+    const float x[1] = {to_f(row[e])};
+    absorb(a, x);
+  }
+  const T* p = row + c.first;
+  int r = t;
+  for (; r + (U - 1) * NTH < c.runs; r += U * NTH) {
+    Run<T> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = load_run(p + 8ll * (r + u * NTH));
+    float x[U * 8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float y[8];
+      unpack(raw[u], y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[u * 8 + j] = y[j];
+    }
+    absorb(a, x);
+  }
+  for (; r < c.runs; r += NTH) {
+    float x[8];
+    unpack(load_run(p + 8ll * r), x);
+    absorb(a, x);
+  }
+  return a;
+}
+
+// Before thread_soft: the CTAs of a cluster announce themselves.
+template <bool CLUSTER>
+__device__ __forceinline__ void row_begin() {
+  if (CLUSTER) cg::this_cluster().barrier_arrive();
+}
+
+// The statistics of the row's threads joined, the same bits in each: a warp, a CTA or a cluster.
+template <int NTH, bool CLUSTER>
+__device__ __forceinline__ Soft row_soft(Soft a, Soft* sh, Soft* xch) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    Soft w;
-    w.m = __shfl_xor_sync(0xffffffffu, v.m, o);
-    w.s = __shfl_xor_sync(0xffffffffu, v.s, o);
-    v = join(v, w);
+    Soft b;
+    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
+    a = join(a, b);
   }
+  if (NTH == 32) {
+    __syncwarp();   // what the lanes have read of the row they may now write
+    return a;
+  }
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = a;
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
-  __syncthreads();
-  Soft t = sh[0];
+  // maximum first, then the sums against it: one exponential a warp instead of a chain of joins
+  float m = -INFINITY, s = 0.f;
 #pragma unroll
-  for (int w = 1; w < NT / 32; ++w) t = join(t, sh[w]);
-  return t;
+  for (int w = 0; w < NTH / 32; ++w) m = fmaxf(m, sh[w].m);
+  const float base = base_of(m);
+  const int lane = threadIdx.x & 31;
+  float f = lane < NTH / 32 ? sh[lane].s * exp_fast(sh[lane].m - base) : 0.f;
+#pragma unroll
+  for (int o = NTH / 64; o > 0; o >>= 1) f += __shfl_xor_sync(0xffffffffu, f, o);
+  s = __shfl_sync(0xffffffffu, f, 0);
+  a.m = m;
+  a.s = s;
+  if (CLUSTER) {
+    cg::cluster_group cl = cg::this_cluster();
+    const int parts = (int)cl.num_blocks();
+    cl.barrier_wait();   // of row_begin: the other CTAs have started
+    if (threadIdx.x < parts) *cl.map_shared_rank(&xch[cl.block_rank()], threadIdx.x) = a;
+    cl.sync();      // every CTA's writes have arrived; nobody writes to another CTA after this
+    m = -INFINITY;
+    for (int k = 0; k < parts; ++k) m = fmaxf(m, xch[k].m);
+    s = 0.f;
+    for (int k = 0; k < parts; ++k) s += xch[k].s * exp_fast(xch[k].m - base_of(m));
+    a.m = m;
+    a.s = s;
+  }
+  return a;
 }
 
-template <typename T>
-__device__ Soft row_soft(const T* x, int vocab, Soft* sh) {
-  Soft v = {-INFINITY, 0.f};
-  for (int j = threadIdx.x; j < vocab; j += NT) add(v, to_f(x[j]));
-  return block_soft(v, sh);
-}
-
-// The row's gradient c (1{j = label} - softmax_j), softmax_j = exp(x_j - base) inv.  Not exp(x_j - lse): in a row of the
-// type's lowest values the logarithm of the sum is lost against the maximum.
-template <typename T>
-__device__ void row_grad(const T* x, T* d, int vocab, long long label, float c, float base, float inv) {
-  for (int j = threadIdx.x; j < vocab; j += NT) {
-    const float p = exp_fast(to_f(x[j]) - base) * inv;
-    d[j] = from_f<T>(j == label ? c * (1.f - p) : -c * p);
+// c (1{j = label} - softmax_j) for this thread's share; softmax_j = exp(x_j - base) inv.  `same`: the gradient's row is
+// aligned as the logits' is.
+template <typename T, int NTH>
+__device__ __forceinline__ void thread_grad(const T* row, T* d, const Cut& c, int t, bool same, int label, float coef, float base,
+                                            float inv) {
+  const float neg = -coef * inv;
+  const int e = edge_of(c, t);
+  if (e >= 0) {
+    const float g = neg * exp_fast(to_f(row[e]) - base);
+    d[e] = from_f<T>(e == label ? coef + g : g);
+  }
+  const T* p = row + c.first;
+  T* q = d + c.first;
+  const int lab = label - c.first;
+  const int lab_run = lab >= 0 ? lab >> 3 : -1;
+  constexpr int U = sizeof(T) == 2 ? 4 : 2;
+  for (int r0 = t; r0 < c.runs; r0 += U * NTH) {
+    Run<T> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r0 + u * NTH < c.runs) raw[u] = load_run(p + 8ll * (r0 + u * NTH));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * NTH;
+      if (r >= c.runs) break;
+      float x[8];
+      unpack(raw[u], x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = neg * exp_fast(x[j] - base);
+      if (r == lab_run) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if ((lab & 7) == j) x[j] += coef;
+      }
+      if (same) {
+        store_run(q + 8ll * r, x);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[8ll * r + j] = from_f<T>(x[j]);
+      }
+    }
   }
 }
-template <typename T>
-__device__ void row_zero(T* d, int vocab) {
-  for (int j = threadIdx.x; j < vocab; j += NT) d[j] = from_f<T>(0.f);
+template <typename T, int NTH>
+__device__ __forceinline__ void thread_zero(T* d, const Cut& c, int t) {   // c cut by the gradient's own alignment
+  const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const int e = edge_of(c, t);
+  if (e >= 0) d[e] = from_f<T>(0.f);
+  for (int r = t; r < c.runs; r += NTH) store_run(d + c.first + 8ll * r, z);
 }
-
 template <typename T>
-__global__ void __launch_bounds__(NT) k_logp(adacgd_token_rows r, float* __restrict__ logp, float* __restrict__ lse,
-                                             float* __restrict__ base_out, float* __restrict__ inv_out) {
-  __shared__ Soft sh[NT / 32];
-  const long long t = blockIdx.x;
-  if (r.mask && !r.mask[t]) {
-    if (threadIdx.x == 0) {
-      logp[t] = 0.f;
-      if (lse) lse[t] = 0.f;
+__device__ __forceinline__ bool same_phase(const T* a, const T* b) { return (((uintptr_t)a ^ (uintptr_t)b) & 15) == 0; }
+
+// Where a thread stands: its row, its number among the row's threads, the row's part it works on.
+template <int NTH, bool CLUSTER> struct Place {
+  static constexpr int CTA = NTH < 128 ? 128 : NTH;
+  static constexpr int ROWS = CTA / NTH;
+  long long row;
+  int t, part, parts;
+  __device__ __forceinline__ Place() {
+    t = NTH == 32 ? (int)(threadIdx.x & 31) : (int)threadIdx.x;
+    part = 0;
+    parts = 1;
+    if (CLUSTER) {
+      part = (int)cg::this_cluster().block_rank();
+      parts = (int)cg::this_cluster().num_blocks();
+    }
+    row = (long long)(blockIdx.x / parts) * ROWS + (NTH == 32 ? threadIdx.x >> 5 : 0);
+  }
+};
+
+// --------------------------------------------------------------------------
+// log-probabilities
+// --------------------------------------------------------------------------
+// zb, sum: z_label - base and s, from which the preference loss takes its log-probabilities in 64 bits; base: for its
+// gradient.  Either all three or logp are given.
+template <typename T, int NTH, bool CLUSTER>
+__global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_logp(adacgd_token_rows r, float* __restrict__ logp, float* __restrict__ lse,
+                                                                   float* __restrict__ zb, float* __restrict__ sum,
+                                                                   float* __restrict__ base_out) {
+  __shared__ Soft sh[32], xch[8];
+  pdl_trigger();
+  const Place<NTH, CLUSTER> at;
+  const long long row = at.row;
+  if (row >= r.tokens) return;       // whole warps; only where NTH == 32
+  if (r.mask && !r.mask[row]) {      // the same in the whole cluster
+    if (at.t == 0 && at.part == 0) {
+      if (logp) logp[row] = 0.f;
+      if (lse) lse[row] = 0.f;
     }
     return;
   }
-  const T* x = (const T*)r.logits + t * r.logits_stride;
-  const Soft v = row_soft(x, (int)r.vocab, sh);
-  if (threadIdx.x == 0) {
-    const long long y = label_at(r, t);
-    const float z = y >= 0 && y < r.vocab ? to_f(x[y]) : NAN, base = base_of(v.m), l = logf(v.s);
-    logp[t] = (z - base) - l;
-    if (lse) lse[t] = base + l;
-    if (base_out) {
-      base_out[t] = base;
-      inv_out[t] = 1.f / v.s;
+  row_begin<CLUSTER>();
+  const T* x = (const T*)r.logits + row * r.logits_stride;
+  const int vocab = (int)r.vocab;
+  float z = 0.f;
+  if (at.t == 0) {
+    const long long y = label_at(r, row);
+    z = y >= 0 && y < vocab ? to_f(x[y]) : NAN;
+  }
+  const Soft a = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut_row(x, vocab, at.part, at.parts), at.t), sh, xch);
+  if (at.t == 0 && at.part == 0) {
+    const float base = base_of(a.m);
+    if (logp) {
+      const float l = logf(a.s);
+      logp[row] = (z - base) - l;
+      if (lse) lse[row] = base + l;
+    } else {
+      zb[row] = z - base;
+      sum[row] = a.s;
+      base_out[row] = base;
     }
   }
 }
 
 template <int NTH>
-__device__ double block_sum_f64(double v, double* sh) {
+__device__ __forceinline__ double block_sum_f64(double v, double* sh) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   __syncthreads();
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
   __syncthreads();
   double t = 0.0;
+#pragma unroll 8
   for (int w = 0; w < NTH / 32; ++w) t += sh[w];
   return t;
 }
 
-// One CTA a pair: margin, loss and the coefficient of the pair's two sequences.
-__global__ void __launch_bounds__(NT) k_pairs(adacgd_preference_args a, const float* __restrict__ logp, float* __restrict__ coef,
-                                              double* __restrict__ part) {
-  __shared__ double sh[NT / 32];
+// True in every thread of the CTA that is the last of `n` to arrive; the counter is zero again then.
+__device__ __forceinline__ bool last_to_arrive(u32* ticket, u32 n) {
+  __shared__ u32 last;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    last = atomicAdd(ticket, 1u) == n - 1u;
+    if (last) *ticket = 0u;
+  }
+  __syncthreads();
+  if (last) __threadfence();
+  return last != 0u;
+}
+
+// --------------------------------------------------------------------------
+// preference loss
+// --------------------------------------------------------------------------
+constexpr int PAIR_NT = 256;
+
+// One CTA a pair: margin, loss and the coefficients of the pair's two sequences; the last CTA takes the mean.
+__global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, const float* __restrict__ zb, const float* __restrict__ sum,
+                                                   float* __restrict__ coef, double* __restrict__ part, u32* ticket) {
+  __shared__ double sh[PAIR_NT / 32];
+  pdl_wait();
+  pdl_trigger();   // the gradient kernel is large: it is let in when this one has its operands
   const long long pairs = a.rows.sequences / 2, each = a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences;
   const long long p = blockIdx.x;
   double d[2], inv[2];
@@ -116,66 +323,82 @@ __global__ void __launch_bounds__(NT) k_pairs(adacgd_preference_args a, const fl
     const long long q = p + k * pairs;
     long long lo, hi;
     seq_bounds(a.rows.seq_start, q, a.rows.tokens, each, &lo, &hi);
-    double sum = 0.0, diff = 0.0, cnt = 0.0;
-    for (long long t = lo + threadIdx.x; t < hi; t += NT) {
+    double total = 0.0, diff = 0.0, cnt = 0.0;
+    for (long long t = lo + threadIdx.x; t < hi; t += PAIR_NT) {
       if (a.rows.mask && !a.rows.mask[t]) continue;
+      const double logp = (double)zb[t] - log((double)sum[t]);
       cnt += 1.0;
-      sum += (double)logp[t];
-      diff += (double)logp[t] - (double)a.ref_logp[t];
+      total += logp;
+      diff += logp - (double)a.ref_logp[t];
     }
-    sum = block_sum_f64<NT>(sum, sh);
-    diff = block_sum_f64<NT>(diff, sh);
-    cnt = block_sum_f64<NT>(cnt, sh);
+    total = block_sum_f64<PAIR_NT>(total, sh);
+    diff = block_sum_f64<PAIR_NT>(diff, sh);
+    cnt = block_sum_f64<PAIR_NT>(cnt, sh);
     inv[k] = a.length_normalized && cnt > 0.0 ? 1.0 / cnt : 1.0;
     d[k] = diff * inv[k];
-    if (threadIdx.x == 0 && a.seq_logp) a.seq_logp[q] = (float)(sum * inv[k]);
+    if (threadIdx.x == 0 && a.seq_logp) a.seq_logp[q] = (float)(total * inv[k]);
   }
-  if (threadIdx.x) return;
-  const double beta = (double)a.beta, h = beta * (d[0] - d[1]), e = (double)a.label_smoothing;
-  double l, g;
-  if (a.kind == ADACGD_PREF_SIGMOID) {
-    const double tail = log1p(exp(-fabs(h)));               // -log sigma(|h|)
-    l = (1.0 - e) * (tail + fmax(-h, 0.0)) + e * (tail + fmax(h, 0.0));
-    const double sg = 1.0 / (1.0 + exp(-h)), sn = 1.0 / (1.0 + exp(h));
-    g = e * sg - (1.0 - e) * sn;
-    if (h != h) l = h;
-  } else if (a.kind == ADACGD_PREF_HINGE) {
-    l = h < 1.0 ? 1.0 - h : (h != h ? h : 0.0);
-    g = h < 1.0 ? -1.0 : (h != h ? h : 0.0);
-  } else {
-    const double u = h / beta - 0.5 / beta;
-    l = u * u;
-    g = 2.0 * u / beta;
+  if (threadIdx.x == 0) {
+    const double beta = (double)a.beta, h = beta * (d[0] - d[1]), e = (double)a.label_smoothing;
+    double l, g;
+    if (a.kind == ADACGD_PREF_SIGMOID) {
+      const double tail = log1p(exp(-fabs(h)));               // -log sigma(|h|)
+      l = (1.0 - e) * (tail + fmax(-h, 0.0)) + e * (tail + fmax(h, 0.0));
+      const double sg = 1.0 / (1.0 + exp(-h)), sn = 1.0 / (1.0 + exp(h));
+      g = e * sg - (1.0 - e) * sn;
+      if (h != h) l = h;
+    } else if (a.kind == ADACGD_PREF_HINGE) {
+      l = h < 1.0 ? 1.0 - h : (h != h ? h : 0.0);
+      g = h < 1.0 ? -1.0 : (h != h ? h : 0.0);
+    } else {
+      const double u = h / beta - 0.5 / beta;
+      l = u * u;
+      g = 2.0 * u / beta;
+    }
+    const double c = (double)a.grad_scale * g * beta / (double)pairs;
+    coef[p] = (float)(c * inv[0]);
+    coef[p + pairs] = (float)(-c * inv[1]);
+    if (a.margin) a.margin[p] = (float)h;
+    part[p] = l;
   }
-  const double c = (double)a.grad_scale * g * beta / (double)pairs;
-  coef[p] = (float)(c * inv[0]);
-  coef[p + pairs] = (float)(-c * inv[1]);
-  if (a.margin) a.margin[p] = (float)h;
-  part[p] = l;
-}
-
-__global__ void __launch_bounds__(NT) k_mean_pairs(const double* __restrict__ part, long long pairs, float* __restrict__ loss) {
-  __shared__ double sh[NT / 32];
+  if (!last_to_arrive(ticket, (u32)pairs)) return;
   double v = 0.0;
-  for (long long p = threadIdx.x; p < pairs; p += NT) v += part[p];
-  v = block_sum_f64<NT>(v, sh);
-  if (threadIdx.x == 0) *loss = (float)(v / (double)pairs);
+  for (long long q = threadIdx.x; q < pairs; q += PAIR_NT) v += __ldcg(&part[q]);
+  v = block_sum_f64<PAIR_NT>(v, sh);
+  if (threadIdx.x == 0) *a.loss = (float)(v / (double)pairs);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(NT) k_preference_grad(adacgd_preference_args a, const float* __restrict__ coef,
-                                                        const float* __restrict__ base, const float* __restrict__ inv) {
-  const long long t = blockIdx.x;
-  T* d = (T*)a.dlogits + t * a.dlogits_stride;
-  if (a.rows.mask && !a.rows.mask[t]) return row_zero(d, (int)a.rows.vocab);
-  const long long q = seq_of(a.rows.seq_start, t, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences);
-  row_grad((const T*)a.rows.logits + t * a.rows.logits_stride, d, (int)a.rows.vocab, label_at(a.rows, t), coef[q],
-           base[t], inv[t]);
+// The gradient once the pairs' coefficients are known: element by element, no reduction.
+template <typename T, int NTH>
+__global__ void __launch_bounds__(Place<NTH, false>::CTA) k_preference_grad(adacgd_preference_args a, const float* __restrict__ coef,
+                                                                            const float* __restrict__ base,
+                                                                            const float* __restrict__ sum, int parts) {
+  const Place<NTH, false> at;
+  const long long row = NTH == 32 ? at.row : at.row / parts;
+  const int part = NTH == 32 ? 0 : (int)(at.row - row * parts);
+  if (row >= a.rows.tokens) return;
+  T* d = (T*)a.dlogits + row * a.dlogits_stride;
+  const int vocab = (int)a.rows.vocab;
+  if (a.rows.mask && !a.rows.mask[row]) {
+    pdl_wait();      // dlogits may be the logits that the first kernel reads
+    thread_zero<T, NTH>(d, cut_row(d, vocab, part, parts), at.t);
+    return;
+  }
+  const long long q = seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences);
+  const long long y = label_at(a.rows, row);
+  const T* x = (const T*)a.rows.logits + row * a.rows.logits_stride;
+  pdl_wait();
+  thread_grad<T, NTH>(x, d, cut_row(x, vocab, part, parts), at.t, same_phase(x, d), y >= 0 && y < vocab ? (int)y : -1, coef[q], base[row],
+                      1.f / sum[row]);
 }
 
+// --------------------------------------------------------------------------
+// policy loss
+// --------------------------------------------------------------------------
 // Weight of every sequence's tokens; one CTA walks all of them.  weight[sequences] = counted tokens.
 __global__ void __launch_bounds__(1024) k_policy_weights(adacgd_policy_args a, float* __restrict__ weight) {
   __shared__ double sh[32];
+  pdl_trigger();
   const long long S = a.rows.sequences, n = a.rows.tokens, each = a.rows.seq_start ? 0 : n / S;
   double total = 0.0, used = 0.0;
   if (a.per_sequence) {
@@ -185,11 +408,18 @@ __global__ void __launch_bounds__(1024) k_policy_weights(adacgd_policy_args a, f
       seq_bounds(a.rows.seq_start, q, n, each, &lo, &hi);
       for (long long t = lo + lane; t < hi; t += 32) c += !a.rows.mask || a.rows.mask[t];
       for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-      if (lane == 0) weight[q] = (float)c;
-      if (lane == 0) { total += (double)c; used += c > 0 ? 1.0 : 0.0; }
+      if (lane == 0) {
+        weight[q] = (float)c;
+        total += (double)c;
+        used += c > 0 ? 1.0 : 0.0;
+      }
     }
+  } else if (a.rows.mask) {
+    long long c = 0;
+    for (long long t = threadIdx.x; t < n; t += 1024) c += a.rows.mask[t] != 0;
+    total = (double)c;
   } else {
-    for (long long t = threadIdx.x; t < n; t += 1024) total += !a.rows.mask || a.rows.mask[t];
+    total = threadIdx.x == 0 ? (double)n : 0.0;
   }
   total = block_sum_f64<1024>(total, sh);
   used = block_sum_f64<1024>(used, sh);
@@ -198,61 +428,73 @@ __global__ void __launch_bounds__(1024) k_policy_weights(adacgd_policy_args a, f
     else weight[q] = total > 0.0 ? (float)(1.0 / total) : 0.f;
   }
   if (threadIdx.x == 0) weight[S] = (float)total;
+  if (n > 0) return;
+  if (threadIdx.x == 0) *a.loss = 0.f;      // no rows: no other kernel follows
+  if (threadIdx.x < 3 && a.stats) a.stats[threadIdx.x] = 0.f;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(NT) k_policy(adacgd_policy_args a, const float* __restrict__ weight, float* __restrict__ tl,
-                                               float* __restrict__ tk, float* __restrict__ tc) {
-  __shared__ Soft sh[NT / 32];
-  const long long t = blockIdx.x;
+// A row's loss and, from the cache, its gradient.  The last CTA adds the rows up in a fixed order.
+template <typename T, int NTH, bool CLUSTER>
+__global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_policy(adacgd_policy_args a, const float* __restrict__ weight, float* tl,
+                                                                     float* tk, float* tc, u32* ticket) {
+  constexpr int CTA = Place<NTH, CLUSTER>::CTA;
+  __shared__ Soft sh[32], xch[8];
+  __shared__ double shd[32];
+  const Place<NTH, CLUSTER> at;
+  const long long row = at.row;
   const int vocab = (int)a.rows.vocab;
-  T* d = a.dlogits ? (T*)a.dlogits + t * a.dlogits_stride : nullptr;
-  if (a.rows.mask && !a.rows.mask[t]) {
-    if (threadIdx.x == 0) {
-      tl[t] = tk[t] = tc[t] = 0.f;
-      if (a.logp) a.logp[t] = 0.f;
+  if (row < a.rows.tokens) {
+    T* d = a.dlogits ? (T*)a.dlogits + row * a.dlogits_stride : nullptr;
+    if (a.rows.mask && !a.rows.mask[row]) {
+      if (at.t == 0 && at.part == 0) {
+        tl[row] = tk[row] = tc[row] = 0.f;
+        if (a.logp) a.logp[row] = 0.f;
+      }
+      if (d) thread_zero<T, NTH>(d, cut_row(d, vocab, at.part, at.parts), at.t);
+      pdl_wait();
+    } else {
+      row_begin<CLUSTER>();
+      const T* x = (const T*)a.rows.logits + row * a.rows.logits_stride;
+      const long long y = label_at(a.rows, row);
+      const int label = y >= 0 && y < vocab ? (int)y : -1;
+      const float z = label >= 0 ? to_f(x[label]) : NAN;
+      const float A = a.advantages[row], old = a.old_logp[row], ref = a.ref_logp ? a.ref_logp[row] : 0.f;
+      const Cut cut = cut_row(x, vocab, at.part, at.parts);
+      const Soft v = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut, at.t), sh, xch);
+      const float base = base_of(v.m), logp = (z - base) - logf(v.s);
+      const long long q = seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences);
+      pdl_wait();
+      const float w = weight[q], r = expf(logp - old);
+      const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
+      const float held = (r < lo ? lo : (r > hi ? hi : r)) * A, gain = r * A;   // NaN goes through
+      float c = gain <= held ? -gain : 0.f, tok = gain <= held ? -gain : -held, kl = 0.f;
+      if (a.ref_logp) {
+        const float u = ref - logp, e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0
+        kl = e1 - u;
+        c = c - a.kl_beta * e1;
+        tok = tok + a.kl_beta * kl;
+      }
+      if (d) thread_grad<T, NTH>(x, d, cut, at.t, same_phase(x, d), label, a.grad_scale * (w * c), base, 1.f / v.s);
+      if (at.t == 0 && at.part == 0) {
+        if (a.logp) a.logp[row] = logp;
+        tl[row] = w * tok;
+        tk[row] = kl;
+        tc[row] = gain > held ? 1.f : 0.f;
+      }
     }
-    if (d) row_zero(d, vocab);
-    return;
+  } else {
+    pdl_wait();
   }
-  const T* x = (const T*)a.rows.logits + t * a.rows.logits_stride;
-  const long long y = label_at(a.rows, t);
-  const float z = y >= 0 && y < vocab ? to_f(x[y]) : NAN;
-  const Soft v = row_soft(x, vocab, sh);
-  const float base = base_of(v.m), l = logf(v.s), logp = (z - base) - l;
-  const long long q = seq_of(a.rows.seq_start, t, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences);
-  const float w = weight[q], A = a.advantages[t], r = expf(logp - a.old_logp[t]);
-  const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
-  const float held = (r < lo ? lo : (r > hi ? hi : r)) * A, gain = r * A;   // NaN goes through
-  float c = gain <= held ? -gain : 0.f, tok = gain <= held ? -gain : -held, kl = 0.f;
-  if (a.ref_logp) {
-    const float u = a.ref_logp[t] - logp, e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0
-    kl = e1 - u;
-    c = c - a.kl_beta * e1;
-    tok = tok + a.kl_beta * kl;
-  }
-  if (d) row_grad(x, d, vocab, y, a.grad_scale * (w * c), base, 1.f / v.s);
-  if (threadIdx.x == 0) {
-    if (a.logp) a.logp[t] = logp;
-    tl[t] = w * tok;
-    tk[t] = kl;
-    tc[t] = gain > held ? 1.f : 0.f;
-  }
-}
-
-__global__ void __launch_bounds__(1024) k_policy_sum(adacgd_policy_args a, const float* __restrict__ weight,
-                                                     const float* __restrict__ tl, const float* __restrict__ tk,
-                                                     const float* __restrict__ tc) {
-  __shared__ double sh[32];
+  if (!last_to_arrive(ticket, gridDim.x)) return;
   double l = 0.0, k = 0.0, c = 0.0;
-  for (long long t = threadIdx.x; t < a.rows.tokens; t += 1024) {
-    l += (double)tl[t];
-    k += (double)tk[t];
-    c += (double)tc[t];
+  for (long long t = threadIdx.x; t < a.rows.tokens; t += CTA) {
+    l += (double)__ldcg(&tl[t]);
+    k += (double)__ldcg(&tk[t]);
+    c += (double)__ldcg(&tc[t]);
   }
-  l = block_sum_f64<1024>(l, sh);
-  k = block_sum_f64<1024>(k, sh);
-  c = block_sum_f64<1024>(c, sh);
+  l = block_sum_f64<CTA>(l, shd);
+  k = block_sum_f64<CTA>(k, shd);
+  c = block_sum_f64<CTA>(c, shd);
   if (threadIdx.x) return;
   const double total = (double)weight[a.rows.sequences];
   *a.loss = (float)l;
@@ -263,32 +505,98 @@ __global__ void __launch_bounds__(1024) k_policy_sum(adacgd_policy_args a, const
   }
 }
 
-int done(int n) { return cudaGetLastError() == cudaSuccess ? n : -1; }
+// --------------------------------------------------------------------------
+// launches
+// --------------------------------------------------------------------------
+// Launches with optional cluster and programmatic dependence on the kernel before.
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kern)(KArgs...), unsigned grid, int block, int cluster, bool pdl, cudaStream_t st, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  int n = 0;
+  if (cluster > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = cluster;
+    at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (pdl) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
+}
 
-template <typename T>
-int logp_t(const adacgd_token_rows& r, float* logp, float* lse, cudaStream_t st) {
-  k_logp<T><<<(unsigned)r.tokens, NT, 0, st>>>(r, logp, lse, nullptr, nullptr);
-  return done(1);
+// Threads a row (32, 128 or 512) and CTAs a row (a cluster, only where rows would leave SMs idle).
+struct Split { int threads, cluster; };
+Split split_of(long long rows, long long vocab, int sms) {
+  Split s;
+  s.threads = vocab <= 1024 ? 32 : (vocab <= 8192 ? 128 : 512);
+  s.cluster = 1;
+  if (rows < sms && vocab > 512) {
+    s.threads = vocab <= 2048 ? 128 : 512;
+    while (s.cluster < 8 && rows * s.cluster * 2 <= 2 * sms && vocab / (s.cluster * 2) >= 4096) s.cluster *= 2;
+  }
+  return s;
+}
+
+#define BY_SPLIT(s, call)                                                                          \
+  (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())     \
+   : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }()) \
+   : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }()) \
+                      : ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }()))
+
+unsigned ctas(long long rows, int rows_per_cta, int cluster) {
+  return (unsigned)((rows + rows_per_cta - 1) / rows_per_cta * cluster);
 }
 
 template <typename T>
-int preference_t(const TrainScratch& s, const adacgd_preference_args& a, cudaStream_t st) {
-  int n = 2;
-  const long long pairs = a.rows.sequences / 2;
-  if (a.rows.tokens) k_logp<T><<<(unsigned)a.rows.tokens, NT, 0, st>>>(a.rows, s.logp, nullptr, s.tok_a, s.tok_b), ++n;
-  k_pairs<<<(unsigned)pairs, NT, 0, st>>>(a, s.logp, s.seq, s.part);
-  k_mean_pairs<<<1, NT, 0, st>>>(s.part, pairs, a.loss);
-  if (a.dlogits && a.rows.tokens) k_preference_grad<T><<<(unsigned)a.rows.tokens, NT, 0, st>>>(a, s.seq, s.tok_a, s.tok_b), ++n;
-  return done(n);
+cudaError_t logp_t(const adacgd_token_rows& r, float* logp, float* lse, float* zb, float* sum, float* base, int sms, cudaStream_t st) {
+  const Split s = split_of(r.tokens, r.vocab, sms);
+  return BY_SPLIT(s, (launch(k_logp<T, NTH, CL>, ctas(r.tokens, Place<NTH, CL>::ROWS, s.cluster), Place<NTH, CL>::CTA, s.cluster, false,
+                             st, r, logp, lse, zb, sum, base)));
 }
 
 template <typename T>
-int policy_t(const TrainScratch& s, const adacgd_policy_args& a, cudaStream_t st) {
-  int n = 2;
-  k_policy_weights<<<1, 1024, 0, st>>>(a, s.seq);
-  if (a.rows.tokens) k_policy<T><<<(unsigned)a.rows.tokens, NT, 0, st>>>(a, s.seq, s.tok_a, s.tok_b, s.tok_c), ++n;
-  k_policy_sum<<<1, 1024, 0, st>>>(a, s.seq, s.tok_a, s.tok_b, s.tok_c);
-  return done(n);
+int preference_t(const TrainScratch& s, const adacgd_preference_args& a, int sms, cudaStream_t st) {
+  int n = 1;
+  const long long rows = a.rows.tokens;
+  if (rows) {
+    if (logp_t<T>(a.rows, nullptr, nullptr, s.tok_a, s.tok_b, s.tok_c, sms, st) != cudaSuccess) return -1;
+    ++n;
+  }
+  if (launch(k_pairs, (unsigned)(a.rows.sequences / 2), PAIR_NT, 1, rows > 0, st, a, s.tok_a, s.tok_b, s.seq, s.part, s.tickets) != cudaSuccess)
+    return -1;
+  if (a.dlogits && rows) {
+    const long long v = a.rows.vocab;
+    cudaError_t e;
+    if (v <= 1024) {
+      e = launch(k_preference_grad<T, 32>, ctas(rows, 4, 1), 128, 1, true, st, a, s.seq, s.tok_c, s.tok_b, 1);
+    } else {
+      const int parts = (int)((v + 32767) / 32768);
+      e = v <= 8192 ? launch(k_preference_grad<T, 128>, (unsigned)rows, 128, 1, true, st, a, s.seq, s.tok_c, s.tok_b, 1)
+                    : launch(k_preference_grad<T, 512>, (unsigned)(rows * parts), 512, 1, true, st, a, s.seq, s.tok_c, s.tok_b, parts);
+    }
+    if (e != cudaSuccess) return -1;
+    ++n;
+  }
+  return n;
+}
+
+template <typename T>
+int policy_t(const TrainScratch& s, const adacgd_policy_args& a, int sms, cudaStream_t st) {
+  if (launch(k_policy_weights, 1u, 1024, 1, false, st, a, s.seq) != cudaSuccess) return -1;
+  if (!a.rows.tokens) return 1;
+  const Split sp = split_of(a.rows.tokens, a.rows.vocab, sms);
+  const cudaError_t e = BY_SPLIT(sp, (launch(k_policy<T, NTH, CL>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, sp.cluster), Place<NTH, CL>::CTA,
+                                             sp.cluster, true, st, a, s.seq, s.tok_a, s.tok_b, s.tok_c, s.tickets + 1)));
+  return e == cudaSuccess ? 2 : -1;
 }
 
 }  // namespace
@@ -301,13 +609,13 @@ int policy_t(const TrainScratch& s, const adacgd_policy_args& a, cudaStream_t st
   }
 
 int launch_token_logp(const adacgd_token_rows& r, float* logp, float* lse, int sms, cudaStream_t st) {
-  BY_TYPE(r.dtype, (logp_t<T>(r, logp, lse, st)))
+  BY_TYPE(r.dtype, (logp_t<T>(r, logp, lse, nullptr, nullptr, nullptr, sms, st) == cudaSuccess ? 1 : -1))
 }
 int launch_preference(const TrainScratch& s, const adacgd_preference_args& a, int sms, cudaStream_t st) {
-  BY_TYPE(a.rows.dtype, (preference_t<T>(s, a, st)))
+  BY_TYPE(a.rows.dtype, (preference_t<T>(s, a, sms, st)))
 }
 int launch_policy(const TrainScratch& s, const adacgd_policy_args& a, int sms, cudaStream_t st) {
-  BY_TYPE(a.rows.dtype, (policy_t<T>(s, a, st)))
+  BY_TYPE(a.rows.dtype, (policy_t<T>(s, a, sms, st)))
 }
 
 }  // namespace adacgd

@@ -20,59 +20,6 @@ namespace adacgd {
 
 namespace {
 
-// Eight consecutive elements as loaded.
-template <typename T> struct Run { uint4 v[sizeof(T) / 2]; };
-
-template <typename T> __device__ __forceinline__ Run<T> load_run(const T* p) {
-  Run<T> r;
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = *(reinterpret_cast<const uint4*>(p) + i);
-  return r;
-}
-__device__ __forceinline__ void unpack(const Run<float>& r, float (&o)[8]) {
-  o[0] = __uint_as_float(r.v[0].x); o[1] = __uint_as_float(r.v[0].y); o[2] = __uint_as_float(r.v[0].z); o[3] = __uint_as_float(r.v[0].w);
-  o[4] = __uint_as_float(r.v[1].x); o[5] = __uint_as_float(r.v[1].y); o[6] = __uint_as_float(r.v[1].z); o[7] = __uint_as_float(r.v[1].w);
-}
-__device__ __forceinline__ void unpack(const Run<__nv_bfloat16>& r, float (&o)[8]) {
-  const u32 w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    o[2 * i] = __uint_as_float(w[i] << 16);
-    o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void unpack(const Run<__half>& r, float (&o)[8]) {
-  const u32 w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-    o[2 * i] = f.x;
-    o[2 * i + 1] = f.y;
-  }
-}
-__device__ __forceinline__ void store_run(float* p, const float (&v)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void store_run(__nv_bfloat16* p, const float (&v)[8]) {
-  u32 w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    w[i] = *reinterpret_cast<const u32*>(&b);
-  }
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void store_run(__half* p, const float (&v)[8]) {
-  u32 w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __half2 b = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-    w[i] = *reinterpret_cast<const u32*>(&b);
-  }
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 // Bit j set: element j of the block is kept.
 __device__ __forceinline__ u32 keep_bits(u64 block, const Drop& d) {
   const uint4 w = philox(block, d);
@@ -383,6 +330,7 @@ __global__ void __launch_bounds__(Shape<NTH>::CTA) k_norm_bwd(adacgd_norm_backwa
     nparts = (int)cg::this_cluster().num_blocks();
     rank = (int)cg::this_cluster().block_rank();
   }
+  if (CLUSTER) cg::this_cluster().sync();   // every CTA has started before any writes into another's shared memory
   const int all = (int)a.cols;
   const int span = CLUSTER ? ((all + nparts - 1) / nparts + 7) / 8 * 8 : all;   // columns of a part, a multiple of eight
   const int c0 = rank * span, cols = min(span, all - c0) < 0 ? 0 : min(span, all - c0);
