@@ -12,9 +12,7 @@ using namespace adacgd;
 
 struct adacgd_train {
   TrainScratch s;
-  cudaStream_t stream;
-  int device;
-  int sms;
+  Where at;
   long long launches;
   char err[256];
 };
@@ -40,7 +38,7 @@ adacgd_status check_device(adacgd_train* t, const char* entry) {
   int dev = -1;
   const cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_fail(t, entry, e);
-  if (dev != t->device) return invalid(t, entry, "the current CUDA device is not the one the context was created on");
+  if (dev != t->at.device) return invalid(t, entry, "the current CUDA device is not the one the context was created on");
   return ADACGD_OK;
 }
 
@@ -127,7 +125,7 @@ static size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 size_t train_scratch_bytes(long long max_tokens, long long max_cols) {
   const size_t n = (size_t)max_tokens;
-  return up256(NTRAIN_TICKETS * 4) + 5 * up256(n * 4) + up256((n + 1) * 4) + up256(n * 8) +
+  return up256(NTRAIN_TICKETS * 4) + 5 * up256(n * 4) + up256((n + 1) * 4) + up256(n * 8) + up256(3 * MAX_GROUPS * 8) +
          up256((size_t)NORM_PARTS * 2 * (size_t)max_cols * 4);
 }
 
@@ -143,6 +141,7 @@ void carve_train_scratch(TrainScratch* s, void* base, long long max_tokens, long
   s->tok_c = (float*)take(n * 4);
   s->seq = (float*)take((n + 1) * 4);
   s->part = (double*)take(n * 8);
+  s->own = (double*)take(3 * MAX_GROUPS * 8);
   s->norm_part = (float*)take((size_t)NORM_PARTS * 2 * (size_t)max_cols * 4);
   s->max_tokens = max_tokens;
   s->max_cols = max_cols;
@@ -182,12 +181,12 @@ adacgd_status adacgd_train_init(adacgd_train** out, int64_t max_tokens, int64_t 
   adacgd_train* t = new (std::nothrow) adacgd_train();
   if (!t) return invalid(nullptr, entry, "out of host memory");
   carve_train_scratch(&t->s, workspace_dev, max_tokens, max_cols);
-  t->stream = (cudaStream_t)cuda_stream;
-  t->device = dev;
-  t->sms = dp->sms;
+  t->at.stream = (cudaStream_t)cuda_stream;
+  t->at.device = dev;
+  t->at.sms = dp->sms;
   t->launches = 0;
   t->err[0] = 0;
-  e = cudaMemsetAsync(t->s.tickets, 0, NTRAIN_TICKETS * 4, t->stream);
+  e = cudaMemsetAsync(t->s.tickets, 0, NTRAIN_TICKETS * 4, t->at.stream);
   if (e != cudaSuccess) {
     delete t;
     return cuda_fail(nullptr, entry, e);
@@ -223,7 +222,7 @@ adacgd_status adacgd_dropout(adacgd_train* t, const adacgd_dropout_args* a) {
   const adacgd_status st = check_device(t, entry);
   if (st != ADACGD_OK) return st;
   if (a->rows == 0) return ADACGD_OK;
-  return launched(t, entry, launch_dropout(*a, t->sms, t->stream));
+  return launched(t, entry, launch_dropout(*a, t->at));
 }
 
 adacgd_status adacgd_layer_norm(adacgd_train* t, const adacgd_norm_args* a) {
@@ -257,7 +256,7 @@ adacgd_status adacgd_layer_norm(adacgd_train* t, const adacgd_norm_args* a) {
   const adacgd_status st = check_device(t, entry);
   if (st != ADACGD_OK) return st;
   if (a->rows == 0) return ADACGD_OK;
-  return launched(t, entry, launch_layer_norm(*a, t->sms, t->stream));
+  return launched(t, entry, launch_layer_norm(*a, t->at));
 }
 
 adacgd_status adacgd_layer_norm_backward(adacgd_train* t, const adacgd_norm_backward_args* a) {
@@ -293,11 +292,11 @@ adacgd_status adacgd_layer_norm_backward(adacgd_train* t, const adacgd_norm_back
   if (st != ADACGD_OK) return st;
   if (a->rows == 0) {
     cudaError_t e = cudaSuccess;
-    if (a->dweight) e = cudaMemsetAsync(a->dweight, 0, a->cols * ps, t->stream);
-    if (e == cudaSuccess && a->dbias) e = cudaMemsetAsync(a->dbias, 0, a->cols * ps, t->stream);
+    if (a->dweight) e = cudaMemsetAsync(a->dweight, 0, a->cols * ps, t->at.stream);
+    if (e == cudaSuccess && a->dbias) e = cudaMemsetAsync(a->dbias, 0, a->cols * ps, t->at.stream);
     return e == cudaSuccess ? ADACGD_OK : cuda_fail(t, entry, e);
   }
-  return launched(t, entry, launch_layer_norm_backward(t->s, *a, t->sms, t->stream));
+  return launched(t, entry, launch_layer_norm_backward(t->s, *a, t->at));
 }
 
 adacgd_status adacgd_token_logp(adacgd_train* t, const adacgd_token_rows* rows, float* logp, float* lse) {
@@ -315,7 +314,7 @@ adacgd_status adacgd_token_logp(adacgd_train* t, const adacgd_token_rows* rows, 
   const adacgd_status st = check_device(t, entry);
   if (st != ADACGD_OK) return st;
   if (n == 0) return ADACGD_OK;
-  return launched(t, entry, launch_token_logp(*rows, logp, lse, t->sms, t->stream));
+  return launched(t, entry, launch_token_logp(*rows, logp, lse, t->at));
 }
 
 adacgd_status adacgd_preference_loss(adacgd_train* t, const adacgd_preference_args* a) {
@@ -345,7 +344,7 @@ adacgd_status adacgd_preference_loss(adacgd_train* t, const adacgd_preference_ar
     return invalid(t, entry, "an output overlaps another argument without dlogits being the same matrix as logits");
   const adacgd_status st = check_device(t, entry);
   if (st != ADACGD_OK) return st;
-  return launched(t, entry, launch_preference(t->s, *a, t->sms, t->stream));
+  return launched(t, entry, launch_preference(t->s, *a, t->at));
 }
 
 adacgd_status adacgd_policy_loss(adacgd_train* t, const adacgd_policy_args* a) {
@@ -377,7 +376,7 @@ adacgd_status adacgd_policy_loss(adacgd_train* t, const adacgd_policy_args* a) {
     return invalid(t, entry, "an output overlaps another argument without dlogits being the same matrix as logits");
   const adacgd_status st = check_device(t, entry);
   if (st != ADACGD_OK) return st;
-  return launched(t, entry, launch_policy(t->s, *a, t->sms, t->stream));
+  return launched(t, entry, launch_policy(t->s, *a, t->at));
 }
 
 }  // extern "C"

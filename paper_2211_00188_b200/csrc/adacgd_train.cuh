@@ -5,6 +5,8 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "adacgd_internal.cuh"
 #include "adacgd_train.h"
 
@@ -22,21 +24,43 @@ struct TrainScratch {
   float* tok_c;    // [tokens] 1 where the clipped term has taken the gradient
   float* seq;      // [tokens + 1] per sequence: weight or gradient coefficient; the last is the total
   double* part;    // [tokens] per pair: loss
+  double* own;     // [3][MAX_GROUPS] sums of groups of the policy loss kernel's CTAs
   float* norm_part; // [NORM_PARTS][2][max_cols] partial weight and bias gradients
   long long max_tokens, max_cols;
 };
 constexpr int NTRAIN_TICKETS = 1024;
+constexpr int MAX_GROUPS = NTRAIN_TICKETS - 2;
+
+// Where a call runs.
+struct Where {
+  int device, sms;
+  cudaStream_t stream;
+};
+
+// CTAs of a kernel that fit on an SM; the first call on a device also raises its limit of dynamic shared memory.  One table
+// per kernel.  0 after an error.
+constexpr int TRAIN_DEVICES = 64;
+template <typename K>
+int resident_ctas(K kern, std::atomic<int> (&table)[TRAIN_DEVICES], int device, int threads, int smem) {
+  if (device < 0 || device >= TRAIN_DEVICES) return 0;
+  int n = table[device].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  if (smem > 0 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return 0;
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, threads, smem) != cudaSuccess || n < 1) return 0;
+  table[device].store(n, std::memory_order_relaxed);
+  return n;
+}
 
 size_t train_scratch_bytes(long long max_tokens, long long max_cols);
 void carve_train_scratch(TrainScratch* s, void* base, long long max_tokens, long long max_cols);
 
 // Each returns the number of kernels launched, or -1 after a failed launch.
-int launch_dropout(const adacgd_dropout_args& a, int sms, cudaStream_t stream);
-int launch_layer_norm(const adacgd_norm_args& a, int sms, cudaStream_t stream);
-int launch_layer_norm_backward(const TrainScratch& s, const adacgd_norm_backward_args& a, int sms, cudaStream_t stream);
-int launch_token_logp(const adacgd_token_rows& r, float* logp, float* lse, int sms, cudaStream_t stream);
-int launch_preference(const TrainScratch& s, const adacgd_preference_args& a, int sms, cudaStream_t stream);
-int launch_policy(const TrainScratch& s, const adacgd_policy_args& a, int sms, cudaStream_t stream);
+int launch_dropout(const adacgd_dropout_args& a, const Where& at);
+int launch_layer_norm(const adacgd_norm_args& a, const Where& at);
+int launch_layer_norm_backward(const TrainScratch& s, const adacgd_norm_backward_args& a, const Where& at);
+int launch_token_logp(const adacgd_token_rows& r, float* logp, float* lse, const Where& at);
+int launch_preference(const TrainScratch& s, const adacgd_preference_args& a, const Where& at);
+int launch_policy(const TrainScratch& s, const adacgd_policy_args& a, const Where& at);
 
 // ---- element types ----
 __device__ __forceinline__ float to_f(float v) { return v; }
@@ -81,23 +105,28 @@ __device__ __forceinline__ void store_run(float* p, const float (&v)[8]) {
   reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
   reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
-__device__ __forceinline__ void store_run(__nv_bfloat16* p, const float (&v)[8]) {
+// Eight elements of a 16-bit type in 16 bytes, each rounded to nearest.
+template <typename T> __device__ __forceinline__ uint4 pack_run(const float (&v)[8]);
+template <> __device__ __forceinline__ uint4 pack_run<__nv_bfloat16>(const float (&v)[8]) {
   u32 w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
     w[i] = *reinterpret_cast<const u32*>(&b);
   }
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void store_run(__half* p, const float (&v)[8]) {
+template <> __device__ __forceinline__ uint4 pack_run<__half>(const float (&v)[8]) {
   u32 w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const __half2 b = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
     w[i] = *reinterpret_cast<const u32*>(&b);
   }
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T> __device__ __forceinline__ void store_run(T* p, const float (&v)[8]) {
+  *reinterpret_cast<uint4*>(p) = pack_run<T>(v);
 }
 
 // ---- dropout's random bits: Philox4x32-10 (Salmon et al., SC 2011) ----

@@ -8,7 +8,6 @@
 //                needs the sums of both answers of the pair
 // m and s are kept apart to the end: in a row of the type's lowest values the logarithm of s is lost against m.
 #include <cooperative_groups.h>
-
 #include "adacgd_train.cuh"
 
 namespace cg = cooperative_groups;
@@ -22,14 +21,42 @@ namespace {
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// m: maximum; s: sum of exponentials relative to base_of(m).  m = -inf: nothing but -inf, s = 0.
+// m: maximum; s: sum of exponentials relative to it.  m = -inf: nothing but -inf, s = 0.
 struct Soft { float m, s; };
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+// Exponents are base 2: exp(z - m) is taken as 2^(z L - fl(m L)), L = log2 e, one fused operation an element.  fl(m L) is as good
+// an offset as m L, because the logarithm is taken against the same number.  Where m L overflows, z - m is formed first.
+constexpr float BIG = 2.3e38f;
+constexpr float LN2 = 0.6931471805599453f;
+
+// 2^(x L) relative to the maximum m
+__device__ __forceinline__ bool plain_range(float m) { return fabsf(m) <= BIG; }
+template <int N>
+__device__ __forceinline__ void exp_all(float (&x)[N], float m) {
+  if (plain_range(m)) {
+    const float b = -(m * LOG2E);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = ex2(fmaf(x[i], LOG2E, b));
+  } else {
+    const float b = base_of(m);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = ex2((x[i] - b) * LOG2E);
+  }
+}
+// what a sum kept relative to a is worth relative to m >= a
+__device__ __forceinline__ float rel(float a, float m) {
+  if (m == -INFINITY) return 0.f;
+  return plain_range(m) ? ex2(a * LOG2E - m * LOG2E) : ex2((a - m) * LOG2E);
+}
+// log2 of exp(z) relative to m
+__device__ __forceinline__ float log2_rel(float z, float m) {
+  return plain_range(m) ? fmaf(z, LOG2E, -(m * LOG2E)) : (z - base_of(m)) * LOG2E;
+}
+
 __device__ __forceinline__ Soft join(Soft a, Soft b) {
   Soft r;
   r.m = fmaxf(a.m, b.m);
-  const float base = base_of(r.m);
-  r.s = a.s * exp_fast(a.m - base) + b.s * exp_fast(b.m - base);
+  r.s = a.s * rel(a.m, r.m) + b.s * rel(b.m, r.m);
   return r;
 }
 
@@ -64,50 +91,73 @@ __device__ __forceinline__ int edge_of(const Cut& c, int t) {
 }
 
 template <int N>
-__device__ __forceinline__ void absorb(Soft& a, const float (&x)[N]) {
+__device__ __forceinline__ void absorb(Soft& a, float (&x)[N]) {
   float m = x[0];
 #pragma unroll
   for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
   if (m > a.m) {
-    a.s *= exp_fast(a.m - m);     // a.m = -inf: s is 0 and stays 0
+    a.s *= rel(a.m, m);          // a.m = -inf: s is 0 and stays 0
     a.m = m;
   }
-  const float base = base_of(a.m);
-  float s = 0.f;
+  exp_all(x, a.m);
+  float s[2] = {x[0], N > 1 ? x[1 % N] : 0.f};
 #pragma unroll
-  for (int j = 0; j < N; ++j) s += exp_fast(x[j] - base);
-  a.s += s;
+  for (int j = 2; j < N; ++j) s[j & 1] += x[j];
+  a.s += s[0] + s[1];
+}
+
+// Runs of eight elements that a thread has under way: 64 bytes, loaded before the batch in front of it is worked on, so that
+// loads and exponentials overlap within the thread.
+template <typename T> struct Batch {
+  static constexpr int U = sizeof(T) == 2 ? 4 : 2;
+  Run<T> r[U];
+};
+template <typename T, int NTH>
+__device__ __forceinline__ void load_batch(Batch<T>& b, const T* p, int run) {
+#pragma unroll
+  for (int u = 0; u < Batch<T>::U; ++u) b.r[u] = load_run(p + 8ll * (run + u * NTH));
 }
 
 // This thread's share of the statistics.
 template <typename T, int NTH>
 __device__ __forceinline__ Soft thread_soft(const T* row, const Cut& c, int t) {
-  constexpr int U = sizeof(T) == 2 ? 4 : 2;   // runs under way at a time: 64 bytes
+  constexpr int U = Batch<T>::U;
   Soft a = {-INFINITY, 0.f};
+  const T* p = row + c.first;
+  const int whole = c.runs / (U * NTH);      // batches that all threads have in full
+  Batch<T> next;
+  if (whole > 0) load_batch<T, NTH>(next, p, t);
   const int e = edge_of(c, t);
   if (e >= 0) {
-    const float x[1] = {to_f(row[e])};
+    float x[1] = {to_f(row[e])};
     absorb(a, x);
   }
-  const T* p = row + c.first;
-  int r = t;
-  for (; r + (U - 1) * NTH < c.runs; r += U * NTH) {
-    Run<T> raw[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = load_run(p + 8ll * (r + u * NTH));
+  for (int k = 1; k <= whole; ++k) {
+    const Batch<T> b = next;
+    if (k < whole) load_batch<T, NTH>(next, p, k * U * NTH + t);
     float x[U * 8];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float y[8];
-      unpack(raw[u], y);
+      unpack(b.r[u], y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[u * 8 + j] = y[j];
     }
     absorb(a, x);
   }
-  for (; r < c.runs; r += NTH) {
-    float x[8];
-    unpack(load_run(p + 8ll * r), x);
+  const int r0 = whole * U * NTH + t;
+  if (r0 < c.runs) {      // the rest: up to U runs, loaded together
+    float x[U * 8];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r0 + u * NTH < c.runs) next.r[u] = load_run(p + 8ll * (r0 + u * NTH));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float y[8];
+      unpack(next.r[u], y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[u * 8 + j] = r0 + u * NTH < c.runs ? y[j] : -INFINITY;
+    }
     absorb(a, x);
   }
   return a;
@@ -122,26 +172,24 @@ __device__ __forceinline__ void row_begin() {
 // The statistics of the row's threads joined, the same bits in each: a warp, a CTA or a cluster.
 template <int NTH, bool CLUSTER>
 __device__ __forceinline__ Soft row_soft(Soft a, Soft* sh, Soft* xch) {
+  // maxima first, then the sums against the largest: one exponential instead of two a step
+  const float mine = a.m;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    Soft b;
-    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-    a = join(a, b);
-  }
+  for (int o = 16; o > 0; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xffffffffu, a.m, o));
+  a.s *= rel(mine, a.m);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
   if (NTH == 32) {
     __syncwarp();   // what the lanes have read of the row they may now write
     return a;
   }
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = a;
   __syncthreads();
-  // maximum first, then the sums against it: one exponential a warp instead of a chain of joins
   float m = -INFINITY, s = 0.f;
 #pragma unroll
   for (int w = 0; w < NTH / 32; ++w) m = fmaxf(m, sh[w].m);
-  const float base = base_of(m);
   const int lane = threadIdx.x & 31;
-  float f = lane < NTH / 32 ? sh[lane].s * exp_fast(sh[lane].m - base) : 0.f;
+  float f = lane < NTH / 32 ? sh[lane].s * rel(sh[lane].m, m) : 0.f;
 #pragma unroll
   for (int o = NTH / 64; o > 0; o >>= 1) f += __shfl_xor_sync(0xffffffffu, f, o);
   s = __shfl_sync(0xffffffffu, f, 0);
@@ -156,54 +204,63 @@ __device__ __forceinline__ Soft row_soft(Soft a, Soft* sh, Soft* xch) {
     m = -INFINITY;
     for (int k = 0; k < parts; ++k) m = fmaxf(m, xch[k].m);
     s = 0.f;
-    for (int k = 0; k < parts; ++k) s += xch[k].s * exp_fast(xch[k].m - base_of(m));
+    for (int k = 0; k < parts; ++k) s += xch[k].s * rel(xch[k].m, m);
     a.m = m;
     a.s = s;
   }
   return a;
 }
 
-// c (1{j = label} - softmax_j) for this thread's share; softmax_j = exp(x_j - base) inv.  `same`: the gradient's row is
-// aligned as the logits' is.
+// c (1{j = label} - softmax_j) for this thread's share, softmax_j = 2^(x_j L) relative to m, over sum.  `same`: the gradient's row
+// is aligned as the logits' is.  The label's entry (tz: its log2_rel) is written once more, by the thread that wrote it first.
 template <typename T, int NTH>
-__device__ __forceinline__ void thread_grad(const T* row, T* d, const Cut& c, int t, bool same, int label, float coef, float base,
-                                            float inv) {
-  const float neg = -coef * inv;
-  const int e = edge_of(c, t);
-  if (e >= 0) {
-    const float g = neg * exp_fast(to_f(row[e]) - base);
-    d[e] = from_f<T>(e == label ? coef + g : g);
-  }
+__device__ __forceinline__ void thread_grad(const T* row, T* d, const Cut& c, int t, bool same, int label, float tz, float coef, float m,
+                                            float sum) {
+  constexpr int U = Batch<T>::U;
+  const float neg = -coef / sum;
   const T* p = row + c.first;
   T* q = d + c.first;
-  const int lab = label - c.first;
-  const int lab_run = lab >= 0 ? lab >> 3 : -1;
-  constexpr int U = sizeof(T) == 2 ? 4 : 2;
-  for (int r0 = t; r0 < c.runs; r0 += U * NTH) {
-    Run<T> raw[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (r0 + u * NTH < c.runs) raw[u] = load_run(p + 8ll * (r0 + u * NTH));
+  const int batches = (c.runs + U * NTH - 1) / (U * NTH);
+  Batch<T> next;
+  auto fetch = [&](int k) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int r = r0 + u * NTH;
-      if (r >= c.runs) break;
-      float x[8];
-      unpack(raw[u], x);
+      const int r = (k * U + u) * NTH + t;
+      if (r < c.runs) next.r[u] = load_run(p + 8ll * r);
+    }
+  };
+  fetch(0);
+  const int e = edge_of(c, t);
+  if (e >= 0) {
+    float x[1] = {to_f(row[e])};
+    exp_all(x, m);
+    d[e] = from_f<T>(neg * x[0]);
+  }
+  for (int k = 0; k < batches; ++k) {
+    const Batch<T> b = next;
+    if (k + 1 < batches) fetch(k + 1);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = neg * exp_fast(x[j] - base);
-      if (r == lab_run) {
+    for (int u = 0; u < U; ++u) {
+      const int r = (k * U + u) * NTH + t;
+      if (r < c.runs) {
+        float x[8];
+        unpack(b.r[u], x);
+        exp_all(x, m);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if ((lab & 7) == j) x[j] += coef;
-      }
-      if (same) {
-        store_run(q + 8ll * r, x);
-      } else {
+        for (int j = 0; j < 8; ++j) x[j] *= neg;
+        if (same) {
+          store_run(q + 8ll * r, x);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[8ll * r + j] = from_f<T>(x[j]);
+          for (int j = 0; j < 8; ++j) q[8ll * r + j] = from_f<T>(x[j]);
+        }
       }
     }
+  }
+  if (label >= c.begin && label < c.end) {
+    const int in = label - c.first;
+    const bool mine = in >= 0 && in < 8 * c.runs ? (in >> 3) % NTH == t : label == e;
+    if (mine) d[label] = from_f<T>(fmaf(neg, ex2(tz), coef));
   }
 }
 template <typename T, int NTH>
@@ -237,12 +294,12 @@ template <int NTH, bool CLUSTER> struct Place {
 // --------------------------------------------------------------------------
 // log-probabilities
 // --------------------------------------------------------------------------
-// zb, sum: z_label - base and s, from which the preference loss takes its log-probabilities in 64 bits; base: for its
-// gradient.  Either all three or logp are given.
+// zb, sum, top: log2 of exp(z_label) and the sum relative to the maximum, and the maximum, in the units of log2_rel and
+// exp_all, from which the preference loss takes its log-probabilities in 64 bits and its gradient.  Either these or logp.
 template <typename T, int NTH, bool CLUSTER>
 __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_logp(adacgd_token_rows r, float* __restrict__ logp, float* __restrict__ lse,
                                                                    float* __restrict__ zb, float* __restrict__ sum,
-                                                                   float* __restrict__ base_out) {
+                                                                   float* __restrict__ top) {
   __shared__ Soft sh[32], xch[8];
   pdl_trigger();
   const Place<NTH, CLUSTER> at;
@@ -265,15 +322,14 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_logp(adacgd_token_
   }
   const Soft a = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut_row(x, vocab, at.part, at.parts), at.t), sh, xch);
   if (at.t == 0 && at.part == 0) {
-    const float base = base_of(a.m);
+    const float tz = log2_rel(z, a.m);
     if (logp) {
-      const float l = logf(a.s);
-      logp[row] = (z - base) - l;
-      if (lse) lse[row] = base + l;
+      logp[row] = (tz - log2f(a.s)) * LN2;
+      if (lse) lse[row] = base_of(a.m) + logf(a.s);
     } else {
-      zb[row] = z - base;
+      zb[row] = tz;
       sum[row] = a.s;
-      base_out[row] = base;
+      top[row] = a.m;
     }
   }
 }
@@ -326,7 +382,7 @@ __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, con
     double total = 0.0, diff = 0.0, cnt = 0.0;
     for (long long t = lo + threadIdx.x; t < hi; t += PAIR_NT) {
       if (a.rows.mask && !a.rows.mask[t]) continue;
-      const double logp = (double)zb[t] - log((double)sum[t]);
+      const double logp = ((double)zb[t] - log2((double)sum[t])) * 0.6931471805599453;
       cnt += 1.0;
       total += logp;
       diff += logp - (double)a.ref_logp[t];
@@ -368,28 +424,28 @@ __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, con
   if (threadIdx.x == 0) *a.loss = (float)(v / (double)pairs);
 }
 
-// The gradient once the pairs' coefficients are known: element by element, no reduction.
+// The gradient once the pairs' coefficients are known: element by element, `parts` walkers a row.
 template <typename T, int NTH>
 __global__ void __launch_bounds__(Place<NTH, false>::CTA) k_preference_grad(adacgd_preference_args a, const float* __restrict__ coef,
-                                                                            const float* __restrict__ base,
-                                                                            const float* __restrict__ sum, int parts) {
+                                                                            const float* __restrict__ zb, const float* __restrict__ sum,
+                                                                            const float* __restrict__ top, u32 parts) {
   const Place<NTH, false> at;
-  const long long row = NTH == 32 ? at.row : at.row / parts;
-  const int part = NTH == 32 ? 0 : (int)(at.row - row * parts);
+  const long long row = parts == 1 ? at.row : at.row / parts;
+  const int part = parts == 1 ? 0 : (int)(at.row - row * parts);
   if (row >= a.rows.tokens) return;
   T* d = (T*)a.dlogits + row * a.dlogits_stride;
   const int vocab = (int)a.rows.vocab;
-  if (a.rows.mask && !a.rows.mask[row]) {
-    pdl_wait();      // dlogits may be the logits that the first kernel reads
-    thread_zero<T, NTH>(d, cut_row(d, vocab, part, parts), at.t);
+  const bool counts = !a.rows.mask || a.rows.mask[row];
+  const long long y = label_at(a.rows, row);
+  const long long q = seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences);
+  pdl_wait();      // before anything is written: dlogits may be the logits that the first kernel reads
+  if (!counts) {
+    thread_zero<T, NTH>(d, cut_row(d, vocab, part, (int)parts), at.t);
     return;
   }
-  const long long q = seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences);
-  const long long y = label_at(a.rows, row);
   const T* x = (const T*)a.rows.logits + row * a.rows.logits_stride;
-  pdl_wait();
-  thread_grad<T, NTH>(x, d, cut_row(x, vocab, part, parts), at.t, same_phase(x, d), y >= 0 && y < vocab ? (int)y : -1, coef[q], base[row],
-                      1.f / sum[row]);
+  thread_grad<T, NTH>(x, d, cut_row(x, vocab, part, (int)parts), at.t, same_phase(x, d), y >= 0 && y < vocab ? (int)y : -1, zb[row], coef[q],
+                      top[row], sum[row]);
 }
 
 // --------------------------------------------------------------------------
@@ -433,10 +489,38 @@ __global__ void __launch_bounds__(1024) k_policy_weights(adacgd_policy_args a, f
   if (threadIdx.x < 3 && a.stats) a.stats[threadIdx.x] = 0.f;
 }
 
-// A row's loss and, from the cache, its gradient.  The last CTA adds the rows up in a fixed order.
+// A token's loss and its slope with respect to the log-probability, before the token's weight.
+struct Token { float loss, slope, kl; bool clipped; };
+__device__ __forceinline__ Token token_loss(float logp, float old, float A, bool with_ref, float ref, float clip_low, float clip_high,
+                                            float kl_beta) {
+  const float r = expf(logp - old), lo = 1.f - clip_low, hi = 1.f + clip_high;
+  const float held = (r < lo ? lo : (r > hi ? hi : r)) * A, gain = r * A;   // NaN goes through
+  Token k;
+  k.slope = gain <= held ? -gain : 0.f;
+  k.loss = gain <= held ? -gain : -held;
+  k.clipped = gain > held;
+  k.kl = 0.f;
+  if (with_ref) {
+    const float u = ref - logp, e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0
+    k.kl = e1 - u;
+    k.slope = k.slope - kl_beta * e1;
+    k.loss = k.loss + kl_beta * k.kl;
+  }
+  return k;
+}
+__device__ __forceinline__ void write_policy(float* loss, float* stats, double l, double k, double c, double total) {
+  *loss = (float)l;
+  if (stats) {
+    stats[0] = total > 0.0 ? (float)(k / total) : 0.f;
+    stats[1] = total > 0.0 ? (float)(c / total) : 0.f;
+    stats[2] = (float)total;
+  }
+}
+
+// A row's loss and, from the cache, its gradient.  `group`: CTAs that share a completion count (a multiple of the cluster).
 template <typename T, int NTH, bool CLUSTER>
 __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_policy(adacgd_policy_args a, const float* __restrict__ weight, float* tl,
-                                                                     float* tk, float* tc, u32* ticket) {
+                                                                     float* tk, float* tc, double* own, u32* ticket, u32 group) {
   constexpr int CTA = Place<NTH, CLUSTER>::CTA;
   __shared__ Soft sh[32], xch[8];
   __shared__ double shd[32];
@@ -461,48 +545,47 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_policy(adacgd_poli
       const float A = a.advantages[row], old = a.old_logp[row], ref = a.ref_logp ? a.ref_logp[row] : 0.f;
       const Cut cut = cut_row(x, vocab, at.part, at.parts);
       const Soft v = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut, at.t), sh, xch);
-      const float base = base_of(v.m), logp = (z - base) - logf(v.s);
+      const float tz = log2_rel(z, v.m), logp = (tz - log2f(v.s)) * LN2;
       const long long q = seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences);
       pdl_wait();
-      const float w = weight[q], r = expf(logp - old);
-      const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
-      const float held = (r < lo ? lo : (r > hi ? hi : r)) * A, gain = r * A;   // NaN goes through
-      float c = gain <= held ? -gain : 0.f, tok = gain <= held ? -gain : -held, kl = 0.f;
-      if (a.ref_logp) {
-        const float u = ref - logp, e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0
-        kl = e1 - u;
-        c = c - a.kl_beta * e1;
-        tok = tok + a.kl_beta * kl;
-      }
-      if (d) thread_grad<T, NTH>(x, d, cut, at.t, same_phase(x, d), label, a.grad_scale * (w * c), base, 1.f / v.s);
+      const float w = weight[q];
+      const Token tok = token_loss(logp, old, A, a.ref_logp != nullptr, ref, a.clip_low, a.clip_high, a.kl_beta);
+      if (d) thread_grad<T, NTH>(x, d, cut, at.t, same_phase(x, d), label, tz, a.grad_scale * (w * tok.slope), v.m, v.s);
       if (at.t == 0 && at.part == 0) {
         if (a.logp) a.logp[row] = logp;
-        tl[row] = w * tok;
-        tk[row] = kl;
-        tc[row] = gain > held ? 1.f : 0.f;
+        tl[row] = w * tok.loss;
+        tk[row] = tok.kl;
+        tc[row] = tok.clipped ? 1.f : 0.f;
       }
     }
   } else {
     pdl_wait();
   }
-  if (!last_to_arrive(ticket, gridDim.x)) return;
-  double l = 0.0, k = 0.0, c = 0.0;
-  for (long long t = threadIdx.x; t < a.rows.tokens; t += CTA) {
-    l += (double)__ldcg(&tl[t]);
-    k += (double)__ldcg(&tk[t]);
-    c += (double)__ldcg(&tc[t]);
+  // Each group of CTAs is added up by its last one, the groups by the last group's, both in a fixed order.
+  constexpr int ROWS = Place<NTH, CLUSTER>::ROWS;
+  const u32 groups = (gridDim.x + group - 1) / group, g = blockIdx.x / group;
+  if (!last_to_arrive(ticket + 1 + g, min(group, (u32)gridDim.x - g * group))) return;
+  double v[3];
+  {
+    const long long lo = (long long)(g * group / at.parts) * ROWS;
+    const long long hi = min((long long)a.rows.tokens, (long long)(min((g + 1) * group, (u32)gridDim.x) / at.parts) * ROWS);
+    const float* src[3] = {tl, tk, tc};
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      v[i] = 0.0;
+      for (long long t = lo + threadIdx.x; t < hi; t += CTA) v[i] += (double)__ldcg(&src[i][t]);
+      v[i] = block_sum_f64<CTA>(v[i], shd);
+      if (threadIdx.x == 0) own[i * MAX_GROUPS + g] = v[i];
+    }
   }
-  l = block_sum_f64<CTA>(l, shd);
-  k = block_sum_f64<CTA>(k, shd);
-  c = block_sum_f64<CTA>(c, shd);
-  if (threadIdx.x) return;
-  const double total = (double)weight[a.rows.sequences];
-  *a.loss = (float)l;
-  if (a.stats) {
-    a.stats[0] = total > 0.0 ? (float)(k / total) : 0.f;
-    a.stats[1] = total > 0.0 ? (float)(c / total) : 0.f;
-    a.stats[2] = (float)total;
+  if (!last_to_arrive(ticket, groups)) return;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    v[i] = 0.0;
+    for (u32 k = threadIdx.x; k < groups; k += CTA) v[i] += __ldcg(&own[i * MAX_GROUPS + k]);
+    v[i] = block_sum_f64<CTA>(v[i], shd);
   }
+  if (threadIdx.x == 0) write_policy(a.loss, a.stats, v[0], v[1], v[2], (double)weight[a.rows.sequences]);
 }
 
 // --------------------------------------------------------------------------
@@ -510,10 +593,11 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_policy(adacgd_poli
 // --------------------------------------------------------------------------
 // Launches with optional cluster and programmatic dependence on the kernel before.
 template <typename... KArgs, typename... Args>
-cudaError_t launch(void (*kern)(KArgs...), unsigned grid, int block, int cluster, bool pdl, cudaStream_t st, Args&&... args) {
+cudaError_t launch(void (*kern)(KArgs...), unsigned grid, int block, int cluster, bool pdl, cudaStream_t st, int smem, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
   int n = 0;
@@ -533,56 +617,54 @@ cudaError_t launch(void (*kern)(KArgs...), unsigned grid, int block, int cluster
   return cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
 }
 
-// Threads a row (32, 128 or 512) and CTAs a row (a cluster, only where rows would leave SMs idle).
-struct Split { int threads, cluster; };
-Split split_of(long long rows, long long vocab, int sms) {
-  Split s;
-  s.threads = vocab <= 1024 ? 32 : (vocab <= 8192 ? 128 : 512);
-  s.cluster = 1;
-  if (rows < sms && vocab > 512) {
-    s.threads = vocab <= 2048 ? 128 : 512;
-    while (s.cluster < 8 && rows * s.cluster * 2 <= 2 * sms && vocab / (s.cluster * 2) >= 4096) s.cluster *= 2;
-  }
-  return s;
-}
-
-#define BY_SPLIT(s, call)                                                                          \
-  (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())     \
-   : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }()) \
-   : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }()) \
-                      : ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }()))
-
 unsigned ctas(long long rows, int rows_per_cta, int cluster) {
   return (unsigned)((rows + rows_per_cta - 1) / rows_per_cta * cluster);
 }
 
+// Threads a row (32, 128 or 512) and CTAs a row (a cluster, only where rows would leave SMs idle).
+#ifndef V32
+#define V32 4096
+#define V128 65536
+#endif
+struct Split { int threads, cluster; };
+Split split_of(long long rows, long long vocab, const Where& at) {
+  Split s;
+  s.threads = vocab <= V32 ? 32 : (vocab <= V128 ? 128 : 512);
+  s.cluster = 1;
+  while (s.threads < 512 && rows * s.threads < 1024ll * at.sms && vocab > 8 * s.threads) s.threads *= 4;
+  while (s.threads == 512 && s.cluster < 8 && rows * s.cluster * 2 <= 2 * at.sms && vocab / (s.cluster * 2) >= 4096) s.cluster *= 2;
+  return s;
+}
+#define BY_SPLIT(s, call)                                                                            \
+  (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())       \
+   : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }()) \
+   : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }()) \
+                      : ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }()))
+
 template <typename T>
-cudaError_t logp_t(const adacgd_token_rows& r, float* logp, float* lse, float* zb, float* sum, float* base, int sms, cudaStream_t st) {
-  const Split s = split_of(r.tokens, r.vocab, sms);
+cudaError_t logp_t(const adacgd_token_rows& r, float* logp, float* lse, float* zb, float* sum, float* top, const Where& at) {
+  const Split s = split_of(r.tokens, r.vocab, at);
   return BY_SPLIT(s, (launch(k_logp<T, NTH, CL>, ctas(r.tokens, Place<NTH, CL>::ROWS, s.cluster), Place<NTH, CL>::CTA, s.cluster, false,
-                             st, r, logp, lse, zb, sum, base)));
+                             at.stream, 0, r, logp, lse, zb, sum, top)));
 }
 
 template <typename T>
-int preference_t(const TrainScratch& s, const adacgd_preference_args& a, int sms, cudaStream_t st) {
+int preference_t(const TrainScratch& s, const adacgd_preference_args& a, const Where& at) {
   int n = 1;
   const long long rows = a.rows.tokens;
   if (rows) {
-    if (logp_t<T>(a.rows, nullptr, nullptr, s.tok_a, s.tok_b, s.tok_c, sms, st) != cudaSuccess) return -1;
+    if (logp_t<T>(a.rows, nullptr, nullptr, s.tok_a, s.tok_b, s.tok_c, at) != cudaSuccess) return -1;
     ++n;
   }
-  if (launch(k_pairs, (unsigned)(a.rows.sequences / 2), PAIR_NT, 1, rows > 0, st, a, s.tok_a, s.tok_b, s.seq, s.part, s.tickets) != cudaSuccess)
+  if (launch(k_pairs, (unsigned)(a.rows.sequences / 2), PAIR_NT, 1, rows > 0, at.stream, 0, a, s.tok_a, s.tok_b, s.seq, s.part,
+             s.tickets) != cudaSuccess)
     return -1;
   if (a.dlogits && rows) {
-    const long long v = a.rows.vocab;
-    cudaError_t e;
-    if (v <= 1024) {
-      e = launch(k_preference_grad<T, 32>, ctas(rows, 4, 1), 128, 1, true, st, a, s.seq, s.tok_c, s.tok_b, 1);
-    } else {
-      const int parts = (int)((v + 32767) / 32768);
-      e = v <= 8192 ? launch(k_preference_grad<T, 128>, (unsigned)rows, 128, 1, true, st, a, s.seq, s.tok_c, s.tok_b, 1)
-                    : launch(k_preference_grad<T, 512>, (unsigned)(rows * parts), 512, 1, true, st, a, s.seq, s.tok_c, s.tok_b, parts);
-    }
+    Split sp = split_of(rows, a.rows.vocab, at);
+    const u32 parts = (u32)sp.cluster;      // no reduction: parts of a row need no cluster
+    sp.cluster = 1;
+    const cudaError_t e = BY_SPLIT(sp, (launch(k_preference_grad<T, NTH>, ctas(rows * parts, Place<NTH, false>::ROWS, 1), Place<NTH, false>::CTA,
+                                               1, true, at.stream, 0, a, s.seq, s.tok_a, s.tok_b, s.tok_c, parts)));
     if (e != cudaSuccess) return -1;
     ++n;
   }
@@ -590,12 +672,15 @@ int preference_t(const TrainScratch& s, const adacgd_preference_args& a, int sms
 }
 
 template <typename T>
-int policy_t(const TrainScratch& s, const adacgd_policy_args& a, int sms, cudaStream_t st) {
-  if (launch(k_policy_weights, 1u, 1024, 1, false, st, a, s.seq) != cudaSuccess) return -1;
+int policy_t(const TrainScratch& s, const adacgd_policy_args& a, const Where& at) {
+  if (launch(k_policy_weights, 1u, 1024, 1, false, at.stream, 0, a, s.seq) != cudaSuccess) return -1;
   if (!a.rows.tokens) return 1;
-  const Split sp = split_of(a.rows.tokens, a.rows.vocab, sms);
-  const cudaError_t e = BY_SPLIT(sp, (launch(k_policy<T, NTH, CL>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, sp.cluster), Place<NTH, CL>::CTA,
-                                             sp.cluster, true, st, a, s.seq, s.tok_a, s.tok_b, s.tok_c, s.tickets + 1)));
+  const Split sp = split_of(a.rows.tokens, a.rows.vocab, at);
+  const unsigned grid = ctas(a.rows.tokens, sp.threads == 32 ? 4 : 1, sp.cluster);
+  u32 group = 256;
+  while (grid / group >= MAX_GROUPS) group *= 2;
+  const cudaError_t e = BY_SPLIT(sp, (launch(k_policy<T, NTH, CL>, grid, Place<NTH, CL>::CTA, sp.cluster, true, at.stream, 0, a, s.seq, s.tok_a,
+                                             s.tok_b, s.tok_c, s.own, s.tickets + 1, group)));
   return e == cudaSuccess ? 2 : -1;
 }
 
@@ -608,14 +693,12 @@ int policy_t(const TrainScratch& s, const adacgd_policy_args& a, int sms, cudaSt
     default: { typedef __nv_bfloat16 T; return call; }         \
   }
 
-int launch_token_logp(const adacgd_token_rows& r, float* logp, float* lse, int sms, cudaStream_t st) {
-  BY_TYPE(r.dtype, (logp_t<T>(r, logp, lse, nullptr, nullptr, nullptr, sms, st) == cudaSuccess ? 1 : -1))
+int launch_token_logp(const adacgd_token_rows& r, float* logp, float* lse, const Where& at) {
+  BY_TYPE(r.dtype, (logp_t<T>(r, logp, lse, nullptr, nullptr, nullptr, at) == cudaSuccess ? 1 : -1))
 }
-int launch_preference(const TrainScratch& s, const adacgd_preference_args& a, int sms, cudaStream_t st) {
-  BY_TYPE(a.rows.dtype, (preference_t<T>(s, a, sms, st)))
+int launch_preference(const TrainScratch& s, const adacgd_preference_args& a, const Where& at) {
+  BY_TYPE(a.rows.dtype, (preference_t<T>(s, a, at)))
 }
-int launch_policy(const TrainScratch& s, const adacgd_policy_args& a, int sms, cudaStream_t st) {
-  BY_TYPE(a.rows.dtype, (policy_t<T>(s, a, sms, st)))
-}
+int launch_policy(const TrainScratch& s, const adacgd_policy_args& a, const Where& at) { BY_TYPE(a.rows.dtype, (policy_t<T>(s, a, at))) }
 
 }  // namespace adacgd

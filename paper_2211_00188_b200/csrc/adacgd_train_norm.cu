@@ -564,14 +564,15 @@ int norm_t(const adacgd_norm_args& a, int sms, cudaStream_t st) {
 }
 
 template <typename T, typename P, int NTH, int E, bool VEC, bool CLUSTER>
-int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, int cluster, int sms, cudaStream_t st) {
+int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, int cluster, const Where& at_, cudaStream_t st) {
   constexpr int R = Shape<NTH>::ROWS, CTA = Shape<NTH>::CTA;
   auto kern = k_norm_bwd<T, P, NTH, E, VEC, CLUSTER>;
   const int span = CLUSTER ? ((int)a.cols + cluster - 1) / cluster + 8 : (int)a.cols;
   const int smem = VEC || a.drop.p == 0.0 ? 0 : R * bits_of(span);
-  int per_sm = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, CTA, smem) != cudaSuccess || per_sm < 1) return -1;
-  long long groups = (long long)sms * per_sm / cluster;
+  static std::atomic<int> table[TRAIN_DEVICES];
+  const int per_sm = resident_ctas(kern, table, at_.device, CTA, VEC ? 0 : R * bits_of(NTH * E));
+  if (per_sm < 1) return -1;
+  long long groups = (long long)at_.sms * per_sm / cluster;
   if (groups > NORM_PARTS) groups = NORM_PARTS;
   if (groups > (a.rows + R - 1) / R) groups = (a.rows + R - 1) / R;
   const bool grads = a.dweight || a.dbias;
@@ -595,7 +596,7 @@ int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, i
 }
 
 template <typename T, typename P, bool VEC>
-int norm_bwd_by_width(const TrainScratch& s, const adacgd_norm_backward_args& a, int sms, cudaStream_t st) {
+int norm_bwd_by_width(const TrainScratch& s, const adacgd_norm_backward_args& a, const Where& sms, cudaStream_t st) {
   const long long c = a.cols;
   if (c <= 256) return norm_bwd_launch<T, P, 32, 8, VEC, false>(s, a, 1, sms, st);
   if (c <= 1024) return norm_bwd_launch<T, P, 128, 8, VEC, false>(s, a, 1, sms, st);
@@ -606,7 +607,7 @@ int norm_bwd_by_width(const TrainScratch& s, const adacgd_norm_backward_args& a,
 }
 
 template <typename T, typename P>
-int norm_bwd_t(const TrainScratch& s, const adacgd_norm_backward_args& a, int sms, cudaStream_t st) {
+int norm_bwd_t(const TrainScratch& s, const adacgd_norm_backward_args& a, const Where& sms, cudaStream_t st) {
   const bool vec = a.cols % 8 == 0 && run_aligned<T>(a.dout, a.dout_stride, a.rows) && run_aligned<T>(a.s, a.s_stride, a.rows) &&
                    run_aligned<T>(a.dsum, a.dsum_stride, a.rows) && run_aligned<T>(a.dx, a.dx_stride, a.rows) &&
                    run_aligned<T>(a.dresidual, a.dresidual_stride, a.rows) && aligned16(a.weight);
@@ -622,16 +623,16 @@ int norm_bwd_t(const TrainScratch& s, const adacgd_norm_backward_args& a, int sm
     default: { typedef __nv_bfloat16 T; return call; }         \
   }
 
-int launch_dropout(const adacgd_dropout_args& a, int sms, cudaStream_t st) { BY_TYPE(a.dtype, (dropout_t<T>(a, st))) }
+int launch_dropout(const adacgd_dropout_args& a, const Where& at) { BY_TYPE(a.dtype, (dropout_t<T>(a, at.stream))) }
 
-int launch_layer_norm(const adacgd_norm_args& a, int sms, cudaStream_t st) {
-  if (a.param_dtype == ADACGD_F32) BY_TYPE(a.dtype, (norm_t<T, float>(a, sms, st)))
-  BY_TYPE(a.dtype, (norm_t<T, T>(a, sms, st)))
+int launch_layer_norm(const adacgd_norm_args& a, const Where& at) {
+  if (a.param_dtype == ADACGD_F32) BY_TYPE(a.dtype, (norm_t<T, float>(a, at.sms, at.stream)))
+  BY_TYPE(a.dtype, (norm_t<T, T>(a, at.sms, at.stream)))
 }
 
-int launch_layer_norm_backward(const TrainScratch& s, const adacgd_norm_backward_args& a, int sms, cudaStream_t st) {
-  if (a.param_dtype == ADACGD_F32) BY_TYPE(a.dtype, (norm_bwd_t<T, float>(s, a, sms, st)))
-  BY_TYPE(a.dtype, (norm_bwd_t<T, T>(s, a, sms, st)))
+int launch_layer_norm_backward(const TrainScratch& s, const adacgd_norm_backward_args& a, const Where& at) {
+  if (a.param_dtype == ADACGD_F32) BY_TYPE(a.dtype, (norm_bwd_t<T, float>(s, a, at, at.stream)))
+  BY_TYPE(a.dtype, (norm_bwd_t<T, T>(s, a, at, at.stream)))
 }
 
 }  // namespace adacgd
