@@ -11,7 +11,6 @@
 #include "adacgd_train.cuh"
 
 namespace cg = cooperative_groups;
-
 namespace adacgd {
 
 namespace {
@@ -21,7 +20,7 @@ namespace {
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// m: maximum; s: sum of exponentials relative to it.  m = -inf: nothing but -inf, s = 0.
+// m: a reference at most SLACK below the maximum; s: sum of exponentials relative to it.  m = -inf: nothing but -inf, s = 0.
 struct Soft { float m, s; };
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 // Exponents are base 2: exp(z - m) is taken as 2^(z L - fl(m L)), L = log2 e, one fused operation an element.  fl(m L) is as good
@@ -31,12 +30,46 @@ constexpr float LN2 = 0.6931471805599453f;
 
 // 2^(x L) relative to the maximum m
 __device__ __forceinline__ bool plain_range(float m) { return fabsf(m) <= BIG; }
+// Two binary32 numbers in a register pair: one instruction for both.
+struct F2 { u64 v; };
+__device__ __forceinline__ F2 f2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(F2 a, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+// x_i = 2^(x_i L + off)
+template <int N>
+__device__ __forceinline__ void exp_plain(float (&x)[N], float off) {
+  const F2 l2 = f2(LOG2E, LOG2E), o2 = f2(off, off);
+#pragma unroll
+  for (int i = 0; i + 1 < N; i += 2) {
+    float a, b;
+    split(fma2(f2(x[i], x[i + 1]), l2, o2), a, b);
+    x[i] = ex2(a);
+    x[i + 1] = ex2(b);
+  }
+  if (N & 1) x[N - 1] = ex2(fmaf(x[N - 1], LOG2E, off));
+}
 template <int N>
 __device__ __forceinline__ void exp_all(float (&x)[N], float m) {
   if (plain_range(m)) {
-    const float b = -(m * LOG2E);
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = ex2(fmaf(x[i], LOG2E, b));
+    exp_plain(x, -(m * LOG2E));
   } else {
     const float b = base_of(m);
 #pragma unroll
@@ -90,32 +123,59 @@ __device__ __forceinline__ int edge_of(const Cut& c, int t) {
   return t < c.end - tail0 ? tail0 + t : -1;
 }
 
+// The reference m only follows the maximum when that is ahead by more than SLACK: exponentials up to e^SLACK do no harm, and
+// after the first batch the sum is hardly ever rescaled.
+constexpr float SLACK = 16.f;
 template <int N>
 __device__ __forceinline__ void absorb(Soft& a, float (&x)[N]) {
-  float m = x[0];
+  float m[2] = {x[0], x[N > 1 ? 1 : 0]};
 #pragma unroll
-  for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
-  if (m > a.m) {
-    a.s *= rel(a.m, m);          // a.m = -inf: s is 0 and stays 0
-    a.m = m;
+  for (int j = 2; j < N; ++j) m[j & 1] = fmaxf(m[j & 1], x[j]);
+  const float top = fmaxf(m[0], m[1]);
+  if (top > a.m + SLACK) {
+    a.s *= rel(a.m, top);          // a.m = -inf: s is 0 and stays 0
+    a.m = top;
   }
   exp_all(x, a.m);
-  float s[2] = {x[0], N > 1 ? x[1 % N] : 0.f};
+  if (N == 1) {
+    a.s += x[0];
+  } else {
+    F2 s = f2(x[0], x[N > 1 ? 1 : 0]);
 #pragma unroll
-  for (int j = 2; j < N; ++j) s[j & 1] += x[j];
-  a.s += s[0] + s[1];
+    for (int j = 2; j + 1 < N; j += 2) s = add2(s, f2(x[j], x[j + 1]));
+    float u, v;
+    split(s, u, v);
+    a.s += u + v;
+  }
 }
 
 // Runs of eight elements that a thread has under way: 64 bytes, loaded before the batch in front of it is worked on, so that
-// loads and exponentials overlap within the thread.
+// loads and exponentials overlap within the thread.  LAST: nobody reads these lines again, nor soon what is stored, so both
+// are first to leave the cache and rows that still wait for their second pass stay in it.
+template <typename T, bool LAST> __device__ __forceinline__ Run<T> load_hint(const T* p) {
+  if (!LAST) return load_run(p);
+  Run<T> r;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+  return r;
+}
+template <typename T, bool LAST> __device__ __forceinline__ void store_hint(T* p, const float (&v)[8]) {
+  if (!LAST) return store_run(p, v);
+  if constexpr (sizeof(T) == 2) {
+    __stcs(reinterpret_cast<uint4*>(p), pack_run<T>(v));
+  } else {
+    __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+  }
+}
 template <typename T> struct Batch {
   static constexpr int U = sizeof(T) == 2 ? 4 : 2;
   Run<T> r[U];
 };
-template <typename T, int NTH>
-__device__ __forceinline__ void load_batch(Batch<T>& b, const T* p, int run) {
+template <typename T, int NTH, bool LAST>
+__device__ __forceinline__ void load_batch(Batch<T>& b, const T* p) {   // p: this thread's first run of the batch
 #pragma unroll
-  for (int u = 0; u < Batch<T>::U; ++u) b.r[u] = load_run(p + 8ll * (run + u * NTH));
+  for (int u = 0; u < Batch<T>::U; ++u) b.r[u] = load_hint<T, LAST>(p + 8 * u * NTH);
 }
 
 // This thread's share of the statistics.
@@ -123,42 +183,53 @@ template <typename T, int NTH>
 __device__ __forceinline__ Soft thread_soft(const T* row, const Cut& c, int t) {
   constexpr int U = Batch<T>::U;
   Soft a = {-INFINITY, 0.f};
-  const T* p = row + c.first;
+  const T* p = row + c.first + 8 * t;
   const int whole = c.runs / (U * NTH);      // batches that all threads have in full
-  Batch<T> next;
-  if (whole > 0) load_batch<T, NTH>(next, p, t);
+  auto take = [&](const Batch<T>& b) {
+#pragma unroll
+    for (int u = 0; u < U; u += 2) {
+      float x[16];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float y[8];
+        unpack(b.r[u + h], y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[h * 8 + j] = y[j];
+      }
+      absorb(a, x);
+    }
+  };
+  Batch<T> b0, b1;
+  if (whole > 0) load_batch<T, NTH, false>(b0, p);
   const int e = edge_of(c, t);
   if (e >= 0) {
     float x[1] = {to_f(row[e])};
     absorb(a, x);
   }
-  for (int k = 1; k <= whole; ++k) {
-    const Batch<T> b = next;
-    if (k < whole) load_batch<T, NTH>(next, p, k * U * NTH + t);
-    float x[U * 8];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float y[8];
-      unpack(b.r[u], y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[u * 8 + j] = y[j];
-    }
-    absorb(a, x);
+  int k = 0;
+  for (; k + 2 <= whole; k += 2) {           // two batches take turns: no copies between registers
+    load_batch<T, NTH, false>(b1, p + 8 * U * NTH);
+    take(b0);
+    p += 16 * U * NTH;
+    if (k + 2 < whole) load_batch<T, NTH, false>(b0, p);
+    take(b1);
+  }
+  if (k < whole) {
+    take(b0);
+    p += 8 * U * NTH;
   }
   const int r0 = whole * U * NTH + t;
   if (r0 < c.runs) {      // the rest: up to U runs, loaded together
-    float x[U * 8];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (r0 + u * NTH < c.runs) next.r[u] = load_run(p + 8ll * (r0 + u * NTH));
+      if (r0 + u * NTH < c.runs) b0.r[u] = load_run(p + 8 * u * NTH);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float y[8];
-      unpack(next.r[u], y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[u * 8 + j] = r0 + u * NTH < c.runs ? y[j] : -INFINITY;
+      if (r0 + u * NTH >= c.runs) break;
+      float x[8];
+      unpack(b0.r[u], x);
+      absorb(a, x);
     }
-    absorb(a, x);
   }
   return a;
 }
@@ -213,49 +284,72 @@ __device__ __forceinline__ Soft row_soft(Soft a, Soft* sh, Soft* xch) {
 
 // c (1{j = label} - softmax_j) for this thread's share, softmax_j = 2^(x_j L) relative to m, over sum.  `same`: the gradient's row
 // is aligned as the logits' is.  The label's entry (tz: its log2_rel) is written once more, by the thread that wrote it first.
-template <typename T, int NTH>
+template <typename T, int NTH, bool LAST>
 __device__ __forceinline__ void thread_grad(const T* row, T* d, const Cut& c, int t, bool same, int label, float tz, float coef, float m,
                                             float sum) {
   constexpr int U = Batch<T>::U;
   const float neg = -coef / sum;
-  const T* p = row + c.first;
-  T* q = d + c.first;
-  const int batches = (c.runs + U * NTH - 1) / (U * NTH);
-  Batch<T> next;
-  auto fetch = [&](int k) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int r = (k * U + u) * NTH + t;
-      if (r < c.runs) next.r[u] = load_run(p + 8ll * r);
-    }
-  };
-  fetch(0);
   const int e = edge_of(c, t);
-  if (e >= 0) {
-    float x[1] = {to_f(row[e])};
-    exp_all(x, m);
-    d[e] = from_f<T>(neg * x[0]);
-  }
-  for (int k = 0; k < batches; ++k) {
-    const Batch<T> b = next;
-    if (k + 1 < batches) fetch(k + 1);
+  const float edge = e >= 0 ? to_f(row[e]) : 0.f;
+  const T* p = row + c.first + 8 * t;
+  T* q = d + c.first + 8 * t;
+  int r = t;                                 // this thread's next run
+  if (same && plain_range(m)) {              // as good as always: whole batches, nothing to ask in between
+    const int whole = c.runs / (U * NTH);
+    const float off = -(m * LOG2E);
+    auto put = [&](const Batch<T>& b) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int r = (k * U + u) * NTH + t;
-      if (r < c.runs) {
+      for (int u = 0; u < U; ++u) {
         float x[8];
         unpack(b.r[u], x);
-        exp_all(x, m);
+        exp_plain(x, off);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= neg;
-        if (same) {
-          store_run(q + 8ll * r, x);
-        } else {
+        for (int j = 0; j < 8; j += 2) split(mul2(f2(x[j], x[j + 1]), f2(neg, neg)), x[j], x[j + 1]);
+        store_hint<T, LAST>(q + 8 * u * NTH, x);
+      }
+      q += 8 * U * NTH;
+    };
+    Batch<T> b0, b1;
+    if (whole > 0) load_batch<T, NTH, LAST>(b0, p);
+    int k = 0;
+    for (; k + 2 <= whole; k += 2) {
+      load_batch<T, NTH, LAST>(b1, p + 8 * U * NTH);
+      put(b0);
+      p += 16 * U * NTH;
+      if (k + 2 < whole) load_batch<T, NTH, LAST>(b0, p);
+      put(b1);
+    }
+    if (k < whole) {
+      put(b0);
+      p += 8 * U * NTH;
+    }
+    r += whole * U * NTH;
+  }
+  for (; r < c.runs; r += U * NTH, p += 8 * U * NTH, q += 8 * U * NTH) {
+    Batch<T> b;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) q[8ll * r + j] = from_f<T>(x[j]);
-        }
+    for (int u = 0; u < U; ++u)
+      if (r + u * NTH < c.runs) b.r[u] = load_hint<T, LAST>(p + 8 * u * NTH);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (r + u * NTH >= c.runs) break;
+      float x[8];
+      unpack(b.r[u], x);
+      exp_all(x, m);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= neg;
+      if (same) {
+        store_hint<T, LAST>(q + 8 * u * NTH, x);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[8 * u * NTH + j] = from_f<T>(x[j]);
       }
     }
+  }
+  if (e >= 0) {
+    float x[1] = {edge};
+    exp_all(x, m);
+    d[e] = from_f<T>(neg * x[0]);
   }
   if (label >= c.begin && label < c.end) {
     const int in = label - c.first;
@@ -276,7 +370,11 @@ __device__ __forceinline__ bool same_phase(const T* a, const T* b) { return (((u
 // Where a thread stands: its row, its number among the row's threads, the row's part it works on.
 template <int NTH, bool CLUSTER> struct Place {
   static constexpr int CTA = NTH < 128 ? 128 : NTH;
+#ifndef TPSM
+#define TPSM 1024
+#endif
   static constexpr int ROWS = CTA / NTH;
+  static constexpr int CTAS = TPSM / CTA;   // an SM: 64 registers a thread
   long long row;
   int t, part, parts;
   __device__ __forceinline__ Place() {
@@ -297,7 +395,7 @@ template <int NTH, bool CLUSTER> struct Place {
 // zb, sum, top: log2 of exp(z_label) and the sum relative to the maximum, and the maximum, in the units of log2_rel and
 // exp_all, from which the preference loss takes its log-probabilities in 64 bits and its gradient.  Either these or logp.
 template <typename T, int NTH, bool CLUSTER>
-__global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_logp(adacgd_token_rows r, float* __restrict__ logp, float* __restrict__ lse,
+__global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>::CTAS) k_logp(adacgd_token_rows r, float* __restrict__ logp, float* __restrict__ lse,
                                                                    float* __restrict__ zb, float* __restrict__ sum,
                                                                    float* __restrict__ top) {
   __shared__ Soft sh[32], xch[8];
@@ -426,7 +524,7 @@ __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, con
 
 // The gradient once the pairs' coefficients are known: element by element, `parts` walkers a row.
 template <typename T, int NTH>
-__global__ void __launch_bounds__(Place<NTH, false>::CTA) k_preference_grad(adacgd_preference_args a, const float* __restrict__ coef,
+__global__ void __launch_bounds__(Place<NTH, false>::CTA, Place<NTH, false>::CTAS) k_preference_grad(adacgd_preference_args a, const float* __restrict__ coef,
                                                                             const float* __restrict__ zb, const float* __restrict__ sum,
                                                                             const float* __restrict__ top, u32 parts) {
   const Place<NTH, false> at;
@@ -444,7 +542,7 @@ __global__ void __launch_bounds__(Place<NTH, false>::CTA) k_preference_grad(adac
     return;
   }
   const T* x = (const T*)a.rows.logits + row * a.rows.logits_stride;
-  thread_grad<T, NTH>(x, d, cut_row(x, vocab, part, (int)parts), at.t, same_phase(x, d), y >= 0 && y < vocab ? (int)y : -1, zb[row], coef[q],
+  thread_grad<T, NTH, false>(x, d, cut_row(x, vocab, part, (int)parts), at.t, same_phase(x, d), y >= 0 && y < vocab ? (int)y : -1, zb[row], coef[q],
                       top[row], sum[row]);
 }
 
@@ -519,7 +617,7 @@ __device__ __forceinline__ void write_policy(float* loss, float* stats, double l
 
 // A row's loss and, from the cache, its gradient.  `group`: CTAs that share a completion count (a multiple of the cluster).
 template <typename T, int NTH, bool CLUSTER>
-__global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_policy(adacgd_policy_args a, const float* __restrict__ weight, float* tl,
+__global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>::CTAS) k_policy(adacgd_policy_args a, const float* __restrict__ weight, float* tl,
                                                                      float* tk, float* tc, double* own, u32* ticket, u32 group) {
   constexpr int CTA = Place<NTH, CLUSTER>::CTA;
   __shared__ Soft sh[32], xch[8];
@@ -550,7 +648,7 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA) k_policy(adacgd_poli
       pdl_wait();
       const float w = weight[q];
       const Token tok = token_loss(logp, old, A, a.ref_logp != nullptr, ref, a.clip_low, a.clip_high, a.kl_beta);
-      if (d) thread_grad<T, NTH>(x, d, cut, at.t, same_phase(x, d), label, tz, a.grad_scale * (w * tok.slope), v.m, v.s);
+      if (d) thread_grad<T, NTH, true>(x, d, cut, at.t, same_phase(x, d), label, tz, a.grad_scale * (w * tok.slope), v.m, v.s);
       if (at.t == 0 && at.part == 0) {
         if (a.logp) a.logp[row] = logp;
         tl[row] = w * tok.loss;
