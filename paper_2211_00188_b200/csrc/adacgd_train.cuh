@@ -23,13 +23,11 @@ struct TrainScratch {
   float* tok_b;    // [tokens] its KL estimate
   float* tok_c;    // [tokens] 1 where the clipped term has taken the gradient
   float* seq;      // [tokens + 1] per sequence: weight or gradient coefficient; the last is the total
-  double* part;    // [tokens] per pair: loss
-  double* own;     // [3][MAX_GROUPS] sums of groups of the policy loss kernel's CTAs
+  double* part;    // [tokens + 3] per pair: loss; per CTA of the token sums: three of them
   float* norm_part; // [NORM_PARTS][2][max_cols] partial weight and bias gradients
   long long max_tokens, max_cols;
 };
-constexpr int NTRAIN_TICKETS = 1024;
-constexpr int MAX_GROUPS = NTRAIN_TICKETS - 2;
+constexpr int NTRAIN_TICKETS = 64;
 
 // Where a call runs.
 struct Where {

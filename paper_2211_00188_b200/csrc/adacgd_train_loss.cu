@@ -262,7 +262,7 @@ __device__ __forceinline__ Soft row_soft(Soft a, Soft* sh, Soft* xch) {
   const int lane = threadIdx.x & 31;
   float f = lane < NTH / 32 ? sh[lane].s * rel(sh[lane].m, m) : 0.f;
 #pragma unroll
-  for (int o = NTH / 64; o > 0; o >>= 1) f += __shfl_xor_sync(0xffffffffu, f, o);
+  for (int o = 16; o > 0; o >>= 1) f += __shfl_xor_sync(0xffffffffu, f, o);
   s = __shfl_sync(0xffffffffu, f, 0);
   a.m = m;
   a.s = s;
@@ -370,11 +370,8 @@ __device__ __forceinline__ bool same_phase(const T* a, const T* b) { return (((u
 // Where a thread stands: its row, its number among the row's threads, the row's part it works on.
 template <int NTH, bool CLUSTER> struct Place {
   static constexpr int CTA = NTH < 128 ? 128 : NTH;
-#ifndef TPSM
-#define TPSM 1024
-#endif
   static constexpr int ROWS = CTA / NTH;
-  static constexpr int CTAS = TPSM / CTA;   // an SM: 64 registers a thread
+  static constexpr int CTAS = 1024 / CTA;   // an SM: 64 registers a thread
   long long row;
   int t, part, parts;
   __device__ __forceinline__ Place() {
@@ -403,7 +400,11 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
   const Place<NTH, CLUSTER> at;
   const long long row = at.row;
   if (row >= r.tokens) return;       // whole warps; only where NTH == 32
-  if (r.mask && !r.mask[row]) {      // the same in the whole cluster
+  const bool counts = !r.mask || r.mask[row];      // fetched together with the label, not one after the other
+  const long long y = label_at(r, row);
+  const int vocab = (int)r.vocab;
+  const T* x = (const T*)r.logits + row * r.logits_stride;
+  if (!counts) {                     // the same in the whole cluster
     if (at.t == 0 && at.part == 0) {
       if (logp) logp[row] = 0.f;
       if (lse) lse[row] = 0.f;
@@ -411,13 +412,7 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
     return;
   }
   row_begin<CLUSTER>();
-  const T* x = (const T*)r.logits + row * r.logits_stride;
-  const int vocab = (int)r.vocab;
-  float z = 0.f;
-  if (at.t == 0) {
-    const long long y = label_at(r, row);
-    z = y >= 0 && y < vocab ? to_f(x[y]) : NAN;
-  }
+  const float z = y >= 0 && y < vocab ? to_f(x[y]) : NAN;
   const Soft a = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut_row(x, vocab, at.part, at.parts), at.t), sh, xch);
   if (at.t == 0 && at.part == 0) {
     const float tz = log2_rel(z, a.m);
@@ -615,73 +610,77 @@ __device__ __forceinline__ void write_policy(float* loss, float* stats, double l
   }
 }
 
-// A row's loss and, from the cache, its gradient.  `group`: CTAs that share a completion count (a multiple of the cluster).
+// A row's loss and, from the cache, its gradient.
 template <typename T, int NTH, bool CLUSTER>
 __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>::CTAS) k_policy(adacgd_policy_args a, const float* __restrict__ weight, float* tl,
-                                                                     float* tk, float* tc, double* own, u32* ticket, u32 group) {
-  constexpr int CTA = Place<NTH, CLUSTER>::CTA;
+                                                                     float* tk, float* tc) {
   __shared__ Soft sh[32], xch[8];
-  __shared__ double shd[32];
+  pdl_trigger();
   const Place<NTH, CLUSTER> at;
   const long long row = at.row;
+  if (row >= a.rows.tokens) return;       // whole warps; only where NTH == 32
   const int vocab = (int)a.rows.vocab;
-  if (row < a.rows.tokens) {
-    T* d = a.dlogits ? (T*)a.dlogits + row * a.dlogits_stride : nullptr;
-    if (a.rows.mask && !a.rows.mask[row]) {
-      if (at.t == 0 && at.part == 0) {
-        tl[row] = tk[row] = tc[row] = 0.f;
-        if (a.logp) a.logp[row] = 0.f;
-      }
-      if (d) thread_zero<T, NTH>(d, cut_row(d, vocab, at.part, at.parts), at.t);
-      pdl_wait();
-    } else {
-      row_begin<CLUSTER>();
-      const T* x = (const T*)a.rows.logits + row * a.rows.logits_stride;
-      const long long y = label_at(a.rows, row);
-      const int label = y >= 0 && y < vocab ? (int)y : -1;
-      const float z = label >= 0 ? to_f(x[label]) : NAN;
-      const float A = a.advantages[row], old = a.old_logp[row], ref = a.ref_logp ? a.ref_logp[row] : 0.f;
-      const Cut cut = cut_row(x, vocab, at.part, at.parts);
-      const Soft v = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut, at.t), sh, xch);
-      const float tz = log2_rel(z, v.m), logp = (tz - log2f(v.s)) * LN2;
-      const long long q = seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences);
-      pdl_wait();
-      const float w = weight[q];
-      const Token tok = token_loss(logp, old, A, a.ref_logp != nullptr, ref, a.clip_low, a.clip_high, a.kl_beta);
-      if (d) thread_grad<T, NTH, true>(x, d, cut, at.t, same_phase(x, d), label, tz, a.grad_scale * (w * tok.slope), v.m, v.s);
-      if (at.t == 0 && at.part == 0) {
-        if (a.logp) a.logp[row] = logp;
-        tl[row] = w * tok.loss;
-        tk[row] = tok.kl;
-        tc[row] = tok.clipped ? 1.f : 0.f;
-      }
+  // fetched together, not one after the other
+  const bool counts = !a.rows.mask || a.rows.mask[row];
+  const long long y = label_at(a.rows, row);
+  const float A = a.advantages[row], old = a.old_logp[row], ref = a.ref_logp ? a.ref_logp[row] : 0.f;
+  T* d = a.dlogits ? (T*)a.dlogits + row * a.dlogits_stride : nullptr;
+  if (!counts) {
+    if (at.t == 0 && at.part == 0) {
+      tl[row] = tk[row] = tc[row] = 0.f;
+      if (a.logp) a.logp[row] = 0.f;
     }
-  } else {
+    if (d) thread_zero<T, NTH>(d, cut_row(d, vocab, at.part, at.parts), at.t);
     pdl_wait();
+    return;
   }
-  // Each group of CTAs is added up by its last one, the groups by the last group's, both in a fixed order.
-  constexpr int ROWS = Place<NTH, CLUSTER>::ROWS;
-  const u32 groups = (gridDim.x + group - 1) / group, g = blockIdx.x / group;
-  if (!last_to_arrive(ticket + 1 + g, min(group, (u32)gridDim.x - g * group))) return;
-  double v[3];
-  {
-    const long long lo = (long long)(g * group / at.parts) * ROWS;
-    const long long hi = min((long long)a.rows.tokens, (long long)(min((g + 1) * group, (u32)gridDim.x) / at.parts) * ROWS);
-    const float* src[3] = {tl, tk, tc};
+  row_begin<CLUSTER>();
+  const T* x = (const T*)a.rows.logits + row * a.rows.logits_stride;
+  const int label = y >= 0 && y < vocab ? (int)y : -1;
+  const float z = label >= 0 ? to_f(x[label]) : NAN;
+  const Cut cut = cut_row(x, vocab, at.part, at.parts);
+  const Soft v = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut, at.t), sh, xch);
+  const float tz = log2_rel(z, v.m), logp = (tz - log2f(v.s)) * LN2;
+  // the same weight for all, or the sequence's
+  const long long q = a.per_sequence ? seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences) : 0;
+  pdl_wait();
+  const float w = weight[q];
+  const Token tok = token_loss(logp, old, A, a.ref_logp != nullptr, ref, a.clip_low, a.clip_high, a.kl_beta);
+  if (at.t == 0 && at.part == 0) {
+    if (a.logp) a.logp[row] = logp;
+    tl[row] = w * tok.loss;
+    tk[row] = tok.kl;
+    tc[row] = tok.clipped ? 1.f : 0.f;
+  }
+  if (d) thread_grad<T, NTH, true>(x, d, cut, at.t, same_phase(x, d), label, tz, a.grad_scale * (w * tok.slope), v.m, v.s);
+}
+
+// The sums over tokens, in a fixed order: a CTA takes SUM_ROWS of them, the last one adds the CTAs'.
+constexpr int SUM_ROWS = 4096, SUM_NT = 512;
+__global__ void __launch_bounds__(SUM_NT) k_policy_sum(adacgd_policy_args a, const float* __restrict__ weight, const float* __restrict__ tl,
+                                                       const float* __restrict__ tk, const float* __restrict__ tc, double* own, u32* ticket) {
+  __shared__ double sh[SUM_NT / 32];
+  pdl_wait();
+  const long long lo = (long long)blockIdx.x * SUM_ROWS, hi = min((long long)a.rows.tokens, lo + SUM_ROWS);
+  double v[3] = {0.0, 0.0, 0.0};
+  for (long long t = lo + threadIdx.x; t < hi; t += SUM_NT) {
+    v[0] += (double)tl[t];
+    v[1] += (double)tk[t];
+    v[2] += (double)tc[t];
+  }
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    v[i] = block_sum_f64<SUM_NT>(v[i], sh);
+    if (threadIdx.x == 0) own[3ll * blockIdx.x + i] = v[i];
+  }
+  if (gridDim.x > 1) {
+    if (!last_to_arrive(ticket, gridDim.x)) return;
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       v[i] = 0.0;
-      for (long long t = lo + threadIdx.x; t < hi; t += CTA) v[i] += (double)__ldcg(&src[i][t]);
-      v[i] = block_sum_f64<CTA>(v[i], shd);
-      if (threadIdx.x == 0) own[i * MAX_GROUPS + g] = v[i];
+      for (u32 k = threadIdx.x; k < gridDim.x; k += SUM_NT) v[i] += __ldcg(&own[3ll * k + i]);
+      v[i] = block_sum_f64<SUM_NT>(v[i], sh);
     }
-  }
-  if (!last_to_arrive(ticket, groups)) return;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    v[i] = 0.0;
-    for (u32 k = threadIdx.x; k < groups; k += CTA) v[i] += __ldcg(&own[i * MAX_GROUPS + k]);
-    v[i] = block_sum_f64<CTA>(v[i], shd);
   }
   if (threadIdx.x == 0) write_policy(a.loss, a.stats, v[0], v[1], v[2], (double)weight[a.rows.sequences]);
 }
@@ -719,30 +718,46 @@ unsigned ctas(long long rows, int rows_per_cta, int cluster) {
   return (unsigned)((rows + rows_per_cta - 1) / rows_per_cta * cluster);
 }
 
-// Threads a row (32, 128 or 512) and CTAs a row (a cluster, only where rows would leave SMs idle).
-#ifndef V32
-#define V32 4096
-#define V128 65536
-#endif
+// Threads a row and CTAs a row (a cluster, only where rows would leave SMs idle).
 struct Split { int threads, cluster; };
-Split split_of(long long rows, long long vocab, const Where& at) {
-  Split s;
-  s.threads = vocab <= V32 ? 32 : (vocab <= V128 ? 128 : 512);
-  s.cluster = 1;
+Split split_of(long long rows, long long vocab, int threads, const Where& at) {
+  Split s = {threads, 1};
   while (s.threads < 512 && rows * s.threads < 1024ll * at.sms && vocab > 8 * s.threads) s.threads *= 4;
-  while (s.threads == 512 && s.cluster < 8 && rows * s.cluster * 2 <= 2 * at.sms && vocab / (s.cluster * 2) >= 4096) s.cluster *= 2;
+  if (s.threads >= 512)
+    while (s.cluster < 8 && rows * s.cluster * 2 <= 2 * at.sms && vocab / (s.cluster * 2) >= 4096) s.cluster *= 2;
+  if (s.threads > 512 && s.cluster > 1) s.threads = 512;
   return s;
 }
-#define BY_SPLIT(s, call)                                                                            \
-  (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())       \
-   : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }()) \
-   : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }()) \
+// One pass: a row's two reductions cost about what 128 elements a thread do, and many rows on an SM hide them.
+Split split_once(long long rows, long long vocab, const Where& at) {
+  return split_of(rows, vocab, vocab <= 8192 ? 32 : (vocab <= 65536 ? 128 : 512), at);
+}
+// Two passes, the second from the cache: what the resident threads hold between their passes (1024 an SM) has to stay in it beside
+// what is written, so a thread may have 400 bytes of a row, and 640 where more threads a row cost more than the cache gives.
+// Policy loss, bfloat16, us at 128 / 256 / 512 / 1024 threads a row: 8192 x 32000 213 / 196 / 239 / -; 8192 x 50001 371 / 316 / 339 /
+// 509; 4096 x 65536 255 / 269 / 208 / -; 4096 x 131072 - / - / 419 / 458; 2048 x 262145 - / - / 511 / 452.
+constexpr int PASS_BYTES = 400, PASS_BYTES_WIDE = 640;
+Split split_twice(long long rows, long long vocab, int size, const Where& at) {
+  const long long bytes = vocab * size;
+  return split_of(rows, vocab, bytes <= 32 * PASS_BYTES ? 32 : bytes <= 128 * PASS_BYTES ? 128 : bytes <= 256 * PASS_BYTES ? 256 : bytes <= 512 * PASS_BYTES_WIDE ? 512 : 1024, at);
+}
+#define BY_SPLIT(s, call)                                                                              \
+  (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())         \
+   : s.threads == 1024 ? ([&] { constexpr int NTH = 1024; constexpr bool CL = false; return call; }()) \
+   : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }())   \
+   : s.threads == 256 ? ([&] { constexpr int NTH = 256; constexpr bool CL = false; return call; }())   \
+   : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }())   \
+                      : ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }()))
+#define BY_SPLIT_ONCE(s, call)                                                                         \
+  (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())         \
+   : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }())   \
+   : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }())   \
                       : ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }()))
 
 template <typename T>
 cudaError_t logp_t(const adacgd_token_rows& r, float* logp, float* lse, float* zb, float* sum, float* top, const Where& at) {
-  const Split s = split_of(r.tokens, r.vocab, at);
-  return BY_SPLIT(s, (launch(k_logp<T, NTH, CL>, ctas(r.tokens, Place<NTH, CL>::ROWS, s.cluster), Place<NTH, CL>::CTA, s.cluster, false,
+  const Split s = split_once(r.tokens, r.vocab, at);
+  return BY_SPLIT_ONCE(s, (launch(k_logp<T, NTH, CL>, ctas(r.tokens, Place<NTH, CL>::ROWS, s.cluster), Place<NTH, CL>::CTA, s.cluster, false,
                              at.stream, 0, r, logp, lse, zb, sum, top)));
 }
 
@@ -758,10 +773,10 @@ int preference_t(const TrainScratch& s, const adacgd_preference_args& a, const W
              s.tickets) != cudaSuccess)
     return -1;
   if (a.dlogits && rows) {
-    Split sp = split_of(rows, a.rows.vocab, at);
+    Split sp = split_once(rows, a.rows.vocab, at);
     const u32 parts = (u32)sp.cluster;      // no reduction: parts of a row need no cluster
     sp.cluster = 1;
-    const cudaError_t e = BY_SPLIT(sp, (launch(k_preference_grad<T, NTH>, ctas(rows * parts, Place<NTH, false>::ROWS, 1), Place<NTH, false>::CTA,
+    const cudaError_t e = BY_SPLIT_ONCE(sp, (launch(k_preference_grad<T, NTH>, ctas(rows * parts, Place<NTH, false>::ROWS, 1), Place<NTH, false>::CTA,
                                                1, true, at.stream, 0, a, s.seq, s.tok_a, s.tok_b, s.tok_c, parts)));
     if (e != cudaSuccess) return -1;
     ++n;
@@ -773,13 +788,13 @@ template <typename T>
 int policy_t(const TrainScratch& s, const adacgd_policy_args& a, const Where& at) {
   if (launch(k_policy_weights, 1u, 1024, 1, false, at.stream, 0, a, s.seq) != cudaSuccess) return -1;
   if (!a.rows.tokens) return 1;
-  const Split sp = split_of(a.rows.tokens, a.rows.vocab, at);
-  const unsigned grid = ctas(a.rows.tokens, sp.threads == 32 ? 4 : 1, sp.cluster);
-  u32 group = 256;
-  while (grid / group >= MAX_GROUPS) group *= 2;
-  const cudaError_t e = BY_SPLIT(sp, (launch(k_policy<T, NTH, CL>, grid, Place<NTH, CL>::CTA, sp.cluster, true, at.stream, 0, a, s.seq, s.tok_a,
-                                             s.tok_b, s.tok_c, s.own, s.tickets + 1, group)));
-  return e == cudaSuccess ? 2 : -1;
+  const Split sp = split_twice(a.rows.tokens, a.rows.vocab, (int)sizeof(T), at);
+  cudaError_t e = BY_SPLIT(sp, (launch(k_policy<T, NTH, CL>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, sp.cluster), Place<NTH, CL>::CTA, sp.cluster,
+                                       true, at.stream, 0, a, s.seq, s.tok_a, s.tok_b, s.tok_c)));
+  if (e == cudaSuccess)
+    e = launch(k_policy_sum, (unsigned)((a.rows.tokens + SUM_ROWS - 1) / SUM_ROWS), SUM_NT, 1, true, at.stream, 0, a, s.seq, s.tok_a, s.tok_b,
+               s.tok_c, s.part, s.tickets + 1);
+  return e == cudaSuccess ? 3 : -1;
 }
 
 }  // namespace
