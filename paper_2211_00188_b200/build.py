@@ -1,16 +1,20 @@
-"""Builds libadacgd.so (sm_100a) in-tree with nvcc.  `python -m paper_2211_00188_b200.build`."""
+"""Builds libadacgd.so (sm_100a) in-tree with nvcc, and with the host compiler the Python binding of the training operators,
+_train_binding.so.  `python -m paper_2211_00188_b200.build`."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libadacgd.so")
+BINDING = os.path.join(PKG, "_train_binding.so")
+BINDING_SOURCE = "adacgd_train_binding.cpp"
 SOURCES = ["adacgd_api.cu", "adacgd_compress.cu", "adacgd_small.cu", "adacgd_noalloc.cu", "adacgd_gradient.cu",
            "adacgd_train.cu", "adacgd_train_norm.cu", "adacgd_train_loss.cu"]
 
@@ -23,9 +27,9 @@ def nvcc_path() -> str:
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     include = os.path.join(ROOT, "include")
     deps = [os.path.join(d, f) for d in (CSRC, include) for f in os.listdir(d)]
     return any(os.path.getmtime(p) > t for p in deps)
@@ -61,7 +65,27 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
         raise RuntimeError("linking libadacgd.so failed")
+    build_binding()
     return LIB
+
+
+def build_binding() -> str:
+    """The extension module that checks torch tensors and calls libadacgd.so (which it finds beside itself)."""
+    import torch
+
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc_path())))
+    include = [os.path.join(ROOT, "include"), sysconfig.get_paths()["include"], os.path.join(root, "include"),
+               os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd += [f"-I{d}" for d in include] + [os.path.join(CSRC, BINDING_SOURCE), "-o", BINDING, "-L" + os.path.join(root, "lib"),
+                                          "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda", "-L" + PKG, "-l:libadacgd.so",
+                                          "-Wl,-rpath,$ORIGIN"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+        raise RuntimeError(f"{cmd[0]} failed on {BINDING_SOURCE}")
+    return BINDING
 
 
 if __name__ == "__main__":
