@@ -127,6 +127,40 @@ template <typename T> __device__ __forceinline__ void store_run(T* p, const floa
   *reinterpret_cast<uint4*>(p) = pack_run<T>(v);
 }
 
+// ---- packed binary32 ----
+// Two binary32 numbers in a register pair: one instruction for both.
+struct F2 { u64 v; };
+__device__ __forceinline__ F2 f2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(F2 a, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+// Eight numbers as four pairs.
+__device__ __forceinline__ void pairs_of(const float (&x)[8], F2 (&o)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = f2(x[2 * i], x[2 * i + 1]);
+}
+__device__ __forceinline__ void floats_of(const F2 (&x)[4], float (&o)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) split(x[i], o[2 * i], o[2 * i + 1]);
+}
+
 // ---- dropout's random bits: Philox4x32-10 (Salmon et al., SC 2011) ----
 struct Drop {        // what the kernels need of adacgd_drop
   bool on;

@@ -115,104 +115,98 @@ __global__ void __launch_bounds__(DROP_NT, 5) k_dropout(const T* x, long long xs
 }
 
 // --------------------------------------------------------------------------
-// a row spread over NTH threads, E elements each
+// rows of runs
 // --------------------------------------------------------------------------
-template <int NTH> struct Shape {
-  static constexpr int CTA = NTH < 128 ? 128 : NTH;   // a row of one warp shares its CTA with three others
+// The fast form.  A run is eight elements whose number (row * cols + col) begins at a multiple of eight, which is also a block
+// of the dropout generator.  In matrices without gaps between rows, and in aligned ones whose width is a multiple of eight, a
+// run is 16-byte aligned in memory, whatever the width; only a row's first and last run may hold elements of its neighbours.
+// `ph` = how many the first run does.  Rows whose numbers differ by a multiple of PERIOD = 8 / gcd(cols, 8) have the same ph, so a
+// walker (NTH threads) that takes such rows only finds the same columns in the same registers for every one of them: weights
+// are loaded once, weight gradients summed in place.
+// A thread copies its runs of the next STAGES rows to shared memory (cp.async) and is the only one to read them back: no barrier,
+// and memory does not wait for a row's reductions.
+constexpr int MAX_PERIOD = 8;
+
+template <typename T, int NTH, int R, int ARRAYS> struct Walk {   // R: runs a thread
+  static constexpr int CTA = NTH <= 32 ? 128 : NTH;
   static constexpr int ROWS = CTA / NTH;
+  static constexpr int PIECES = sizeof(T) / 2;                    // 16-byte pieces of a run
+  static constexpr int STAGE = ARRAYS * R * PIECES * CTA * 16;    // bytes
+  static constexpr int FIT = 200 * 1024 / (STAGE * (512 / CTA));           // registers allow 512 threads on an SM
+  static constexpr int STAGES = FIT >= 4 ? 4 : 2 * STAGE <= 200 * 1024 ? 2 : 1;
+  static constexpr int SMEM = STAGES * STAGE;
 };
 
-template <int NTH, bool VEC>
-__device__ __forceinline__ int col_of(int e, int t) { return VEC ? ((e >> 3) * NTH + t) * 8 + (e & 7) : e * NTH + t; }
-
-// The row's elements in 32 bits; columns at or past `cols` are 0.
-template <typename T, int NTH, int E, bool VEC>
-__device__ __forceinline__ void load_row(const T* row, int cols, int t, float (&o)[E]) {
-  if (VEC) {
-#pragma unroll
-    for (int g = 0; g < E / 8; ++g) {
-      const int c = (g * NTH + t) * 8;
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.f;
-      if (c < cols) unpack(load_run(row + c), v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[g * 8 + j] = v[j];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = e * NTH + t;
-      o[e] = c < cols ? to_f(row[c]) : 0.f;
-    }
-  }
+struct Walker {
+  long long row, step;
+  int t, slot, ph;
+};
+// Which rows a thread's walker takes: those of one class modulo the period, evenly dealt among the class's walkers.
+template <int NTH>
+__device__ __forceinline__ Walker walker_of(int cols, int group, int groups) {
+  constexpr int CTA = NTH <= 32 ? 128 : NTH, ROWS = CTA / NTH;
+  const int period = MAX_PERIOD / (cols & 1 ? 1 : (cols & 2 ? 2 : (cols & 4 ? 4 : 8)));
+  Walker w;
+  w.t = threadIdx.x % NTH;
+  w.slot = threadIdx.x / NTH;
+  const long long id = (long long)group * ROWS + w.slot, all = (long long)groups * ROWS;   // all: a multiple of the period
+  w.row = id;
+  w.step = all;
+  w.ph = (int)((id % period) * cols & 7);
+  return w;
 }
 
-template <typename T, int NTH, int E, bool VEC>
-__device__ __forceinline__ void store_row(T* row, int cols, int t, const float (&v)[E]) {
-  if (VEC) {
-#pragma unroll
-    for (int g = 0; g < E / 8; ++g) {
-      const int c = (g * NTH + t) * 8;
-      float w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = v[g * 8 + j];
-      if (c < cols) store_run(row + c, w);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = e * NTH + t;
-      if (c < cols) row[c] = from_f<T>(v[e]);
-    }
-  }
+__device__ __forceinline__ void copy16(u32 to, const void* from, int bytes) {   // the rest of the 16 bytes becomes zero
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// v[e] = dropout of v[e], or with BASE base[e] + dropout of v[e]; i0 = number of the element in the row's first column.  bits: the row's share of shared
-// memory (one byte a block), filled by fill_bits before the last barrier.
-template <int NTH, int E, bool VEC, bool BASE>
-__device__ __forceinline__ void drop_row(float (&v)[E], const float (&base)[E], int cols, int t, u64 i0, const Drop& d,
-                                         const unsigned char* bits) {
-  if (VEC) {
+// Sends a thread's runs of one row of one array on their way.  `last`: the matrix ends `left` elements behind the row's first run.
+template <typename T, int NTH, int R, int CTA>
+__device__ __forceinline__ void send_runs(u32 to, const T* first, int runs, int t, bool last, int left) {
 #pragma unroll
-    for (int g = 0; g < E / 8; ++g) {
-      const int c = (g * NTH + t) * 8;
-      if (c < cols) {
-        const uint4 w = philox((i0 + c) >> 3, d);
+  for (int r = 0; r < R; ++r) {
+    const int g = r * NTH + t;
+    if (g < runs) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          v[g * 8 + j] = !kept(w, j, d) ? (BASE ? base[g * 8 + j] : 0.f)
-                                        : (BASE ? scaled(v[g * 8 + j], base[g * 8 + j], d) : v[g * 8 + j] * d.scale);
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const int at = 8 * g + i * (16 / (int)sizeof(T));
+        int bytes = 16;
+        if (last) bytes = max(0, min(16, (left - at) * (int)sizeof(T)));
+        if (bytes > 0) copy16(to + (r * (sizeof(T) / 2) + i) * CTA * 16, first + at, bytes);
       }
     }
-  } else {
-    const int ph = (int)(i0 & 7);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = e * NTH + t;
-      if (c < cols) v[e] = (bits[(c + ph) >> 3] >> ((c + ph) & 7)) & 1 ? (BASE ? scaled(v[e], base[e], d) : v[e] * d.scale) : (BASE ? base[e] : 0.f);
-    }
   }
 }
-template <int NTH>
-__device__ __forceinline__ void fill_bits(unsigned char* bits, int cols, int t, u64 i0, const Drop& d) {
-  const int nb = ((int)(i0 & 7) + cols + 7) >> 3;
-  for (int b = t; b < nb; b += NTH) bits[b] = (unsigned char)keep_bits((i0 >> 3) + b, d);
-}
-__host__ __device__ constexpr int bits_of(int cols) { return ((cols + 14) / 8 + 15) / 16 * 16; }
-
-template <int NTH>
-__device__ __forceinline__ void row_sync() {
-  if (NTH == 32) __syncwarp();
-  else __syncthreads();
-}
-
-// Sum over the row's threads, the same bits in each; `sh` must not be in use by an earlier sum.
-template <int NTH>
-__device__ __forceinline__ float row_sum(float v, float* sh) {
+template <typename T, int CTA>
+__device__ __forceinline__ void take_run(const uint4* from, int r, float (&o)[8]) {
+  Run<T> v;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if (NTH == 32) return v;
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) v.v[i] = from[(r * (sizeof(T) / 2) + i) * CTA];
+  unpack(v, o);
+}
+// Whether some of a run's elements belong to other rows.  Without EDGE (widths of whole runs) none do, and nothing is asked.
+template <bool EDGE>
+__device__ __forceinline__ bool ragged(int c, int cols) { return EDGE && (c < 0 || c + 8 > cols); }
+// Stores a run, or of one at a row's end what belongs to the row.  row: its first element, c: column of the run's first.
+template <bool EDGE, typename T>
+__device__ __forceinline__ void put_run(T* row, int c, int cols, const float (&v)[8]) {
+  if (!EDGE || (c >= 0 && c + 8 <= cols)) {
+    store_run(row + c, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c + j >= 0 && c + j < cols) row[c + j] = from_f<T>(v[j]);
+  }
+}
+
+// Sum over a walker's threads, the same bits in each; `sh` alternates.  NTH <= 32: within the warp.
+template <int NTH>
+__device__ __forceinline__ float walker_sum(float v, float* sh) {
+#pragma unroll
+  for (int o = (NTH < 32 ? NTH : 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (NTH <= 32) return v;
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
   __syncthreads();
   float t = 0.f;
@@ -221,59 +215,174 @@ __device__ __forceinline__ float row_sum(float v, float* sh) {
   return t;
 }
 
+// Eight weights from column c on, `other` outside the row.
+template <typename P>
+__device__ __forceinline__ void load_weights(const P* w, int c, int cols, float other, float (&o)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) o[j] = w && c + j >= 0 && c + j < cols ? to_f(w[c + j]) : other;
+}
+// Kept in the parameter's own type: half the registers.
+template <typename P> struct Held {
+  uint4 v;
+  __device__ __forceinline__ void set(const float (&x)[8]) { v = pack_run<P>(x); }   // exact: x came from P
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    Run<P> r;
+    r.v[0] = v;
+    unpack(r, x);
+  }
+};
+template <> struct Held<float> {
+  float v[8];
+  __device__ __forceinline__ void set(const float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = x[j];
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = v[j];
+  }
+};
+
 // --------------------------------------------------------------------------
 // layer norm
 // --------------------------------------------------------------------------
-// The mean first, then the squares about it: two sums over registers, no cancellation.
-template <typename T, typename P, int NTH, int E, bool VEC>
-__global__ void __launch_bounds__(Shape<NTH>::CTA) k_norm(adacgd_norm_args a, Drop d) {
-  __shared__ float sh[2][32];
-  extern __shared__ unsigned char dyn[];
-  const int t = NTH == 32 ? (int)(threadIdx.x & 31) : (int)threadIdx.x;
-  const long long row = (long long)blockIdx.x * Shape<NTH>::ROWS + (NTH == 32 ? threadIdx.x >> 5 : 0);
-  if (row >= a.rows) return;               // whole warps, and only where NTH == 32: no barrier follows then
-  const int cols = (int)a.cols;
+// A walker takes one row, CTAs are handed out by the hardware: the row's two sums and the loads of other rows on the SM hide each
+// other.  The mean first, then the squares about it, over registers: no cancellation.
+template <int NTH> struct Group {
+  static constexpr int CTA = NTH <= 32 ? 128 : NTH;
+  static constexpr int ROWS = CTA / NTH;
+};
+template <typename T, typename P, int NTH, int R, bool EDGE>
+__global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant__ adacgd_norm_args a, const __grid_constant__ Drop d) {
+  __shared__ float sh[2][NTH < 32 ? 1 : NTH / 32];
+  const int cols = (int)a.cols, t = threadIdx.x % NTH;
+  const long long row = (long long)blockIdx.x * Group<NTH>::ROWS + threadIdx.x / NTH;
+  if (NTH >= 32 && row >= a.rows) return;          // whole warps; no barrier follows where a CTA has several rows
+  const bool live = row < a.rows;
   const u64 i0 = (u64)row * (u64)cols;
-  unsigned char* bits = dyn + (NTH == 32 ? (threadIdx.x >> 5) * bits_of(cols) : 0);
-  float v[E], base[E];
-  load_row<T, NTH, E, VEC>((const T*)a.x + row * a.x_stride, cols, t, v);
+  const int ph = EDGE ? (int)(i0 & 7) : 0, runs = live ? (ph + cols + 7) >> 3 : 0;
+  const T* const x = (const T*)a.x + row * a.x_stride - ph;
+  const T* const res = a.residual ? (const T*)a.residual + row * a.residual_stride - ph : nullptr;
+  // a matrix's last run may reach past its end: its own row's elements are read one by one then
+  const bool tail = EDGE && (row == a.rows - 1) && ((ph + cols) & 7);
+  Run<T> raw[R], rest[R];
 #pragma unroll
-  for (int e = 0; e < E; ++e) base[e] = 0.f;
-  if (a.residual) load_row<T, NTH, E, VEC>((const T*)a.residual + row * a.residual_stride, cols, t, base);
-  if (d.on) {
-    if (!VEC) {
-      fill_bits<NTH>(bits, cols, t, i0, d);
-      row_sync<NTH>();
+  for (int r = 0; r < R; ++r) {
+    const int g = r * NTH + t;
+    if (g < runs && !(tail && g == runs - 1)) {
+      raw[r] = load_run(x + 8 * g);
+      if (res) rest[r] = load_run(res + 8 * g);
     }
-    if (a.residual) drop_row<NTH, E, VEC, true>(v, base, cols, t, i0, d, bits);
-    else drop_row<NTH, E, VEC, false>(v, base, cols, t, i0, d, bits);
-  } else if (a.residual) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = base[e] + v[e];
   }
-  float acc = 0.f;
+  uint4 bits[R];                                   // made while the loads are under way
+  if (d.on) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc += v[e];
-  const float mean = row_sum<NTH>(acc, sh[0]) / (float)cols;
-  acc = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (col_of<NTH, VEC>(e, t) < cols) acc = fmaf(v[e] - mean, v[e] - mean, acc);
-  const float rstd = 1.f / sqrtf(row_sum<NTH>(acc, sh[1]) / (float)cols + a.eps);
-  if (a.sum) store_row<T, NTH, E, VEC>((T*)a.sum + row * a.sum_stride, cols, t, v);
-#pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = (v[e] - mean) * rstd;
-  if (a.weight) {
-    load_row<P, NTH, E, VEC>((const P*)a.weight, cols, t, base);
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] *= base[e];
+    for (int r = 0; r < R; ++r) bits[r] = philox((i0 >> 3) + (u64)(r * NTH + t), d);
   }
-  if (a.bias) {
-    load_row<P, NTH, E, VEC>((const P*)a.bias, cols, t, base);
+  F2 v[R][4], acc = f2(0.f, 0.f);
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] += base[e];
+  for (int r = 0; r < R; ++r) {
+    const int g = r * NTH + t, c = g * 8 - ph;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[r][j] = f2(0.f, 0.f);
+    if (g < runs) {
+      float u[8], b[8];
+      if (tail && g == runs - 1) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          u[j] = c + j >= 0 && c + j < cols ? to_f(x[8 * g + j]) : 0.f;
+          b[j] = res && c + j >= 0 && c + j < cols ? to_f(res[8 * g + j]) : 0.f;
+        }
+      } else {
+        unpack(raw[r], u);
+        if (res) unpack(rest[r], b);
+      }
+      if (d.on) {
+        if (res) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) u[j] = kept(bits[r], j, d) ? scaled(u[j], b[j], d) : b[j];
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) u[j] = kept(bits[r], j, d) ? u[j] * d.scale : 0.f;
+        }
+      }
+      if (ragged<EDGE>(c, cols)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + j < 0 || c + j >= cols) u[j] = b[j] = 0.f;
+      }
+      pairs_of(u, v[r]);
+      if (res && !d.on) {
+        F2 b2[4];
+        pairs_of(b, b2);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[r][j] = add2(v[r][j], b2[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc = add2(acc, v[r][j]);
+    }
   }
-  store_row<T, NTH, E, VEC>((T*)a.out + row * a.out_stride, cols, t, v);
+  float lo, hi;
+  split(acc, lo, hi);
+  const float mean = walker_sum<NTH>(lo + hi, sh[0]) / (float)cols;
+  const F2 minus = f2(-mean, -mean);
+  acc = f2(0.f, 0.f);
+  float edge = 0.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int g = r * NTH + t, c = g * 8 - ph;
+    if (g < runs) {
+      if (ragged<EDGE>(c, cols)) {
+        float u[8];
+        floats_of(v[r], u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + j >= 0 && c + j < cols) edge = fmaf(u[j] - mean, u[j] - mean, edge);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const F2 z = add2(v[r][j], minus);
+          acc = fma2(z, z, acc);
+        }
+      }
+    }
+  }
+  split(acc, lo, hi);
+  const float rstd = 1.f / sqrtf(walker_sum<NTH>(lo + hi + edge, sh[1]) / (float)cols + a.eps);
+  if (!live) return;
+  T* const out = (T*)a.out + row * a.out_stride;
+  T* const sum = a.sum ? (T*)a.sum + row * a.sum_stride : nullptr;
+  const P* const weight = (const P*)a.weight;
+  const P* const bias = (const P*)a.bias;
+  const F2 scale = f2(rstd, rstd);
+  const bool even = ((((uintptr_t)weight | (uintptr_t)bias) & 15) == 0) && ph == 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int g = r * NTH + t, c = g * 8 - ph;
+    if (g < runs) {
+      float u[8], p[8], q[8];
+      if (sum) {
+        floats_of(v[r], u);
+        put_run<EDGE>(sum, c, cols, u);
+      }
+      if (even && !ragged<EDGE>(c, cols)) {
+        if (weight) unpack(load_run(weight + c), p);
+        if (bias) unpack(load_run(bias + c), q);
+      } else {
+        load_weights(weight, c, cols, 1.f, p);
+        load_weights(bias, c, cols, 0.f, q);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        F2 z = mul2(add2(v[r][j], minus), scale);
+        if (weight && bias) z = fma2(z, f2(p[2 * j], p[2 * j + 1]), f2(q[2 * j], q[2 * j + 1]));
+        else if (weight) z = mul2(z, f2(p[2 * j], p[2 * j + 1]));
+        else if (bias) z = add2(z, f2(q[2 * j], q[2 * j + 1]));
+        split(z, u[2 * j], u[2 * j + 1]);
+      }
+      put_run<EDGE>(out, c, cols, u);
+    }
+  }
   if (t == 0) {
     if (a.mean) a.mean[row] = mean;
     if (a.rstd) a.rstd[row] = rstd;
@@ -283,197 +392,368 @@ __global__ void __launch_bounds__(Shape<NTH>::CTA) k_norm(adacgd_norm_args a, Dr
 // --------------------------------------------------------------------------
 // layer norm, backward
 // --------------------------------------------------------------------------
-// What a thread has loaded of one row of one matrix.
-template <typename T, int E, bool VEC> struct Raw;
-template <typename T, int E> struct Raw<T, E, true> {
-  Run<T> r[E / 8];
-  template <int NTH> __device__ __forceinline__ void load(const T* row, int cols, int t) {
-#pragma unroll
-    for (int g = 0; g < E / 8; ++g) {
-      const int c = (g * NTH + t) * 8;
-      if (c < cols) r[g] = load_run(row + c);
-    }
-  }
-  __device__ __forceinline__ void get(int g, float (&o)[8]) const { unpack(r[g], o); }
-};
-template <typename T, int E> struct Raw<T, E, false> {
-  T r[E];
-  template <int NTH> __device__ __forceinline__ void load(const T* row, int cols, int t) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = e * NTH + t;
-      if (c < cols) r[e] = row[c];
-    }
-  }
-  __device__ __forceinline__ void get(int g, float (&o)[8]) const {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = to_f(r[g * 8 + j]);
-  }
-};
-
-// A CTA walks rows and keeps the weight gradients of its columns in registers: dout and s are read once for both results.
-// The next row's loads are issued as soon as the current row has been unpacked, so they are under way while the row's two
-// sums are formed and its gradient is written.  Rows wider than NTH * E are cut into as many column parts as the cluster
-// has CTAs; the two sums then meet in distributed shared memory.
-//   ds = rstd g + dsum - rstd mean(g) - h rstd mean(g h)
-template <typename T, typename P, int NTH, int E, bool VEC, bool CLUSTER>
-__global__ void __launch_bounds__(Shape<NTH>::CTA) k_norm_bwd(adacgd_norm_backward_args a, Drop d, float* __restrict__ part,
-                                                              long long max_cols) {
-  constexpr int CTA = Shape<NTH>::CTA, ROWS = Shape<NTH>::ROWS;
-  __shared__ float sh[2][2][32];
-  __shared__ float2 xch[2][8];
-  extern __shared__ unsigned char dyn[];
-  const int t = NTH == 32 ? (int)(threadIdx.x & 31) : (int)threadIdx.x;
-  const int warp = threadIdx.x >> 5;
+//   h = (s - mean) rstd,  g = dout weight,  ds = rstd (g - mean(g) - h mean(g h)) + dsum
+// dout and s are read once for all results: first for the two sums and the weight gradients, then, from shared memory, for ds.
+// Rows wider than NTH * R runs are cut into as many column parts as the cluster has CTAs; the two sums then meet in distributed
+// shared memory.
+// K rows go through the two phases together, so that their reductions share one barrier.
+template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE>
+__global__ void __launch_bounds__(Walk<T, NTH, R, 3>::CTA) k_norm_bwd(const __grid_constant__ adacgd_norm_backward_args a,
+                                                                      const __grid_constant__ Drop d, float* __restrict__ part,
+                                                                      long long max_cols) {
+  typedef Walk<T, NTH, R, 3> W;
+  constexpr int CTA = W::CTA, S = W::STAGES, A = R * W::PIECES * CTA, K = S >= 4 ? 2 : 1, WARPS = NTH < 32 ? 1 : NTH / 32;
+  extern __shared__ uint4 ring[];
+  __shared__ float sh[2][2 * K][WARPS];
+  __shared__ float xch[2][8][2 * K];
   int nparts = 1, rank = 0;
   if (CLUSTER) {
     nparts = (int)cg::this_cluster().num_blocks();
     rank = (int)cg::this_cluster().block_rank();
+    cg::this_cluster().sync();   // every CTA has started before any writes into another's shared memory
   }
-  if (CLUSTER) cg::this_cluster().sync();   // every CTA has started before any writes into another's shared memory
-  const int all = (int)a.cols;
-  const int span = CLUSTER ? ((all + nparts - 1) / nparts + 7) / 8 * 8 : all;   // columns of a part, a multiple of eight
-  const int c0 = rank * span, cols = min(span, all - c0) < 0 ? 0 : min(span, all - c0);
-  const long long group = blockIdx.x / nparts, step = (long long)(gridDim.x / nparts) * ROWS;
-  const bool grads = part != nullptr;
-  float dw[E], db[E];
+  const int cols = (int)a.cols;
+  const Walker w = walker_of<NTH>(cols, blockIdx.x / nparts, gridDim.x / nparts);
+  const int ph = EDGE ? w.ph : 0;
+  const int all = (ph + cols + 7) >> 3;                          // runs of a row, and this part's first and number
+  const int g0 = CLUSTER ? (int)((long long)all * rank / nparts) : 0;
+  const int runs = CLUSTER ? (int)((long long)all * (rank + 1) / nparts) - g0 : all;
+  const int shift = ph - 8 * g0;                                 // column of run g: 8 g - shift
+  const T* const dout = (const T*)a.dout - shift;
+  const T* const s_in = (const T*)a.s - shift;
+  const T* const dsum = a.dsum ? (const T*)a.dsum - shift : nullptr;
+  uint4* const mine = ring + threadIdx.x;
+  const u32 mine32 = (u32)__cvta_generic_to_shared(mine);
+  const float inv = 1.f / (float)cols;
+  Held<P> wt[R];
+  F2 dw[R][4], db[R][4];
 #pragma unroll
-  for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
-  unsigned char* bits = dyn + (NTH == 32 ? warp * bits_of(cols) : 0);
-
-  Raw<T, E, VEC> rdy, rs, rds;
-  float mean = 0.f, rstd = 0.f;
-  long long row = group * ROWS + (NTH == 32 ? warp : 0);
-  const T* dout = (const T*)a.dout + c0;
-  const T* s = (const T*)a.s + c0;
-  const T* dsum = a.dsum ? (const T*)a.dsum + c0 : nullptr;
-  const P* weight = a.weight ? (const P*)a.weight + c0 : nullptr;
-  if (row < a.rows) {
-    rdy.template load<NTH>(dout + row * a.dout_stride, cols, t);
-    rs.template load<NTH>(s + row * a.s_stride, cols, t);
-    if (dsum) rds.template load<NTH>(dsum + row * a.dsum_stride, cols, t);
-    mean = a.mean[row];
-    rstd = a.rstd[row];
+  for (int r = 0; r < R; ++r) {
+    float o[8];
+    load_weights((const P*)a.weight, (r * NTH + w.t) * 8 - shift, cols, 1.f, o);
+    wt[r].set(o);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dw[r][j] = db[r][j] = f2(0.f, 0.f);
   }
-  int parity = 0;
-  for (; row < a.rows; row += step, parity ^= 1) {
-    float v[E], h[E], p = 0.f, q = 0.f;
+  auto send = [&](long long row, int stage) {
+    if (row < a.rows) {
+      const u32 to = mine32 + (u32)(stage * 3 * A * 16);
+      const bool last = EDGE && row == a.rows - 1;
+      send_runs<T, NTH, R, CTA>(to, dout + row * a.dout_stride, runs, w.t, last, shift + cols);
+      send_runs<T, NTH, R, CTA>(to + A * 16, s_in + row * a.s_stride, runs, w.t, last, shift + cols);
+      if (dsum) send_runs<T, NTH, R, CTA>(to + 2 * A * 16, dsum + row * a.dsum_stride, runs, w.t, last, shift + cols);
+    }
+    copy_commit();
+  };
 #pragma unroll
-    for (int g = 0; g < E / 8; ++g) {
-      float x[8], y[8], w[8], z[8];
-      rdy.get(g, y);
-      rs.get(g, x);
-      if (dsum) rds.get(g, z);
-      if (VEC) {
-        const int c = (g * NTH + t) * 8;
-        if (weight && c < cols) unpack(load_run(weight + c), w);
-      } else if (weight) {
+  for (int s = 0; s < S; ++s) send(w.row + s * w.step, s);
+  float mean[K], rstd[K];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int c = (g * 8 + j) * NTH + t;
-          if (c < cols) w[j] = to_f(weight[c]);
+  for (int k = 0; k < K; ++k) {
+    const long long row = w.row + k * w.step;
+    mean[k] = row < a.rows ? a.mean[row] : 0.f;
+    rstd[k] = row < a.rows ? a.rstd[row] : 0.f;
+  }
+  int stage = 0, parity = 0;
+  // walkers of one warp go on together, also when the last ones have no row left
+  for (long long row = w.row, lead = w.row - w.slot % (NTH < 32 ? 32 / NTH : 1); lead < a.rows; row += K * w.step, lead += K * w.step) {
+    float mu[K], rs[K], sums[2 * K];
+    bool live[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      live[k] = row + k * w.step < a.rows;
+      mu[k] = mean[k];
+      rs[k] = rstd[k];
+      const long long next = row + (K + k) * w.step;
+      if (next < a.rows) {
+        mean[k] = a.mean[next];
+        rstd[k] = a.rstd[next];
+      }
+    }
+    copy_wait<S - K>();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint4* const at = mine + (stage + k) * 3 * A;
+      F2 p2 = f2(0.f, 0.f), q2 = p2;
+      const F2 mu2 = f2(-mu[k], -mu[k]), rs2 = f2(rs[k], rs[k]);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int g = r * NTH + w.t, c = g * 8 - shift;
+        if (g < runs && live[k]) {
+          float y[8], h[8], v[8];
+          take_run<T, CTA>(at, r, y);
+          take_run<T, CTA>(at + A, r, h);
+          if (ragged<EDGE>(c, cols)) {      // what belongs to other rows counts nothing
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (c + j < 0 || c + j >= cols) {
+                y[j] = 0.f;
+                h[j] = mu[k];
+              }
+          }
+          wt[r].get(v);
+          F2 y2[4], h2[4], v2[4];
+          pairs_of(y, y2);
+          pairs_of(h, h2);
+          pairs_of(v, v2);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            h2[j] = mul2(add2(h2[j], mu2), rs2);
+            dw[r][j] = fma2(y2[j], h2[j], dw[r][j]);
+            db[r][j] = add2(db[r][j], y2[j]);
+            v2[j] = mul2(v2[j], y2[j]);
+            p2 = add2(p2, v2[j]);
+            q2 = fma2(v2[j], h2[j], q2);
+          }
         }
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int e = g * 8 + j;
-        const bool in = col_of<NTH, VEC>(e, t) < cols;
-        const float hh = in ? (x[j] - mean) * rstd : 0.f, dy = in ? y[j] : 0.f;
-        const float gw = weight && in ? dy * w[j] : dy;
-        p += gw;
-        q = fmaf(gw, hh, q);
-        dw[e] = fmaf(dy, hh, dw[e]);
-        db[e] += dy;
-        h[e] = hh;
-        v[e] = dsum && in ? fmaf(rstd, gw, z[j]) : rstd * gw;
-      }
+      float odd;
+      split(p2, sums[2 * k], odd);
+      sums[2 * k] += odd;
+      split(q2, sums[2 * k + 1], odd);
+      sums[2 * k + 1] += odd;
     }
-    const float rs_now = rstd;
-    const long long next = row + step;
-    if (next < a.rows) {
-      rdy.template load<NTH>(dout + next * a.dout_stride, cols, t);
-      rs.template load<NTH>(s + next * a.s_stride, cols, t);
-      if (dsum) rds.template load<NTH>(dsum + next * a.dsum_stride, cols, t);
-      mean = a.mean[next];
-      rstd = a.rstd[next];
-    }
-    const u64 i0 = (u64)row * (u64)all + (u64)c0;
-    if (!VEC && d.on) fill_bits<NTH>(bits, cols, t, i0, d);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      p += __shfl_xor_sync(0xffffffffu, p, o);
-      q += __shfl_xor_sync(0xffffffffu, q, o);
+    for (int o = (NTH < 32 ? NTH : 32) / 2; o > 0; o >>= 1) {
+#pragma unroll
+      for (int i = 0; i < 2 * K; ++i) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], o);
     }
     if (NTH > 32) {
       if ((threadIdx.x & 31) == 0) {
-        sh[parity][0][warp] = p;
-        sh[parity][1][warp] = q;
+#pragma unroll
+        for (int i = 0; i < 2 * K; ++i) sh[parity][i][threadIdx.x >> 5] = sums[i];
       }
       __syncthreads();
-      p = q = 0.f;
 #pragma unroll
-      for (int w = 0; w < NTH / 32; ++w) {
-        p += sh[parity][0][w];
-        q += sh[parity][1][w];
+      for (int i = 0; i < 2 * K; ++i) {
+        sums[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < WARPS; ++j) sums[i] += sh[parity][i][j];
       }
       if (CLUSTER) {
         cg::cluster_group cl = cg::this_cluster();
-        if (threadIdx.x < nparts) *cl.map_shared_rank(&xch[parity][rank], threadIdx.x) = make_float2(p, q);
-        cl.sync();     // the slots of this parity are written again only behind the next row's barrier
-        p = q = 0.f;
-        for (int k = 0; k < nparts; ++k) {
-          p += xch[parity][k].x;
-          q += xch[parity][k].y;
+        if (threadIdx.x < nparts) {
+          float* const to = cl.map_shared_rank(&xch[parity][rank][0], threadIdx.x);
+#pragma unroll
+          for (int i = 0; i < 2 * K; ++i) to[i] = sums[i];
+        }
+        cl.sync();     // the slots of this parity are written again only behind the next rows' barrier
+#pragma unroll
+        for (int i = 0; i < 2 * K; ++i) {
+          sums[i] = 0.f;
+          for (int j = 0; j < nparts; ++j) sums[i] += xch[parity][j][i];
         }
       }
-    } else {
-      __syncwarp();
+      parity ^= 1;
     }
-    p = rs_now * (p / (float)all);
-    q = rs_now * (q / (float)all);
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = fmaf(-h[e], q, v[e] - p);
-    if (a.dresidual) store_row<T, NTH, E, VEC>((T*)a.dresidual + row * a.dresidual_stride + c0, cols, t, v);
-    if (d.on) {
-      drop_row<NTH, E, VEC, false>(v, v, cols, t, i0, d, bits);
-      if (!VEC) row_sync<NTH>();   // the bits are written again for the next row
+    for (int k = 0; k < K; ++k) {
+      const long long now = row + k * w.step;
+      if (live[k]) {
+        const uint4* const at = mine + (stage + k) * 3 * A;
+        const float p = sums[2 * k] * inv, cq = -(rs[k] * rs[k]) * (sums[2 * k + 1] * inv);
+        const F2 mu2 = f2(-mu[k], -mu[k]), rs2 = f2(rs[k], rs[k]), cq2 = f2(cq, cq), p2 = f2(-p, -p);
+        T* const dx = (T*)a.dx + now * a.dx_stride;
+        T* const dr = a.dresidual ? (T*)a.dresidual + now * a.dresidual_stride : nullptr;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const int g = r * NTH + w.t, c = g * 8 - shift;
+          if (g < runs) {
+            float y[8], h[8], v[8];
+            uint4 bits;
+            if (d.on) bits = philox(((u64)now * (u64)cols >> 3) + (u64)(g0 + g), d);
+            take_run<T, CTA>(at, r, y);
+            take_run<T, CTA>(at + A, r, h);
+            wt[r].get(v);
+            F2 y2[4], h2[4], v2[4];
+            pairs_of(y, y2);
+            pairs_of(h, h2);
+            pairs_of(v, v2);
+            // rs (g - p) - (s - mu) rs^2 q [+ dsum]
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y2[j] = fma2(add2(h2[j], mu2), cq2, mul2(fma2(y2[j], v2[j], p2), rs2));
+            if (dsum) {
+              take_run<T, CTA>(at + 2 * A, r, v);
+              pairs_of(v, v2);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) y2[j] = add2(y2[j], v2[j]);
+            }
+            floats_of(y2, y);
+            if (dr) put_run<EDGE>(dr, c, cols, y);
+            if (d.on) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) y[j] = kept(bits, j, d) ? y[j] * d.scale : 0.f;
+            }
+            put_run<EDGE>(dx, c, cols, y);
+          }
+        }
+      }
+      send(now + (long long)S * w.step, stage + k);
     }
-    store_row<T, NTH, E, VEC>((T*)a.dx + row * a.dx_stride + c0, cols, t, v);
+    stage = stage + K == S ? 0 : stage + K;
   }
+  copy_wait<0>();
   if (CLUSTER) cg::this_cluster().sync();   // no CTA leaves while another may still write into its shared memory
-  if (!grads) return;
-  float* pw = part + 2ll * group * max_cols + c0;
-  float* pb = pw + max_cols;
-  if (ROWS == 1) {
+  if (!part) return;
+  float* const pw = part + 2ll * (blockIdx.x / nparts) * max_cols;
+  float* const pb = pw + max_cols;
+  if (W::ROWS == 1) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = col_of<NTH, VEC>(e, t);
-      if (c < cols) {
-        pw[c] = dw[e];
-        pb[c] = db[e];
-      }
-    }
-  } else {   // the four warps' sums, in warp order
-    __shared__ float acc[ROWS == 1 ? 1 : 2][ROWS == 1 ? 1 : NTH * E];
-    for (int w = 0; w < ROWS; ++w) {
-      if (warp == w) {
+    for (int r = 0; r < R; ++r) {
+      float u[8], v[8];
+      floats_of(dw[r], u);
+      floats_of(db[r], v);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int i = e * 32 + t;
-          acc[0][i] = w ? acc[0][i] + dw[e] : dw[e];
-          acc[1][i] = w ? acc[1][i] + db[e] : db[e];
+      for (int j = 0; j < 8; ++j) {
+        const int g = r * NTH + w.t, c = g * 8 - shift + j;
+        if (g < runs && c >= 0 && c < cols) {
+          pw[c] = u[j];
+          pb[c] = v[j];
         }
       }
-      __syncthreads();
     }
-    for (int i = threadIdx.x; i < NTH * E; i += CTA) {
-      const int c = col_of<NTH, VEC>(i / 32, i & 31);
-      if (c < cols) {
-        pw[c] = acc[0][i];
-        pb[c] = acc[1][i];
+  } else {   // the CTA's walkers one after the other
+    float* const acc = reinterpret_cast<float*>(ring);     // the ring is empty now
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * cols; i += CTA) acc[i] = 0.f;
+    for (int k = 0; k < W::ROWS; ++k) {
+      __syncthreads();
+      if (w.slot == k) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          float u[8], v[8];
+          floats_of(dw[r], u);
+          floats_of(db[r], v);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int g = r * NTH + w.t, c = g * 8 - shift + j;
+            if (g < runs && c >= 0 && c < cols) {
+              acc[c] += u[j];
+              acc[cols + c] += v[j];
+            }
+          }
+        }
       }
     }
+    __syncthreads();
+    for (int c = threadIdx.x; c < cols; c += CTA) {
+      pw[c] = acc[c];
+      pb[c] = acc[cols + c];
+    }
   }
+}
+
+// --------------------------------------------------------------------------
+// rows that lie on no runs
+// --------------------------------------------------------------------------
+// Any stride, any alignment: a thread owns every NTH-th column and loads elements one by one.  The generator's bits for a row are
+// made block by block and passed through shared memory.
+__host__ __device__ constexpr int bits_of(int cols) { return ((cols + 14) / 8 + 15) / 16 * 16; }
+constexpr int ANY_NT = 256;
+
+__device__ __forceinline__ void fill_bits(unsigned char* bits, int cols, u64 i0, const Drop& d) {
+  const int nb = ((int)(i0 & 7) + cols + 7) >> 3;
+  for (int b = threadIdx.x; b < nb; b += ANY_NT) bits[b] = (unsigned char)keep_bits((i0 >> 3) + b, d);
+  __syncthreads();
+}
+__device__ __forceinline__ bool bit_at(const unsigned char* bits, int c, u64 i0) {
+  const int i = c + (int)(i0 & 7);
+  return (bits[i >> 3] >> (i & 7)) & 1;
+}
+
+// One CTA a row, which waits in shared memory.
+template <typename T, typename P>
+__global__ void __launch_bounds__(ANY_NT) k_norm_any(const __grid_constant__ adacgd_norm_args a, const __grid_constant__ Drop d) {
+  extern __shared__ uint4 dyn[];
+  __shared__ float sh[2][ANY_NT / 32];
+  const long long row = blockIdx.x;
+  const int cols = (int)a.cols;
+  float* const srow = reinterpret_cast<float*>(dyn);
+  unsigned char* const bits = reinterpret_cast<unsigned char*>(srow + (cols + 3) / 4 * 4);
+  const u64 i0 = (u64)row * (u64)cols;
+  const T* x = (const T*)a.x + row * a.x_stride;
+  const T* res = a.residual ? (const T*)a.residual + row * a.residual_stride : nullptr;
+  if (d.on) fill_bits(bits, cols, i0, d);
+  float acc = 0.f;
+#pragma unroll 4
+  for (int c = threadIdx.x; c < cols; c += ANY_NT) {
+    const float b = res ? to_f(res[c]) : 0.f;
+    float v = to_f(x[c]);
+    if (d.on) v = !bit_at(bits, c, i0) ? b : (res ? scaled(v, b, d) : v * d.scale);
+    else if (res) v = b + v;
+    srow[c] = v;
+    acc += v;
+  }
+  const float mean = walker_sum<ANY_NT>(acc, sh[0]) / (float)cols;
+  acc = 0.f;
+  for (int c = threadIdx.x; c < cols; c += ANY_NT) acc = fmaf(srow[c] - mean, srow[c] - mean, acc);
+  const float rstd = 1.f / sqrtf(walker_sum<ANY_NT>(acc, sh[1]) / (float)cols + a.eps);
+  T* out = (T*)a.out + row * a.out_stride;
+  T* sum = a.sum ? (T*)a.sum + row * a.sum_stride : nullptr;
+  const P* w = (const P*)a.weight;
+  const P* b = (const P*)a.bias;
+#pragma unroll 4
+  for (int c = threadIdx.x; c < cols; c += ANY_NT) {
+    const float v = srow[c];
+    if (sum) sum[c] = from_f<T>(v);
+    out[c] = from_f<T>(fmaf((v - mean) * rstd, w ? to_f(w[c]) : 1.f, b ? to_f(b[c]) : 0.f));
+  }
+  if (threadIdx.x == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+}
+
+// One CTA a row, read twice.
+template <typename T, typename P>
+__global__ void __launch_bounds__(ANY_NT) k_norm_bwd_any(const __grid_constant__ adacgd_norm_backward_args a, const __grid_constant__ Drop d) {
+  extern __shared__ uint4 dyn[];
+  __shared__ float sh[2][ANY_NT / 32];
+  const long long row = blockIdx.x;
+  const int cols = (int)a.cols;
+  unsigned char* const bits = reinterpret_cast<unsigned char*>(dyn);
+  const u64 i0 = (u64)row * (u64)cols;
+  const T* dy = (const T*)a.dout + row * a.dout_stride;
+  const T* s = (const T*)a.s + row * a.s_stride;
+  const T* ds = a.dsum ? (const T*)a.dsum + row * a.dsum_stride : nullptr;
+  T* dx = (T*)a.dx + row * a.dx_stride;
+  T* dr = a.dresidual ? (T*)a.dresidual + row * a.dresidual_stride : nullptr;
+  const P* w = (const P*)a.weight;
+  const float mean = a.mean[row], rstd = a.rstd[row];
+  if (d.on) fill_bits(bits, cols, i0, d);
+  float p = 0.f, q = 0.f;
+#pragma unroll 4
+  for (int c = threadIdx.x; c < cols; c += ANY_NT) {
+    const float g = to_f(dy[c]) * (w ? to_f(w[c]) : 1.f);
+    p += g;
+    q = fmaf(g, (to_f(s[c]) - mean) * rstd, q);
+  }
+  p = walker_sum<ANY_NT>(p, sh[0]) / (float)cols;
+  q = walker_sum<ANY_NT>(q, sh[1]) / (float)cols;
+#pragma unroll 4
+  for (int c = threadIdx.x; c < cols; c += ANY_NT) {
+    float v = rstd * (fmaf(to_f(dy[c]), w ? to_f(w[c]) : 1.f, -p) - ((to_f(s[c]) - mean) * rstd) * q);
+    if (ds) v += to_f(ds[c]);
+    if (dr) dr[c] = from_f<T>(v);
+    if (d.on) v = bit_at(bits, c, i0) ? v * d.scale : 0.f;
+    dx[c] = from_f<T>(v);
+  }
+}
+// Its partial weight gradients, before dx is written (it may be dout or s): a thread a column, a slice of rows a CTA row.
+template <typename T>
+__global__ void __launch_bounds__(ANY_NT) k_norm_dw_any(const __grid_constant__ adacgd_norm_backward_args a, float* __restrict__ part, long long max_cols) {
+  const int c = blockIdx.x * ANY_NT + threadIdx.x;
+  if (c >= a.cols) return;
+  const long long lo = a.rows * blockIdx.y / gridDim.y, hi = a.rows * (blockIdx.y + 1) / gridDim.y;
+  float dw = 0.f, db = 0.f;
+#pragma unroll 4
+  for (long long r = lo; r < hi; ++r) {
+    const float g = to_f(((const T*)a.dout)[r * a.dout_stride + c]);
+    dw = fmaf(g, (to_f(((const T*)a.s)[r * a.s_stride + c]) - a.mean[r]) * a.rstd[r], dw);
+    db += g;
+  }
+  part[(2ll * blockIdx.y) * max_cols + c] = dw;
+  part[(2ll * blockIdx.y + 1) * max_cols + c] = db;
 }
 
 // Adds the CTAs' partial weight gradients: a column a thread of the x dimension, SLICES threads share its partials.
@@ -512,7 +792,6 @@ template <typename T>
 bool run_aligned(const void* p, long long stride, long long rows) {
   return !p || (((uintptr_t)p & 15) == 0 && (rows == 1 || (stride * (long long)sizeof(T)) % 16 == 0));
 }
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 template <typename T>
 int dropout_t(adacgd_dropout_args a, cudaStream_t st) {
@@ -530,88 +809,135 @@ int dropout_t(adacgd_dropout_args a, cudaStream_t st) {
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
-template <typename T, typename P, int NTH, int E, bool VEC>
-int norm_launch(const adacgd_norm_args& a, cudaStream_t st) {
-  constexpr int R = Shape<NTH>::ROWS;
-  const int smem = VEC || a.drop.p == 0.0 ? 0 : R * bits_of((int)a.cols);
-  k_norm<T, P, NTH, E, VEC><<<(unsigned)((a.rows + R - 1) / R), Shape<NTH>::CTA, smem, st>>>(a, make_drop(a.drop));
+// Whether a call's matrices lie on runs: no gaps between rows, or aligned rows of a multiple of eight columns.
+struct Runs {
+  bool whole, flat;
+  long long cols, rows;
+  template <typename T> void look(const void* p, long long stride) {
+    if (!p) return;
+    flat = flat && ((uintptr_t)p & 15) == 0 && (stride == cols || rows == 1);
+    whole = whole && run_aligned<T>(p, stride, rows);
+  }
+  bool good() const { return flat || (whole && cols % 8 == 0); }
+};
+
+template <typename T, typename P, int NTH, int R>
+int norm_launch(const adacgd_norm_args& a, const Where& at) {
+  constexpr int ROWS = Group<NTH>::ROWS;
+  auto kern = a.cols % 8 ? k_norm<T, P, NTH, R, true> : k_norm<T, P, NTH, R, false>;
+  kern<<<(unsigned)((a.rows + ROWS - 1) / ROWS), Group<NTH>::CTA, 0, at.stream>>>(a, make_drop(a.drop));
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
-template <typename T, typename P, bool VEC>
-int norm_by_width(const adacgd_norm_args& a, int sms, cudaStream_t st) {
-  const long long c = a.cols;
-  if (a.rows <= 2 * sms && c > 256) {   // few rows: more threads a row, a shorter chain each
-    if (c <= 1024) return norm_launch<T, P, 128, 8, VEC>(a, st);
-    if (c <= 4096) return norm_launch<T, P, 512, 8, VEC>(a, st);
-    if (c <= 8192) return norm_launch<T, P, 1024, 8, VEC>(a, st);
-  }
-  if (c <= 256) return norm_launch<T, P, 32, 8, VEC>(a, st);
-  if (c <= 1024) return norm_launch<T, P, 32, 32, VEC>(a, st);
-  if (c <= 2048) return norm_launch<T, P, 128, 16, VEC>(a, st);
-  if (c <= 4096) return norm_launch<T, P, 256, 16, VEC>(a, st);
-  if (c <= 8192) return norm_launch<T, P, 512, 16, VEC>(a, st);
-  if (c <= 16384) return norm_launch<T, P, 1024, 16, VEC>(a, st);
-  return norm_launch<T, P, 1024, 32, VEC>(a, st);
-}
-
 template <typename T, typename P>
-int norm_t(const adacgd_norm_args& a, int sms, cudaStream_t st) {
-  const bool vec = a.cols % 8 == 0 && run_aligned<T>(a.x, a.x_stride, a.rows) && run_aligned<T>(a.residual, a.residual_stride, a.rows) &&
-                   run_aligned<T>(a.out, a.out_stride, a.rows) && run_aligned<T>(a.sum, a.sum_stride, a.rows) &&
-                   aligned16(a.weight) && aligned16(a.bias);
-  return vec ? norm_by_width<T, P, true>(a, sms, st) : norm_by_width<T, P, false>(a, sms, st);
+int norm_t(const adacgd_norm_args& a, const Where& at) {
+  Runs k = {true, true, a.cols, a.rows};
+  k.look<T>(a.x, a.x_stride);
+  k.look<T>(a.residual, a.residual_stride);
+  k.look<T>(a.out, a.out_stride);
+  k.look<T>(a.sum, a.sum_stride);
+  const long long n = (a.cols + (a.cols % 8 ? 14 : 0)) / 8;      // the most runs of a row
+  if (!k.good() || n > 2048) {
+    static std::atomic<int> table[TRAIN_DEVICES];
+    const int smem = (int)((a.cols + 3) / 4 * 16) + (a.drop.p > 0.0 ? bits_of((int)a.cols) : 0);
+    auto kern = k_norm_any<T, P>;
+    if (resident_ctas(kern, table, at.device, ANY_NT, ADACGD_TRAIN_MAX_COLS * 4 + bits_of(ADACGD_TRAIN_MAX_COLS)) < 1) return -1;
+    kern<<<(unsigned)a.rows, ANY_NT, smem, at.stream>>>(a, make_drop(a.drop));
+    return cudaGetLastError() == cudaSuccess ? 1 : -1;
+  }
+  if (a.rows <= 2 * at.sms && n > 32) {   // few rows: more threads a row, a shorter chain each
+    if (n <= 128) return norm_launch<T, P, 128, 1>(a, at);
+    if (n <= 512) return norm_launch<T, P, 512, 1>(a, at);
+    if (n <= 1024) return norm_launch<T, P, 1024, 1>(a, at);
+  }
+  if (n <= 8) return norm_launch<T, P, 8, 1>(a, at);
+  if (n <= 16) return norm_launch<T, P, 16, 1>(a, at);
+  if (n <= 32) return norm_launch<T, P, 32, 1>(a, at);
+  if (n <= 64) return norm_launch<T, P, 32, 2>(a, at);
+  if (n <= 128) return norm_launch<T, P, 32, 4>(a, at);
+  if (n <= 256) return norm_launch<T, P, 128, 2>(a, at);
+  if (n <= 512) return norm_launch<T, P, 256, 2>(a, at);
+  if (n <= 1024) return norm_launch<T, P, 512, 2>(a, at);
+  return norm_launch<T, P, 1024, 2>(a, at);
 }
 
-template <typename T, typename P, int NTH, int E, bool VEC, bool CLUSTER>
-int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, int cluster, const Where& at_, cudaStream_t st) {
-  constexpr int R = Shape<NTH>::ROWS, CTA = Shape<NTH>::CTA;
-  auto kern = k_norm_bwd<T, P, NTH, E, VEC, CLUSTER>;
-  const int span = CLUSTER ? ((int)a.cols + cluster - 1) / cluster + 8 : (int)a.cols;
-  const int smem = VEC || a.drop.p == 0.0 ? 0 : R * bits_of(span);
-  static std::atomic<int> table[TRAIN_DEVICES];
-  const int per_sm = resident_ctas(kern, table, at_.device, CTA, VEC ? 0 : R * bits_of(NTH * E));
-  if (per_sm < 1) return -1;
-  long long groups = (long long)at_.sms * per_sm / cluster;
-  if (groups > NORM_PARTS) groups = NORM_PARTS;
-  if (groups > (a.rows + R - 1) / R) groups = (a.rows + R - 1) / R;
-  const bool grads = a.dweight || a.dbias;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(groups * cluster));
-  cfg.blockDim = dim3(CTA);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = cluster;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = CLUSTER ? 1 : 0;
-  if (cudaLaunchKernelEx(&cfg, kern, a, make_drop(a.drop), grads ? s.norm_part : (float*)nullptr, s.max_cols) != cudaSuccess) return -1;
-  if (!grads) return 1;
+template <typename P>
+int sum_parts(const TrainScratch& s, const adacgd_norm_backward_args& a, long long parts, const Where& at) {
   const int cols = (int)a.cols;
-  k_norm_dw_sum<P><<<(cols + SUM_COLS - 1) / SUM_COLS, dim3(SUM_COLS, SUM_SLICES), 0, st>>>(s.norm_part, s.max_cols, (int)groups, cols,
-                                                                                       (P*)a.dweight, (P*)a.dbias);
+  k_norm_dw_sum<P><<<(cols + SUM_COLS - 1) / SUM_COLS, dim3(SUM_COLS, SUM_SLICES), 0, at.stream>>>(s.norm_part, s.max_cols, (int)parts, cols,
+                                                                                              (P*)a.dweight, (P*)a.dbias);
   return cudaGetLastError() == cudaSuccess ? 2 : -1;
 }
 
-template <typename T, typename P, bool VEC>
-int norm_bwd_by_width(const TrainScratch& s, const adacgd_norm_backward_args& a, const Where& sms, cudaStream_t st) {
-  const long long c = a.cols;
-  if (c <= 256) return norm_bwd_launch<T, P, 32, 8, VEC, false>(s, a, 1, sms, st);
-  if (c <= 1024) return norm_bwd_launch<T, P, 128, 8, VEC, false>(s, a, 1, sms, st);
-  if (c <= 2048) return norm_bwd_launch<T, P, 128, 16, VEC, false>(s, a, 1, sms, st);
-  if (c <= 4096) return norm_bwd_launch<T, P, 256, 16, VEC, false>(s, a, 1, sms, st);
-  if (c <= 8192) return norm_bwd_launch<T, P, 512, 16, VEC, false>(s, a, 1, sms, st);
-  return norm_bwd_launch<T, P, 512, 16, VEC, true>(s, a, c <= 16384 ? 2 : 4, sms, st);
+template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE>
+int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, int cluster, const Where& at) {
+  typedef Walk<T, NTH, R, 3> W;
+  static std::atomic<int> table[TRAIN_DEVICES];
+  auto kern = k_norm_bwd<T, P, NTH, R, CLUSTER, EDGE>;
+  const int per_sm = resident_ctas(kern, table, at.device, W::CTA, W::SMEM);
+  if (per_sm < 1) return -1;
+  long long groups = (a.rows + W::ROWS - 1) / W::ROWS, most = (long long)per_sm * at.sms / cluster;
+  if (most > NORM_PARTS) most = NORM_PARTS;
+  if (groups > most) groups = most;
+  const int need = MAX_PERIOD / W::ROWS > 1 ? MAX_PERIOD / W::ROWS : 1;
+  if (EDGE) groups = groups < need ? need : groups / need * need;
+  const bool grads = a.dweight || a.dbias;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(groups * cluster));
+  cfg.blockDim = dim3(W::CTA);
+  cfg.dynamicSmemBytes = W::SMEM;
+  cfg.stream = at.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CLUSTER ? 1 : 0;
+  if (cudaLaunchKernelEx(&cfg, kern, a, make_drop(a.drop), grads ? s.norm_part : (float*)nullptr, s.max_cols) != cudaSuccess) return -1;
+  return grads ? sum_parts<P>(s, a, groups, at) : 1;
+}
+
+template <typename T, typename P, bool EDGE>
+int norm_bwd_by_width(const TrainScratch& s, const adacgd_norm_backward_args& a, long long n, const Where& at) {
+  if (n <= 8) return norm_bwd_launch<T, P, 8, 1, false, EDGE>(s, a, 1, at);
+  if (n <= 16) return norm_bwd_launch<T, P, 16, 1, false, EDGE>(s, a, 1, at);
+  if (n <= 32) return norm_bwd_launch<T, P, 32, 1, false, EDGE>(s, a, 1, at);
+  if (n <= 64) return norm_bwd_launch<T, P, 32, 2, false, EDGE>(s, a, 1, at);
+#ifdef B64
+  if (n <= 128) return norm_bwd_launch<T, P, 64, 2, false, EDGE>(s, a, 1, at);
+#else
+  if (n <= 128) return norm_bwd_launch<T, P, 128, 1, false, EDGE>(s, a, 1, at);
+#endif
+  if (n <= 256) return norm_bwd_launch<T, P, 128, 2, false, EDGE>(s, a, 1, at);
+  if (n <= 512) return norm_bwd_launch<T, P, 256, 2, false, EDGE>(s, a, 1, at);
+  if (n <= 1024) return norm_bwd_launch<T, P, 512, 2, false, EDGE>(s, a, 1, at);
+  return norm_bwd_launch<T, P, 512, 2, true, EDGE>(s, a, (int)((n + 1023) / 1024), at);
 }
 
 template <typename T, typename P>
-int norm_bwd_t(const TrainScratch& s, const adacgd_norm_backward_args& a, const Where& sms, cudaStream_t st) {
-  const bool vec = a.cols % 8 == 0 && run_aligned<T>(a.dout, a.dout_stride, a.rows) && run_aligned<T>(a.s, a.s_stride, a.rows) &&
-                   run_aligned<T>(a.dsum, a.dsum_stride, a.rows) && run_aligned<T>(a.dx, a.dx_stride, a.rows) &&
-                   run_aligned<T>(a.dresidual, a.dresidual_stride, a.rows) && aligned16(a.weight);
-  return vec ? norm_bwd_by_width<T, P, true>(s, a, sms, st) : norm_bwd_by_width<T, P, false>(s, a, sms, st);
+int norm_bwd_t(const TrainScratch& s, const adacgd_norm_backward_args& a, const Where& at) {
+  Runs k = {true, true, a.cols, a.rows};
+  k.look<T>(a.dout, a.dout_stride);
+  k.look<T>(a.s, a.s_stride);
+  k.look<T>(a.dsum, a.dsum_stride);
+  k.look<T>(a.dx, a.dx_stride);
+  k.look<T>(a.dresidual, a.dresidual_stride);
+  const long long n = (a.cols + (a.cols % 8 ? 14 : 0)) / 8;
+  if (!k.good()) {
+    int launched = 1;
+    if (a.dweight || a.dbias) {
+      const int tiles = (int)((a.cols + ANY_NT - 1) / ANY_NT);
+      long long parts = 8ll * at.sms / tiles + 1;
+      if (parts > NORM_PARTS) parts = NORM_PARTS;
+      if (parts > a.rows) parts = a.rows;
+      k_norm_dw_any<T><<<dim3(tiles, (unsigned)parts), ANY_NT, 0, at.stream>>>(a, s.norm_part, s.max_cols);
+      if (sum_parts<P>(s, a, parts, at) < 0) return -1;
+      launched = 3;
+    }
+    k_norm_bwd_any<T, P><<<(unsigned)a.rows, ANY_NT, a.drop.p > 0.0 ? bits_of((int)a.cols) : 0, at.stream>>>(a, make_drop(a.drop));
+    return cudaGetLastError() == cudaSuccess ? launched : -1;
+  }
+  return a.cols % 8 ? norm_bwd_by_width<T, P, true>(s, a, n, at) : norm_bwd_by_width<T, P, false>(s, a, n, at);
 }
 
 }  // namespace
@@ -626,13 +952,13 @@ int norm_bwd_t(const TrainScratch& s, const adacgd_norm_backward_args& a, const 
 int launch_dropout(const adacgd_dropout_args& a, const Where& at) { BY_TYPE(a.dtype, (dropout_t<T>(a, at.stream))) }
 
 int launch_layer_norm(const adacgd_norm_args& a, const Where& at) {
-  if (a.param_dtype == ADACGD_F32) BY_TYPE(a.dtype, (norm_t<T, float>(a, at.sms, at.stream)))
-  BY_TYPE(a.dtype, (norm_t<T, T>(a, at.sms, at.stream)))
+  if (a.param_dtype == ADACGD_F32) BY_TYPE(a.dtype, (norm_t<T, float>(a, at)))
+  BY_TYPE(a.dtype, (norm_t<T, T>(a, at)))
 }
 
 int launch_layer_norm_backward(const TrainScratch& s, const adacgd_norm_backward_args& a, const Where& at) {
-  if (a.param_dtype == ADACGD_F32) BY_TYPE(a.dtype, (norm_bwd_t<T, float>(s, a, at, at.stream)))
-  BY_TYPE(a.dtype, (norm_bwd_t<T, T>(s, a, at, at.stream)))
+  if (a.param_dtype == ADACGD_F32) BY_TYPE(a.dtype, (norm_bwd_t<T, float>(s, a, at)))
+  BY_TYPE(a.dtype, (norm_bwd_t<T, T>(s, a, at)))
 }
 
 }  // namespace adacgd
