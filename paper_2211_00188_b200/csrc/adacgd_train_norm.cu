@@ -132,8 +132,10 @@ template <typename T, int NTH, int R, int ARRAYS> struct Walk {   // R: runs a t
   static constexpr int ROWS = CTA / NTH;
   static constexpr int PIECES = sizeof(T) / 2;                    // 16-byte pieces of a run
   static constexpr int STAGE = ARRAYS * R * PIECES * CTA * 16;    // bytes
-  static constexpr int FIT = 200 * 1024 / (STAGE * (512 / CTA));           // registers allow 512 threads on an SM
-  static constexpr int STAGES = FIT >= 4 ? 4 : 2 * STAGE <= 200 * 1024 ? 2 : 1;
+  // registers allow 512 threads on an SM; 32-bit rows have half the elements a byte, so half of those threads keep up
+  static constexpr int THREADS = sizeof(T) == 4 ? 256 : 512;
+  static constexpr int FIT = 200 * 1024 / (STAGE * (THREADS > CTA ? THREADS / CTA : 1));
+  static constexpr int STAGES = FIT >= 4 ? 4 : FIT >= 2 ? FIT : 1;
   static constexpr int SMEM = STAGES * STAGE;
 };
 
@@ -221,6 +223,44 @@ __device__ __forceinline__ void load_weights(const P* w, int c, int cols, float 
 #pragma unroll
   for (int j = 0; j < 8; ++j) o[j] = w && c + j >= 0 && c + j < cols ? to_f(w[c + j]) : other;
 }
+// The same inside a 16-byte aligned vector, for any c: the aligned pieces around them, shifted.
+__device__ __forceinline__ void shift_weights(const float* w, int c, float (&o)[8]) {
+  const int off = c & 3;
+  const float4* p = reinterpret_cast<const float4*>(w + (c - off));
+  const float4 x = p[0], y = p[1];
+  if (off == 0) {
+    o[0] = x.x; o[1] = x.y; o[2] = x.z; o[3] = x.w; o[4] = y.x; o[5] = y.y; o[6] = y.z; o[7] = y.w;
+    return;
+  }
+  const float4 z = p[2];
+  if (off == 1) {
+    o[0] = x.y; o[1] = x.z; o[2] = x.w; o[3] = y.x; o[4] = y.y; o[5] = y.z; o[6] = y.w; o[7] = z.x;
+  } else if (off == 2) {
+    o[0] = x.z; o[1] = x.w; o[2] = y.x; o[3] = y.y; o[4] = y.z; o[5] = y.w; o[6] = z.x; o[7] = z.y;
+  } else {
+    o[0] = x.w; o[1] = y.x; o[2] = y.y; o[3] = y.z; o[4] = y.w; o[5] = z.x; o[6] = z.y; o[7] = z.z;
+  }
+}
+template <typename P>
+__device__ __forceinline__ void shift_weights(const P* w, int c, float (&o)[8]) {
+  const int off = c & 7;
+  const uint4* p = reinterpret_cast<const uint4*>(w + (c - off));
+  const uint4 x = p[0];
+  const uint4 y = off ? p[1] : x;
+  u32 a[5];
+  switch (off >> 1) {
+    case 0: a[0] = x.x; a[1] = x.y; a[2] = x.z; a[3] = x.w; a[4] = y.x; break;
+    case 1: a[0] = x.y; a[1] = x.z; a[2] = x.w; a[3] = y.x; a[4] = y.y; break;
+    case 2: a[0] = x.z; a[1] = x.w; a[2] = y.x; a[3] = y.y; a[4] = y.z; break;
+    default: a[0] = x.w; a[1] = y.x; a[2] = y.y; a[3] = y.z; a[4] = y.w; break;
+  }
+  const u32 by = (off & 1) * 16;
+  Run<P> r;
+  r.v[0] = make_uint4(__funnelshift_r(a[0], a[1], by), __funnelshift_r(a[1], a[2], by), __funnelshift_r(a[2], a[3], by),
+                      __funnelshift_r(a[3], a[4], by));
+  unpack(r, o);
+}
+
 // Kept in the parameter's own type: half the registers.
 template <typename P> struct Held {
   uint4 v;
@@ -355,7 +395,7 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
   const P* const weight = (const P*)a.weight;
   const P* const bias = (const P*)a.bias;
   const F2 scale = f2(rstd, rstd);
-  const bool even = ((((uintptr_t)weight | (uintptr_t)bias) & 15) == 0) && ph == 0;
+  const bool even = (((uintptr_t)weight | (uintptr_t)bias) & 15) == 0;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int g = r * NTH + t, c = g * 8 - ph;
@@ -365,9 +405,12 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
         floats_of(v[r], u);
         put_run<EDGE>(sum, c, cols, u);
       }
-      if (even && !ragged<EDGE>(c, cols)) {
+      if (even && !EDGE) {
         if (weight) unpack(load_run(weight + c), p);
         if (bias) unpack(load_run(bias + c), q);
+      } else if (even && c >= 0 && c + 16 <= cols) {     // the pieces read end within 15 elements
+        if (weight) shift_weights(weight, c, p);
+        if (bias) shift_weights(bias, c, q);
       } else {
         load_weights(weight, c, cols, 1.f, p);
         load_weights(bias, c, cols, 0.f, q);
@@ -397,11 +440,11 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
 // Rows wider than NTH * R runs are cut into as many column parts as the cluster has CTAs; the two sums then meet in distributed
 // shared memory.
 // K rows go through the two phases together, so that their reductions share one barrier.
-template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE>
-__global__ void __launch_bounds__(Walk<T, NTH, R, 3>::CTA) k_norm_bwd(const __grid_constant__ adacgd_norm_backward_args a,
+template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE, int ARRAYS>
+__global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const __grid_constant__ adacgd_norm_backward_args a,
                                                                       const __grid_constant__ Drop d, float* __restrict__ part,
                                                                       long long max_cols) {
-  typedef Walk<T, NTH, R, 3> W;
+  typedef Walk<T, NTH, R, ARRAYS> W;      // ARRAYS: 3 with dsum, 2 without
   constexpr int CTA = W::CTA, S = W::STAGES, A = R * W::PIECES * CTA, K = S >= 4 ? 2 : 1, WARPS = NTH < 32 ? 1 : NTH / 32;
   extern __shared__ uint4 ring[];
   __shared__ float sh[2][2 * K][WARPS];
@@ -437,11 +480,11 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, 3>::CTA) k_norm_bwd(const __gr
   }
   auto send = [&](long long row, int stage) {
     if (row < a.rows) {
-      const u32 to = mine32 + (u32)(stage * 3 * A * 16);
+      const u32 to = mine32 + (u32)(stage * ARRAYS * A * 16);
       const bool last = EDGE && row == a.rows - 1;
       send_runs<T, NTH, R, CTA>(to, dout + row * a.dout_stride, runs, w.t, last, shift + cols);
       send_runs<T, NTH, R, CTA>(to + A * 16, s_in + row * a.s_stride, runs, w.t, last, shift + cols);
-      if (dsum) send_runs<T, NTH, R, CTA>(to + 2 * A * 16, dsum + row * a.dsum_stride, runs, w.t, last, shift + cols);
+      if (ARRAYS == 3) send_runs<T, NTH, R, CTA>(to + 2 * A * 16, dsum + row * a.dsum_stride, runs, w.t, last, shift + cols);
     }
     copy_commit();
   };
@@ -473,7 +516,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, 3>::CTA) k_norm_bwd(const __gr
     copy_wait<S - K>();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint4* const at = mine + (stage + k) * 3 * A;
+      const uint4* const at = mine + (stage + k) * ARRAYS * A;
       F2 p2 = f2(0.f, 0.f), q2 = p2;
       const F2 mu2 = f2(-mu[k], -mu[k]), rs2 = f2(rs[k], rs[k]);
 #pragma unroll
@@ -550,7 +593,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, 3>::CTA) k_norm_bwd(const __gr
     for (int k = 0; k < K; ++k) {
       const long long now = row + k * w.step;
       if (live[k]) {
-        const uint4* const at = mine + (stage + k) * 3 * A;
+        const uint4* const at = mine + (stage + k) * ARRAYS * A;
         const float p = sums[2 * k] * inv, cq = -(rs[k] * rs[k]) * (sums[2 * k + 1] * inv);
         const F2 mu2 = f2(-mu[k], -mu[k]), rs2 = f2(rs[k], rs[k]), cq2 = f2(cq, cq), p2 = f2(-p, -p);
         T* const dx = (T*)a.dx + now * a.dx_stride;
@@ -572,7 +615,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, 3>::CTA) k_norm_bwd(const __gr
             // rs (g - p) - (s - mu) rs^2 q [+ dsum]
 #pragma unroll
             for (int j = 0; j < 4; ++j) y2[j] = fma2(add2(h2[j], mu2), cq2, mul2(fma2(y2[j], v2[j], p2), rs2));
-            if (dsum) {
+            if (ARRAYS == 3) {
               take_run<T, CTA>(at + 2 * A, r, v);
               pairs_of(v, v2);
 #pragma unroll
@@ -837,7 +880,7 @@ int norm_t(const adacgd_norm_args& a, const Where& at) {
   k.look<T>(a.out, a.out_stride);
   k.look<T>(a.sum, a.sum_stride);
   const long long n = (a.cols + (a.cols % 8 ? 14 : 0)) / 8;      // the most runs of a row
-  if (!k.good() || n > 2048) {
+  if (!k.good() || n > 4096) {
     static std::atomic<int> table[TRAIN_DEVICES];
     const int smem = (int)((a.cols + 3) / 4 * 16) + (a.drop.p > 0.0 ? bits_of((int)a.cols) : 0);
     auto kern = k_norm_any<T, P>;
@@ -858,7 +901,8 @@ int norm_t(const adacgd_norm_args& a, const Where& at) {
   if (n <= 256) return norm_launch<T, P, 128, 2>(a, at);
   if (n <= 512) return norm_launch<T, P, 256, 2>(a, at);
   if (n <= 1024) return norm_launch<T, P, 512, 2>(a, at);
-  return norm_launch<T, P, 1024, 2>(a, at);
+  if (n <= 2048) return norm_launch<T, P, 1024, 2>(a, at);
+  return norm_launch<T, P, 1024, 4>(a, at);
 }
 
 template <typename P>
@@ -869,14 +913,19 @@ int sum_parts(const TrainScratch& s, const adacgd_norm_backward_args& a, long lo
   return cudaGetLastError() == cudaSuccess ? 2 : -1;
 }
 
-template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE>
-int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, int cluster, const Where& at) {
-  typedef Walk<T, NTH, R, 3> W;
+template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE, int ARRAYS>
+int norm_bwd_arrays(const TrainScratch& s, const adacgd_norm_backward_args& a, int cluster, const Where& at) {
+  typedef Walk<T, NTH, R, ARRAYS> W;
   static std::atomic<int> table[TRAIN_DEVICES];
-  auto kern = k_norm_bwd<T, P, NTH, R, CLUSTER, EDGE>;
+  auto kern = k_norm_bwd<T, P, NTH, R, CLUSTER, EDGE, ARRAYS>;
   const int per_sm = resident_ctas(kern, table, at.device, W::CTA, W::SMEM);
   if (per_sm < 1) return -1;
-  long long groups = (a.rows + W::ROWS - 1) / W::ROWS, most = (long long)per_sm * at.sms / cluster;
+  // a walker's partial sums are written and read once more: it should have a few rows of its own
+#ifndef OWN
+#define OWN 1
+#endif
+  long long groups = (a.rows + OWN * W::ROWS - 1) / (OWN * W::ROWS), most = (long long)per_sm * at.sms / cluster;
+  if (groups < at.sms) groups = at.sms < a.rows / W::ROWS + 1 ? at.sms : a.rows / W::ROWS + 1;
   if (most > NORM_PARTS) most = NORM_PARTS;
   if (groups > most) groups = most;
   const int need = MAX_PERIOD / W::ROWS > 1 ? MAX_PERIOD / W::ROWS : 1;
@@ -897,17 +946,19 @@ int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, i
   return grads ? sum_parts<P>(s, a, groups, at) : 1;
 }
 
+template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE>
+int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, int cluster, const Where& at) {
+  return a.dsum ? norm_bwd_arrays<T, P, NTH, R, CLUSTER, EDGE, 3>(s, a, cluster, at)
+                : norm_bwd_arrays<T, P, NTH, R, CLUSTER, EDGE, 2>(s, a, cluster, at);
+}
+
 template <typename T, typename P, bool EDGE>
 int norm_bwd_by_width(const TrainScratch& s, const adacgd_norm_backward_args& a, long long n, const Where& at) {
   if (n <= 8) return norm_bwd_launch<T, P, 8, 1, false, EDGE>(s, a, 1, at);
   if (n <= 16) return norm_bwd_launch<T, P, 16, 1, false, EDGE>(s, a, 1, at);
   if (n <= 32) return norm_bwd_launch<T, P, 32, 1, false, EDGE>(s, a, 1, at);
   if (n <= 64) return norm_bwd_launch<T, P, 32, 2, false, EDGE>(s, a, 1, at);
-#ifdef B64
   if (n <= 128) return norm_bwd_launch<T, P, 64, 2, false, EDGE>(s, a, 1, at);
-#else
-  if (n <= 128) return norm_bwd_launch<T, P, 128, 1, false, EDGE>(s, a, 1, at);
-#endif
   if (n <= 256) return norm_bwd_launch<T, P, 128, 2, false, EDGE>(s, a, 1, at);
   if (n <= 512) return norm_bwd_launch<T, P, 256, 2, false, EDGE>(s, a, 1, at);
   if (n <= 1024) return norm_bwd_launch<T, P, 512, 2, false, EDGE>(s, a, 1, at);
