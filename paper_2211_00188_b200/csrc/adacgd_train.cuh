@@ -69,13 +69,21 @@ template <> __device__ __forceinline__ float from_f<float>(float v) { return v; 
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// ---- eight consecutive elements, moved in 16-byte pieces ----
+// ---- eight consecutive elements: 16 bytes, or 32 of binary32, aligned to their size ----
 template <typename T> struct Run { uint4 v[sizeof(T) / 2]; };
 
 template <typename T> __device__ __forceinline__ Run<T> load_run(const T* p) {
   Run<T> r;
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = *(reinterpret_cast<const uint4*>(p) + i);
+  r.v[0] = *reinterpret_cast<const uint4*>(p);
+  return r;
+}
+// one 32-byte access: two of 16 bytes would each use half of every sector they touch
+template <> __device__ __forceinline__ Run<float> load_run<float>(const float* p) {
+  Run<float> r;
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r.v[0].x), "=r"(r.v[0].y), "=r"(r.v[0].z), "=r"(r.v[0].w), "=r"(r.v[1].x), "=r"(r.v[1].y), "=r"(r.v[1].z), "=r"(r.v[1].w)
+               : "l"(p)
+               : "memory");
   return r;
 }
 __device__ __forceinline__ void unpack(const Run<float>& r, float (&o)[8]) {
@@ -100,8 +108,9 @@ __device__ __forceinline__ void unpack(const Run<__half>& r, float (&o)[8]) {
   }
 }
 __device__ __forceinline__ void store_run(float* p, const float (&v)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]),
+               "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
 }
 // Eight elements of a 16-bit type in 16 bytes, each rounded to nearest.
 template <typename T> __device__ __forceinline__ uint4 pack_run(const float (&v)[8]);

@@ -74,14 +74,14 @@ __device__ __forceinline__ long long label_at(const adacgd_token_rows& r, long l
   return r.label_bytes == 8 ? (long long)((const int64_t*)r.labels)[t] : (long long)((const int32_t*)r.labels)[t];
 }
 
-// A row, or a cluster part of it, cut at 16-byte boundaries: elements [first, first + 8 runs) in whole runs of eight,
+// A row, or a cluster part of it, cut at run boundaries: elements [first, first + 8 runs) in whole runs of eight,
 // [begin, first) and [first + 8 runs, end) one by one (at most seven each).
 struct Cut {
   int begin, first, runs, end;
 };
 template <typename T>
 __device__ __forceinline__ Cut cut_row(const T* row, int vocab, int part, int parts) {
-  constexpr int ALIGN = 16 / sizeof(T);
+  constexpr int ALIGN = 8;
   const int head = min(vocab, (int)((ALIGN - ((uintptr_t)row / sizeof(T)) % ALIGN) % ALIGN));
   const int runs = (vocab - head) >> 3;
   const int r0 = (int)((long long)runs * part / parts), r1 = (int)((long long)runs * (part + 1) / parts);
@@ -130,20 +130,16 @@ __device__ __forceinline__ void absorb(Soft& a, float (&x)[N]) {
 // loads and exponentials overlap within the thread.  LAST: nobody reads these lines again, nor soon what is stored, so both
 // are first to leave the cache and rows that still wait for their second pass stay in it.
 template <typename T, bool LAST> __device__ __forceinline__ Run<T> load_hint(const T* p) {
-  if (!LAST) return load_run(p);
-  Run<T> r;
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-  return r;
+  if constexpr (LAST && sizeof(T) == 2) {
+    Run<T> r;
+    r.v[0] = __ldcs(reinterpret_cast<const uint4*>(p));
+    return r;
+  }
+  return load_run(p);
 }
 template <typename T, bool LAST> __device__ __forceinline__ void store_hint(T* p, const float (&v)[8]) {
-  if (!LAST) return store_run(p, v);
-  if constexpr (sizeof(T) == 2) {
-    __stcs(reinterpret_cast<uint4*>(p), pack_run<T>(v));
-  } else {
-    __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
-  }
+  if constexpr (LAST && sizeof(T) == 2) __stcs(reinterpret_cast<uint4*>(p), pack_run<T>(v));
+  else store_run(p, v);
 }
 template <typename T> struct Batch {
   static constexpr int U = sizeof(T) == 2 ? 4 : 2;
@@ -342,7 +338,9 @@ __device__ __forceinline__ void thread_zero(T* d, const Cut& c, int t) {   // c 
   for (int r = t; r < c.runs; r += NTH) store_run(d + c.first + 8ll * r, z);
 }
 template <typename T>
-__device__ __forceinline__ bool same_phase(const T* a, const T* b) { return (((uintptr_t)a ^ (uintptr_t)b) & 15) == 0; }
+__device__ __forceinline__ bool same_phase(const T* a, const T* b) {
+  return (((uintptr_t)a ^ (uintptr_t)b) & (8 * sizeof(T) - 1)) == 0;
+}
 
 // Where a thread stands: its row, its number among the row's threads, the row's part it works on.
 template <int NTH, bool CLUSTER> struct Place {

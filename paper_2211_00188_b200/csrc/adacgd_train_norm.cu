@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(DROP_NT, 5) k_dropout(const T* x, long long xs
 // --------------------------------------------------------------------------
 // The fast form.  A run is eight elements whose number (row * cols + col) begins at a multiple of eight, which is also a block
 // of the dropout generator.  In matrices without gaps between rows, and in aligned ones whose width is a multiple of eight, a
-// run is 16-byte aligned in memory, whatever the width; only a row's first and last run may hold elements of its neighbours.
+// run is aligned to its size in memory, whatever the width; only a row's first and last run may hold elements of its neighbours.
 // `ph` = how many the first run does.  Rows whose numbers differ by a multiple of PERIOD = 8 / gcd(cols, 8) have the same ph, so a
 // walker (NTH threads) that takes such rows only finds the same columns in the same registers for every one of them: weights
 // are loaded once, weight gradients summed in place.
@@ -127,8 +127,9 @@ __global__ void __launch_bounds__(DROP_NT, 5) k_dropout(const T* x, long long xs
 // and memory does not wait for a row's reductions.
 constexpr int MAX_PERIOD = 8;
 
+__host__ __device__ constexpr int walk_cta(int nth) { return nth < 256 ? 256 : nth; }   // narrow rows: several walkers a CTA, whose partial sums it adds
 template <typename T, int NTH, int R, int ARRAYS> struct Walk {   // R: runs a thread
-  static constexpr int CTA = NTH <= 32 ? 128 : NTH;
+  static constexpr int CTA = walk_cta(NTH);
   static constexpr int ROWS = CTA / NTH;
   static constexpr int PIECES = sizeof(T) / 2;                    // 16-byte pieces of a run
   static constexpr int STAGE = ARRAYS * R * PIECES * CTA * 16;    // bytes
@@ -146,7 +147,7 @@ struct Walker {
 // Which rows a thread's walker takes: those of one class modulo the period, evenly dealt among the class's walkers.
 template <int NTH>
 __device__ __forceinline__ Walker walker_of(int cols, int group, int groups) {
-  constexpr int CTA = NTH <= 32 ? 128 : NTH, ROWS = CTA / NTH;
+  constexpr int ROWS = walk_cta(NTH) / NTH;
   const int period = MAX_PERIOD / (cols & 1 ? 1 : (cols & 2 ? 2 : (cols & 4 ? 4 : 8)));
   Walker w;
   w.t = threadIdx.x % NTH;
@@ -165,42 +166,63 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Sends a thread's runs of one row of one array on their way.  `last`: the matrix ends `left` elements behind the row's first run.
+// Binary32: the lanes of a row's warp copy each other's pieces, consecutive ones together, because a lane's own two would be
+// halves of sectors; they meet at warp_meets() before they read and before they send again.
+template <typename T>
+__device__ __forceinline__ void warp_meets() {
+  if (sizeof(T) == 4) __syncwarp();
+}
 template <typename T, int NTH, int R, int CTA>
-__device__ __forceinline__ void send_runs(u32 to, const T* first, int runs, int t, bool last, int left) {
+__device__ __forceinline__ void send_runs(u32 ring32, const T* first, int runs, int t, bool last, int left) {
+  constexpr int L = NTH < 32 ? NTH : 32, PIECES = sizeof(T) / 2, E = 16 / (int)sizeof(T);
+  const int tl = t % L;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int g = r * NTH + t;
-    if (g < runs) {
 #pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-        const int at = 8 * g + i * (16 / (int)sizeof(T));
+    for (int i = 0; i < PIECES; ++i) {
+      const int q = PIECES * (r * NTH + t - tl) + tl + i * L;          // piece of the row
+      if (q < PIECES * runs) {
         int bytes = 16;
-        if (last) bytes = max(0, min(16, (left - at) * (int)sizeof(T)));
-        if (bytes > 0) copy16(to + (r * (sizeof(T) / 2) + i) * CTA * 16, first + at, bytes);
+        if (last) bytes = max(0, min(16, (left - q * E) * (int)sizeof(T)));
+        if (bytes > 0) copy16(ring32 + (u32)(r * PIECES * CTA + PIECES * ((int)threadIdx.x - tl) + tl + i * L) * 16, first + q * E, bytes);
       }
     }
   }
 }
+// A thread's r-th run of an array's stage.
 template <typename T, int CTA>
-__device__ __forceinline__ void take_run(const uint4* from, int r, float (&o)[8]) {
+__device__ __forceinline__ void take_run(const uint4* stage, int r, float (&o)[8]) {
+  constexpr int PIECES = sizeof(T) / 2;
   Run<T> v;
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) v.v[i] = from[(r * (sizeof(T) / 2) + i) * CTA];
+  for (int i = 0; i < PIECES; ++i) v.v[i] = stage[r * PIECES * CTA + PIECES * threadIdx.x + i];
   unpack(v, o);
 }
 // Whether some of a run's elements belong to other rows.  Without EDGE (widths of whole runs) none do, and nothing is asked.
 template <bool EDGE>
 __device__ __forceinline__ bool ragged(int c, int cols) { return EDGE && (c < 0 || c + 8 > cols); }
+// Whether the run in which a row ends (element number `end` is the first behind it) reaches past the matrix.
+__device__ __forceinline__ bool passes_end(u64 end, u64 elements) { return ((end + 7) & ~7ull) > elements; }
+// First in what only ragged runs do: keeps the compiler from executing it for all of them, with predicates.
+__device__ __forceinline__ void seldom() { asm volatile(""); }
 // Stores a run, or of one at a row's end what belongs to the row.  row: its first element, c: column of the run's first.
 template <bool EDGE, typename T>
 __device__ __forceinline__ void put_run(T* row, int c, int cols, const float (&v)[8]) {
-  if (!EDGE || (c >= 0 && c + 8 <= cols)) {
+  if (!ragged<EDGE>(c, cols)) {
     store_run(row + c, v);
   } else {
+    seldom();
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (c + j >= 0 && c + j < cols) row[c + j] = from_f<T>(v[j]);
   }
+}
+
+// The walker's own barrier where its CTA has several.
+template <int NTH, int CTA>
+__device__ __forceinline__ void walker_sync() {
+  if (NTH == CTA) __syncthreads();
+  else asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / NTH), "n"(NTH) : "memory");
 }
 
 // Sum over a walker's threads, the same bits in each; `sh` alternates.  NTH <= 32: within the warp.
@@ -303,8 +325,8 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
   const int ph = EDGE ? (int)(i0 & 7) : 0, runs = live ? (ph + cols + 7) >> 3 : 0;
   const T* const x = (const T*)a.x + row * a.x_stride - ph;
   const T* const res = a.residual ? (const T*)a.residual + row * a.residual_stride - ph : nullptr;
-  // a matrix's last run may reach past its end: its own row's elements are read one by one then
-  const bool tail = EDGE && (row == a.rows - 1) && ((ph + cols) & 7);
+  // the matrix's last run may reach past its end: the row's own elements are read one by one then
+  const bool tail = EDGE && passes_end(i0 + cols, (u64)a.rows * cols);
   Run<T> raw[R], rest[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -328,6 +350,7 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
     if (g < runs) {
       float u[8], b[8];
       if (tail && g == runs - 1) {
+        seldom();
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           u[j] = c + j >= 0 && c + j < cols ? to_f(x[8 * g + j]) : 0.f;
@@ -347,6 +370,7 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
         }
       }
       if (ragged<EDGE>(c, cols)) {
+        seldom();
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           if (c + j < 0 || c + j >= cols) u[j] = b[j] = 0.f;
@@ -373,6 +397,7 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
     const int g = r * NTH + t, c = g * 8 - ph;
     if (g < runs) {
       if (ragged<EDGE>(c, cols)) {
+        seldom();
         float u[8];
         floats_of(v[r], u);
 #pragma unroll
@@ -412,6 +437,7 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
         if (weight) shift_weights(weight, c, p);
         if (bias) shift_weights(bias, c, q);
       } else {
+        seldom();
         load_weights(weight, c, cols, 1.f, p);
         load_weights(bias, c, cols, 0.f, q);
       }
@@ -447,7 +473,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
   typedef Walk<T, NTH, R, ARRAYS> W;      // ARRAYS: 3 with dsum, 2 without
   constexpr int CTA = W::CTA, S = W::STAGES, A = R * W::PIECES * CTA, K = S >= 4 ? 2 : 1, WARPS = NTH < 32 ? 1 : NTH / 32;
   extern __shared__ uint4 ring[];
-  __shared__ float sh[2][2 * K][WARPS];
+  __shared__ float sh_all[W::ROWS][2][2 * K][WARPS];
   __shared__ float xch[2][8][2 * K];
   int nparts = 1, rank = 0;
   if (CLUSTER) {
@@ -457,6 +483,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
   }
   const int cols = (int)a.cols;
   const Walker w = walker_of<NTH>(cols, blockIdx.x / nparts, gridDim.x / nparts);
+  float (&sh)[2][2 * K][WARPS] = sh_all[w.slot];
   const int ph = EDGE ? w.ph : 0;
   const int all = (ph + cols + 7) >> 3;                          // runs of a row, and this part's first and number
   const int g0 = CLUSTER ? (int)((long long)all * rank / nparts) : 0;
@@ -465,26 +492,28 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
   const T* const dout = (const T*)a.dout - shift;
   const T* const s_in = (const T*)a.s - shift;
   const T* const dsum = a.dsum ? (const T*)a.dsum - shift : nullptr;
-  uint4* const mine = ring + threadIdx.x;
-  const u32 mine32 = (u32)__cvta_generic_to_shared(mine);
+  const u32 ring32 = (u32)__cvta_generic_to_shared(ring);
   const float inv = 1.f / (float)cols;
   Held<P> wt[R];
   F2 dw[R][4], db[R][4];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     float o[8];
-    load_weights((const P*)a.weight, (r * NTH + w.t) * 8 - shift, cols, 1.f, o);
+    const int c = (r * NTH + w.t) * 8 - shift;
+    if (a.weight && (uintptr_t)a.weight % 16 == 0 && c >= 0 && c + 16 <= cols) shift_weights((const P*)a.weight, c, o);
+    else load_weights((const P*)a.weight, c, cols, 1.f, o);
     wt[r].set(o);
 #pragma unroll
     for (int j = 0; j < 4; ++j) dw[r][j] = db[r][j] = f2(0.f, 0.f);
   }
   auto send = [&](long long row, int stage) {
     if (row < a.rows) {
-      const u32 to = mine32 + (u32)(stage * ARRAYS * A * 16);
-      const bool last = EDGE && row == a.rows - 1;
-      send_runs<T, NTH, R, CTA>(to, dout + row * a.dout_stride, runs, w.t, last, shift + cols);
-      send_runs<T, NTH, R, CTA>(to + A * 16, s_in + row * a.s_stride, runs, w.t, last, shift + cols);
-      if (ARRAYS == 3) send_runs<T, NTH, R, CTA>(to + 2 * A * 16, dsum + row * a.dsum_stride, runs, w.t, last, shift + cols);
+      const u32 to = ring32 + (u32)(stage * ARRAYS * A * 16);
+      const bool last = EDGE && passes_end((u64)(row + 1) * cols, (u64)a.rows * cols);
+      const int left = last ? (int)((a.rows - row) * cols) + shift : 0;
+      send_runs<T, NTH, R, CTA>(to, dout + row * a.dout_stride, runs, w.t, last, left);
+      send_runs<T, NTH, R, CTA>(to + A * 16, s_in + row * a.s_stride, runs, w.t, last, left);
+      if (ARRAYS == 3) send_runs<T, NTH, R, CTA>(to + 2 * A * 16, dsum + row * a.dsum_stride, runs, w.t, last, left);
     }
     copy_commit();
   };
@@ -514,9 +543,10 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
       }
     }
     copy_wait<S - K>();
+    warp_meets<T>();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint4* const at = mine + (stage + k) * ARRAYS * A;
+      const uint4* const at = ring + (stage + k) * ARRAYS * A;
       F2 p2 = f2(0.f, 0.f), q2 = p2;
       const F2 mu2 = f2(-mu[k], -mu[k]), rs2 = f2(rs[k], rs[k]);
 #pragma unroll
@@ -527,6 +557,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
           take_run<T, CTA>(at, r, y);
           take_run<T, CTA>(at + A, r, h);
           if (ragged<EDGE>(c, cols)) {      // what belongs to other rows counts nothing
+            seldom();
 #pragma unroll
             for (int j = 0; j < 8; ++j)
               if (c + j < 0 || c + j >= cols) {
@@ -564,9 +595,9 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
     if (NTH > 32) {
       if ((threadIdx.x & 31) == 0) {
 #pragma unroll
-        for (int i = 0; i < 2 * K; ++i) sh[parity][i][threadIdx.x >> 5] = sums[i];
+        for (int i = 0; i < 2 * K; ++i) sh[parity][i][w.t >> 5] = sums[i];
       }
-      __syncthreads();
+      walker_sync<NTH, CTA>();
 #pragma unroll
       for (int i = 0; i < 2 * K; ++i) {
         sums[i] = 0.f;
@@ -593,7 +624,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
     for (int k = 0; k < K; ++k) {
       const long long now = row + k * w.step;
       if (live[k]) {
-        const uint4* const at = mine + (stage + k) * ARRAYS * A;
+        const uint4* const at = ring + (stage + k) * ARRAYS * A;
         const float p = sums[2 * k] * inv, cq = -(rs[k] * rs[k]) * (sums[2 * k + 1] * inv);
         const F2 mu2 = f2(-mu[k], -mu[k]), rs2 = f2(rs[k], rs[k]), cq2 = f2(cq, cq), p2 = f2(-p, -p);
         T* const dx = (T*)a.dx + now * a.dx_stride;
@@ -631,8 +662,10 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
           }
         }
       }
-      send(now + (long long)S * w.step, stage + k);
     }
+    warp_meets<T>();
+#pragma unroll
+    for (int k = 0; k < K; ++k) send(row + (S + k) * w.step, stage + k);
     stage = stage + K == S ? 0 : stage + K;
   }
   copy_wait<0>();
@@ -799,13 +832,15 @@ __global__ void __launch_bounds__(ANY_NT) k_norm_dw_any(const __grid_constant__ 
   part[(2ll * blockIdx.y + 1) * max_cols + c] = db;
 }
 
-// Adds the CTAs' partial weight gradients: a column a thread of the x dimension, SLICES threads share its partials.
-constexpr int SUM_COLS = 32, SUM_SLICES = 16;
+// Adds the CTAs' partial weight gradients: SUM_COLS columns a CTA, SUM_SLICES threads share a column's partials.  Few columns a CTA,
+// so that the partials, which still lie in the cache, are fetched by many SMs at once.
+constexpr int SUM_COLS = 8, SUM_SLICES = 64;
 template <typename P>
 __global__ void __launch_bounds__(SUM_COLS* SUM_SLICES) k_norm_dw_sum(const float* __restrict__ part, long long max_cols, int parts,
                                                                       int cols, P* __restrict__ dw, P* __restrict__ db) {
   __shared__ double sh[2][SUM_SLICES][SUM_COLS];
-  const int c = blockIdx.x * SUM_COLS + threadIdx.x, s = threadIdx.y;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int x = threadIdx.x % SUM_COLS, s = threadIdx.x / SUM_COLS, c = blockIdx.x * SUM_COLS + x;
   double a = 0.0, b = 0.0;
   if (c < cols) {
 #pragma unroll 4
@@ -814,16 +849,26 @@ __global__ void __launch_bounds__(SUM_COLS* SUM_SLICES) k_norm_dw_sum(const floa
       b += (double)part[(2ll * k + 1) * max_cols + c];
     }
   }
-  sh[0][s][threadIdx.x] = a;
-  sh[1][s][threadIdx.x] = b;
-  __syncthreads();
-  if (s || c >= cols) return;
-  a = b = 0.0;
+  sh[0][s][x] = a;
+  sh[1][s][x] = b;
 #pragma unroll
-  for (int k = 0; k < SUM_SLICES; ++k) {
-    a += sh[0][k][threadIdx.x];
-    b += sh[1][k][threadIdx.x];
+  for (int w = SUM_SLICES / 8; w >= 1; w /= 8) {      // eight neighbours at a time, in order
+    __syncthreads();
+    if (s < w) {
+      a = b = 0.0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        a += sh[0][s * 8 + k][x];
+        b += sh[1][s * 8 + k][x];
+      }
+    }
+    __syncthreads();
+    if (s < w) {
+      sh[0][s][x] = a;
+      sh[1][s][x] = b;
+    }
   }
+  if (s || c >= cols) return;
   if (dw) dw[c] = from_f<P>((float)a);
   if (db) db[c] = from_f<P>((float)b);
 }
@@ -833,7 +878,7 @@ __global__ void __launch_bounds__(SUM_COLS* SUM_SLICES) k_norm_dw_sum(const floa
 // --------------------------------------------------------------------------
 template <typename T>
 bool run_aligned(const void* p, long long stride, long long rows) {
-  return !p || (((uintptr_t)p & 15) == 0 && (rows == 1 || (stride * (long long)sizeof(T)) % 16 == 0));
+  return !p || ((uintptr_t)p % (8 * sizeof(T)) == 0 && (rows == 1 || stride % 8 == 0));
 }
 
 template <typename T>
@@ -858,7 +903,7 @@ struct Runs {
   long long cols, rows;
   template <typename T> void look(const void* p, long long stride) {
     if (!p) return;
-    flat = flat && ((uintptr_t)p & 15) == 0 && (stride == cols || rows == 1);
+    flat = flat && (uintptr_t)p % (8 * sizeof(T)) == 0 && (stride == cols || rows == 1);
     whole = whole && run_aligned<T>(p, stride, rows);
   }
   bool good() const { return flat || (whole && cols % 8 == 0); }
@@ -908,9 +953,18 @@ int norm_t(const adacgd_norm_args& a, const Where& at) {
 template <typename P>
 int sum_parts(const TrainScratch& s, const adacgd_norm_backward_args& a, long long parts, const Where& at) {
   const int cols = (int)a.cols;
-  k_norm_dw_sum<P><<<(cols + SUM_COLS - 1) / SUM_COLS, dim3(SUM_COLS, SUM_SLICES), 0, at.stream>>>(s.norm_part, s.max_cols, (int)parts, cols,
-                                                                                              (P*)a.dweight, (P*)a.dbias);
-  return cudaGetLastError() == cudaSuccess ? 2 : -1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((cols + SUM_COLS - 1) / SUM_COLS));
+  cfg.blockDim = dim3(SUM_COLS * SUM_SLICES);
+  cfg.stream = at.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_norm_dw_sum<P>, (const float*)s.norm_part, s.max_cols, (int)parts, cols, (P*)a.dweight, (P*)a.dbias) == cudaSuccess
+             ? 2
+             : -1;
 }
 
 template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE, int ARRAYS>
@@ -920,12 +974,7 @@ int norm_bwd_arrays(const TrainScratch& s, const adacgd_norm_backward_args& a, i
   auto kern = k_norm_bwd<T, P, NTH, R, CLUSTER, EDGE, ARRAYS>;
   const int per_sm = resident_ctas(kern, table, at.device, W::CTA, W::SMEM);
   if (per_sm < 1) return -1;
-  // a walker's partial sums are written and read once more: it should have a few rows of its own
-#ifndef OWN
-#define OWN 1
-#endif
-  long long groups = (a.rows + OWN * W::ROWS - 1) / (OWN * W::ROWS), most = (long long)per_sm * at.sms / cluster;
-  if (groups < at.sms) groups = at.sms < a.rows / W::ROWS + 1 ? at.sms : a.rows / W::ROWS + 1;
+  long long groups = (a.rows + W::ROWS - 1) / W::ROWS, most = (long long)per_sm * at.sms / cluster;
   if (most > NORM_PARTS) most = NORM_PARTS;
   if (groups > most) groups = most;
   const int need = MAX_PERIOD / W::ROWS > 1 ? MAX_PERIOD / W::ROWS : 1;
