@@ -119,12 +119,12 @@ __global__ void __launch_bounds__(DROP_NT, 5) k_dropout(const T* x, long long xs
 // --------------------------------------------------------------------------
 // The fast form.  A run is eight elements whose number (row * cols + col) begins at a multiple of eight, which is also a block
 // of the dropout generator.  In matrices without gaps between rows, and in aligned ones whose width is a multiple of eight, a
-// run is aligned to its size in memory, whatever the width; only a row's first and last run may hold elements of its neighbours.
-// `ph` = how many the first run does.  Rows whose numbers differ by a multiple of PERIOD = 8 / gcd(cols, 8) have the same ph, so a
-// walker (NTH threads) that takes such rows only finds the same columns in the same registers for every one of them: weights
+// run is aligned to its size in memory, whatever the width.  A row is its whole runs and, with EDGE (other widths), up to seven
+// elements in front of them and seven behind, which threads take one each: a warp would execute a run that only partly belongs
+// to the row element by element, for every row.
+// `ph` = where in its run a row begins.  Rows whose numbers differ by a multiple of PERIOD = 8 / gcd(cols, 8) have the same ph, so
+// a walker (NTH threads) that takes such rows only finds the same columns in the same registers for every one of them: weights
 // are loaded once, weight gradients summed in place.
-// A thread copies its runs of the next STAGES rows to shared memory (cp.async) and is the only one to read them back: no barrier,
-// and memory does not wait for a row's reductions.
 constexpr int MAX_PERIOD = 8;
 
 __host__ __device__ constexpr int walk_cta(int nth) { return nth < 256 ? 256 : nth; }   // narrow rows: several walkers a CTA, whose partial sums it adds
@@ -139,6 +139,24 @@ template <typename T, int NTH, int R, int ARRAYS> struct Walk {   // R: runs a t
   static constexpr int STAGES = FIT >= 4 ? 4 : FIT >= 2 ? FIT : 1;
   static constexpr int SMEM = STAGES * STAGE;
 };
+
+// A row's whole runs, and the column outside them that a thread takes (-1: none).
+struct Lie {
+  int first, runs, edge;
+};
+template <bool EDGE>
+__device__ __forceinline__ Lie lie_of(int ph, int cols, int t) {
+  Lie l;
+  l.first = EDGE ? min(cols, (8 - ph) & 7) : 0;
+  l.runs = (cols - l.first) >> 3;
+  l.edge = -1;
+  if (EDGE) {
+    const int c = t < l.first ? t : 8 * l.runs + t;      // behind the runs: first + 8 runs + (t - first)
+    if (c < cols) l.edge = c;
+    if (t >= 16) l.edge = -1;
+  }
+  return l;
+}
 
 struct Walker {
   long long row, step;
@@ -159,13 +177,13 @@ __device__ __forceinline__ Walker walker_of(int cols, int group, int groups) {
   return w;
 }
 
-__device__ __forceinline__ void copy16(u32 to, const void* from, int bytes) {   // the rest of the 16 bytes becomes zero
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+__device__ __forceinline__ void copy16(u32 to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Sends a thread's runs of one row of one array on their way.  `last`: the matrix ends `left` elements behind the row's first run.
+// Sends a row's runs of one array on their way.
 // Binary32: the lanes of a row's warp copy each other's pieces, consecutive ones together, because a lane's own two would be
 // halves of sectors; they meet at warp_meets() before they read and before they send again.
 template <typename T>
@@ -173,7 +191,7 @@ __device__ __forceinline__ void warp_meets() {
   if (sizeof(T) == 4) __syncwarp();
 }
 template <typename T, int NTH, int R, int CTA>
-__device__ __forceinline__ void send_runs(u32 ring32, const T* first, int runs, int t, bool last, int left) {
+__device__ __forceinline__ void send_runs(u32 ring32, const T* first, int runs, int t) {
   constexpr int L = NTH < 32 ? NTH : 32, PIECES = sizeof(T) / 2, E = 16 / (int)sizeof(T);
   const int tl = t % L;
 #pragma unroll
@@ -181,11 +199,7 @@ __device__ __forceinline__ void send_runs(u32 ring32, const T* first, int runs, 
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int q = PIECES * (r * NTH + t - tl) + tl + i * L;          // piece of the row
-      if (q < PIECES * runs) {
-        int bytes = 16;
-        if (last) bytes = max(0, min(16, (left - q * E) * (int)sizeof(T)));
-        if (bytes > 0) copy16(ring32 + (u32)(r * PIECES * CTA + PIECES * ((int)threadIdx.x - tl) + tl + i * L) * 16, first + q * E, bytes);
-      }
+      if (q < PIECES * runs) copy16(ring32 + (u32)(r * PIECES * CTA + PIECES * ((int)threadIdx.x - tl) + tl + i * L) * 16, first + q * E);
     }
   }
 }
@@ -198,26 +212,6 @@ __device__ __forceinline__ void take_run(const uint4* stage, int r, float (&o)[8
   for (int i = 0; i < PIECES; ++i) v.v[i] = stage[r * PIECES * CTA + PIECES * threadIdx.x + i];
   unpack(v, o);
 }
-// Whether some of a run's elements belong to other rows.  Without EDGE (widths of whole runs) none do, and nothing is asked.
-template <bool EDGE>
-__device__ __forceinline__ bool ragged(int c, int cols) { return EDGE && (c < 0 || c + 8 > cols); }
-// Whether the run in which a row ends (element number `end` is the first behind it) reaches past the matrix.
-__device__ __forceinline__ bool passes_end(u64 end, u64 elements) { return ((end + 7) & ~7ull) > elements; }
-// First in what only ragged runs do: keeps the compiler from executing it for all of them, with predicates.
-__device__ __forceinline__ void seldom() { asm volatile(""); }
-// Stores a run, or of one at a row's end what belongs to the row.  row: its first element, c: column of the run's first.
-template <bool EDGE, typename T>
-__device__ __forceinline__ void put_run(T* row, int c, int cols, const float (&v)[8]) {
-  if (!ragged<EDGE>(c, cols)) {
-    store_run(row + c, v);
-  } else {
-    seldom();
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j >= 0 && c + j < cols) row[c + j] = from_f<T>(v[j]);
-  }
-}
-
 // The walker's own barrier where its CTA has several.
 template <int NTH, int CTA>
 __device__ __forceinline__ void walker_sync() {
@@ -239,13 +233,7 @@ __device__ __forceinline__ float walker_sum(float v, float* sh) {
   return t;
 }
 
-// Eight weights from column c on, `other` outside the row.
-template <typename P>
-__device__ __forceinline__ void load_weights(const P* w, int c, int cols, float other, float (&o)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) o[j] = w && c + j >= 0 && c + j < cols ? to_f(w[c + j]) : other;
-}
-// The same inside a 16-byte aligned vector, for any c: the aligned pieces around them, shifted.
+// Eight weights of a 16-byte aligned vector from any column c on: the aligned pieces around them, shifted.
 __device__ __forceinline__ void shift_weights(const float* w, int c, float (&o)[8]) {
   const int off = c & 3;
   const float4* p = reinterpret_cast<const float4*>(w + (c - off));
@@ -283,6 +271,19 @@ __device__ __forceinline__ void shift_weights(const P* w, int c, float (&o)[8]) 
   unpack(r, o);
 }
 
+// Eight weights from column c on (c + 8 <= cols), `other` without a vector.
+template <typename P>
+__device__ __forceinline__ void load_weights(const P* w, int c, int cols, float other, float (&o)[8]) {
+  if (!w) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = other;
+  } else if (((uintptr_t)w & 15) == 0 && c + 16 <= cols) {     // the pieces read end within 15 elements
+    shift_weights(w, c, o);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = to_f(w[c + j]);
+  }
+}
 // Kept in the parameter's own type: half the registers.
 template <typename P> struct Held {
   uint4 v;
@@ -322,44 +323,39 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
   if (NTH >= 32 && row >= a.rows) return;          // whole warps; no barrier follows where a CTA has several rows
   const bool live = row < a.rows;
   const u64 i0 = (u64)row * (u64)cols;
-  const int ph = EDGE ? (int)(i0 & 7) : 0, runs = live ? (ph + cols + 7) >> 3 : 0;
-  const T* const x = (const T*)a.x + row * a.x_stride - ph;
-  const T* const res = a.residual ? (const T*)a.residual + row * a.residual_stride - ph : nullptr;
-  // the matrix's last run may reach past its end: the row's own elements are read one by one then
-  const bool tail = EDGE && passes_end(i0 + cols, (u64)a.rows * cols);
+  Lie l = lie_of<EDGE>((int)(i0 & 7), cols, t);
+  if (!live) {
+    l.runs = 0;
+    l.edge = -1;
+  }
+  const T* const x = (const T*)a.x + row * a.x_stride;
+  const T* const res = a.residual ? (const T*)a.residual + row * a.residual_stride : nullptr;
   Run<T> raw[R], rest[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int g = r * NTH + t;
-    if (g < runs && !(tail && g == runs - 1)) {
-      raw[r] = load_run(x + 8 * g);
-      if (res) rest[r] = load_run(res + 8 * g);
+    if (g < l.runs) {
+      raw[r] = load_run(x + l.first + 8 * g);
+      if (res) rest[r] = load_run(res + l.first + 8 * g);
     }
+  }
+  float ev = 0.f, er = 0.f;
+  if (EDGE && l.edge >= 0) {
+    ev = to_f(x[l.edge]);
+    if (res) er = to_f(res[l.edge]);
   }
   uint4 bits[R];                                   // made while the loads are under way
   if (d.on) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) bits[r] = philox((i0 >> 3) + (u64)(r * NTH + t), d);
+    for (int r = 0; r < R; ++r) bits[r] = philox(((i0 + l.first) >> 3) + (u64)(r * NTH + t), d);
   }
   F2 v[R][4], acc = f2(0.f, 0.f);
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int g = r * NTH + t, c = g * 8 - ph;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[r][j] = f2(0.f, 0.f);
-    if (g < runs) {
+    if (r * NTH + t < l.runs) {
       float u[8], b[8];
-      if (tail && g == runs - 1) {
-        seldom();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          u[j] = c + j >= 0 && c + j < cols ? to_f(x[8 * g + j]) : 0.f;
-          b[j] = res && c + j >= 0 && c + j < cols ? to_f(res[8 * g + j]) : 0.f;
-        }
-      } else {
-        unpack(raw[r], u);
-        if (res) unpack(rest[r], b);
-      }
+      unpack(raw[r], u);
+      if (res) unpack(rest[r], b);
       if (d.on) {
         if (res) {
 #pragma unroll
@@ -368,12 +364,6 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
 #pragma unroll
           for (int j = 0; j < 8; ++j) u[j] = kept(bits[r], j, d) ? u[j] * d.scale : 0.f;
         }
-      }
-      if (ragged<EDGE>(c, cols)) {
-        seldom();
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < 0 || c + j >= cols) u[j] = b[j] = 0.f;
       }
       pairs_of(u, v[r]);
       if (res && !d.on) {
@@ -386,60 +376,50 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
       for (int j = 0; j < 4; ++j) acc = add2(acc, v[r][j]);
     }
   }
+  if (EDGE && l.edge >= 0) {
+    if (!d.on) ev = er + ev;
+    else ev = res ? drop_one(ev, er, i0 + l.edge, d) : drop_one(ev, i0 + l.edge, d);
+  }
   float lo, hi;
   split(acc, lo, hi);
-  const float mean = walker_sum<NTH>(lo + hi, sh[0]) / (float)cols;
+  const float mean = walker_sum<NTH>(lo + hi + ev, sh[0]) / (float)cols;
   const F2 minus = f2(-mean, -mean);
   acc = f2(0.f, 0.f);
-  float edge = 0.f;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int g = r * NTH + t, c = g * 8 - ph;
-    if (g < runs) {
-      if (ragged<EDGE>(c, cols)) {
-        seldom();
-        float u[8];
-        floats_of(v[r], u);
+    if (r * NTH + t < l.runs) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j >= 0 && c + j < cols) edge = fmaf(u[j] - mean, u[j] - mean, edge);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const F2 z = add2(v[r][j], minus);
-          acc = fma2(z, z, acc);
-        }
+      for (int j = 0; j < 4; ++j) {
+        const F2 z = add2(v[r][j], minus);
+        acc = fma2(z, z, acc);
       }
     }
   }
   split(acc, lo, hi);
-  const float rstd = 1.f / sqrtf(walker_sum<NTH>(lo + hi + edge, sh[1]) / (float)cols + a.eps);
+  if (EDGE && l.edge >= 0) lo = fmaf(ev - mean, ev - mean, lo);
+  const float rstd = 1.f / sqrtf(walker_sum<NTH>(lo + hi, sh[1]) / (float)cols + a.eps);
   if (!live) return;
   T* const out = (T*)a.out + row * a.out_stride;
   T* const sum = a.sum ? (T*)a.sum + row * a.sum_stride : nullptr;
   const P* const weight = (const P*)a.weight;
   const P* const bias = (const P*)a.bias;
   const F2 scale = f2(rstd, rstd);
-  const bool even = (((uintptr_t)weight | (uintptr_t)bias) & 15) == 0;
+  const bool even = !EDGE && (((uintptr_t)weight | (uintptr_t)bias) & (8 * sizeof(P) - 1)) == 0;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int g = r * NTH + t, c = g * 8 - ph;
-    if (g < runs) {
+    const int g = r * NTH + t, c = l.first + 8 * g;
+    if (g < l.runs) {
       float u[8], p[8], q[8];
       if (sum) {
         floats_of(v[r], u);
-        put_run<EDGE>(sum, c, cols, u);
+        store_run(sum + c, u);
       }
-      if (even && !EDGE) {
+      if (even) {
         if (weight) unpack(load_run(weight + c), p);
         if (bias) unpack(load_run(bias + c), q);
-      } else if (even && c >= 0 && c + 16 <= cols) {     // the pieces read end within 15 elements
-        if (weight) shift_weights(weight, c, p);
-        if (bias) shift_weights(bias, c, q);
       } else {
-        seldom();
-        load_weights(weight, c, cols, 1.f, p);
-        load_weights(bias, c, cols, 0.f, q);
+        if (weight) load_weights(weight, c, cols, 1.f, p);
+        if (bias) load_weights(bias, c, cols, 0.f, q);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -449,8 +429,12 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
         else if (bias) z = add2(z, f2(q[2 * j], q[2 * j + 1]));
         split(z, u[2 * j], u[2 * j + 1]);
       }
-      put_run<EDGE>(out, c, cols, u);
+      store_run(out + c, u);
     }
+  }
+  if (EDGE && l.edge >= 0) {
+    if (sum) sum[l.edge] = from_f<T>(ev);
+    out[l.edge] = from_f<T>(fmaf((ev - mean) * rstd, weight ? to_f(weight[l.edge]) : 1.f, bias ? to_f(bias[l.edge]) : 0.f));
   }
   if (t == 0) {
     if (a.mean) a.mean[row] = mean;
@@ -484,63 +468,72 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
   const int cols = (int)a.cols;
   const Walker w = walker_of<NTH>(cols, blockIdx.x / nparts, gridDim.x / nparts);
   float (&sh)[2][2 * K][WARPS] = sh_all[w.slot];
-  const int ph = EDGE ? w.ph : 0;
-  const int all = (ph + cols + 7) >> 3;                          // runs of a row, and this part's first and number
-  const int g0 = CLUSTER ? (int)((long long)all * rank / nparts) : 0;
-  const int runs = CLUSTER ? (int)((long long)all * (rank + 1) / nparts) - g0 : all;
-  const int shift = ph - 8 * g0;                                 // column of run g: 8 g - shift
-  const T* const dout = (const T*)a.dout - shift;
-  const T* const s_in = (const T*)a.s - shift;
-  const T* const dsum = a.dsum ? (const T*)a.dsum - shift : nullptr;
+  const Lie l = lie_of<EDGE>(w.ph, cols, w.t);
+  const int g0 = CLUSTER ? (int)((long long)l.runs * rank / nparts) : 0;                  // this part's first run and their number
+  const int runs = CLUSTER ? (int)((long long)l.runs * (rank + 1) / nparts) - g0 : l.runs;
+  const int first = l.first + 8 * g0;
+  const int edge = rank == 0 ? l.edge : -1;                                               // the first part takes the edges
+  const T* const dout = (const T*)a.dout;
+  const T* const s_in = (const T*)a.s;
+  const T* const dsum = (const T*)a.dsum;
   const u32 ring32 = (u32)__cvta_generic_to_shared(ring);
   const float inv = 1.f / (float)cols;
   Held<P> wt[R];
   F2 dw[R][4], db[R][4];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    float o[8];
-    const int c = (r * NTH + w.t) * 8 - shift;
-    if (a.weight && (uintptr_t)a.weight % 16 == 0 && c >= 0 && c + 16 <= cols) shift_weights((const P*)a.weight, c, o);
-    else load_weights((const P*)a.weight, c, cols, 1.f, o);
+    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int g = r * NTH + w.t;
+    if (g < runs) load_weights((const P*)a.weight, first + 8 * g, cols, 1.f, o);
     wt[r].set(o);
 #pragma unroll
     for (int j = 0; j < 4; ++j) dw[r][j] = db[r][j] = f2(0.f, 0.f);
   }
+  const float ew = EDGE && edge >= 0 && a.weight ? to_f(((const P*)a.weight)[edge]) : 1.f;
+  float edw = 0.f, edb = 0.f;
   auto send = [&](long long row, int stage) {
     if (row < a.rows) {
       const u32 to = ring32 + (u32)(stage * ARRAYS * A * 16);
-      const bool last = EDGE && passes_end((u64)(row + 1) * cols, (u64)a.rows * cols);
-      const int left = last ? (int)((a.rows - row) * cols) + shift : 0;
-      send_runs<T, NTH, R, CTA>(to, dout + row * a.dout_stride, runs, w.t, last, left);
-      send_runs<T, NTH, R, CTA>(to + A * 16, s_in + row * a.s_stride, runs, w.t, last, left);
-      if (ARRAYS == 3) send_runs<T, NTH, R, CTA>(to + 2 * A * 16, dsum + row * a.dsum_stride, runs, w.t, last, left);
+      send_runs<T, NTH, R, CTA>(to, dout + row * a.dout_stride + first, runs, w.t);
+      send_runs<T, NTH, R, CTA>(to + A * 16, s_in + row * a.s_stride + first, runs, w.t);
+      if (ARRAYS == 3) send_runs<T, NTH, R, CTA>(to + 2 * A * 16, dsum + row * a.dsum_stride + first, runs, w.t);
     }
     copy_commit();
   };
 #pragma unroll
   for (int s = 0; s < S; ++s) send(w.row + s * w.step, s);
-  float mean[K], rstd[K];
+  // what comes through registers: statistics and edges of the rows next in turn
+  float mean[K], rstd[K], ny[K], ns[K], nd[K];
+  auto ask = [&](int k, long long row) {
+    if (row < a.rows) {
+      mean[k] = a.mean[row];
+      rstd[k] = a.rstd[row];
+      if (EDGE && edge >= 0) {
+        ny[k] = to_f(dout[row * a.dout_stride + edge]);
+        ns[k] = to_f(s_in[row * a.s_stride + edge]);
+        if (ARRAYS == 3) nd[k] = to_f(dsum[row * a.dsum_stride + edge]);
+      }
+    }
+  };
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const long long row = w.row + k * w.step;
-    mean[k] = row < a.rows ? a.mean[row] : 0.f;
-    rstd[k] = row < a.rows ? a.rstd[row] : 0.f;
+    mean[k] = rstd[k] = ny[k] = ns[k] = nd[k] = 0.f;
+    ask(k, w.row + k * w.step);
   }
   int stage = 0, parity = 0;
   // walkers of one warp go on together, also when the last ones have no row left
   for (long long row = w.row, lead = w.row - w.slot % (NTH < 32 ? 32 / NTH : 1); lead < a.rows; row += K * w.step, lead += K * w.step) {
-    float mu[K], rs[K], sums[2 * K];
+    float mu[K], rs[K], ey[K], es[K], ed[K], sums[2 * K];
     bool live[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       live[k] = row + k * w.step < a.rows;
       mu[k] = mean[k];
       rs[k] = rstd[k];
-      const long long next = row + (K + k) * w.step;
-      if (next < a.rows) {
-        mean[k] = a.mean[next];
-        rstd[k] = a.rstd[next];
-      }
+      ey[k] = ny[k];
+      es[k] = ns[k];
+      ed[k] = nd[k];
+      ask(k, row + (K + k) * w.step);
     }
     copy_wait<S - K>();
     warp_meets<T>();
@@ -551,20 +544,10 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
       const F2 mu2 = f2(-mu[k], -mu[k]), rs2 = f2(rs[k], rs[k]);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const int g = r * NTH + w.t, c = g * 8 - shift;
-        if (g < runs && live[k]) {
+        if (r * NTH + w.t < runs && live[k]) {
           float y[8], h[8], v[8];
           take_run<T, CTA>(at, r, y);
           take_run<T, CTA>(at + A, r, h);
-          if (ragged<EDGE>(c, cols)) {      // what belongs to other rows counts nothing
-            seldom();
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (c + j < 0 || c + j >= cols) {
-                y[j] = 0.f;
-                h[j] = mu[k];
-              }
-          }
           wt[r].get(v);
           F2 y2[4], h2[4], v2[4];
           pairs_of(y, y2);
@@ -586,6 +569,13 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
       sums[2 * k] += odd;
       split(q2, sums[2 * k + 1], odd);
       sums[2 * k + 1] += odd;
+      if (EDGE && edge >= 0 && live[k]) {
+        const float h = (es[k] - mu[k]) * rs[k], g = ey[k] * ew;
+        edw = fmaf(ey[k], h, edw);
+        edb += ey[k];
+        sums[2 * k] += g;
+        sums[2 * k + 1] = fmaf(g, h, sums[2 * k + 1]);
+      }
     }
 #pragma unroll
     for (int o = (NTH < 32 ? NTH : 32) / 2; o > 0; o >>= 1) {
@@ -631,11 +621,11 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
         T* const dr = a.dresidual ? (T*)a.dresidual + now * a.dresidual_stride : nullptr;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const int g = r * NTH + w.t, c = g * 8 - shift;
+          const int g = r * NTH + w.t, c = first + 8 * g;
           if (g < runs) {
             float y[8], h[8], v[8];
             uint4 bits;
-            if (d.on) bits = philox(((u64)now * (u64)cols >> 3) + (u64)(g0 + g), d);
+            if (d.on) bits = philox((((u64)now * (u64)cols + first) >> 3) + (u64)g, d);
             take_run<T, CTA>(at, r, y);
             take_run<T, CTA>(at + A, r, h);
             wt[r].get(v);
@@ -653,13 +643,19 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
               for (int j = 0; j < 4; ++j) y2[j] = add2(y2[j], v2[j]);
             }
             floats_of(y2, y);
-            if (dr) put_run<EDGE>(dr, c, cols, y);
+            if (dr) store_run(dr + c, y);
             if (d.on) {
 #pragma unroll
               for (int j = 0; j < 8; ++j) y[j] = kept(bits, j, d) ? y[j] * d.scale : 0.f;
             }
-            put_run<EDGE>(dx, c, cols, y);
+            store_run(dx + c, y);
           }
+        }
+        if (EDGE && edge >= 0) {
+          float y = fmaf(es[k] - mu[k], cq, (fmaf(ey[k], ew, -p)) * rs[k]);
+          if (ARRAYS == 3) y += ed[k];
+          if (dr) dr[edge] = from_f<T>(y);
+          dx[edge] = from_f<T>(d.on ? drop_one(y, (u64)now * (u64)cols + edge, d) : y);
         }
       }
     }
@@ -681,12 +677,16 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
       floats_of(db[r], v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int g = r * NTH + w.t, c = g * 8 - shift + j;
-        if (g < runs && c >= 0 && c < cols) {
+        const int g = r * NTH + w.t, c = first + 8 * g + j;
+        if (g < runs) {
           pw[c] = u[j];
           pb[c] = v[j];
         }
       }
+    }
+    if (EDGE && edge >= 0) {
+      pw[edge] = edw;
+      pb[edge] = edb;
     }
   } else {   // the CTA's walkers one after the other
     float* const acc = reinterpret_cast<float*>(ring);     // the ring is empty now
@@ -702,12 +702,16 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
           floats_of(db[r], v);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int g = r * NTH + w.t, c = g * 8 - shift + j;
-            if (g < runs && c >= 0 && c < cols) {
+            const int g = r * NTH + w.t, c = first + 8 * g + j;
+            if (g < runs) {
               acc[c] += u[j];
               acc[cols + c] += v[j];
             }
           }
+        }
+        if (EDGE && edge >= 0) {
+          acc[edge] += edw;
+          acc[cols + edge] += edb;
         }
       }
     }
@@ -924,7 +928,7 @@ int norm_t(const adacgd_norm_args& a, const Where& at) {
   k.look<T>(a.residual, a.residual_stride);
   k.look<T>(a.out, a.out_stride);
   k.look<T>(a.sum, a.sum_stride);
-  const long long n = (a.cols + (a.cols % 8 ? 14 : 0)) / 8;      // the most runs of a row
+  const long long n = a.cols / 8;      // the most runs of a row
   if (!k.good() || n > 4096) {
     static std::atomic<int> table[TRAIN_DEVICES];
     const int smem = (int)((a.cols + 3) / 4 * 16) + (a.drop.p > 0.0 ? bits_of((int)a.cols) : 0);
@@ -938,7 +942,7 @@ int norm_t(const adacgd_norm_args& a, const Where& at) {
     if (n <= 512) return norm_launch<T, P, 512, 1>(a, at);
     if (n <= 1024) return norm_launch<T, P, 1024, 1>(a, at);
   }
-  if (n <= 8) return norm_launch<T, P, 8, 1>(a, at);
+  if (n <= 8 && a.cols % 8 == 0) return norm_launch<T, P, 8, 1>(a, at);      // edges take sixteen threads
   if (n <= 16) return norm_launch<T, P, 16, 1>(a, at);
   if (n <= 32) return norm_launch<T, P, 32, 1>(a, at);
   if (n <= 64) return norm_launch<T, P, 32, 2>(a, at);
@@ -1003,7 +1007,7 @@ int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, i
 
 template <typename T, typename P, bool EDGE>
 int norm_bwd_by_width(const TrainScratch& s, const adacgd_norm_backward_args& a, long long n, const Where& at) {
-  if (n <= 8) return norm_bwd_launch<T, P, 8, 1, false, EDGE>(s, a, 1, at);
+  if (!EDGE && n <= 8) return norm_bwd_launch<T, P, 8, 1, false, false>(s, a, 1, at);      // edges take sixteen threads
   if (n <= 16) return norm_bwd_launch<T, P, 16, 1, false, EDGE>(s, a, 1, at);
   if (n <= 32) return norm_bwd_launch<T, P, 32, 1, false, EDGE>(s, a, 1, at);
   if (n <= 64) return norm_bwd_launch<T, P, 32, 2, false, EDGE>(s, a, 1, at);
@@ -1022,7 +1026,7 @@ int norm_bwd_t(const TrainScratch& s, const adacgd_norm_backward_args& a, const 
   k.look<T>(a.dsum, a.dsum_stride);
   k.look<T>(a.dx, a.dx_stride);
   k.look<T>(a.dresidual, a.dresidual_stride);
-  const long long n = (a.cols + (a.cols % 8 ? 14 : 0)) / 8;
+  const long long n = a.cols / 8;
   if (!k.good()) {
     int launched = 1;
     if (a.dweight || a.dbias) {
