@@ -498,9 +498,10 @@ __global__ void __launch_bounds__(Place<NTH, false>::CTA, Place<NTH, false>::CTA
                                                                             const float* __restrict__ zb, const float* __restrict__ sum,
                                                                             const float* __restrict__ top, u32 parts) {
   const Place<NTH, false> at;
-  const long long row = parts == 1 ? at.row : at.row / parts;
-  const int part = parts == 1 ? 0 : (int)(at.row - row * parts);
-  if (row >= a.rows.tokens) return;
+  const long long turn = parts == 1 ? at.row : at.row / parts;
+  const int part = parts == 1 ? 0 : (int)(at.row - turn * parts);
+  if (turn >= a.rows.tokens) return;
+  const long long row = a.rows.tokens - 1 - turn;      // backwards: the rows read last are still in the cache
   T* d = (T*)a.dlogits + row * a.dlogits_stride;
   const int vocab = (int)a.rows.vocab;
   const bool counts = !a.rows.mask || a.rows.mask[row];

@@ -459,6 +459,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
   extern __shared__ uint4 ring[];
   __shared__ float sh_all[W::ROWS][2][2 * K][WARPS];
   __shared__ float xch[2][8][2 * K];
+  asm volatile("griddepcontrol.launch_dependents;");     // the sum of the partials may take its place and wait
   int nparts = 1, rank = 0;
   if (CLUSTER) {
     nparts = (int)cg::this_cluster().num_blocks();
@@ -669,18 +670,18 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
   if (!part) return;
   float* const pw = part + 2ll * (blockIdx.x / nparts) * max_cols;
   float* const pb = pw + max_cols;
-  if (W::ROWS == 1) {
+  if (CLUSTER) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float u[8], v[8];
       floats_of(dw[r], u);
       floats_of(db[r], v);
+      const int g = r * NTH + w.t;
+      if (g < runs) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int g = r * NTH + w.t, c = first + 8 * g + j;
-        if (g < runs) {
-          pw[c] = u[j];
-          pb[c] = v[j];
+        for (int j = 0; j < 8; ++j) {
+          pw[first + 8 * g + j] = u[j];
+          pb[first + 8 * g + j] = v[j];
         }
       }
     }
@@ -688,38 +689,38 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
       pw[edge] = edw;
       pb[edge] = edb;
     }
-  } else {   // the CTA's walkers one after the other
-    float* const acc = reinterpret_cast<float*>(ring);     // the ring is empty now
+    return;
+  }
+  // The CTA's walkers one after the other, through shared memory (the ring is empty now): written from the registers, every
+  // store would touch a sector for four bytes of it.
+  float* const acc = reinterpret_cast<float*>(ring);
+  for (int k = 0; k < W::ROWS; ++k) {
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * cols; i += CTA) acc[i] = 0.f;
-    for (int k = 0; k < W::ROWS; ++k) {
-      __syncthreads();
-      if (w.slot == k) {
+    if (w.slot == k) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          float u[8], v[8];
-          floats_of(dw[r], u);
-          floats_of(db[r], v);
+      for (int r = 0; r < R; ++r) {
+        float u[8], v[8];
+        floats_of(dw[r], u);
+        floats_of(db[r], v);
+        const int g = r * NTH + w.t, c = first + 8 * g;
+        if (g < runs) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int g = r * NTH + w.t, c = first + 8 * g + j;
-            if (g < runs) {
-              acc[c] += u[j];
-              acc[cols + c] += v[j];
-            }
+            acc[c + j] = k ? acc[c + j] + u[j] : u[j];
+            acc[cols + c + j] = k ? acc[cols + c + j] + v[j] : v[j];
           }
         }
-        if (EDGE && edge >= 0) {
-          acc[edge] += edw;
-          acc[cols + edge] += edb;
-        }
+      }
+      if (EDGE && edge >= 0) {
+        acc[edge] = k ? acc[edge] + edw : edw;
+        acc[cols + edge] = k ? acc[cols + edge] + edb : edb;
       }
     }
-    __syncthreads();
-    for (int c = threadIdx.x; c < cols; c += CTA) {
-      pw[c] = acc[c];
-      pb[c] = acc[cols + c];
-    }
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < cols; c += CTA) {
+    pw[c] = acc[c];
+    pb[c] = acc[cols + c];
   }
 }
 
