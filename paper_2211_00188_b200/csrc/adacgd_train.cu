@@ -125,7 +125,7 @@ static size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 size_t train_scratch_bytes(long long max_tokens, long long max_cols) {
   const size_t n = (size_t)max_tokens;
-  return up256(NTRAIN_TICKETS * 4) + 5 * up256(n * 4) + up256((n + 1) * 4) + up256((n + 3) * 8) +
+  return up256(NTRAIN_TICKETS * 4) + 3 * up256(n * 4) + up256((n + 1) * 4) + up256((n + 3) * 8) + up256(3ull * MAX_SMALL_CTAS * 8) +
          up256((size_t)NORM_PARTS * 2 * (size_t)max_cols * 4);
 }
 
@@ -134,13 +134,12 @@ void carve_train_scratch(TrainScratch* s, void* base, long long max_tokens, long
   const size_t n = (size_t)max_tokens;
   auto take = [&](size_t bytes) { char* p = b; b += up256(bytes); return p; };
   s->tickets = (u32*)take(NTRAIN_TICKETS * 4);
-  s->logp = (float*)take(n * 4);
-  s->lse = (float*)take(n * 4);
   s->tok_a = (float*)take(n * 4);
   s->tok_b = (float*)take(n * 4);
   s->tok_c = (float*)take(n * 4);
   s->seq = (float*)take((n + 1) * 4);
   s->part = (double*)take((n + 3) * 8);
+  s->own = (double*)take(3ull * MAX_SMALL_CTAS * 8);
   s->norm_part = (float*)take((size_t)NORM_PARTS * 2 * (size_t)max_cols * 4);
   s->max_tokens = max_tokens;
   s->max_cols = max_cols;

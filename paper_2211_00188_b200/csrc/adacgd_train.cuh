@@ -17,17 +17,17 @@ constexpr int NORM_PARTS = 592;  // most partial rows of a weight gradient: four
 // The context's workspace, carved by carve_train_scratch.
 struct TrainScratch {
   u32* tickets;    // [NTRAIN_TICKETS] completion counts, zero between calls
-  float* logp;     // [tokens] log-probabilities (where the caller wants none)
-  float* lse;      // [tokens] log of the sum of exponentials
   float* tok_a;    // [tokens] a token's weighted loss
   float* tok_b;    // [tokens] its KL estimate
   float* tok_c;    // [tokens] 1 where the clipped term has taken the gradient
   float* seq;      // [tokens + 1] per sequence: weight or gradient coefficient; the last is the total
   double* part;    // [tokens + 3] per pair: loss; per CTA of the token sums: three of them
+  double* own;     // [3][MAX_SMALL_CTAS] sums of the CTAs of a small policy loss
   float* norm_part; // [NORM_PARTS][2][max_cols] partial weight and bias gradients
   long long max_tokens, max_cols;
 };
 constexpr int NTRAIN_TICKETS = 64;
+constexpr int MAX_SMALL_CTAS = 2048 * 8;   // 2048 rows in clusters of at most eight
 
 // Where a call runs.
 struct Where {
@@ -235,7 +235,6 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 constexpr float LOG2E = 1.4426950408889634f;
-__device__ __forceinline__ float exp_fast(float x) { return ex2(x * LOG2E); }
 
 // The first token of sequence q and the one behind its last, cut off at the ends of the batch.
 __device__ __forceinline__ void seq_bounds(const int32_t* start, long long q, long long tokens, long long each,

@@ -63,13 +63,6 @@ __device__ __forceinline__ float log2_rel(float z, float m) {
   return plain_range(m) ? fmaf(z, LOG2E, -(m * LOG2E)) : (z - base_of(m)) * LOG2E;
 }
 
-__device__ __forceinline__ Soft join(Soft a, Soft b) {
-  Soft r;
-  r.m = fmaxf(a.m, b.m);
-  r.s = a.s * rel(a.m, r.m) + b.s * rel(b.m, r.m);
-  return r;
-}
-
 __device__ __forceinline__ long long label_at(const adacgd_token_rows& r, long long t) {
   return r.label_bytes == 8 ? (long long)((const int64_t*)r.labels)[t] : (long long)((const int32_t*)r.labels)[t];
 }
@@ -92,7 +85,8 @@ __device__ __forceinline__ Cut cut_row(const T* row, int vocab, int part, int pa
   c.end = part == parts - 1 ? vocab : head + 8 * r1;
   return c;
 }
-// Element of the ragged ends that thread t handles, or -1.
+// Element number t of the ragged ends, or -1.  Fourteen at most, so a thread handles EDGES of them: numbers t, t + NTH.
+template <int NTH> constexpr int EDGES = NTH < 14 ? 2 : 1;
 __device__ __forceinline__ int edge_of(const Cut& c, int t) {
   const int head = c.first - c.begin, tail0 = c.first + 8 * c.runs;
   if (t < head) return c.begin + t;
@@ -174,10 +168,13 @@ __device__ __forceinline__ Soft thread_soft(const T* row, const Cut& c, int t) {
   };
   Batch<T> b0, b1;
   if (whole > 0) load_batch<T, NTH, false>(b0, p);
-  const int e = edge_of(c, t);
-  if (e >= 0) {
-    float x[1] = {to_f(row[e])};
-    absorb(a, x);
+#pragma unroll
+  for (int k = 0; k < EDGES<NTH>; ++k) {
+    const int e = edge_of(c, t + k * NTH);
+    if (e >= 0) {
+      float x[1] = {to_f(row[e])};
+      absorb(a, x);
+    }
   }
   int k = 0;
   for (; k + 2 <= whole; k += 2) {           // two batches take turns: no copies between registers
@@ -213,18 +210,25 @@ __device__ __forceinline__ void row_begin() {
   if (CLUSTER) cg::this_cluster().barrier_arrive();
 }
 
-// The statistics of the row's threads joined, the same bits in each: a warp, a CTA or a cluster.
+// The lanes of a warp that share a row; the others may have another one, or none.
+template <int NTH>
+__device__ __forceinline__ u32 row_lanes() {
+  return NTH >= 32 ? 0xffffffffu : ((1u << (NTH & 31)) - 1u) << (threadIdx.x & 31 & ~(NTH - 1));
+}
+// The statistics of the row's threads joined, the same bits in each: lanes of a warp, a CTA or a cluster.
 template <int NTH, bool CLUSTER>
 __device__ __forceinline__ Soft row_soft(Soft a, Soft* sh, Soft* xch) {
   // maxima first, then the sums against the largest: one exponential instead of two a step
+  constexpr int HALF = (NTH < 32 ? NTH : 32) / 2;
+  const u32 lanes = row_lanes<NTH>();
   const float mine = a.m;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xffffffffu, a.m, o));
+  for (int o = HALF; o > 0; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(lanes, a.m, o));
   a.s *= rel(mine, a.m);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
-  if (NTH == 32) {
-    __syncwarp();   // what the lanes have read of the row they may now write
+  for (int o = HALF; o > 0; o >>= 1) a.s += __shfl_xor_sync(lanes, a.s, o);
+  if (NTH <= 32) {
+    __syncwarp(lanes);   // what the lanes have read of the row they may now write
     return a;
   }
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = a;
@@ -262,8 +266,13 @@ __device__ __forceinline__ void thread_grad(const T* row, T* d, const Cut& c, in
                                             float sum) {
   constexpr int U = Batch<T>::U;
   const float neg = -coef / sum;
-  const int e = edge_of(c, t);
-  const float edge = e >= 0 ? to_f(row[e]) : 0.f;
+  int e[EDGES<NTH>];
+  float edge[EDGES<NTH>];
+#pragma unroll
+  for (int k = 0; k < EDGES<NTH>; ++k) {
+    e[k] = edge_of(c, t + k * NTH);
+    edge[k] = e[k] >= 0 ? to_f(row[e[k]]) : 0.f;
+  }
   const T* p = row + c.first + 8 * t;
   T* q = d + c.first + 8 * t;
   int r = t;                                 // this thread's next run
@@ -319,22 +328,30 @@ __device__ __forceinline__ void thread_grad(const T* row, T* d, const Cut& c, in
       }
     }
   }
-  if (e >= 0) {
-    float x[1] = {edge};
-    exp_all(x, m);
-    d[e] = from_f<T>(neg * x[0]);
+#pragma unroll
+  for (int k = 0; k < EDGES<NTH>; ++k) {
+    if (e[k] >= 0) {
+      float x[1] = {edge[k]};
+      exp_all(x, m);
+      d[e[k]] = from_f<T>(neg * x[0]);
+    }
   }
   if (label >= c.begin && label < c.end) {
     const int in = label - c.first;
-    const bool mine = in >= 0 && in < 8 * c.runs ? (in >> 3) % NTH == t : label == e;
+    bool mine = in >= 0 && in < 8 * c.runs && (in >> 3) % NTH == t;
+#pragma unroll
+    for (int k = 0; k < EDGES<NTH>; ++k) mine = mine || label == e[k];
     if (mine) d[label] = from_f<T>(fmaf(neg, ex2(tz), coef));
   }
 }
 template <typename T, int NTH>
 __device__ __forceinline__ void thread_zero(T* d, const Cut& c, int t) {   // c cut by the gradient's own alignment
   const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  const int e = edge_of(c, t);
-  if (e >= 0) d[e] = from_f<T>(0.f);
+#pragma unroll
+  for (int k = 0; k < EDGES<NTH>; ++k) {
+    const int e = edge_of(c, t + k * NTH);
+    if (e >= 0) d[e] = from_f<T>(0.f);
+  }
   for (int r = t; r < c.runs; r += NTH) store_run(d + c.first + 8ll * r, z);
 }
 template <typename T>
@@ -350,14 +367,14 @@ template <int NTH, bool CLUSTER> struct Place {
   long long row;
   int t, part, parts;
   __device__ __forceinline__ Place() {
-    t = NTH == 32 ? (int)(threadIdx.x & 31) : (int)threadIdx.x;
+    t = NTH < 128 ? (int)threadIdx.x % NTH : (int)threadIdx.x;
     part = 0;
     parts = 1;
     if (CLUSTER) {
       part = (int)cg::this_cluster().block_rank();
       parts = (int)cg::this_cluster().num_blocks();
     }
-    row = (long long)(blockIdx.x / parts) * ROWS + (NTH == 32 ? threadIdx.x >> 5 : 0);
+    row = (long long)(blockIdx.x / parts) * ROWS + (NTH < 128 ? threadIdx.x / NTH : 0);
   }
 };
 
@@ -374,7 +391,7 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
   pdl_trigger();
   const Place<NTH, CLUSTER> at;
   const long long row = at.row;
-  if (row >= r.tokens) return;       // whole warps; only where NTH == 32
+  if (row >= r.tokens) return;       // all of the row's lanes; only where NTH <= 32
   const bool counts = !r.mask || r.mask[row];      // fetched together with the label, not one after the other
   const long long y = label_at(r, row);
   const int vocab = (int)r.vocab;
@@ -434,60 +451,96 @@ __device__ __forceinline__ bool last_to_arrive(u32* ticket, u32 n) {
 // --------------------------------------------------------------------------
 constexpr int PAIR_NT = 256;
 
-// One CTA a pair: margin, loss and the coefficients of the pair's two sequences; the last CTA takes the mean.
+// A pair's margin, loss and the coefficients of its two sequences, from the sums of log-probabilities, of their differences to the
+// reference and of counted tokens over the preferred ([0]) and the rejected ([1]) answer.
+__device__ __forceinline__ double finish_pair(const adacgd_preference_args& a, long long p, long long pairs, const double (&total)[2],
+                                              const double (&diff)[2], const double (&cnt)[2], float* __restrict__ coef) {
+  double d[2], inv[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    inv[k] = a.length_normalized && cnt[k] > 0.0 ? 1.0 / cnt[k] : 1.0;
+    d[k] = diff[k] * inv[k];
+    if (a.seq_logp) a.seq_logp[p + k * pairs] = (float)(total[k] * inv[k]);
+  }
+  const double beta = (double)a.beta, h = beta * (d[0] - d[1]), e = (double)a.label_smoothing;
+  double l, g;
+  if (a.kind == ADACGD_PREF_SIGMOID) {
+    const double tail = log1p(exp(-fabs(h)));               // -log sigma(|h|)
+    l = (1.0 - e) * (tail + fmax(-h, 0.0)) + e * (tail + fmax(h, 0.0));
+    const double sg = 1.0 / (1.0 + exp(-h)), sn = 1.0 / (1.0 + exp(h));
+    g = e * sg - (1.0 - e) * sn;
+    if (h != h) l = h;
+  } else if (a.kind == ADACGD_PREF_HINGE) {
+    l = h < 1.0 ? 1.0 - h : (h != h ? h : 0.0);
+    g = h < 1.0 ? -1.0 : (h != h ? h : 0.0);
+  } else {
+    const double u = h / beta - 0.5 / beta;
+    l = u * u;
+    g = 2.0 * u / beta;
+  }
+  const double c = (double)a.grad_scale * g * beta / (double)pairs;
+  coef[p] = (float)(c * inv[0]);
+  coef[p + pairs] = (float)(-c * inv[1]);
+  if (a.margin) a.margin[p] = (float)h;
+  return l;
+}
+
+// `slices` CTAs a pair.  One: it also finishes the pair, and the last CTA of all takes the mean of the losses.  More: the last CTA
+// adds the slices' six sums of each pair and finishes the pairs.
 __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, const float* __restrict__ zb, const float* __restrict__ sum,
-                                                   float* __restrict__ coef, double* __restrict__ part, u32* ticket) {
+                                                   float* __restrict__ coef, double* __restrict__ part, u32 slices, u32* ticket) {
   __shared__ double sh[PAIR_NT / 32];
   pdl_wait();
   pdl_trigger();   // the gradient kernel is large: it is let in when this one has its operands
   const long long pairs = a.rows.sequences / 2, each = a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences;
-  const long long p = blockIdx.x;
-  double d[2], inv[2];
+  const long long p = blockIdx.x / slices, slice = blockIdx.x - p * slices;
+  double total[2], diff[2], cnt[2];
+#pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const long long q = p + k * pairs;
     long long lo, hi;
-    seq_bounds(a.rows.seq_start, q, a.rows.tokens, each, &lo, &hi);
-    double total = 0.0, diff = 0.0, cnt = 0.0;
-    for (long long t = lo + threadIdx.x; t < hi; t += PAIR_NT) {
+    seq_bounds(a.rows.seq_start, p + k * pairs, a.rows.tokens, each, &lo, &hi);
+    total[k] = diff[k] = cnt[k] = 0.0;
+    for (long long t = lo + slice * PAIR_NT + threadIdx.x; t < hi; t += (long long)slices * PAIR_NT) {
       if (a.rows.mask && !a.rows.mask[t]) continue;
       const double logp = ((double)zb[t] - log2((double)sum[t])) * 0.6931471805599453;
-      cnt += 1.0;
-      total += logp;
-      diff += logp - (double)a.ref_logp[t];
+      cnt[k] += 1.0;
+      total[k] += logp;
+      diff[k] += logp - (double)a.ref_logp[t];
     }
-    total = block_sum_f64<PAIR_NT>(total, sh);
-    diff = block_sum_f64<PAIR_NT>(diff, sh);
-    cnt = block_sum_f64<PAIR_NT>(cnt, sh);
-    inv[k] = a.length_normalized && cnt > 0.0 ? 1.0 / cnt : 1.0;
-    d[k] = diff * inv[k];
-    if (threadIdx.x == 0 && a.seq_logp) a.seq_logp[q] = (float)(total * inv[k]);
+    total[k] = block_sum_f64<PAIR_NT>(total[k], sh);
+    diff[k] = block_sum_f64<PAIR_NT>(diff[k], sh);
+    cnt[k] = block_sum_f64<PAIR_NT>(cnt[k], sh);
   }
   if (threadIdx.x == 0) {
-    const double beta = (double)a.beta, h = beta * (d[0] - d[1]), e = (double)a.label_smoothing;
-    double l, g;
-    if (a.kind == ADACGD_PREF_SIGMOID) {
-      const double tail = log1p(exp(-fabs(h)));               // -log sigma(|h|)
-      l = (1.0 - e) * (tail + fmax(-h, 0.0)) + e * (tail + fmax(h, 0.0));
-      const double sg = 1.0 / (1.0 + exp(-h)), sn = 1.0 / (1.0 + exp(h));
-      g = e * sg - (1.0 - e) * sn;
-      if (h != h) l = h;
-    } else if (a.kind == ADACGD_PREF_HINGE) {
-      l = h < 1.0 ? 1.0 - h : (h != h ? h : 0.0);
-      g = h < 1.0 ? -1.0 : (h != h ? h : 0.0);
+    if (slices == 1) {
+      part[p] = finish_pair(a, p, pairs, total, diff, cnt, coef);
     } else {
-      const double u = h / beta - 0.5 / beta;
-      l = u * u;
-      g = 2.0 * u / beta;
+      double* const q = part + 6ll * blockIdx.x;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        q[k] = total[k];
+        q[2 + k] = diff[k];
+        q[4 + k] = cnt[k];
+      }
     }
-    const double c = (double)a.grad_scale * g * beta / (double)pairs;
-    coef[p] = (float)(c * inv[0]);
-    coef[p + pairs] = (float)(-c * inv[1]);
-    if (a.margin) a.margin[p] = (float)h;
-    part[p] = l;
   }
-  if (!last_to_arrive(ticket, (u32)pairs)) return;
+  if (!last_to_arrive(ticket, gridDim.x)) return;
   double v = 0.0;
-  for (long long q = threadIdx.x; q < pairs; q += PAIR_NT) v += __ldcg(&part[q]);
+  for (long long q = threadIdx.x; q < pairs; q += PAIR_NT) {
+    if (slices == 1) {
+      v += __ldcg(&part[q]);
+      continue;
+    }
+    double s[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
+    for (u32 k = 0; k < slices; ++k) {
+#pragma unroll
+      for (int i = 0; i < 6; ++i) s[i] += __ldcg(&part[6 * (q * slices + k) + i]);
+    }
+    total[0] = s[0]; total[1] = s[1];
+    diff[0] = s[2]; diff[1] = s[3];
+    cnt[0] = s[4]; cnt[1] = s[5];
+    v += finish_pair(a, q, pairs, total, diff, cnt, coef);
+  }
   v = block_sum_f64<PAIR_NT>(v, sh);
   if (threadIdx.x == 0) *a.loss = (float)(v / (double)pairs);
 }
@@ -586,49 +639,125 @@ __device__ __forceinline__ void write_policy(float* loss, float* stats, double l
   }
 }
 
+// Counted tokens among `n`, a share of them for each of NTH threads.
+template <int NTH>
+__device__ __forceinline__ int count_share(const uint8_t* mask, int n, int t) {
+  int c = 0;
+  if (((uintptr_t)mask & 15) == 0) {
+    for (int i = t * 16; i + 16 <= n; i += NTH * 16) {
+      const uint4 v = *reinterpret_cast<const uint4*>(mask + i);
+      const u32 w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        u32 x = w[k];             // the lowest bit of each byte becomes the disjunction of its eight
+        x |= x >> 4;
+        x |= x >> 2;
+        x |= x >> 1;
+        c += __popc(x & 0x01010101u);
+      }
+    }
+    const int rest = n / 16 * 16 + t;
+    if (t < 16 && rest < n) c += mask[rest] != 0;
+  } else {
+    for (int i = t; i < n; i += NTH) c += mask[i] != 0;
+  }
+  return c;
+}
+
 // A row's loss and, from the cache, its gradient.
-template <typename T, int NTH, bool CLUSTER>
+// SMALL (few tokens, where a launch costs more than the work it saves): the CTAs' sums are added by the last one, and without
+// `weight` every row counts the tokens itself; otherwise a kernel before gives the weights and one behind takes the sums.
+constexpr long long SMALL_TOKENS = 2048;
+template <typename T, int NTH, bool CLUSTER, bool SMALL>
 __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>::CTAS) k_policy(adacgd_policy_args a, const float* __restrict__ weight, float* tl,
-                                                                     float* tk, float* tc) {
+                                                                     float* tk, float* tc, double* own, u32* ticket) {
+  constexpr int CTA = Place<NTH, CLUSTER>::CTA, ROWS = Place<NTH, CLUSTER>::ROWS;
   __shared__ Soft sh[32], xch[8];
+  __shared__ int counted[32];
+  __shared__ double mine[3][ROWS];
   pdl_trigger();
   const Place<NTH, CLUSTER> at;
   const long long row = at.row;
-  if (row >= a.rows.tokens) return;       // whole warps; only where NTH == 32
-  const int vocab = (int)a.rows.vocab;
+  if (!SMALL && row >= a.rows.tokens) return;       // all of the row's lanes; only where NTH <= 32
+  const int vocab = (int)a.rows.vocab, slot = NTH < 128 ? threadIdx.x / NTH : 0;
+  const bool here = row < a.rows.tokens;
   // fetched together, not one after the other
-  const bool counts = !a.rows.mask || a.rows.mask[row];
-  const long long y = label_at(a.rows, row);
-  const float A = a.advantages[row], old = a.old_logp[row], ref = a.ref_logp ? a.ref_logp[row] : 0.f;
+  const bool counts = here && (!a.rows.mask || a.rows.mask[row]);
+  const long long y = here ? label_at(a.rows, row) : -1;
+  const float A = here ? a.advantages[row] : 0.f, old = here ? a.old_logp[row] : 0.f, ref = here && a.ref_logp ? a.ref_logp[row] : 0.f;
   T* d = a.dlogits ? (T*)a.dlogits + row * a.dlogits_stride : nullptr;
+  int total = 0;
+  if (SMALL && !weight) {
+    total = (int)a.rows.tokens;
+    if (a.rows.mask) {
+      int c = count_share<NTH>(a.rows.mask, total, at.t);
+#pragma unroll
+      for (int o = (NTH < 32 ? NTH : 32) / 2; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+      total = c;
+      if (NTH > 32) {
+        if ((threadIdx.x & 31) == 0) counted[threadIdx.x >> 5] = c;
+        __syncthreads();
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < NTH / 32; ++w) total += counted[w];
+      }
+    }
+  }
+  if (SMALL && at.t == 0) mine[0][slot] = mine[1][slot] = mine[2][slot] = 0.0;
   if (!counts) {
-    if (at.t == 0 && at.part == 0) {
-      tl[row] = tk[row] = tc[row] = 0.f;
+    if (here && at.t == 0 && at.part == 0) {
+      if (!SMALL) tl[row] = tk[row] = tc[row] = 0.f;
       if (a.logp) a.logp[row] = 0.f;
     }
-    if (d) thread_zero<T, NTH>(d, cut_row(d, vocab, at.part, at.parts), at.t);
+    if (here && d) thread_zero<T, NTH>(d, cut_row(d, vocab, at.part, at.parts), at.t);
     pdl_wait();
-    return;
+    if (!SMALL) return;
+  } else {
+    row_begin<CLUSTER>();
+    const T* x = (const T*)a.rows.logits + row * a.rows.logits_stride;
+    const int label = y >= 0 && y < vocab ? (int)y : -1;
+    const float z = label >= 0 ? to_f(x[label]) : NAN;
+    const Cut cut = cut_row(x, vocab, at.part, at.parts);
+    const Soft v = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut, at.t), sh, xch);
+    const float tz = log2_rel(z, v.m), logp = (tz - log2f(v.s)) * LN2;
+    // the same weight for all, or the sequence's
+    const long long q = a.per_sequence ? seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences) : 0;
+    pdl_wait();
+    const float w = SMALL && !weight ? (float)(1.0 / (double)total) : weight[q];
+    const Token tok = token_loss(logp, old, A, a.ref_logp != nullptr, ref, a.clip_low, a.clip_high, a.kl_beta);
+    if (at.t == 0 && at.part == 0) {
+      if (a.logp) a.logp[row] = logp;
+      if (SMALL) {
+        mine[0][slot] = (double)(w * tok.loss);
+        mine[1][slot] = (double)tok.kl;
+        mine[2][slot] = tok.clipped ? 1.0 : 0.0;
+      } else {
+        tl[row] = w * tok.loss;
+        tk[row] = tok.kl;
+        tc[row] = tok.clipped ? 1.f : 0.f;
+      }
+    }
+    if (d) thread_grad<T, NTH, true>(x, d, cut, at.t, same_phase(x, d), label, tz, a.grad_scale * (w * tok.slope), v.m, v.s);
   }
-  row_begin<CLUSTER>();
-  const T* x = (const T*)a.rows.logits + row * a.rows.logits_stride;
-  const int label = y >= 0 && y < vocab ? (int)y : -1;
-  const float z = label >= 0 ? to_f(x[label]) : NAN;
-  const Cut cut = cut_row(x, vocab, at.part, at.parts);
-  const Soft v = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut, at.t), sh, xch);
-  const float tz = log2_rel(z, v.m), logp = (tz - log2f(v.s)) * LN2;
-  // the same weight for all, or the sequence's
-  const long long q = a.per_sequence ? seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences) : 0;
-  pdl_wait();
-  const float w = weight[q];
-  const Token tok = token_loss(logp, old, A, a.ref_logp != nullptr, ref, a.clip_low, a.clip_high, a.kl_beta);
-  if (at.t == 0 && at.part == 0) {
-    if (a.logp) a.logp[row] = logp;
-    tl[row] = w * tok.loss;
-    tk[row] = tok.kl;
-    tc[row] = tok.clipped ? 1.f : 0.f;
+  if (!SMALL) return;
+  __syncthreads();
+  if (threadIdx.x < 3) {
+    double v = 0.0;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) v += mine[threadIdx.x][r];
+    own[3ll * blockIdx.x + threadIdx.x] = v;
   }
-  if (d) thread_grad<T, NTH, true>(x, d, cut, at.t, same_phase(x, d), label, tz, a.grad_scale * (w * tok.slope), v.m, v.s);
+  if (!last_to_arrive(ticket, gridDim.x)) return;
+  __shared__ double shd[CTA / 32];
+  double v[3] = {0.0, 0.0, 0.0};
+#pragma unroll 4
+  for (u32 k = threadIdx.x; k < gridDim.x; k += CTA) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) v[i] += __ldcg(&own[3ll * k + i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 3; ++i) v[i] = block_sum_f64<CTA>(v[i], shd);
+  if (threadIdx.x == 0) write_policy(a.loss, a.stats, v[0], v[1], v[2], weight ? (double)weight[a.rows.sequences] : (double)total);
 }
 
 // The sums over tokens, in a fixed order: a CTA takes SUM_ROWS of them, the last one adds the CTAs'.
@@ -698,15 +827,15 @@ unsigned ctas(long long rows, int rows_per_cta, int cluster) {
 struct Split { int threads, cluster; };
 Split split_of(long long rows, long long vocab, int threads, const Where& at) {
   Split s = {threads, 1};
-  while (s.threads < 512 && rows * s.threads < 1024ll * at.sms && vocab > 8 * s.threads) s.threads *= 4;
+  while (s.threads < 512 && rows * s.threads < 1024ll * at.sms && vocab > 8 * s.threads) s.threads = s.threads < 32 ? 32 : s.threads * 4;
   if (s.threads >= 512)
     while (s.cluster < 8 && rows * s.cluster * 2 <= 2 * at.sms && vocab / (s.cluster * 2) >= 4096) s.cluster *= 2;
   if (s.threads > 512 && s.cluster > 1) s.threads = 512;
   return s;
 }
 // One pass: a row's two reductions cost about what 128 elements a thread do, and many rows on an SM hide them.
-Split split_once(long long rows, long long vocab, const Where& at) {
-  return split_of(rows, vocab, vocab <= 8192 ? 32 : (vocab <= 65536 ? 128 : 512), at);
+Split split_once(long long rows, long long vocab, int size, const Where& at) {
+  return split_of(rows, vocab, vocab * size <= 4096 ? 8 : vocab <= 8192 ? 32 : (vocab <= 65536 ? 128 : 512), at);
 }
 // Two passes, the second from the cache: what the resident threads hold between their passes (1024 an SM) has to stay in it beside
 // what is written, so a thread may have 400 bytes of a row, and 640 where more threads a row cost more than the cache gives.
@@ -715,7 +844,7 @@ Split split_once(long long rows, long long vocab, const Where& at) {
 constexpr int PASS_BYTES = 400, PASS_BYTES_WIDE = 640;
 Split split_twice(long long rows, long long vocab, int size, const Where& at) {
   const long long bytes = vocab * size;
-  return split_of(rows, vocab, bytes <= 32 * PASS_BYTES ? 32 : bytes <= 128 * PASS_BYTES ? 128 : bytes <= 256 * PASS_BYTES ? 256 : bytes <= 512 * PASS_BYTES_WIDE ? 512 : 1024, at);
+  return split_of(rows, vocab, bytes <= 8 * PASS_BYTES ? 8 : bytes <= 32 * PASS_BYTES ? 32 : bytes <= 128 * PASS_BYTES ? 128 : bytes <= 256 * PASS_BYTES ? 256 : bytes <= 512 * PASS_BYTES_WIDE ? 512 : 1024, at);
 }
 #define BY_SPLIT(s, call)                                                                              \
   (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())         \
@@ -723,16 +852,18 @@ Split split_twice(long long rows, long long vocab, int size, const Where& at) {
    : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }())   \
    : s.threads == 256 ? ([&] { constexpr int NTH = 256; constexpr bool CL = false; return call; }())   \
    : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }())   \
-                      : ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }()))
+   : s.threads == 32 ? ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }())     \
+                     : ([&] { constexpr int NTH = 8; constexpr bool CL = false; return call; }()))
 #define BY_SPLIT_ONCE(s, call)                                                                         \
   (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())         \
    : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }())   \
    : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }())   \
-                      : ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }()))
+   : s.threads == 32 ? ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }())     \
+                     : ([&] { constexpr int NTH = 8; constexpr bool CL = false; return call; }()))
 
 template <typename T>
 cudaError_t logp_t(const adacgd_token_rows& r, float* logp, float* lse, float* zb, float* sum, float* top, const Where& at) {
-  const Split s = split_once(r.tokens, r.vocab, at);
+  const Split s = split_once(r.tokens, r.vocab, (int)sizeof(T), at);
   return BY_SPLIT_ONCE(s, (launch(k_logp<T, NTH, CL>, ctas(r.tokens, Place<NTH, CL>::ROWS, s.cluster), Place<NTH, CL>::CTA, s.cluster, false,
                              at.stream, 0, r, logp, lse, zb, sum, top)));
 }
@@ -745,11 +876,16 @@ int preference_t(const TrainScratch& s, const adacgd_preference_args& a, const W
     if (logp_t<T>(a.rows, nullptr, nullptr, s.tok_a, s.tok_b, s.tok_c, at) != cudaSuccess) return -1;
     ++n;
   }
-  if (launch(k_pairs, (unsigned)(a.rows.sequences / 2), PAIR_NT, 1, rows > 0, at.stream, 0, a, s.tok_a, s.tok_b, s.seq, s.part,
+  // Slices of at least two tokens a thread, as long as SMs are free.  The six sums of each fit: 6 pairs slices <= 6 tokens / 1024.
+  const long long pairs = a.rows.sequences / 2;
+  long long slices = rows / a.rows.sequences / (2 * PAIR_NT);
+  if (slices * pairs > at.sms) slices = at.sms / pairs;
+  if (slices < 1) slices = 1;
+  if (launch(k_pairs, (unsigned)(pairs * slices), PAIR_NT, 1, rows > 0, at.stream, 0, a, s.tok_a, s.tok_b, s.seq, s.part, (u32)slices,
              s.tickets) != cudaSuccess)
     return -1;
   if (a.dlogits && rows) {
-    Split sp = split_once(rows, a.rows.vocab, at);
+    Split sp = split_once(rows, a.rows.vocab, (int)sizeof(T), at);
     const u32 parts = (u32)sp.cluster;      // no reduction: parts of a row need no cluster
     sp.cluster = 1;
     const cudaError_t e = BY_SPLIT_ONCE(sp, (launch(k_preference_grad<T, NTH>, ctas(rows * parts, Place<NTH, false>::ROWS, 1), Place<NTH, false>::CTA,
@@ -762,11 +898,23 @@ int preference_t(const TrainScratch& s, const adacgd_preference_args& a, const W
 
 template <typename T>
 int policy_t(const TrainScratch& s, const adacgd_policy_args& a, const Where& at) {
-  if (launch(k_policy_weights, 1u, 1024, 1, false, at.stream, 0, a, s.seq) != cudaSuccess) return -1;
-  if (!a.rows.tokens) return 1;
+  const bool small = a.rows.tokens > 0 && a.rows.tokens <= SMALL_TOKENS;
+  int n = 1;
+  if (!small || a.per_sequence) {
+    if (launch(k_policy_weights, 1u, 1024, 1, false, at.stream, 0, a, s.seq) != cudaSuccess) return -1;
+    if (!a.rows.tokens) return 1;
+    n = 2;
+  }
   const Split sp = split_twice(a.rows.tokens, a.rows.vocab, (int)sizeof(T), at);
-  cudaError_t e = BY_SPLIT(sp, (launch(k_policy<T, NTH, CL>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, sp.cluster), Place<NTH, CL>::CTA, sp.cluster,
-                                       true, at.stream, 0, a, s.seq, s.tok_a, s.tok_b, s.tok_c)));
+  if (small) {
+    const float* weight = a.per_sequence ? s.seq : nullptr;
+    return BY_SPLIT(sp, (launch(k_policy<T, NTH, CL, true>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, sp.cluster), Place<NTH, CL>::CTA, sp.cluster,
+                                a.per_sequence != 0, at.stream, 0, a, weight, s.tok_a, s.tok_b, s.tok_c, s.own, s.tickets + 1))) == cudaSuccess
+               ? n
+               : -1;
+  }
+  cudaError_t e = BY_SPLIT(sp, (launch(k_policy<T, NTH, CL, false>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, sp.cluster), Place<NTH, CL>::CTA, sp.cluster,
+                                       true, at.stream, 0, a, s.seq, s.tok_a, s.tok_b, s.tok_c, s.own, s.tickets + 1)));
   if (e == cudaSuccess)
     e = launch(k_policy_sum, (unsigned)((a.rows.tokens + SUM_ROWS - 1) / SUM_ROWS), SUM_NT, 1, true, at.stream, 0, a, s.seq, s.tok_a, s.tok_b,
                s.tok_c, s.part, s.tickets + 1);

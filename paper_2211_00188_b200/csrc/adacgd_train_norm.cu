@@ -930,7 +930,7 @@ int norm_t(const adacgd_norm_args& a, const Where& at) {
   k.look<T>(a.out, a.out_stride);
   k.look<T>(a.sum, a.sum_stride);
   const long long n = a.cols / 8;      // the most runs of a row
-  if (!k.good() || n > 4096) {
+  if (!k.good()) {
     static std::atomic<int> table[TRAIN_DEVICES];
     const int smem = (int)((a.cols + 3) / 4 * 16) + (a.drop.p > 0.0 ? bits_of((int)a.cols) : 0);
     auto kern = k_norm_any<T, P>;
