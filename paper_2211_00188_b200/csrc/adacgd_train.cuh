@@ -22,12 +22,12 @@ struct TrainScratch {
   float* tok_c;    // [tokens] 1 where the clipped term has taken the gradient
   float* seq;      // [tokens + 1] per sequence: weight or gradient coefficient; the last is the total
   double* part;    // [tokens + 3] per pair: loss; per CTA of the token sums: three of them
-  double* own;     // [3][MAX_SMALL_CTAS] sums of the CTAs of a small policy loss
+  double* own;     // [MAX_SMALL_CTAS][3] sums of the CTAs of a small policy loss
   float* norm_part; // [NORM_PARTS][2][max_cols] partial weight and bias gradients
   long long max_tokens, max_cols;
 };
 constexpr int NTRAIN_TICKETS = 64;
-constexpr int MAX_SMALL_CTAS = 2048 * 8;   // 2048 rows in clusters of at most eight
+constexpr int MAX_SMALL_CTAS = 2048;   // of a small policy loss: a row each at most
 
 // Where a call runs.
 struct Where {

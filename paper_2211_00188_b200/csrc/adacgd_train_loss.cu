@@ -1,7 +1,8 @@
 // Token log-probabilities, the preference loss and the clipped policy loss with their gradients (adacgd_train.h).
 //
-// Everything here is passes over rows of logits, a few operations and one or two exponentials an element: memory sets the
-// time (the exponential unit, 16 a clock and SM, is at 70 % when 16-bit logits arrive at the copy rate).
+// Everything here is passes over rows of logits, a few operations and one exponential an element and pass: memory sets the time of
+// the first pass (the exponential unit, 16 a clock and SM, is at 70 % when 16-bit logits arrive at the copy rate), memory and the
+// exponential together that of the second, which also writes.
 //   statistics   one pass with the running maximum and sum: sum_j exp(z_j) = s exp(m)
 //   gradient     c (1{j = label} - exp(z_j - m) / s); for the policy loss c is known as soon as the row's log-probability
 //                is, so the same kernel reads the row again, now from the cache, and writes it; the preference loss first
@@ -28,7 +29,7 @@ __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f 
 constexpr float BIG = 2.3e38f;
 constexpr float LN2 = 0.6931471805599453f;
 
-// 2^(x L) relative to the maximum m
+// Whether m L and z L, z <= m + SLACK, are finite.  -inf is not.
 __device__ __forceinline__ bool plain_range(float m) { return fabsf(m) <= BIG; }
 // x_i = 2^(x_i L + off)
 template <int N>
@@ -381,8 +382,12 @@ template <int NTH, bool CLUSTER> struct Place {
 // --------------------------------------------------------------------------
 // log-probabilities
 // --------------------------------------------------------------------------
-// zb, sum, top: log2 of exp(z_label) and the sum relative to the maximum, and the maximum, in the units of log2_rel and
-// exp_all, from which the preference loss takes its log-probabilities in 64 bits and its gradient.  Either these or logp.
+//   logp = z_label - m - log s
+// One pass, two 64-byte batches a thread under way.  4096 rows x 65536 bfloat16 88 us = 6.1 TB/s, 93 % of the copy rate; 131072 x 512,
+// where a row is one memory latency and two reductions, 29 us = 4.6 TB/s.  Rows walked by as many CTAs as fit lost to CTAs handed out
+// by the hardware: no gain on full batches, 140 against 113 us with a third of the rows masked.
+// zb, sum, top: log2 of exp(z_label) and the sum, both relative to the reference, and the reference, as log2_rel and exp_all take
+// them; from these the preference loss has its log-probabilities in 64 bits and its gradient.  Either these or logp.
 template <typename T, int NTH, bool CLUSTER>
 __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>::CTAS) k_logp(adacgd_token_rows r, float* __restrict__ logp, float* __restrict__ lse,
                                                                    float* __restrict__ zb, float* __restrict__ sum,
@@ -545,7 +550,9 @@ __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, con
   if (threadIdx.x == 0) *a.loss = (float)(v / (double)pairs);
 }
 
-// The gradient once the pairs' coefficients are known: element by element, `parts` walkers a row.
+// The gradient once the pairs' coefficients are known: element by element, `parts` places a row.  The logits have to be read again
+// (512 MB do not stay in the cache), so the call moves three units where log-probabilities of the policy kind move two: 4096 x 32000
+// bfloat16, two thirds of the tokens counted, 116 us against a floor of 67 for one read and one write, 94 for the two reads.
 template <typename T, int NTH>
 __global__ void __launch_bounds__(Place<NTH, false>::CTA, Place<NTH, false>::CTAS) k_preference_grad(adacgd_preference_args a, const float* __restrict__ coef,
                                                                             const float* __restrict__ zb, const float* __restrict__ sum,
@@ -664,10 +671,14 @@ __device__ __forceinline__ int count_share(const uint8_t* mask, int n, int t) {
   return c;
 }
 
-// A row's loss and, from the cache, its gradient.
-// SMALL (few tokens, where a launch costs more than the work it saves): the CTAs' sums are added by the last one, and without
-// `weight` every row counts the tokens itself; otherwise a kernel before gives the weights and one behind takes the sums.
-constexpr long long SMALL_TOKENS = 2048;
+// A row's loss and, from the cache, its gradient.  4096 x 131072 bfloat16, two thirds of the rows counted: 361 us = 5.0 TB/s of DRAM
+// traffic, beside which a third as much again comes from the cache.  Rows kept in shared memory between the passes: 521 against 420 us
+// with all rows counted, for want of threads; an asynchronous ring instead of the register batches 55 to 62 % of the copy rate.
+// SMALL: every row counts the tokens itself and the last CTA adds the CTAs' sums; otherwise a kernel before gives the weights and one
+// behind takes the sums.  One kernel instead of three in a call of little work, us in a graph: 528 rows x 1001 7.1 against 8.3, 2048 x
+// 256 7.0 against 8.0.  Not for long rows, where the CTAs' fence and count at the end cost more: 16 x 32000 8.9 against 8.3, 2000 x
+// 32000 52 against 48; nor for weights by sequence, whose kernel stays: no difference.
+constexpr long long SMALL_ELEMENTS = 1 << 21;
 template <typename T, int NTH, bool CLUSTER, bool SMALL>
 __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>::CTAS) k_policy(adacgd_policy_args a, const float* __restrict__ weight, float* tl,
                                                                      float* tk, float* tc, double* own, u32* ticket) {
@@ -687,7 +698,7 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
   const float A = here ? a.advantages[row] : 0.f, old = here ? a.old_logp[row] : 0.f, ref = here && a.ref_logp ? a.ref_logp[row] : 0.f;
   T* d = a.dlogits ? (T*)a.dlogits + row * a.dlogits_stride : nullptr;
   int total = 0;
-  if (SMALL && !weight) {
+  if (SMALL) {
     total = (int)a.rows.tokens;
     if (a.rows.mask) {
       int c = count_share<NTH>(a.rows.mask, total, at.t);
@@ -723,12 +734,12 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
     // the same weight for all, or the sequence's
     const long long q = a.per_sequence ? seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences) : 0;
     pdl_wait();
-    const float w = SMALL && !weight ? (float)(1.0 / (double)total) : weight[q];
+    const float w = SMALL ? (float)(1.0 / (double)total) : weight[q];
     const Token tok = token_loss(logp, old, A, a.ref_logp != nullptr, ref, a.clip_low, a.clip_high, a.kl_beta);
     if (at.t == 0 && at.part == 0) {
       if (a.logp) a.logp[row] = logp;
       if (SMALL) {
-        mine[0][slot] = (double)(w * tok.loss);
+        mine[0][slot] = (double)w * (double)tok.loss;
         mine[1][slot] = (double)tok.kl;
         mine[2][slot] = tok.clipped ? 1.0 : 0.0;
       } else {
@@ -757,7 +768,7 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
   }
 #pragma unroll
   for (int i = 0; i < 3; ++i) v[i] = block_sum_f64<CTA>(v[i], shd);
-  if (threadIdx.x == 0) write_policy(a.loss, a.stats, v[0], v[1], v[2], weight ? (double)weight[a.rows.sequences] : (double)total);
+  if (threadIdx.x == 0) write_policy(a.loss, a.stats, v[0], v[1], v[2], (double)total);
 }
 
 // The sums over tokens, in a fixed order: a CTA takes SUM_ROWS of them, the last one adds the CTAs'.
@@ -826,40 +837,45 @@ unsigned ctas(long long rows, int rows_per_cta, int cluster) {
 // Threads a row and CTAs a row (a cluster, only where rows would leave SMs idle).
 struct Split { int threads, cluster; };
 Split split_of(long long rows, long long vocab, int threads, const Where& at) {
-  Split s = {threads, 1};
+  Split s = {threads, 1};   // with rows for all SMs
   while (s.threads < 512 && rows * s.threads < 1024ll * at.sms && vocab > 8 * s.threads) s.threads = s.threads < 32 ? 32 : s.threads * 4;
   if (s.threads >= 512)
     while (s.cluster < 8 && rows * s.cluster * 2 <= 2 * at.sms && vocab / (s.cluster * 2) >= 4096) s.cluster *= 2;
   if (s.threads > 512 && s.cluster > 1) s.threads = 512;
   return s;
 }
-// One pass: a row's two reductions cost about what 128 elements a thread do, and many rows on an SM hide them.
+// One pass: a row's two reductions cost every warp the same, about what 128 elements a thread do, and many rows on an SM hide them; so
+// as few threads a row as that.  Log-probabilities of 2^27 elements (2^16 rows of 512), us at 8 / 32 / 128 / 512 threads a row:
+// bfloat16 512 wide 29 / 70 / - / -; 1536 70 / 93 / - / -; 2048 91 / 93 / 275 / -; 4096 95 / 88 / 135 / -; 8192 98 / 89 / 97 / 312; 16384
+// - / 89 / 84 / 161; 32768 - / 101 / 86 / 109; 131072 - / - / 93 / 86; binary32 1024 wide 82 / 85; 1536 121 / 117.
 Split split_once(long long rows, long long vocab, int size, const Where& at) {
   return split_of(rows, vocab, vocab * size <= 4096 ? 8 : vocab <= 8192 ? 32 : (vocab <= 65536 ? 128 : 512), at);
 }
 // Two passes, the second from the cache: what the resident threads hold between their passes (1024 an SM) has to stay in it beside
 // what is written, so a thread may have 400 bytes of a row, and 640 where more threads a row cost more than the cache gives.
-// Policy loss, bfloat16, us at 128 / 256 / 512 / 1024 threads a row: 8192 x 32000 213 / 196 / 239 / -; 8192 x 50001 371 / 316 / 339 /
-// 509; 4096 x 65536 255 / 269 / 208 / -; 4096 x 131072 - / - / 419 / 458; 2048 x 262145 - / - / 511 / 452.
+// Policy loss, us at 8 / 32 / 128 / 256 / 512 / 1024 threads a row, bfloat16: 131072 x 1024 109 / 137; 131072 x 1536 164 / 186; 131072 x
+// 2048 222 / 204; 65536 x 4096 - / 191 / 256; 32768 x 8192 - / 214 / 203; 8192 x 32000 - / - / 213 / 196 / 239; 8192 x 50001 371 / 316 /
+// 339 / 509 from 128 on; 4096 x 65536 255 / 269 / 208 from 128 on; 4096 x 131072 419 / 458 and 2048 x 262145 511 / 452 at 512 / 1024;
+// binary32: 131072 x 512 105 / 124; 131072 x 1024 251 / 191; 65536 x 4096 - / 473 / 366.
 constexpr int PASS_BYTES = 400, PASS_BYTES_WIDE = 640;
 Split split_twice(long long rows, long long vocab, int size, const Where& at) {
   const long long bytes = vocab * size;
-  return split_of(rows, vocab, bytes <= 8 * PASS_BYTES ? 8 : bytes <= 32 * PASS_BYTES ? 32 : bytes <= 128 * PASS_BYTES ? 128 : bytes <= 256 * PASS_BYTES ? 256 : bytes <= 512 * PASS_BYTES_WIDE ? 512 : 1024, at);
+  for (int threads : {8, 32, 128, 256})
+    if (bytes <= threads * PASS_BYTES) return split_of(rows, vocab, threads, at);
+  return split_of(rows, vocab, bytes <= 512 * PASS_BYTES_WIDE ? 512 : 1024, at);
 }
-#define BY_SPLIT(s, call)                                                                              \
+#define BY_THREADS(s, call)                                                                            \
+  (s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }())     \
+   : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }())   \
+   : s.threads == 32 ? ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }())     \
+                     : ([&] { constexpr int NTH = 8; constexpr bool CL = false; return call; }()))
+#define BY_SPLIT_ONCE(s, call) \
+  (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }()) : BY_THREADS(s, call))
+#define BY_SPLIT_TWICE(s, call)                                                                        \
   (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())         \
    : s.threads == 1024 ? ([&] { constexpr int NTH = 1024; constexpr bool CL = false; return call; }()) \
-   : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }())   \
    : s.threads == 256 ? ([&] { constexpr int NTH = 256; constexpr bool CL = false; return call; }())   \
-   : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }())   \
-   : s.threads == 32 ? ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }())     \
-                     : ([&] { constexpr int NTH = 8; constexpr bool CL = false; return call; }()))
-#define BY_SPLIT_ONCE(s, call)                                                                         \
-  (s.cluster > 1 ? ([&] { constexpr int NTH = 512; constexpr bool CL = true; return call; }())         \
-   : s.threads == 512 ? ([&] { constexpr int NTH = 512; constexpr bool CL = false; return call; }())   \
-   : s.threads == 128 ? ([&] { constexpr int NTH = 128; constexpr bool CL = false; return call; }())   \
-   : s.threads == 32 ? ([&] { constexpr int NTH = 32; constexpr bool CL = false; return call; }())     \
-                     : ([&] { constexpr int NTH = 8; constexpr bool CL = false; return call; }()))
+                      : BY_THREADS(s, call))
 
 template <typename T>
 cudaError_t logp_t(const adacgd_token_rows& r, float* logp, float* lse, float* zb, float* sum, float* top, const Where& at) {
@@ -898,22 +914,17 @@ int preference_t(const TrainScratch& s, const adacgd_preference_args& a, const W
 
 template <typename T>
 int policy_t(const TrainScratch& s, const adacgd_policy_args& a, const Where& at) {
-  const bool small = a.rows.tokens > 0 && a.rows.tokens <= SMALL_TOKENS;
-  int n = 1;
-  if (!small || a.per_sequence) {
-    if (launch(k_policy_weights, 1u, 1024, 1, false, at.stream, 0, a, s.seq) != cudaSuccess) return -1;
-    if (!a.rows.tokens) return 1;
-    n = 2;
-  }
   const Split sp = split_twice(a.rows.tokens, a.rows.vocab, (int)sizeof(T), at);
-  if (small) {
-    const float* weight = a.per_sequence ? s.seq : nullptr;
-    return BY_SPLIT(sp, (launch(k_policy<T, NTH, CL, true>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, sp.cluster), Place<NTH, CL>::CTA, sp.cluster,
-                                a.per_sequence != 0, at.stream, 0, a, weight, s.tok_a, s.tok_b, s.tok_c, s.own, s.tickets + 1))) == cudaSuccess
-               ? n
+  if (!a.per_sequence && sp.cluster == 1 && a.rows.tokens > 0 && a.rows.tokens <= MAX_SMALL_CTAS &&
+      a.rows.tokens * a.rows.vocab <= SMALL_ELEMENTS &&
+      sp.threads != 256 && sp.threads != 1024)      // rows so long have clusters when they are so few
+    return BY_THREADS(sp, (launch(k_policy<T, NTH, CL, true>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, 1), Place<NTH, CL>::CTA, 1, false, at.stream, 0,
+                                  a, (const float*)nullptr, s.tok_a, s.tok_b, s.tok_c, s.own, s.tickets + 1))) == cudaSuccess
+               ? 1
                : -1;
-  }
-  cudaError_t e = BY_SPLIT(sp, (launch(k_policy<T, NTH, CL, false>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, sp.cluster), Place<NTH, CL>::CTA, sp.cluster,
+  if (launch(k_policy_weights, 1u, 1024, 1, false, at.stream, 0, a, s.seq) != cudaSuccess) return -1;
+  if (!a.rows.tokens) return 1;
+  cudaError_t e = BY_SPLIT_TWICE(sp, (launch(k_policy<T, NTH, CL, false>, ctas(a.rows.tokens, Place<NTH, CL>::ROWS, sp.cluster), Place<NTH, CL>::CTA, sp.cluster,
                                        true, at.stream, 0, a, s.seq, s.tok_a, s.tok_b, s.tok_c, s.own, s.tickets + 1)));
   if (e == cudaSuccess)
     e = launch(k_policy_sum, (unsigned)((a.rows.tokens + SUM_ROWS - 1) / SUM_ROWS), SUM_NT, 1, true, at.stream, 0, a, s.seq, s.tok_a, s.tok_b,

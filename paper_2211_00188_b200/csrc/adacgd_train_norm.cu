@@ -1,15 +1,11 @@
 // Dropout and layer norm with the residual sum and dropout in front of it, forward and backward (adacgd_train.h).
 //
 // All three are bound by memory: a few operations an element against 4 to 20 bytes of traffic.  So every element is read
-// once and written once, a row stays in registers between its statistics and its result, and what is left is to keep
-// enough loads in flight.
+// once and written once, a row stays on the SM between its statistics and its result (forward in registers, backward in shared
+// memory), and what is left is to keep enough loads in flight.
 //
-// Two ways to spread a row over threads:
-//   VEC   a thread owns runs of eight consecutive columns and moves them in 16-byte pieces.  Eight columns are also one
-//         block of the dropout generator, so a run costs one call of it.  Needs 16-byte aligned rows (base, stride, weight)
-//         and a multiple of eight columns.
-//   else  a thread owns every NTH-th column, loaded one by one: a warp's 32 elements are consecutive, whatever the
-//         alignment.  The generator's bits for the row are made once, block by block, and passed through shared memory.
+// The unit is a run of eight elements, which is 16 bytes (32 of binary32) and one block of the dropout generator.  Matrices whose
+// rows do not lie on runs (gaps or alignments that shift from row to row) take kernels that go element by element.
 #include <cooperative_groups.h>
 
 #include "adacgd_train.cuh"
@@ -309,8 +305,12 @@ template <> struct Held<float> {
 // --------------------------------------------------------------------------
 // layer norm
 // --------------------------------------------------------------------------
-// A walker takes one row, CTAs are handed out by the hardware: the row's two sums and the loads of other rows on the SM hide each
-// other.  The mean first, then the squares about it, over registers: no cancellation.
+//   v = dropout(x) + residual,  mean = sum v / n,  rstd = 1 / sqrt(sum (v - mean)^2 / n + eps),  out = (v - mean) rstd weight + bias
+// NTH threads take one row, CTAs are handed out by the hardware: the row's two sums and the loads of other rows on the SM hide each
+// other (a grid of as many CTAs as fit, with rows through an asynchronous ring, took 404 us where this took 374).  The mean first,
+// then the squares about it, over registers: no cancellation.
+// 32768 x 8192 bfloat16 with residual and sum (four arrays, 2.1 GB): 318 us = 6.75 TB/s, the copy rate; with dropout 355 us, where
+// the generator's products and the selections fill the issue slots.
 template <int NTH> struct Group {
   static constexpr int CTA = NTH <= 32 ? 128 : NTH;
   static constexpr int ROWS = CTA / NTH;
@@ -446,10 +446,14 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
 // layer norm, backward
 // --------------------------------------------------------------------------
 //   h = (s - mean) rstd,  g = dout weight,  ds = rstd (g - mean(g) - h mean(g h)) + dsum
+//   dresidual = ds,  dx = the forward pass's dropout of ds,  dweight = sum over rows of dout h,  dbias = sum over rows of dout
 // dout and s are read once for all results: first for the two sums and the weight gradients, then, from shared memory, for ds.
 // Rows wider than NTH * R runs are cut into as many column parts as the cluster has CTAs; the two sums then meet in distributed
 // shared memory.
-// K rows go through the two phases together, so that their reductions share one barrier.
+// K rows go through the two phases together, so that their reductions share one barrier: 465 -> 341 us at 32768 x 8192 bfloat16,
+// K = 1 -> 2; now 321 us = 6.7 TB/s, the copy rate, and 440 us = 6.1 TB/s with dropout (five arrays).  The weight gradients of a
+// column stay in the registers of the thread that always meets it, so the grid is as many CTAs as fit, and rows come through a ring
+// of asynchronous copies because registers hold no second row.
 template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE, int ARRAYS>
 __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const __grid_constant__ adacgd_norm_backward_args a,
                                                                       const __grid_constant__ Drop d, float* __restrict__ part,
@@ -694,7 +698,23 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
   // The CTA's walkers one after the other, through shared memory (the ring is empty now): written from the registers, every
   // store would touch a sector for four bytes of it.
   float* const acc = reinterpret_cast<float*>(ring);
-  for (int k = 0; k < W::ROWS; ++k) {
+  // Without edges the walkers of a warp have the same columns: they are added first, eight turns instead of up to 32.
+  constexpr int TOGETHER = !EDGE && NTH < 32 ? 32 / NTH : 1;
+#pragma unroll
+  for (int o = NTH; o < NTH * TOGETHER; o <<= 1) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        F2 u, v;
+        u.v = __shfl_xor_sync(0xffffffffu, dw[r][j].v, o);
+        v.v = __shfl_xor_sync(0xffffffffu, db[r][j].v, o);
+        dw[r][j] = add2(dw[r][j], u);
+        db[r][j] = add2(db[r][j], v);
+      }
+    }
+  }
+  for (int k = 0; k < W::ROWS; k += TOGETHER) {
     __syncthreads();
     if (w.slot == k) {
 #pragma unroll
@@ -838,7 +858,8 @@ __global__ void __launch_bounds__(ANY_NT) k_norm_dw_any(const __grid_constant__ 
 }
 
 // Adds the CTAs' partial weight gradients: SUM_COLS columns a CTA, SUM_SLICES threads share a column's partials.  Few columns a CTA,
-// so that the partials, which still lie in the cache, are fetched by many SMs at once.
+// so that the partials, which still lie in the cache, are fetched by many SMs at once.  In 64 bits and in a fixed order: the result
+// repeats bit for bit.  One tenth of the time at 32768 x 8192, half of it where there are few rows.
 constexpr int SUM_COLS = 8, SUM_SLICES = 64;
 template <typename P>
 __global__ void __launch_bounds__(SUM_COLS* SUM_SLICES) k_norm_dw_sum(const float* __restrict__ part, long long max_cols, int parts,
@@ -917,7 +938,7 @@ struct Runs {
 template <typename T, typename P, int NTH, int R>
 int norm_launch(const adacgd_norm_args& a, const Where& at) {
   constexpr int ROWS = Group<NTH>::ROWS;
-  auto kern = a.cols % 8 ? k_norm<T, P, NTH, R, true> : k_norm<T, P, NTH, R, false>;
+  auto kern = a.cols % 8 ? k_norm<T, P, NTH, R, (NTH >= 16)> : k_norm<T, P, NTH, R, false>;      // edges take sixteen threads
   kern<<<(unsigned)((a.rows + ROWS - 1) / ROWS), Group<NTH>::CTA, 0, at.stream>>>(a, make_drop(a.drop));
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
@@ -938,20 +959,28 @@ int norm_t(const adacgd_norm_args& a, const Where& at) {
     kern<<<(unsigned)a.rows, ANY_NT, smem, at.stream>>>(a, make_drop(a.drop));
     return cudaGetLastError() == cudaSuccess ? 1 : -1;
   }
-  if (a.rows <= 2 * at.sms && n > 32) {   // few rows: more threads a row, a shorter chain each
+  // Few rows: more threads a row, a shorter chain each.  us in a graph, 1 / 148 / 296 rows of bfloat16, so and as below: 1024 columns
+  // 2.06 / 2.36 / 2.49 and 3.11 / 3.50 / 3.51; 4096 2.49 / 2.84 / 3.26 and 3.25 / 3.62 / 4.05.  8192 columns over 1024 threads gain
+  // 0.13 us for one row and lose 1.8 for 296.
+  if (a.rows <= 2 * at.sms && n > 32) {
     if (n <= 128) return norm_launch<T, P, 128, 1>(a, at);
     if (n <= 512) return norm_launch<T, P, 512, 1>(a, at);
-    if (n <= 1024) return norm_launch<T, P, 1024, 1>(a, at);
   }
-  if (n <= 8 && a.cols % 8 == 0) return norm_launch<T, P, 8, 1>(a, at);      // edges take sixteen threads
-  if (n <= 16) return norm_launch<T, P, 16, 1>(a, at);
-  if (n <= 32) return norm_launch<T, P, 32, 1>(a, at);
+  // As few threads a row as its length in registers allows: the reductions cost every warp the same.  us for 2^27 elements with a
+  // residual, bfloat16, p = 0 / p = 0.1, here and at twice the threads: 64 columns 160 / 181 and 185 / 220; 128 162 / 183, 185 / 222;
+  // 256 161 / 183, 187 / 222; 4096 161 / 170, 177 / 193; 8192 164 / 181, 190 / 205; 16384 241 / 251, 249 / 251.  Four runs of binary32
+  // take twice the registers: 8192 columns 316 (344 at 8185) against 312 (325) with two.
+  const bool edge = a.cols % 8 != 0;                                         // takes sixteen threads
+  if (n <= 8 && !edge) return norm_launch<T, P, 4, 2>(a, at);
+  if (n <= 16 && !edge) return norm_launch<T, P, 8, 2>(a, at);
+  if (n <= 32) return norm_launch<T, P, 16, 2>(a, at);
   if (n <= 64) return norm_launch<T, P, 32, 2>(a, at);
   if (n <= 128) return norm_launch<T, P, 32, 4>(a, at);
   if (n <= 256) return norm_launch<T, P, 128, 2>(a, at);
-  if (n <= 512) return norm_launch<T, P, 256, 2>(a, at);
+  if (n <= 512) return norm_launch<T, P, 128, 4>(a, at);
+  if (sizeof(T) == 2 && n <= 1024) return norm_launch<T, P, 256, 4>(a, at);
   if (n <= 1024) return norm_launch<T, P, 512, 2>(a, at);
-  if (n <= 2048) return norm_launch<T, P, 1024, 2>(a, at);
+  if (n <= 2048) return norm_launch<T, P, 512, 4>(a, at);
   return norm_launch<T, P, 1024, 4>(a, at);
 }
 
@@ -1011,10 +1040,20 @@ int norm_bwd_by_width(const TrainScratch& s, const adacgd_norm_backward_args& a,
   if (!EDGE && n <= 8) return norm_bwd_launch<T, P, 8, 1, false, false>(s, a, 1, at);      // edges take sixteen threads
   if (n <= 16) return norm_bwd_launch<T, P, 16, 1, false, EDGE>(s, a, 1, at);
   if (n <= 32) return norm_bwd_launch<T, P, 32, 1, false, EDGE>(s, a, 1, at);
-  if (n <= 64) return norm_bwd_launch<T, P, 32, 2, false, EDGE>(s, a, 1, at);
-  if (n <= 128) return norm_bwd_launch<T, P, 64, 2, false, EDGE>(s, a, 1, at);
-  if (n <= 256) return norm_bwd_launch<T, P, 128, 2, false, EDGE>(s, a, 1, at);
-  if (n <= 512) return norm_bwd_launch<T, P, 256, 2, false, EDGE>(s, a, 1, at);
+  // One run a thread for binary32, of which an SM holds half as many rows, and where a walker gets few rows; else two, which share a
+  // reduction.  us, one / two, with dsum: bfloat16 1024 columns, 512 rows 9.8 / 12.7, 4096 15.2 / 18.6, 8192 22.9 / 21.4, 65536 121 /
+  // 98; 4096 columns, 512 rows 12.9 / 14.7, 4096 39 / 35, 16384 121 / 94; binary32 1024 columns, 512 rows 10.8 / 12.7, 16384 53 / 56.
+  if (sizeof(T) == 4 || a.rows * a.cols <= 32768ll * at.sms) {
+    if (n <= 64) return norm_bwd_launch<T, P, 64, 1, false, EDGE>(s, a, 1, at);
+    if (n <= 128) return norm_bwd_launch<T, P, 128, 1, false, EDGE>(s, a, 1, at);
+    if (n <= 256) return norm_bwd_launch<T, P, 256, 1, false, EDGE>(s, a, 1, at);
+    if (n <= 512) return norm_bwd_launch<T, P, 512, 1, false, EDGE>(s, a, 1, at);
+  } else {
+    if (n <= 64) return norm_bwd_launch<T, P, 32, 2, false, EDGE>(s, a, 1, at);
+    if (n <= 128) return norm_bwd_launch<T, P, 64, 2, false, EDGE>(s, a, 1, at);
+    if (n <= 256) return norm_bwd_launch<T, P, 128, 2, false, EDGE>(s, a, 1, at);
+    if (n <= 512) return norm_bwd_launch<T, P, 256, 2, false, EDGE>(s, a, 1, at);
+  }
   if (n <= 1024) return norm_bwd_launch<T, P, 512, 2, false, EDGE>(s, a, 1, at);
   return norm_bwd_launch<T, P, 512, 2, true, EDGE>(s, a, (int)((n + 1023) / 1024), at);
 }

@@ -739,3 +739,54 @@ def test_refusals(ops):
     small.close()
     with pytest.raises(RuntimeError):
         small.dropout(x, out, p=0.1, seed=0)
+
+
+@pytest.mark.parametrize("steps,vocab,dtype", [(1024, 40, "bf16"), (1025, 40, "bf16"), (2500, 1001, "f32"), (2500, 520, "f16")])
+@pytest.mark.parametrize("per_sequence", [False, True])
+@pytest.mark.parametrize("masked", [False, True])
+def test_policy_loss_of_many_tokens(ops, steps, vocab, dtype, per_sequence, masked):
+    """Token counts on both sides of the sizes at which the sums move to kernels of their own."""
+    seqs, dt = 2, TYPES[dtype]
+    n = seqs * steps
+    z, y, rng = make_rows(n, vocab, dt, seed=8)
+    mask = rng.random(n) < 0.6 if masked else np.ones(n, bool)
+    logp0 = O.token_logp(host(z), y.cpu().numpy())[0]
+    old, adv = dev(logp0 + 0.05), dev(rng.normal(size=n))
+    loss, stats, d = torch.empty(1, device="cuda"), torch.empty(3, device="cuda"), torch.empty_like(z)
+    ops.policy_loss(z, y, old, adv, loss, d, mask=torch.from_numpy(mask).cuda() if masked else None, sequences=seqs,
+                    per_sequence=per_sequence, stats=stats)
+    f = lambda v: float(np.float32(v))  # noqa: E731
+    want = O.policy(host(z), y.cpu().numpy(), host(old), host(adv), mask, seqs, None, None, f(0.2), f(0.2), 0.0, per_sequence, 1.0)
+    tol = logp_tol(host(z), vocab)
+    r = np.exp(want["logp"] - host(old))
+    w = mask / max(1, mask.sum())
+    if per_sequence:
+        w = np.concatenate([m / (2 * m.sum()) for m in np.split(mask, 2)])
+    terr = (tol + 8 * E) * r * np.abs(host(adv))
+    close(loss, np.array([want["loss"]]), 2 * (w * terr).sum() + 8 * E * (w * r * np.abs(host(adv))).sum(), "loss")
+    assert stats[2].item() == mask.sum() and stats[1].item() == pytest.approx(want["stats"][1], abs=4 * E)
+    soft = O.token_logp(host(z), y.cpu().numpy(), mask)[2]
+    close(d, want["dlogits"], grad_tol(want["dlogits"], want["per_token"], soft, tol, dt, 1.0, w * terr * 2 + 4 * E * np.abs(want["per_token"])),
+          "dlogits")
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_preference_loss_of_long_sequences(ops, packed):
+    """Pairs long enough to be summed by several CTAs."""
+    seqs, steps, vocab = 4, 3000, 24
+    n = seqs * steps
+    z, y, rng = make_rows(n, vocab, torch.float32, seed=4, scale=1.0)
+    mask = rng.random(n) < 0.8
+    ref = dev(O.token_logp(host(z), y.cpu().numpy())[0] + rng.normal(size=n) * 0.01)
+    start = np.array([0, 1, 700, 7000, n], np.int32) if packed else None
+    loss, margin, sums, d = torch.empty(1, device="cuda"), torch.empty(2, device="cuda"), torch.empty(4, device="cuda"), torch.empty_like(z)
+    kw = dict(seq_start=torch.from_numpy(start).cuda()) if packed else dict(sequences=seqs)
+    ops.preference_loss(z, y, ref, loss, d, beta=0.5, mask=torch.from_numpy(mask).cuda(), margin=margin, seq_logp=sums, **kw)
+    want = O.preference(host(z), y.cpu().numpy(), host(ref), mask, None if packed else seqs, start, beta=0.5)
+    # every token's log-probability is off by at most `tol`, all of them the same way at worst
+    tol = logp_tol(host(z), vocab)
+    assert abs(loss.item() - want["loss"]) <= 0.5 * (tol * mask).sum() + 4 * E * abs(want["loss"])
+    close(margin, want["margin"], 0.5 * (tol * mask).sum() + 4 * E * np.abs(want["margin"]), "margin")
+    close(sums, want["seq_logp"], (tol * mask).sum() + 4 * E * np.abs(want["seq_logp"]), "seq_logp")
+    top = np.abs(want["dlogits"]).max()
+    close(d, want["dlogits"], top * (0.5 * (tol * mask).sum() + 32 * E) + 1e-30 + 0 * want["dlogits"], "dlogits")
