@@ -14,7 +14,8 @@
  *     Inputs have to be ready, and outputs are ready, in that stream's order.  One call at a time per context.
  *   - A context is bound to the device that was current at adacgd_train_init, as adacgd_ctx is.
  *   - Matrices are row-major with a row stride in elements and unit column stride; vectors are contiguous.  No
- *     alignment beyond the element's own is needed; 16-byte aligned rows, or rows that are misaligned alike, are faster.
+ *     alignment beyond the element's own is needed; rows aligned to 16 bytes
+ *     (32 for binary32), or misaligned alike, are faster.
  *   - Element types: binary32, binary16, bfloat16 (ADACGD_F32, _F16, _BF16).  All sums, statistics, probabilities and
  *     logarithms are kept in binary32 or binary64 and a result is rounded once, to its own type, when it is stored.
  *   - An output may be the very same matrix (pointer and stride) as an input unless a call says otherwise; other
