@@ -17,7 +17,7 @@ constexpr int NORM_PARTS = 592;  // most partial rows of a weight gradient: four
 // The context's workspace, carved by carve_train_scratch.
 struct TrainScratch {
   u32* tickets;    // [NTRAIN_TICKETS] completion counts, zero between calls
-  float* tok_a;    // [tokens] a token's weighted loss
+  float* tok_a;    // [tokens] a token's loss
   float* tok_b;    // [tokens] its KL estimate
   float* tok_c;    // [tokens] 1 where the clipped term has taken the gradient
   float* seq;      // [tokens + 1] per sequence: weight or gradient coefficient; the last is the total

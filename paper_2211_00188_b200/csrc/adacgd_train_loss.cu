@@ -671,7 +671,7 @@ __device__ __forceinline__ int count_share(const uint8_t* mask, int n, int t) {
   return c;
 }
 
-// A row's loss and, from the cache, its gradient.  4096 x 131072 bfloat16, two thirds of the rows counted: 361 us = 5.0 TB/s of DRAM
+// A row's loss and, from the cache, its gradient.  4096 x 131072 bfloat16, two thirds of the rows counted: 350 us = 5.1 TB/s of DRAM
 // traffic, beside which a third as much again comes from the cache.  Rows kept in shared memory between the passes: 521 against 420 us
 // with all rows counted, for want of threads; an asynchronous ring instead of the register batches 55 to 62 % of the copy rate.
 // SMALL: every row counts the tokens itself and the last CTA adds the CTAs' sums; otherwise a kernel before gives the weights and one
@@ -743,7 +743,7 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
         mine[1][slot] = (double)tok.kl;
         mine[2][slot] = tok.clipped ? 1.0 : 0.0;
       } else {
-        tl[row] = w * tok.loss;
+        tl[row] = tok.loss;
         tk[row] = tok.kl;
         tc[row] = tok.clipped ? 1.f : 0.f;
       }
@@ -780,7 +780,8 @@ __global__ void __launch_bounds__(SUM_NT) k_policy_sum(adacgd_policy_args a, con
   const long long lo = (long long)blockIdx.x * SUM_ROWS, hi = min((long long)a.rows.tokens, lo + SUM_ROWS);
   double v[3] = {0.0, 0.0, 0.0};
   for (long long t = lo + threadIdx.x; t < hi; t += SUM_NT) {
-    v[0] += (double)tl[t];
+    const long long q = a.per_sequence ? seq_of(a.rows.seq_start, t, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences) : 0;
+    v[0] += (double)weight[q] * (double)tl[t];     // weighted here: losses of both signs cancel, a product rounded before would show
     v[1] += (double)tk[t];
     v[2] += (double)tc[t];
   }
