@@ -663,8 +663,7 @@ __device__ __forceinline__ int count_share(const uint8_t* mask, int n, int t) {
         c += __popc(x & 0x01010101u);
       }
     }
-    const int rest = n / 16 * 16 + t;
-    if (t < 16 && rest < n) c += mask[rest] != 0;
+    for (int i = n / 16 * 16 + t; i < n; i += NTH) c += mask[i] != 0;   // up to fifteen, which can be more than NTH
   } else {
     for (int i = t; i < n; i += NTH) c += mask[i] != 0;
   }

@@ -1,0 +1,60 @@
+"""Inputs at the edge of what the training operators take, against the binary64 restatement (oracle/training_oracle.py).  Tolerances and
+their derivation are those of test_training_gpu.py unless a test says otherwise."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2211_00188_b200 as pkg
+from oracle import training_oracle as O
+from test_training_gpu import E, close, dev, grad_tol, host, logp_tol, make_rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    return pkg.TrainingOps(70000, 32768)
+
+
+# ----------------------------------------------------------------------------- counting tokens
+
+def masks(n, which, rng):
+    m = np.zeros(n, bool)
+    if which == "all":
+        m[:] = True
+    elif which == "last":
+        m[-1] = True
+    elif which == "rest":
+        m[n // 16 * 16 + 8:] = True                          # what lies behind the eighth token after the last whole sixteen
+    else:
+        m[:] = rng.random(n) < 0.6
+        m[0] = True
+    return m
+
+
+@pytest.mark.parametrize("n", [9, 10, 12, 13, 15, 31, 41, 1005, 2047])
+@pytest.mark.parametrize("vocab", [5, 40, 64, 65, 200])
+@pytest.mark.parametrize("which", ["all", "last", "rest", "some"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_policy_loss_counts_every_token(ops, n, vocab, which, shift):
+    z, y, rng = make_rows(n, vocab, torch.float32, seed=11)
+    mask = masks(n, which, rng)
+    buf = torch.zeros(n + 16, dtype=torch.bool, device="cuda")
+    dm = buf[shift:shift + n]                                # a mask on 16 bytes, and one off them
+    dm.copy_(torch.from_numpy(mask))
+    buf[shift + n:] = True                                   # behind the mask: not part of it
+    logp0 = O.token_logp(host(z), y.cpu().numpy())[0]
+    old, adv = dev(logp0 + 0.05), dev(rng.normal(size=n))
+    loss, stats, d = torch.empty(1, device="cuda"), torch.empty(3, device="cuda"), torch.empty_like(z)
+    ops.policy_loss(z, y, old, adv, loss, d, mask=dm, stats=stats)
+    f = lambda v: float(np.float32(v))  # noqa: E731
+    want = O.policy(host(z), y.cpu().numpy(), host(old), host(adv), mask, 1, None, None, f(0.2), f(0.2))
+    assert stats[2].item() == mask.sum()
+    tol = logp_tol(host(z), vocab)
+    r = np.exp(want["logp"] - host(old))
+    w = mask / mask.sum()
+    terr = (tol + 8 * E) * r * np.abs(host(adv))
+    close(loss, np.array([want["loss"]]), 2 * (w * terr).sum() + 8 * E * (w * r * np.abs(host(adv))).sum(), "loss")
+    soft = O.token_logp(host(z), y.cpu().numpy(), mask)[2]
+    close(d, want["dlogits"], grad_tol(want["dlogits"], want["per_token"], soft, tol, torch.float32, 1.0,
+                                       w * terr * 2 + 4 * E * np.abs(want["per_token"])), "dlogits")
