@@ -162,7 +162,7 @@ def policy(logits, labels, old_logp, advantages, mask=None, sequences=None, seq_
     for t in np.flatnonzero(counted):
         A, r = float(advantages[t]), np.exp(logp[t] - float(old_logp[t]))
         gain, held = r * A, min(max(r, 1 - clip_low), 1 + clip_high) * A
-        l, c = -min(gain, held), (-gain if gain <= held else 0.0)
+        l, c = (-held, 0.0) if gain > held else (-gain, -gain)        # NaN goes through
         if ref_logp is not None:
             u = float(ref_logp[t]) - logp[t]
             l += kl_beta * (np.expm1(u) - u)

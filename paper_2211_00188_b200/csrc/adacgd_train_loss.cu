@@ -622,12 +622,13 @@ __global__ void __launch_bounds__(1024) k_policy_weights(adacgd_policy_args a, f
 struct Token { float loss, slope, kl; bool clipped; };
 __device__ __forceinline__ Token token_loss(float logp, float old, float A, bool with_ref, float ref, float clip_low, float clip_high,
                                             float kl_beta) {
-  const float r = expf(logp - old), lo = 1.f - clip_low, hi = 1.f + clip_high;
-  const float held = (r < lo ? lo : (r > hi ? hi : r)) * A, gain = r * A;   // NaN goes through
+  const float x = logp - old, r = expf(x), lo = 1.f - clip_low, hi = 1.f + clip_high;
+  // NaN goes through, but not inf * 0 where r has only passed binary32's range
+  const float held = (r < lo ? lo : (r > hi ? hi : r)) * A, gain = A == 0.f && fabsf(x) < INFINITY ? 0.f : r * A;
   Token k;
-  k.slope = gain <= held ? -gain : 0.f;
-  k.loss = gain <= held ? -gain : -held;
   k.clipped = gain > held;
+  k.slope = k.clipped ? 0.f : -gain;     // a NaN is not clipped away: it reaches loss and gradient
+  k.loss = k.clipped ? -held : -gain;
   k.kl = 0.f;
   if (with_ref) {
     const float u = ref - logp, e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0

@@ -6,7 +6,7 @@ import torch
 
 import paper_2211_00188_b200 as pkg
 from oracle import training_oracle as O
-from test_training_gpu import E, close, dev, grad_tol, host, logp_tol, make_rows
+from test_training_gpu import E, TYPES, close, dev, grad_tol, host, logp_tol, make_rows
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,44 @@ def test_policy_loss_counts_every_token(ops, n, vocab, which, shift):
     soft = O.token_logp(host(z), y.cpu().numpy(), mask)[2]
     close(d, want["dlogits"], grad_tol(want["dlogits"], want["per_token"], soft, tol, torch.float32, 1.0,
                                        w * terr * 2 + 4 * E * np.abs(want["per_token"])), "dlogits")
+
+
+# ----------------------------------------------------------------------------- NaN
+
+@pytest.mark.parametrize("per_sequence", [False, True])      # one kernel, three kernels
+@pytest.mark.parametrize("with_ref", [False, True])
+@pytest.mark.parametrize("what", ["label", "old", "advantage"])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("vocab", [40, 500])
+def test_policy_gradient_of_a_nan_ratio_is_nan(ops, per_sequence, with_ref, what, dtype, vocab):
+    z, y, _ = make_rows(6, vocab, TYPES[dtype])
+    logp = O.token_logp(host(z), y.cpu().numpy())[0]
+    old, ref, adv = dev(logp), dev(logp + 0.1), torch.ones(6, device="cuda")
+    bad = [1, 4]
+    if what == "label":
+        y[1], y[4] = -1, vocab
+    else:
+        (old if what == "old" else adv)[bad] = float("nan")
+    loss, d = torch.empty(1, device="cuda"), torch.zeros_like(z)
+    ops.policy_loss(z, y, old, adv, loss, d, sequences=2, per_sequence=per_sequence, ref_logp=ref if with_ref else None,
+                    kl_beta=0.1 if with_ref else 0.0)
+    assert torch.isnan(loss).all()
+    assert torch.isnan(d[bad]).all()
+    assert torch.isfinite(d[[0, 2, 3, 5]]).all()
+    want = O.policy(host(z), y.cpu().numpy(), host(old), host(adv), None, 2, ref_logp=host(ref) if with_ref else None,
+                    kl_beta=0.1 if with_ref else 0.0, per_sequence=per_sequence)
+    assert np.array_equal(np.isnan(want["dlogits"]), np.isnan(host(d)))
+
+
+@pytest.mark.parametrize("per_sequence", [False, True])
+def test_policy_without_advantage_has_no_gradient_whatever_the_ratio(ops, per_sequence):
+    """exp(logp - old) = e^100 is no number of binary32; times an advantage of zero it is zero all the same."""
+    z, y, _ = make_rows(4, 60, torch.float32)
+    logp = O.token_logp(host(z), y.cpu().numpy())[0]
+    old, adv = dev(logp - 100), torch.tensor([0.0, 0.0, 2.0, 0.0], device="cuda")
+    loss, stats, d = torch.empty(1, device="cuda"), torch.empty(3, device="cuda"), torch.full_like(z, 3.0)
+    ops.policy_loss(z, y, old, adv, loss, d, sequences=2, per_sequence=per_sequence, stats=stats)
+    want = O.policy(host(z), y.cpu().numpy(), host(old), host(adv), None, 2, per_sequence=per_sequence)
+    assert not d.any() and not want["dlogits"].any()             # the third token is clipped
+    close(loss, np.array([want["loss"]]), 4 * E, "loss")
+    assert stats[1].item() == 0.25
