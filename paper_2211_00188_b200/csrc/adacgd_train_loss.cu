@@ -17,7 +17,8 @@ namespace adacgd {
 namespace {
 
 // Programmatic dependent launch: the kernels of a call may become resident early and wait for their predecessors' results
-// where they need them.
+// where they need them.  What a predecessor writes is never taken as const __restrict__: that promises data which nobody writes
+// while the kernel runs, and lets its loads go ahead of the wait.
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -492,7 +493,7 @@ __device__ __forceinline__ double finish_pair(const adacgd_preference_args& a, l
 
 // `slices` CTAs a pair.  One: it also finishes the pair, and the last CTA of all takes the mean of the losses.  More: the last CTA
 // adds the slices' six sums of each pair and finishes the pairs.
-__global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, const float* __restrict__ zb, const float* __restrict__ sum,
+__global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, const float* zb, const float* sum,
                                                    float* __restrict__ coef, double* __restrict__ part, u32 slices, u32* ticket) {
   __shared__ double sh[PAIR_NT / 32];
   pdl_wait();
@@ -554,9 +555,9 @@ __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, con
 // (512 MB do not stay in the cache), so the call moves three units where log-probabilities of the policy kind move two: 4096 x 32000
 // bfloat16, two thirds of the tokens counted, 116 us against a floor of 67 for one read and one write, 94 for the two reads.
 template <typename T, int NTH>
-__global__ void __launch_bounds__(Place<NTH, false>::CTA, Place<NTH, false>::CTAS) k_preference_grad(adacgd_preference_args a, const float* __restrict__ coef,
-                                                                            const float* __restrict__ zb, const float* __restrict__ sum,
-                                                                            const float* __restrict__ top, u32 parts) {
+__global__ void __launch_bounds__(Place<NTH, false>::CTA, Place<NTH, false>::CTAS) k_preference_grad(adacgd_preference_args a, const float* coef,
+                                                                            const float* zb, const float* sum,
+                                                                            const float* top, u32 parts) {
   const Place<NTH, false> at;
   const long long turn = parts == 1 ? at.row : at.row / parts;
   const int part = parts == 1 ? 0 : (int)(at.row - turn * parts);
@@ -680,7 +681,7 @@ __device__ __forceinline__ int count_share(const uint8_t* mask, int n, int t) {
 // 32000 52 against 48; nor for weights by sequence, whose kernel stays: no difference.
 constexpr long long SMALL_ELEMENTS = 1 << 21;
 template <typename T, int NTH, bool CLUSTER, bool SMALL>
-__global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>::CTAS) k_policy(adacgd_policy_args a, const float* __restrict__ weight, float* tl,
+__global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>::CTAS) k_policy(adacgd_policy_args a, const float* weight, float* tl,
                                                                      float* tk, float* tc, double* own, u32* ticket) {
   constexpr int CTA = Place<NTH, CLUSTER>::CTA, ROWS = Place<NTH, CLUSTER>::ROWS;
   __shared__ Soft sh[32], xch[8];
@@ -773,8 +774,8 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
 
 // The sums over tokens, in a fixed order: a CTA takes SUM_ROWS of them, the last one adds the CTAs'.
 constexpr int SUM_ROWS = 4096, SUM_NT = 512;
-__global__ void __launch_bounds__(SUM_NT) k_policy_sum(adacgd_policy_args a, const float* __restrict__ weight, const float* __restrict__ tl,
-                                                       const float* __restrict__ tk, const float* __restrict__ tc, double* own, u32* ticket) {
+__global__ void __launch_bounds__(SUM_NT) k_policy_sum(adacgd_policy_args a, const float* weight, const float* tl,
+                                                       const float* tk, const float* tc, double* own, u32* ticket) {
   __shared__ double sh[SUM_NT / 32];
   pdl_wait();
   const long long lo = (long long)blockIdx.x * SUM_ROWS, hi = min((long long)a.rows.tokens, lo + SUM_ROWS);

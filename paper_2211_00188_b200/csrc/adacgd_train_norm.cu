@@ -862,7 +862,7 @@ __global__ void __launch_bounds__(ANY_NT) k_norm_dw_any(const __grid_constant__ 
 // repeats bit for bit.  One tenth of the time at 32768 x 8192, half of it where there are few rows.
 constexpr int SUM_COLS = 8, SUM_SLICES = 64;
 template <typename P>
-__global__ void __launch_bounds__(SUM_COLS* SUM_SLICES) k_norm_dw_sum(const float* __restrict__ part, long long max_cols, int parts,
+__global__ void __launch_bounds__(SUM_COLS* SUM_SLICES) k_norm_dw_sum(const float* part, long long max_cols, int parts,
                                                                       int cols, P* __restrict__ dw, P* __restrict__ db) {
   __shared__ double sh[2][SUM_SLICES][SUM_COLS];
   asm volatile("griddepcontrol.wait;" ::: "memory");
