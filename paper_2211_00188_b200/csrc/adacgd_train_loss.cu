@@ -26,11 +26,11 @@ __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;"
 struct Soft { float m, s; };
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 // Exponents are base 2: exp(z - m) is taken as 2^(z L - fl(m L)), L = log2 e, one fused operation an element.  fl(m L) is as good
-// an offset as m L, because the logarithm is taken against the same number.  Where m L overflows, z - m is formed first.
-constexpr float BIG = 2.3e38f;
+// an offset as m L, because the logarithm is taken against the same number, as long as its rounding is a small number itself: up to
+// |m| = 2^22 it is at most 1/4.  Beyond, as in rows that a mask has filled with -1e10, z - m is formed first.
+constexpr float BIG = 4194304.f;
 constexpr float LN2 = 0.6931471805599453f;
 
-// Whether m L and z L, z <= m + SLACK, are finite.  -inf is not.
 __device__ __forceinline__ bool plain_range(float m) { return fabsf(m) <= BIG; }
 // x_i = 2^(x_i L + off)
 template <int N>
@@ -55,10 +55,14 @@ __device__ __forceinline__ void exp_all(float (&x)[N], float m) {
     for (int i = 0; i < N; ++i) x[i] = ex2((x[i] - b) * LOG2E);
   }
 }
-// what a sum kept relative to a is worth relative to m >= a
+// what a sum kept relative to a is worth relative to m >= a: 2 to the difference of their offsets, each rounded or not as above
 __device__ __forceinline__ float rel(float a, float m) {
   if (m == -INFINITY) return 0.f;
-  return plain_range(m) ? ex2(a * LOG2E - m * LOG2E) : ex2((a - m) * LOG2E);
+  const bool pa = plain_range(a), pm = plain_range(m);
+  if (pa && pm) return ex2(a * LOG2E - m * LOG2E);
+  if (pm) return ex2(fmaf(a, LOG2E, -(m * LOG2E)));
+  if (pa) return ex2(fmaf(-m, LOG2E, a * LOG2E));
+  return ex2((a - m) * LOG2E);
 }
 // log2 of exp(z) relative to m
 __device__ __forceinline__ float log2_rel(float z, float m) {

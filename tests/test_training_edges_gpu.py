@@ -99,3 +99,50 @@ def test_policy_without_advantage_has_no_gradient_whatever_the_ratio(ops, per_se
     assert not d.any() and not want["dlogits"].any()             # the third token is clipped
     close(loss, np.array([want["loss"]]), 4 * E, "loss")
     assert stats[1].item() == 0.25
+
+
+# ----------------------------------------------------------------------------- logits far from zero
+
+def far_rows(dt, vocab):
+    """Rows whose logits lie near a distant value, equal or a few units of the type apart, and their labels."""
+    rng = np.random.default_rng(vocab)
+    rows = []
+    for at in (-1e10, 1e10, -1e30, 1e30, -2.2e38, 3e9, -4194304.0, 4194304.0, 2.0 ** 23):
+        rows.append(np.full(vocab, at))
+    if dt == torch.float32:
+        for at in (-4194304.0, 4194304.0):                       # half a unit apart there, on both sides of a power of two
+            rows.append(at + rng.integers(-8, 9, vocab) * 0.5)
+            rows.append(at + np.sort(rng.integers(-8, 9, vocab)) * 0.5)
+    else:
+        rows.append(np.where(rng.random(vocab) < 0.5, 2048.0, 2048.0 + (16.0 if dt == torch.bfloat16 else 2.0)))
+    z = dev(np.stack(rows), dt)
+    y = torch.from_numpy(rng.integers(0, vocab, len(rows))).cuda()
+    return z, y
+
+
+@pytest.mark.parametrize("vocab", [7, 40, 3000, 40000, 290001])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_far_from_zero(ops, vocab, dtype):
+    """A row that is masked as a whole by -1e10 or -1e30 is a uniform one.  Differences of such logits are exact, so the tolerance goes
+    by the largest difference and not by the logits."""
+    dt = TYPES[dtype]
+    z, y = far_rows(dt, vocab)
+    n = len(y)
+    logp = torch.empty(n, device="cuda")
+    ops.token_logp(z, y, logp)
+    hz = host(z)
+    wl, _, soft = O.token_logp(hz, y.cpu().numpy())
+    tol = (vocab / 128 + 64) * E + 4 * E * (hz.max(1) - hz.min(1) + np.log(vocab))
+    close(logp, wl, tol, "logp")
+    loss, d = torch.empty(1, device="cuda"), torch.empty_like(z)
+    adv = torch.ones(n, device="cuda")
+    ops.policy_loss(z, y, dev(wl), adv, loss, d)
+    per = -np.exp(wl - host(dev(wl))) / n
+    want = np.zeros_like(hz)
+    want -= per[:, None] * soft
+    want[np.arange(n), y.cpu().numpy()] += per
+    close(d, want, grad_tol(want, per, soft, tol, dt, c_err=(2 * tol + 8 * E) / n), "dlogits")
+    seqs = n // 2 * 2
+    margin, sums = torch.empty(seqs // 2, device="cuda"), torch.empty(seqs, device="cuda")
+    ops.preference_loss(z[:seqs], y[:seqs], torch.zeros(seqs, device="cuda"), loss, d[:seqs], sequences=seqs, seq_logp=sums, margin=margin)
+    close(sums, wl[:seqs], tol[:seqs] + 4 * E * np.abs(wl[:seqs]), "seq_logp")
