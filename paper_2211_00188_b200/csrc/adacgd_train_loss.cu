@@ -22,16 +22,18 @@ namespace {
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// m: a reference at most SLACK below the maximum; s: sum of exponentials relative to it.  m = -inf: nothing but -inf, s = 0.
+// m: a reference at most SLACK below the maximum; s: sum of exponentials relative to it (to its offset, see below).  m = -inf: nothing but -inf, s = 0.
 struct Soft { float m, s; };
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-// Exponents are base 2: exp(z - m) is taken as 2^(z L - fl(m L)), L = log2 e, one fused operation an element.  fl(m L) is as good
-// an offset as m L, because the logarithm is taken against the same number, as long as its rounding is a small number itself: up to
-// |m| = 2^22 it is at most 1/4.  Beyond, as in rows that a mask has filled with -1e10, z - m is formed first.
-constexpr float BIG = 4194304.f;
-constexpr float LN2 = 0.6931471805599453f;
+// Exponents are base 2: exp(z - m) is taken as 2^(z L - o), L = log2 e, one fused operation an element.  The offset o is m L to the
+// nearest integer: as good as m L, because the logarithm is taken against the same number, and sums kept relative to different m
+// differ by a power of two, which costs no rounding.  Beyond |m| = 2^21, where integers beside m L become coarse (a row that a mask
+// has filled with -1e10), z - m is formed first.
+constexpr float BIG = 2097152.f;
 
 __device__ __forceinline__ bool plain_range(float m) { return fabsf(m) <= BIG; }
+// Added to a number below 2^22 and taken off again, 1.5 2^23 leaves the nearest integer.
+__device__ __forceinline__ float offset_of(float m) { return fmaf(m, LOG2E, 12582912.f) - 12582912.f; }
 // x_i = 2^(x_i L + off)
 template <int N>
 __device__ __forceinline__ void exp_plain(float (&x)[N], float off) {
@@ -48,25 +50,49 @@ __device__ __forceinline__ void exp_plain(float (&x)[N], float off) {
 template <int N>
 __device__ __forceinline__ void exp_all(float (&x)[N], float m) {
   if (plain_range(m)) {
-    exp_plain(x, -(m * LOG2E));
+    exp_plain(x, -offset_of(m));
   } else {
     const float b = base_of(m);
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = ex2((x[i] - b) * LOG2E);
   }
 }
-// what a sum kept relative to a is worth relative to m >= a: 2 to the difference of their offsets, each rounded or not as above
+// what a sum kept relative to a is worth relative to m >= a
 __device__ __forceinline__ float rel(float a, float m) {
   if (m == -INFINITY) return 0.f;
   const bool pa = plain_range(a), pm = plain_range(m);
-  if (pa && pm) return ex2(a * LOG2E - m * LOG2E);
-  if (pm) return ex2(fmaf(a, LOG2E, -(m * LOG2E)));
-  if (pa) return ex2(fmaf(-m, LOG2E, a * LOG2E));
+  if (pa && pm) {
+    const float k = offset_of(a) - offset_of(m);     // an integer, at most 0
+    return k < -126.f ? 0.f : __int_as_float(((int)k + 127) << 23);
+  }
+  if (pm) return ex2(fmaf(a, LOG2E, -offset_of(m)));
+  if (pa) return ex2(fmaf(-m, LOG2E, offset_of(a)));
   return ex2((a - m) * LOG2E);
 }
 // log2 of exp(z) relative to m
 __device__ __forceinline__ float log2_rel(float z, float m) {
-  return plain_range(m) ? fmaf(z, LOG2E, -(m * LOG2E)) : (z - base_of(m)) * LOG2E;
+  return plain_range(m) ? fmaf(z, LOG2E, -offset_of(m)) : (z - base_of(m)) * LOG2E;
+}
+
+// log softmax of a row's entry z, and the logarithm of its sum of exponentials, from the reference and the sum.  Added up in 64 bits:
+// where the row's largest entry is SLACK above m, both terms have that size and nearly cancel, and z L may pass binary32's range.  The
+// sum's exponent k is split off and joins the offset, an integer too; what remains, log2f of [0.75, 1.5), is off by less than 2^-24.
+struct Log2 { float k, f; };
+__device__ __forceinline__ Log2 log2_sum(float s) {
+  const int b = __float_as_int(s), k = b >= 0x00800000 && b < 0x7f800000 ? (b - 0x3f400000) >> 23 : 0;     // not of 0, inf and NaN
+  return {(float)k, log2f(__int_as_float(b - (k << 23)))};
+}
+constexpr double LN2 = 0.6931471805599453;
+__device__ __forceinline__ double logp64(float z, const Soft& a) {
+  const Log2 l = log2_sum(a.s);
+  const double t = plain_range(a.m) ? fma((double)z, (double)LOG2E, -(double)(offset_of(a.m) + l.k))
+                                    : ((double)z - (double)base_of(a.m)) * (double)LOG2E - (double)l.k;
+  return (t - (double)l.f) * LN2;
+}
+__device__ __forceinline__ double lse64(const Soft& a) {
+  const Log2 l = log2_sum(a.s);
+  const double b = (double)base_of(a.m), o = plain_range(a.m) ? fma(b, -(double)LOG2E, (double)(offset_of(a.m) + l.k)) : (double)l.k;
+  return b + (o + (double)l.f) * LN2;
 }
 
 __device__ __forceinline__ long long label_at(const adacgd_token_rows& r, long long t) {
@@ -101,8 +127,9 @@ __device__ __forceinline__ int edge_of(const Cut& c, int t) {
 }
 
 // The reference m only follows the maximum when that is ahead by more than SLACK: exponentials up to e^SLACK do no harm, and
-// after the first batch the sum is hardly ever rescaled.
-constexpr float SLACK = 16.f;
+// after the first batch the sum is hardly ever rescaled.  10: the exponents, SLACK L and half a unit, stay below 16, so the largest
+// terms are off by 2^-21 L^-1 at most from their arguments' rounding; 16 gave twice that and 8 no measured gain.
+constexpr float SLACK = 10.f;
 template <int N>
 __device__ __forceinline__ void absorb(Soft& a, float (&x)[N]) {
   float m[2] = {x[0], x[N > 1 ? 1 : 0]};
@@ -284,7 +311,7 @@ __device__ __forceinline__ void thread_grad(const T* row, T* d, const Cut& c, in
   int r = t;                                 // this thread's next run
   if (same && plain_range(m)) {              // as good as always: whole batches, nothing to ask in between
     const int whole = c.runs / (U * NTH);
-    const float off = -(m * LOG2E);
+    const float off = -offset_of(m);
     auto put = [&](const Batch<T>& b) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -391,11 +418,11 @@ template <int NTH, bool CLUSTER> struct Place {
 // One pass, two 64-byte batches a thread under way.  4096 rows x 65536 bfloat16 88 us = 6.1 TB/s, 93 % of the copy rate; 131072 x 512,
 // where a row is one memory latency and two reductions, 29 us = 4.6 TB/s.  Rows walked by as many CTAs as fit lost to CTAs handed out
 // by the hardware: no gain on full batches, 140 against 113 us with a third of the rows masked.
-// zb, sum, top: log2 of exp(z_label) and the sum, both relative to the reference, and the reference, as log2_rel and exp_all take
-// them; from these the preference loss has its log-probabilities in 64 bits and its gradient.  Either these or logp.
+// zl, sum, top: the label's entry, the sum and the reference, from which the preference loss has its log-probabilities in 64 bits and
+// its gradient.  Either these or logp.
 template <typename T, int NTH, bool CLUSTER>
 __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>::CTAS) k_logp(adacgd_token_rows r, float* __restrict__ logp, float* __restrict__ lse,
-                                                                   float* __restrict__ zb, float* __restrict__ sum,
+                                                                   float* __restrict__ zl, float* __restrict__ sum,
                                                                    float* __restrict__ top) {
   __shared__ Soft sh[32], xch[8];
   pdl_trigger();
@@ -417,12 +444,11 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
   const float z = y >= 0 && y < vocab ? to_f(x[y]) : NAN;
   const Soft a = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut_row(x, vocab, at.part, at.parts), at.t), sh, xch);
   if (at.t == 0 && at.part == 0) {
-    const float tz = log2_rel(z, a.m);
     if (logp) {
-      logp[row] = (tz - log2f(a.s)) * LN2;
-      if (lse) lse[row] = base_of(a.m) + logf(a.s);
+      logp[row] = (float)logp64(z, a);
+      if (lse) lse[row] = (float)lse64(a);
     } else {
-      zb[row] = tz;
+      zl[row] = z;
       sum[row] = a.s;
       top[row] = a.m;
     }
@@ -497,8 +523,8 @@ __device__ __forceinline__ double finish_pair(const adacgd_preference_args& a, l
 
 // `slices` CTAs a pair.  One: it also finishes the pair, and the last CTA of all takes the mean of the losses.  More: the last CTA
 // adds the slices' six sums of each pair and finishes the pairs.
-__global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, const float* zb, const float* sum,
-                                                   float* __restrict__ coef, double* __restrict__ part, u32 slices, u32* ticket) {
+__global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, const float* zl, const float* sum,
+                                                   const float* top, float* __restrict__ coef, double* __restrict__ part, u32 slices, u32* ticket) {
   __shared__ double sh[PAIR_NT / 32];
   pdl_wait();
   pdl_trigger();   // the gradient kernel is large: it is let in when this one has its operands
@@ -512,7 +538,7 @@ __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, con
     total[k] = diff[k] = cnt[k] = 0.0;
     for (long long t = lo + slice * PAIR_NT + threadIdx.x; t < hi; t += (long long)slices * PAIR_NT) {
       if (a.rows.mask && !a.rows.mask[t]) continue;
-      const double logp = ((double)zb[t] - log2((double)sum[t])) * 0.6931471805599453;
+      const double logp = logp64(zl[t], Soft{top[t], sum[t]});
       cnt[k] += 1.0;
       total[k] += logp;
       diff[k] += logp - (double)a.ref_logp[t];
@@ -560,7 +586,7 @@ __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, con
 // bfloat16, two thirds of the tokens counted, 116 us against a floor of 67 for one read and one write, 94 for the two reads.
 template <typename T, int NTH>
 __global__ void __launch_bounds__(Place<NTH, false>::CTA, Place<NTH, false>::CTAS) k_preference_grad(adacgd_preference_args a, const float* coef,
-                                                                            const float* zb, const float* sum,
+                                                                            const float* zl, const float* sum,
                                                                             const float* top, u32 parts) {
   const Place<NTH, false> at;
   const long long turn = parts == 1 ? at.row : at.row / parts;
@@ -578,8 +604,8 @@ __global__ void __launch_bounds__(Place<NTH, false>::CTA, Place<NTH, false>::CTA
     return;
   }
   const T* x = (const T*)a.rows.logits + row * a.rows.logits_stride;
-  thread_grad<T, NTH, false>(x, d, cut_row(x, vocab, part, (int)parts), at.t, same_phase(x, d), y >= 0 && y < vocab ? (int)y : -1, zb[row], coef[q],
-                      top[row], sum[row]);
+  thread_grad<T, NTH, false>(x, d, cut_row(x, vocab, part, (int)parts), at.t, same_phase(x, d), y >= 0 && y < vocab ? (int)y : -1,
+                             log2_rel(zl[row], top[row]), coef[q], top[row], sum[row]);
 }
 
 // --------------------------------------------------------------------------
@@ -735,7 +761,7 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
     const float z = label >= 0 ? to_f(x[label]) : NAN;
     const Cut cut = cut_row(x, vocab, at.part, at.parts);
     const Soft v = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut, at.t), sh, xch);
-    const float tz = log2_rel(z, v.m), logp = (tz - log2f(v.s)) * LN2;
+    const float logp = (float)logp64(z, v);
     // the same weight for all, or the sequence's
     const long long q = a.per_sequence ? seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences) : 0;
     pdl_wait();
@@ -753,7 +779,7 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
         tc[row] = tok.clipped ? 1.f : 0.f;
       }
     }
-    if (d) thread_grad<T, NTH, true>(x, d, cut, at.t, same_phase(x, d), label, tz, a.grad_scale * (w * tok.slope), v.m, v.s);
+    if (d) thread_grad<T, NTH, true>(x, d, cut, at.t, same_phase(x, d), label, log2_rel(z, v.m), a.grad_scale * (w * tok.slope), v.m, v.s);
   }
   if (!SMALL) return;
   __syncthreads();
@@ -884,10 +910,10 @@ Split split_twice(long long rows, long long vocab, int size, const Where& at) {
                       : BY_THREADS(s, call))
 
 template <typename T>
-cudaError_t logp_t(const adacgd_token_rows& r, float* logp, float* lse, float* zb, float* sum, float* top, const Where& at) {
+cudaError_t logp_t(const adacgd_token_rows& r, float* logp, float* lse, float* zl, float* sum, float* top, const Where& at) {
   const Split s = split_once(r.tokens, r.vocab, (int)sizeof(T), at);
   return BY_SPLIT_ONCE(s, (launch(k_logp<T, NTH, CL>, ctas(r.tokens, Place<NTH, CL>::ROWS, s.cluster), Place<NTH, CL>::CTA, s.cluster, false,
-                             at.stream, 0, r, logp, lse, zb, sum, top)));
+                             at.stream, 0, r, logp, lse, zl, sum, top)));
 }
 
 template <typename T>
@@ -903,7 +929,7 @@ int preference_t(const TrainScratch& s, const adacgd_preference_args& a, const W
   long long slices = rows / a.rows.sequences / (2 * PAIR_NT);
   if (slices * pairs > at.sms) slices = at.sms / pairs;
   if (slices < 1) slices = 1;
-  if (launch(k_pairs, (unsigned)(pairs * slices), PAIR_NT, 1, rows > 0, at.stream, 0, a, s.tok_a, s.tok_b, s.seq, s.part, (u32)slices,
+  if (launch(k_pairs, (unsigned)(pairs * slices), PAIR_NT, 1, rows > 0, at.stream, 0, a, s.tok_a, s.tok_b, s.tok_c, s.seq, s.part, (u32)slices,
              s.tickets) != cudaSuccess)
     return -1;
   if (a.dlogits && rows) {

@@ -146,3 +146,74 @@ def test_rows_far_from_zero(ops, vocab, dtype):
     margin, sums = torch.empty(seqs // 2, device="cuda"), torch.empty(seqs, device="cuda")
     ops.preference_loss(z[:seqs], y[:seqs], torch.zeros(seqs, device="cuda"), loss, d[:seqs], sequences=seqs, seq_logp=sums, margin=margin)
     close(sums, wl[:seqs], tol[:seqs] + 4 * E * np.abs(wl[:seqs]), "seq_logp")
+
+
+def test_label_at_the_types_lowest_value_has_a_finite_logp(ops):
+    """A label that a mask has set to the type's lowest value: its log-probability is that value, not -inf, and two of them differ
+    by nothing."""
+    for dtype in ("f32", "bf16"):
+        dt = TYPES[dtype]
+        for vocab in (40, 3000, 40000, 290001):
+            z, y, _ = make_rows(4, vocab, dt)
+            lowest = torch.finfo(dt).min
+            z[torch.arange(4, device="cuda"), y] = lowest
+            logp = torch.empty(4, device="cuda")
+            ops.token_logp(z, y, logp)
+            # beside a number of 2^127 log s is nothing: one rounding of the product and one of the result
+            close(logp, np.full(4, float(lowest)), 4 * E * abs(float(lowest)), "logp")
+            loss, margin, d = torch.empty(1, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(z)
+            ops.preference_loss(z, y, logp, loss, d, sequences=2, margin=margin)
+            # the reference is the value itself: what is left of the difference is a rounding of 2^128, but no NaN
+            assert torch.isfinite(margin).all() and torch.isfinite(loss).all() and not torch.isnan(d).any()
+
+
+# ----------------------------------------------------------------------------- accuracy of log-probabilities
+
+@pytest.mark.parametrize("dtype,n,vocab", [("bf16", 4096, 4000), ("bf16", 2048, 50001), ("bf16", 1024, 131072), ("f32", 2048, 8000), ("f16", 4096, 300)])
+def test_log_probabilities_are_at_least_as_exact_as_the_plain_form(ops, dtype, n, vocab):
+    """Root mean square error over many tokens against binary64, beside that of the formula in elementary binary32 operations
+    (which has the maximum subtracted first).  Errors of a few roundings each, independent from row to row: with a thousand rows the two
+    figures are known to a few per cent."""
+    dt = TYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    z = (torch.randn(n, vocab, generator=gen, device="cuda") * 2).to(dt)
+    y = torch.randint(vocab, (n,), generator=gen, device="cuda")
+    z.scatter_add_(1, y[:, None], (torch.randn(n, 1, generator=gen, device="cuda") * 3 + 6).to(dt))
+    logp, lse, plogp = (torch.empty(n, device="cuda") for _ in range(3))
+    ops.token_logp(z, y, logp, lse=lse)
+    ops.policy_loss(z, y, torch.zeros(n, device="cuda"), torch.ones(n, device="cuda"), torch.empty(1, device="cuda"), logp=plogp)
+    f = z.float()
+    top = f.amax(1, keepdim=True)
+    total = (f - top).exp().sum(1)
+    plain = f.gather(1, y[:, None])[:, 0] - top[:, 0] - total.log()
+    plain_lse = top[:, 0] + total.log()
+    wide = z.double()
+    want_lse = torch.logsumexp(wide, 1)
+    want = wide.gather(1, y[:, None])[:, 0] - want_lse
+    rms = lambda a, b: (a.double() - b).square().mean().sqrt().item()  # noqa: E731
+    assert rms(logp, want) <= rms(plain, want)
+    assert rms(plogp, want) <= rms(plain, want)
+    assert rms(lse, want_lse) <= 1.25 * rms(plain_lse, want_lse)      # both end in one rounding of the same size
+
+
+@pytest.mark.parametrize("vocab", [7, 1001, 40000, 290001])
+def test_rows_on_both_sides_of_the_largest_offset(ops, vocab):
+    """Logits around +-2^21, where the kernels' form of the exponent changes, a quarter or half a unit apart: one thread's share of a row
+    may lie below it, another's beyond.  Differences are exact, as above."""
+    rng = np.random.default_rng(vocab)
+    steps = rng.integers(-40, 41, vocab) * 0.25
+    rows = [at + s for at in (-2.0 ** 21, 2.0 ** 21) for s in (steps, np.sort(steps), np.sort(steps)[::-1])]
+    z = dev(np.stack(rows))
+    y = torch.from_numpy(rng.integers(0, vocab, len(rows))).cuda()
+    logp = torch.empty(len(rows), device="cuda")
+    ops.token_logp(z, y, logp)
+    hz = host(z)
+    wl, _, soft = O.token_logp(hz, y.cpu().numpy())
+    tol = (vocab / 128 + 64) * E + 4 * E * (hz.max(1) - hz.min(1) + np.log(vocab))
+    close(logp, wl, tol, "logp")
+    loss, d = torch.empty(1, device="cuda"), torch.empty_like(z)
+    ops.policy_loss(z, y, dev(wl), torch.ones(len(rows), device="cuda"), loss, d)
+    per = -np.exp(wl - host(dev(wl))) / len(rows)
+    want = -per[:, None] * soft
+    want[np.arange(len(rows)), y.cpu().numpy()] += per
+    close(d, want, grad_tol(want, per, soft, tol, torch.float32, c_err=(2 * tol + 8 * E) / len(rows)), "dlogits")
