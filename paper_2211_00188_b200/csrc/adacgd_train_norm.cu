@@ -620,7 +620,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
       const long long now = row + k * w.step;
       if (live[k]) {
         const uint4* const at = ring + (stage + k) * ARRAYS * A;
-        const float p = sums[2 * k] * inv, cq = -(rs[k] * rs[k]) * (sums[2 * k + 1] * inv);
+        const float p = sums[2 * k] * inv, cq = -rs[k] * (sums[2 * k + 1] * inv);
         const F2 mu2 = f2(-mu[k], -mu[k]), rs2 = f2(rs[k], rs[k]), cq2 = f2(cq, cq), p2 = f2(-p, -p);
         T* const dx = (T*)a.dx + now * a.dx_stride;
         T* const dr = a.dresidual ? (T*)a.dresidual + now * a.dresidual_stride : nullptr;
@@ -638,9 +638,9 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
             pairs_of(y, y2);
             pairs_of(h, h2);
             pairs_of(v, v2);
-            // rs (g - p) - (s - mu) rs^2 q [+ dsum]
+            // rs ((g - p) - (s - mu) (rs q)) [+ dsum]: rs^2 may be out of range where rs is not
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y2[j] = fma2(add2(h2[j], mu2), cq2, mul2(fma2(y2[j], v2[j], p2), rs2));
+            for (int j = 0; j < 4; ++j) y2[j] = mul2(fma2(add2(h2[j], mu2), cq2, fma2(y2[j], v2[j], p2)), rs2);
             if (ARRAYS == 3) {
               take_run<T, CTA>(at + 2 * A, r, v);
               pairs_of(v, v2);
@@ -657,7 +657,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
           }
         }
         if (EDGE && edge >= 0) {
-          float y = fmaf(es[k] - mu[k], cq, (fmaf(ey[k], ew, -p)) * rs[k]);
+          float y = fmaf(es[k] - mu[k], cq, fmaf(ey[k], ew, -p)) * rs[k];
           if (ARRAYS == 3) y += ed[k];
           if (dr) dr[edge] = from_f<T>(y);
           dx[edge] = from_f<T>(d.on ? drop_one(y, (u64)now * (u64)cols + edge, d) : y);

@@ -6,7 +6,7 @@ import torch
 
 import paper_2211_00188_b200 as pkg
 from oracle import training_oracle as O
-from test_training_gpu import E, TYPES, close, dev, grad_tol, host, logp_tol, make_rows
+from test_training_gpu import E, TINY, TYPES, U, close, dev, grad_tol, host, logp_tol, make_rows, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -217,3 +217,33 @@ def test_rows_on_both_sides_of_the_largest_offset(ops, vocab):
     want = -per[:, None] * soft
     want[np.arange(len(rows)), y.cpu().numpy()] += per
     close(d, want, grad_tol(want, per, soft, tol, torch.float32, c_err=(2 * tol + 8 * E) / len(rows)), "dlogits")
+
+
+# ----------------------------------------------------------------------------- layer norm, backward
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(9, 64), (9, 65), (40, 1001), (300, 1024), (5, 8192), (3, 16384), (3, 20001)])
+@pytest.mark.parametrize("scale", [1e22, 1e25, 1e-22])
+@pytest.mark.parametrize("with_dsum", [False, True])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_norm_backward_of_rows_with_a_large_or_small_spread(ops, dtype, rows, cols, scale, with_dsum, shift):
+    """rstd is far from one, its square no number of binary32; every factor of the formula is.  `shift`: off the runs."""
+    dt = TYPES[dtype]
+    rng = np.random.default_rng(rows + cols)
+    s = dev(rng.normal(size=(rows, cols)) * scale, dt)
+    hs = host(s)
+    mean, rstd = dev(hs.mean(1)), dev(1 / hs.std(1))
+    dy, w = dev(rng.normal(size=(rows, cols)), dt), dev(rng.normal(size=cols) * 0.3 + 1)
+    dsum = dev(rng.normal(size=(rows, cols)) / scale, dt) if with_dsum else None
+    dx, dw = strided(torch.zeros_like(s), 0, shift), torch.empty(cols, device="cuda")
+    ops.layer_norm_backward(strided(dy, 0, shift), strided(s, 0, shift), mean, rstd, dx, weight=w, dweight=dw,
+                            dsum=strided(dsum, 0, shift) if with_dsum else None)
+    hd, hw = host(dy), host(w)
+    want, _, ww, _ = O.layer_norm_backward(hd, hs, host(mean), host(rstd), hw, host(dsum) if with_dsum else None)
+    r = host(rstd)[:, None]
+    h = np.abs(hs - host(mean)[:, None]) * r + E * np.abs(hs) * r
+    g = np.abs(hd * hw)
+    K = cols / 128 + 32
+    mag = r * (g + g.mean(1, keepdims=True) + h * (g * h).mean(1, keepdims=True)) + (np.abs(host(dsum)) if with_dsum else 0)
+    close(dx, want, U[dt] * np.abs(want) + K * E * mag + TINY[dt], "dx")
+    close(dw, ww, (rows + 33) * E * (np.abs(hd) * h).sum(0), "dweight")
