@@ -482,7 +482,11 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
   const T* const s_in = (const T*)a.s;
   const T* const dsum = (const T*)a.dsum;
   const u32 ring32 = (u32)__cvta_generic_to_shared(ring);
-  const float inv = 1.f / (float)cols;
+  const float inv = 1.f / (float)cols, less = fmaf(-inv, (float)cols, 1.f) * inv;
+  auto mean_of = [&](float sum) {      // sum / cols with one rounding, 1 / cols being inv + less: a constant's mean is the constant
+    const float m = sum * inv;
+    return fabsf(m) < INFINITY ? fmaf(sum, inv, sum * less) : m;
+  };
   Held<P> wt[R];
   F2 dw[R][4], db[R][4];
 #pragma unroll
@@ -620,7 +624,7 @@ __global__ void __launch_bounds__(Walk<T, NTH, R, ARRAYS>::CTA) k_norm_bwd(const
       const long long now = row + k * w.step;
       if (live[k]) {
         const uint4* const at = ring + (stage + k) * ARRAYS * A;
-        const float p = sums[2 * k] * inv, cq = -rs[k] * (sums[2 * k + 1] * inv);
+        const float p = mean_of(sums[2 * k]), cq = -rs[k] * mean_of(sums[2 * k + 1]);
         const F2 mu2 = f2(-mu[k], -mu[k]), rs2 = f2(rs[k], rs[k]), cq2 = f2(cq, cq), p2 = f2(-p, -p);
         T* const dx = (T*)a.dx + now * a.dx_stride;
         T* const dr = a.dresidual ? (T*)a.dresidual + now * a.dresidual_stride : nullptr;

@@ -247,3 +247,17 @@ def test_norm_backward_of_rows_with_a_large_or_small_spread(ops, dtype, rows, co
     mag = r * (g + g.mean(1, keepdims=True) + h * (g * h).mean(1, keepdims=True)) + (np.abs(host(dsum)) if with_dsum else 0)
     close(dx, want, U[dt] * np.abs(want) + K * E * mag + TINY[dt], "dx")
     close(dw, ww, (rows + 33) * E * (np.abs(hd) * h).sum(0), "dweight")
+
+
+@pytest.mark.parametrize("cols", [41, 47, 49, 82, 94, 98, 976, 1001, 8200, 20000])
+@pytest.mark.parametrize("p", [0.0, 0.25])
+def test_norm_backward_takes_out_a_constant_exactly(ops, cols, p):
+    """dout constant, h = +-1 in pairs: every sum is exact in binary32 (multiples of 2^20 below 2^44), mean(g) is g and mean(g h)
+    is 0, so ds is 0.  1 / cols is no binary number, and a product with its rounding misses g by a unit in the last place for some cols."""
+    rows = 5
+    s = torch.zeros(rows, cols, device="cuda")
+    s[:, 0:cols // 2 * 2:2], s[:, 1:cols // 2 * 2:2] = 1.0, -1.0
+    dy = torch.full_like(s, 2.0 ** 20)
+    dx = torch.empty_like(s)
+    ops.layer_norm_backward(dy, s, torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda"), dx, p=p, seed=1)
+    assert not dx.any()
