@@ -151,8 +151,8 @@ adacgd_status adacgd_token_logp(adacgd_train* t, const adacgd_token_rows* rows, 
  *   SIGMOID  l = -(1 - e) log sigma(h) - e log sigma(-h), e = label_smoothing
  *   HINGE    l = max(0, 1 - h)
  *   SQUARE   l = (h / beta - 1 / (2 beta))^2
- * A sequence without counted tokens has d_q = 0.  The differences are taken token by token because the two sums are large
- * and nearly equal. */
+ * A sequence without counted tokens has d_q = 0.  With e = 0 the second logarithm is left out, infinite or not.  The
+ * differences are taken token by token because the two sums are large and nearly equal. */
 #define ADACGD_PREF_SIGMOID 0
 #define ADACGD_PREF_HINGE 1
 #define ADACGD_PREF_SQUARE 2
@@ -176,7 +176,7 @@ adacgd_status adacgd_preference_loss(adacgd_train* t, const adacgd_preference_ar
  *   l_t = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_beta (exp(u) - u - 1),   loss = sum_t w_t l_t,
  * w_t = 1 / (counted tokens), or with per_sequence 1 / (sequences with a counted token * counted tokens of t's sequence).
  * Where the clipped term is the smaller one its gradient is zero; where the two are equal the gradient is the first's.
- * No counted token: loss 0.  kl_beta = 0 with ref_logp = NULL leaves the KL term out. */
+ * No counted token: loss 0.  kl_beta = 0 leaves the KL term out of loss and gradient, with ref_logp or without. */
 typedef struct {
   adacgd_token_rows rows;
   const float* old_logp;    /* [tokens] log-probabilities under the policy that answered */

@@ -127,7 +127,7 @@ def preference(logits, labels, ref_logp, mask=None, sequences=None, seq_start=No
     h = beta * (np.array(diff[:half]) - np.array(diff[half:]))
     if kind == "sigmoid":
         e = label_smoothing
-        loss = (1 - e) * np.logaddexp(0, -h) + e * np.logaddexp(0, h)
+        loss = (1 - e) * np.logaddexp(0, -h) + (e * np.logaddexp(0, h) if e else 0.0)      # weight zero: left out
         g = e / (1 + np.exp(-h)) - (1 - e) / (1 + np.exp(h))
     elif kind == "hinge":
         loss, g = np.maximum(0, 1 - h), np.where(h < 1, -1.0, 0.0)
@@ -165,8 +165,9 @@ def policy(logits, labels, old_logp, advantages, mask=None, sequences=None, seq_
         l, c = (-held, 0.0) if gain > held else (-gain, -gain)        # NaN goes through
         if ref_logp is not None:
             u = float(ref_logp[t]) - logp[t]
-            l += kl_beta * (np.expm1(u) - u)
-            c += kl_beta * -np.expm1(u)
+            if kl_beta:                                                # weight zero: left out
+                l += kl_beta * (np.expm1(u) - u)
+                c += kl_beta * -np.expm1(u)
             kl_sum += np.expm1(u) - u
         clipped += gain > held
         loss += w[t] * l

@@ -502,7 +502,7 @@ __device__ __forceinline__ double finish_pair(const adacgd_preference_args& a, l
   double l, g;
   if (a.kind == ADACGD_PREF_SIGMOID) {
     const double tail = log1p(exp(-fabs(h)));               // -log sigma(|h|)
-    l = (1.0 - e) * (tail + fmax(-h, 0.0)) + e * (tail + fmax(h, 0.0));
+    l = (1.0 - e) * (tail + fmax(-h, 0.0)) + (e > 0.0 ? e * (tail + fmax(h, 0.0)) : 0.0);   // h = inf: no 0 inf
     const double sg = 1.0 / (1.0 + exp(-h)), sn = 1.0 / (1.0 + exp(h));
     g = e * sg - (1.0 - e) * sn;
     if (h != h) l = h;
@@ -664,8 +664,10 @@ __device__ __forceinline__ Token token_loss(float logp, float old, float A, bool
   if (with_ref) {
     const float u = ref - logp, e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0
     k.kl = e1 - u;
-    k.slope = k.slope - kl_beta * e1;
-    k.loss = k.loss + kl_beta * k.kl;
+    if (kl_beta > 0.f) {                          // else the term is a statistic alone, which may overflow
+      k.slope = k.slope - kl_beta * e1;
+      k.loss = k.loss + kl_beta * k.kl;
+    }
   }
   return k;
 }

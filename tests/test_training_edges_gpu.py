@@ -261,3 +261,34 @@ def test_norm_backward_takes_out_a_constant_exactly(ops, cols, p):
     dx = torch.empty_like(s)
     ops.layer_norm_backward(dy, s, torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda"), dx, p=p, seed=1)
     assert not dx.any()
+
+
+# ----------------------------------------------------------------------------- terms of weight zero
+
+def test_preference_without_smoothing_survives_an_impossible_answer(ops):
+    """A rejected answer of probability zero: h = +inf, -log sigma(h) = 0.  The smoothing term has weight zero and is left out."""
+    z, y, _ = make_rows(4, 70, torch.float32)
+    z[3, y[3]] = -float("inf")
+    ref = torch.zeros(4, device="cuda")
+    loss, margin, d = torch.empty(1, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(z)
+    ops.preference_loss(z, y, ref, loss, d, sequences=2, margin=margin)
+    assert margin.item() == float("inf") and loss.item() == 0.0 and not d.any()
+    z2 = torch.cat([z[2:], z[:2]]).contiguous()                  # now the preferred one
+    y2 = torch.cat([y[2:], y[:2]])
+    ops.preference_loss(z2, y2, ref, loss, d, sequences=2, margin=margin)
+    assert margin.item() == -float("inf") and loss.item() == float("inf")
+
+
+@pytest.mark.parametrize("per_sequence", [False, True])
+def test_policy_statistics_without_the_kl_term_leave_the_loss_alone(ops, per_sequence):
+    """kl_beta = 0 with ref_logp: the KL statistic may overflow, loss and gradient are those without it."""
+    z, y, rng = make_rows(6, 300, torch.float32)
+    logp = O.token_logp(host(z), y.cpu().numpy())[0]
+    old, adv, ref = dev(logp + 0.05), dev(rng.normal(size=6)), dev(logp + 0.1)
+    ref[2] = 200.0                                               # exp(u) overflows binary32
+    loss, stats, d = torch.empty(1, device="cuda"), torch.empty(3, device="cuda"), torch.empty_like(z)
+    other, e = torch.empty(1, device="cuda"), torch.empty_like(z)
+    ops.policy_loss(z, y, old, adv, loss, d, sequences=2, per_sequence=per_sequence, ref_logp=ref, stats=stats)
+    ops.policy_loss(z, y, old, adv, other, e, sequences=2, per_sequence=per_sequence)
+    assert torch.isfinite(other).all() and torch.equal(loss, other) and torch.equal(d, e)
+    assert stats[0].item() == float("inf")
