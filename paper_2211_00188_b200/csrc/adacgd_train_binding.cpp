@@ -4,11 +4,15 @@
 //
 // Every function takes the handle first and returns the entry point's status, or RETRY when another stream or device is
 // current (the Python side orders the streams and calls again with the handle's `force` set).  Wrong arguments raise ValueError.
+//
+// The calls are not recorded by autograd.  So an output that requires a gradient is refused while gradients are recorded, and the
+// version of what a call has written moves on, as after any other modification in place.
 #include <Python.h>
 
 #include <string>
 
 #include <ATen/core/Tensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -40,19 +44,32 @@ int type_code(at::ScalarType t) {
   }
 }
 
+enum Use { IN, OUT };
+
 const at::Tensor* tensor(PyObject* o, const char* name, bool optional) {
   if (o == Py_None && optional) return nullptr;
   if (!THPVariable_Check(o)) refuse(name, "must be a tensor");
   return &THPVariable_Unpack(o);
 }
 
-// What the matrices of a call share: set by the first.
+// What the matrices of a call share: set by the first.  And the call's outputs.
 struct Shape {
   const Handle* h;
+  const at::Tensor* written[8];
+  int outputs = 0;
   int64_t rows = 0, cols = 0;
   at::ScalarType type = at::kFloat;
   int code = 0;
 
+  explicit Shape(const Handle* handle) : h(handle) {}
+  void output(const at::Tensor& t, const char* name) {
+    if (t.requires_grad() && c10::GradMode::is_enabled()) refuse(name, "requires a gradient, and the call is not recorded: use torch.no_grad() or a detached tensor");
+    written[outputs++] = &t;
+  }
+  void count_versions() const {
+    for (int i = 0; i < outputs; ++i)
+      if (!written[i]->is_inference()) written[i]->unsafeGetTensorImpl()->bump_version();
+  }
   void lead(PyObject* o, const char* name, const void** p, int64_t* stride) {
     const at::Tensor& t = *tensor(o, name, false);
     type = t.scalar_type();
@@ -62,7 +79,7 @@ struct Shape {
     cols = t.size(1);
     place(t, name, p, stride);
   }
-  void matrix(PyObject* o, const char* name, bool optional, const void** p, int64_t* stride) const {
+  void matrix(PyObject* o, const char* name, Use use, bool optional, const void** p, int64_t* stride) {
     *p = nullptr;
     *stride = 0;
     const at::Tensor* t = tensor(o, name, optional);
@@ -71,6 +88,7 @@ struct Shape {
     if (t->dim() != 2 || t->size(0) != rows || t->size(1) != cols)
       refuse(name, "must have the shape (" + std::to_string(rows) + ", " + std::to_string(cols) + ")");
     place(*t, name, p, stride);
+    if (use == OUT) output(*t, name);
   }
   void place(const at::Tensor& t, const char* name, const void** p, int64_t* stride) const {
     if (!t.is_cuda() || t.get_device() != h->index) refuse(name, "must be on cuda:" + std::to_string(h->index));
@@ -83,11 +101,13 @@ struct Shape {
     *p = t.data_ptr();
     *stride = s;
   }
-  void* vector(PyObject* o, const char* name, bool optional, int64_t n, at::ScalarType want) const {
+  void* vector(PyObject* o, const char* name, Use use, bool optional, int64_t n, at::ScalarType want) {
     const at::Tensor* t = tensor(o, name, optional);
     if (!t) return nullptr;
     if (t->scalar_type() != want) refuse(name, std::string("must have the type ") + c10::toString(want));
-    return contiguous(*t, name, n);
+    void* const p = contiguous(*t, name, n);
+    if (use == OUT) output(*t, name);
+    return p;
   }
   void* contiguous(const at::Tensor& t, const char* name, int64_t n) const {
     if (!t.is_cuda() || t.get_device() != h->index) refuse(name, "must be on cuda:" + std::to_string(h->index));
@@ -95,21 +115,27 @@ struct Shape {
     return t.data_ptr();
   }
   // weight-like vectors: all of the matrices' type or all float32
-  int params(std::initializer_list<std::pair<PyObject*, const char*>> list, void** out) const {
+  struct Param {
+    PyObject* o;
+    const char* name;
+    Use use;
+  };
+  int params(std::initializer_list<Param> list, void** out) {
     at::ScalarType want = type;
     bool first = true;
-    for (const auto& e : list) {
-      const at::Tensor* t = tensor(e.first, e.second, true);
+    for (const Param& e : list) {
+      const at::Tensor* t = tensor(e.o, e.name, true);
       *out = nullptr;
       if (t) {
         if (first) {
           want = t->scalar_type();
-          if (want != type && want != at::kFloat) refuse(e.second, "must be float32 or of the matrices' type");
+          if (want != type && want != at::kFloat) refuse(e.name, "must be float32 or of the matrices' type");
           first = false;
         } else if (t->scalar_type() != want) {
-          refuse(e.second, "must have the type of the other weight-like arguments");
+          refuse(e.name, "must have the type of the other weight-like arguments");
         }
-        *out = contiguous(*t, e.second, cols);
+        *out = contiguous(*t, e.name, cols);
+        if (e.use == OUT) output(*t, e.name);
       }
       ++out;
     }
@@ -182,6 +208,7 @@ PyObject* call(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, F body) {
                           (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h->index).stream() == h->stream);
     };
     status = body(s, ready);
+    if (status == ADACGD_OK) s.count_versions();
     return PyLong_FromLong(status);
   } catch (const Refused& r) {
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, r.what.c_str());
@@ -191,16 +218,16 @@ PyObject* call(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, F body) {
   return nullptr;
 }
 
-#define MAT(name, i, optional)                                         \
-  s.matrix(a[i], #name, optional, (const void**)&r.name, &r.name##_stride)
+#define MAT(name, i, use, optional)                                         \
+  s.matrix(a[i], #name, use, optional, (const void**)&r.name, &r.name##_stride)
 
 // (handle, x, out, residual, p, seed, offset)
 PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(a, n, 7, [&](Shape& s, auto ready) -> long {
     adacgd_dropout_args r;
     s.lead(a[1], "x", &r.x, &r.x_stride);
-    MAT(out, 2, false);
-    MAT(residual, 3, true);
+    MAT(out, 2, OUT, false);
+    MAT(residual, 3, IN, true);
     r.rows = s.rows;
     r.cols = s.cols;
     r.dtype = s.code;
@@ -215,15 +242,15 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(a, n, 13, [&](Shape& s, auto ready) -> long {
     adacgd_norm_args r;
     s.lead(a[1], "x", &r.x, &r.x_stride);
-    MAT(out, 2, false);
-    MAT(residual, 6, true);
-    MAT(sum, 7, true);
+    MAT(out, 2, OUT, false);
+    MAT(residual, 6, IN, true);
+    MAT(sum, 7, OUT, true);
     void* p[2];
-    r.param_dtype = s.params({{a[3], "weight"}, {a[4], "bias"}}, p);
+    r.param_dtype = s.params({{a[3], "weight", IN}, {a[4], "bias", IN}}, p);
     r.weight = p[0];
     r.bias = p[1];
-    r.mean = (float*)s.vector(a[8], "mean", true, s.rows, at::kFloat);
-    r.rstd = (float*)s.vector(a[9], "rstd", true, s.rows, at::kFloat);
+    r.mean = (float*)s.vector(a[8], "mean", OUT, true, s.rows, at::kFloat);
+    r.rstd = (float*)s.vector(a[9], "rstd", OUT, true, s.rows, at::kFloat);
     r.rows = s.rows;
     r.cols = s.cols;
     r.dtype = s.code;
@@ -239,14 +266,14 @@ PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(a, n, 14, [&](Shape& s, auto ready) -> long {
     adacgd_norm_backward_args r;
     s.lead(a[1], "dout", &r.dout, &r.dout_stride);
-    MAT(s, 2, false);
-    MAT(dx, 5, false);
-    MAT(dsum, 9, true);
-    MAT(dresidual, 10, true);
-    r.mean = (const float*)s.vector(a[3], "mean", false, s.rows, at::kFloat);
-    r.rstd = (const float*)s.vector(a[4], "rstd", false, s.rows, at::kFloat);
+    MAT(s, 2, IN, false);
+    MAT(dx, 5, OUT, false);
+    MAT(dsum, 9, IN, true);
+    MAT(dresidual, 10, OUT, true);
+    r.mean = (const float*)s.vector(a[3], "mean", IN, false, s.rows, at::kFloat);
+    r.rstd = (const float*)s.vector(a[4], "rstd", IN, false, s.rows, at::kFloat);
     void* p[3];
-    r.param_dtype = s.params({{a[6], "weight"}, {a[7], "dweight"}, {a[8], "dbias"}}, p);
+    r.param_dtype = s.params({{a[6], "weight", IN}, {a[7], "dweight", OUT}, {a[8], "dbias", OUT}}, p);
     r.weight = p[0];
     r.dweight = p[1];
     r.dbias = p[2];
@@ -263,8 +290,8 @@ PyObject* token_logp(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(a, n, 6, [&](Shape& s, auto ready) -> long {
     adacgd_token_rows r;
     s.token_rows(&r, a[1], a[2], a[4], Py_None, Py_None);
-    float* logp = (float*)s.vector(a[3], "logp", false, s.rows, at::kFloat);
-    float* lse = (float*)s.vector(a[5], "lse", true, s.rows, at::kFloat);
+    float* logp = (float*)s.vector(a[3], "logp", OUT, false, s.rows, at::kFloat);
+    float* lse = (float*)s.vector(a[5], "lse", OUT, true, s.rows, at::kFloat);
     return ready() ? (long)adacgd_token_logp(s.h->ctx, &r, logp, lse) : RETRY;
   });
 }
@@ -275,16 +302,16 @@ PyObject* preference_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(a, n, 16, [&](Shape& s, auto ready) -> long {
     adacgd_preference_args r;
     s.token_rows(&r.rows, a[1], a[2], a[6], a[8], a[7]);
-    r.ref_logp = (const float*)s.vector(a[3], "ref_logp", false, s.rows, at::kFloat);
-    r.loss = (float*)s.vector(a[4], "loss", false, 1, at::kFloat);
-    MAT(dlogits, 5, true);
+    r.ref_logp = (const float*)s.vector(a[3], "ref_logp", IN, false, s.rows, at::kFloat);
+    r.loss = (float*)s.vector(a[4], "loss", OUT, false, 1, at::kFloat);
+    MAT(dlogits, 5, OUT, true);
     r.beta = (float)number(a[9]);
     r.kind = (int32_t)bits(a[10]);
     r.label_smoothing = (float)number(a[11]);
     r.length_normalized = truth(a[12]);
     r.grad_scale = (float)number(a[13]);
-    r.margin = (float*)s.vector(a[14], "margin", true, r.rows.sequences / 2, at::kFloat);
-    r.seq_logp = (float*)s.vector(a[15], "seq_logp", true, r.rows.sequences, at::kFloat);
+    r.margin = (float*)s.vector(a[14], "margin", OUT, true, r.rows.sequences / 2, at::kFloat);
+    r.seq_logp = (float*)s.vector(a[15], "seq_logp", OUT, true, r.rows.sequences, at::kFloat);
     r.reserved = 0;
     return ready() ? (long)adacgd_preference_loss(s.h->ctx, &r) : RETRY;
   });
@@ -296,18 +323,18 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(a, n, 18, [&](Shape& s, auto ready) -> long {
     adacgd_policy_args r;
     s.token_rows(&r.rows, a[1], a[2], a[7], a[9], a[8]);
-    r.old_logp = (const float*)s.vector(a[3], "old_logp", false, s.rows, at::kFloat);
-    r.advantages = (const float*)s.vector(a[4], "advantages", false, s.rows, at::kFloat);
-    r.loss = (float*)s.vector(a[5], "loss", false, 1, at::kFloat);
-    MAT(dlogits, 6, true);
-    r.ref_logp = (const float*)s.vector(a[10], "ref_logp", true, s.rows, at::kFloat);
+    r.old_logp = (const float*)s.vector(a[3], "old_logp", IN, false, s.rows, at::kFloat);
+    r.advantages = (const float*)s.vector(a[4], "advantages", IN, false, s.rows, at::kFloat);
+    r.loss = (float*)s.vector(a[5], "loss", OUT, false, 1, at::kFloat);
+    MAT(dlogits, 6, OUT, true);
+    r.ref_logp = (const float*)s.vector(a[10], "ref_logp", IN, true, s.rows, at::kFloat);
     r.clip_low = (float)number(a[11]);
     r.clip_high = (float)number(a[12]);
     r.kl_beta = (float)number(a[13]);
     r.per_sequence = truth(a[14]);
     r.grad_scale = (float)number(a[15]);
-    r.logp = (float*)s.vector(a[16], "logp", true, s.rows, at::kFloat);
-    r.stats = (float*)s.vector(a[17], "stats", true, 3, at::kFloat);
+    r.logp = (float*)s.vector(a[16], "logp", OUT, true, s.rows, at::kFloat);
+    r.stats = (float*)s.vector(a[17], "stats", OUT, true, 3, at::kFloat);
     r.reserved = 0;
     return ready() ? (long)adacgd_policy_loss(s.h->ctx, &r) : RETRY;
   });

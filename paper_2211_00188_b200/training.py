@@ -68,8 +68,12 @@ class TrainingOps:
     ordered behind that stream's work, and that stream waits for it.  One thread at a time per context.
 
     Matrices are 2-D with unit column stride and any row stride, of type float32, float16 or bfloat16; vectors are
-    contiguous.  Outputs may be the very same tensor as an input matrix of the same call (in place).  Wrong tensors
-    raise ValueError, what the library refuses AdacgdError."""
+    contiguous.  Rows must not overlap: an expanded row is refused.  Outputs may be the very same tensor as an input matrix
+    of the same call (in place).  Wrong tensors raise ValueError, what the library refuses AdacgdError.
+
+    The calls are outside autograd: they are not recorded, whether or not an input requires a gradient; the backward
+    passes are the calls themselves.  An output that requires a gradient is refused while gradients are recorded, and
+    what a call writes counts as modified in place, so a graph that has saved it says so when it runs backwards."""
 
     def __init__(self, max_tokens: int, max_cols: int = 8192, *, device="cuda:0", stream=None):
         import torch

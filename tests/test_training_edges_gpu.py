@@ -292,3 +292,63 @@ def test_policy_statistics_without_the_kl_term_leave_the_loss_alone(ops, per_seq
     ops.policy_loss(z, y, old, adv, other, e, sequences=2, per_sequence=per_sequence)
     assert torch.isfinite(other).all() and torch.equal(loss, other) and torch.equal(d, e)
     assert stats[0].item() == float("inf")
+
+
+# ----------------------------------------------------------------------------- automatic differentiation
+
+def test_calls_are_outside_automatic_differentiation(ops):
+    """An output that is part of a recorded graph is refused, and what a call writes counts as modified in place."""
+    x = torch.randn(4, 16, device="cuda")
+    w = torch.randn(16, device="cuda", requires_grad=True)
+    out = torch.empty_like(x)
+    ops.layer_norm(x, out, weight=w)                             # inputs may require gradients; the call is not recorded
+    assert not out.requires_grad
+    grad = torch.empty(4, 16, device="cuda", requires_grad=True)
+    vec = torch.empty(4, device="cuda", requires_grad=True)
+    z, y, v = torch.randn(6, 10, device="cuda"), torch.zeros(6, dtype=torch.int64, device="cuda"), torch.zeros(6, device="cuda")
+    loss, one = torch.empty(1, device="cuda"), torch.empty(1, device="cuda", requires_grad=True)
+    refused = [lambda: ops.dropout(x, grad, p=0.1, seed=0), lambda: ops.layer_norm(x, grad), lambda: ops.layer_norm(x, out, mean=vec),
+               lambda: ops.layer_norm(x, out, sum_out=grad),
+               lambda: ops.layer_norm_backward(x, x, v[:4], v[:4], out, weight=w, dweight=w),
+               lambda: ops.token_logp(z, y, v.clone().requires_grad_()), lambda: ops.preference_loss(z, y, v, one, sequences=2),
+               lambda: ops.policy_loss(z, y, v, v, loss, z.clone().requires_grad_())]
+    before = ops.launch_count()
+    for k, call in enumerate(refused):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+            pytest.fail(f"refusal {k} went through")
+    assert ops.launch_count() == before
+    with torch.no_grad():
+        ops.layer_norm(x, grad)                                  # nothing is being recorded
+    ops.layer_norm(x, out)
+    assert torch.equal(grad.detach(), out)
+    a = torch.randn(4, 16, device="cuda", requires_grad=True)
+    s = a * 1.0
+    t = s.square().sum()                                         # keeps s
+    with torch.no_grad():
+        ops.dropout(x, s, p=0.0, seed=0)                         # overwrites it
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        t.backward()
+    with torch.inference_mode():
+        i = torch.empty(4, 16, device="cuda")
+    ops.dropout(x, i, p=0.0, seed=0)                             # inference tensors have no version to count
+    assert torch.equal(i, x)
+    versions = (out._version, loss._version)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ops.layer_norm(x, out)                                   # by way of another stream too
+    torch.cuda.current_stream().wait_stream(side)
+    ops.policy_loss(z, y, v, v, loss)
+    assert out._version == versions[0] + 1 and loss._version == versions[1] + 1
+
+
+def test_one_token_norm_repeats_bit_for_bit(ops):
+    x, res = (torch.randn(1, 4096, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    w, b = (torch.randn(4096, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    seen = []
+    for _ in range(200):
+        out, total, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+        ops.layer_norm(x, out, weight=w, bias=b, residual=res, sum_out=total, mean=mean, rstd=rstd)
+        seen.append((out, total, mean, rstd))
+    for other in seen[1:]:
+        assert all(torch.equal(a, c) for a, c in zip(seen[0], other))
