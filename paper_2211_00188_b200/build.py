@@ -7,6 +7,7 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+from importlib import metadata
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -15,6 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libadacgd.so")
 BINDING = os.path.join(PKG, "_train_binding.so")
 BINDING_SOURCE = "adacgd_train_binding.cpp"
+STAMP = BINDING + ".for"   # the interpreter and torch the binding was compiled for
 SOURCES = ["adacgd_api.cu", "adacgd_compress.cu", "adacgd_small.cu", "adacgd_noalloc.cu", "adacgd_gradient.cu",
            "adacgd_train.cu", "adacgd_train_norm.cu", "adacgd_train_loss.cu"]
 
@@ -26,18 +28,50 @@ def nvcc_path() -> str:
     raise RuntimeError("nvcc not found")
 
 
-def needs_build() -> bool:
-    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
-        return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
+def _older(target: str, sources) -> bool:
+    return not os.path.exists(target) or any(os.path.getmtime(p) > os.path.getmtime(target) for p in sources)
+
+
+def _headers():
     include = os.path.join(ROOT, "include")
-    deps = [os.path.join(d, f) for d in (CSRC, include) for f in os.listdir(d)]
-    return any(os.path.getmtime(p) > t for p in deps)
+    return [os.path.join(include, f) for f in os.listdir(include)]
+
+
+def library_is_stale() -> bool:
+    return _older(LIB, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != BINDING_SOURCE] + _headers())
+
+
+def binding_target() -> str:
+    """What the binding's object code depends on besides its source: it uses CPython's and torch's binary interfaces."""
+    return f"{sysconfig.get_config_var('SOABI')}, torch {metadata.version('torch')}"
+
+
+def binding_built_for():
+    """The binding_target() that _train_binding.so was compiled for; None if that is not known."""
+    try:
+        with open(STAMP) as f:
+            return f.read().strip()
+    except OSError:
+        return None
+
+
+def binding_is_stale() -> bool:
+    return _older(BINDING, [os.path.join(CSRC, BINDING_SOURCE)] + _headers()) or binding_built_for() != binding_target()
+
+
+def needs_build() -> bool:
+    return library_is_stale() or binding_is_stale()
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not needs_build():
-        return LIB
+    if force or library_is_stale():
+        build_library(verbose)
+    if force or binding_is_stale():
+        build_binding()
+    return LIB
+
+
+def build_library(verbose: bool = False) -> str:
     flags = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
              "-fmad=false",  # every binary32 operation of the bit-exact path is a single rounding
              "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -65,7 +99,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
         raise RuntimeError("linking libadacgd.so failed")
-    build_binding()
     return LIB
 
 
@@ -85,6 +118,8 @@ def build_binding() -> str:
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
         raise RuntimeError(f"{cmd[0]} failed on {BINDING_SOURCE}")
+    with open(STAMP, "w") as f:
+        f.write(binding_target() + "\n")
     return BINDING
 
 

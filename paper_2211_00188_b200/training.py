@@ -53,8 +53,14 @@ def load_training_library():
 def _load_binding():
     import torch  # noqa: F401  (the module links against its libraries)
 
+    from . import build
+
     if not os.path.exists(os.path.join(os.path.dirname(os.path.abspath(__file__)), "_train_binding.so")):
         raise ImportError("_train_binding.so is missing: run `python -m paper_2211_00188_b200.build`")
+    built_for = build.binding_built_for()
+    if built_for not in (None, build.binding_target()):
+        raise ImportError(f"_train_binding.so was built for {built_for}, this is {build.binding_target()}: run "
+                          "`python -m paper_2211_00188_b200.build`")
     from . import _train_binding
 
     return _train_binding
