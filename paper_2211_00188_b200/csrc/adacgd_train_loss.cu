@@ -649,11 +649,12 @@ __global__ void __launch_bounds__(1024) k_policy_weights(adacgd_policy_args a, f
   if (threadIdx.x < 3 && a.stats) a.stats[threadIdx.x] = 0.f;
 }
 
-// A token's loss and its slope with respect to the log-probability, before the token's weight.
+// A token's loss and its slope with respect to the log-probability, before the token's weight.  The differences of log-probabilities
+// are small beside them, so they are taken before the rounding to 32 bits.
 struct Token { float loss, slope, kl; bool clipped; };
-__device__ __forceinline__ Token token_loss(float logp, float old, float A, bool with_ref, float ref, float clip_low, float clip_high,
+__device__ __forceinline__ Token token_loss(double logp, float old, float A, bool with_ref, float ref, float clip_low, float clip_high,
                                             float kl_beta) {
-  const float x = logp - old, r = expf(x), lo = 1.f - clip_low, hi = 1.f + clip_high;
+  const float x = (float)(logp - (double)old), r = expf(x), lo = 1.f - clip_low, hi = 1.f + clip_high;
   // NaN goes through, but not inf * 0 where r has only passed binary32's range
   const float held = (r < lo ? lo : (r > hi ? hi : r)) * A, gain = A == 0.f && fabsf(x) < INFINITY ? 0.f : r * A;
   Token k;
@@ -662,7 +663,7 @@ __device__ __forceinline__ Token token_loss(float logp, float old, float A, bool
   k.loss = k.clipped ? -held : -gain;
   k.kl = 0.f;
   if (with_ref) {
-    const float u = ref - logp, e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0
+    const float u = (float)((double)ref - logp), e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0
     k.kl = e1 - u;
     if (kl_beta > 0.f) {                          // else the term is a statistic alone, which may overflow
       k.slope = k.slope - kl_beta * e1;
@@ -763,14 +764,14 @@ __global__ void __launch_bounds__(Place<NTH, CLUSTER>::CTA, Place<NTH, CLUSTER>:
     const float z = label >= 0 ? to_f(x[label]) : NAN;
     const Cut cut = cut_row(x, vocab, at.part, at.parts);
     const Soft v = row_soft<NTH, CLUSTER>(thread_soft<T, NTH>(x, cut, at.t), sh, xch);
-    const float logp = (float)logp64(z, v);
+    const double logp = logp64(z, v);
     // the same weight for all, or the sequence's
     const long long q = a.per_sequence ? seq_of(a.rows.seq_start, row, a.rows.sequences, a.rows.seq_start ? 0 : a.rows.tokens / a.rows.sequences) : 0;
     pdl_wait();
     const float w = SMALL ? (float)(1.0 / (double)total) : weight[q];
     const Token tok = token_loss(logp, old, A, a.ref_logp != nullptr, ref, a.clip_low, a.clip_high, a.kl_beta);
     if (at.t == 0 && at.part == 0) {
-      if (a.logp) a.logp[row] = logp;
+      if (a.logp) a.logp[row] = (float)logp;
       if (SMALL) {
         mine[0][slot] = (double)w * (double)tok.loss;
         mine[1][slot] = (double)tok.kl;

@@ -352,3 +352,42 @@ def test_one_token_norm_repeats_bit_for_bit(ops):
         seen.append((out, total, mean, rstd))
     for other in seen[1:]:
         assert all(torch.equal(a, c) for a, c in zip(seen[0], other))
+
+
+@pytest.mark.parametrize("n,vocab", [(1024, 8000), (512, 100003)])
+def test_policy_loss_is_at_least_as_exact_as_the_plain_form(ops, n, vocab):
+    """Errors of loss and gradient against binary64 over eight batches (root mean square), beside those of the formula in elementary
+    binary32 operations.  Ratios are near one, so what counts is the difference of log-probabilities.  The gradient's error is relative;
+    the loss is a sum of terms of both signs that may come out anywhere near zero, so its error is taken as it is."""
+    lo = hi = float(np.float32(0.2))
+    kb = float(np.float32(0.04))
+    found = np.zeros((8, 4))
+    for k in range(8):
+        gen = torch.Generator(device="cuda").manual_seed(1000 + k)
+        normal = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")  # noqa: E731
+        z, y = normal(n, vocab) * 2, torch.randint(vocab, (n,), generator=gen, device="cuda")
+        z.scatter_add_(1, y[:, None], normal(n, 1) * 3 + 6)
+        true = torch.log_softmax(z.double(), 1)
+        at = true.gather(1, y[:, None])[:, 0]
+        old, ref, A = (at + 0.15 * normal(n)).float(), (at + 0.25 * normal(n)).float(), normal(n)
+
+        def rest(logp, soft, old, ref, A):
+            r, u = (logp - old).exp(), ref - logp
+            gain, held = r * A, r.clamp(1 - lo, 1 + hi) * A
+            loss = (kb * (u.exp() - u - 1) - torch.minimum(gain, held)).sum() / n
+            slope = (torch.where(gain <= held, -gain, torch.zeros_like(gain)) + kb * (1 - u.exp())) / n
+            d = soft * -slope[:, None]
+            return loss, d.scatter_add_(1, y[:, None], slope[:, None])
+
+        exact_loss, exact_d = rest(at, true.exp(), old.double(), ref.double(), A.double())
+        e = (z - z.amax(1, keepdim=True)).exp()
+        total = e.sum(1)
+        plain = (z - z.amax(1, keepdim=True)).gather(1, y[:, None])[:, 0] - total.log()
+        plain_loss, plain_d = rest(plain, e / total[:, None], old, ref, A)
+        loss, d = torch.empty(1, device="cuda"), torch.empty_like(z)
+        ops.policy_loss(z, y, old, A, loss, d, ref_logp=ref, clip_low=0.2, clip_high=0.2, kl_beta=0.04)
+        off = lambda v, w: ((v.double() - w).norm() / w.norm()).item()  # noqa: E731
+        miss = lambda v: abs(v.item() - exact_loss.item())  # noqa: E731
+        found[k] = miss(loss), miss(plain_loss), off(d, exact_d), off(plain_d, exact_d)
+    own_loss, plain_loss, own_d, plain_d = np.sqrt((found ** 2).mean(0))
+    assert own_loss <= plain_loss and own_d <= plain_d, found
