@@ -94,6 +94,11 @@ __device__ __forceinline__ double lse64(const Soft& a) {
   const double b = (double)base_of(a.m), o = plain_range(a.m) ? fma(b, -(double)LOG2E, (double)(offset_of(a.m) + l.k)) : (double)l.k;
   return b + (o + (double)l.f) * LN2;
 }
+// logp less another model's, which comes rounded to 32 bits.  Beyond 2^10, as of a label that a mask has set to -1e9, that rounding
+// would be most of the difference, so there both are taken rounded.
+__device__ __forceinline__ double logp_less(double logp, float other) {
+  return (fabs(logp) > 1024.0 ? (double)(float)logp : logp) - (double)other;
+}
 
 __device__ __forceinline__ long long label_at(const adacgd_token_rows& r, long long t) {
   return r.label_bytes == 8 ? (long long)((const int64_t*)r.labels)[t] : (long long)((const int32_t*)r.labels)[t];
@@ -541,7 +546,7 @@ __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, con
       const double logp = logp64(zl[t], Soft{top[t], sum[t]});
       cnt[k] += 1.0;
       total[k] += logp;
-      diff[k] += logp - (double)a.ref_logp[t];
+      diff[k] += logp_less(logp, a.ref_logp[t]);
     }
     total[k] = block_sum_f64<PAIR_NT>(total[k], sh);
     diff[k] = block_sum_f64<PAIR_NT>(diff[k], sh);
@@ -654,7 +659,7 @@ __global__ void __launch_bounds__(1024) k_policy_weights(adacgd_policy_args a, f
 struct Token { float loss, slope, kl; bool clipped; };
 __device__ __forceinline__ Token token_loss(double logp, float old, float A, bool with_ref, float ref, float clip_low, float clip_high,
                                             float kl_beta) {
-  const float x = (float)(logp - (double)old), r = expf(x), lo = 1.f - clip_low, hi = 1.f + clip_high;
+  const float x = (float)logp_less(logp, old), r = expf(x), lo = 1.f - clip_low, hi = 1.f + clip_high;
   // NaN goes through, but not inf * 0 where r has only passed binary32's range
   const float held = (r < lo ? lo : (r > hi ? hi : r)) * A, gain = A == 0.f && fabsf(x) < INFINITY ? 0.f : r * A;
   Token k;
@@ -663,7 +668,7 @@ __device__ __forceinline__ Token token_loss(double logp, float old, float A, boo
   k.loss = k.clipped ? -held : -gain;
   k.kl = 0.f;
   if (with_ref) {
-    const float u = (float)((double)ref - logp), e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0
+    const float u = -(float)logp_less(logp, ref), e1 = expm1f(u);   // exp(u) - 1 without cancellation near 0
     k.kl = e1 - u;
     if (kl_beta > 0.f) {                          // else the term is a statistic alone, which may overflow
       k.slope = k.slope - kl_beta * e1;

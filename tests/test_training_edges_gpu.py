@@ -163,7 +163,7 @@ def test_label_at_the_types_lowest_value_has_a_finite_logp(ops):
             close(logp, np.full(4, float(lowest)), 4 * E * abs(float(lowest)), "logp")
             loss, margin, d = torch.empty(1, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(z)
             ops.preference_loss(z, y, logp, loss, d, sequences=2, margin=margin)
-            # the reference is the value itself: what is left of the difference is a rounding of 2^128, but no NaN
+            # the reference is the value itself: no NaN from the difference of two such
             assert torch.isfinite(margin).all() and torch.isfinite(loss).all() and not torch.isnan(d).any()
 
 
@@ -391,3 +391,25 @@ def test_policy_loss_is_at_least_as_exact_as_the_plain_form(ops, n, vocab):
         found[k] = miss(loss), miss(plain_loss), off(d, exact_d), off(plain_d, exact_d)
     own_loss, plain_loss, own_d, plain_d = np.sqrt((found ** 2).mean(0))
     assert own_loss <= plain_loss and own_d <= plain_d, found
+
+
+@pytest.mark.parametrize("value", [-3e4, -1e9, -1e30, None])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [40, 3000, 290001])
+def test_a_masked_label_is_the_same_under_the_same_model(ops, value, dtype, vocab):
+    """Labels that a mask has set to a low value (None: the type's lowest), with the log-probabilities of the same logits as the old policy's
+    and the reference's: ratios are one and margins zero, although a log-probability of -1e9 is only given to the nearest 64."""
+    dt = TYPES[dtype]
+    z, y, rng = make_rows(8, vocab, dt)
+    z[torch.arange(8, device="cuda"), y] = torch.finfo(dt).min if value is None else value
+    logp, loss, margin, d = torch.empty(8, device="cuda"), torch.empty(1, device="cuda"), torch.empty(2, device="cuda"), torch.empty_like(z)
+    stats = torch.empty(3, device="cuda")
+    ops.token_logp(z, y, logp)
+    ops.preference_loss(z, y, logp, loss, d, sequences=4, margin=margin)
+    assert not margin.any() and abs(loss.item() - np.log(2)) < 4 * E
+    A = dev(rng.normal(size=8))
+    ops.policy_loss(z, y, logp, A, loss, d, ref_logp=logp, kl_beta=0.1, stats=stats)
+    assert abs(loss.item() + A.double().mean().item()) <= 4 * E * A.abs().mean().item()
+    assert stats[0].item() == 0 and stats[1].item() == 0
+    got = d.double()[torch.arange(8, device="cuda"), y]                  # -A / n (1 - 0): the label's own probability is zero
+    close(got, -host(A) / 8, (U[dt] + 4 * E) * np.abs(host(A)) / 8, "dlogits")
