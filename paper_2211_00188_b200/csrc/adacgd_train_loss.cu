@@ -420,8 +420,8 @@ template <int NTH, bool CLUSTER> struct Place {
 // log-probabilities
 // --------------------------------------------------------------------------
 //   logp = z_label - m - log s
-// One pass, two 64-byte batches a thread under way.  4096 rows x 65536 bfloat16 88 us = 6.1 TB/s, 93 % of the copy rate; 131072 x 512,
-// where a row is one memory latency and two reductions, 29 us = 4.6 TB/s.  Rows walked by as many CTAs as fit lost to CTAs handed out
+// One pass, two 64-byte batches a thread under way.  4096 rows x 65536 bfloat16 91 us = 5.9 TB/s, 91 % of the copy rate; 131072 x 512,
+// where a row is one memory latency and two reductions, 31 us = 4.3 TB/s.  Rows walked by as many CTAs as fit lost to CTAs handed out
 // by the hardware: no gain on full batches, 140 against 113 us with a third of the rows masked.
 // zl, sum, top: the label's entry, the sum and the reference, from which the preference loss has its log-probabilities in 64 bits and
 // its gradient.  Either these or logp.
@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(PAIR_NT) k_pairs(adacgd_preference_args a, con
 
 // The gradient once the pairs' coefficients are known: element by element, `parts` places a row.  The logits have to be read again
 // (512 MB do not stay in the cache), so the call moves three units where log-probabilities of the policy kind move two: 4096 x 32000
-// bfloat16, two thirds of the tokens counted, 116 us against a floor of 67 for one read and one write, 94 for the two reads.
+// bfloat16, two thirds of the tokens counted, 117 us against a floor of 67 for one read and one write, 94 for the two reads.
 template <typename T, int NTH>
 __global__ void __launch_bounds__(Place<NTH, false>::CTA, Place<NTH, false>::CTAS) k_preference_grad(adacgd_preference_args a, const float* coef,
                                                                             const float* zl, const float* sum,
@@ -710,7 +710,7 @@ __device__ __forceinline__ int count_share(const uint8_t* mask, int n, int t) {
   return c;
 }
 
-// A row's loss and, from the cache, its gradient.  4096 x 131072 bfloat16, two thirds of the rows counted: 350 us = 5.1 TB/s of DRAM
+// A row's loss and, from the cache, its gradient.  4096 x 131072 bfloat16, two thirds of the rows counted: 345 us = 5.2 TB/s of DRAM
 // traffic, beside which a third as much again comes from the cache.  Rows kept in shared memory between the passes: 521 against 420 us
 // with all rows counted, for want of threads; an asynchronous ring instead of the register batches 55 to 62 % of the copy rate.
 // SMALL: every row counts the tokens itself and the last CTA adds the CTAs' sums; otherwise a kernel before gives the weights and one
@@ -885,18 +885,18 @@ Split split_of(long long rows, long long vocab, int threads, const Where& at) {
   return s;
 }
 // One pass: a row's two reductions cost every warp the same, about what 128 elements a thread do, and many rows on an SM hide them; so
-// as few threads a row as that.  Log-probabilities of 2^27 elements (2^16 rows of 512), us at 8 / 32 / 128 / 512 threads a row:
-// bfloat16 512 wide 29 / 70 / - / -; 1536 70 / 93 / - / -; 2048 91 / 93 / 275 / -; 4096 95 / 88 / 135 / -; 8192 98 / 89 / 97 / 312; 16384
-// - / 89 / 84 / 161; 32768 - / 101 / 86 / 109; 131072 - / - / 93 / 86; binary32 1024 wide 82 / 85; 1536 121 / 117.
+// as few threads a row as that.  Log-probabilities of 2^28 elements, us at 8 / 32 / 128 / 512 threads a row: bfloat16 512 wide 101 / 283 /
+// - / -; 1536 90 / 127 / - / -; 2048 91 / 97 / 292 / -; 4096 95 / 89 / 144 / -; 8192 96 / 88 / 101 / 330; 16384 - / 89 / 86 / 170; 32768 - /
+// 101 / 86 / 113; 131072 - / - / 93 / 87; binary32, 131072 rows, 1024 wide 82 / 88; 1536 121 / 119.
 Split split_once(long long rows, long long vocab, int size, const Where& at) {
   return split_of(rows, vocab, vocab * size <= 4096 ? 8 : vocab <= 8192 ? 32 : (vocab <= 65536 ? 128 : 512), at);
 }
 // Two passes, the second from the cache: what the resident threads hold between their passes (1024 an SM) has to stay in it beside
 // what is written, so a thread may have 400 bytes of a row, and 640 where more threads a row cost more than the cache gives.
-// Policy loss, us at 8 / 32 / 128 / 256 / 512 / 1024 threads a row, bfloat16: 131072 x 1024 109 / 137; 131072 x 1536 164 / 186; 131072 x
-// 2048 222 / 204; 65536 x 4096 - / 191 / 256; 32768 x 8192 - / 214 / 203; 8192 x 32000 - / - / 213 / 196 / 239; 8192 x 50001 371 / 316 /
-// 339 / 509 from 128 on; 4096 x 65536 255 / 269 / 208 from 128 on; 4096 x 131072 419 / 458 and 2048 x 262145 511 / 452 at 512 / 1024;
-// binary32: 131072 x 512 105 / 124; 131072 x 1024 251 / 191; 65536 x 4096 - / 473 / 366.
+// Policy loss, us at 8 / 32 / 128 / 256 / 512 / 1024 threads a row, bfloat16: 131072 x 1024 110 / 143; 131072 x 1536 160 / 195; 131072 x
+// 2048 218 / 209; 65536 x 4096 - / 194 / 273; 32768 x 8192 - / 213 / 208; 8192 x 32000 - / - / 211 / 200 / 248; 8192 x 50001 368 / 313 /
+// 351 / 537 from 128 on; 4096 x 65536 255 / 212 / 209 from 128 on; 4096 x 131072 416 / 467 and 2048 x 262145 511 / 464 at 512 / 1024;
+// binary32: 131072 x 512 109 / 136; 131072 x 1024 251 / 197; 65536 x 4096 - / 474 / 378.
 constexpr int PASS_BYTES = 400, PASS_BYTES_WIDE = 640;
 Split split_twice(long long rows, long long vocab, int size, const Where& at) {
   const long long bytes = vocab * size;

@@ -309,7 +309,7 @@ template <> struct Held<float> {
 // NTH threads take one row, CTAs are handed out by the hardware: the row's two sums and the loads of other rows on the SM hide each
 // other (a grid of as many CTAs as fit, with rows through an asynchronous ring, took 404 us where this took 374).  The mean first,
 // then the squares about it, over registers: no cancellation.
-// 32768 x 8192 bfloat16 with residual and sum (four arrays, 2.1 GB): 318 us = 6.75 TB/s, the copy rate; with dropout 355 us, where
+// 32768 x 8192 bfloat16 with residual and sum (four arrays, 2.1 GB): 316 us = 6.8 TB/s, the copy rate; with dropout 353 us, where
 // the generator's products and the selections fill the issue slots.
 template <int NTH> struct Group {
   static constexpr int CTA = NTH <= 32 ? 128 : NTH;
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(Group<NTH>::CTA) k_norm(const __grid_constant_
 // Rows wider than NTH * R runs are cut into as many column parts as the cluster has CTAs; the two sums then meet in distributed
 // shared memory.
 // K rows go through the two phases together, so that their reductions share one barrier: 465 -> 341 us at 32768 x 8192 bfloat16,
-// K = 1 -> 2; now 321 us = 6.7 TB/s, the copy rate, and 440 us = 6.1 TB/s with dropout (five arrays).  The weight gradients of a
+// K = 1 -> 2; now 325 us = 6.6 TB/s, the copy rate, and 440 us = 6.1 TB/s with dropout (five arrays).  The weight gradients of a
 // column stay in the registers of the thread that always meets it, so the grid is as many CTAs as fit, and rows come through a ring
 // of asynchronous copies because registers hold no second row.
 template <typename T, typename P, int NTH, int R, bool CLUSTER, bool EDGE, int ARRAYS>
@@ -1041,7 +1041,9 @@ int norm_bwd_launch(const TrainScratch& s, const adacgd_norm_backward_args& a, i
 
 template <typename T, typename P, bool EDGE>
 int norm_bwd_by_width(const TrainScratch& s, const adacgd_norm_backward_args& a, long long n, const Where& at) {
-  if (!EDGE && n <= 8) return norm_bwd_launch<T, P, 8, 1, false, false>(s, a, 1, at);      // edges take sixteen threads
+  // Up to 64 columns, us at 8 / 16 threads a row: bfloat16 512 rows 8.4 / 8.7, 16384 11.1 / 12.5, 131072 20.6 / 30.9; binary32 16384 rows 10.9 /
+  // 12.5, 131072 23.1 / 28.3 and with dsum 31.1 / 32.1.  Edges take sixteen threads.
+  if (!EDGE && n <= 8) return norm_bwd_launch<T, P, 8, 1, false, false>(s, a, 1, at);
   if (n <= 16) return norm_bwd_launch<T, P, 16, 1, false, EDGE>(s, a, 1, at);
   if (n <= 32) return norm_bwd_launch<T, P, 32, 1, false, EDGE>(s, a, 1, at);
   // One run a thread for binary32, of which an SM holds half as many rows, and where a walker gets few rows; else two, which share a
