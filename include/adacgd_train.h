@@ -3,7 +3,8 @@
  *
  * adacgd.h starts from a worker's gradient X_i = grad f_i(x).  When f_i is the loss of a language model the worker
  * fine-tunes, that gradient comes out of matrix products (a library's) and of the operators below, which stand between
- * and behind those products: layer norm with the residual sum and dropout in front of it, dropout on its own, the
+ * and behind those products: the embedding lookup and its gradient, norm and rotation of queries and keys, attention,
+ * layer norm with the residual sum and dropout in front of it, dropout on its own, the
  * log-probabilities of given tokens, and the two losses a fine-tuning worker minimises -- the preference loss over
  * pairs of answers (the logistic loss of a margin, as in Section 6 of the paper, with a.x replaced by a paired log
  * ratio) and the clipped policy loss with a KL term -- with their gradients with respect to the logits.
@@ -194,6 +195,126 @@ typedef struct {
   int32_t reserved;         /* must be 0 */
 } adacgd_policy_args;
 adacgd_status adacgd_policy_loss(adacgd_train* t, const adacgd_policy_args* a);
+
+/* Embedding lookup: out[t] = scale * table[ids[t]] for tokens that count, 0 for the others.  An id outside [0, vocab) on a
+ * token that counts makes that row NaN. */
+typedef struct {
+  int64_t tokens, vocab, cols;
+  const void* ids;      /* [tokens] int64 or int32 */
+  const uint8_t* mask;  /* [tokens], non-zero = counts; NULL: all count */
+  const void* table;    int64_t table_stride;
+  void* out;            int64_t out_stride;
+  float scale;          /* finite */
+  int32_t dtype;        /* of table and out */
+  int32_t id_bytes;     /* 8 or 4 */
+  int32_t reserved;     /* must be 0 */
+} adacgd_embedding_args;
+adacgd_status adacgd_embedding(adacgd_train* t, const adacgd_embedding_args* a);
+
+/* Gradient of the lookup: dtable[v] = [base[v] +] scale * sum of dout[t] over the tokens t that count and have ids[t] = v.
+ * Tokens are sorted by id, those of one id in the order of the batch, and summed in that order in pieces: binary32 chains
+ * of at most max(64, tokens / 592) rows, joined in binary32 in order.  Ids outside [0, vocab) add to nothing.  Every row of dtable is written,
+ * unless base is the very same matrix: then rows without tokens stay as they are.  tokens <= max_tokens, cols <= max_cols. */
+typedef struct {
+  int64_t tokens, vocab, cols;
+  const void* ids;
+  const uint8_t* mask;
+  const void* dout;     int64_t dout_stride;
+  const void* base;     int64_t base_stride;     /* or NULL */
+  void* dtable;         int64_t dtable_stride;
+  float scale;
+  int32_t dtype;        /* of dout */
+  int32_t table_dtype;  /* of base and dtable: dtype or ADACGD_F32 */
+  int32_t id_bytes;
+} adacgd_embedding_backward_args;
+adacgd_status adacgd_embedding_backward(adacgd_train* t, const adacgd_embedding_backward_args* a);
+
+/* Norm and rotation of queries and keys.  A row holds its heads side by side, head_dim elements each.  With x a head,
+ *   n = x (mean(x^2) + eps)^(-1/2) weight,
+ * and the first 2 pairs elements of n are turned in pairs (a, b), by the angle position * freq[i] for pair i:
+ *   a' = a cos - b sin,  b' = b cos + a sin;   (a, b) = elements (i, pairs + i), or with interleaved (2 i, 2 i + 1).
+ * The angle is the product of the position and the binary32 number freq[i], formed and reduced in binary64.  k may be NULL
+ * with key_heads = 0; pairs = 0 is the norm alone. */
+typedef struct {
+  int64_t tokens, heads, key_heads;
+  int32_t head_dim;        /* in [1, ADACGD_TRAIN_MAX_HEAD] */
+  int32_t pairs;           /* in [0, head_dim / 2] */
+  const void* q;           int64_t q_stride;       /* [tokens, heads * head_dim] */
+  const void* k;           int64_t k_stride;       /* [tokens, key_heads * head_dim] */
+  void* q_out;             int64_t q_out_stride;
+  void* k_out;             int64_t k_out_stride;
+  const void* q_weight;    /* [head_dim] or NULL (1) */
+  const void* k_weight;
+  const void* positions;   /* [tokens] int64 or int32; NULL where pairs = 0 */
+  const float* freq;       /* [pairs] */
+  float eps;               /* finite, >= 0 */
+  int32_t dtype;           /* of the matrices */
+  int32_t param_dtype;     /* of the weights: dtype or ADACGD_F32 */
+  int32_t position_bytes;  /* 8 or 4 */
+  int32_t interleaved;
+  int32_t reserved;        /* must be 0 */
+} adacgd_qk_norm_args;
+#define ADACGD_TRAIN_MAX_HEAD 512
+adacgd_status adacgd_qk_norm(adacgd_train* t, const adacgd_qk_norm_args* a);
+
+/* Its backward pass, from the inputs of the forward pass.  `f` describes the forward call; its q_out and k_out are read and hold the
+ * gradients with respect to the outputs.  With dn those gradients turned back, r = (mean(x^2) + eps)^(-1/2), g = dn weight:
+ *   dx = r (g - x r mean(g x r)),   dweight = sum over tokens and heads of dn x r.
+ * cols of q and k <= max_cols, tokens <= max_tokens. */
+typedef struct {
+  adacgd_qk_norm_args f;
+  void* dq;                int64_t dq_stride;
+  void* dk;                int64_t dk_stride;
+  void* dq_weight;         /* [head_dim] or NULL, param_dtype */
+  void* dk_weight;
+} adacgd_qk_norm_backward_args;
+adacgd_status adacgd_qk_norm_backward(adacgd_train* t, const adacgd_qk_norm_backward_args* a);
+
+/* Attention over the tokens of each sequence.  Sequences are rows [seq_start[q], seq_start[q + 1]), or equal runs, as in
+ * adacgd_token_rows; rows that belong to none are left as they are in every output.  Query head h reads key head h / (heads / key_heads).  Token i sees token j of its own
+ * sequence if both count (mask) and, where causal, j <= i.  With s_ij = scale q_i.k_j over those j,
+ *   lse_i = log sum_j exp(s_ij),   out_i = sum_j exp(s_ij - lse_i) v_j;
+ * tokens that do not count have out = 0 and lse = -inf.  Products and sums are kept in binary32; for the 16-bit types
+ * exp(s_ij - c) is rounded to that type as an operand of the second product, with a power of two c near the row's largest s that keeps it in range.
+ * What is stored in rows of tokens that do not count, or of other sequences, reaches no result; Inf or NaN in a token that counts may reach
+ * every row of its sequence.  No output may overlap anything. */
+typedef struct {
+  int64_t tokens, sequences;
+  const int32_t* seq_start; /* [sequences + 1] or NULL */
+  const uint8_t* mask;      /* [tokens] or NULL */
+  const void* q;            int64_t q_stride;     /* [tokens, heads * head_dim] */
+  const void* k;            int64_t k_stride;     /* [tokens, key_heads * head_dim] */
+  const void* v;            int64_t v_stride;     /* [tokens, key_heads * head_dim] */
+  int32_t heads, key_heads; /* key_heads divides heads */
+  int32_t head_dim;         /* in [1, ADACGD_ATTENTION_MAX_HEAD] */
+  int32_t causal;
+  float scale;              /* finite, > 0 */
+  int32_t dtype;
+} adacgd_attention_inputs;
+#define ADACGD_ATTENTION_MAX_HEAD 256
+typedef struct {
+  adacgd_attention_inputs in;
+  void* out;                int64_t out_stride;   /* [tokens, heads * head_dim] */
+  float* lse;               /* [heads][tokens] or NULL */
+} adacgd_attention_args;
+adacgd_status adacgd_attention(adacgd_train* t, const adacgd_attention_args* a);
+
+/* Backward pass, from what the forward pass stored; the probabilities p_ij = exp(s_ij - lse_i) are computed again.
+ *   d_i = dout_i.out_i,   ds_ij = p_ij (dout_i.v_j - d_i),
+ *   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,   dv_j = sum_i p_ij dout_i,
+ * the sums over i running over the query heads that share the key head too.  row_dot receives d (0 for tokens that do not count).
+ * p and ds are rounded to the 16-bit types as operands of products.  Rows of tokens that do not count are 0 in dq, dk and dv. */
+typedef struct {
+  adacgd_attention_inputs in;
+  const void* out;          int64_t out_stride;
+  const void* dout;         int64_t dout_stride;
+  const float* lse;         /* [heads][tokens] */
+  float* row_dot;           /* [heads][tokens] */
+  void* dq;                 int64_t dq_stride;
+  void* dk;                 int64_t dk_stride;
+  void* dv;                 int64_t dv_stride;
+} adacgd_attention_backward_args;
+adacgd_status adacgd_attention_backward(adacgd_train* t, const adacgd_attention_backward_args* a);
 
 #ifdef __cplusplus
 }

@@ -175,3 +175,118 @@ def policy(logits, labels, old_logp, advantages, mask=None, sequences=None, seq_
     k = counted.sum()
     return dict(loss=loss, logp=logp, stats=np.array([kl_sum / k if k else 0.0, clipped / k if k else 0.0, k]),
                 per_token=per_token, dlogits=grad_scale * _dlogits(per_token, labels, soft, counted))
+
+
+def embedding(tokens, table, scale=1.0, mask=None):
+    table = np.asarray(table, np.float64)
+    out = np.zeros((len(tokens), table.shape[1]))
+    for t, v in enumerate(tokens):
+        if mask is None or mask[t]:
+            out[t] = scale * table[int(v)] if 0 <= int(v) < len(table) else np.nan
+    return out
+
+
+def embedding_backward(tokens, dout, vocab, scale=1.0, mask=None, base=None):
+    dout = np.asarray(dout, np.float64)
+    total = np.zeros((vocab, dout.shape[1]))
+    for t, v in enumerate(tokens):
+        if (mask is None or mask[t]) and 0 <= int(v) < vocab:
+            total[int(v)] += dout[t]
+    return scale * total + (0.0 if base is None else np.asarray(base, np.float64))
+
+
+def _turned(x, positions, freq, interleaved, back=False):
+    """x [tokens, heads, dim] with its pairs turned."""
+    y = x.copy()
+    for i, f in enumerate(freq):
+        p, q = (2 * i, 2 * i + 1) if interleaved else (i, len(freq) + i)
+        angle = np.asarray(positions, np.float64) * float(f) * (-1.0 if back else 1.0)
+        c, s = np.cos(angle)[:, None], np.sin(angle)[:, None]
+        y[..., p], y[..., q] = x[..., p] * c - x[..., q] * s, x[..., q] * c + x[..., p] * s
+    return y
+
+
+def qk_norm(x, head_dim, weight=None, eps=1e-6, positions=None, freq=(), interleaved=False):
+    """q or k alone; [tokens, heads * head_dim]"""
+    x = np.asarray(x, np.float64)
+    h = x.reshape(len(x), -1, head_dim)
+    n = h / np.sqrt((h * h).mean(2, keepdims=True) + eps) * (1.0 if weight is None else np.asarray(weight, np.float64))
+    return _turned(n, positions, freq, interleaved).reshape(x.shape)
+
+
+def qk_norm_backward(dout, x, head_dim, weight=None, eps=1e-6, positions=None, freq=(), interleaved=False):
+    """(dx, dweight)"""
+    x = np.asarray(x, np.float64)
+    h = x.reshape(len(x), -1, head_dim)
+    dn = _turned(np.asarray(dout, np.float64).reshape(h.shape), positions, freq, interleaved, back=True)
+    r = 1.0 / np.sqrt((h * h).mean(2, keepdims=True) + eps)
+    g = dn * (1.0 if weight is None else np.asarray(weight, np.float64))
+    dx = r * (g - h * r * (g * h * r).mean(2, keepdims=True))
+    return dx.reshape(x.shape), (dn * h * r).sum((0, 1))
+
+
+def _seen(a, b, causal, counted):
+    """[queries, keys] of rows a .. b"""
+    ok = counted[a:b, None] & counted[None, a:b]
+    return np.tril(ok) if causal else ok
+
+
+def attention(q, k, v, heads, sequences=None, seq_start=None, causal=True, scale=None, mask=None):
+    """(out, lse); rows of no sequence: NaN"""
+    q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
+    n, dim = len(q), q.shape[1] // heads
+    group = heads * dim // k.shape[1]
+    scale = dim ** -0.5 if scale is None else scale
+    counted = np.ones(n, bool) if mask is None else np.asarray(mask).astype(bool)
+    out, lse = np.full(q.shape, np.nan), np.full((heads, n), np.nan)
+    for a, b in runs(n, sequences, seq_start):
+        ok = _seen(a, b, causal, counted)
+        for h in range(heads):
+            mine, shared = slice(h * dim, (h + 1) * dim), slice(h // group * dim, (h // group + 1) * dim)
+            for i in range(a, b):
+                sees = a + np.flatnonzero(ok[i - a])
+                if not len(sees):
+                    out[i, mine], lse[h, i] = 0.0, -np.inf
+                    continue
+                s = scale * (k[sees, shared] @ q[i, mine])
+                m = s.max()
+                e = np.exp(s - m)
+                lse[h, i] = m + np.log(e.sum())
+                out[i, mine] = (e / e.sum()) @ v[sees, shared]
+    return out, lse
+
+
+def attention_backward(dout, q, k, v, out, lse, heads, sequences=None, seq_start=None, causal=True, scale=None, mask=None):
+    """dict(dq, dk, dv, row_dot), and what a tolerance is made of: sums of the absolute values of the terms (aq, ak, av).
+    Rows of no sequence: NaN."""
+    dout, q, k, v, out, lse = (np.asarray(x, np.float64) for x in (dout, q, k, v, out, lse))
+    n, dim = len(q), q.shape[1] // heads
+    group = heads * dim // k.shape[1]
+    scale = dim ** -0.5 if scale is None else scale
+    counted = np.ones(n, bool) if mask is None else np.asarray(mask).astype(bool)
+    r = {"dq": np.full(q.shape, np.nan), "dk": np.full(k.shape, np.nan), "dv": np.full(k.shape, np.nan), "row_dot": np.full((heads, n), np.nan),
+         "aq": np.zeros(q.shape), "ak": np.zeros(k.shape), "av": np.zeros(k.shape)}
+    for a, b in runs(n, sequences, seq_start):
+        ok = _seen(a, b, causal, counted)
+        for name in ("dq", "dk", "dv"):
+            r[name][a:b] = 0.0
+        c = counted[a:b, None]
+        for h in range(heads):
+            mine, shared = slice(h * dim, (h + 1) * dim), slice(h // group * dim, (h // group + 1) * dim)
+            qs, do, os = (np.where(c, x[a:b, mine], 0.0) for x in (q, dout, out))
+            ks, vs = (np.where(c, x[a:b, shared], 0.0) for x in (k, v))
+            with np.errstate(over="ignore", invalid="ignore"):
+                p = np.where(ok, np.exp(scale * (qs @ ks.T) - np.where(counted[a:b], lse[h, a:b], 0.0)[:, None]), 0.0)
+            dot = (do * os).sum(1)
+            r["row_dot"][h, a:b] = dot
+            dp = do @ vs.T
+            ds = p * (dp - dot[:, None])
+            r["dq"][a:b, mine] += scale * ds @ ks
+            r["dk"][a:b, shared] += scale * ds.T @ qs
+            r["dv"][a:b, shared] += p.T @ do
+            # a rounded ds is off by its own rounding and by those of p (relative to ds) and of the sums in dp and dot
+            ad = p * (np.abs(do) @ np.abs(vs).T + (np.abs(do) * np.abs(os)).sum(1)[:, None])
+            r["aq"][a:b, mine] += scale * ad @ np.abs(ks)
+            r["ak"][a:b, shared] += scale * ad.T @ np.abs(qs)
+            r["av"][a:b, shared] += p.T @ np.abs(do)
+    return r

@@ -1,5 +1,6 @@
 // C ABI of the training operators (adacgd_train.h): contexts and the checks of arguments.  The kernels are in
-// adacgd_train_norm.cu (dropout, layer norm) and adacgd_train_loss.cu (log-probabilities and the losses).
+// adacgd_train_norm.cu (dropout, layer norm), adacgd_train_loss.cu (log-probabilities and the losses), adacgd_train_embed.cu (lookup),
+// adacgd_train_rotary.cu (norm and rotation of queries and keys) and adacgd_train_attention*.cu.
 #include <math.h>
 #include <stdio.h>
 #include <string.h>
@@ -116,6 +117,54 @@ const char* check_rows(const adacgd_train* t, const adacgd_token_rows& r, bool s
 }
 
 bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+bool good_param(int32_t param, int32_t dtype) { return param == dtype || param == ADACGD_F32; }
+bool finite(float v) { return !isnan(v) && !isinf(v); }
+
+const char* check_ids(const void* ids, int32_t bytes, long long tokens) {
+  if (bytes != 4 && bytes != 8) return "id_bytes must be 4 or 8";
+  if (tokens > 0 && (!ids || ((uintptr_t)ids) % bytes)) return "ids must be non-NULL and aligned";
+  return nullptr;
+}
+
+const char* check_qk(const adacgd_qk_norm_args& a) {
+  if (a.tokens < 0 || a.tokens >= (1ll << 31)) return "tokens must be in [0, 2^31)";
+  if (a.heads < 1 || a.heads > 65535 || a.key_heads < 0 || a.key_heads > 65535) return "heads must be in [1, 65535], key_heads in [0, 65535]";
+  if (a.head_dim < 1 || a.head_dim > ADACGD_TRAIN_MAX_HEAD) return "head_dim must be in [1, ADACGD_TRAIN_MAX_HEAD = 512]";
+  if (a.pairs < 0 || a.pairs > a.head_dim / 2) return "pairs must be in [0, head_dim / 2]";
+  if (!good_type(a.dtype)) return "unknown dtype";
+  if (!good_param(a.param_dtype, a.dtype)) return "param_dtype must be dtype or ADACGD_F32";
+  if (!(a.eps >= 0.f) || isinf(a.eps)) return "eps must be finite and >= 0";
+  if (a.reserved) return "reserved must be 0";
+  const long long qc = a.heads * a.head_dim, kc = a.key_heads * a.head_dim;
+  const char* m = check_matrix(a.q, a.q_stride, a.tokens, qc, a.dtype, false);
+  if (!m) m = check_matrix(a.q_out, a.q_out_stride, a.tokens, qc, a.dtype, false);
+  if (!m) m = check_matrix(a.k, a.k_stride, a.tokens, kc, a.dtype, kc == 0);
+  if (!m) m = check_matrix(a.k_out, a.k_out_stride, a.tokens, kc, a.dtype, kc == 0);
+  if (!m && (((uintptr_t)a.q_weight | (uintptr_t)a.k_weight) % size_of(a.param_dtype))) m = "a weight is not aligned to its element";
+  if (!m && a.pairs > 0) {
+    if (a.position_bytes != 4 && a.position_bytes != 8) m = "position_bytes must be 4 or 8";
+    else if (a.tokens > 0 && (!a.positions || ((uintptr_t)a.positions) % a.position_bytes)) m = "positions must be non-NULL and aligned";
+    else if (!a.freq || !aligned4(a.freq)) m = "freq must be non-NULL and aligned";
+  }
+  return m;
+}
+
+const char* check_attention(const adacgd_attention_inputs& a) {
+  if (a.tokens < 0 || a.tokens >= (1ll << 31)) return "tokens must be in [0, 2^31)";
+  if (a.sequences < 1 || a.sequences >= (1ll << 31)) return "sequences must be in [1, 2^31)";
+  if (((uintptr_t)a.seq_start) & 3) return "seq_start is not aligned";
+  if (!a.seq_start && a.tokens % a.sequences) return "without seq_start, sequences must divide tokens";
+  if (a.heads < 1 || a.heads > 65535 || a.key_heads < 1 || a.heads % a.key_heads)
+    return "heads must be in [1, 65535] and key_heads a divisor of it";
+  if (a.head_dim < 1 || a.head_dim > ADACGD_ATTENTION_MAX_HEAD) return "head_dim must be in [1, ADACGD_ATTENTION_MAX_HEAD = 256]";
+  if (!good_type(a.dtype)) return "unknown dtype";
+  if (!(a.scale > 0.f) || isinf(a.scale)) return "scale must be finite and > 0";
+  const long long qc = (long long)a.heads * a.head_dim, kc = (long long)a.key_heads * a.head_dim;
+  const char* m = check_matrix(a.q, a.q_stride, a.tokens, qc, a.dtype, false);
+  if (!m) m = check_matrix(a.k, a.k_stride, a.tokens, kc, a.dtype, false);
+  if (!m) m = check_matrix(a.v, a.v_stride, a.tokens, kc, a.dtype, false);
+  return m;
+}
 
 }  // namespace
 
@@ -375,6 +424,159 @@ adacgd_status adacgd_policy_loss(adacgd_train* t, const adacgd_policy_args* a) {
   const adacgd_status st = check_device(t, entry);
   if (st != ADACGD_OK) return st;
   return launched(t, entry, launch_policy(t->s, *a, t->at));
+}
+
+adacgd_status adacgd_embedding(adacgd_train* t, const adacgd_embedding_args* a) {
+  const char* entry = "adacgd_embedding";
+  if (!t || !a) return invalid(t, entry, "context or arguments are NULL");
+  if (a->tokens < 0 || a->tokens >= (1ll << 31)) return invalid(t, entry, "tokens must be in [0, 2^31)");
+  if (a->vocab < 1 || a->vocab >= (1ll << 31)) return invalid(t, entry, "vocab must be in [1, 2^31)");
+  if (a->cols < 1 || a->cols > (1ll << 24)) return invalid(t, entry, "cols must be in [1, 2^24]");
+  if (!good_type(a->dtype)) return invalid(t, entry, "unknown dtype");
+  if (!finite(a->scale)) return invalid(t, entry, "scale must be finite");
+  if (a->reserved) return invalid(t, entry, "reserved must be 0");
+  const char* m = check_ids(a->ids, a->id_bytes, a->tokens);
+  if (!m) m = check_matrix(a->table, a->table_stride, a->vocab, a->cols, a->dtype, false);
+  if (!m) m = check_matrix(a->out, a->out_stride, a->tokens, a->cols, a->dtype, false);
+  if (m) return invalid(t, entry, m);
+  const size_t es = size_of(a->dtype);
+  Region table = region(a->table, a->table_stride, a->cols, a->vocab, es, false);
+  table.matrix = false;                              // rows go elsewhere: never in place
+  const Region r[] = {table, region(a->out, a->out_stride, a->cols, a->tokens, es, true),
+                      vec(a->ids, a->tokens, a->id_bytes, false), vec(a->mask, a->tokens, 1, false)};
+  if (any_conflict(r, 4)) return invalid(t, entry, "out overlaps another argument");
+  const adacgd_status st = check_device(t, entry);
+  if (st != ADACGD_OK) return st;
+  if (a->tokens == 0) return ADACGD_OK;
+  return launched(t, entry, launch_embedding(*a, t->at));
+}
+
+adacgd_status adacgd_embedding_backward(adacgd_train* t, const adacgd_embedding_backward_args* a) {
+  const char* entry = "adacgd_embedding_backward";
+  if (!t || !a) return invalid(t, entry, "context or arguments are NULL");
+  if (a->tokens < 0 || a->tokens > t->s.max_tokens) return invalid(t, entry, "tokens must be in [0, max_tokens]");
+  if (a->vocab < 1 || a->vocab >= (1ll << 31)) return invalid(t, entry, "vocab must be in [1, 2^31)");
+  if (a->cols < 1 || a->cols > t->s.max_cols) return invalid(t, entry, "cols must be in [1, max_cols]");
+  if (!good_type(a->dtype)) return invalid(t, entry, "unknown dtype");
+  if (!good_param(a->table_dtype, a->dtype)) return invalid(t, entry, "table_dtype must be dtype or ADACGD_F32");
+  if (!finite(a->scale)) return invalid(t, entry, "scale must be finite");
+  const char* m = check_ids(a->ids, a->id_bytes, a->tokens);
+  if (!m) m = check_matrix(a->dout, a->dout_stride, a->tokens, a->cols, a->dtype, false);
+  if (!m) m = check_matrix(a->base, a->base_stride, a->vocab, a->cols, a->table_dtype, true);
+  if (!m) m = check_matrix(a->dtable, a->dtable_stride, a->vocab, a->cols, a->table_dtype, false);
+  if (m) return invalid(t, entry, m);
+  const size_t es = size_of(a->dtype), ts = size_of(a->table_dtype);
+  Region dout = region(a->dout, a->dout_stride, a->cols, a->tokens, es, false);
+  dout.matrix = false;
+  const Region r[] = {dout, region(a->base, a->base_stride, a->cols, a->vocab, ts, false),
+                      region(a->dtable, a->dtable_stride, a->cols, a->vocab, ts, true),
+                      vec(a->ids, a->tokens, a->id_bytes, false), vec(a->mask, a->tokens, 1, false)};
+  if (any_conflict(r, 5)) return invalid(t, entry, "dtable overlaps another argument without being the same matrix as base");
+  const adacgd_status st = check_device(t, entry);
+  if (st != ADACGD_OK) return st;
+  return launched(t, entry, launch_embedding_backward(t->s, *a, t->at));
+}
+
+adacgd_status adacgd_qk_norm(adacgd_train* t, const adacgd_qk_norm_args* a) {
+  const char* entry = "adacgd_qk_norm";
+  if (!t || !a) return invalid(t, entry, "context or arguments are NULL");
+  const char* m = check_qk(*a);
+  if (m) return invalid(t, entry, m);
+  const size_t es = size_of(a->dtype), ps = size_of(a->param_dtype);
+  const long long n = a->tokens, qc = a->heads * a->head_dim, kc = a->key_heads * a->head_dim;
+  const Region r[] = {region(a->q, a->q_stride, qc, n, es, false), region(a->k, a->k_stride, kc, n, es, false),
+                      region(a->q_out, a->q_out_stride, qc, n, es, true), region(a->k_out, a->k_out_stride, kc, n, es, true),
+                      vec(a->q_weight, a->head_dim, ps, false), vec(a->k_weight, a->head_dim, ps, false),
+                      vec(a->positions, a->pairs ? n : 0, a->position_bytes, false), vec(a->freq, a->pairs, 4, false)};
+  // k_out in q's place, or q_out in k's, is no operation in place
+  if (any_conflict(r, 8) || (n && kc && (a->q == a->k_out || a->k == a->q_out)))
+    return invalid(t, entry, "an output overlaps another argument without being the same matrix as its input");
+  const adacgd_status st = check_device(t, entry);
+  if (st != ADACGD_OK) return st;
+  if (n == 0) return ADACGD_OK;
+  return launched(t, entry, launch_qk_norm(*a, t->at));
+}
+
+adacgd_status adacgd_qk_norm_backward(adacgd_train* t, const adacgd_qk_norm_backward_args* b) {
+  const char* entry = "adacgd_qk_norm_backward";
+  if (!t || !b) return invalid(t, entry, "context or arguments are NULL");
+  const adacgd_qk_norm_args& a = b->f;
+  const char* m = check_qk(a);
+  const long long n = a.tokens, qc = a.heads * a.head_dim, kc = a.key_heads * a.head_dim;
+  if (!m && n > t->s.max_tokens) m = "tokens must be in [0, max_tokens]";
+  if (!m && (qc > t->s.max_cols || kc > t->s.max_cols)) m = "heads * head_dim must be in [1, max_cols]";
+  if (!m) m = check_matrix(b->dq, b->dq_stride, n, qc, a.dtype, false);
+  if (!m) m = check_matrix(b->dk, b->dk_stride, n, kc, a.dtype, kc == 0);
+  if (!m && (((uintptr_t)b->dq_weight | (uintptr_t)b->dk_weight) % size_of(a.param_dtype))) m = "a weight's gradient is not aligned to its element";
+  if (m) return invalid(t, entry, m);
+  const size_t es = size_of(a.dtype), ps = size_of(a.param_dtype);
+  const Region r[] = {region(a.q, a.q_stride, qc, n, es, false), region(a.k, a.k_stride, kc, n, es, false),
+                      region(a.q_out, a.q_out_stride, qc, n, es, false), region(a.k_out, a.k_out_stride, kc, n, es, false),
+                      region(b->dq, b->dq_stride, qc, n, es, true), region(b->dk, b->dk_stride, kc, n, es, true),
+                      vec(a.q_weight, a.head_dim, ps, false), vec(a.k_weight, a.head_dim, ps, false),
+                      vec(a.positions, a.pairs ? n : 0, a.position_bytes, false), vec(a.freq, a.pairs, 4, false),
+                      vec(b->dq_weight, a.head_dim, ps, true), vec(b->dk_weight, a.head_dim, ps, true)};
+  if (any_conflict(r, 12) || (n && kc && (b->dq == a.k || b->dq == a.k_out || b->dk == a.q || b->dk == a.q_out)))
+    return invalid(t, entry, "an output overlaps another argument without being the same matrix as its input or gradient");
+  const adacgd_status st = check_device(t, entry);
+  if (st != ADACGD_OK) return st;
+  if (n == 0) {
+    cudaError_t e = cudaSuccess;
+    if (b->dq_weight) e = cudaMemsetAsync(b->dq_weight, 0, a.head_dim * ps, t->at.stream);
+    if (e == cudaSuccess && b->dk_weight) e = cudaMemsetAsync(b->dk_weight, 0, a.head_dim * ps, t->at.stream);
+    return e == cudaSuccess ? ADACGD_OK : cuda_fail(t, entry, e);
+  }
+  return launched(t, entry, launch_qk_norm_backward(t->s, *b, t->at));
+}
+
+adacgd_status adacgd_attention(adacgd_train* t, const adacgd_attention_args* g) {
+  const char* entry = "adacgd_attention";
+  if (!t || !g) return invalid(t, entry, "context or arguments are NULL");
+  const adacgd_attention_inputs& a = g->in;
+  const char* m = check_attention(a);
+  const long long n = a.tokens, qc = (long long)a.heads * a.head_dim, kc = (long long)a.key_heads * a.head_dim;
+  if (!m) m = check_matrix(g->out, g->out_stride, n, qc, a.dtype, false);
+  if (!m && !aligned4(g->lse)) m = "lse is not aligned";
+  if (m) return invalid(t, entry, m);
+  const size_t es = size_of(a.dtype);
+  Region r[] = {region(a.q, a.q_stride, qc, n, es, false), region(a.k, a.k_stride, kc, n, es, false),
+                region(a.v, a.v_stride, kc, n, es, false), region(g->out, g->out_stride, qc, n, es, true),
+                vec(g->lse, n * a.heads, 4, true), vec(a.seq_start, a.sequences + 1, 4, false), vec(a.mask, n, 1, false)};
+  for (Region& e : r) e.matrix = false;
+  if (any_conflict(r, 7)) return invalid(t, entry, "an output overlaps another argument");
+  const adacgd_status st = check_device(t, entry);
+  if (st != ADACGD_OK) return st;
+  if (n == 0) return ADACGD_OK;
+  return launched(t, entry, launch_attention(*g, t->at));
+}
+
+adacgd_status adacgd_attention_backward(adacgd_train* t, const adacgd_attention_backward_args* g) {
+  const char* entry = "adacgd_attention_backward";
+  if (!t || !g) return invalid(t, entry, "context or arguments are NULL");
+  const adacgd_attention_inputs& a = g->in;
+  const char* m = check_attention(a);
+  const long long n = a.tokens, qc = (long long)a.heads * a.head_dim, kc = (long long)a.key_heads * a.head_dim;
+  if (!m) m = check_matrix(g->out, g->out_stride, n, qc, a.dtype, false);
+  if (!m) m = check_matrix(g->dout, g->dout_stride, n, qc, a.dtype, false);
+  if (!m) m = check_matrix(g->dq, g->dq_stride, n, qc, a.dtype, false);
+  if (!m) m = check_matrix(g->dk, g->dk_stride, n, kc, a.dtype, false);
+  if (!m) m = check_matrix(g->dv, g->dv_stride, n, kc, a.dtype, false);
+  if (!m && n > 0 && (!g->lse || !g->row_dot)) m = "lse and row_dot must be non-NULL";
+  if (!m && !(aligned4(g->lse) && aligned4(g->row_dot))) m = "lse or row_dot is not aligned";
+  if (m) return invalid(t, entry, m);
+  const size_t es = size_of(a.dtype);
+  Region r[] = {region(a.q, a.q_stride, qc, n, es, false), region(a.k, a.k_stride, kc, n, es, false),
+                region(a.v, a.v_stride, kc, n, es, false), region(g->out, g->out_stride, qc, n, es, false),
+                region(g->dout, g->dout_stride, qc, n, es, false), region(g->dq, g->dq_stride, qc, n, es, true),
+                region(g->dk, g->dk_stride, kc, n, es, true), region(g->dv, g->dv_stride, kc, n, es, true),
+                vec(g->lse, n * a.heads, 4, false), vec(g->row_dot, n * a.heads, 4, true),
+                vec(a.seq_start, a.sequences + 1, 4, false), vec(a.mask, n, 1, false)};
+  for (Region& e : r) e.matrix = false;
+  if (any_conflict(r, 12)) return invalid(t, entry, "an output overlaps another argument");
+  const adacgd_status st = check_device(t, entry);
+  if (st != ADACGD_OK) return st;
+  if (n == 0) return ADACGD_OK;
+  return launched(t, entry, launch_attention_backward(*g, t->at));
 }
 
 }  // extern "C"

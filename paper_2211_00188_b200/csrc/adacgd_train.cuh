@@ -17,13 +17,13 @@ constexpr int NORM_PARTS = 592;  // most partial rows of a weight gradient: four
 // The context's workspace, carved by carve_train_scratch.
 struct TrainScratch {
   u32* tickets;    // [NTRAIN_TICKETS] completion counts, zero between calls
-  float* tok_a;    // [tokens] a token's loss
-  float* tok_b;    // [tokens] its KL estimate
+  float* tok_a;    // [tokens] a token's loss;                      in the gradient of a lookup these four are the tokens' ids and
+  float* tok_b;    // [tokens] its KL estimate;                     numbers, being sorted
   float* tok_c;    // [tokens] 1 where the clipped term has taken the gradient
   float* seq;      // [tokens + 1] per sequence: weight or gradient coefficient; the last is the total
   double* part;    // [tokens + 3] per pair: loss; per CTA of the token sums: three of them
   double* own;     // [MAX_SMALL_CTAS][3] sums of the CTAs of a small policy loss
-  float* norm_part; // [NORM_PARTS][2][max_cols] partial weight and bias gradients
+  float* norm_part; // [NORM_PARTS][2][max_cols] partial weight and bias gradients, or partial rows of a table's gradient
   long long max_tokens, max_cols;
 };
 constexpr int NTRAIN_TICKETS = 64;
@@ -59,6 +59,12 @@ int launch_layer_norm_backward(const TrainScratch& s, const adacgd_norm_backward
 int launch_token_logp(const adacgd_token_rows& r, float* logp, float* lse, const Where& at);
 int launch_preference(const TrainScratch& s, const adacgd_preference_args& a, const Where& at);
 int launch_policy(const TrainScratch& s, const adacgd_policy_args& a, const Where& at);
+int launch_embedding(const adacgd_embedding_args& a, const Where& at);
+int launch_embedding_backward(const TrainScratch& s, const adacgd_embedding_backward_args& a, const Where& at);
+int launch_qk_norm(const adacgd_qk_norm_args& a, const Where& at);
+int launch_qk_norm_backward(const TrainScratch& s, const adacgd_qk_norm_backward_args& a, const Where& at);
+int launch_attention(const adacgd_attention_args& a, const Where& at);
+int launch_attention_backward(const adacgd_attention_backward_args& a, const Where& at);
 
 // ---- element types ----
 __device__ __forceinline__ float to_f(float v) { return v; }

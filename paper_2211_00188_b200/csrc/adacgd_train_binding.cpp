@@ -9,6 +9,7 @@
 // version of what a call has written moves on, as after any other modification in place.
 #include <Python.h>
 
+#include <cmath>
 #include <string>
 
 #include <ATen/core/Tensor.h>
@@ -80,23 +81,28 @@ struct Shape {
     place(t, name, p, stride);
   }
   void matrix(PyObject* o, const char* name, Use use, bool optional, const void** p, int64_t* stride) {
+    matrix_of(o, name, use, optional, rows, cols, type, p, stride);
+  }
+  // A matrix of its own shape and type.
+  void matrix_of(PyObject* o, const char* name, Use use, bool optional, int64_t n, int64_t width, at::ScalarType want, const void** p,
+                 int64_t* stride) {
     *p = nullptr;
     *stride = 0;
     const at::Tensor* t = tensor(o, name, optional);
     if (!t) return;
-    if (t->scalar_type() != type) refuse(name, "must have the type of the other matrices");
-    if (t->dim() != 2 || t->size(0) != rows || t->size(1) != cols)
-      refuse(name, "must have the shape (" + std::to_string(rows) + ", " + std::to_string(cols) + ")");
+    if (t->scalar_type() != want) refuse(name, want == type ? "must have the type of the other matrices" : std::string("must have the type ") + c10::toString(want));
+    if (t->dim() != 2 || t->size(0) != n || t->size(1) != width)
+      refuse(name, "must have the shape (" + std::to_string(n) + ", " + std::to_string(width) + ")");
     place(*t, name, p, stride);
     if (use == OUT) output(*t, name);
   }
   void place(const at::Tensor& t, const char* name, const void** p, int64_t* stride) const {
     if (!t.is_cuda() || t.get_device() != h->index) refuse(name, "must be on cuda:" + std::to_string(h->index));
-    if (cols > 1 && t.stride(1) != 1) refuse(name, "must have unit column stride");
+    if (t.size(1) > 1 && t.stride(1) != 1) refuse(name, "must have unit column stride");
     int64_t s = t.stride(0);
-    if (s < cols) {
-      if (rows > 1) refuse(name, "has rows that overlap");
-      s = cols;
+    if (s < t.size(1)) {
+      if (t.size(0) > 1) refuse(name, "has rows that overlap");
+      s = t.size(1);
     }
     *p = t.data_ptr();
     *stride = s;
@@ -120,7 +126,8 @@ struct Shape {
     const char* name;
     Use use;
   };
-  int params(std::initializer_list<Param> list, void** out) {
+  int params(std::initializer_list<Param> list, void** out) { return params(list, out, cols); }
+  int params(std::initializer_list<Param> list, void** out, int64_t n) {
     at::ScalarType want = type;
     bool first = true;
     for (const Param& e : list) {
@@ -134,7 +141,7 @@ struct Shape {
         } else if (t->scalar_type() != want) {
           refuse(e.name, "must have the type of the other weight-like arguments");
         }
-        *out = contiguous(*t, e.name, cols);
+        *out = contiguous(*t, e.name, n);
         if (e.use == OUT) output(*t, e.name);
       }
       ++out;
@@ -146,27 +153,36 @@ struct Shape {
     r->tokens = rows;
     r->vocab = cols;
     r->dtype = code;
-    const at::Tensor& y = *tensor(labels, "labels", false);
-    if (y.scalar_type() != at::kLong && y.scalar_type() != at::kInt) refuse("labels", "must be int64 or int32");
-    r->label_bytes = y.scalar_type() == at::kLong ? 8 : 4;
-    r->labels = contiguous(y, "labels", rows);
-    r->mask = nullptr;
-    if (const at::Tensor* m = tensor(mask, "mask", true)) {
-      if (m->scalar_type() != at::kBool && m->scalar_type() != at::kByte) refuse("mask", "must be bool or uint8");
-      r->mask = (const uint8_t*)contiguous(*m, "mask", rows);
-    }
+    r->labels = whole_numbers(labels, "labels", rows, &r->label_bytes);
+    r->mask = counted(mask, rows);
+    runs(seq_start, sequences, &r->seq_start, &r->sequences);
+  }
+  // int64 or int32
+  const void* whole_numbers(PyObject* o, const char* name, int64_t n, int32_t* bytes) {
+    const at::Tensor& y = *tensor(o, name, false);
+    if (y.scalar_type() != at::kLong && y.scalar_type() != at::kInt) refuse(name, "must be int64 or int32");
+    *bytes = y.scalar_type() == at::kLong ? 8 : 4;
+    return contiguous(y, name, n);
+  }
+  const uint8_t* counted(PyObject* mask, int64_t n) {
+    const at::Tensor* m = tensor(mask, "mask", true);
+    if (!m) return nullptr;
+    if (m->scalar_type() != at::kBool && m->scalar_type() != at::kByte) refuse("mask", "must be bool or uint8");
+    return (const uint8_t*)contiguous(*m, "mask", n);
+  }
+  void runs(PyObject* seq_start, PyObject* sequences, const int32_t** start, int64_t* count) {
     int64_t given = -1;
     if (sequences != Py_None) {
       given = PyLong_AsLongLong(sequences);
       if (given == -1 && PyErr_Occurred()) throw Refused{""};
     }
-    r->seq_start = nullptr;
-    r->sequences = given < 0 && sequences == Py_None ? 1 : given;
+    *start = nullptr;
+    *count = given < 0 && sequences == Py_None ? 1 : given;
     if (const at::Tensor* s = tensor(seq_start, "seq_start", true)) {
       if (s->scalar_type() != at::kInt) refuse("seq_start", "must be int32");
       if (sequences != Py_None && given != s->numel() - 1) refuse("sequences", "and seq_start disagree");
-      r->sequences = s->numel() - 1;
-      r->seq_start = (const int32_t*)contiguous(*s, "seq_start", s->numel());
+      *count = s->numel() - 1;
+      *start = (const int32_t*)contiguous(*s, "seq_start", s->numel());
     }
   }
 };
@@ -340,6 +356,180 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (handle, tokens, table, out, scale, mask)
+PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(a, n, 6, [&](Shape& s, auto ready) -> long {
+    adacgd_embedding_args r;
+    s.lead(a[2], "table", &r.table, &r.table_stride);
+    r.vocab = s.rows;
+    r.cols = s.cols;
+    r.dtype = s.code;
+    const at::Tensor& ids = *tensor(a[1], "tokens", false);
+    r.tokens = ids.numel();
+    r.ids = s.whole_numbers(a[1], "tokens", r.tokens, &r.id_bytes);
+    r.mask = s.counted(a[5], r.tokens);
+    s.matrix_of(a[3], "out", OUT, false, r.tokens, s.cols, s.type, (const void**)&r.out, &r.out_stride);
+    r.scale = (float)number(a[4]);
+    r.reserved = 0;
+    return ready() ? (long)adacgd_embedding(s.h->ctx, &r) : RETRY;
+  });
+}
+
+// (handle, tokens, dout, dtable, scale, mask, base)
+PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(a, n, 7, [&](Shape& s, auto ready) -> long {
+    adacgd_embedding_backward_args r;
+    s.lead(a[2], "dout", &r.dout, &r.dout_stride);
+    r.tokens = s.rows;
+    r.cols = s.cols;
+    r.dtype = s.code;
+    r.ids = s.whole_numbers(a[1], "tokens", s.rows, &r.id_bytes);
+    r.mask = s.counted(a[5], s.rows);
+    const at::Tensor& d = *tensor(a[3], "dtable", false);
+    if (d.dim() != 2) refuse("dtable", "must be a 2-D tensor");
+    if (d.scalar_type() != s.type && d.scalar_type() != at::kFloat) refuse("dtable", "must be float32 or of dout's type");
+    r.vocab = d.size(0);
+    r.table_dtype = type_code(d.scalar_type());
+    s.matrix_of(a[3], "dtable", OUT, false, r.vocab, s.cols, d.scalar_type(), (const void**)&r.dtable, &r.dtable_stride);
+    s.matrix_of(a[6], "base", IN, true, r.vocab, s.cols, d.scalar_type(), &r.base, &r.base_stride);
+    r.scale = (float)number(a[4]);
+    return ready() ? (long)adacgd_embedding_backward(s.h->ctx, &r) : RETRY;
+  });
+}
+
+int64_t whole(PyObject* o) {
+  const int64_t v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw Refused{""};
+  return v;
+}
+
+// What qk_norm and its backward pass share: q and k (the inputs), positions, freq, head_dim, eps, interleaved; the weights are the caller's.
+void heads_of(Shape& s, adacgd_qk_norm_args* r, PyObject* q, PyObject* k, PyObject* positions, PyObject* freq, PyObject* head_dim, PyObject* eps,
+              PyObject* interleaved) {
+  s.lead(q, "q", &r->q, &r->q_stride);
+  const int64_t dim = whole(head_dim);
+  if (dim < 1 || dim > ADACGD_TRAIN_MAX_HEAD) refuse("head_dim", "must be in [1, " + std::to_string(ADACGD_TRAIN_MAX_HEAD) + "]");
+  if (s.cols < 1 || s.cols % dim) refuse("q", "must have a multiple of head_dim columns");
+  r->head_dim = (int32_t)dim;
+  r->tokens = s.rows;
+  r->heads = s.cols / dim;
+  r->key_heads = 0;
+  r->dtype = s.code;
+  r->k = nullptr;
+  r->k_stride = 0;
+  if (const at::Tensor* t = tensor(k, "k", true)) {
+    if (t->dim() != 2 || t->size(1) < 1 || t->size(1) % dim) refuse("k", "must be a 2-D tensor with a multiple of head_dim columns");
+    r->key_heads = t->size(1) / dim;
+    s.matrix_of(k, "k", IN, false, s.rows, t->size(1), s.type, &r->k, &r->k_stride);
+  }
+  r->pairs = 0;
+  r->freq = nullptr;
+  r->positions = nullptr;
+  r->position_bytes = 8;
+  if (const at::Tensor* f = tensor(freq, "freq", true)) {
+    if (f->scalar_type() != at::kFloat) refuse("freq", "must have the type Float");
+    if (f->numel() > dim / 2) refuse("freq", "must have at most head_dim / 2 elements");
+    r->pairs = (int32_t)f->numel();
+    r->freq = (const float*)s.contiguous(*f, "freq", f->numel());
+    if (positions == Py_None) refuse("positions", "must be given with freq");
+    r->positions = s.whole_numbers(positions, "positions", s.rows, &r->position_bytes);
+  }
+  r->eps = (float)number(eps);
+  r->interleaved = truth(interleaved);
+  r->reserved = 0;
+}
+
+// (handle, q, k, q_out, k_out, positions, freq, head_dim, q_weight, k_weight, eps, interleaved)
+PyObject* qk_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(a, n, 12, [&](Shape& s, auto ready) -> long {
+    adacgd_qk_norm_args r;
+    heads_of(s, &r, a[1], a[2], a[5], a[6], a[7], a[10], a[11]);
+    const bool keys = r.key_heads > 0;
+    if (!keys && (a[4] != Py_None || a[9] != Py_None)) refuse("k_out", "and k_weight go with k");
+    MAT(q_out, 3, OUT, false);
+    s.matrix_of(a[4], "k_out", OUT, !keys, s.rows, r.key_heads * r.head_dim, s.type, (const void**)&r.k_out, &r.k_out_stride);
+    void* p[2];
+    r.param_dtype = s.params({{a[8], "q_weight", IN}, {a[9], "k_weight", IN}}, p, r.head_dim);
+    r.q_weight = p[0];
+    r.k_weight = p[1];
+    return ready() ? (long)adacgd_qk_norm(s.h->ctx, &r) : RETRY;
+  });
+}
+
+// (handle, dq_out, dk_out, q, k, dq, dk, positions, freq, head_dim, q_weight, k_weight, dq_weight, dk_weight, eps, interleaved)
+PyObject* qk_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(a, n, 16, [&](Shape& s, auto ready) -> long {
+    adacgd_qk_norm_backward_args r;
+    heads_of(s, &r.f, a[3], a[4], a[7], a[8], a[9], a[14], a[15]);
+    const bool keys = r.f.key_heads > 0;
+    const int64_t kc = r.f.key_heads * r.f.head_dim;
+    if (!keys && (a[2] != Py_None || a[6] != Py_None || a[11] != Py_None || a[13] != Py_None)) refuse("dk_out", "dk, k_weight and dk_weight go with k");
+    s.matrix_of(a[1], "dq_out", IN, false, s.rows, s.cols, s.type, (const void**)&r.f.q_out, &r.f.q_out_stride);
+    s.matrix_of(a[2], "dk_out", IN, !keys, s.rows, kc, s.type, (const void**)&r.f.k_out, &r.f.k_out_stride);
+    s.matrix_of(a[5], "dq", OUT, false, s.rows, s.cols, s.type, (const void**)&r.dq, &r.dq_stride);
+    s.matrix_of(a[6], "dk", OUT, !keys, s.rows, kc, s.type, (const void**)&r.dk, &r.dk_stride);
+    void* p[4];
+    r.f.param_dtype = s.params({{a[10], "q_weight", IN}, {a[11], "k_weight", IN}, {a[12], "dq_weight", OUT}, {a[13], "dk_weight", OUT}}, p, r.f.head_dim);
+    r.f.q_weight = p[0];
+    r.f.k_weight = p[1];
+    r.dq_weight = p[2];
+    r.dk_weight = p[3];
+    return ready() ? (long)adacgd_qk_norm_backward(s.h->ctx, &r) : RETRY;
+  });
+}
+
+// q, k and v, the heads they hold, and the sequences.
+void attention_of(Shape& s, adacgd_attention_inputs* r, PyObject* q, PyObject* k, PyObject* v, PyObject* heads, PyObject* sequences, PyObject* seq_start,
+                  PyObject* causal, PyObject* scale, PyObject* mask) {
+  s.lead(q, "q", &r->q, &r->q_stride);
+  const int64_t count = whole(heads);
+  if (count < 1 || count > 65535 || s.cols < 1 || s.cols % count) refuse("heads", "must be in [1, 65535] and divide q's columns");
+  const int64_t dim = s.cols / count;
+  if (dim > ADACGD_ATTENTION_MAX_HEAD) refuse("q", "must have at most " + std::to_string(ADACGD_ATTENTION_MAX_HEAD) + " columns a head");
+  const at::Tensor& kt = *tensor(k, "k", false);
+  const int64_t kc = kt.dim() == 2 ? kt.size(1) : 0;
+  if (kc < 1 || kc % dim || count % (kc / dim)) refuse("k", "must be a 2-D tensor of key heads whose number divides heads");
+  r->heads = (int32_t)count;
+  r->key_heads = (int32_t)(kc / dim);
+  r->head_dim = (int32_t)dim;
+  r->tokens = s.rows;
+  r->dtype = s.code;
+  s.matrix_of(k, "k", IN, false, s.rows, kc, s.type, &r->k, &r->k_stride);
+  s.matrix_of(v, "v", IN, false, s.rows, kc, s.type, &r->v, &r->v_stride);
+  s.runs(seq_start, sequences, &r->seq_start, &r->sequences);
+  r->causal = truth(causal);
+  r->scale = scale == Py_None ? (float)(1.0 / std::sqrt((double)dim)) : (float)number(scale);
+  r->mask = s.counted(mask, s.rows);
+}
+
+// (handle, q, k, v, out, lse, heads, sequences, seq_start, causal, scale, mask)
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(a, n, 12, [&](Shape& s, auto ready) -> long {
+    adacgd_attention_args r;
+    attention_of(s, &r.in, a[1], a[2], a[3], a[6], a[7], a[8], a[9], a[10], a[11]);
+    MAT(out, 4, OUT, false);
+    r.lse = (float*)s.vector(a[5], "lse", OUT, true, s.rows * r.in.heads, at::kFloat);
+    return ready() ? (long)adacgd_attention(s.h->ctx, &r) : RETRY;
+  });
+}
+
+// (handle, dout, q, k, v, out, lse, row_dot, dq, dk, dv, heads, sequences, seq_start, causal, scale, mask)
+PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(a, n, 17, [&](Shape& s, auto ready) -> long {
+    adacgd_attention_backward_args r;
+    attention_of(s, &r.in, a[2], a[3], a[4], a[11], a[12], a[13], a[14], a[15], a[16]);
+    const int64_t kc = (int64_t)r.in.key_heads * r.in.head_dim;
+    MAT(dout, 1, IN, false);
+    MAT(out, 5, IN, false);
+    r.lse = (const float*)s.vector(a[6], "lse", IN, false, s.rows * r.in.heads, at::kFloat);
+    r.row_dot = (float*)s.vector(a[7], "row_dot", OUT, false, s.rows * r.in.heads, at::kFloat);
+    MAT(dq, 8, OUT, false);
+    s.matrix_of(a[9], "dk", OUT, false, s.rows, kc, s.type, (const void**)&r.dk, &r.dk_stride);
+    s.matrix_of(a[10], "dv", OUT, false, s.rows, kc, s.type, (const void**)&r.dv, &r.dv_stride);
+    return ready() ? (long)adacgd_attention_backward(s.h->ctx, &r) : RETRY;
+  });
+}
+
 void release(PyObject* c) { delete (Handle*)PyCapsule_GetPointer(c, "adacgd_train"); }
 
 // bind(context, device index, stream) -> handle
@@ -365,7 +555,9 @@ PyObject* force(PyObject*, PyObject* args) {
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(dropout),         FAST(layer_norm),      FAST(layer_norm_backward), FAST(token_logp),
-                         FAST(preference_loss), FAST(policy_loss),     {"bind", bind, METH_VARARGS, nullptr},
+                         FAST(preference_loss), FAST(policy_loss),     FAST(embedding),           FAST(embedding_backward),
+                         FAST(qk_norm),         FAST(qk_norm_backward), FAST(attention),          FAST(attention_backward),
+                         {"bind", bind, METH_VARARGS, nullptr},
                          {"force", force, METH_VARARGS, nullptr},      {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train_binding", "Binding of the training operators.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,7 +1,7 @@
 """Operators of a worker's local training step: the entry points of include/adacgd_train.h on torch tensors.
 
-They stand between and behind a model's matrix products: layer norm with the residual sum and dropout in front of it,
-dropout, log-probabilities of given tokens, and the preference and policy losses with their gradients with respect to
+They stand between and behind a model's matrix products: embedding lookup, norm and rotation of queries and keys, attention,
+each with its backward pass, layer norm with the residual sum and dropout in front of it, dropout, log-probabilities of given tokens, and the preference and policy losses with their gradients with respect to
 the logits.  What a worker computes with them is a gradient X_i = grad f_i(x), which `AdaCGD.compress` takes.
 
 Every output is a tensor of the caller's; the arithmetic is in the kernels of libadacgd.so and there is no other path.
@@ -19,7 +19,8 @@ from .binding import AdacgdError, load_library
 TRAIN_SYMBOLS = [
     "adacgd_train_workspace_bytes", "adacgd_train_init", "adacgd_train_destroy", "adacgd_train_last_error",
     "adacgd_train_launch_count", "adacgd_dropout", "adacgd_layer_norm", "adacgd_layer_norm_backward",
-    "adacgd_token_logp", "adacgd_preference_loss", "adacgd_policy_loss",
+    "adacgd_token_logp", "adacgd_preference_loss", "adacgd_policy_loss", "adacgd_embedding", "adacgd_embedding_backward",
+    "adacgd_qk_norm", "adacgd_qk_norm_backward", "adacgd_attention", "adacgd_attention_backward",
 ]
 MAX_COLS = 32768
 PREFERENCE_KINDS = {"sigmoid": 0, "hinge": 1, "square": 2}
@@ -43,7 +44,8 @@ def load_training_library():
         lib.adacgd_train_launch_count.argtypes = [vp]
         lib.adacgd_train_launch_count.restype = i64
         for name in ("adacgd_dropout", "adacgd_layer_norm", "adacgd_layer_norm_backward", "adacgd_preference_loss",
-                     "adacgd_policy_loss"):
+                     "adacgd_policy_loss", "adacgd_embedding", "adacgd_embedding_backward", "adacgd_qk_norm", "adacgd_qk_norm_backward",
+                     "adacgd_attention", "adacgd_attention_backward"):
             getattr(lib, name).argtypes = [vp, vp]
         lib.adacgd_token_logp.argtypes = [vp, vp, vp, vp]
         _bound = True
@@ -69,7 +71,7 @@ def _load_binding():
 class TrainingOps:
     """Owns a context of the training operators and the device workspace behind it.
 
-    max_tokens bounds the rows of a norm's backward pass and of logits, max_cols the columns of a norm's backward pass.
+    max_tokens bounds the rows of a norm's or lookup's backward pass and of logits, max_cols the columns of those backward passes.
     Work runs on `stream` (default: the stream that is current now).  A call made while another stream is current is
     ordered behind that stream's work, and that stream waits for it.  One thread at a time per context.
 
@@ -204,6 +206,67 @@ class TrainingOps:
         call = self.native.policy_loss
         args = (self.handle, logits, labels, old_logp, advantages, loss, dlogits, mask, sequences, seq_start, ref_logp, clip_low,
                 clip_high, kl_beta, per_sequence, grad_scale, logp, stats)
+        status = call(*args)
+        if status:
+            self._again(status, call, *args)
+
+    def embedding(self, tokens, table, out, *, scale: float = 1.0, mask=None):
+        """adacgd_embedding: out[t] = scale * table[tokens[t]], 0 where the mask is false."""
+        call, args = self.native.embedding, (self.handle, tokens, table, out, scale, mask)
+        status = call(*args)
+        if status:
+            self._again(status, call, *args)
+
+    def embedding_backward(self, tokens, dout, dtable, *, scale: float = 1.0, mask=None, base=None):
+        """adacgd_embedding_backward: dtable = [base +] scale * sum of dout's rows by token, every row of it; dtable may be base
+        itself.  dtable is of dout's type or float32."""
+        call, args = self.native.embedding_backward, (self.handle, tokens, dout, dtable, scale, mask, base)
+        status = call(*args)
+        if status:
+            self._again(status, call, *args)
+
+    def qk_norm(self, q, k, q_out, k_out, positions=None, freq=None, *, head_dim: int, q_weight=None, k_weight=None, eps: float = 1e-6,
+                interleaved: bool = False):
+        """adacgd_qk_norm: every head of q and k divided by its root mean square, times the weight, its first 2 len(freq) elements
+        turned by the angles position * freq (float32), in halves or, interleaved, in neighbours.  k and k_out may be None."""
+        call = self.native.qk_norm
+        args = (self.handle, q, k, q_out, k_out, positions, freq, head_dim, q_weight, k_weight, eps, interleaved)
+        status = call(*args)
+        if status:
+            self._again(status, call, *args)
+
+    def qk_norm_backward(self, dq_out, dk_out, q, k, dq, dk, positions=None, freq=None, *, head_dim: int, q_weight=None, k_weight=None,
+                         dq_weight=None, dk_weight=None, eps: float = 1e-6, interleaved: bool = False):
+        """adacgd_qk_norm_backward: dq, dk and where given the weights' gradients, from the gradients of the outputs and the inputs
+        of qk_norm."""
+        call = self.native.qk_norm_backward
+        args = (self.handle, dq_out, dk_out, q, k, dq, dk, positions, freq, head_dim, q_weight, k_weight, dq_weight, dk_weight, eps,
+                interleaved)
+        status = call(*args)
+        if status:
+            self._again(status, call, *args)
+
+    def attention(self, q, k, v, out, *, heads: int, lse=None, sequences: Optional[int] = None, seq_start=None, causal: bool = True,
+                  scale: Optional[float] = None, mask=None):
+        """adacgd_attention over each sequence's tokens; scale defaults to head_dim ** -0.5.  k and v hold the key heads, whose number
+        divides heads.  lse, float32 [heads, tokens], is what the backward pass needs.  Tokens where the mask is false are neither
+        queries nor keys; their out is 0."""
+        if sequences is None and seq_start is None:
+            raise ValueError("attention needs sequences or seq_start")
+        call = self.native.attention
+        args = (self.handle, q, k, v, out, lse, heads, sequences, seq_start, causal, scale, mask)
+        status = call(*args)
+        if status:
+            self._again(status, call, *args)
+
+    def attention_backward(self, dout, q, k, v, out, lse, row_dot, dq, dk, dv, *, heads: int, sequences: Optional[int] = None,
+                           seq_start=None, causal: bool = True, scale: Optional[float] = None, mask=None):
+        """adacgd_attention_backward: dq, dk and dv from dout and what attention took and stored.  row_dot, float32 [heads, tokens], is
+        written on the way: the products of dout's and out's rows."""
+        if sequences is None and seq_start is None:
+            raise ValueError("attention_backward needs sequences or seq_start")
+        call = self.native.attention_backward
+        args = (self.handle, dout, q, k, v, out, lse, row_dot, dq, dk, dv, heads, sequences, seq_start, causal, scale, mask)
         status = call(*args)
         if status:
             self._again(status, call, *args)
