@@ -19,7 +19,7 @@ BINDING_SOURCE = "adacgd_train_binding.cpp"
 STAMP = BINDING + ".for"   # the interpreter and torch the binding was compiled for
 SOURCES = ["adacgd_api.cu", "adacgd_compress.cu", "adacgd_small.cu", "adacgd_noalloc.cu", "adacgd_gradient.cu",
            "adacgd_train.cu", "adacgd_train_norm.cu", "adacgd_train_loss.cu", "adacgd_train_embed.cu", "adacgd_train_rotary.cu",
-           "adacgd_train_attention.cu"]
+           "adacgd_train_attention.cu", "adacgd_train_attention_mma.cu"]
 
 
 def nvcc_path() -> str:

@@ -381,8 +381,16 @@ template <typename T> int bwd_t(const adacgd_attention_backward_args& g, const W
     default: { typedef __nv_bfloat16 T; return call; }         \
   }
 
-int launch_attention(const adacgd_attention_args& a, const Where& at) { BY_TYPE(a.in.dtype, (fwd_t<T>(a, at))) }
+int launch_attention(const adacgd_attention_args& a, const Where& at) {
+  const int n = launch_attention_mma(a, at);
+  if (n) return n;
+  BY_TYPE(a.in.dtype, (fwd_t<T>(a, at)))
+}
 
-int launch_attention_backward(const adacgd_attention_backward_args& a, const Where& at) { BY_TYPE(a.in.dtype, (bwd_t<T>(a, at))) }
+int launch_attention_backward(const adacgd_attention_backward_args& a, const Where& at) {
+  const int n = launch_attention_backward_mma(a, at);
+  if (n) return n;
+  BY_TYPE(a.in.dtype, (bwd_t<T>(a, at)))
+}
 
 }  // namespace adacgd

@@ -1,0 +1,809 @@
+// Attention and its backward pass for the 16-bit types on the tensor cores: heads of up to 128 elements (a multiple of 8), rows on
+// 16 bytes.  Bound by the products and, beside them, by the exponentials (16 a clock and SM, where a product of 128 x 128 x 128 takes
+// 512 clocks and its scores' exponentials 1024).
+//
+// Common to the three kernels.  A CTA holds one tile of rows and walks over the tiles it meets; tiles are 128 rows of 64 or
+// 128 columns in shared memory, rows of 128 bytes, swizzled, brought by one warp's tensor copies, which fill columns behind a
+// head's end with zeros.  One thread issues the products; their operands are tiles and, for probabilities and ds, tensor memory, where
+// the eight other warps, a thread a row, put them in place of the scores they were made from.
+// A row that does not count, or belongs to another sequence, must not reach a sum over rows even as 0 x NaN: where a tile that is summed over has
+// such rows, the copying warp sets them to zero before it hands the tile on.
+//
+// The backward pass is two kernels that each compute the scores again, seven products for the five that are needed: every sum stays in one
+// CTA's tensor memory, without atomics, and dq needs no binary32 array.
+#include <type_traits>
+
+#include "adacgd_tcgen05.cuh"
+#include "adacgd_train_attention.cuh"
+
+namespace adacgd {
+namespace {
+
+constexpr int TILE = 128, HALF = TILE * 128;       // rows of a tile; bytes of 64 of its columns
+constexpr int MMA_CTA = 320, MMA_WARP = 8, COPY_WARP = 9;
+
+struct Maps {
+  CUtensorMap q, k, v, dout;
+};
+
+// ---- the copying warp ----
+template <int DP> __device__ __forceinline__ void copy_tile(u32 dst, const CUtensorMap* map, int head, long long row, u32 bar) {
+#pragma unroll
+  for (int h = 0; h < DP / 64; ++h) tma_load_3d(dst + h * HALF, map, 64 * h, head, (int)row, bar);
+}
+// Bits of the rows first .. first + 127 that count.
+__device__ __forceinline__ void counted(const adacgd_attention_inputs& a, const Tile& t, int first, u32 (&words)[4]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int i = first + 32 * w + lane;
+    words[w] = __ballot_sync(0xffffffffu, i < t.length && (!a.mask || a.mask[t.row + i]));
+  }
+}
+__device__ __forceinline__ bool all_count(const u32 (&words)[4]) { return (words[0] & words[1] & words[2] & words[3]) == 0xffffffffu; }
+
+// Brings a tile and hands it on by `full`.  Rows whose bit is not set are zeroed where `clean`: then the copy arrives at `aside` first.
+template <int DP>
+__device__ __forceinline__ bool bring(u32 dst, const CUtensorMap* map, int head, long long row, const u32 (&words)[4], bool clean, u32 full, u32 aside,
+                                      u32& aside_parity, volatile int* dead) {
+  const int lane = threadIdx.x & 31;
+  const bool fix = clean && !all_count(words);
+  if (lane == 0) {
+    mbar_expect(fix ? aside : full, DP * 256);
+    copy_tile<DP>(dst, map, head, row, fix ? aside : full);
+  }
+  if (!fix) return true;
+  if (!mbar_wait(aside, aside_parity, dead)) return false;
+  aside_parity ^= 1;
+#pragma unroll 1
+  for (int r = lane >> 3; r < TILE; r += 4) {
+    if (words[r >> 5] >> (r & 31) & 1) continue;
+#pragma unroll
+    for (int h = 0; h < DP / 64; ++h)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + h * HALF + r * 128 + (lane & 7) * 16), "r"(0) : "memory");
+  }
+  fence_async_smem();
+  __syncwarp();
+  if (lane == 0) mbar_arrive(full);
+  return true;
+}
+
+// After a wait that ran out: the copies under way must have ended before the CTA's memory goes to another.
+__device__ __forceinline__ void settle(u32 bar, u32 parity) { mbar_wait(bar, parity, nullptr); }
+
+// ---- the product thread ----
+// d = a b^T over 16 * STEPS columns of both tiles.
+template <bool BF16, int DP> __device__ __forceinline__ void product_nt(u32 d, u32 a, u32 b) {
+#pragma unroll
+  for (int k = 0; k < DP / 16; ++k) {
+    const u32 off = (k / 4) * HALF + (k % 4) * 32;
+    mma_ss(d, operand(a + off, 16), operand(b + off, 16), product_of(BF16, TILE, false), k > 0);
+  }
+}
+// d [128 x DP] += p tile, p in tensor memory: 16 rows of the tile a step.  The second half of p's columns begins `gap` columns behind the
+// first one's start.
+template <bool BF16, int DP> __device__ __forceinline__ void product_pn(u32 d, u32 p, u32 gap, u32 tile, bool add) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    mma_ts(d, p + (k / 4) * gap + (k % 4) * 8, operand(tile + k * 2048, HALF), product_of(BF16, DP, true), add || k > 0);
+}
+
+// ---- rows of results ----
+// Stores factor * (DP columns of tensor memory) as one row of `dim` elements, or zeros.
+template <bool BF16, int DP>
+__device__ __forceinline__ void store_row(void* base, long long stride, long long row, int head, int dim, u32 tmem, float factor, bool inside, bool zero) {
+  char* const to = (char*)base + (row * stride + (long long)head * dim) * 2;
+#pragma unroll
+  for (int c = 0; c < DP; c += 32) {
+    u32 r[32];
+    __syncwarp();
+    tmem_ld32(tmem + c, r);
+    tmem_wait_ld();
+    tmem_hold(r);
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) {
+      if (!inside || c + j >= dim) continue;
+      u32 w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = zero ? 0u : pack2<BF16>(__uint_as_float(r[j + 2 * i]) * factor, __uint_as_float(r[j + 2 * i + 1]) * factor);
+      *reinterpret_cast<uint4*>(to + (c + j) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+// What a kernel leaves whose wait has run out: NaN in either type.
+__device__ __forceinline__ void poison_row(void* base, long long stride, long long row, int head, int dim) {
+  unsigned short* const to = (unsigned short*)base + row * stride + (long long)head * dim;
+  for (int d = 0; d < dim; ++d) to[d] = 0x7fff;
+}
+
+__device__ __forceinline__ u32 low_bits(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
+
+// --------------------------------------------------------------------------
+// forward
+// --------------------------------------------------------------------------
+// A CTA takes two tiles of queries of a head, A and B.  While the products of one run, four warps turn the scores of the other into
+// probabilities: S = Q K^T, the row's maximum, p = 2^(c s - c max) in S's place, O += p V.  The maximum that p is taken against is
+// moved only when it has grown by more than 2^8, so O, which stays in tensor memory, is hardly ever rescaled; p is at most 256 then, and the
+// division by the sum at the end takes it out.
+template <int DP> struct FwdLayout {
+  static constexpr int BYTES = DP * 256, STAGES = DP == 128 ? 5 : 8, RING = 2 * BYTES, BARS = RING + STAGES * BYTES;
+  static constexpr int TOTAL = BARS + 256;
+};
+
+template <bool BF16, int DP>
+__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_mma(const __grid_constant__ Maps maps, adacgd_attention_args g) {
+  typedef FwdLayout<DP> L;
+  extern __shared__ __align__(1024) unsigned char mma_smem[];
+  const adacgd_attention_inputs& a = g.in;
+  const int head = (int)(blockIdx.x % a.heads);
+  Tile t;
+  if (!tile_of(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, 2 * TILE, &t)) return;   // long ones first where causal
+  const u32 base = smem_addr(mma_smem), bars = base + L::BARS;
+  const u32 q_full = bars, aside = bars + 8, s_full = bars + 16, p_full = bars + 32, o_full = bars + 48, full = bars + 64, empty = full + 8 * L::STAGES;
+  u32* const tmem_at = reinterpret_cast<u32*>(mma_smem + L::BARS + 64 + 16 * L::STAGES);
+  volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    mbar_init(aside, 1);
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(s_full + 8 * x, 1);
+      mbar_init(p_full + 8 * x, 128);
+      mbar_init(o_full + 8 * x, 1);
+    }
+    for (int i = 0; i < L::STAGES; ++i) {
+      mbar_init(full + 8 * i, 1);
+      mbar_init(empty + 8 * i, 1);
+    }
+    *dead = 0;
+    mbar_init_fence();
+  }
+  if (warp == MMA_WARP) tmem_alloc(smem_addr(tmem_at), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const u32 tmem = *tmem_at;
+  const int kh = head / (a.heads / a.key_heads);
+  const int tiles = (t.length + TILE - 1) / TILE;              // of keys
+  int count[2];                                                // that A and B meet
+  count[0] = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
+  count[1] = t.first + TILE >= t.length ? 0 : (a.causal ? min(tiles, t.first / TILE + 2) : tiles);
+  const int n = max(count[0], count[1]);
+  if (warp == COPY_WARP) {
+    if (lane == 0) {
+      mbar_expect(q_full, (count[1] ? 2 : 1) * L::BYTES);
+      copy_tile<DP>(base, &maps.q, head, t.row + t.first, q_full);
+      if (count[1]) copy_tile<DP>(base + L::BYTES, &maps.q, head, t.row + t.first + TILE, q_full);
+    }
+    u32 side = 0, words[4];
+    int i = 0;
+    bool ok = true;
+    for (; ok && i < 2 * n; ++i) {                             // tiles of keys and values in turn, the last ones first
+      const int st = i % L::STAGES, first = (n - 1 - i / 2) * TILE;
+      if (i >= L::STAGES && !mbar_wait(empty + 8 * st, (i / L::STAGES - 1) & 1, dead)) break;
+      if (!(i & 1)) counted(a, t, first, words);
+      ok = bring<DP>(base + L::RING + st * L::BYTES, i & 1 ? &maps.v : &maps.k, kh, t.row + first, words, i & 1, full + 8 * st, aside, side, dead);
+    }
+    if (*dead) {
+      settle(q_full, 0);
+      for (int b = max(0, i - L::STAGES); b < i; ++b) settle(full + 8 * (b % L::STAGES), (b / L::STAGES) & 1);
+    }
+  } else if (warp == MMA_WARP) {
+    if (lane == 0) {
+      bool ok = mbar_wait(q_full, 0, dead);
+      for (int j = 0; ok && j <= n; ++j) {
+        const int ik = 2 * j, iv = 2 * j - 1, sk = ik % L::STAGES, sv = iv % L::STAGES;
+        if (j < n && !(ok = mbar_wait(full + 8 * sk, (ik / L::STAGES) & 1, dead))) break;
+        if (j > 0 && !(ok = mbar_wait(full + 8 * sv, (iv / L::STAGES) & 1, dead))) break;
+        for (int x = 0; ok && x < 2; ++x) {
+          const int u = j - (n - count[x]);                    // the step as x counts
+          if (u < 0 || count[x] == 0) continue;
+          const u32 s = tmem + x * TILE, o = tmem + 2 * TILE + x * DP;
+          if (u > 0) {
+            if (!(ok = mbar_wait(p_full + 8 * x, (u - 1) & 1, dead))) break;
+            tc_fence_after();
+            product_pn<BF16, DP>(o, s, 32, base + L::RING + sv * L::BYTES, u > 1);
+          }
+          if (j < n) {
+            tc_fence_after();
+            product_nt<BF16, DP>(s, base + x * L::BYTES, base + L::RING + sk * L::BYTES);
+            mma_commit(s_full + 8 * x);
+          } else {
+            mma_commit(o_full + 8 * x);
+          }
+        }
+        if (!ok) break;
+        if (j < n) mma_commit(empty + 8 * sk);
+        if (j > 0) mma_commit(empty + 8 * sv);
+      }
+      if (*dead) {
+        mma_commit(aside);                                     // nobody else uses it any more, or its wait has run out too
+        settle(aside, 0);
+      }
+    }
+  } else {
+    const int x = warp >> 2, i = t.first + x * TILE + (warp & 3) * 32 + lane;
+    const u32 lanes = (u32)(warp & 3) << 21, s_at = tmem + x * TILE + lanes, o_at = tmem + 2 * TILE + x * DP + lanes;
+    const float c = a.scale * LOG2E;
+    float top = -INFINITY, sum = 0.f;
+    bool ok = true;
+    for (int u = 0; u < count[x]; ++u) {
+      const int j0 = (count[x] - 1 - u) * TILE;
+      u32 words[4];
+      const bool mask = a.mask || j0 + TILE > t.length || (a.causal && j0 + TILE > t.first + x * TILE);
+      if (mask) {
+        counted(a, t, j0, words);
+        if (a.causal)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) words[w] &= low_bits(i + 1 - j0 - 32 * w);
+      }
+      if (!(ok = mbar_wait(s_full + 8 * x, u & 1, dead))) break;
+      tc_fence_after();
+      u32 s[4][32];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) tmem_ld32(s_at + 32 * w, s[w]);
+      tmem_wait_ld();
+#pragma unroll
+      for (int w = 0; w < 4; ++w) tmem_hold(s[w]);
+      if (mask)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int k = 0; k < 32; ++k) s[w][k] = words[w] >> k & 1 ? s[w][k] : 0xff800000u;
+      float m[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        m[w] = __uint_as_float(s[w][0]);
+#pragma unroll
+        for (int k = 1; k < 32; ++k) m[w] = fmaxf(m[w], __uint_as_float(s[w][k]));
+      }
+      const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+      if (u == 0) {
+        top = most;
+      } else if (__any_sync(0xffffffffu, (most - top) * c > 8.f)) {   // -inf - -inf is NaN: no
+        const float now = fmaxf(top, most), f = now == -INFINITY ? 1.f : ex2((top - now) * c);
+        sum *= f;
+        top = now;
+#pragma unroll
+        for (int d = 0; d < DP; d += 32) {
+          u32 o[32];
+          tmem_ld32(o_at + d, o);
+          tmem_wait_ld();
+          tmem_hold(o);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+          tmem_st32(o_at + d, o);
+        }
+      }
+      const float low = top == -INFINITY ? 0.f : -top * c;
+      const F2 c2 = f2(c, c), low2 = f2(low, low);
+      F2 sum2 = f2(sum, 0.f);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        u32 p[16];
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+          float y0, y1;
+          split(fma2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), c2, low2), y0, y1);
+          y0 = ex2(y0);
+          y1 = ex2(y1);
+          sum2 = add2(sum2, f2(y0, y1));
+          p[k / 2] = pack2<BF16>(y0, y1);
+        }
+        tmem_st16(s_at + 16 * w, p);
+      }
+      float e0, e1;
+      split(sum2, e0, e1);
+      sum = e0 + e1;
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(p_full + 8 * x);
+    }
+    if (count[x] && ok && mbar_wait(o_full + 8 * x, 0, dead)) {
+      tc_fence_after();
+      const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
+      store_row<BF16, DP>(g.out, g.out_stride, t.row + i, head, a.head_dim, o_at, 1.f / sum, inside, !on);
+      if (inside && g.lse) g.lse[(long long)head * a.tokens + t.row + i] = on ? fmaf(top, a.scale, logf(sum)) : -INFINITY;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == MMA_WARP) tmem_free(tmem, 512);
+  if (*dead && threadIdx.x < 2 * TILE && t.first + (int)threadIdx.x < t.length)
+    poison_row(g.out, g.out_stride, t.row + t.first + threadIdx.x, head, a.head_dim);
+}
+
+// --------------------------------------------------------------------------
+// backward: dq
+// --------------------------------------------------------------------------
+// A CTA takes a tile of queries and walks over tiles of keys: S = Q K^T, dP = dO V^T, ds = p (dP - row_dot) in S's place, dQ += ds K.
+// S has two places, so that the next one is there while this one's exponentials run; dP is free again once ds has been made.
+// The eight warps share a tile by halves of its columns.
+template <int DP> struct DqLayout {
+  static constexpr int BYTES = DP * 256, KS = DP == 128 ? 3 : 4, VS = DP == 128 ? 2 : 4, RING = 2 * BYTES;
+  static constexpr int PART = RING + (KS + VS) * BYTES, BARS = PART + 1024, TOTAL = BARS + 256;
+};
+
+template <bool BF16, int DP>
+__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g) {
+  typedef DqLayout<DP> L;
+  extern __shared__ __align__(1024) unsigned char mma_smem[];
+  const adacgd_attention_inputs& a = g.in;
+  const int head = (int)(blockIdx.x % a.heads);
+  Tile t;
+  if (!tile_of(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, TILE, &t)) return;
+  const u32 base = smem_addr(mma_smem), bars = base + L::BARS;
+  const u32 q_full = bars, aside = bars + 8, s_full = bars + 16, dp_full = bars + 32, ds_full = bars + 40, dq_full = bars + 48, k_full = bars + 64,
+            k_empty = k_full + 8 * L::KS, v_full = k_empty + 8 * L::KS, v_empty = v_full + 8 * L::VS;
+  u32* const tmem_at = reinterpret_cast<u32*>(mma_smem + L::BARS + 64 + 16 * (L::KS + L::VS));
+  volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
+  float* const part = reinterpret_cast<float*>(mma_smem + L::PART);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    mbar_init(aside, 1);
+    mbar_init(s_full, 1);
+    mbar_init(s_full + 8, 1);
+    mbar_init(dp_full, 1);
+    mbar_init(ds_full, 256);
+    mbar_init(dq_full, 1);
+    for (int i = 0; i < L::KS; ++i) {
+      mbar_init(k_full + 8 * i, 1);
+      mbar_init(k_empty + 8 * i, 1);
+    }
+    for (int i = 0; i < L::VS; ++i) {
+      mbar_init(v_full + 8 * i, 1);
+      mbar_init(v_empty + 8 * i, 1);
+    }
+    *dead = 0;
+    mbar_init_fence();
+  }
+  if (warp == MMA_WARP) tmem_alloc(smem_addr(tmem_at), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const u32 tmem = *tmem_at, dp_at = tmem + 2 * TILE, dq_at = tmem + 3 * TILE;
+  const u32 q_tile = base, do_tile = base + L::BYTES, k_tiles = base + L::RING, v_tiles = k_tiles + L::KS * L::BYTES;
+  const int kh = head / (a.heads / a.key_heads), tiles = (t.length + TILE - 1) / TILE;
+  const int n = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
+  if (warp == COPY_WARP) {
+    if (lane == 0) {
+      mbar_expect(q_full, 2 * L::BYTES);
+      copy_tile<DP>(q_tile, &maps.q, head, t.row + t.first, q_full);
+      copy_tile<DP>(do_tile, &maps.dout, head, t.row + t.first, q_full);
+    }
+    u32 side = 0, words[4];
+    int nk = 0, nv = 0;
+    for (int j = 0; j < n; ++j) {
+      const int first = (n - 1 - j) * TILE, sk = j % L::KS, sv = j % L::VS;
+      counted(a, t, first, words);
+      if (j >= L::KS && !mbar_wait(k_empty + 8 * sk, (j / L::KS - 1) & 1, dead)) break;
+      ++nk;
+      if (!bring<DP>(k_tiles + sk * L::BYTES, &maps.k, kh, t.row + first, words, true, k_full + 8 * sk, aside, side, dead)) break;
+      if (j >= L::VS && !mbar_wait(v_empty + 8 * sv, (j / L::VS - 1) & 1, dead)) break;
+      ++nv;
+      bring<DP>(v_tiles + sv * L::BYTES, &maps.v, kh, t.row + first, words, false, v_full + 8 * sv, aside, side, dead);
+    }
+    if (*dead) {
+      settle(q_full, 0);
+      for (int b = max(0, nk - L::KS); b < nk; ++b) settle(k_full + 8 * (b % L::KS), (b / L::KS) & 1);
+      for (int b = max(0, nv - L::VS); b < nv; ++b) settle(v_full + 8 * (b % L::VS), (b / L::VS) & 1);
+    }
+  } else if (warp == MMA_WARP) {
+    if (lane == 0) {
+      auto scores = [&](int j) {                               // S of step j
+        const int st = j % L::KS;
+        if (!mbar_wait(k_full + 8 * st, (j / L::KS) & 1, dead)) return false;
+        tc_fence_after();
+        product_nt<BF16, DP>(tmem + (j & 1) * TILE, q_tile, k_tiles + st * L::BYTES);
+        mma_commit(s_full + 8 * (j & 1));
+        return true;
+      };
+      auto shares = [&](int j) {                               // dP of step j
+        const int st = j % L::VS;
+        if (!mbar_wait(v_full + 8 * st, (j / L::VS) & 1, dead)) return false;
+        tc_fence_after();
+        product_nt<BF16, DP>(dp_at, do_tile, v_tiles + st * L::BYTES);
+        mma_commit(dp_full);
+        mma_commit(v_empty + 8 * st);
+        return true;
+      };
+      bool ok = mbar_wait(q_full, 0, dead) && scores(0) && shares(0) && (n < 2 || scores(1));
+      for (int j = 0; ok && j < n; ++j) {
+        if (!mbar_wait(ds_full, j & 1, dead)) break;
+        tc_fence_after();
+        if (j + 1 < n && !shares(j + 1)) break;
+        product_pn<BF16, DP>(dq_at, tmem + (j & 1) * TILE, 64, k_tiles + (j % L::KS) * L::BYTES, j > 0);
+        mma_commit(k_empty + 8 * (j % L::KS));
+        if (j + 1 == n) mma_commit(dq_full);
+        if (j + 2 < n && !scores(j + 2)) break;
+      }
+      if (*dead) {
+        mma_commit(aside);
+        settle(aside, 0);
+      }
+    }
+  } else {
+    const int half = warp >> 2, r = (warp & 3) * 32 + lane, i = t.first + r;
+    const u32 lanes = (u32)(warp & 3) << 21;
+    const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
+    const long long at = (long long)head * a.tokens + t.row + i;
+    float dot = 0.f;
+    if (on) {                                                  // each half of the warps takes 64 of the head's elements
+      const char* const x = (const char*)g.dout + ((t.row + i) * g.dout_stride + (long long)head * a.head_dim) * 2;
+      const char* const y = (const char*)g.out + ((t.row + i) * g.out_stride + (long long)head * a.head_dim) * 2;
+      typedef typename std::conditional<BF16, __nv_bfloat16, __half>::type T;
+      for (int d = 64 * half; d < min(a.head_dim, 64 * half + 64); d += 8) {
+        float u[8], v[8];
+        unpack(load_run((const T*)x + d), u);
+        unpack(load_run((const T*)y + d), v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dot = fmaf(u[k], v[k], dot);
+      }
+    }
+    part[half * TILE + r] = dot;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    dot = part[r] + part[TILE + r];
+    if (half == 0 && inside) g.row_dot[at] = dot;
+    const float low = on ? -g.lse[at] * LOG2E : -INFINITY, c = a.scale * LOG2E;
+    const F2 c2 = f2(c, c), low2 = f2(low, low), dot2 = f2(-dot, -dot);
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      const int j0 = (n - 1 - j) * TILE;
+      const u32 s_at = tmem + (j & 1) * TILE + 64 * half + lanes;
+      u32 words[4];
+      const bool mask = a.mask || j0 + TILE > t.length || (a.causal && j0 + TILE > t.first);
+      if (mask) {
+        counted(a, t, j0, words);
+        if (a.causal)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) words[w] &= low_bits(i + 1 - j0 - 32 * w);
+      }
+      if (!(ok = mbar_wait(s_full + 8 * (j & 1), (j >> 1) & 1, dead))) break;
+      tc_fence_after();
+      u32 s[2][32];
+      tmem_ld32(s_at, s[0]);
+      tmem_ld32(s_at + 32, s[1]);
+      tmem_wait_ld();
+      tmem_hold(s[0]);
+      tmem_hold(s[1]);
+      F2 p[2][16];
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+          float y0, y1;
+          split(fma2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), c2, low2), y0, y1);
+          p[w][k / 2] = f2(ex2(y0), ex2(y1));
+        }
+      if (!(ok = mbar_wait(dp_full, j & 1, dead))) break;
+      tc_fence_after();
+      tmem_ld32(dp_at + 64 * half + lanes, s[0]);
+      tmem_ld32(dp_at + 64 * half + 32 + lanes, s[1]);
+      tmem_wait_ld();
+      tmem_hold(s[0]);
+      tmem_hold(s[1]);
+      u32 ds[32];
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+          float y0, y1;
+          split(mul2(p[w][k / 2], add2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), dot2)), y0, y1);
+          if (mask) {
+            const u32 bits = half ? words[2 + w] : words[w];
+            y0 = bits >> k & 1 ? y0 : 0.f;
+            y1 = bits >> (k + 1) & 1 ? y1 : 0.f;
+          }
+          ds[16 * w + k / 2] = pack2<BF16>(y0, y1);
+        }
+      tmem_st32(s_at, ds);
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(ds_full);
+    }
+    if (ok && mbar_wait(dq_full, 0, dead) && half == 0) {
+      tc_fence_after();
+      store_row<BF16, DP>(g.dq, g.dq_stride, t.row + i, head, a.head_dim, dq_at + lanes, a.scale, inside, !on);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == MMA_WARP) tmem_free(tmem, 512);
+  if (*dead && threadIdx.x < TILE && t.first + (int)threadIdx.x < t.length)
+    poison_row(g.dq, g.dq_stride, t.row + t.first + threadIdx.x, head, a.head_dim);
+}
+
+// --------------------------------------------------------------------------
+// backward: dk and dv
+// --------------------------------------------------------------------------
+// A CTA takes a tile of keys and walks over the tiles of queries, of all the heads that share it: S^T = K Q^T, p^T in its place, dV += p^T dO;
+// dP^T = V dO^T, ds^T in its place, dK += ds^T Q.  Transposed, both probabilities and ds are operands as they lie in tensor
+// memory, and Q and dO serve as they were brought, once by rows and once by columns.  The rows' log sums and products lie in shared memory, where all threads
+// read the same ones.  Products go in the order dV(i) S(i+1) dK(i) dP(i+1): while the first two run, ds(i) is made, during the others p(i+1).
+template <int DP> struct DkvLayout {
+  static constexpr int BYTES = DP * 256, STAGES = DP == 128 ? 5 : 8, RING = 2 * BYTES, STATS = RING + STAGES * BYTES;
+  static constexpr int BARS = STATS + 2 * 2 * TILE * 4, TOTAL = BARS + 256;
+};
+
+template <bool BF16, int DP>
+__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g) {
+  typedef DkvLayout<DP> L;
+  extern __shared__ __align__(1024) unsigned char mma_smem[];
+  const adacgd_attention_inputs& a = g.in;
+  const int kh = (int)(blockIdx.x % a.key_heads), group = a.heads / a.key_heads;
+  Tile t;
+  if (!tile_of(a, blockIdx.x / a.key_heads, TILE, &t)) return;
+  const u32 base = smem_addr(mma_smem), bars = base + L::BARS;
+  const u32 kv_full = bars, aside = bars + 8, s_full = bars + 16, dp_full = bars + 24, p_full = bars + 32, ds_full = bars + 40, end_full = bars + 48,
+            full = bars + 56, empty = full + 8 * L::STAGES;
+  u32* const tmem_at = reinterpret_cast<u32*>(mma_smem + L::BARS + 56 + 16 * L::STAGES);
+  volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
+  float* const stats = reinterpret_cast<float*>(mma_smem + L::STATS);   // [2 steps][-lse log2 e, -row_dot][128]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(kv_full, 1);
+    mbar_init(aside, 1);
+    mbar_init(s_full, 1);
+    mbar_init(dp_full, 1);
+    mbar_init(p_full, 256);
+    mbar_init(ds_full, 256);
+    mbar_init(end_full, 1);
+    for (int i = 0; i < L::STAGES; ++i) {
+      mbar_init(full + 8 * i, 1);
+      mbar_init(empty + 8 * i, 1);
+    }
+    *dead = 0;
+    mbar_init_fence();
+  }
+  if (warp == MMA_WARP) tmem_alloc(smem_addr(tmem_at), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const u32 tmem = *tmem_at, dp_at = tmem + TILE, dv_at = tmem + 2 * TILE, dk_at = dv_at + DP;
+  const u32 k_tile = base, v_tile = base + L::BYTES, ring = base + L::RING;
+  const int begin = a.causal ? t.first / TILE : 0, each = (t.length + TILE - 1) / TILE - begin, n = each * group;
+  if (warp == COPY_WARP) {
+    if (lane == 0) {
+      mbar_expect(kv_full, 2 * L::BYTES);
+      copy_tile<DP>(k_tile, &maps.k, kh, t.row + t.first, kv_full);
+      copy_tile<DP>(v_tile, &maps.v, kh, t.row + t.first, kv_full);
+    }
+    u32 side = 0, words[4];
+    int i = 0;
+    bool ok = true;
+    for (; ok && i < 2 * n; ++i) {                             // tiles of queries and of dout in turn
+      const int st = i % L::STAGES, j = i / 2, head = kh * group + j / each, first = (begin + j % each) * TILE;
+      if (i >= L::STAGES && !mbar_wait(empty + 8 * st, (i / L::STAGES - 1) & 1, dead)) break;
+      if (!(i & 1)) {
+        counted(a, t, first, words);
+      } else {
+        // With dout, whose slot was the queries' of two steps ago or later ones': the step that used these numbers before has ended.
+        if (i >= 4 && L::STAGES > 5 && !mbar_wait(empty + 8 * ((i - 5) % L::STAGES), ((i - 5) / L::STAGES) & 1, dead)) break;
+        float* const to = stats + (j & 1) * 2 * TILE;
+        const long long at = (long long)head * a.tokens + t.row + first;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const bool on = words[w] >> lane & 1;
+          to[32 * w + lane] = on ? -g.lse[at + 32 * w + lane] * LOG2E : -INFINITY;
+          to[TILE + 32 * w + lane] = on ? -g.row_dot[at + 32 * w + lane] : 0.f;
+        }
+        __syncwarp();
+      }
+      ok = bring<DP>(ring + st * L::BYTES, i & 1 ? &maps.dout : &maps.q, head, t.row + first, words, true, full + 8 * st, aside, side, dead);
+    }
+    if (*dead) {
+      settle(kv_full, 0);
+      for (int b = max(0, i - L::STAGES); b < i; ++b) settle(full + 8 * (b % L::STAGES), (b / L::STAGES) & 1);
+    }
+  } else if (warp == MMA_WARP) {
+    if (lane == 0) {
+      auto tile = [&](int i) { return ring + (i % L::STAGES) * L::BYTES; };
+      auto scores = [&](int j) {
+        if (!mbar_wait(full + 8 * (2 * j % L::STAGES), (2 * j / L::STAGES) & 1, dead)) return false;
+        tc_fence_after();
+        product_nt<BF16, DP>(tmem, k_tile, tile(2 * j));
+        mma_commit(s_full);
+        return true;
+      };
+      auto shares = [&](int j) {
+        if (!mbar_wait(full + 8 * ((2 * j + 1) % L::STAGES), ((2 * j + 1) / L::STAGES) & 1, dead)) return false;
+        tc_fence_after();
+        product_nt<BF16, DP>(dp_at, v_tile, tile(2 * j + 1));
+        mma_commit(dp_full);
+        return true;
+      };
+      bool ok = mbar_wait(kv_full, 0, dead) && scores(0) && shares(0);
+      for (int j = 0; ok && j < n; ++j) {
+        if (!mbar_wait(p_full, j & 1, dead)) break;
+        tc_fence_after();
+        product_pn<BF16, DP>(dv_at, tmem, 64, tile(2 * j + 1), j > 0);
+        mma_commit(empty + 8 * ((2 * j + 1) % L::STAGES));
+        if (j + 1 < n && !scores(j + 1)) break;
+        if (!mbar_wait(ds_full, j & 1, dead)) break;
+        tc_fence_after();
+        product_pn<BF16, DP>(dk_at, dp_at, 64, tile(2 * j), j > 0);
+        mma_commit(empty + 8 * (2 * j % L::STAGES));
+        if (j + 1 < n && !shares(j + 1)) break;
+      }
+      if (!*dead) mma_commit(end_full);
+      else {
+        mma_commit(aside);
+        settle(aside, 0);
+      }
+    }
+  } else {
+    const int half = warp >> 2, i = t.first + (warp & 3) * 32 + lane;   // the thread's key
+    const u32 lanes = (u32)(warp & 3) << 21, s_at = tmem + 64 * half + lanes, d_at = dp_at + 64 * half + lanes;
+    const float c = a.scale * LOG2E;
+    const F2 c2 = f2(c, c);
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      const int first = (begin + j % each) * TILE + 64 * half;
+      const float* const low = stats + (j & 1) * 2 * TILE + 64 * half;
+      const bool mask = a.causal && first < t.first + TILE;              // queries before the key
+      // the log sums come with dout's tile
+      if (!(ok = mbar_wait(full + 8 * ((2 * j + 1) % L::STAGES), ((2 * j + 1) / L::STAGES) & 1, dead))) break;
+      if (!(ok = mbar_wait(s_full, j & 1, dead))) break;
+      tc_fence_after();
+      u32 s[2][32];
+      tmem_ld32(s_at, s[0]);
+      tmem_ld32(s_at + 32, s[1]);
+      tmem_wait_ld();
+      tmem_hold(s[0]);
+      tmem_hold(s[1]);
+      F2 p[2][16];
+      u32 w16[32];
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) {
+          const float4 l = *reinterpret_cast<const float4*>(low + 32 * w + k);
+          float y0, y1, y2, y3;
+          split(fma2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), c2, f2(l.x, l.y)), y0, y1);
+          split(fma2(f2(__uint_as_float(s[w][k + 2]), __uint_as_float(s[w][k + 3])), c2, f2(l.z, l.w)), y2, y3);
+          y0 = ex2(y0);
+          y1 = ex2(y1);
+          y2 = ex2(y2);
+          y3 = ex2(y3);
+          if (mask) {
+            const int q = first + 32 * w + k;
+            y0 = q >= i ? y0 : 0.f;
+            y1 = q + 1 >= i ? y1 : 0.f;
+            y2 = q + 2 >= i ? y2 : 0.f;
+            y3 = q + 3 >= i ? y3 : 0.f;
+          }
+          p[w][k / 2] = f2(y0, y1);
+          p[w][k / 2 + 1] = f2(y2, y3);
+          w16[16 * w + k / 2] = pack2<BF16>(y0, y1);
+          w16[16 * w + k / 2 + 1] = pack2<BF16>(y2, y3);
+        }
+      tmem_st32(s_at, w16);
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(p_full);
+      if (!(ok = mbar_wait(dp_full, j & 1, dead))) break;
+      tc_fence_after();
+      tmem_ld32(d_at, s[0]);
+      tmem_ld32(d_at + 32, s[1]);
+      tmem_wait_ld();
+      tmem_hold(s[0]);
+      tmem_hold(s[1]);
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) {
+          const float4 l = *reinterpret_cast<const float4*>(low + TILE + 32 * w + k);
+          float y0, y1, y2, y3;
+          split(mul2(p[w][k / 2], add2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), f2(l.x, l.y))), y0, y1);
+          split(mul2(p[w][k / 2 + 1], add2(f2(__uint_as_float(s[w][k + 2]), __uint_as_float(s[w][k + 3])), f2(l.z, l.w))), y2, y3);
+          w16[16 * w + k / 2] = pack2<BF16>(y0, y1);
+          w16[16 * w + k / 2 + 1] = pack2<BF16>(y2, y3);
+        }
+      tmem_st32(d_at, w16);
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(ds_full);
+    }
+    if (ok && mbar_wait(end_full, 0, dead)) {
+      tc_fence_after();
+      const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
+      if (half == 0) store_row<BF16, DP>(g.dk, g.dk_stride, t.row + i, kh, a.head_dim, dk_at + lanes, a.scale, inside, !on);
+      else store_row<BF16, DP>(g.dv, g.dv_stride, t.row + i, kh, a.head_dim, dv_at + lanes, 1.f, inside, !on);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == MMA_WARP) tmem_free(tmem, 512);
+  if (*dead && threadIdx.x < TILE && t.first + (int)threadIdx.x < t.length) {
+    poison_row(g.dk, g.dk_stride, t.row + t.first + threadIdx.x, kh, a.head_dim);
+    poison_row(g.dv, g.dv_stride, t.row + t.first + threadIdx.x, kh, a.head_dim);
+  }
+}
+
+// --------------------------------------------------------------------------
+// launches
+// --------------------------------------------------------------------------
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encoder() {
+  static const EncodeTiled fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) return (EncodeTiled) nullptr;
+    return (EncodeTiled)p;
+  }();
+  return fn;
+}
+
+bool rows_on_16(const void* p, long long stride, long long rows) { return ((uintptr_t)p & 15) == 0 && (rows <= 1 || stride % 8 == 0); }
+
+// Tokens x heads x elements; a box is 128 tokens of one head's 64 elements.
+bool map_of(CUtensorMap* m, const void* p, long long stride, const adacgd_attention_inputs& a, int heads) {
+  const long long row = (long long)heads * a.head_dim;
+  if (a.tokens == 1 || stride < row) stride = row;             // of a single row it may be anything
+  const cuuint64_t dims[3] = {(cuuint64_t)a.head_dim, (cuuint64_t)heads, (cuuint64_t)a.tokens};
+  const cuuint64_t strides[2] = {(cuuint64_t)a.head_dim * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {64, 1, TILE}, steps[3] = {1, 1, 1};
+  return encoder()(m, a.dtype == ADACGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims,
+                   strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool takes(const adacgd_attention_inputs& a) {
+  return a.dtype != ADACGD_F32 && a.head_dim % 8 == 0 && a.head_dim <= 128 && rows_on_16(a.q, a.q_stride, a.tokens) &&
+         rows_on_16(a.k, a.k_stride, a.tokens) && rows_on_16(a.v, a.v_stride, a.tokens) && tile_slots(a, TILE) * a.heads < (1ll << 31) && encoder();
+}
+
+template <typename K, typename A>
+bool launch_mma(K kern, std::atomic<int> (&table)[TRAIN_DEVICES], int smem, long long ctas, const Maps& m, const A& g, const Where& at) {
+  if (resident_ctas(kern, table, at.device, MMA_CTA, smem) < 1) return false;
+  kern<<<(unsigned)ctas, MMA_CTA, smem, at.stream>>>(m, g);
+  return cudaGetLastError() == cudaSuccess;
+}
+
+template <bool BF16, int DP> int fwd_mma(const Maps& m, const adacgd_attention_args& g, const Where& at) {
+  static std::atomic<int> table[TRAIN_DEVICES];
+  return launch_mma(k_attention_mma<BF16, DP>, table, FwdLayout<DP>::TOTAL, tile_slots(g.in, 2 * TILE) * g.in.heads, m, g, at) ? 1 : -1;
+}
+template <bool BF16, int DP> int bwd_mma(const Maps& m, const adacgd_attention_backward_args& g, const Where& at) {
+  static std::atomic<int> table[2][TRAIN_DEVICES];
+  const long long slots = tile_slots(g.in, TILE);
+  if (!launch_mma(k_attention_dq_mma<BF16, DP>, table[0], DqLayout<DP>::TOTAL, slots * g.in.heads, m, g, at)) return -1;
+  return launch_mma(k_attention_dkv_mma<BF16, DP>, table[1], DkvLayout<DP>::TOTAL, slots * g.in.key_heads, m, g, at) ? 2 : -1;
+}
+
+}  // namespace
+
+#define BY_KIND(call)                                                                                                    \
+  if (a.dtype == ADACGD_BF16) { constexpr bool BF16 = true; BY_WIDTH(call) }                                             \
+  { constexpr bool BF16 = false; BY_WIDTH(call) }
+#define BY_WIDTH(call)                                                                                                   \
+  if (a.head_dim <= 64) { constexpr int DP = 64; return call; }                                                          \
+  { constexpr int DP = 128; return call; }
+
+int launch_attention_mma(const adacgd_attention_args& g, const Where& at) {
+  const adacgd_attention_inputs& a = g.in;
+  if (!takes(a) || !rows_on_16(g.out, g.out_stride, a.tokens)) return 0;
+  Maps m = {};
+  if (!map_of(&m.q, a.q, a.q_stride, a, a.heads) || !map_of(&m.k, a.k, a.k_stride, a, a.key_heads) || !map_of(&m.v, a.v, a.v_stride, a, a.key_heads)) return 0;
+  BY_KIND((fwd_mma<BF16, DP>(m, g, at)))
+}
+
+int launch_attention_backward_mma(const adacgd_attention_backward_args& g, const Where& at) {
+  const adacgd_attention_inputs& a = g.in;
+  if (!takes(a) || !rows_on_16(g.out, g.out_stride, a.tokens) || !rows_on_16(g.dout, g.dout_stride, a.tokens) ||
+      !rows_on_16(g.dq, g.dq_stride, a.tokens) || !rows_on_16(g.dk, g.dk_stride, a.tokens) || !rows_on_16(g.dv, g.dv_stride, a.tokens))
+    return 0;
+  Maps m = {};
+  if (!map_of(&m.q, a.q, a.q_stride, a, a.heads) || !map_of(&m.k, a.k, a.k_stride, a, a.key_heads) || !map_of(&m.v, a.v, a.v_stride, a, a.key_heads) ||
+      !map_of(&m.dout, g.dout, g.dout_stride, a, a.heads))
+    return 0;
+  BY_KIND((bwd_mma<BF16, DP>(m, g, at)))
+}
+
+}  // namespace adacgd
