@@ -11,8 +11,6 @@
 //
 // The backward pass is two kernels that each compute the scores again, seven products for the five that are needed: every sum stays in one
 // CTA's tensor memory, without atomics, and dq needs no binary32 array.
-#include <type_traits>
-
 #include "adacgd_tcgen05.cuh"
 #include "adacgd_train_attention.cuh"
 
@@ -125,7 +123,7 @@ __device__ __forceinline__ u32 low_bits(int n) { return n <= 0 ? 0u : (n >= 32 ?
 // A CTA takes two tiles of queries of a head, A and B.  While the products of one run, four warps turn the scores of the other into
 // probabilities: S = Q K^T, the row's maximum, p = 2^(c s - c max) in S's place, O += p V.  The maximum that p is taken against is
 // moved only when it has grown by more than 2^8, so O, which stays in tensor memory, is hardly ever rescaled; p is at most 256 then, and the
-// division by the sum at the end takes it out.
+// division by the sum at the end takes it out.  binary16 has few numbers below 1: there p is taken 2^7 times larger, at most 2^15.
 template <int DP> struct FwdLayout {
   static constexpr int BYTES = DP * 256, STAGES = DP == 128 ? 5 : 8, RING = 2 * BYTES, BARS = RING + STAGES * BYTES;
   static constexpr int TOTAL = BARS + 256;
@@ -276,7 +274,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_mma(const __grid_const
           tmem_st32(o_at + d, o);
         }
       }
-      const float low = top == -INFINITY ? 0.f : -top * c;
+      const float low = (top == -INFINITY ? 0.f : -top * c) + (BF16 ? 0.f : 7.f);
       const F2 c2 = f2(c, c), low2 = f2(low, low);
       F2 sum2 = f2(sum, 0.f);
 #pragma unroll
@@ -304,7 +302,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_mma(const __grid_const
       tc_fence_after();
       const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
       store_row<BF16, DP>(g.out, g.out_stride, t.row + i, head, a.head_dim, o_at, 1.f / sum, inside, !on);
-      if (inside && g.lse) g.lse[(long long)head * a.tokens + t.row + i] = on ? fmaf(top, a.scale, logf(sum)) : -INFINITY;
+      if (inside && g.lse) g.lse[(long long)head * a.tokens + t.row + i] = on ? fmaf(top, a.scale, logf(BF16 ? sum : sum * 0.0078125f)) : -INFINITY;
     }
   }
   tc_fence_before();
@@ -313,6 +311,89 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_mma(const __grid_const
   if (warp == MMA_WARP) tmem_free(tmem, 512);
   if (*dead && threadIdx.x < 2 * TILE && t.first + (int)threadIdx.x < t.length)
     poison_row(g.out, g.out_stride, t.row + t.first + threadIdx.x, head, a.head_dim);
+}
+
+// --------------------------------------------------------------------------
+// backward: the range of ds
+// --------------------------------------------------------------------------
+// bfloat16 holds ds as it is.  binary16 would lose what is below 2^-14, and gradients are often that small, so there ds is multiplied by a power
+// of two that brings the largest one possible, |dout_i| (|v_j| + |out_i|) <= 2 max|dout_i| max|v_j|, below 2^14.  This kernel takes those two
+// maxima, a pair a CTA, and the rows' products dout.out; half a warp takes a head's row.
+constexpr int DOT_CTA = 256, DOT_CTAS = 296;
+
+__global__ void __launch_bounds__(DOT_CTA) k_attention_dot(adacgd_attention_backward_args g, float* most) {
+  const adacgd_attention_inputs& a = g.in;
+  const int lane = threadIdx.x & 15, d = lane * 8;
+  const bool in = d < a.head_dim;
+  const long long slots = (long long)gridDim.x * (DOT_CTA / 16), slot = (long long)blockIdx.x * (DOT_CTA / 16) + threadIdx.x / 16;
+  long long lo = 0, hi = a.tokens, unused;
+  if (a.seq_start) {                                  // rows of no sequence keep their row_dot and do not count
+    seq_bounds(a.seq_start, 0, a.tokens, 0, &lo, &unused);
+    seq_bounds(a.seq_start, a.sequences - 1, a.tokens, 0, &unused, &hi);
+  }
+  auto sum = [](float v) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  };
+  float mo = 0.f, mv = 0.f;
+  const long long queries = (hi - lo) * a.heads, keys = (hi - lo) * a.key_heads;
+  for (long long i0 = slot - (threadIdx.x / 16 & 1); i0 < queries; i0 += slots) {   // both halves of a warp alike
+    const long long i = i0 + (threadIdx.x / 16 & 1), t = lo + i / a.heads;
+    const int h = (int)(i % a.heads);
+    const bool row = i < queries, on = row && (!a.mask || a.mask[t]);
+    float x[8], y[8], dot = 0.f, sq = 0.f;
+    if (on && in) {
+      unpack(load_run((const __half*)g.dout + t * g.dout_stride + h * a.head_dim + d), x);
+      unpack(load_run((const __half*)g.out + t * g.out_stride + h * a.head_dim + d), y);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        dot = fmaf(x[k], y[k], dot);
+        sq = fmaf(x[k], x[k], sq);
+      }
+    }
+    dot = sum(dot);
+    mo = fmaxf(mo, sum(sq));
+    if (row && lane == 0) g.row_dot[(long long)h * a.tokens + t] = dot;
+  }
+  for (long long i0 = slot - (threadIdx.x / 16 & 1); i0 < keys; i0 += slots) {
+    const long long i = i0 + (threadIdx.x / 16 & 1), t = lo + i / a.key_heads;
+    float x[8], sq = 0.f;
+    if (i < keys && in && (!a.mask || a.mask[t])) {
+      unpack(load_run((const __half*)a.v + t * a.v_stride + (i % a.key_heads) * a.head_dim + d), x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sq = fmaf(x[k], x[k], sq);
+    }
+    mv = fmaxf(mv, sum(sq));
+  }
+  __shared__ float part[2][DOT_CTA / 16];
+  if (lane == 0) {
+    part[0][threadIdx.x / 16] = mo;
+    part[1][threadIdx.x / 16] = mv;
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    float m = 0.f;
+    for (int i = 0; i < DOT_CTA / 16; ++i) m = fmaxf(m, part[threadIdx.x][i]);
+    most[2 * blockIdx.x + threadIdx.x] = m;
+  }
+}
+
+// The power of two: called by whole warps.
+__device__ __forceinline__ float range_of(const float* most, int parts) {
+  float mo = 0.f, mv = 0.f;
+  for (int i = threadIdx.x & 31; i < parts; i += 32) {
+    mo = fmaxf(mo, __ldcg(most + 2 * i));
+    mv = fmaxf(mv, __ldcg(most + 2 * i + 1));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, o));
+    mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, o));
+  }
+  const float bound = 2.002f * sqrtf(mo) * sqrtf(mv);
+  if (!(bound > 0.f) || isinf(bound)) return 1.f;
+  return __int_as_float(((int)fminf(fmaxf(13.f - floorf(log2f(bound)), -60.f), 60.f) + 127) << 23);
 }
 
 // --------------------------------------------------------------------------
@@ -327,7 +408,7 @@ template <int DP> struct DqLayout {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g) {
+__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most, int parts) {
   typedef DqLayout<DP> L;
   extern __shared__ __align__(1024) unsigned char mma_smem[];
   const adacgd_attention_inputs& a = g.in;
@@ -430,25 +511,29 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
     const u32 lanes = (u32)(warp & 3) << 21;
     const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
     const long long at = (long long)head * a.tokens + t.row + i;
-    float dot = 0.f;
-    if (on) {                                                  // each half of the warps takes 64 of the head's elements
-      const char* const x = (const char*)g.dout + ((t.row + i) * g.dout_stride + (long long)head * a.head_dim) * 2;
-      const char* const y = (const char*)g.out + ((t.row + i) * g.out_stride + (long long)head * a.head_dim) * 2;
-      typedef typename std::conditional<BF16, __nv_bfloat16, __half>::type T;
-      for (int d = 64 * half; d < min(a.head_dim, 64 * half + 64); d += 8) {
-        float u[8], v[8];
-        unpack(load_run((const T*)x + d), u);
-        unpack(load_run((const T*)y + d), v);
+    float dot = 0.f, range = 1.f;
+    if (BF16) {
+      if (on) {                                                // each half of the warps takes 64 of the head's elements
+        const __nv_bfloat16* const x = (const __nv_bfloat16*)g.dout + (t.row + i) * g.dout_stride + (long long)head * a.head_dim;
+        const __nv_bfloat16* const y = (const __nv_bfloat16*)g.out + (t.row + i) * g.out_stride + (long long)head * a.head_dim;
+        for (int d = 64 * half; d < min(a.head_dim, 64 * half + 64); d += 8) {
+          float u[8], v[8];
+          unpack(load_run(x + d), u);
+          unpack(load_run(y + d), v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dot = fmaf(u[k], v[k], dot);
+          for (int k = 0; k < 8; ++k) dot = fmaf(u[k], v[k], dot);
+        }
       }
+      part[half * TILE + r] = dot;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      dot = part[r] + part[TILE + r];
+      if (half == 0 && inside) g.row_dot[at] = dot;
+    } else {
+      range = range_of(most, parts);
+      if (on) dot = __ldcg(g.row_dot + at) * range;
     }
-    part[half * TILE + r] = dot;
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    dot = part[r] + part[TILE + r];
-    if (half == 0 && inside) g.row_dot[at] = dot;
     const float low = on ? -g.lse[at] * LOG2E : -INFINITY, c = a.scale * LOG2E;
-    const F2 c2 = f2(c, c), low2 = f2(low, low), dot2 = f2(-dot, -dot);
+    const F2 c2 = f2(c, c), low2 = f2(low, low), dot2 = f2(-dot, -dot), range2 = f2(range, range);
     bool ok = true;
     for (int j = 0; j < n; ++j) {
       const int j0 = (n - 1 - j) * TILE;
@@ -491,7 +576,8 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
 #pragma unroll
         for (int k = 0; k < 32; k += 2) {
           float y0, y1;
-          split(mul2(p[w][k / 2], add2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), dot2)), y0, y1);
+          const F2 dp = f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1]));
+          split(mul2(p[w][k / 2], BF16 ? add2(dp, dot2) : fma2(dp, range2, dot2)), y0, y1);
           if (mask) {
             const u32 bits = half ? words[2 + w] : words[w];
             y0 = bits >> k & 1 ? y0 : 0.f;
@@ -506,7 +592,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
     }
     if (ok && mbar_wait(dq_full, 0, dead) && half == 0) {
       tc_fence_after();
-      store_row<BF16, DP>(g.dq, g.dq_stride, t.row + i, head, a.head_dim, dq_at + lanes, a.scale, inside, !on);
+      store_row<BF16, DP>(g.dq, g.dq_stride, t.row + i, head, a.head_dim, dq_at + lanes, a.scale / range, inside, !on);
     }
   }
   tc_fence_before();
@@ -530,7 +616,7 @@ template <int DP> struct DkvLayout {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g) {
+__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most, int parts) {
   typedef DkvLayout<DP> L;
   extern __shared__ __align__(1024) unsigned char mma_smem[];
   const adacgd_attention_inputs& a = g.in;
@@ -542,7 +628,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
             full = bars + 56, empty = full + 8 * L::STAGES;
   u32* const tmem_at = reinterpret_cast<u32*>(mma_smem + L::BARS + 56 + 16 * L::STAGES);
   volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
-  float* const stats = reinterpret_cast<float*>(mma_smem + L::STATS);   // [2 steps][-lse log2 e, -row_dot][128]
+  float* const stats = reinterpret_cast<float*>(mma_smem + L::STATS);   // [2 steps][-lse log2 e, -row_dot][128], scaled as p and ds are
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     mbar_init(kv_full, 1);
@@ -565,6 +651,8 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
   tc_fence_after();
   const u32 tmem = *tmem_at, dp_at = tmem + TILE, dv_at = tmem + 2 * TILE, dk_at = dv_at + DP;
   const u32 k_tile = base, v_tile = base + L::BYTES, ring = base + L::RING;
+  // binary16: p is taken 2^14 times larger, ds by its range (see above)
+  const float range = BF16 ? 1.f : range_of(most, parts), shift = BF16 ? 0.f : 14.f, back = BF16 ? 1.f : 6.103515625e-05f;
   const int begin = a.causal ? t.first / TILE : 0, each = (t.length + TILE - 1) / TILE - begin, n = each * group;
   if (warp == COPY_WARP) {
     if (lane == 0) {
@@ -588,8 +676,8 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const bool on = words[w] >> lane & 1;
-          to[32 * w + lane] = on ? -g.lse[at + 32 * w + lane] * LOG2E : -INFINITY;
-          to[TILE + 32 * w + lane] = on ? -g.row_dot[at + 32 * w + lane] : 0.f;
+          to[32 * w + lane] = on ? fmaf(g.lse[at + 32 * w + lane], -LOG2E, shift) : -INFINITY;
+          to[TILE + 32 * w + lane] = on ? -g.row_dot[at + 32 * w + lane] * (range * back) : 0.f;
         }
         __syncwarp();
       }
@@ -639,7 +727,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
     const int half = warp >> 2, i = t.first + (warp & 3) * 32 + lane;   // the thread's key
     const u32 lanes = (u32)(warp & 3) << 21, s_at = tmem + 64 * half + lanes, d_at = dp_at + 64 * half + lanes;
     const float c = a.scale * LOG2E;
-    const F2 c2 = f2(c, c);
+    const F2 c2 = f2(c, c), range2 = f2(range * back, range * back);
     bool ok = true;
     for (int j = 0; j < n; ++j) {
       const int first = (begin + j % each) * TILE + 64 * half;
@@ -698,8 +786,9 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
         for (int k = 0; k < 32; k += 4) {
           const float4 l = *reinterpret_cast<const float4*>(low + TILE + 32 * w + k);
           float y0, y1, y2, y3;
-          split(mul2(p[w][k / 2], add2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), f2(l.x, l.y))), y0, y1);
-          split(mul2(p[w][k / 2 + 1], add2(f2(__uint_as_float(s[w][k + 2]), __uint_as_float(s[w][k + 3])), f2(l.z, l.w))), y2, y3);
+          const F2 u = f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), v = f2(__uint_as_float(s[w][k + 2]), __uint_as_float(s[w][k + 3]));
+          split(mul2(p[w][k / 2], BF16 ? add2(u, f2(l.x, l.y)) : fma2(u, range2, f2(l.x, l.y))), y0, y1);
+          split(mul2(p[w][k / 2 + 1], BF16 ? add2(v, f2(l.z, l.w)) : fma2(v, range2, f2(l.z, l.w))), y2, y3);
           w16[16 * w + k / 2] = pack2<BF16>(y0, y1);
           w16[16 * w + k / 2 + 1] = pack2<BF16>(y2, y3);
         }
@@ -711,8 +800,8 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
     if (ok && mbar_wait(end_full, 0, dead)) {
       tc_fence_after();
       const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
-      if (half == 0) store_row<BF16, DP>(g.dk, g.dk_stride, t.row + i, kh, a.head_dim, dk_at + lanes, a.scale, inside, !on);
-      else store_row<BF16, DP>(g.dv, g.dv_stride, t.row + i, kh, a.head_dim, dv_at + lanes, 1.f, inside, !on);
+      if (half == 0) store_row<BF16, DP>(g.dk, g.dk_stride, t.row + i, kh, a.head_dim, dk_at + lanes, a.scale / range, inside, !on);
+      else store_row<BF16, DP>(g.dv, g.dv_stride, t.row + i, kh, a.head_dim, dv_at + lanes, back, inside, !on);
     }
   }
   tc_fence_before();
@@ -759,22 +848,31 @@ bool takes(const adacgd_attention_inputs& a) {
          rows_on_16(a.k, a.k_stride, a.tokens) && rows_on_16(a.v, a.v_stride, a.tokens) && tile_slots(a, TILE) * a.heads < (1ll << 31) && encoder();
 }
 
-template <typename K, typename A>
-bool launch_mma(K kern, std::atomic<int> (&table)[TRAIN_DEVICES], int smem, long long ctas, const Maps& m, const A& g, const Where& at) {
+template <typename K, typename... A>
+bool launch_mma(K kern, std::atomic<int> (&table)[TRAIN_DEVICES], int smem, long long ctas, const Where& at, const A&... args) {
   if (resident_ctas(kern, table, at.device, MMA_CTA, smem) < 1) return false;
-  kern<<<(unsigned)ctas, MMA_CTA, smem, at.stream>>>(m, g);
+  kern<<<(unsigned)ctas, MMA_CTA, smem, at.stream>>>(args...);
   return cudaGetLastError() == cudaSuccess;
 }
 
 template <bool BF16, int DP> int fwd_mma(const Maps& m, const adacgd_attention_args& g, const Where& at) {
   static std::atomic<int> table[TRAIN_DEVICES];
-  return launch_mma(k_attention_mma<BF16, DP>, table, FwdLayout<DP>::TOTAL, tile_slots(g.in, 2 * TILE) * g.in.heads, m, g, at) ? 1 : -1;
+  return launch_mma(k_attention_mma<BF16, DP>, table, FwdLayout<DP>::TOTAL, tile_slots(g.in, 2 * TILE) * g.in.heads, at, m, g) ? 1 : -1;
 }
-template <bool BF16, int DP> int bwd_mma(const Maps& m, const adacgd_attention_backward_args& g, const Where& at) {
+template <bool BF16, int DP> int bwd_mma(const TrainScratch& ws, const Maps& m, const adacgd_attention_backward_args& g, const Where& at) {
   static std::atomic<int> table[2][TRAIN_DEVICES];
   const long long slots = tile_slots(g.in, TILE);
-  if (!launch_mma(k_attention_dq_mma<BF16, DP>, table[0], DqLayout<DP>::TOTAL, slots * g.in.heads, m, g, at)) return -1;
-  return launch_mma(k_attention_dkv_mma<BF16, DP>, table[1], DkvLayout<DP>::TOTAL, slots * g.in.key_heads, m, g, at) ? 2 : -1;
+  float* const most = ws.norm_part;                            // of at least 2 * NORM_PARTS numbers
+  int parts = 0;
+  if (!BF16) {
+    const long long want = (g.in.tokens * g.in.heads + DOT_CTA / 16 - 1) / (DOT_CTA / 16);
+    parts = (int)(want < DOT_CTAS ? want : DOT_CTAS);
+    k_attention_dot<<<parts, DOT_CTA, 0, at.stream>>>(g, most);
+    if (cudaGetLastError() != cudaSuccess) return -1;
+  }
+  if (!launch_mma(k_attention_dq_mma<BF16, DP>, table[0], DqLayout<DP>::TOTAL, slots * g.in.heads, at, m, g, (const float*)most, parts)) return -1;
+  if (!launch_mma(k_attention_dkv_mma<BF16, DP>, table[1], DkvLayout<DP>::TOTAL, slots * g.in.key_heads, at, m, g, (const float*)most, parts)) return -1;
+  return BF16 ? 2 : 3;
 }
 
 }  // namespace
@@ -794,7 +892,7 @@ int launch_attention_mma(const adacgd_attention_args& g, const Where& at) {
   BY_KIND((fwd_mma<BF16, DP>(m, g, at)))
 }
 
-int launch_attention_backward_mma(const adacgd_attention_backward_args& g, const Where& at) {
+int launch_attention_backward_mma(const TrainScratch& ws, const adacgd_attention_backward_args& g, const Where& at) {
   const adacgd_attention_inputs& a = g.in;
   if (!takes(a) || !rows_on_16(g.out, g.out_stride, a.tokens) || !rows_on_16(g.dout, g.dout_stride, a.tokens) ||
       !rows_on_16(g.dq, g.dq_stride, a.tokens) || !rows_on_16(g.dk, g.dk_stride, a.tokens) || !rows_on_16(g.dv, g.dv_stride, a.tokens))
@@ -803,7 +901,7 @@ int launch_attention_backward_mma(const adacgd_attention_backward_args& g, const
   if (!map_of(&m.q, a.q, a.q_stride, a, a.heads) || !map_of(&m.k, a.k, a.k_stride, a, a.key_heads) || !map_of(&m.v, a.v, a.v_stride, a, a.key_heads) ||
       !map_of(&m.dout, g.dout, g.dout_stride, a, a.heads))
     return 0;
-  BY_KIND((bwd_mma<BF16, DP>(m, g, at)))
+  BY_KIND((bwd_mma<BF16, DP>(ws, m, g, at)))
 }
 
 }  // namespace adacgd

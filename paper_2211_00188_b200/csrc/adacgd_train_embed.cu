@@ -222,7 +222,7 @@ __device__ __forceinline__ int lower_bound_lane(const u32* keys, int lo, int hi,
   return lo;
 }
 
-constexpr int SUM_CTA = 256, SUM_ROWS = 32, SUM_MIN = 64;
+constexpr int SUM_CTA = 256, SUM_ROWS = 32, SUM_MIN = 64, SUM_STAGE = 512;   // most rows of the table a CTA takes; tokens staged
 constexpr int MAX_WINDOWS = NORM_PARTS;   // two partial sums a window
 
 struct SumArgs {
@@ -236,20 +236,21 @@ struct SumArgs {
   long long vocab, cols;
   int n, most;      // tokens; rows of one id that one thread sums: longer runs go by windows of that length
   int windows, slices;   // CTAs of the long runs: windows * slices, a slice being SUM_CTA vectors of each row at a time
+  int rows;         // of the table, that a CTA takes
   float scale;
   bool leave;       // rows without tokens stay as they are
 };
 
-// Sum of the rows places[lo .. hi) in columns [N c, N c + N), four loads in flight.
+// Sum of the rows places[lo .. hi) (a global or a shared array) in columns [N c, N c + N), four loads in flight.
 template <typename T, int N>
-__device__ __forceinline__ void sum_rows(const SumArgs& s, int lo, int hi, long long c, float (&acc)[N]) {
+__device__ __forceinline__ void sum_rows(const SumArgs& s, const u32* places, int lo, int hi, long long c, float (&acc)[N]) {
 #pragma unroll
   for (int j = 0; j < N; ++j) acc[j] = 0.f;
   int i = lo;
   for (; i + 4 <= hi; i += 4) {
     float v[4][N];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) Elems<T, N>::load((const T*)s.dout + (long long)__ldcg(s.places + i + k) * s.dout_stride + c * N, v[k]);
+    for (int k = 0; k < 4; ++k) Elems<T, N>::load((const T*)s.dout + (long long)places[i + k] * s.dout_stride + c * N, v[k]);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -257,7 +258,7 @@ __device__ __forceinline__ void sum_rows(const SumArgs& s, int lo, int hi, long 
   }
   for (; i < hi; ++i) {
     float v[N];
-    Elems<T, N>::load((const T*)s.dout + (long long)__ldcg(s.places + i) * s.dout_stride + c * N, v);
+    Elems<T, N>::load((const T*)s.dout + (long long)places[i] * s.dout_stride + c * N, v);
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] += v[j];
   }
@@ -273,7 +274,7 @@ __device__ __forceinline__ void finish_row(const SumArgs& s, long long v, long l
 }
 
 // The first CTAs take a window of the sorted tokens each (and a slice of its columns), for ids with more than `most` tokens; the
-// others SUM_ROWS rows of the table.  TPR threads a row.
+// others `rows` rows of the table.  TPR threads a row.
 template <typename T, typename O, int N, int TPR>
 __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -281,6 +282,7 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
   const long long vecs = s.cols / N;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __shared__ int edge[SUM_ROWS + 1];
+  __shared__ u32 staged[SUM_STAGE];
   const unsigned long_ctas = (unsigned)s.windows * s.slices;
   if (blockIdx.x < long_ctas) {
     const int w = (int)(blockIdx.x / s.slices), lo = w * s.most, hi = min(s.n, lo + s.most);
@@ -304,15 +306,15 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
       float* const part = s.part + (2ll * w + k) * s.part_stride;
       for (long long c = (long long)slice * SUM_CTA + threadIdx.x; c < vecs; c += (long long)s.slices * SUM_CTA) {
         float acc[N];
-        sum_rows<T, N>(s, from, to, c, acc);
+        sum_rows<T, N>(s, s.places, from, to, c, acc);
 #pragma unroll
         for (int j = 0; j < N; ++j) part[c * N + j] = acc[j];
       }
     }
     return;
   }
-  const long long v0 = (long long)(blockIdx.x - long_ctas) * SUM_ROWS;
-  const int rows = (int)min((long long)SUM_ROWS, s.vocab - v0);
+  const long long v0 = (long long)(blockIdx.x - long_ctas) * s.rows;
+  const int rows = (int)min((long long)s.rows, s.vocab - v0);
   if (warp < 2) {
     const int e = lower_bound_warp(s.keys, 0, s.n, (u32)(v0 + (warp ? rows : 0)));
     if (lane == 0) edge[warp ? rows : 0] = e;
@@ -320,6 +322,9 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
   __syncthreads();
   const int lo = edge[0], hi = edge[rows];
   __syncthreads();
+  const bool stage = hi - lo <= SUM_STAGE;            // the tokens' numbers ahead of the loads that need them
+  if (stage)
+    for (int i = threadIdx.x; i < hi - lo; i += SUM_CTA) staged[i] = __ldcg(s.places + lo + i);
   if (threadIdx.x < rows) edge[threadIdx.x] = lo == hi ? lo : lower_bound_lane(s.keys, lo, hi, (u32)(v0 + threadIdx.x));
   __syncthreads();
   const int t = threadIdx.x % TPR;
@@ -328,7 +333,8 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
     if ((from == to && s.leave) || to - from > s.most) continue;
     for (long long c = t; c < vecs; c += TPR) {
       float acc[N];
-      sum_rows<T, N>(s, from, to, c, acc);
+      if (stage) sum_rows<T, N>(s, staged, from - lo, to - lo, c, acc);
+      else sum_rows<T, N>(s, s.places, from, to, c, acc);
       finish_row<O, N>(s, v0 + r, c, acc);
     }
   }
@@ -386,7 +392,11 @@ template <typename T, typename O, int N, int TPR>
 int sum_launch(SumArgs s, const Where& at) {
   const long long slices = (s.cols / N + SUM_CTA - 1) / SUM_CTA;
   s.slices = (int)(slices < 16 ? slices : 16);
-  const long long blocks = (long long)s.windows * s.slices + (s.vocab + SUM_ROWS - 1) / SUM_ROWS;
+  // Rows of the table one after the other are a chain of memory latencies: few of them a CTA as long as that gives every SM only a
+  // few CTAs.
+  s.rows = SUM_ROWS;
+  while (s.rows > SUM_CTA / TPR && s.rows > 1 && s.vocab < 8ll * s.rows * at.sms) s.rows /= 2;
+  const long long blocks = (long long)s.windows * s.slices + (s.vocab + s.rows - 1) / s.rows;
   if (!launch_dependent(k_embedding_sum<T, O, N, TPR>, dim3((unsigned)blocks), SUM_CTA, at, s)) return -1;
   if (!s.windows) return 1;
   return launch_dependent(k_embedding_join<O, N>, dim3((unsigned)s.windows, (unsigned)s.slices), SUM_CTA, at, s) ? 2 : -1;

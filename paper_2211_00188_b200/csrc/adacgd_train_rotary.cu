@@ -42,7 +42,7 @@ __device__ __forceinline__ long long place(long long stride, long long t, int h,
 // --------------------------------------------------------------------------
 // heads of whole aligned runs
 // --------------------------------------------------------------------------
-constexpr int ROT_CTA = 256, ROT_WARPS = ROT_CTA / 32;
+constexpr int ROT_CTA = 256;
 constexpr int ROT_MAX_TOKENS = 8;
 
 // How the partner of a pair is reached: NEAR within the lane (neighbours), LANE in another lane at the same place, ROW through shared
@@ -278,6 +278,252 @@ __global__ void __launch_bounds__(ROT_CTA) k_qk_norm_bwd(adacgd_qk_norm_backward
   }
 }
 
+// --------------------------------------------------------------------------
+// heads of two runs a lane
+// --------------------------------------------------------------------------
+// Where a head is a multiple of 16 long, a lane takes run l and the run half a head further: with the usual rotation, of whole
+// heads in halves, both elements of a pair are its own, and so they are with neighbours.  A warp takes a token, or a part of its heads where
+// there are few tokens, makes the token's cosines and sines once and keeps its lanes' in registers, as it does the weights.
+constexpr int TWO_CTA = 128, TWO_WARPS = TWO_CTA / 32, MAX_PAIRS = 128;
+
+// Cosines and sines of the lane's pairs, packed in twos.  HALVES: pair 8 l + j couples the runs' j-th elements.  Otherwise pair 4 l + i is
+// elements 2 i and 2 i + 1 of the first run, and those of the second follow.
+template <bool HALVES>
+__device__ __forceinline__ void lane_turns(const adacgd_qk_norm_args& a, long long t, int l, bool in, float* table, bool back, F2 (&c)[4], F2 (&s)[4]) {
+  float* const sines = table + MAX_PAIRS;
+  __syncwarp();
+  const long long position = a.pairs ? position_at(a, t) : 0;
+  for (int i = threadIdx.x & 31; i < a.head_dim / 2; i += 32) {
+    float x = 1.f, y = 0.f;
+    if (i < a.pairs) turn(position, a.freq[i], &x, &y);
+    table[i] = x;
+    sines[i] = back ? -y : y;
+  }
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int i = HALVES ? 8 * l + 2 * j : (j < 2 ? 4 * l + 2 * j : 4 * (l + a.head_dim / 16) + 2 * (j - 2));
+    c[j] = in ? *reinterpret_cast<const F2*>(table + i) : f2(1.f, 1.f);
+    s[j] = in ? *reinterpret_cast<const F2*>(sines + i) : f2(0.f, 0.f);
+  }
+}
+__device__ __forceinline__ F2 minus(F2 a) {
+  F2 r;
+  r.v = a.v ^ 0x8000000080000000ull;
+  return r;
+}
+// Turns the lane's sixteen elements: four packed pairs a run.
+template <bool HALVES> __device__ __forceinline__ void turn_two(F2 (&x)[8], const F2 (&c)[4], const F2 (&s)[4]) {
+  if (HALVES) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const F2 a = x[j], b = x[4 + j];
+      x[j] = fma2(a, c[j], mul2(b, minus(s[j])));
+      x[4 + j] = fma2(b, c[j], mul2(a, s[j]));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {                     // element pair j: its turn is half of c[j / 2]
+      float a, b, cx, cy, sx, sy;
+      split(x[j], a, b);
+      split(c[j / 2], cx, cy);
+      split(s[j / 2], sx, sy);
+      const float u = j & 1 ? cy : cx, v = j & 1 ? sy : sx;
+      x[j] = f2(fmaf(a, u, -(b * v)), fmaf(b, u, a * v));
+    }
+  }
+}
+template <typename T> __device__ __forceinline__ void runs_of(const Run<T>& a, const Run<T>& b, F2 (&x)[8]) {
+  float v[8];
+  unpack(a, v);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = f2(v[2 * j], v[2 * j + 1]);
+  unpack(b, v);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[4 + j] = f2(v[2 * j], v[2 * j + 1]);
+}
+template <typename T> __device__ __forceinline__ void store_two(T* first, T* second, const F2 (&x)[8]) {
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) split(x[j], v[2 * j], v[2 * j + 1]);
+  store_run(first, v);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) split(x[4 + j], v[2 * j], v[2 * j + 1]);
+  store_run(second, v);
+}
+template <typename P> __device__ __forceinline__ void lane_weights(const void* w, int e, int half, bool in, F2 (&out)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int at = (j < 4 ? e : e + half) + 2 * (j & 3);
+    out[j] = in ? f2(param<P>(w, at), param<P>(w, at + 1)) : f2(0.f, 0.f);
+  }
+}
+__device__ __forceinline__ float dot16(const F2 (&x)[8], const F2 (&y)[8]) {
+  F2 s = mul2(x[0], y[0]), u = mul2(x[1], y[1]);
+#pragma unroll
+  for (int j = 2; j < 8; j += 2) {
+    s = fma2(x[j], y[j], s);
+    u = fma2(x[j + 1], y[j + 1], u);
+  }
+  float a, b;
+  split(add2(s, u), a, b);
+  return a + b;
+}
+
+// Heads [lo, hi) of one matrix row, LPH lanes a head and BATCH rounds of loads ahead.
+template <typename T, int LPH, bool HALVES, int BATCH>
+__device__ __forceinline__ void norm_heads(const T* x, T* out, int lo, int hi, int dim, float eps, int group, int e, bool in, const F2 (&w)[8],
+                                           const F2 (&c)[4], const F2 (&s)[4]) {
+  constexpr int G = 32 / LPH;
+  const int half = dim / 2;
+  const float inv = 1.f / (float)dim;
+  Run<T> a[BATCH], b[BATCH];
+  auto fetch = [&](int k, int h) {
+    if (h < hi && in) {
+      a[k] = load_run(x + (long long)h * dim + e);
+      b[k] = load_run(x + (long long)h * dim + e + half);
+    } else {
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(T) / 2; ++j) a[k].v[j] = b[k].v[j] = make_uint4(0, 0, 0, 0);
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < BATCH; ++k) fetch(k, lo + k * G + group);
+  for (int h0 = lo; h0 < hi; h0 += BATCH * G) {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int h = h0 + k * G + group;
+      F2 v[8];
+      runs_of(a[k], b[k], v);
+      fetch(k, h + BATCH * G);
+      const float r = rsqrtf(fmaf(head_sum<LPH>(dot16(v, v)), inv, eps));
+      const F2 r2 = f2(r, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = mul2(mul2(v[j], r2), w[j]);
+      turn_two<HALVES>(v, c, s);
+      if (h < hi && in) store_two(out + (long long)h * dim + e, out + (long long)h * dim + e + half, v);
+    }
+  }
+}
+
+// parts: warps a token.
+template <typename T, typename P, int LPH, bool HALVES>
+__global__ void __launch_bounds__(TWO_CTA) k_qk_norm_two(adacgd_qk_norm_args a, int parts) {
+  constexpr int BATCH = sizeof(T) == 4 ? 1 : 2;
+  __shared__ __align__(16) float tables[TWO_WARPS][2 * MAX_PAIRS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPH, group = lane / LPH, e = 8 * l;
+  const long long item = (long long)blockIdx.x * TWO_WARPS + warp, t = item / parts;
+  if (t >= a.tokens) return;
+  const bool in = l < a.head_dim / 16;
+  const int heads = (int)(a.heads + a.key_heads), part = (int)(item % parts);
+  const int lo = (int)((long long)heads * part / parts), hi = (int)((long long)heads * (part + 1) / parts), nq = (int)a.heads;
+  F2 c[4], s[4], w[8];
+  lane_turns<HALVES>(a, t, l, in, tables[warp], false, c, s);
+  if (lo < nq) {
+    lane_weights<P>(a.q_weight, e, a.head_dim / 2, in, w);
+    norm_heads<T, LPH, HALVES, BATCH>((const T*)a.q + t * a.q_stride, (T*)a.q_out + t * a.q_out_stride, lo, min(hi, nq), a.head_dim, a.eps, group, e, in, w, c, s);
+  }
+  if (hi > nq) {
+    lane_weights<P>(a.k_weight, e, a.head_dim / 2, in, w);
+    norm_heads<T, LPH, HALVES, BATCH>((const T*)a.k + t * a.k_stride, (T*)a.k_out + t * a.k_out_stride, max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e,
+                                      in, w, c, s);
+  }
+}
+
+template <typename T, int LPH, bool HALVES, int BATCH>
+__device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, int lo, int hi, int dim, float eps, int group, int e, bool in,
+                                               const F2 (&w)[8], const F2 (&c)[4], const F2 (&s)[4], F2 (&dw)[8]) {
+  constexpr int G = 32 / LPH;
+  const int half = dim / 2;
+  const float inv = 1.f / (float)dim;
+  Run<T> a[BATCH], b[BATCH], p[BATCH], q[BATCH];
+  auto fetch = [&](int k, int h) {
+    if (h < hi && in) {
+      const long long at = (long long)h * dim + e;
+      a[k] = load_run(x + at);
+      b[k] = load_run(x + at + half);
+      p[k] = load_run(y + at);
+      q[k] = load_run(y + at + half);
+    } else {
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(T) / 2; ++j) a[k].v[j] = b[k].v[j] = p[k].v[j] = q[k].v[j] = make_uint4(0, 0, 0, 0);
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < BATCH; ++k) fetch(k, lo + k * G + group);
+  for (int h0 = lo; h0 < hi; h0 += BATCH * G) {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int h = h0 + k * G + group;
+      F2 v[8], d[8];
+      runs_of(a[k], b[k], v);
+      runs_of(p[k], q[k], d);
+      fetch(k, h + BATCH * G);
+      turn_two<HALVES>(d, c, s);
+      const float r = rsqrtf(fmaf(head_sum<LPH>(dot16(v, v)), inv, eps));
+      const F2 r2 = f2(r, r);
+      const bool live = h < hi && in;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = mul2(v[j], r2);                       // x r
+        if (live) dw[j] = fma2(d[j], v[j], dw[j]);
+        d[j] = mul2(d[j], w[j]);                     // g
+      }
+      const float m = -head_sum<LPH>(dot16(d, v)) * inv;
+      const F2 m2 = f2(m, m);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) d[j] = mul2(r2, fma2(m2, v[j], d[j]));
+      if (live) store_two(out + (long long)h * dim + e, out + (long long)h * dim + e + half, d);
+    }
+  }
+}
+
+template <typename T, typename P, int LPH, bool HALVES>
+__global__ void __launch_bounds__(TWO_CTA, 4) k_qk_norm_two_bwd(adacgd_qk_norm_backward_args g, int parts, float* part, long long part_stride) {
+  constexpr int BATCH = 1, DIM = 16 * LPH, SLOTS = TWO_CTA / LPH;
+  const adacgd_qk_norm_args& a = g.f;
+  __shared__ __align__(16) float tables[TWO_WARPS][2 * MAX_PAIRS], rows[SLOTS * DIM];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPH, group = lane / LPH, e = 8 * l, half = a.head_dim / 2;
+  const bool in = l < a.head_dim / 16;
+  const int heads = (int)(a.heads + a.key_heads), nq = (int)a.heads;
+  F2 dwq[8], dwk[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) dwq[j] = dwk[j] = f2(0.f, 0.f);
+  const long long items = a.tokens * parts;
+  for (long long item = (long long)blockIdx.x * TWO_WARPS + warp; item < items; item += (long long)gridDim.x * TWO_WARPS) {
+    const long long t = item / parts;
+    const int mine = (int)(item % parts), lo = (int)((long long)heads * mine / parts), hi = (int)((long long)heads * (mine + 1) / parts);
+    F2 c[4], s[4], w[8];
+    lane_turns<HALVES>(a, t, l, in, tables[warp], true, c, s);
+    if (lo < nq) {
+      lane_weights<P>(a.q_weight, e, half, in, w);
+      norm_heads_bwd<T, LPH, HALVES, BATCH>((const T*)a.q + t * a.q_stride, (const T*)a.q_out + t * a.q_out_stride, (T*)g.dq + t * g.dq_stride, lo,
+                                            min(hi, nq), a.head_dim, a.eps, group, e, in, w, c, s, dwq);
+    }
+    if (hi > nq) {
+      lane_weights<P>(a.k_weight, e, half, in, w);
+      norm_heads_bwd<T, LPH, HALVES, BATCH>((const T*)a.k + t * a.k_stride, (const T*)a.k_out + t * a.k_out_stride, (T*)g.dk + t * g.dk_stride,
+                                            max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e, in, w, c, s, dwk);
+    }
+  }
+  if (!part) return;
+  const int slot = threadIdx.x / LPH;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    __syncthreads();
+    if (in) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) *reinterpret_cast<F2*>(rows + slot * DIM + (j < 4 ? e : e + half) + 2 * (j & 3)) = k ? dwk[j] : dwq[j];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.head_dim; i += TWO_CTA) {
+      float sum = 0.f;
+      for (int j = 0; j < SLOTS; ++j) sum += rows[j * DIM + i];
+      part[(2ll * blockIdx.x + k) * part_stride + i] = sum;
+    }
+  }
+}
+
 // Joins the CTAs' partial gradients in order, in binary64: a warp a column.
 template <typename P>
 __global__ void __launch_bounds__(256) k_qk_norm_dw(const float* part, long long part_stride, int parts, int dim, void* dqw, void* dkw) {
@@ -472,6 +718,44 @@ int norm_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g
   return grads ? join_weights<P>(g, s, (int)ctas, at) : 1;
 }
 
+// Heads of two runs a lane: lengths by 16, whole heads turned in halves, or neighbours, or none.
+bool two_runs(const adacgd_qk_norm_args& a) { return a.head_dim % 16 == 0 && (a.interleaved || a.pairs == 0 || 2 * a.pairs == a.head_dim); }
+// Warps a token: one where that gives every SM sixteen of them.
+int parts_of(const adacgd_qk_norm_args& a, int lph, const Where& at) {
+  const long long heads = a.heads + a.key_heads, most = (heads + 32 / lph - 1) / (32 / lph);
+  long long parts = 16ll * at.sms / a.tokens;
+  if (parts > most) parts = most;
+  return (int)(parts < 1 ? 1 : parts);
+}
+
+template <typename T, typename P, int LPH, bool HALVES>
+int two_launch(const adacgd_qk_norm_args& a, const Where& at) {
+  const int parts = parts_of(a, LPH, at);
+  const long long ctas = (a.tokens * parts + TWO_WARPS - 1) / TWO_WARPS;
+  k_qk_norm_two<T, P, LPH, HALVES><<<(unsigned)ctas, TWO_CTA, 0, at.stream>>>(a, parts);
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
+template <typename T, typename P, int LPH, bool HALVES>
+int two_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g, const Where& at) {
+  const int parts = parts_of(g.f, LPH, at);
+  long long ctas = (g.f.tokens * parts + TWO_WARPS - 1) / TWO_WARPS;
+  if (ctas > 4ll * at.sms) ctas = 4ll * at.sms;
+  if (ctas > NORM_PARTS) ctas = NORM_PARTS;
+  const bool grads = g.dq_weight || g.dk_weight;
+  k_qk_norm_two_bwd<T, P, LPH, HALVES><<<(unsigned)ctas, TWO_CTA, 0, at.stream>>>(g, parts, grads ? s.norm_part : (float*)nullptr, s.max_cols);
+  if (cudaGetLastError() != cudaSuccess) return -1;
+  return grads ? join_weights<P>(g, s, (int)ctas, at) : 1;
+}
+
+#define BY_LANES(call)                                                                                 \
+  if (a.head_dim <= 32) { constexpr int LPH = 2; BY_TURN(call) }                                       \
+  if (a.head_dim <= 64) { constexpr int LPH = 4; BY_TURN(call) }                                       \
+  if (a.head_dim <= 128) { constexpr int LPH = 8; BY_TURN(call) }                                      \
+  { constexpr int LPH = 16; BY_TURN(call) }
+#define BY_TURN(call)                                                                                  \
+  if (!a.interleaved && a.pairs) { constexpr bool HALVES = true; return call; }                        \
+  { constexpr bool HALVES = false; return call; }
+
 #define BY_HEAD(call)                                                                                  \
   const Reach reach = reach_of(a);                                                                     \
   if (a.head_dim <= 64) { constexpr int LPH = 8; BY_REACH(call) }                                      \
@@ -488,6 +772,7 @@ int norm_t(const adacgd_qk_norm_args& a, const Where& at) {
     k_qk_norm_any<T, P><<<(unsigned)a.tokens, ANY_CTA, (2 + ANY_WARPS) * a.head_dim * 4, at.stream>>>(a);
     return cudaGetLastError() == cudaSuccess ? 1 : -1;
   }
+  if (two_runs(a)) { BY_LANES((two_launch<T, P, LPH, HALVES>(a, at))) }
   BY_HEAD((norm_launch<T, P, LPH, REACH>(a, at)))
 }
 
@@ -504,6 +789,7 @@ int norm_bwd_t(const TrainScratch& s, const adacgd_qk_norm_backward_args& g, con
     if (cudaGetLastError() != cudaSuccess) return -1;
     return grads ? join_weights<P>(g, s, ctas, at) : 1;
   }
+  if (two_runs(a)) { BY_LANES((two_bwd_launch<T, P, LPH, HALVES>(s, g, at))) }
   BY_HEAD((norm_bwd_launch<T, P, LPH, REACH>(s, g, at)))
 }
 
