@@ -34,7 +34,7 @@ __device__ __forceinline__ u64 now_ns() {
 // Waits for the phase with this parity, for two seconds at most: nothing here takes a thousandth of that, so a wait that runs out means that
 // the kernel is wrong.  It then says so in `dead`, on which all the CTA's waits give up.
 constexpr u64 WAIT_NS = 2000000000ull;
-__device__ __noinline__ bool mbar_wait_long(u32 bar, u32 parity, volatile int* dead) {
+__device__ __forceinline__ bool mbar_wait_long(u32 bar, u32 parity, volatile int* dead) {
   const u64 begin = now_ns();
   for (;;) {
     if (mbar_try(bar, parity)) return true;

@@ -18,7 +18,8 @@ namespace adacgd {
 namespace {
 
 constexpr int TILE = 128, HALF = TILE * 128;       // rows of a tile; bytes of 64 of its columns
-constexpr int MMA_CTA = 320, MMA_WARP = 8, COPY_WARP = 9;
+constexpr int FWD_CTA = 384, FWD_ROWS = 8;         // threads; warps that hold rows, before the product and the copying warp
+constexpr int BWD_CTA = 576, BWD_ROWS = 16;
 
 struct Maps {
   CUtensorMap q, k, v, dout;
@@ -78,35 +79,32 @@ template <bool BF16, int DP> __device__ __forceinline__ void product_nt(u32 d, u
     mma_ss(d, operand(a + off, 16), operand(b + off, 16), product_of(BF16, TILE, false), k > 0);
   }
 }
-// d [128 x DP] += p tile, p in tensor memory: 16 rows of the tile a step.  The second half of p's columns begins `gap` columns behind the
-// first one's start.
-template <bool BF16, int DP> __device__ __forceinline__ void product_pn(u32 d, u32 p, u32 gap, u32 tile, bool add) {
+// d [128 x DP] += p tile, p in tensor memory: 16 rows of the tile a step.  p was put in the place of 128 columns of scores, by parts of
+// them: 16 PER numbers in the first half of a part's columns.
+template <bool BF16, int DP, int PER> __device__ __forceinline__ void product_pn(u32 d, u32 p, u32 tile, bool add) {
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    mma_ts(d, p + (k / 4) * gap + (k % 4) * 8, operand(tile + k * 2048, HALF), product_of(BF16, DP, true), add || k > 0);
+    mma_ts(d, p + (k / PER) * PER * 16 + (k % PER) * 8, operand(tile + k * 2048, HALF), product_of(BF16, DP, true), add || k > 0);
 }
 
 // ---- rows of results ----
-// Stores factor * (DP columns of tensor memory) as one row of `dim` elements, or zeros.
-template <bool BF16, int DP>
-__device__ __forceinline__ void store_row(void* base, long long stride, long long row, int head, int dim, u32 tmem, float factor, bool inside, bool zero) {
+// Stores factor * (32 columns of tensor memory) as elements c .. c + 31 of a row of `dim`, or zeros.
+template <bool BF16>
+__device__ __forceinline__ void store_cols(void* base, long long stride, long long row, int head, int dim, int c, u32 tmem, float factor, bool inside, bool zero) {
   char* const to = (char*)base + (row * stride + (long long)head * dim) * 2;
+  u32 r[32];
+  __syncwarp();
+  tmem_ld32(tmem + c, r);
+  tmem_wait_ld();
+  tmem_hold(r);
 #pragma unroll
-  for (int c = 0; c < DP; c += 32) {
-    u32 r[32];
-    __syncwarp();
-    tmem_ld32(tmem + c, r);
-    tmem_wait_ld();
-    tmem_hold(r);
+  for (int j = 0; j < 32; j += 8) {
+    if (!inside || c + j >= dim) continue;
+    u32 w[4];
 #pragma unroll
-    for (int j = 0; j < 32; j += 8) {
-      if (!inside || c + j >= dim) continue;
-      u32 w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        w[i] = zero ? 0u : pack2<BF16>(__uint_as_float(r[j + 2 * i]) * factor, __uint_as_float(r[j + 2 * i + 1]) * factor);
-      *reinterpret_cast<uint4*>(to + (c + j) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    for (int i = 0; i < 4; ++i)
+      w[i] = zero ? 0u : pack2<BF16>(__uint_as_float(r[j + 2 * i]) * factor, __uint_as_float(r[j + 2 * i + 1]) * factor);
+    *reinterpret_cast<uint4*>(to + (c + j) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 // What a kernel leaves whose wait has run out: NaN in either type.
@@ -130,7 +128,7 @@ template <int DP> struct FwdLayout {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_mma(const __grid_constant__ Maps maps, adacgd_attention_args g) {
+__global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_constant__ Maps maps, adacgd_attention_args g) {
   typedef FwdLayout<DP> L;
   extern __shared__ __align__(1024) unsigned char mma_smem[];
   const adacgd_attention_inputs& a = g.in;
@@ -157,7 +155,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_mma(const __grid_const
     *dead = 0;
     mbar_init_fence();
   }
-  if (warp == MMA_WARP) tmem_alloc(smem_addr(tmem_at), 512);
+  if (warp == FWD_ROWS) tmem_alloc(smem_addr(tmem_at), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -168,59 +166,64 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_mma(const __grid_const
   count[0] = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
   count[1] = t.first + TILE >= t.length ? 0 : (a.causal ? min(tiles, t.first / TILE + 2) : tiles);
   const int n = max(count[0], count[1]);
-  if (warp == COPY_WARP) {
-    if (lane == 0) {
-      mbar_expect(q_full, (count[1] ? 2 : 1) * L::BYTES);
-      copy_tile<DP>(base, &maps.q, head, t.row + t.first, q_full);
-      if (count[1]) copy_tile<DP>(base + L::BYTES, &maps.q, head, t.row + t.first + TILE, q_full);
-    }
-    u32 side = 0, words[4];
-    int i = 0;
-    bool ok = true;
-    for (; ok && i < 2 * n; ++i) {                             // tiles of keys and values in turn, the last ones first
-      const int st = i % L::STAGES, first = (n - 1 - i / 2) * TILE;
-      if (i >= L::STAGES && !mbar_wait(empty + 8 * st, (i / L::STAGES - 1) & 1, dead)) break;
-      if (!(i & 1)) counted(a, t, first, words);
-      ok = bring<DP>(base + L::RING + st * L::BYTES, i & 1 ? &maps.v : &maps.k, kh, t.row + first, words, i & 1, full + 8 * st, aside, side, dead);
-    }
-    if (*dead) {
-      settle(q_full, 0);
-      for (int b = max(0, i - L::STAGES); b < i; ++b) settle(full + 8 * (b % L::STAGES), (b / L::STAGES) & 1);
-    }
-  } else if (warp == MMA_WARP) {
-    if (lane == 0) {
-      bool ok = mbar_wait(q_full, 0, dead);
-      for (int j = 0; ok && j <= n; ++j) {
-        const int ik = 2 * j, iv = 2 * j - 1, sk = ik % L::STAGES, sv = iv % L::STAGES;
-        if (j < n && !(ok = mbar_wait(full + 8 * sk, (ik / L::STAGES) & 1, dead))) break;
-        if (j > 0 && !(ok = mbar_wait(full + 8 * sv, (iv / L::STAGES) & 1, dead))) break;
-        for (int x = 0; ok && x < 2; ++x) {
-          const int u = j - (n - count[x]);                    // the step as x counts
-          if (u < 0 || count[x] == 0) continue;
-          const u32 s = tmem + x * TILE, o = tmem + 2 * TILE + x * DP;
-          if (u > 0) {
-            if (!(ok = mbar_wait(p_full + 8 * x, (u - 1) & 1, dead))) break;
-            tc_fence_after();
-            product_pn<BF16, DP>(o, s, 32, base + L::RING + sv * L::BYTES, u > 1);
-          }
-          if (j < n) {
-            tc_fence_after();
-            product_nt<BF16, DP>(s, base + x * L::BYTES, base + L::RING + sk * L::BYTES);
-            mma_commit(s_full + 8 * x);
-          } else {
-            mma_commit(o_full + 8 * x);
-          }
-        }
-        if (!ok) break;
-        if (j < n) mma_commit(empty + 8 * sk);
-        if (j > 0) mma_commit(empty + 8 * sv);
+  // A row's 128 scores are held at once: of the CTA's 384 x 168 registers the row warps get 208 each, the others 88.
+  if (warp >= FWD_ROWS) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == FWD_ROWS + 1) {
+      if (lane == 0) {
+        mbar_expect(q_full, (count[1] ? 2 : 1) * L::BYTES);
+        copy_tile<DP>(base, &maps.q, head, t.row + t.first, q_full);
+        if (count[1]) copy_tile<DP>(base + L::BYTES, &maps.q, head, t.row + t.first + TILE, q_full);
+      }
+      u32 side = 0, words[4];
+      int i = 0;
+      bool ok = true;
+      for (; ok && i < 2 * n; ++i) {                             // tiles of keys and values in turn, the last ones first
+        const int st = i % L::STAGES, first = (n - 1 - i / 2) * TILE;
+        if (i >= L::STAGES && !mbar_wait(empty + 8 * st, (i / L::STAGES - 1) & 1, dead)) break;
+        if (!(i & 1)) counted(a, t, first, words);
+        ok = bring<DP>(base + L::RING + st * L::BYTES, i & 1 ? &maps.v : &maps.k, kh, t.row + first, words, i & 1, full + 8 * st, aside, side, dead);
       }
       if (*dead) {
-        mma_commit(aside);                                     // nobody else uses it any more, or its wait has run out too
-        settle(aside, 0);
+        settle(q_full, 0);
+        for (int b = max(0, i - L::STAGES); b < i; ++b) settle(full + 8 * (b % L::STAGES), (b / L::STAGES) & 1);
+      }
+    } else if (warp == FWD_ROWS) {
+      if (lane == 0) {
+        bool ok = mbar_wait(q_full, 0, dead);
+        for (int j = 0; ok && j <= n; ++j) {
+          const int ik = 2 * j, iv = 2 * j - 1, sk = ik % L::STAGES, sv = iv % L::STAGES;
+          if (j < n && !(ok = mbar_wait(full + 8 * sk, (ik / L::STAGES) & 1, dead))) break;
+          if (j > 0 && !(ok = mbar_wait(full + 8 * sv, (iv / L::STAGES) & 1, dead))) break;
+          for (int x = 0; ok && x < 2; ++x) {
+            const int u = j - (n - count[x]);                    // the step as x counts
+            if (u < 0 || count[x] == 0) continue;
+            const u32 s = tmem + x * TILE, o = tmem + 2 * TILE + x * DP;
+            if (u > 0) {
+              if (!(ok = mbar_wait(p_full + 8 * x, (u - 1) & 1, dead))) break;
+              tc_fence_after();
+              product_pn<BF16, DP, 8>(o, s, base + L::RING + sv * L::BYTES, u > 1);
+            }
+            if (j < n) {
+              tc_fence_after();
+              product_nt<BF16, DP>(s, base + x * L::BYTES, base + L::RING + sk * L::BYTES);
+              mma_commit(s_full + 8 * x);
+            } else {
+              mma_commit(o_full + 8 * x);
+            }
+          }
+          if (!ok) break;
+          if (j < n) mma_commit(empty + 8 * sk);
+          if (j > 0) mma_commit(empty + 8 * sv);
+        }
+        if (*dead) {
+          mma_commit(aside);                                     // nobody else uses it any more, or its wait has run out too
+          settle(aside, 0);
+        }
       }
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int x = warp >> 2, i = t.first + x * TILE + (warp & 3) * 32 + lane;
     const u32 lanes = (u32)(warp & 3) << 21, s_at = tmem + x * TILE + lanes, o_at = tmem + 2 * TILE + x * DP + lanes;
     const float c = a.scale * LOG2E;
@@ -301,14 +304,15 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_mma(const __grid_const
     if (count[x] && ok && mbar_wait(o_full + 8 * x, 0, dead)) {
       tc_fence_after();
       const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
-      store_row<BF16, DP>(g.out, g.out_stride, t.row + i, head, a.head_dim, o_at, 1.f / sum, inside, !on);
+#pragma unroll
+      for (int d = 0; d < DP; d += 32) store_cols<BF16>(g.out, g.out_stride, t.row + i, head, a.head_dim, d, o_at, 1.f / sum, inside, !on);
       if (inside && g.lse) g.lse[(long long)head * a.tokens + t.row + i] = on ? fmaf(top, a.scale, logf(BF16 ? sum : sum * 0.0078125f)) : -INFINITY;
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == MMA_WARP) tmem_free(tmem, 512);
+  if (warp == FWD_ROWS) tmem_free(tmem, 512);
   if (*dead && threadIdx.x < 2 * TILE && t.first + (int)threadIdx.x < t.length)
     poison_row(g.out, g.out_stride, t.row + t.first + threadIdx.x, head, a.head_dim);
 }
@@ -401,14 +405,15 @@ __device__ __forceinline__ float range_of(const float* most, int parts) {
 // --------------------------------------------------------------------------
 // A CTA takes a tile of queries and walks over tiles of keys: S = Q K^T, dP = dO V^T, ds = p (dP - row_dot) in S's place, dQ += ds K.
 // S has two places, so that the next one is there while this one's exponentials run; dP is free again once ds has been made.
-// The eight warps share a tile by halves of its columns.
+// Sixteen warps share a tile by quarters of its columns: eight with twice the columns each left a scheduler two warps, whose chains of
+// conversions and exponentials nothing filled (4600 clocks a step; 1536 of products).
 template <int DP> struct DqLayout {
   static constexpr int BYTES = DP * 256, KS = DP == 128 ? 3 : 4, VS = DP == 128 ? 2 : 4, RING = 2 * BYTES;
-  static constexpr int PART = RING + (KS + VS) * BYTES, BARS = PART + 1024, TOTAL = BARS + 256;
+  static constexpr int PART = RING + (KS + VS) * BYTES, BARS = PART + 4 * TILE * 4, TOTAL = BARS + 256;
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most, int parts) {
+__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most, int parts) {
   typedef DqLayout<DP> L;
   extern __shared__ __align__(1024) unsigned char mma_smem[];
   const adacgd_attention_inputs& a = g.in;
@@ -428,7 +433,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
     mbar_init(s_full, 1);
     mbar_init(s_full + 8, 1);
     mbar_init(dp_full, 1);
-    mbar_init(ds_full, 256);
+    mbar_init(ds_full, 32 * BWD_ROWS);
     mbar_init(dq_full, 1);
     for (int i = 0; i < L::KS; ++i) {
       mbar_init(k_full + 8 * i, 1);
@@ -441,7 +446,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
     *dead = 0;
     mbar_init_fence();
   }
-  if (warp == MMA_WARP) tmem_alloc(smem_addr(tmem_at), 512);
+  if (warp == BWD_ROWS) tmem_alloc(smem_addr(tmem_at), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -449,7 +454,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
   const u32 q_tile = base, do_tile = base + L::BYTES, k_tiles = base + L::RING, v_tiles = k_tiles + L::KS * L::BYTES;
   const int kh = head / (a.heads / a.key_heads), tiles = (t.length + TILE - 1) / TILE;
   const int n = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
-  if (warp == COPY_WARP) {
+  if (warp == BWD_ROWS + 1) {
     if (lane == 0) {
       mbar_expect(q_full, 2 * L::BYTES);
       copy_tile<DP>(q_tile, &maps.q, head, t.row + t.first, q_full);
@@ -472,7 +477,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
       for (int b = max(0, nk - L::KS); b < nk; ++b) settle(k_full + 8 * (b % L::KS), (b / L::KS) & 1);
       for (int b = max(0, nv - L::VS); b < nv; ++b) settle(v_full + 8 * (b % L::VS), (b / L::VS) & 1);
     }
-  } else if (warp == MMA_WARP) {
+  } else if (warp == BWD_ROWS) {
     if (lane == 0) {
       auto scores = [&](int j) {                               // S of step j
         const int st = j % L::KS;
@@ -496,7 +501,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
         if (!mbar_wait(ds_full, j & 1, dead)) break;
         tc_fence_after();
         if (j + 1 < n && !shares(j + 1)) break;
-        product_pn<BF16, DP>(dq_at, tmem + (j & 1) * TILE, 64, k_tiles + (j % L::KS) * L::BYTES, j > 0);
+        product_pn<BF16, DP, 2>(dq_at, tmem + (j & 1) * TILE, k_tiles + (j % L::KS) * L::BYTES, j > 0);
         mma_commit(k_empty + 8 * (j % L::KS));
         if (j + 1 == n) mma_commit(dq_full);
         if (j + 2 < n && !scores(j + 2)) break;
@@ -507,16 +512,16 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
       }
     }
   } else {
-    const int half = warp >> 2, r = (warp & 3) * 32 + lane, i = t.first + r;
+    const int part_of = warp >> 2, r = (warp & 3) * 32 + lane, i = t.first + r;
     const u32 lanes = (u32)(warp & 3) << 21;
     const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
     const long long at = (long long)head * a.tokens + t.row + i;
     float dot = 0.f, range = 1.f;
     if (BF16) {
-      if (on) {                                                // each half of the warps takes 64 of the head's elements
+      if (on) {                                                // each quarter of the warps takes 32 of the head's elements
         const __nv_bfloat16* const x = (const __nv_bfloat16*)g.dout + (t.row + i) * g.dout_stride + (long long)head * a.head_dim;
         const __nv_bfloat16* const y = (const __nv_bfloat16*)g.out + (t.row + i) * g.out_stride + (long long)head * a.head_dim;
-        for (int d = 64 * half; d < min(a.head_dim, 64 * half + 64); d += 8) {
+        for (int d = 32 * part_of; d < min(a.head_dim, 32 * part_of + 32); d += 8) {
           float u[8], v[8];
           unpack(load_run(x + d), u);
           unpack(load_run(y + d), v);
@@ -524,10 +529,10 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
           for (int k = 0; k < 8; ++k) dot = fmaf(u[k], v[k], dot);
         }
       }
-      part[half * TILE + r] = dot;
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      dot = part[r] + part[TILE + r];
-      if (half == 0 && inside) g.row_dot[at] = dot;
+      part[part_of * TILE + r] = dot;
+      asm volatile("bar.sync 1, 512;" ::: "memory");
+      dot = (part[r] + part[TILE + r]) + (part[2 * TILE + r] + part[3 * TILE + r]);
+      if (part_of == 0 && inside) g.row_dot[at] = dot;
     } else {
       range = range_of(most, parts);
       if (on) dot = __ldcg(g.row_dot + at) * range;
@@ -537,68 +542,58 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dq_mma(const __grid_co
     bool ok = true;
     for (int j = 0; j < n; ++j) {
       const int j0 = (n - 1 - j) * TILE;
-      const u32 s_at = tmem + (j & 1) * TILE + 64 * half + lanes;
-      u32 words[4];
+      const u32 s_at = tmem + (j & 1) * TILE + 32 * part_of + lanes;
+      u32 bits = 0xffffffffu;
       const bool mask = a.mask || j0 + TILE > t.length || (a.causal && j0 + TILE > t.first);
       if (mask) {
-        counted(a, t, j0, words);
-        if (a.causal)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) words[w] &= low_bits(i + 1 - j0 - 32 * w);
+        const int key = j0 + 32 * part_of;
+        bits = __ballot_sync(0xffffffffu, key + lane < t.length && (!a.mask || a.mask[t.row + key + lane]));
+        if (a.causal) bits &= low_bits(i + 1 - key);
       }
       if (!(ok = mbar_wait(s_full + 8 * (j & 1), (j >> 1) & 1, dead))) break;
       tc_fence_after();
-      u32 s[2][32];
-      tmem_ld32(s_at, s[0]);
-      tmem_ld32(s_at + 32, s[1]);
+      u32 s[32];
+      tmem_ld32(s_at, s);
       tmem_wait_ld();
-      tmem_hold(s[0]);
-      tmem_hold(s[1]);
-      F2 p[2][16];
+      tmem_hold(s);
+      F2 p[16];
 #pragma unroll
-      for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int k = 0; k < 32; k += 2) {
-          float y0, y1;
-          split(fma2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), c2, low2), y0, y1);
-          p[w][k / 2] = f2(ex2(y0), ex2(y1));
-        }
+      for (int k = 0; k < 32; k += 2) {
+        float y0, y1;
+        split(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, low2), y0, y1);
+        p[k / 2] = f2(ex2(y0), ex2(y1));
+      }
       if (!(ok = mbar_wait(dp_full, j & 1, dead))) break;
       tc_fence_after();
-      tmem_ld32(dp_at + 64 * half + lanes, s[0]);
-      tmem_ld32(dp_at + 64 * half + 32 + lanes, s[1]);
+      tmem_ld32(dp_at + 32 * part_of + lanes, s);
       tmem_wait_ld();
-      tmem_hold(s[0]);
-      tmem_hold(s[1]);
-      u32 ds[32];
+      tmem_hold(s);
+      u32 ds[16];
 #pragma unroll
-      for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int k = 0; k < 32; k += 2) {
-          float y0, y1;
-          const F2 dp = f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1]));
-          split(mul2(p[w][k / 2], BF16 ? add2(dp, dot2) : fma2(dp, range2, dot2)), y0, y1);
-          if (mask) {
-            const u32 bits = half ? words[2 + w] : words[w];
-            y0 = bits >> k & 1 ? y0 : 0.f;
-            y1 = bits >> (k + 1) & 1 ? y1 : 0.f;
-          }
-          ds[16 * w + k / 2] = pack2<BF16>(y0, y1);
+      for (int k = 0; k < 32; k += 2) {
+        float y0, y1;
+        const F2 dp = f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1]));
+        split(mul2(p[k / 2], BF16 ? add2(dp, dot2) : fma2(dp, range2, dot2)), y0, y1);
+        if (mask) {
+          y0 = bits >> k & 1 ? y0 : 0.f;
+          y1 = bits >> (k + 1) & 1 ? y1 : 0.f;
         }
-      tmem_st32(s_at, ds);
+        ds[k / 2] = pack2<BF16>(y0, y1);
+      }
+      tmem_st16(s_at, ds);
       tmem_wait_st();
       tc_fence_before();
       mbar_arrive(ds_full);
     }
-    if (ok && mbar_wait(dq_full, 0, dead) && half == 0) {
+    if (ok && mbar_wait(dq_full, 0, dead) && 32 * part_of < DP) {
       tc_fence_after();
-      store_row<BF16, DP>(g.dq, g.dq_stride, t.row + i, head, a.head_dim, dq_at + lanes, a.scale / range, inside, !on);
+      store_cols<BF16>(g.dq, g.dq_stride, t.row + i, head, a.head_dim, 32 * part_of, dq_at + lanes, a.scale / range, inside, !on);
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == MMA_WARP) tmem_free(tmem, 512);
+  if (warp == BWD_ROWS) tmem_free(tmem, 512);
   if (*dead && threadIdx.x < TILE && t.first + (int)threadIdx.x < t.length)
     poison_row(g.dq, g.dq_stride, t.row + t.first + threadIdx.x, head, a.head_dim);
 }
@@ -616,7 +611,7 @@ template <int DP> struct DkvLayout {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most, int parts) {
+__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most, int parts) {
   typedef DkvLayout<DP> L;
   extern __shared__ __align__(1024) unsigned char mma_smem[];
   const adacgd_attention_inputs& a = g.in;
@@ -635,8 +630,8 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
     mbar_init(aside, 1);
     mbar_init(s_full, 1);
     mbar_init(dp_full, 1);
-    mbar_init(p_full, 256);
-    mbar_init(ds_full, 256);
+    mbar_init(p_full, 32 * BWD_ROWS);
+    mbar_init(ds_full, 32 * BWD_ROWS);
     mbar_init(end_full, 1);
     for (int i = 0; i < L::STAGES; ++i) {
       mbar_init(full + 8 * i, 1);
@@ -645,7 +640,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
     *dead = 0;
     mbar_init_fence();
   }
-  if (warp == MMA_WARP) tmem_alloc(smem_addr(tmem_at), 512);
+  if (warp == BWD_ROWS) tmem_alloc(smem_addr(tmem_at), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -654,7 +649,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
   // binary16: p is taken 2^14 times larger, ds by its range (see above)
   const float range = BF16 ? 1.f : range_of(most, parts), shift = BF16 ? 0.f : 14.f, back = BF16 ? 1.f : 6.103515625e-05f;
   const int begin = a.causal ? t.first / TILE : 0, each = (t.length + TILE - 1) / TILE - begin, n = each * group;
-  if (warp == COPY_WARP) {
+  if (warp == BWD_ROWS + 1) {
     if (lane == 0) {
       mbar_expect(kv_full, 2 * L::BYTES);
       copy_tile<DP>(k_tile, &maps.k, kh, t.row + t.first, kv_full);
@@ -687,7 +682,7 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
       settle(kv_full, 0);
       for (int b = max(0, i - L::STAGES); b < i; ++b) settle(full + 8 * (b % L::STAGES), (b / L::STAGES) & 1);
     }
-  } else if (warp == MMA_WARP) {
+  } else if (warp == BWD_ROWS) {
     if (lane == 0) {
       auto tile = [&](int i) { return ring + (i % L::STAGES) * L::BYTES; };
       auto scores = [&](int j) {
@@ -708,12 +703,12 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
       for (int j = 0; ok && j < n; ++j) {
         if (!mbar_wait(p_full, j & 1, dead)) break;
         tc_fence_after();
-        product_pn<BF16, DP>(dv_at, tmem, 64, tile(2 * j + 1), j > 0);
+        product_pn<BF16, DP, 2>(dv_at, tmem, tile(2 * j + 1), j > 0);
         mma_commit(empty + 8 * ((2 * j + 1) % L::STAGES));
         if (j + 1 < n && !scores(j + 1)) break;
         if (!mbar_wait(ds_full, j & 1, dead)) break;
         tc_fence_after();
-        product_pn<BF16, DP>(dk_at, dp_at, 64, tile(2 * j), j > 0);
+        product_pn<BF16, DP, 2>(dk_at, dp_at, tile(2 * j), j > 0);
         mma_commit(empty + 8 * (2 * j % L::STAGES));
         if (j + 1 < n && !shares(j + 1)) break;
       }
@@ -724,75 +719,67 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
       }
     }
   } else {
-    const int half = warp >> 2, i = t.first + (warp & 3) * 32 + lane;   // the thread's key
-    const u32 lanes = (u32)(warp & 3) << 21, s_at = tmem + 64 * half + lanes, d_at = dp_at + 64 * half + lanes;
+    const int part_of = warp >> 2, i = t.first + (warp & 3) * 32 + lane;   // the thread's key
+    const u32 lanes = (u32)(warp & 3) << 21, s_at = tmem + 32 * part_of + lanes, d_at = dp_at + 32 * part_of + lanes;
     const float c = a.scale * LOG2E;
     const F2 c2 = f2(c, c), range2 = f2(range * back, range * back);
     bool ok = true;
     for (int j = 0; j < n; ++j) {
-      const int first = (begin + j % each) * TILE + 64 * half;
-      const float* const low = stats + (j & 1) * 2 * TILE + 64 * half;
+      const int first = (begin + j % each) * TILE + 32 * part_of;
+      const float* const low = stats + (j & 1) * 2 * TILE + 32 * part_of;
       const bool mask = a.causal && first < t.first + TILE;              // queries before the key
       // the log sums come with dout's tile
       if (!(ok = mbar_wait(full + 8 * ((2 * j + 1) % L::STAGES), ((2 * j + 1) / L::STAGES) & 1, dead))) break;
       if (!(ok = mbar_wait(s_full, j & 1, dead))) break;
       tc_fence_after();
-      u32 s[2][32];
-      tmem_ld32(s_at, s[0]);
-      tmem_ld32(s_at + 32, s[1]);
+      u32 s[32];
+      tmem_ld32(s_at, s);
       tmem_wait_ld();
-      tmem_hold(s[0]);
-      tmem_hold(s[1]);
-      F2 p[2][16];
-      u32 w16[32];
+      tmem_hold(s);
+      F2 p[16];
+      u32 w16[16];
 #pragma unroll
-      for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int k = 0; k < 32; k += 4) {
-          const float4 l = *reinterpret_cast<const float4*>(low + 32 * w + k);
-          float y0, y1, y2, y3;
-          split(fma2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), c2, f2(l.x, l.y)), y0, y1);
-          split(fma2(f2(__uint_as_float(s[w][k + 2]), __uint_as_float(s[w][k + 3])), c2, f2(l.z, l.w)), y2, y3);
-          y0 = ex2(y0);
-          y1 = ex2(y1);
-          y2 = ex2(y2);
-          y3 = ex2(y3);
-          if (mask) {
-            const int q = first + 32 * w + k;
-            y0 = q >= i ? y0 : 0.f;
-            y1 = q + 1 >= i ? y1 : 0.f;
-            y2 = q + 2 >= i ? y2 : 0.f;
-            y3 = q + 3 >= i ? y3 : 0.f;
-          }
-          p[w][k / 2] = f2(y0, y1);
-          p[w][k / 2 + 1] = f2(y2, y3);
-          w16[16 * w + k / 2] = pack2<BF16>(y0, y1);
-          w16[16 * w + k / 2 + 1] = pack2<BF16>(y2, y3);
+      for (int k = 0; k < 32; k += 4) {
+        const float4 l = *reinterpret_cast<const float4*>(low + k);
+        float y0, y1, y2, y3;
+        split(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, f2(l.x, l.y)), y0, y1);
+        split(fma2(f2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, f2(l.z, l.w)), y2, y3);
+        y0 = ex2(y0);
+        y1 = ex2(y1);
+        y2 = ex2(y2);
+        y3 = ex2(y3);
+        if (mask) {
+          const int q = first + k;
+          y0 = q >= i ? y0 : 0.f;
+          y1 = q + 1 >= i ? y1 : 0.f;
+          y2 = q + 2 >= i ? y2 : 0.f;
+          y3 = q + 3 >= i ? y3 : 0.f;
         }
-      tmem_st32(s_at, w16);
+        p[k / 2] = f2(y0, y1);
+        p[k / 2 + 1] = f2(y2, y3);
+        w16[k / 2] = pack2<BF16>(y0, y1);
+        w16[k / 2 + 1] = pack2<BF16>(y2, y3);
+      }
+      tmem_st16(s_at, w16);
       tmem_wait_st();
       tc_fence_before();
       mbar_arrive(p_full);
       if (!(ok = mbar_wait(dp_full, j & 1, dead))) break;
       tc_fence_after();
-      tmem_ld32(d_at, s[0]);
-      tmem_ld32(d_at + 32, s[1]);
+      tmem_ld32(d_at, s);
       tmem_wait_ld();
-      tmem_hold(s[0]);
-      tmem_hold(s[1]);
+      tmem_hold(s);
 #pragma unroll
-      for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int k = 0; k < 32; k += 4) {
-          const float4 l = *reinterpret_cast<const float4*>(low + TILE + 32 * w + k);
-          float y0, y1, y2, y3;
-          const F2 u = f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), v = f2(__uint_as_float(s[w][k + 2]), __uint_as_float(s[w][k + 3]));
-          split(mul2(p[w][k / 2], BF16 ? add2(u, f2(l.x, l.y)) : fma2(u, range2, f2(l.x, l.y))), y0, y1);
-          split(mul2(p[w][k / 2 + 1], BF16 ? add2(v, f2(l.z, l.w)) : fma2(v, range2, f2(l.z, l.w))), y2, y3);
-          w16[16 * w + k / 2] = pack2<BF16>(y0, y1);
-          w16[16 * w + k / 2 + 1] = pack2<BF16>(y2, y3);
-        }
-      tmem_st32(d_at, w16);
+      for (int k = 0; k < 32; k += 4) {
+        const float4 l = *reinterpret_cast<const float4*>(low + TILE + k);
+        float y0, y1, y2, y3;
+        const F2 u = f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), v = f2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3]));
+        split(mul2(p[k / 2], BF16 ? add2(u, f2(l.x, l.y)) : fma2(u, range2, f2(l.x, l.y))), y0, y1);
+        split(mul2(p[k / 2 + 1], BF16 ? add2(v, f2(l.z, l.w)) : fma2(v, range2, f2(l.z, l.w))), y2, y3);
+        w16[k / 2] = pack2<BF16>(y0, y1);
+        w16[k / 2 + 1] = pack2<BF16>(y2, y3);
+      }
+      tmem_st16(d_at, w16);
       tmem_wait_st();
       tc_fence_before();
       mbar_arrive(ds_full);
@@ -800,14 +787,16 @@ __global__ void __launch_bounds__(MMA_CTA, 1) k_attention_dkv_mma(const __grid_c
     if (ok && mbar_wait(end_full, 0, dead)) {
       tc_fence_after();
       const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
-      if (half == 0) store_row<BF16, DP>(g.dk, g.dk_stride, t.row + i, kh, a.head_dim, dk_at + lanes, a.scale / range, inside, !on);
-      else store_row<BF16, DP>(g.dv, g.dv_stride, t.row + i, kh, a.head_dim, dv_at + lanes, back, inside, !on);
+      if (32 * part_of < DP) {
+        store_cols<BF16>(g.dk, g.dk_stride, t.row + i, kh, a.head_dim, 32 * part_of, dk_at + lanes, a.scale / range, inside, !on);
+        store_cols<BF16>(g.dv, g.dv_stride, t.row + i, kh, a.head_dim, 32 * part_of, dv_at + lanes, back, inside, !on);
+      }
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == MMA_WARP) tmem_free(tmem, 512);
+  if (warp == BWD_ROWS) tmem_free(tmem, 512);
   if (*dead && threadIdx.x < TILE && t.first + (int)threadIdx.x < t.length) {
     poison_row(g.dk, g.dk_stride, t.row + t.first + threadIdx.x, kh, a.head_dim);
     poison_row(g.dv, g.dv_stride, t.row + t.first + threadIdx.x, kh, a.head_dim);
@@ -849,15 +838,15 @@ bool takes(const adacgd_attention_inputs& a) {
 }
 
 template <typename K, typename... A>
-bool launch_mma(K kern, std::atomic<int> (&table)[TRAIN_DEVICES], int smem, long long ctas, const Where& at, const A&... args) {
-  if (resident_ctas(kern, table, at.device, MMA_CTA, smem) < 1) return false;
-  kern<<<(unsigned)ctas, MMA_CTA, smem, at.stream>>>(args...);
+bool launch_mma(K kern, std::atomic<int> (&table)[TRAIN_DEVICES], int threads, int smem, long long ctas, const Where& at, const A&... args) {
+  if (resident_ctas(kern, table, at.device, threads, smem) < 1) return false;
+  kern<<<(unsigned)ctas, threads, smem, at.stream>>>(args...);
   return cudaGetLastError() == cudaSuccess;
 }
 
 template <bool BF16, int DP> int fwd_mma(const Maps& m, const adacgd_attention_args& g, const Where& at) {
   static std::atomic<int> table[TRAIN_DEVICES];
-  return launch_mma(k_attention_mma<BF16, DP>, table, FwdLayout<DP>::TOTAL, tile_slots(g.in, 2 * TILE) * g.in.heads, at, m, g) ? 1 : -1;
+  return launch_mma(k_attention_mma<BF16, DP>, table, FWD_CTA, FwdLayout<DP>::TOTAL, tile_slots(g.in, 2 * TILE) * g.in.heads, at, m, g) ? 1 : -1;
 }
 template <bool BF16, int DP> int bwd_mma(const TrainScratch& ws, const Maps& m, const adacgd_attention_backward_args& g, const Where& at) {
   static std::atomic<int> table[2][TRAIN_DEVICES];
@@ -870,8 +859,8 @@ template <bool BF16, int DP> int bwd_mma(const TrainScratch& ws, const Maps& m, 
     k_attention_dot<<<parts, DOT_CTA, 0, at.stream>>>(g, most);
     if (cudaGetLastError() != cudaSuccess) return -1;
   }
-  if (!launch_mma(k_attention_dq_mma<BF16, DP>, table[0], DqLayout<DP>::TOTAL, slots * g.in.heads, at, m, g, (const float*)most, parts)) return -1;
-  if (!launch_mma(k_attention_dkv_mma<BF16, DP>, table[1], DkvLayout<DP>::TOTAL, slots * g.in.key_heads, at, m, g, (const float*)most, parts)) return -1;
+  if (!launch_mma(k_attention_dq_mma<BF16, DP>, table[0], BWD_CTA, DqLayout<DP>::TOTAL, slots * g.in.heads, at, m, g, (const float*)most, parts)) return -1;
+  if (!launch_mma(k_attention_dkv_mma<BF16, DP>, table[1], BWD_CTA, DkvLayout<DP>::TOTAL, slots * g.in.key_heads, at, m, g, (const float*)most, parts)) return -1;
   return BF16 ? 2 : 3;
 }
 
