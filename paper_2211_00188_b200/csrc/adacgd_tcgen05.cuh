@@ -26,30 +26,26 @@ __device__ __forceinline__ bool mbar_try(u32 bar, u32 parity) {
       : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ u64 now_ns() {
-  u64 t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
-// Waits for the phase with this parity, for two seconds at most: nothing here takes a thousandth of that, so a wait that runs out means that
-// the kernel is wrong.  It then says so in `dead`, on which all the CTA's waits give up.
-constexpr u64 WAIT_NS = 2000000000ull;
-__device__ __forceinline__ bool mbar_wait_long(u32 bar, u32 parity, volatile int* dead) {
-  const u64 begin = now_ns();
+// Waits for the phase with this parity, for about two seconds at most: nothing here takes a thousandth of that, so a wait that runs out means
+// that the kernel is wrong.  It then says so in `dead`, on which all the CTA's waits give up.
+constexpr long long WAIT_CLOCKS = 4000000000ll;
+__device__ __forceinline__ bool mbar_wait(u32 bar, u32 parity, volatile int* dead) {
+  if (mbar_try(bar, parity)) return true;
+  const long long begin = clock64();
+#pragma unroll 1
   for (;;) {
-    if (mbar_try(bar, parity)) return true;
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try(bar, parity)) return true;
     if (dead && *dead) return false;
-    if (now_ns() - begin > WAIT_NS) break;
+    if (clock64() - begin > WAIT_CLOCKS) break;
   }
   if (dead) *dead = 1;
   return false;
 }
-__device__ __forceinline__ bool mbar_wait(u32 bar, u32 parity, volatile int* dead) {
-#pragma unroll 1
-  for (int i = 0; i < 16; ++i)
-    if (mbar_try(bar, parity)) return true;
-  return mbar_wait_long(bar, parity, dead);
-}
+
+// The same by a whole warp, which stays together.
+__device__ __forceinline__ bool mbar_wait_warp(u32 bar, u32 parity, volatile int* dead) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, dead)); }
 
 // ---- tensor copies ----
 __device__ __forceinline__ void tma_load_3d(u32 dst, const CUtensorMap* map, int x, int y, int z, u32 bar) {
@@ -117,21 +113,31 @@ __device__ __forceinline__ u64 operand(u32 addr, u32 chunk) {
 __host__ __device__ constexpr u32 product_of(bool bf16, int n, bool b_mn_major) {
   return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (b_mn_major ? 1u : 0u) << 16 | (u32)(n >> 3) << 17 | (u32)(128 >> 4) << 24;
 }
-__device__ __forceinline__ void mma_ss(u32 d, u64 a, u64 b, u32 what, bool add) {
+// One lane issues; the warp stays together and `leader` is a predicate, so that addresses and descriptions stay in uniform registers.  (With
+// the products inside a branch of one lane every operand was moved there first, and issuing took longer than the products.)
+__device__ __forceinline__ u32 elect_leader() {
+  u32 r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void mma_ss(u32 leader, u32 d, u64 a, u64 b, u32 what, bool add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
-      "r"(what), "r"((u32)add)
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::
+          "r"(d), "l"(a), "l"(b), "r"(what), "r"((u32)add), "r"(leader)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(u32 d, u32 a, u64 b, u32 what, bool add) {
+__device__ __forceinline__ void mma_ts(u32 leader, u32 d, u32 a, u64 b, u32 what, bool add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b),
-      "r"(what), "r"((u32)add)
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::
+          "r"(d), "r"(a), "l"(b), "r"(what), "r"((u32)add), "r"(leader)
       : "memory");
 }
 // Arrives at the barrier when all products that this thread has issued are done.
-__device__ __forceinline__ void mma_commit(u32 bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void mma_commit(u32 leader, u32 bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(leader)
+      : "memory");
 }
 
 // ---- pairs of 16-bit numbers ----

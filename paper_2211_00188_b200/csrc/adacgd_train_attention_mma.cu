@@ -70,21 +70,21 @@ __device__ __forceinline__ bool bring(u32 dst, const CUtensorMap* map, int head,
 // After a wait that ran out: the copies under way must have ended before the CTA's memory goes to another.
 __device__ __forceinline__ void settle(u32 bar, u32 parity) { mbar_wait(bar, parity, nullptr); }
 
-// ---- the product thread ----
+// ---- the product warp ----
 // d = a b^T over 16 * STEPS columns of both tiles.
-template <bool BF16, int DP> __device__ __forceinline__ void product_nt(u32 d, u32 a, u32 b) {
+template <bool BF16, int DP> __device__ __forceinline__ void product_nt(u32 leader, u32 d, u32 a, u32 b) {
 #pragma unroll
   for (int k = 0; k < DP / 16; ++k) {
     const u32 off = (k / 4) * HALF + (k % 4) * 32;
-    mma_ss(d, operand(a + off, 16), operand(b + off, 16), product_of(BF16, TILE, false), k > 0);
+    mma_ss(leader, d, operand(a + off, 16), operand(b + off, 16), product_of(BF16, TILE, false), k > 0);
   }
 }
 // d [128 x DP] += p tile, p in tensor memory: 16 rows of the tile a step.  p was put in the place of 128 columns of scores, by parts of
 // them: 16 PER numbers in the first half of a part's columns.
-template <bool BF16, int DP, int PER> __device__ __forceinline__ void product_pn(u32 d, u32 p, u32 tile, bool add) {
+template <bool BF16, int DP, int PER> __device__ __forceinline__ void product_pn(u32 leader, u32 d, u32 p, u32 tile, bool add) {
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    mma_ts(d, p + (k / PER) * PER * 16 + (k % PER) * 8, operand(tile + k * 2048, HALF), product_of(BF16, DP, true), add || k > 0);
+    mma_ts(leader, d, p + (k / PER) * PER * 16 + (k % PER) * 8, operand(tile + k * 2048, HALF), product_of(BF16, DP, true), add || k > 0);
 }
 
 // ---- rows of results ----
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
   const u32 q_full = bars, aside = bars + 8, s_full = bars + 16, p_full = bars + 32, o_full = bars + 48, full = bars + 64, empty = full + 8 * L::STAGES;
   u32* const tmem_at = reinterpret_cast<u32*>(mma_smem + L::BARS + 64 + 16 * L::STAGES);
   volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
     mbar_init(aside, 1);
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const u32 tmem = *tmem_at;
+  const u32 tmem = __shfl_sync(0xffffffffu, *tmem_at, 0);
   const int kh = head / (a.heads / a.key_heads);
   const int tiles = (t.length + TILE - 1) / TILE;              // of keys
   int count[2];                                                // that A and B meet
@@ -189,35 +189,36 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
         for (int b = max(0, i - L::STAGES); b < i; ++b) settle(full + 8 * (b % L::STAGES), (b / L::STAGES) & 1);
       }
     } else if (warp == FWD_ROWS) {
-      if (lane == 0) {
-        bool ok = mbar_wait(q_full, 0, dead);
+      {
+      const u32 leader = elect_leader();
+        bool ok = mbar_wait_warp(q_full, 0, dead);
         for (int j = 0; ok && j <= n; ++j) {
           const int ik = 2 * j, iv = 2 * j - 1, sk = ik % L::STAGES, sv = iv % L::STAGES;
-          if (j < n && !(ok = mbar_wait(full + 8 * sk, (ik / L::STAGES) & 1, dead))) break;
-          if (j > 0 && !(ok = mbar_wait(full + 8 * sv, (iv / L::STAGES) & 1, dead))) break;
+          if (j < n && !(ok = mbar_wait_warp(full + 8 * sk, (ik / L::STAGES) & 1, dead))) break;
+          if (j > 0 && !(ok = mbar_wait_warp(full + 8 * sv, (iv / L::STAGES) & 1, dead))) break;
           for (int x = 0; ok && x < 2; ++x) {
             const int u = j - (n - count[x]);                    // the step as x counts
             if (u < 0 || count[x] == 0) continue;
             const u32 s = tmem + x * TILE, o = tmem + 2 * TILE + x * DP;
             if (u > 0) {
-              if (!(ok = mbar_wait(p_full + 8 * x, (u - 1) & 1, dead))) break;
+              if (!(ok = mbar_wait_warp(p_full + 8 * x, (u - 1) & 1, dead))) break;
               tc_fence_after();
-              product_pn<BF16, DP, 8>(o, s, base + L::RING + sv * L::BYTES, u > 1);
+              product_pn<BF16, DP, 8>(leader, o, s, base + L::RING + sv * L::BYTES, u > 1);
             }
             if (j < n) {
               tc_fence_after();
-              product_nt<BF16, DP>(s, base + x * L::BYTES, base + L::RING + sk * L::BYTES);
-              mma_commit(s_full + 8 * x);
+              product_nt<BF16, DP>(leader, s, base + x * L::BYTES, base + L::RING + sk * L::BYTES);
+              mma_commit(leader, s_full + 8 * x);
             } else {
-              mma_commit(o_full + 8 * x);
+              mma_commit(leader, o_full + 8 * x);
             }
           }
           if (!ok) break;
-          if (j < n) mma_commit(empty + 8 * sk);
-          if (j > 0) mma_commit(empty + 8 * sv);
+          if (j < n) mma_commit(leader, empty + 8 * sk);
+          if (j > 0) mma_commit(leader, empty + 8 * sv);
         }
         if (*dead) {
-          mma_commit(aside);                                     // nobody else uses it any more, or its wait has run out too
+          mma_commit(leader, aside);                                     // nobody else uses it any more, or its wait has run out too
           settle(aside, 0);
         }
       }
@@ -426,7 +427,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
   u32* const tmem_at = reinterpret_cast<u32*>(mma_smem + L::BARS + 64 + 16 * (L::KS + L::VS));
   volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
   float* const part = reinterpret_cast<float*>(mma_smem + L::PART);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
     mbar_init(aside, 1);
@@ -450,7 +451,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const u32 tmem = *tmem_at, dp_at = tmem + 2 * TILE, dq_at = tmem + 3 * TILE;
+  const u32 tmem = __shfl_sync(0xffffffffu, *tmem_at, 0), dp_at = tmem + 2 * TILE, dq_at = tmem + 3 * TILE;
   const u32 q_tile = base, do_tile = base + L::BYTES, k_tiles = base + L::RING, v_tiles = k_tiles + L::KS * L::BYTES;
   const int kh = head / (a.heads / a.key_heads), tiles = (t.length + TILE - 1) / TILE;
   const int n = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
@@ -478,36 +479,37 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
       for (int b = max(0, nv - L::VS); b < nv; ++b) settle(v_full + 8 * (b % L::VS), (b / L::VS) & 1);
     }
   } else if (warp == BWD_ROWS) {
-    if (lane == 0) {
+    {
+      const u32 leader = elect_leader();
       auto scores = [&](int j) {                               // S of step j
         const int st = j % L::KS;
-        if (!mbar_wait(k_full + 8 * st, (j / L::KS) & 1, dead)) return false;
+        if (!mbar_wait_warp(k_full + 8 * st, (j / L::KS) & 1, dead)) return false;
         tc_fence_after();
-        product_nt<BF16, DP>(tmem + (j & 1) * TILE, q_tile, k_tiles + st * L::BYTES);
-        mma_commit(s_full + 8 * (j & 1));
+        product_nt<BF16, DP>(leader, tmem + (j & 1) * TILE, q_tile, k_tiles + st * L::BYTES);
+        mma_commit(leader, s_full + 8 * (j & 1));
         return true;
       };
       auto shares = [&](int j) {                               // dP of step j
         const int st = j % L::VS;
-        if (!mbar_wait(v_full + 8 * st, (j / L::VS) & 1, dead)) return false;
+        if (!mbar_wait_warp(v_full + 8 * st, (j / L::VS) & 1, dead)) return false;
         tc_fence_after();
-        product_nt<BF16, DP>(dp_at, do_tile, v_tiles + st * L::BYTES);
-        mma_commit(dp_full);
-        mma_commit(v_empty + 8 * st);
+        product_nt<BF16, DP>(leader, dp_at, do_tile, v_tiles + st * L::BYTES);
+        mma_commit(leader, dp_full);
+        mma_commit(leader, v_empty + 8 * st);
         return true;
       };
-      bool ok = mbar_wait(q_full, 0, dead) && scores(0) && shares(0) && (n < 2 || scores(1));
+      bool ok = mbar_wait_warp(q_full, 0, dead) && scores(0) && shares(0) && (n < 2 || scores(1));
       for (int j = 0; ok && j < n; ++j) {
-        if (!mbar_wait(ds_full, j & 1, dead)) break;
+        if (!mbar_wait_warp(ds_full, j & 1, dead)) break;
         tc_fence_after();
         if (j + 1 < n && !shares(j + 1)) break;
-        product_pn<BF16, DP, 2>(dq_at, tmem + (j & 1) * TILE, k_tiles + (j % L::KS) * L::BYTES, j > 0);
-        mma_commit(k_empty + 8 * (j % L::KS));
-        if (j + 1 == n) mma_commit(dq_full);
+        product_pn<BF16, DP, 2>(leader, dq_at, tmem + (j & 1) * TILE, k_tiles + (j % L::KS) * L::BYTES, j > 0);
+        mma_commit(leader, k_empty + 8 * (j % L::KS));
+        if (j + 1 == n) mma_commit(leader, dq_full);
         if (j + 2 < n && !scores(j + 2)) break;
       }
       if (*dead) {
-        mma_commit(aside);
+        mma_commit(leader, aside);
         settle(aside, 0);
       }
     }
@@ -624,7 +626,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   u32* const tmem_at = reinterpret_cast<u32*>(mma_smem + L::BARS + 56 + 16 * L::STAGES);
   volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
   float* const stats = reinterpret_cast<float*>(mma_smem + L::STATS);   // [2 steps][-lse log2 e, -row_dot][128], scaled as p and ds are
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     mbar_init(kv_full, 1);
     mbar_init(aside, 1);
@@ -644,7 +646,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const u32 tmem = *tmem_at, dp_at = tmem + TILE, dv_at = tmem + 2 * TILE, dk_at = dv_at + DP;
+  const u32 tmem = __shfl_sync(0xffffffffu, *tmem_at, 0), dp_at = tmem + TILE, dv_at = tmem + 2 * TILE, dk_at = dv_at + DP;
   const u32 k_tile = base, v_tile = base + L::BYTES, ring = base + L::RING;
   // binary16: p is taken 2^14 times larger, ds by its range (see above)
   const float range = BF16 ? 1.f : range_of(most, parts), shift = BF16 ? 0.f : 14.f, back = BF16 ? 1.f : 6.103515625e-05f;
@@ -683,38 +685,39 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
       for (int b = max(0, i - L::STAGES); b < i; ++b) settle(full + 8 * (b % L::STAGES), (b / L::STAGES) & 1);
     }
   } else if (warp == BWD_ROWS) {
-    if (lane == 0) {
+    {
+      const u32 leader = elect_leader();
       auto tile = [&](int i) { return ring + (i % L::STAGES) * L::BYTES; };
       auto scores = [&](int j) {
-        if (!mbar_wait(full + 8 * (2 * j % L::STAGES), (2 * j / L::STAGES) & 1, dead)) return false;
+        if (!mbar_wait_warp(full + 8 * (2 * j % L::STAGES), (2 * j / L::STAGES) & 1, dead)) return false;
         tc_fence_after();
-        product_nt<BF16, DP>(tmem, k_tile, tile(2 * j));
-        mma_commit(s_full);
+        product_nt<BF16, DP>(leader, tmem, k_tile, tile(2 * j));
+        mma_commit(leader, s_full);
         return true;
       };
       auto shares = [&](int j) {
-        if (!mbar_wait(full + 8 * ((2 * j + 1) % L::STAGES), ((2 * j + 1) / L::STAGES) & 1, dead)) return false;
+        if (!mbar_wait_warp(full + 8 * ((2 * j + 1) % L::STAGES), ((2 * j + 1) / L::STAGES) & 1, dead)) return false;
         tc_fence_after();
-        product_nt<BF16, DP>(dp_at, v_tile, tile(2 * j + 1));
-        mma_commit(dp_full);
+        product_nt<BF16, DP>(leader, dp_at, v_tile, tile(2 * j + 1));
+        mma_commit(leader, dp_full);
         return true;
       };
-      bool ok = mbar_wait(kv_full, 0, dead) && scores(0) && shares(0);
+      bool ok = mbar_wait_warp(kv_full, 0, dead) && scores(0) && shares(0);
       for (int j = 0; ok && j < n; ++j) {
-        if (!mbar_wait(p_full, j & 1, dead)) break;
+        if (!mbar_wait_warp(p_full, j & 1, dead)) break;
         tc_fence_after();
-        product_pn<BF16, DP, 2>(dv_at, tmem, tile(2 * j + 1), j > 0);
-        mma_commit(empty + 8 * ((2 * j + 1) % L::STAGES));
+        product_pn<BF16, DP, 2>(leader, dv_at, tmem, tile(2 * j + 1), j > 0);
+        mma_commit(leader, empty + 8 * ((2 * j + 1) % L::STAGES));
         if (j + 1 < n && !scores(j + 1)) break;
-        if (!mbar_wait(ds_full, j & 1, dead)) break;
+        if (!mbar_wait_warp(ds_full, j & 1, dead)) break;
         tc_fence_after();
-        product_pn<BF16, DP, 2>(dk_at, dp_at, tile(2 * j), j > 0);
-        mma_commit(empty + 8 * (2 * j % L::STAGES));
+        product_pn<BF16, DP, 2>(leader, dk_at, dp_at, tile(2 * j), j > 0);
+        mma_commit(leader, empty + 8 * (2 * j % L::STAGES));
         if (j + 1 < n && !shares(j + 1)) break;
       }
-      if (!*dead) mma_commit(end_full);
+      if (!*dead) mma_commit(leader, end_full);
       else {
-        mma_commit(aside);
+        mma_commit(leader, aside);
         settle(aside, 0);
       }
     }
