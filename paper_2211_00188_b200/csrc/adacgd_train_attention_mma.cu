@@ -11,6 +11,8 @@
 //
 // The backward pass is two kernels that each compute the scores again, seven products for the five that are needed: every sum stays in one
 // CTA's tensor memory, without atomics, and dq needs no binary32 array.
+#include <type_traits>
+
 #include "adacgd_tcgen05.cuh"
 #include "adacgd_train_attention.cuh"
 
@@ -112,6 +114,45 @@ __device__ __forceinline__ void poison_row(void* base, long long stride, long lo
   unsigned short* const to = (unsigned short*)base + row * stride + (long long)head * dim;
   for (int d = 0; d < dim; ++d) to[d] = 0x7fff;
 }
+
+// 2^x of a pair on the multiplying units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 with the least relative error on
+// [-1/2, 1/2] (2.7e-6, computed by exchange; its mean is 4e-8), 2^n as a factor so that NaN stays NaN.  Below 2^-126 the result is 2^-126.
+__device__ __forceinline__ float at_least(float x, float low) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(low));
+  return r;
+}
+__device__ __forceinline__ F2 exp2_by_products(float x0, float x1) {
+  const float big = 12582912.f;                                // 1.5 2^23: adding it rounds to an integer, in the low bits of the sum
+  const F2 x = f2(at_least(x0, -126.f), at_least(x1, -126.f)), t = add2(x, f2(big, big)), n = add2(t, f2(-big, -big));
+  const F2 f = fma2(n, f2(-1.f, -1.f), x);
+  F2 y = fma2(f2(0x1.3997d6p-7f, 0x1.3997d6p-7f), f, f2(0x1.ca1440p-5f, 0x1.ca1440p-5f));
+  y = fma2(y, f, f2(0x1.ec06dap-3f, 0x1.ec06dap-3f));
+  y = fma2(y, f, f2(0x1.62e0dcp-1f, 0x1.62e0dcp-1f));
+  y = fma2(y, f, f2(0x1.ffffe8p-1f, 0x1.ffffe8p-1f));
+  float t0, t1;
+  split(t, t0, t1);
+  return mul2(y, f2(__uint_as_float((__float_as_uint(t0) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t1) << 23) + 0x3f800000u)));
+}
+// 2^x of the pair with this number: the hardware's function gives four a clock and scheduler, which is half of the products' pace, so three pairs
+// of eight take the other way.
+template <bool MIXED> __device__ __forceinline__ F2 exp2_pair(F2 x, int number) {
+  float a, b;
+  split(x, a, b);
+  const int i = MIXED ? number & 7 : 0;
+  return i == 1 || i == 4 || i == 6 ? exp2_by_products(a, b) : f2(ex2(a), ex2(b));
+}
+
+typedef std::integral_constant<bool, false> No;
+typedef std::integral_constant<bool, true> Yes;
+#ifndef FWDMIX
+#define FWDMIX true
+#endif
+#ifndef BWDMIX
+#define BWDMIX true
+#endif
+typedef std::integral_constant<bool, FWDMIX> FwdMixed;
+typedef std::integral_constant<bool, BWDMIX> BwdMixed;
 
 __device__ __forceinline__ u32 low_bits(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
 
@@ -281,20 +322,23 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
       const float low = (top == -INFINITY ? 0.f : -top * c) + (BF16 ? 0.f : 7.f);
       const F2 c2 = f2(c, c), low2 = f2(low, low);
       F2 sum2 = f2(sum, 0.f);
+      auto shares = [&](auto mixed) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        u32 p[16];
+        for (int w = 0; w < 4; ++w) {
+          u32 p[16];
 #pragma unroll
-        for (int k = 0; k < 32; k += 2) {
-          float y0, y1;
-          split(fma2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), c2, low2), y0, y1);
-          y0 = ex2(y0);
-          y1 = ex2(y1);
-          sum2 = add2(sum2, f2(y0, y1));
-          p[k / 2] = pack2<BF16>(y0, y1);
+          for (int k = 0; k < 32; k += 2) {
+            const F2 y = exp2_pair<decltype(mixed)::value>(fma2(f2(__uint_as_float(s[w][k]), __uint_as_float(s[w][k + 1])), c2, low2), k / 2);
+            float y0, y1;
+            split(y, y0, y1);
+            sum2 = add2(sum2, y);
+            p[k / 2] = pack2<BF16>(y0, y1);
+          }
+          tmem_st16(s_at + 16 * w, p);
         }
-        tmem_st16(s_at + 16 * w, p);
-      }
+      };
+      if (mask) shares(No{});                                  // what is hidden has to be exactly zero
+      else shares(FwdMixed{});
       float e0, e1;
       split(sum2, e0, e1);
       sum = e0 + e1;
@@ -560,28 +604,28 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
       tmem_hold(s);
       F2 p[16];
 #pragma unroll
-      for (int k = 0; k < 32; k += 2) {
-        float y0, y1;
-        split(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, low2), y0, y1);
-        p[k / 2] = f2(ex2(y0), ex2(y1));
-      }
+      for (int k = 0; k < 32; k += 2) p[k / 2] = exp2_pair<BwdMixed::value>(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, low2), k / 2);
       if (!(ok = mbar_wait(dp_full, j & 1, dead))) break;
       tc_fence_after();
       tmem_ld32(dp_at + 32 * part_of + lanes, s);
       tmem_wait_ld();
       tmem_hold(s);
       u32 ds[16];
+      auto products = [&](auto masked) {
 #pragma unroll
-      for (int k = 0; k < 32; k += 2) {
-        float y0, y1;
-        const F2 dp = f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1]));
-        split(mul2(p[k / 2], BF16 ? add2(dp, dot2) : fma2(dp, range2, dot2)), y0, y1);
-        if (mask) {
-          y0 = bits >> k & 1 ? y0 : 0.f;
-          y1 = bits >> (k + 1) & 1 ? y1 : 0.f;
+        for (int k = 0; k < 32; k += 2) {
+          float y0, y1;
+          const F2 dp = f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1]));
+          split(mul2(p[k / 2], BF16 ? add2(dp, dot2) : fma2(dp, range2, dot2)), y0, y1);
+          if (decltype(masked)::value) {
+            y0 = bits >> k & 1 ? y0 : 0.f;
+            y1 = bits >> (k + 1) & 1 ? y1 : 0.f;
+          }
+          ds[k / 2] = pack2<BF16>(y0, y1);
         }
-        ds[k / 2] = pack2<BF16>(y0, y1);
-      }
+      };
+      if (mask) products(Yes{});
+      else products(No{});
       tmem_st16(s_at, ds);
       tmem_wait_st();
       tc_fence_before();
@@ -741,28 +785,28 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
       tmem_hold(s);
       F2 p[16];
       u32 w16[16];
+      auto shares = [&](auto masked) {
 #pragma unroll
-      for (int k = 0; k < 32; k += 4) {
-        const float4 l = *reinterpret_cast<const float4*>(low + k);
-        float y0, y1, y2, y3;
-        split(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, f2(l.x, l.y)), y0, y1);
-        split(fma2(f2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, f2(l.z, l.w)), y2, y3);
-        y0 = ex2(y0);
-        y1 = ex2(y1);
-        y2 = ex2(y2);
-        y3 = ex2(y3);
-        if (mask) {
-          const int q = first + k;
-          y0 = q >= i ? y0 : 0.f;
-          y1 = q + 1 >= i ? y1 : 0.f;
-          y2 = q + 2 >= i ? y2 : 0.f;
-          y3 = q + 3 >= i ? y3 : 0.f;
+        for (int k = 0; k < 32; k += 4) {
+          const float4 l = *reinterpret_cast<const float4*>(low + k);
+          float y0, y1, y2, y3;
+          split(exp2_pair<BwdMixed::value>(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, f2(l.x, l.y)), k / 2), y0, y1);
+          split(exp2_pair<BwdMixed::value>(fma2(f2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, f2(l.z, l.w)), k / 2 + 1), y2, y3);
+          if (decltype(masked)::value) {
+            const int q = first + k;
+            y0 = q >= i ? y0 : 0.f;
+            y1 = q + 1 >= i ? y1 : 0.f;
+            y2 = q + 2 >= i ? y2 : 0.f;
+            y3 = q + 3 >= i ? y3 : 0.f;
+          }
+          p[k / 2] = f2(y0, y1);
+          p[k / 2 + 1] = f2(y2, y3);
+          w16[k / 2] = pack2<BF16>(y0, y1);
+          w16[k / 2 + 1] = pack2<BF16>(y2, y3);
         }
-        p[k / 2] = f2(y0, y1);
-        p[k / 2 + 1] = f2(y2, y3);
-        w16[k / 2] = pack2<BF16>(y0, y1);
-        w16[k / 2 + 1] = pack2<BF16>(y2, y3);
-      }
+      };
+      if (mask) shares(Yes{});
+      else shares(No{});
       tmem_st16(s_at, w16);
       tmem_wait_st();
       tc_fence_before();
