@@ -134,25 +134,23 @@ __device__ __forceinline__ F2 exp2_by_products(float x0, float x1) {
   split(t, t0, t1);
   return mul2(y, f2(__uint_as_float((__float_as_uint(t0) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t1) << 23) + 0x3f800000u)));
 }
-// 2^x of the pair with this number: the hardware's function gives four a clock and scheduler, which is half of the products' pace, so three pairs
-// of eight take the other way.
-template <bool MIXED> __device__ __forceinline__ F2 exp2_pair(F2 x, int number) {
+__device__ __forceinline__ F2 exp2_pair(F2 x) {
   float a, b;
   split(x, a, b);
+  return f2(ex2(a), ex2(b));
+}
+// The pair with this number of a row: the hardware's function gives four a clock and scheduler, half of the products' pace, so in the
+// forward pass three pairs of eight take the other way (453 -> 443 us; backward there was nothing in it).
+template <bool MIXED> __device__ __forceinline__ F2 exp2_pair(F2 x, int number) {
   const int i = MIXED ? number & 7 : 0;
-  return i == 1 || i == 4 || i == 6 ? exp2_by_products(a, b) : f2(ex2(a), ex2(b));
+  if (i != 1 && i != 4 && i != 6) return exp2_pair(x);
+  float a, b;
+  split(x, a, b);
+  return exp2_by_products(a, b);
 }
 
 typedef std::integral_constant<bool, false> No;
 typedef std::integral_constant<bool, true> Yes;
-#ifndef FWDMIX
-#define FWDMIX true
-#endif
-#ifndef BWDMIX
-#define BWDMIX true
-#endif
-typedef std::integral_constant<bool, FWDMIX> FwdMixed;
-typedef std::integral_constant<bool, BWDMIX> BwdMixed;
 
 __device__ __forceinline__ u32 low_bits(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
 
@@ -338,7 +336,7 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
         }
       };
       if (mask) shares(No{});                                  // what is hidden has to be exactly zero
-      else shares(FwdMixed{});
+      else shares(Yes{});
       float e0, e1;
       split(sum2, e0, e1);
       sum = e0 + e1;
@@ -604,7 +602,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
       tmem_hold(s);
       F2 p[16];
 #pragma unroll
-      for (int k = 0; k < 32; k += 2) p[k / 2] = exp2_pair<BwdMixed::value>(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, low2), k / 2);
+      for (int k = 0; k < 32; k += 2) p[k / 2] = exp2_pair(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, low2));
       if (!(ok = mbar_wait(dp_full, j & 1, dead))) break;
       tc_fence_after();
       tmem_ld32(dp_at + 32 * part_of + lanes, s);
@@ -647,10 +645,12 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
 // --------------------------------------------------------------------------
 // backward: dk and dv
 // --------------------------------------------------------------------------
-// A CTA takes a tile of keys and walks over the tiles of queries, of all the heads that share it: S^T = K Q^T, p^T in its place, dV += p^T dO;
-// dP^T = V dO^T, ds^T in its place, dK += ds^T Q.  Transposed, both probabilities and ds are operands as they lie in tensor
-// memory, and Q and dO serve as they were brought, once by rows and once by columns.  The rows' log sums and products lie in shared memory, where all threads
-// read the same ones.  Products go in the order dV(i) S(i+1) dK(i) dP(i+1): while the first two run, ds(i) is made, during the others p(i+1).
+// A CTA takes a tile of keys and walks over the tiles of queries, of all the heads that share it: S^T = K Q^T, dP^T = V dO^T, then p^T and ds^T
+// side by side in dP's place, dV += p^T dO, dK += ds^T Q.  Transposed, p and ds are operands as they lie in tensor memory, and Q and dO
+// serve as they were brought, once by rows and once by columns.  The rows' log sums and products lie in shared memory, where all threads
+// read the same ones.  p waits in registers until dP has been read: so the next S is formed as soon as this one has been, under its exponentials, and
+// the other three products run under those of the next step.  (p in the place of S, as soon as it is known, held the next S back behind dV: 3310 clocks
+// a step, of which the products take 2048.)
 template <int DP> struct DkvLayout {
   static constexpr int BYTES = DP * 256, STAGES = DP == 128 ? 5 : 8, RING = 2 * BYTES, STATS = RING + STAGES * BYTES;
   static constexpr int BARS = STATS + 2 * 2 * TILE * 4, TOTAL = BARS + 256;
@@ -665,7 +665,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   Tile t;
   if (!tile_of(a, blockIdx.x / a.key_heads, TILE, &t)) return;
   const u32 base = smem_addr(mma_smem), bars = base + L::BARS;
-  const u32 kv_full = bars, aside = bars + 8, s_full = bars + 16, dp_full = bars + 24, p_full = bars + 32, ds_full = bars + 40, end_full = bars + 48,
+  const u32 kv_full = bars, aside = bars + 8, s_full = bars + 16, dp_full = bars + 24, s_read = bars + 32, ds_full = bars + 40, end_full = bars + 48,
             full = bars + 56, empty = full + 8 * L::STAGES;
   u32* const tmem_at = reinterpret_cast<u32*>(mma_smem + L::BARS + 56 + 16 * L::STAGES);
   volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
@@ -676,7 +676,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
     mbar_init(aside, 1);
     mbar_init(s_full, 1);
     mbar_init(dp_full, 1);
-    mbar_init(p_full, 32 * BWD_ROWS);
+    mbar_init(s_read, 32 * BWD_ROWS);
     mbar_init(ds_full, 32 * BWD_ROWS);
     mbar_init(end_full, 1);
     for (int i = 0; i < L::STAGES; ++i) {
@@ -748,13 +748,11 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
       };
       bool ok = mbar_wait_warp(kv_full, 0, dead) && scores(0) && shares(0);
       for (int j = 0; ok && j < n; ++j) {
-        if (!mbar_wait_warp(p_full, j & 1, dead)) break;
-        tc_fence_after();
-        product_pn<BF16, DP, 2>(leader, dv_at, tmem, tile(2 * j + 1), j > 0);
-        mma_commit(leader, empty + 8 * ((2 * j + 1) % L::STAGES));
-        if (j + 1 < n && !scores(j + 1)) break;
+        if (j + 1 < n && !(mbar_wait_warp(s_read, j & 1, dead) && scores(j + 1))) break;
         if (!mbar_wait_warp(ds_full, j & 1, dead)) break;
         tc_fence_after();
+        product_pn<BF16, DP, 2>(leader, dv_at, dp_at + 16, tile(2 * j + 1), j > 0);
+        mma_commit(leader, empty + 8 * ((2 * j + 1) % L::STAGES));
         product_pn<BF16, DP, 2>(leader, dk_at, dp_at, tile(2 * j), j > 0);
         mma_commit(leader, empty + 8 * (2 * j % L::STAGES));
         if (j + 1 < n && !shares(j + 1)) break;
@@ -783,15 +781,16 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
       tmem_ld32(s_at, s);
       tmem_wait_ld();
       tmem_hold(s);
+      tc_fence_before();
+      mbar_arrive(s_read);
       F2 p[16];
-      u32 w16[16];
       auto shares = [&](auto masked) {
 #pragma unroll
         for (int k = 0; k < 32; k += 4) {
           const float4 l = *reinterpret_cast<const float4*>(low + k);
           float y0, y1, y2, y3;
-          split(exp2_pair<BwdMixed::value>(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, f2(l.x, l.y)), k / 2), y0, y1);
-          split(exp2_pair<BwdMixed::value>(fma2(f2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, f2(l.z, l.w)), k / 2 + 1), y2, y3);
+          split(exp2_pair(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, f2(l.x, l.y))), y0, y1);
+          split(exp2_pair(fma2(f2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, f2(l.z, l.w))), y2, y3);
           if (decltype(masked)::value) {
             const int q = first + k;
             y0 = q >= i ? y0 : 0.f;
@@ -801,21 +800,23 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
           }
           p[k / 2] = f2(y0, y1);
           p[k / 2 + 1] = f2(y2, y3);
-          w16[k / 2] = pack2<BF16>(y0, y1);
-          w16[k / 2 + 1] = pack2<BF16>(y2, y3);
         }
       };
       if (mask) shares(Yes{});
       else shares(No{});
-      tmem_st16(s_at, w16);
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(p_full);
       if (!(ok = mbar_wait(dp_full, j & 1, dead))) break;
       tc_fence_after();
       tmem_ld32(d_at, s);
       tmem_wait_ld();
       tmem_hold(s);
+      u32 w16[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        float y0, y1;
+        split(p[k], y0, y1);
+        w16[k] = pack2<BF16>(y0, y1);
+      }
+      tmem_st16(d_at + 16, w16);
 #pragma unroll
       for (int k = 0; k < 32; k += 4) {
         const float4 l = *reinterpret_cast<const float4*>(low + TILE + k);
