@@ -27,6 +27,7 @@ struct TrainScratch {
   long long max_tokens, max_cols;
 };
 constexpr int NTRAIN_TICKETS = 64;
+constexpr int ATTENTION_TICKET = 63;   // the losses count from the front
 constexpr int MAX_SMALL_CTAS = 2048;   // of a small policy loss: a row each at most
 
 // Where a call runs.

@@ -23,19 +23,27 @@ struct Tile {
   int length;      // and its rows
   int first;       // the tile's first row within it
 };
-// A tile by its number.  False: there is none.  All threads of a CTA may call it with the same arguments.
+// A tile by its number.  False: there is none.  Called by whole warps with the same arguments: a warp looks at 32 sequences a round.
 __device__ __forceinline__ bool tile_of(const adacgd_attention_inputs& a, long long slot, int B, Tile* t) {
   long long q = 0, tile, lo, hi;
   if (a.seq_start) {
-    long long l = 0, h = a.sequences;                // the last q whose numbers begin at or before the slot
-    while (h - l > 1) {
-      const long long mid = (l + h) >> 1;
-      long long s = a.seq_start[mid];
-      s = s < 0 ? 0 : (s > a.tokens ? a.tokens : s);
-      if (s / B + mid <= slot) l = mid; else h = mid;
+    // a lane holds the start of sequence l + lane * step; in the last round the steps are one and the next lane's is the end
+    long long l = 0, h = a.sequences, start;
+    int m;
+    for (;;) {
+      const long long step = (h - l + 30) / 31, at = l + (threadIdx.x & 31) * step;
+      start = a.seq_start[at < a.sequences ? at : a.sequences];
+      start = start < 0 ? 0 : (start > a.tokens ? a.tokens : start);
+      m = __popc(__ballot_sync(0xffffffffu, at < h && (threadIdx.x & 31) < 31 && start / B + at <= slot));   // the last that begins at or before the slot
+      if (m > 0) --m;
+      if (step == 1) break;
+      l += m * step;
+      h = l + step < h ? l + step : h;
     }
-    q = l;
-    seq_bounds(a.seq_start, q, a.tokens, 0, &lo, &hi);
+    q = l + m;
+    lo = __shfl_sync(0xffffffffu, start, m);
+    hi = __shfl_sync(0xffffffffu, start, m + 1);
+    if (hi < lo) hi = lo;
     tile = slot - (lo / B + q);
   } else {
     const long long each = a.tokens / a.sequences, per = (each + B - 1) / B;

@@ -179,7 +179,13 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
   u32* const tmem_at = reinterpret_cast<u32*>(mma_smem + L::BARS + 64 + 16 * L::STAGES);
   volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) {
+  const int kh = head / (a.heads / a.key_heads);
+  const int tiles = (t.length + TILE - 1) / TILE;              // of keys
+  int count[2];                                                // that A and B meet
+  count[0] = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
+  count[1] = t.first + TILE >= t.length ? 0 : (a.causal ? min(tiles, t.first / TILE + 2) : tiles);
+  const int n = max(count[0], count[1]);
+  if (warp == FWD_ROWS + 1 && lane == 0) {
     mbar_init(q_full, 1);
     mbar_init(aside, 1);
     for (int x = 0; x < 2; ++x) {
@@ -193,34 +199,26 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
     }
     *dead = 0;
     mbar_init_fence();
+    mbar_expect(q_full, (count[1] ? 2 : 1) * L::BYTES);         // the first copies start before the CTA's warps have met
+    copy_tile<DP>(base, &maps.q, head, t.row + t.first, q_full);
+    if (count[1]) copy_tile<DP>(base + L::BYTES, &maps.q, head, t.row + t.first + TILE, q_full);
   }
   if (warp == FWD_ROWS) tmem_alloc(smem_addr(tmem_at), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const u32 tmem = __shfl_sync(0xffffffffu, *tmem_at, 0);
-  const int kh = head / (a.heads / a.key_heads);
-  const int tiles = (t.length + TILE - 1) / TILE;              // of keys
-  int count[2];                                                // that A and B meet
-  count[0] = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
-  count[1] = t.first + TILE >= t.length ? 0 : (a.causal ? min(tiles, t.first / TILE + 2) : tiles);
-  const int n = max(count[0], count[1]);
   // A row's 128 scores are held at once: of the CTA's 384 x 168 registers the row warps get 208 each, the others 88.
   if (warp >= FWD_ROWS) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == FWD_ROWS + 1) {
-      if (lane == 0) {
-        mbar_expect(q_full, (count[1] ? 2 : 1) * L::BYTES);
-        copy_tile<DP>(base, &maps.q, head, t.row + t.first, q_full);
-        if (count[1]) copy_tile<DP>(base + L::BYTES, &maps.q, head, t.row + t.first + TILE, q_full);
-      }
       u32 side = 0, words[4];
       int i = 0;
       bool ok = true;
       for (; ok && i < 2 * n; ++i) {                             // tiles of keys and values in turn, the last ones first
         const int st = i % L::STAGES, first = (n - 1 - i / 2) * TILE;
         if (i >= L::STAGES && !mbar_wait(empty + 8 * st, (i / L::STAGES - 1) & 1, dead)) break;
-        if (!(i & 1)) counted(a, t, first, words);
+        if (i & 1) counted(a, t, first, words);                // only values are summed over
         ok = bring<DP>(base + L::RING + st * L::BYTES, i & 1 ? &maps.v : &maps.k, kh, t.row + first, words, i & 1, full + 8 * st, aside, side, dead);
       }
       if (*dead) {
@@ -365,14 +363,27 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
 // --------------------------------------------------------------------------
 // bfloat16 holds ds as it is.  binary16 would lose what is below 2^-14, and gradients are often that small, so there ds is multiplied by a power
 // of two that brings the largest one possible, |dout_i| (|v_j| + |out_i|) <= 2 max|dout_i| max|v_j|, below 2^14.  This kernel takes those two
-// maxima, a pair a CTA, and the rows' products dout.out; half a warp takes a head's row.
-constexpr int DOT_CTA = 256, DOT_CTAS = 296;
+// maxima, a pair a CTA, and the rows' products dout.out; LPR lanes take a head's row, four rows at a time.
+constexpr int DOT_CTA = 256, DOT_CTAS = NORM_PARTS - 1, DOT_ROWS = 4;
 
-__global__ void __launch_bounds__(DOT_CTA) k_attention_dot(adacgd_attention_backward_args g, float* most) {
+// Row number i as a token (behind the first one) and a head.
+__device__ __forceinline__ void row_of(long long i, int heads, long long* t, int* h) {
+  if (i >> 32) {
+    *t = i / heads;
+    *h = (int)(i % heads);
+  } else {
+    *t = (u32)i / (u32)heads;
+    *h = (int)((u32)i % (u32)heads);
+  }
+}
+
+template <int LPR>
+__global__ void __launch_bounds__(DOT_CTA) k_attention_dot(adacgd_attention_backward_args g, float* most, u32* ticket) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const adacgd_attention_inputs& a = g.in;
-  const int lane = threadIdx.x & 15, d = lane * 8;
+  const int lane = threadIdx.x % LPR, d = lane * 8;
   const bool in = d < a.head_dim;
-  const long long slots = (long long)gridDim.x * (DOT_CTA / 16), slot = (long long)blockIdx.x * (DOT_CTA / 16) + threadIdx.x / 16;
+  constexpr int GROUPS = DOT_CTA / LPR;
   long long lo = 0, hi = a.tokens, unused;
   if (a.seq_start) {                                  // rows of no sequence keep their row_dot and do not count
     seq_bounds(a.seq_start, 0, a.tokens, 0, &lo, &unused);
@@ -380,65 +391,99 @@ __global__ void __launch_bounds__(DOT_CTA) k_attention_dot(adacgd_attention_back
   }
   auto sum = [](float v) {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   };
   float mo = 0.f, mv = 0.f;
   const long long queries = (hi - lo) * a.heads, keys = (hi - lo) * a.key_heads;
-  for (long long i0 = slot - (threadIdx.x / 16 & 1); i0 < queries; i0 += slots) {   // both halves of a warp alike
-    const long long i = i0 + (threadIdx.x / 16 & 1), t = lo + i / a.heads;
-    const int h = (int)(i % a.heads);
-    const bool row = i < queries, on = row && (!a.mask || a.mask[t]);
-    float x[8], y[8], dot = 0.f, sq = 0.f;
-    if (on && in) {
-      unpack(load_run((const __half*)g.dout + t * g.dout_stride + h * a.head_dim + d), x);
-      unpack(load_run((const __half*)g.out + t * g.out_stride + h * a.head_dim + d), y);
+  // a CTA's rows of a round lie side by side
+  for (long long i0 = (long long)blockIdx.x * GROUPS * DOT_ROWS; i0 < queries; i0 += (long long)gridDim.x * GROUPS * DOT_ROWS) {
+    Run<__half> x[DOT_ROWS], y[DOT_ROWS];
+    long long t[DOT_ROWS];
+    int h[DOT_ROWS];
+    bool on[DOT_ROWS];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        dot = fmaf(x[k], y[k], dot);
-        sq = fmaf(x[k], x[k], sq);
+    for (int u = 0; u < DOT_ROWS; ++u) {
+      const long long i = i0 + u * GROUPS + threadIdx.x / LPR;
+      row_of(i < queries ? i : 0, a.heads, &t[u], &h[u]);
+      t[u] += lo;
+      on[u] = i < queries && (!a.mask || a.mask[t[u]]);
+      if (on[u] && in) {
+        x[u] = load_run((const __half*)g.dout + t[u] * g.dout_stride + (long long)h[u] * a.head_dim + d);
+        y[u] = load_run((const __half*)g.out + t[u] * g.out_stride + (long long)h[u] * a.head_dim + d);
       }
     }
-    dot = sum(dot);
-    mo = fmaxf(mo, sum(sq));
-    if (row && lane == 0) g.row_dot[(long long)h * a.tokens + t] = dot;
+#pragma unroll
+    for (int u = 0; u < DOT_ROWS; ++u) {
+      float p[8], q[8], dot = 0.f, sq = 0.f;
+      if (on[u] && in) {
+        unpack(x[u], p);
+        unpack(y[u], q);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          dot = fmaf(p[k], q[k], dot);
+          sq = fmaf(p[k], p[k], sq);
+        }
+      }
+      dot = sum(dot);
+      mo = fmaxf(mo, sum(sq));
+      if (lane == 0 && i0 + u * GROUPS + threadIdx.x / LPR < queries) g.row_dot[(long long)h[u] * a.tokens + t[u]] = dot;
+    }
   }
-  for (long long i0 = slot - (threadIdx.x / 16 & 1); i0 < keys; i0 += slots) {
-    const long long i = i0 + (threadIdx.x / 16 & 1), t = lo + i / a.key_heads;
+  for (long long i0 = (long long)blockIdx.x * GROUPS; i0 < keys; i0 += (long long)gridDim.x * GROUPS) {
+    const long long i = i0 + threadIdx.x / LPR;
+    long long t;
+    int h;
+    row_of(i < keys ? i : 0, a.key_heads, &t, &h);
+    t += lo;
     float x[8], sq = 0.f;
     if (i < keys && in && (!a.mask || a.mask[t])) {
-      unpack(load_run((const __half*)a.v + t * a.v_stride + (i % a.key_heads) * a.head_dim + d), x);
+      unpack(load_run((const __half*)a.v + t * a.v_stride + (long long)h * a.head_dim + d), x);
 #pragma unroll
       for (int k = 0; k < 8; ++k) sq = fmaf(x[k], x[k], sq);
     }
     mv = fmaxf(mv, sum(sq));
   }
-  __shared__ float part[2][DOT_CTA / 16];
+  __shared__ float part[2][GROUPS];
   if (lane == 0) {
-    part[0][threadIdx.x / 16] = mo;
-    part[1][threadIdx.x / 16] = mv;
+    part[0][threadIdx.x / LPR] = mo;
+    part[1][threadIdx.x / LPR] = mv;
   }
   __syncthreads();
+  __shared__ bool last;
   if (threadIdx.x < 2) {
     float m = 0.f;
-    for (int i = 0; i < DOT_CTA / 16; ++i) m = fmaxf(m, part[threadIdx.x][i]);
-    most[2 * blockIdx.x + threadIdx.x] = m;
+    for (int i = 0; i < GROUPS; ++i) m = fmaxf(m, part[threadIdx.x][i]);
+    __stcg(most + 2 + 2 * blockIdx.x + threadIdx.x, m);
+    __threadfence();
   }
-}
-
-// The power of two: called by whole warps.
-__device__ __forceinline__ float range_of(const float* most, int parts) {
-  float mo = 0.f, mv = 0.f;
-  for (int i = threadIdx.x & 31; i < parts; i += 32) {
-    mo = fmaxf(mo, __ldcg(most + 2 * i));
-    mv = fmaxf(mv, __ldcg(most + 2 * i + 1));
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(ticket, 1u) + 1 == gridDim.x;
+  __syncthreads();
+  if (!last || threadIdx.x >= 32) return;                     // the last CTA to finish joins them
+  __threadfence();
+  float a0 = 0.f, a1 = 0.f;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += 32) {
+    const float2 m = __ldcg(reinterpret_cast<const float2*>(most) + 1 + i);
+    a0 = fmaxf(a0, m.x);
+    a1 = fmaxf(a1, m.y);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, o));
-    mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, o));
+    a0 = fmaxf(a0, __shfl_xor_sync(0xffffffffu, a0, o));
+    a1 = fmaxf(a1, __shfl_xor_sync(0xffffffffu, a1, o));
   }
-  const float bound = 2.002f * sqrtf(mo) * sqrtf(mv);
+  if (threadIdx.x == 0) {
+    most[0] = a0;
+    most[1] = a1;
+    *ticket = 0;
+  }
+}
+
+// The power of two.
+__device__ __forceinline__ float range_of(const float* most) {
+  const float2 m = __ldcg(reinterpret_cast<const float2*>(most));
+  const float bound = 2.002f * sqrtf(m.x) * sqrtf(m.y);
   if (!(bound > 0.f) || isinf(bound)) return 1.f;
   return __int_as_float(((int)fminf(fmaxf(13.f - floorf(log2f(bound)), -60.f), 60.f) + 127) << 23);
 }
@@ -456,11 +501,12 @@ template <int DP> struct DqLayout {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most, int parts) {
+__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most) {
   typedef DqLayout<DP> L;
   extern __shared__ __align__(1024) unsigned char mma_smem[];
   const adacgd_attention_inputs& a = g.in;
   const int head = (int)(blockIdx.x % a.heads);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Tile t;
   if (!tile_of(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, TILE, &t)) return;
   const u32 base = smem_addr(mma_smem), bars = base + L::BARS;
@@ -470,7 +516,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
   volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
   float* const part = reinterpret_cast<float*>(mma_smem + L::PART);
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) {
+  if (warp == BWD_ROWS + 1 && lane == 0) {
     mbar_init(q_full, 1);
     mbar_init(aside, 1);
     mbar_init(s_full, 1);
@@ -488,6 +534,9 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
     }
     *dead = 0;
     mbar_init_fence();
+    mbar_expect(q_full, 2 * L::BYTES);                         // the first copies start before the CTA's warps have met
+    copy_tile<DP>(base, &maps.q, head, t.row + t.first, q_full);
+    copy_tile<DP>(base + L::BYTES, &maps.dout, head, t.row + t.first, q_full);
   }
   if (warp == BWD_ROWS) tmem_alloc(smem_addr(tmem_at), 512);
   tc_fence_before();
@@ -498,11 +547,6 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
   const int kh = head / (a.heads / a.key_heads), tiles = (t.length + TILE - 1) / TILE;
   const int n = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
   if (warp == BWD_ROWS + 1) {
-    if (lane == 0) {
-      mbar_expect(q_full, 2 * L::BYTES);
-      copy_tile<DP>(q_tile, &maps.q, head, t.row + t.first, q_full);
-      copy_tile<DP>(do_tile, &maps.dout, head, t.row + t.first, q_full);
-    }
     u32 side = 0, words[4];
     int nk = 0, nv = 0;
     for (int j = 0; j < n; ++j) {
@@ -578,8 +622,10 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
       dot = (part[r] + part[TILE + r]) + (part[2 * TILE + r] + part[3 * TILE + r]);
       if (part_of == 0 && inside) g.row_dot[at] = dot;
     } else {
-      range = range_of(most, parts);
-      if (on) dot = __ldcg(g.row_dot + at) * range;
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      if (on) dot = __ldcg(g.row_dot + at);
+      range = range_of(most);
+      dot *= range;
     }
     const float low = on ? -g.lse[at] * LOG2E : -INFINITY, c = a.scale * LOG2E;
     const F2 c2 = f2(c, c), low2 = f2(low, low), dot2 = f2(-dot, -dot), range2 = f2(range, range);
@@ -657,13 +703,16 @@ template <int DP> struct DkvLayout {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most, int parts) {
+__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most) {
   typedef DkvLayout<DP> L;
   extern __shared__ __align__(1024) unsigned char mma_smem[];
   const adacgd_attention_inputs& a = g.in;
   const int kh = (int)(blockIdx.x % a.key_heads), group = a.heads / a.key_heads;
   Tile t;
-  if (!tile_of(a, blockIdx.x / a.key_heads, TILE, &t)) return;
+  if (!tile_of(a, blockIdx.x / a.key_heads, TILE, &t)) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");           // this kernel ends after the one before it, whatever there is to do
+    return;
+  }
   const u32 base = smem_addr(mma_smem), bars = base + L::BARS;
   const u32 kv_full = bars, aside = bars + 8, s_full = bars + 16, dp_full = bars + 24, s_read = bars + 32, ds_full = bars + 40, end_full = bars + 48,
             full = bars + 56, empty = full + 8 * L::STAGES;
@@ -671,7 +720,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
   float* const stats = reinterpret_cast<float*>(mma_smem + L::STATS);   // [2 steps][-lse log2 e, -row_dot][128], scaled as p and ds are
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) {
+  if (warp == BWD_ROWS + 1 && lane == 0) {
     mbar_init(kv_full, 1);
     mbar_init(aside, 1);
     mbar_init(s_full, 1);
@@ -685,6 +734,9 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
     }
     *dead = 0;
     mbar_init_fence();
+    mbar_expect(kv_full, 2 * L::BYTES);                        // the first copies start before the CTA's warps have met
+    copy_tile<DP>(base, &maps.k, kh, t.row + t.first, kv_full);
+    copy_tile<DP>(base + L::BYTES, &maps.v, kh, t.row + t.first, kv_full);
   }
   if (warp == BWD_ROWS) tmem_alloc(smem_addr(tmem_at), 512);
   tc_fence_before();
@@ -693,17 +745,13 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   const u32 tmem = __shfl_sync(0xffffffffu, *tmem_at, 0), dp_at = tmem + TILE, dv_at = tmem + 2 * TILE, dk_at = dv_at + DP;
   const u32 k_tile = base, v_tile = base + L::BYTES, ring = base + L::RING;
   // binary16: p is taken 2^14 times larger, ds by its range (see above)
-  const float range = BF16 ? 1.f : range_of(most, parts), shift = BF16 ? 0.f : 14.f, back = BF16 ? 1.f : 6.103515625e-05f;
+  const float shift = BF16 ? 0.f : 14.f, back = BF16 ? 1.f : 6.103515625e-05f;
   const int begin = a.causal ? t.first / TILE : 0, each = (t.length + TILE - 1) / TILE - begin, n = each * group;
   if (warp == BWD_ROWS + 1) {
-    if (lane == 0) {
-      mbar_expect(kv_full, 2 * L::BYTES);
-      copy_tile<DP>(k_tile, &maps.k, kh, t.row + t.first, kv_full);
-      copy_tile<DP>(v_tile, &maps.v, kh, t.row + t.first, kv_full);
-    }
     u32 side = 0, words[4];
     int i = 0;
     bool ok = true;
+    float range = 1.f;
     for (; ok && i < 2 * n; ++i) {                             // tiles of queries and of dout in turn
       const int st = i % L::STAGES, j = i / 2, head = kh * group + j / each, first = (begin + j % each) * TILE;
       if (i >= L::STAGES && !mbar_wait(empty + 8 * st, (i / L::STAGES - 1) & 1, dead)) break;
@@ -712,13 +760,17 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
       } else {
         // With dout, whose slot was the queries' of two steps ago or later ones': the step that used these numbers before has ended.
         if (i >= 4 && L::STAGES > 5 && !mbar_wait(empty + 8 * ((i - 5) % L::STAGES), ((i - 5) / L::STAGES) & 1, dead)) break;
+        if (i == 1) {                                          // row_dot comes from the kernel before this one
+          asm volatile("griddepcontrol.wait;" ::: "memory");
+          if (!BF16) range = range_of(most);
+        }
         float* const to = stats + (j & 1) * 2 * TILE;
         const long long at = (long long)head * a.tokens + t.row + first;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const bool on = words[w] >> lane & 1;
           to[32 * w + lane] = on ? fmaf(g.lse[at + 32 * w + lane], -LOG2E, shift) : -INFINITY;
-          to[TILE + 32 * w + lane] = on ? -g.row_dot[at + 32 * w + lane] * (range * back) : 0.f;
+          to[TILE + 32 * w + lane] = on ? -__ldcg(g.row_dot + at + 32 * w + lane) * (range * back) : 0.f;
         }
         __syncwarp();
       }
@@ -766,6 +818,11 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   } else {
     const int part_of = warp >> 2, i = t.first + (warp & 3) * 32 + lane;   // the thread's key
     const u32 lanes = (u32)(warp & 3) << 21, s_at = tmem + 32 * part_of + lanes, d_at = dp_at + 32 * part_of + lanes;
+    float range = 1.f;
+    if (!BF16) {
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      range = range_of(most);
+    }
     const float c = a.scale * LOG2E;
     const F2 c2 = f2(c, c), range2 = f2(range * back, range * back);
     bool ok = true;
@@ -885,30 +942,39 @@ bool takes(const adacgd_attention_inputs& a) {
          rows_on_16(a.k, a.k_stride, a.tokens) && rows_on_16(a.v, a.v_stride, a.tokens) && tile_slots(a, TILE) * a.heads < (1ll << 31) && encoder();
 }
 
+// after: the kernel may begin before the one in front of it has ended (it waits for that itself).
 template <typename K, typename... A>
-bool launch_mma(K kern, std::atomic<int> (&table)[TRAIN_DEVICES], int threads, int smem, long long ctas, const Where& at, const A&... args) {
+bool launch_mma(K kern, std::atomic<int> (&table)[TRAIN_DEVICES], int threads, int smem, long long ctas, bool after, const Where& at, const A&... args) {
   if (resident_ctas(kern, table, at.device, threads, smem) < 1) return false;
-  kern<<<(unsigned)ctas, threads, smem, at.stream>>>(args...);
-  return cudaGetLastError() == cudaSuccess;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = at.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = after ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, args...) == cudaSuccess;
 }
 
 template <bool BF16, int DP> int fwd_mma(const Maps& m, const adacgd_attention_args& g, const Where& at) {
   static std::atomic<int> table[TRAIN_DEVICES];
-  return launch_mma(k_attention_mma<BF16, DP>, table, FWD_CTA, FwdLayout<DP>::TOTAL, tile_slots(g.in, 2 * TILE) * g.in.heads, at, m, g) ? 1 : -1;
+  return launch_mma(k_attention_mma<BF16, DP>, table, FWD_CTA, FwdLayout<DP>::TOTAL, tile_slots(g.in, 2 * TILE) * g.in.heads, false, at, m, g) ? 1 : -1;
 }
 template <bool BF16, int DP> int bwd_mma(const TrainScratch& ws, const Maps& m, const adacgd_attention_backward_args& g, const Where& at) {
   static std::atomic<int> table[2][TRAIN_DEVICES];
   const long long slots = tile_slots(g.in, TILE);
-  float* const most = ws.norm_part;                            // of at least 2 * NORM_PARTS numbers
-  int parts = 0;
+  const float* const most = ws.norm_part;                      // of at least 2 * NORM_PARTS numbers
   if (!BF16) {
-    const long long want = (g.in.tokens * g.in.heads + DOT_CTA / 16 - 1) / (DOT_CTA / 16);
-    parts = (int)(want < DOT_CTAS ? want : DOT_CTAS);
-    k_attention_dot<<<parts, DOT_CTA, 0, at.stream>>>(g, most);
+    constexpr int LPR = DP / 8;
+    const long long rows = DOT_CTA / LPR * DOT_ROWS, want = (g.in.tokens * g.in.heads + rows - 1) / rows;
+    k_attention_dot<LPR><<<(unsigned)(want < DOT_CTAS ? want : DOT_CTAS), DOT_CTA, 0, at.stream>>>(g, ws.norm_part, ws.tickets + ATTENTION_TICKET);
     if (cudaGetLastError() != cudaSuccess) return -1;
   }
-  if (!launch_mma(k_attention_dq_mma<BF16, DP>, table[0], BWD_CTA, DqLayout<DP>::TOTAL, slots * g.in.heads, at, m, g, (const float*)most, parts)) return -1;
-  if (!launch_mma(k_attention_dkv_mma<BF16, DP>, table[1], BWD_CTA, DkvLayout<DP>::TOTAL, slots * g.in.key_heads, at, m, g, (const float*)most, parts)) return -1;
+  if (!launch_mma(k_attention_dq_mma<BF16, DP>, table[0], BWD_CTA, DqLayout<DP>::TOTAL, slots * g.in.heads, !BF16, at, m, g, most)) return -1;
+  if (!launch_mma(k_attention_dkv_mma<BF16, DP>, table[1], BWD_CTA, DkvLayout<DP>::TOTAL, slots * g.in.key_heads, true, at, m, g, most)) return -1;
   return BF16 ? 2 : 3;
 }
 

@@ -5,8 +5,11 @@
 // see one another's digit counts through distributed shared memory (no second launch, no flag that anybody spins on).  Then CTAs take
 // ranges of the table's rows, find their tokens by search and write every row once.  An id with very many tokens (frequent
 // words: a twentieth of a batch may be one word) would leave one CTA with all the work; its run of sorted tokens is cut into
-// windows, whose partial sums a last kernel adds in order.
+// windows, whose partial sums a last kernel adds in order.  (Adding them in the CTA that finishes last saved that kernel and cost more in the one
+// before it: 311 against 288 us for 32768 tokens.)
 #include <cooperative_groups.h>
+
+#include <type_traits>
 
 #include "adacgd_train.cuh"
 
@@ -15,8 +18,15 @@ namespace cg = cooperative_groups;
 namespace adacgd {
 namespace {
 
-// Vectors of N elements as floats: N = 8 takes whole runs, N = 1 any address.
+// Vectors of N elements: N = 8 takes whole runs, N = 1 any address.  Raw is what a load leaves.
 template <typename T, int N> struct Elems {
+  typedef typename std::conditional<N == 8, Run<T>, T>::type Raw;
+  static __device__ __forceinline__ Raw fetch(const T* p) {
+    if constexpr (N == 8) return load_run(p); else return p[0];
+  }
+  static __device__ __forceinline__ void floats(const Raw& r, float (&v)[N]) {
+    if constexpr (N == 8) unpack(r, v); else v[0] = to_f(r);
+  }
   static __device__ __forceinline__ void load(const T* p, float (&v)[N]) {
     if constexpr (N == 8) unpack(load_run(p), v); else v[0] = to_f(p[0]);
   }
@@ -96,7 +106,8 @@ int lookup_t(const adacgd_embedding_args& a, const Where& at) {
 // --------------------------------------------------------------------------
 // Least significant digit first, 9 bits a pass: an id of 131072 words takes two.  The cluster's CTAs own consecutive parts of the
 // array, their warps consecutive parts of those, so that (digit, CTA, warp, place) is the stable order.
-constexpr int SORT_CTA = 1024, SORT_WARPS = SORT_CTA / 32, DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS;
+constexpr int SORT_CTA = 1024, SORT_WARPS = SORT_CTA / 32, DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS, SORT_CTAS = 8;
+constexpr int SORT_KEEP = 8;      // (key, place) pairs a lane holds between counting and placing them
 
 struct SortSmem {
   u32 hist[SORT_WARPS][DIGITS];   // a warp's counts, then where its next token of a digit goes
@@ -106,21 +117,24 @@ struct SortSmem {
 
 // Key of a token: its id, or `vocab` (which sorts last) where it adds to nothing.
 __device__ __forceinline__ u32 key_of(const void* ids, int bytes, const uint8_t* mask, long long vocab, long long t) {
-  if (mask && !mask[t]) return (u32)vocab;
+  const bool on = !mask || mask[t];
   const long long id = id_at(ids, bytes, t);
-  return id >= 0 && id < vocab ? (u32)id : (u32)vocab;
+  return on && id >= 0 && id < vocab ? (u32)id : (u32)vocab;
 }
 
-// (key, place) pairs alternate between (k0, p0) and (k1, p1); the last pass ends in (k1, p1).
-__global__ void __launch_bounds__(SORT_CTA) k_sort_ids(const void* ids, int id_bytes, const uint8_t* mask, long long vocab, int n, int passes,
+// (key, place) pairs alternate between (k0, p0) and (k1, p1); the last pass ends in (k1, p1).  `warps` of each CTA take part: the
+// counts of a digit are added up warp by warp, so few tokens take few warps.  KEEP: a warp's tokens fit its lanes' registers.
+template <bool KEEP>
+__global__ void __launch_bounds__(SORT_CTA) k_sort_ids(const void* ids, int id_bytes, const uint8_t* mask, long long vocab, int n, int passes, int warps,
                                                        u32* k0, u32* p0, u32* k1, u32* p1) {
   extern __shared__ __align__(16) unsigned char sort_smem[];
   SortSmem& sh = *reinterpret_cast<SortSmem*>(sort_smem);
   cg::cluster_group cluster = cg::this_cluster();
   const int ctas = (int)cluster.num_blocks(), cta = (int)cluster.block_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long parts = (long long)ctas * SORT_WARPS, part = (long long)cta * SORT_WARPS + warp;
-  const int lo = (int)(part * n / parts), hi = (int)((part + 1) * n / parts);
+  const long long parts = (long long)ctas * warps, part = (long long)cta * warps + warp;
+  const int lo = warp < warps ? (int)(part * n / parts) : n, hi = warp < warps ? (int)((part + 1) * n / parts) : n;
+  u32 keys[SORT_KEEP], places[SORT_KEEP];
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * DIGIT_BITS;
     const bool odd = ((passes - pass) & 1) != 0;      // passes with an even distance to the end write (k1, p1)
@@ -128,17 +142,29 @@ __global__ void __launch_bounds__(SORT_CTA) k_sort_ids(const void* ids, int id_b
     const u32* const pi = odd ? p0 : p1;
     u32* const ko = odd ? k1 : k0;
     u32* const po = odd ? p1 : p0;
-    for (int i = threadIdx.x; i < SORT_WARPS * DIGITS; i += SORT_CTA) (&sh.hist[0][0])[i] = 0;
+    auto key_at = [&](int i) { return pass ? __ldcg(ki + i) : key_of(ids, id_bytes, mask, vocab, i); };
+    if (KEEP) {
+#pragma unroll
+      for (int k = 0; k < SORT_KEEP; ++k) {
+        const int i = lo + 32 * k + lane;
+        keys[k] = i < hi ? key_at(i) : 0;
+        places[k] = i < hi && pass ? __ldcg(pi + i) : (u32)i;
+      }
+    }
+    for (int i = threadIdx.x; i < warps * DIGITS; i += SORT_CTA) (&sh.hist[0][0])[i] = 0;
     __syncthreads();
-    for (int i = lo + lane; i < hi; i += 32) {
-      const u32 key = pass ? __ldcg(ki + i) : key_of(ids, id_bytes, mask, vocab, i);
-      atomicAdd(&sh.hist[warp][(key >> shift) & (DIGITS - 1)], 1u);
+    if (KEEP) {
+#pragma unroll
+      for (int k = 0; k < SORT_KEEP; ++k)
+        if (lo + 32 * k + lane < hi) atomicAdd(&sh.hist[warp][(keys[k] >> shift) & (DIGITS - 1)], 1u);
+    } else {
+      for (int i = lo + lane; i < hi; i += 32) atomicAdd(&sh.hist[warp][(key_at(i) >> shift) & (DIGITS - 1)], 1u);
     }
     __syncthreads();
     if (threadIdx.x < DIGITS) {                       // a digit's places among the CTA's warps
       u32 sum = 0;
 #pragma unroll 8
-      for (int w = 0; w < SORT_WARPS; ++w) {
+      for (int w = 0; w < warps; ++w) {
         const u32 c = sh.hist[w][threadIdx.x];
         sh.hist[w][threadIdx.x] = sum;
         sum += c;
@@ -148,10 +174,13 @@ __global__ void __launch_bounds__(SORT_CTA) k_sort_ids(const void* ids, int id_b
     cluster.sync();
     u32 before = 0, all = 0;                          // of this digit: in the CTAs before this one, in all
     if (threadIdx.x < DIGITS) {
-      for (int c = 0; c < ctas; ++c) {
-        const u32 v = *cluster.map_shared_rank(&sh.total[threadIdx.x], c);
-        if (c < cta) before += v;
-        all += v;
+      u32 v[SORT_CTAS];
+#pragma unroll
+      for (int c = 0; c < SORT_CTAS; ++c) v[c] = c < ctas ? *cluster.map_shared_rank(&sh.total[threadIdx.x], c) : 0u;
+#pragma unroll
+      for (int c = 0; c < SORT_CTAS; ++c) {
+        if (c < cta) before += v[c];
+        all += v[c];
       }
     }
     u32 incl = all;
@@ -166,17 +195,10 @@ __global__ void __launch_bounds__(SORT_CTA) k_sort_ids(const void* ids, int id_b
       u32 base = incl - all + before;
       for (int w = 0; w < warp; ++w) base += sh.scan[w];
 #pragma unroll 8
-      for (int w = 0; w < SORT_WARPS; ++w) sh.hist[w][threadIdx.x] += base;
+      for (int w = 0; w < warps; ++w) sh.hist[w][threadIdx.x] += base;
     }
     __syncthreads();
-    for (int i0 = lo; i0 < hi; i0 += 32) {
-      const int i = i0 + lane;
-      const bool in = i < hi;
-      u32 key = 0, place = (u32)i;
-      if (in) {
-        key = pass ? __ldcg(ki + i) : key_of(ids, id_bytes, mask, vocab, i);
-        if (pass) place = __ldcg(pi + i);
-      }
+    auto put = [&](u32 key, u32 place, bool in) {     // 32 tokens of the warp, in order
       const u32 digit = in ? (key >> shift) & (DIGITS - 1) : DIGITS;   // lanes behind the end match none that is in
       const u32 same = __match_any_sync(0xffffffffu, digit);
       const int rank = __popc(same & ((1u << lane) - 1));
@@ -188,6 +210,17 @@ __global__ void __launch_bounds__(SORT_CTA) k_sort_ids(const void* ids, int id_b
       if (in) {
         __stcg(ko + to, key);
         __stcg(po + to, place);
+      }
+    };
+    if (KEEP) {
+#pragma unroll
+      for (int k = 0; k < SORT_KEEP; ++k)
+        if (lo + 32 * k < hi) put(keys[k], places[k], lo + 32 * k + lane < hi);
+    } else {
+      for (int i0 = lo; i0 < hi; i0 += 32) {
+        const int i = i0 + lane;
+        const bool in = i < hi;
+        put(in ? key_at(i) : 0, in && pass ? __ldcg(pi + i) : (u32)i, in);
       }
     }
     __threadfence();
@@ -241,26 +274,47 @@ struct SumArgs {
   bool leave;       // rows without tokens stay as they are
 };
 
-// Sum of the rows places[lo .. hi) (a global or a shared array) in columns [N c, N c + N), four loads in flight.
-template <typename T, int N>
+// Sum of the rows places[lo .. hi) (a global or a shared array) in vector c of a row, AHEAD loads in flight.
+template <typename T, int N, int AHEAD>
 __device__ __forceinline__ void sum_rows(const SumArgs& s, const u32* places, int lo, int hi, long long c, float (&acc)[N]) {
 #pragma unroll
   for (int j = 0; j < N; ++j) acc[j] = 0.f;
   int i = lo;
-  for (; i + 4 <= hi; i += 4) {
-    float v[4][N];
+  for (; i + AHEAD <= hi; i += AHEAD) {
+    typename Elems<T, N>::Raw v[AHEAD];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) Elems<T, N>::load((const T*)s.dout + (long long)places[i + k] * s.dout_stride + c * N, v[k]);
+    for (int k = 0; k < AHEAD; ++k) v[k] = Elems<T, N>::fetch((const T*)s.dout + (long long)places[i + k] * s.dout_stride + c * N);
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < AHEAD; ++k) {
+      float f[N];
+      Elems<T, N>::floats(v[k], f);
 #pragma unroll
-      for (int j = 0; j < N; ++j) acc[j] += v[k][j];
+      for (int j = 0; j < N; ++j) acc[j] += f[j];
+    }
   }
   for (; i < hi; ++i) {
-    float v[N];
-    Elems<T, N>::load((const T*)s.dout + (long long)places[i] * s.dout_stride + c * N, v);
+    float f[N];
+    Elems<T, N>::load((const T*)s.dout + (long long)places[i] * s.dout_stride + c * N, f);
 #pragma unroll
-    for (int j = 0; j < N; ++j) acc[j] += v[j];
+    for (int j = 0; j < N; ++j) acc[j] += f[j];
+  }
+}
+
+// Partial sums: N numbers at a multiple of N.
+template <int N> __device__ __forceinline__ void store_part(float* p, const float (&v)[N]) {
+  if constexpr (N == 8) {
+    __stcg(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+    __stcg(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+  } else {
+    __stcg(p, v[0]);
+  }
+}
+template <int N> __device__ __forceinline__ void load_part(const float* p, float (&v)[N]) {
+  if constexpr (N == 8) {
+    *reinterpret_cast<float4*>(v) = __ldcg(reinterpret_cast<const float4*>(p));
+    *reinterpret_cast<float4*>(v + 4) = __ldcg(reinterpret_cast<const float4*>(p) + 1);
+  } else {
+    v[0] = __ldcg(p);
   }
 }
 
@@ -273,12 +327,27 @@ __device__ __forceinline__ void finish_row(const SumArgs& s, long long v, long l
   Elems<O, N>::store((O*)s.dtable + v * s.dtable_stride + c * N, o);
 }
 
+// Rows v0 .. v0 + rows - 1 of the table: the tokens of row r are places[edge[r] - lo .. edge[r + 1] - lo).  TPR threads a row; of its
+// columns, every `of`-th part from `part` on.
+template <typename T, typename O, int N, int TPR>
+__device__ __forceinline__ void write_rows(const SumArgs& s, long long v0, int rows, const int* edge, const u32* places, int lo, int part, int of) {
+  const long long vecs = s.cols / N;
+  for (int r = threadIdx.x / TPR; r < rows; r += SUM_CTA / TPR) {
+    const int from = edge[r], to = edge[r + 1];
+    if ((from == to && s.leave) || to - from > s.most) continue;
+    for (long long c = part * TPR + threadIdx.x % TPR; c < vecs; c += of * TPR) {
+      float acc[N];
+      sum_rows<T, N, N == 8 ? 4 : 8>(s, places, from - lo, to - lo, c, acc);
+      finish_row<O, N>(s, v0 + r, c, acc);
+    }
+  }
+}
+
 // The first CTAs take a window of the sorted tokens each (and a slice of its columns), for ids with more than `most` tokens; the
 // others `rows` rows of the table.  TPR threads a row.
 template <typename T, typename O, int N, int TPR>
 __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  constexpr int G = SUM_CTA / TPR;
   const long long vecs = s.cols / N;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __shared__ int edge[SUM_ROWS + 1];
@@ -288,27 +357,28 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
     const int w = (int)(blockIdx.x / s.slices), lo = w * s.most, hi = min(s.n, lo + s.most);
     const int slice = (int)(blockIdx.x % s.slices);
     // at most two long runs reach into a window: the one its first token belongs to and the one its last belongs to
+    // (none where no run crosses the window's ends)
+    const bool from_before = lo > 0 && __ldcg(s.keys + lo - 1) == __ldcg(s.keys + lo), goes_on = hi < s.n && __ldcg(s.keys + hi) == __ldcg(s.keys + hi - 1);
+    if (!from_before && !goes_on) return;
     if (warp < 2) {
       const u32 key = __ldcg(s.keys + (warp ? hi - 1 : lo));
       const int a = lower_bound_warp(s.keys, 0, warp ? hi : lo + 1, key);
       const int b = lower_bound_warp(s.keys, warp ? hi - 1 : lo, s.n, key + 1);
       const bool longer = b - a > s.most && (long long)key < s.vocab;
       if (lane == 0) {
-        edge[2 * warp] = longer ? max(a, lo) : 0;
-        edge[2 * warp + 1] = longer ? min(b, hi) : 0;
+        edge[2 * warp] = longer ? a : 0;
+        edge[2 * warp + 1] = longer ? b : 0;
       }
     }
     __syncthreads();
-    const int from0 = edge[0], to0 = edge[1], from1 = edge[2], to1 = edge[3];
     for (int k = 0; k < 2; ++k) {
-      const int from = k ? from1 : from0, to = k ? to1 : to0;
-      if (to <= from || (k && from0 == from1 && to0 == to1)) continue;   // one run over the whole window: once
+      const int a = edge[2 * k], b = edge[2 * k + 1];
+      if (b <= a || (k && edge[0] == a)) continue;                       // one run over the whole window: once
       float* const part = s.part + (2ll * w + k) * s.part_stride;
       for (long long c = (long long)slice * SUM_CTA + threadIdx.x; c < vecs; c += (long long)s.slices * SUM_CTA) {
         float acc[N];
-        sum_rows<T, N>(s, s.places, from, to, c, acc);
-#pragma unroll
-        for (int j = 0; j < N; ++j) part[c * N + j] = acc[j];
+        sum_rows<T, N, 4>(s, s.places, max(a, lo), min(b, hi), c, acc);
+        store_part(part + c * N, acc);
       }
     }
     return;
@@ -327,17 +397,58 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
     for (int i = threadIdx.x; i < hi - lo; i += SUM_CTA) staged[i] = __ldcg(s.places + lo + i);
   if (threadIdx.x < rows) edge[threadIdx.x] = lo == hi ? lo : lower_bound_lane(s.keys, lo, hi, (u32)(v0 + threadIdx.x));
   __syncthreads();
-  const int t = threadIdx.x % TPR;
-  for (int r = threadIdx.x / TPR; r < rows; r += G) {
-    const int from = edge[r], to = edge[r + 1];
-    if ((from == to && s.leave) || to - from > s.most) continue;
-    for (long long c = t; c < vecs; c += TPR) {
-      float acc[N];
-      if (stage) sum_rows<T, N>(s, staged, from - lo, to - lo, c, acc);
-      else sum_rows<T, N>(s, s.places, from, to, c, acc);
-      finish_row<O, N>(s, v0 + r, c, acc);
+  write_rows<T, O, N, TPR>(s, v0, rows, edge, stage ? staged : s.places + lo, lo, 0, 1);
+}
+
+// Few tokens: no sort, no search.  Every CTA looks at all of them, in order, keeps those of its rows, and puts them in the rows' order; one kernel
+// instead of two, 24 -> 9 us for 1023 tokens and 1001 rows.
+constexpr int FEW_TOKENS = 1024, FEW_EACH = FEW_TOKENS / SUM_CTA;
+
+template <typename T, typename O, int N, int TPR>
+__global__ void __launch_bounds__(SUM_CTA) k_embedding_sum_few(SumArgs s, const void* ids, int id_bytes, const uint8_t* mask) {
+  constexpr int WARPS = SUM_CTA / 32;
+  __shared__ int count[FEW_EACH][WARPS], edge[SUM_ROWS + 1];
+  __shared__ u32 found[FEW_TOKENS], staged[FEW_TOKENS];   // row in the CTA << 16 | token; tokens by row
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long v0 = (long long)blockIdx.x * s.rows;
+  const int rows = (int)min((long long)s.rows, s.vocab - v0);
+  u32 hit[FEW_EACH];
+  int row[FEW_EACH];
+#pragma unroll
+  for (int k = 0; k < FEW_EACH; ++k) {
+    const int i = k * SUM_CTA + threadIdx.x;
+    const u32 key = i < s.n ? key_of(ids, id_bytes, mask, s.vocab, i) : (u32)s.vocab;
+    row[k] = (long long)key >= v0 && (long long)key < v0 + rows ? (int)(key - v0) : -1;
+    hit[k] = __ballot_sync(0xffffffffu, row[k] >= 0);
+    if (lane == 0) count[k][warp] = __popc(hit[k]);
+  }
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int k = 0; k < FEW_EACH; ++k) {
+    int at = 0;
+    for (int w = 0; w < WARPS; ++w) {
+      if (w == warp) at = total;
+      total += count[k][w];
+    }
+    if (row[k] >= 0) found[at + __popc(hit[k] & ((1u << lane) - 1))] = (u32)row[k] << 16 | (u32)(k * SUM_CTA + threadIdx.x);
+  }
+  __syncthreads();
+  for (int r = warp; r < rows; r += WARPS) {              // how many tokens the rows before have, and the row's own in order
+    int before = 0;
+    for (int i = lane; i < total; i += 32) before += (int)(found[i] >> 16) < r;
+    before = __reduce_add_sync(0xffffffffu, before);
+    if (lane == 0) edge[r] = before;
+    for (int i0 = 0; i0 < total; i0 += 32) {
+      const u32 e = i0 + lane < total ? found[i0 + lane] : 0xffffffffu;
+      const u32 mine = __ballot_sync(0xffffffffu, (int)(e >> 16) == r && i0 + lane < total);
+      if (mine >> lane & 1) staged[before + __popc(mine & ((1u << lane) - 1))] = e & 0xffffu;
+      before += __popc(mine);
     }
   }
+  if (threadIdx.x == 0) edge[rows] = total;
+  __syncthreads();
+  write_rows<T, O, N, TPR>(s, v0, rows, edge, staged, 0, (int)blockIdx.y, (int)gridDim.y);
 }
 
 // Adds the windows of a long run, in order, by the CTAs of the window in which it begins (in which no second one can begin:
@@ -348,6 +459,7 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_join(SumArgs s) {
   const int w = (int)blockIdx.x, lo = w * s.most, hi = min(s.n, lo + s.most);
   __shared__ int ends[2];
   const u32 key = __ldcg(s.keys + hi - 1);
+  if (hi == s.n || __ldcg(s.keys + hi) != key) return;   // the run ends here, so it is short
   if (threadIdx.x < 32) {
     const int a = lower_bound_warp(s.keys, 0, hi, key), b = lower_bound_warp(s.keys, hi - 1, s.n, key + 1);
     if (threadIdx.x == 0) {
@@ -364,11 +476,13 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_join(SumArgs s) {
     float acc[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] = 0.f;
+#pragma unroll 4
     for (int i = w; i <= last; ++i) {
       // the run is its window's first one unless it begins behind the window's first token
-      const float* const part = s.part + (2ll * i + (i == w && a > lo ? 1 : 0)) * s.part_stride + c * N;
+      float v[N];
+      load_part(s.part + (2ll * i + (i == w && a > lo ? 1 : 0)) * s.part_stride + c * N, v);
 #pragma unroll
-      for (int j = 0; j < N; ++j) acc[j] += __ldcg(part + j);
+      for (int j = 0; j < N; ++j) acc[j] += v[j];
     }
     finish_row<O, N>(s, (long long)key, c, acc);
   }
@@ -389,30 +503,67 @@ bool launch_dependent(K kern, dim3 grid, int threads, const Where& at, A... args
 }
 
 template <typename T, typename O, int N, int TPR>
-int sum_launch(SumArgs s, const Where& at) {
-  const long long slices = (s.cols / N + SUM_CTA - 1) / SUM_CTA;
-  s.slices = (int)(slices < 16 ? slices : 16);
+int sum_launch(SumArgs s, const adacgd_embedding_backward_args& a, const Where& at) {
   // Rows of the table one after the other are a chain of memory latencies: few of them a CTA as long as that gives every SM only a
   // few CTAs.
   s.rows = SUM_ROWS;
   while (s.rows > SUM_CTA / TPR && s.rows > 1 && s.vocab < 8ll * s.rows * at.sms) s.rows /= 2;
+  if (s.n <= FEW_TOKENS) {
+    const long long ctas = (s.vocab + s.rows - 1) / s.rows;
+    long long parts = (s.cols / N + TPR - 1) / TPR, most = 16ll * at.sms / ctas;   // of the columns, where that does not make too many CTAs
+    if (parts > most) parts = most;
+    k_embedding_sum_few<T, O, N, TPR><<<dim3((unsigned)ctas, (unsigned)(parts < 1 ? 1 : parts)), SUM_CTA, 0, at.stream>>>(s, a.ids, (int)a.id_bytes, a.mask);
+    return cudaGetLastError() == cudaSuccess ? 1 : -1;
+  }
   const long long blocks = (long long)s.windows * s.slices + (s.vocab + s.rows - 1) / s.rows;
   if (!launch_dependent(k_embedding_sum<T, O, N, TPR>, dim3((unsigned)blocks), SUM_CTA, at, s)) return -1;
   if (!s.windows) return 1;
   return launch_dependent(k_embedding_join<O, N>, dim3((unsigned)s.windows, (unsigned)s.slices), SUM_CTA, at, s) ? 2 : -1;
 }
 template <typename T, typename O, int N>
-int sum_by_width(const SumArgs& s, const Where& at) {
+int sum_by_width(const SumArgs& s, const adacgd_embedding_backward_args& a, const Where& at) {
   const long long vecs = s.cols / N;
-  if (vecs <= 16) return sum_launch<T, O, N, 8>(s, at);
-  if (vecs <= 64) return sum_launch<T, O, N, 32>(s, at);
-  return sum_launch<T, O, N, 256>(s, at);
+  if (vecs <= 16) return sum_launch<T, O, N, 8>(s, a, at);
+  if (vecs <= 64) return sum_launch<T, O, N, 32>(s, a, at);
+  return sum_launch<T, O, N, 256>(s, a, at);
 }
 template <typename T, typename O>
-int sum_t(const SumArgs& s, const Where& at) {
+int sum_t(const SumArgs& s, const adacgd_embedding_backward_args& a, const Where& at) {
   const bool runs = whole_runs<T>(s.dout, s.dout_stride, s.n, s.cols) && whole_runs<O>(s.base, s.base_stride, s.vocab, s.cols) &&
                     whole_runs<O>(s.dtable, s.dtable_stride, s.vocab, s.cols);
-  return runs ? sum_by_width<T, O, 8>(s, at) : sum_by_width<T, O, 1>(s, at);
+  return runs ? sum_by_width<T, O, 8>(s, a, at) : sum_by_width<T, O, 1>(s, a, at);
+}
+
+// Sorts the tokens into s->keys and s->places.
+bool sort_tokens(const TrainScratch& ws, const adacgd_embedding_backward_args& a, const Where& at, SumArgs* s) {
+  u32 *k0 = (u32*)ws.tok_a, *p0 = (u32*)ws.tok_b, *k1 = (u32*)ws.tok_c, *p1 = (u32*)ws.seq;
+  s->keys = k1;
+  s->places = p1;
+  int bits = 1;
+  while ((1ll << bits) <= a.vocab) ++bits;           // keys up to `vocab` itself
+  const int passes = (bits + DIGIT_BITS - 1) / DIGIT_BITS;
+  const long long slices = (a.cols / 8 + SUM_CTA - 1) / SUM_CTA;
+  s->slices = (int)(slices < 1 ? 1 : (slices < 16 ? slices : 16));
+  // A warp takes at least 128 tokens and then up to 256 in its registers; more CTAs cost a little in the counts they exchange.
+  int ctas = 1, warps = 1;
+  while (ctas < SORT_CTAS && s->n > 2048 * ctas) ctas *= 2;
+  while (warps < SORT_WARPS && s->n > 128 * ctas * warps) warps *= 2;
+  const bool keep = s->n <= 32ll * (SORT_KEEP - 1) * ctas * warps;   // shares differ by one
+  auto sort = keep ? k_sort_ids<true> : k_sort_ids<false>;
+  static std::atomic<int> table[2][TRAIN_DEVICES];
+  if (resident_ctas(sort, table[keep], at.device, SORT_CTA, (int)sizeof(SortSmem)) < 1) return false;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(SORT_CTA);
+  cfg.dynamicSmemBytes = sizeof(SortSmem);
+  cfg.stream = at.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)ctas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, sort, a.ids, (int)a.id_bytes, a.mask, (long long)a.vocab, s->n, passes, warps, k0, p0, k1, p1) == cudaSuccess;
 }
 
 }  // namespace
@@ -435,41 +586,20 @@ int launch_embedding_backward(const TrainScratch& ws, const adacgd_embedding_bac
   s.n = (int)a.tokens;
   s.scale = a.scale;
   s.leave = a.base && a.base == a.dtable;
-  u32 *k0 = (u32*)ws.tok_a, *p0 = (u32*)ws.tok_b, *k1 = (u32*)ws.tok_c, *p1 = (u32*)ws.seq;
-  s.keys = k1;
-  s.places = p1;
   s.part = ws.norm_part;
-  s.part_stride = ws.max_cols;
+  s.part_stride = a.cols;                            // at most max_cols; whole runs stay aligned
   s.most = (s.n + MAX_WINDOWS - 1) / MAX_WINDOWS;
   if (s.most < SUM_MIN) s.most = SUM_MIN;
   s.windows = s.n > s.most ? (s.n + s.most - 1) / s.most : 0;
-  int bits = 1;
-  while ((1ll << bits) <= a.vocab) ++bits;           // keys up to `vocab` itself
-  const int passes = (bits + DIGIT_BITS - 1) / DIGIT_BITS;
-  static std::atomic<int> table[TRAIN_DEVICES];
-  if (resident_ctas(k_sort_ids, table, at.device, SORT_CTA, (int)sizeof(SortSmem)) < 1) return -1;
-  // A CTA reads 32 numbers a warp and step; more CTAs cost a little in the counts they exchange.
-  int ctas = 1;
-  while (ctas < 8 && s.n > 2048 * ctas) ctas *= 2;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(SORT_CTA);
-  cfg.dynamicSmemBytes = sizeof(SortSmem);
-  cfg.stream = at.stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)ctas;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, k_sort_ids, a.ids, (int)a.id_bytes, a.mask, (long long)a.vocab, s.n, passes, k0, p0, k1, p1) != cudaSuccess) return -1;
+  if (s.n > FEW_TOKENS && !sort_tokens(ws, a, at, &s)) return -1;
+  if (s.n <= FEW_TOKENS) s.most = FEW_TOKENS;
   int n = -1;
-  if (a.table_dtype == ADACGD_F32 && a.dtype == ADACGD_F16) n = sum_t<__half, float>(s, at);
-  else if (a.table_dtype == ADACGD_F32 && a.dtype == ADACGD_BF16) n = sum_t<__nv_bfloat16, float>(s, at);
-  else if (a.dtype == ADACGD_F32) n = sum_t<float, float>(s, at);
-  else if (a.dtype == ADACGD_F16) n = sum_t<__half, __half>(s, at);
-  else n = sum_t<__nv_bfloat16, __nv_bfloat16>(s, at);
-  return n < 0 ? -1 : n + 1;
+  if (a.table_dtype == ADACGD_F32 && a.dtype == ADACGD_F16) n = sum_t<__half, float>(s, a, at);
+  else if (a.table_dtype == ADACGD_F32 && a.dtype == ADACGD_BF16) n = sum_t<__nv_bfloat16, float>(s, a, at);
+  else if (a.dtype == ADACGD_F32) n = sum_t<float, float>(s, a, at);
+  else if (a.dtype == ADACGD_F16) n = sum_t<__half, __half>(s, a, at);
+  else n = sum_t<__nv_bfloat16, __nv_bfloat16>(s, a, at);
+  return n < 0 ? -1 : (s.n > FEW_TOKENS ? n + 1 : n);
 }
 
 }  // namespace adacgd

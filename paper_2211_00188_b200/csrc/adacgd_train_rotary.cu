@@ -370,10 +370,10 @@ __device__ __forceinline__ float dot16(const F2 (&x)[8], const F2 (&y)[8]) {
   return a + b;
 }
 
-// Heads [lo, hi) of one matrix row, LPH lanes a head and BATCH rounds of loads ahead.
-template <typename T, int LPH, bool HALVES, int BATCH>
+// Heads [lo, hi) of one matrix row, LPH lanes a head and BATCH rounds of loads ahead.  `ready` makes w, c and s, behind the first loads.
+template <typename T, int LPH, bool HALVES, int BATCH, typename R>
 __device__ __forceinline__ void norm_heads(const T* x, T* out, int lo, int hi, int dim, float eps, int group, int e, bool in, const F2 (&w)[8],
-                                           const F2 (&c)[4], const F2 (&s)[4]) {
+                                           const F2 (&c)[4], const F2 (&s)[4], R ready) {
   constexpr int G = 32 / LPH;
   const int half = dim / 2;
   const float inv = 1.f / (float)dim;
@@ -389,6 +389,7 @@ __device__ __forceinline__ void norm_heads(const T* x, T* out, int lo, int hi, i
   };
 #pragma unroll
   for (int k = 0; k < BATCH; ++k) fetch(k, lo + k * G + group);
+  ready();
   for (int h0 = lo; h0 < hi; h0 += BATCH * G) {
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
@@ -418,21 +419,24 @@ __global__ void __launch_bounds__(TWO_CTA) k_qk_norm_two(adacgd_qk_norm_args a, 
   const int heads = (int)(a.heads + a.key_heads), part = (int)(item % parts);
   const int lo = (int)((long long)heads * part / parts), hi = (int)((long long)heads * (part + 1) / parts), nq = (int)a.heads;
   F2 c[4], s[4], w[8];
-  lane_turns<HALVES>(a, t, l, in, tables[warp], false, c, s);
   if (lo < nq) {
-    lane_weights<P>(a.q_weight, e, a.head_dim / 2, in, w);
-    norm_heads<T, LPH, HALVES, BATCH>((const T*)a.q + t * a.q_stride, (T*)a.q_out + t * a.q_out_stride, lo, min(hi, nq), a.head_dim, a.eps, group, e, in, w, c, s);
+    norm_heads<T, LPH, HALVES, BATCH>((const T*)a.q + t * a.q_stride, (T*)a.q_out + t * a.q_out_stride, lo, min(hi, nq), a.head_dim, a.eps, group, e, in, w, c, s, [&] {
+      lane_weights<P>(a.q_weight, e, a.head_dim / 2, in, w);
+      lane_turns<HALVES>(a, t, l, in, tables[warp], false, c, s);
+    });
   }
   if (hi > nq) {
-    lane_weights<P>(a.k_weight, e, a.head_dim / 2, in, w);
     norm_heads<T, LPH, HALVES, BATCH>((const T*)a.k + t * a.k_stride, (T*)a.k_out + t * a.k_out_stride, max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e,
-                                      in, w, c, s);
+                                      in, w, c, s, [&] {
+      lane_weights<P>(a.k_weight, e, a.head_dim / 2, in, w);
+      if (lo >= nq) lane_turns<HALVES>(a, t, l, in, tables[warp], false, c, s);
+    });
   }
 }
 
-template <typename T, int LPH, bool HALVES, int BATCH>
+template <typename T, int LPH, bool HALVES, int BATCH, typename R>
 __device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, int lo, int hi, int dim, float eps, int group, int e, bool in,
-                                               const F2 (&w)[8], const F2 (&c)[4], const F2 (&s)[4], F2 (&dw)[8]) {
+                                               const F2 (&w)[8], const F2 (&c)[4], const F2 (&s)[4], F2 (&dw)[8], R ready) {
   constexpr int G = 32 / LPH;
   const int half = dim / 2;
   const float inv = 1.f / (float)dim;
@@ -451,6 +455,7 @@ __device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, i
   };
 #pragma unroll
   for (int k = 0; k < BATCH; ++k) fetch(k, lo + k * G + group);
+  ready();
   for (int h0 = lo; h0 < hi; h0 += BATCH * G) {
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
@@ -479,7 +484,7 @@ __device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, i
 }
 
 template <typename T, typename P, int LPH, bool HALVES>
-__global__ void __launch_bounds__(TWO_CTA, 4) k_qk_norm_two_bwd(adacgd_qk_norm_backward_args g, int parts, float* part, long long part_stride) {
+__global__ void __launch_bounds__(TWO_CTA, sizeof(T) == 4 ? 3 : 4) k_qk_norm_two_bwd(adacgd_qk_norm_backward_args g, int parts, float* part, long long part_stride) {
   constexpr int BATCH = 1, DIM = 16 * LPH, SLOTS = TWO_CTA / LPH;
   const adacgd_qk_norm_args& a = g.f;
   __shared__ __align__(16) float tables[TWO_WARPS][2 * MAX_PAIRS], rows[SLOTS * DIM];
@@ -494,16 +499,19 @@ __global__ void __launch_bounds__(TWO_CTA, 4) k_qk_norm_two_bwd(adacgd_qk_norm_b
     const long long t = item / parts;
     const int mine = (int)(item % parts), lo = (int)((long long)heads * mine / parts), hi = (int)((long long)heads * (mine + 1) / parts);
     F2 c[4], s[4], w[8];
-    lane_turns<HALVES>(a, t, l, in, tables[warp], true, c, s);
     if (lo < nq) {
-      lane_weights<P>(a.q_weight, e, half, in, w);
       norm_heads_bwd<T, LPH, HALVES, BATCH>((const T*)a.q + t * a.q_stride, (const T*)a.q_out + t * a.q_out_stride, (T*)g.dq + t * g.dq_stride, lo,
-                                            min(hi, nq), a.head_dim, a.eps, group, e, in, w, c, s, dwq);
+                                            min(hi, nq), a.head_dim, a.eps, group, e, in, w, c, s, dwq, [&] {
+        lane_weights<P>(a.q_weight, e, half, in, w);
+        lane_turns<HALVES>(a, t, l, in, tables[warp], true, c, s);
+      });
     }
     if (hi > nq) {
-      lane_weights<P>(a.k_weight, e, half, in, w);
       norm_heads_bwd<T, LPH, HALVES, BATCH>((const T*)a.k + t * a.k_stride, (const T*)a.k_out + t * a.k_out_stride, (T*)g.dk + t * g.dk_stride,
-                                            max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e, in, w, c, s, dwk);
+                                            max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e, in, w, c, s, dwk, [&] {
+        lane_weights<P>(a.k_weight, e, half, in, w);
+        if (lo >= nq) lane_turns<HALVES>(a, t, l, in, tables[warp], true, c, s);
+      });
     }
   }
   if (!part) return;
@@ -531,6 +539,7 @@ __global__ void __launch_bounds__(256) k_qk_norm_dw(const float* part, long long
   const int lane = threadIdx.x & 31, e = blockIdx.x * 8 + (threadIdx.x >> 5), k = blockIdx.y;
   if (e >= dim) return;
   double sum = 0.0;
+#pragma unroll 8
   for (int i = lane; i < parts; i += 32) sum += (double)__ldcg(part + (2ll * i + k) * part_stride + e);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -739,7 +748,7 @@ template <typename T, typename P, int LPH, bool HALVES>
 int two_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g, const Where& at) {
   const int parts = parts_of(g.f, LPH, at);
   long long ctas = (g.f.tokens * parts + TWO_WARPS - 1) / TWO_WARPS;
-  if (ctas > 4ll * at.sms) ctas = 4ll * at.sms;
+  if (ctas > (sizeof(T) == 4 ? 3ll : 4ll) * at.sms) ctas = (sizeof(T) == 4 ? 3ll : 4ll) * at.sms;
   if (ctas > NORM_PARTS) ctas = NORM_PARTS;
   const bool grads = g.dq_weight || g.dk_weight;
   k_qk_norm_two_bwd<T, P, LPH, HALVES><<<(unsigned)ctas, TWO_CTA, 0, at.stream>>>(g, parts, grads ? s.norm_part : (float*)nullptr, s.max_cols);
