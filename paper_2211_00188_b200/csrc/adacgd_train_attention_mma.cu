@@ -32,14 +32,20 @@ template <int DP> __device__ __forceinline__ void copy_tile(u32 dst, const CUten
 #pragma unroll
   for (int h = 0; h < DP / 64; ++h) tma_load_3d(dst + h * HALF, map, 64 * h, head, (int)row, bar);
 }
-// Bits of the rows first .. first + 127 that count.
-__device__ __forceinline__ void counted(const adacgd_attention_inputs& a, const Tile& t, int first, u32 (&words)[4]) {
-  const int lane = threadIdx.x & 31;
+// Which of the rows first .. first + 127 count: read a tile ahead (a byte of the mask a lane and 32 rows), put together where they are needed.
+struct Counts {
+  bool on[4];
+};
+__device__ __forceinline__ void read_counts(const adacgd_attention_inputs& a, const Tile& t, int first, Counts& c) {
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const int i = first + 32 * w + lane;
-    words[w] = __ballot_sync(0xffffffffu, i < t.length && (!a.mask || a.mask[t.row + i]));
+    const int i = first + 32 * w + (threadIdx.x & 31);
+    c.on[w] = i >= 0 && i < t.length && (!a.mask || a.mask[t.row + i]);
   }
+}
+__device__ __forceinline__ void words_of(const Counts& c, u32 (&words)[4]) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) words[w] = __ballot_sync(0xffffffffu, c.on[w]);
 }
 __device__ __forceinline__ bool all_count(const u32 (&words)[4]) { return (words[0] & words[1] & words[2] & words[3]) == 0xffffffffu; }
 
@@ -71,6 +77,41 @@ __device__ __forceinline__ bool bring(u32 dst, const CUtensorMap* map, int head,
 
 // After a wait that ran out: the copies under way must have ended before the CTA's memory goes to another.
 __device__ __forceinline__ void settle(u32 bar, u32 parity) { mbar_wait(bar, parity, nullptr); }
+
+// The tiles of the item's sequence between its first and its last token that counts: [begin, end), none if nothing counts.  A padded
+// batch has nothing but padding in the others.  By the whole CTA, whose shared memory is not in use yet.
+__device__ __forceinline__ void trim(const adacgd_attention_inputs& a, const Tile& t, int* scratch, int* begin, int* end) {
+  *begin = 0;
+  *end = (t.length + TILE - 1) / TILE;
+  if (!a.mask) return;
+  if (threadIdx.x == 0) {
+    scratch[0] = t.length;
+    scratch[1] = 0;
+  }
+  __syncthreads();
+  int lo = t.length, hi = 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < t.length; i += blockDim.x)
+    if (a.mask[t.row + i]) {
+      lo = min(lo, i);
+      hi = i + 1;
+    }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if ((threadIdx.x & 31) == 0) {
+    atomicMin(scratch, lo);
+    atomicMax(scratch + 1, hi);
+  }
+  __syncthreads();
+  *begin = scratch[0] / TILE;
+  *end = scratch[1] ? (scratch[1] + TILE - 1) / TILE : *begin;
+  __syncthreads();
+}
+// Zeros in a row.
+__device__ __forceinline__ void zero_row(void* base, long long stride, long long row, int head, int dim) {
+  uint4* const to = reinterpret_cast<uint4*>((char*)base + (row * stride + (long long)head * dim) * 2);
+  for (int d = 0; d < dim / 8; ++d) to[d] = make_uint4(0, 0, 0, 0);
+}
 
 // ---- the product warp ----
 // d = a b^T over 16 * STEPS columns of both tiles.
@@ -180,11 +221,22 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
   volatile int* const dead = reinterpret_cast<int*>(tmem_at + 1);
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int kh = head / (a.heads / a.key_heads);
-  const int tiles = (t.length + TILE - 1) / TILE;              // of keys
-  int count[2];                                                // that A and B meet
-  count[0] = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
-  count[1] = t.first + TILE >= t.length ? 0 : (a.causal ? min(tiles, t.first / TILE + 2) : tiles);
-  const int n = max(count[0], count[1]);
+  int begin, end, count[2];                                    // tiles of keys; how many of them A and B meet
+  trim(a, t, reinterpret_cast<int*>(mma_smem), &begin, &end);
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int mine = t.first / TILE + x;                       // without a row that counts: none
+    count[x] = mine < begin || mine >= end ? 0 : (a.causal ? mine + 1 : end) - begin;
+  }
+  const int n = max(count[0], count[1]), last = a.causal ? begin + n : end;   // the walk goes from the last tile down to the first
+  if (n == 0) {
+    const int i = t.first + (int)threadIdx.x;
+    if (threadIdx.x < 2 * TILE && i < t.length) {
+      zero_row(g.out, g.out_stride, t.row + i, head, a.head_dim);
+      if (g.lse) g.lse[(long long)head * a.tokens + t.row + i] = -INFINITY;
+    }
+    return;
+  }
   if (warp == FWD_ROWS + 1 && lane == 0) {
     mbar_init(q_full, 1);
     mbar_init(aside, 1);
@@ -199,8 +251,8 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
     }
     *dead = 0;
     mbar_init_fence();
-    mbar_expect(q_full, (count[1] ? 2 : 1) * L::BYTES);         // the first copies start before the CTA's warps have met
-    copy_tile<DP>(base, &maps.q, head, t.row + t.first, q_full);
+    mbar_expect(q_full, ((count[0] ? 1 : 0) + (count[1] ? 1 : 0)) * L::BYTES);   // the first copies start before the CTA's warps have met
+    if (count[0]) copy_tile<DP>(base, &maps.q, head, t.row + t.first, q_full);
     if (count[1]) copy_tile<DP>(base + L::BYTES, &maps.q, head, t.row + t.first + TILE, q_full);
   }
   if (warp == FWD_ROWS) tmem_alloc(smem_addr(tmem_at), 512);
@@ -213,12 +265,17 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == FWD_ROWS + 1) {
       u32 side = 0, words[4];
+      Counts ahead;
+      read_counts(a, t, (last - 1) * TILE, ahead);
       int i = 0;
       bool ok = true;
       for (; ok && i < 2 * n; ++i) {                             // tiles of keys and values in turn, the last ones first
-        const int st = i % L::STAGES, first = (n - 1 - i / 2) * TILE;
+        const int st = i % L::STAGES, first = (last - 1 - i / 2) * TILE;
         if (i >= L::STAGES && !mbar_wait(empty + 8 * st, (i / L::STAGES - 1) & 1, dead)) break;
-        if (i & 1) counted(a, t, first, words);                // only values are summed over
+        if (i & 1) {                                           // only values are summed over
+          words_of(ahead, words);
+          read_counts(a, t, first - TILE, ahead);
+        }
         ok = bring<DP>(base + L::RING + st * L::BYTES, i & 1 ? &maps.v : &maps.k, kh, t.row + first, words, i & 1, full + 8 * st, aside, side, dead);
       }
       if (*dead) {
@@ -267,16 +324,19 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
     const float c = a.scale * LOG2E;
     float top = -INFINITY, sum = 0.f;
     bool ok = true;
+    // A and B end with the same tile; where causal, A's walk begins a tile later
+    const int top_tile = begin + count[x];
+    Counts ahead;
+    if (count[x]) read_counts(a, t, (top_tile - 1) * TILE, ahead);
     for (int u = 0; u < count[x]; ++u) {
-      const int j0 = (count[x] - 1 - u) * TILE;
+      const int j0 = (top_tile - 1 - u) * TILE;
       u32 words[4];
-      const bool mask = a.mask || j0 + TILE > t.length || (a.causal && j0 + TILE > t.first + x * TILE);
-      if (mask) {
-        counted(a, t, j0, words);
-        if (a.causal)
+      words_of(ahead, words);
+      if (u + 1 < count[x]) read_counts(a, t, j0 - TILE, ahead);
+      const bool edge = a.causal && j0 + TILE > t.first + x * TILE, mask = edge || !all_count(words);
+      if (edge)
 #pragma unroll
-          for (int w = 0; w < 4; ++w) words[w] &= low_bits(i + 1 - j0 - 32 * w);
-      }
+        for (int w = 0; w < 4; ++w) words[w] &= low_bits(i + 1 - j0 - 32 * w);
       if (!(ok = mbar_wait(s_full + 8 * x, u & 1, dead))) break;
       tc_fence_after();
       u32 s[4][32];
@@ -341,6 +401,10 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
       tmem_wait_st();
       tc_fence_before();
       mbar_arrive(p_full + 8 * x);
+    }
+    if (count[x] == 0 && i < t.length) {
+      zero_row(g.out, g.out_stride, t.row + i, head, a.head_dim);
+      if (g.lse) g.lse[(long long)head * a.tokens + t.row + i] = -INFINITY;
     }
     if (count[x] && ok && mbar_wait(o_full + 8 * x, 0, dead)) {
       tc_fence_after();
@@ -509,6 +573,18 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Tile t;
   if (!tile_of(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, TILE, &t)) return;
+  int begin, end;                                              // tiles of keys
+  trim(a, t, reinterpret_cast<int*>(mma_smem), &begin, &end);
+  if (t.first / TILE < begin || t.first / TILE >= end) {        // no row that counts
+    const int i = t.first + (int)threadIdx.x;
+    if (threadIdx.x < TILE && i < t.length) {
+      zero_row(g.dq, g.dq_stride, t.row + i, head, a.head_dim);
+      if (BF16) g.row_dot[(long long)head * a.tokens + t.row + i] = 0.f;
+    }
+    if (!BF16) asm volatile("griddepcontrol.wait;" ::: "memory");   // this kernel ends after the one before it, whatever there is to do
+    return;
+  }
+  const int last = a.causal ? t.first / TILE + 1 : end, n = last - begin;
   const u32 base = smem_addr(mma_smem), bars = base + L::BARS;
   const u32 q_full = bars, aside = bars + 8, s_full = bars + 16, dp_full = bars + 32, ds_full = bars + 40, dq_full = bars + 48, k_full = bars + 64,
             k_empty = k_full + 8 * L::KS, v_full = k_empty + 8 * L::KS, v_empty = v_full + 8 * L::VS;
@@ -544,14 +620,16 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
   tc_fence_after();
   const u32 tmem = __shfl_sync(0xffffffffu, *tmem_at, 0), dp_at = tmem + 2 * TILE, dq_at = tmem + 3 * TILE;
   const u32 q_tile = base, do_tile = base + L::BYTES, k_tiles = base + L::RING, v_tiles = k_tiles + L::KS * L::BYTES;
-  const int kh = head / (a.heads / a.key_heads), tiles = (t.length + TILE - 1) / TILE;
-  const int n = a.causal ? min(tiles, t.first / TILE + 1) : tiles;
+  const int kh = head / (a.heads / a.key_heads);
   if (warp == BWD_ROWS + 1) {
     u32 side = 0, words[4];
+    Counts ahead;
+    read_counts(a, t, (last - 1) * TILE, ahead);
     int nk = 0, nv = 0;
     for (int j = 0; j < n; ++j) {
-      const int first = (n - 1 - j) * TILE, sk = j % L::KS, sv = j % L::VS;
-      counted(a, t, first, words);
+      const int first = (last - 1 - j) * TILE, sk = j % L::KS, sv = j % L::VS;
+      words_of(ahead, words);
+      read_counts(a, t, first - TILE, ahead);
       if (j >= L::KS && !mbar_wait(k_empty + 8 * sk, (j / L::KS - 1) & 1, dead)) break;
       ++nk;
       if (!bring<DP>(k_tiles + sk * L::BYTES, &maps.k, kh, t.row + first, words, true, k_full + 8 * sk, aside, side, dead)) break;
@@ -630,16 +708,16 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
     const float low = on ? -g.lse[at] * LOG2E : -INFINITY, c = a.scale * LOG2E;
     const F2 c2 = f2(c, c), low2 = f2(low, low), dot2 = f2(-dot, -dot), range2 = f2(range, range);
     bool ok = true;
+    const int column = 32 * part_of + lane;
+    auto counts = [&](int first) { return first + column >= 0 && first + column < t.length && (!a.mask || a.mask[t.row + first + column]); };
+    bool ahead = counts((last - 1) * TILE);
     for (int j = 0; j < n; ++j) {
-      const int j0 = (n - 1 - j) * TILE;
+      const int j0 = (last - 1 - j) * TILE;
       const u32 s_at = tmem + (j & 1) * TILE + 32 * part_of + lanes;
-      u32 bits = 0xffffffffu;
-      const bool mask = a.mask || j0 + TILE > t.length || (a.causal && j0 + TILE > t.first);
-      if (mask) {
-        const int key = j0 + 32 * part_of;
-        bits = __ballot_sync(0xffffffffu, key + lane < t.length && (!a.mask || a.mask[t.row + key + lane]));
-        if (a.causal) bits &= low_bits(i + 1 - key);
-      }
+      u32 bits = __ballot_sync(0xffffffffu, ahead);
+      if (j + 1 < n) ahead = counts(j0 - TILE);
+      const bool edge = a.causal && j0 + TILE > t.first, mask = edge || bits != 0xffffffffu;
+      if (edge) bits &= low_bits(i + 1 - j0 - 32 * part_of);
       if (!(ok = mbar_wait(s_full + 8 * (j & 1), (j >> 1) & 1, dead))) break;
       tc_fence_after();
       u32 s[32];
@@ -713,6 +791,17 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
     asm volatile("griddepcontrol.wait;" ::: "memory");           // this kernel ends after the one before it, whatever there is to do
     return;
   }
+  int low_tile, high_tile;                                     // of queries
+  trim(a, t, reinterpret_cast<int*>(mma_smem), &low_tile, &high_tile);
+  if (t.first / TILE < low_tile || t.first / TILE >= high_tile) {   // no key that counts
+    const int i = t.first + (int)threadIdx.x;
+    if (threadIdx.x < TILE && i < t.length) {
+      zero_row(g.dk, g.dk_stride, t.row + i, kh, a.head_dim);
+      zero_row(g.dv, g.dv_stride, t.row + i, kh, a.head_dim);
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    return;
+  }
   const u32 base = smem_addr(mma_smem), bars = base + L::BARS;
   const u32 kv_full = bars, aside = bars + 8, s_full = bars + 16, dp_full = bars + 24, s_read = bars + 32, ds_full = bars + 40, end_full = bars + 48,
             full = bars + 56, empty = full + 8 * L::STAGES;
@@ -746,9 +835,11 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   const u32 k_tile = base, v_tile = base + L::BYTES, ring = base + L::RING;
   // binary16: p is taken 2^14 times larger, ds by its range (see above)
   const float shift = BF16 ? 0.f : 14.f, back = BF16 ? 1.f : 6.103515625e-05f;
-  const int begin = a.causal ? t.first / TILE : 0, each = (t.length + TILE - 1) / TILE - begin, n = each * group;
+  const int begin = a.causal ? t.first / TILE : low_tile, each = high_tile - begin, n = each * group;
   if (warp == BWD_ROWS + 1) {
     u32 side = 0, words[4];
+    Counts ahead;
+    read_counts(a, t, begin * TILE, ahead);
     int i = 0;
     bool ok = true;
     float range = 1.f;
@@ -756,7 +847,8 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
       const int st = i % L::STAGES, j = i / 2, head = kh * group + j / each, first = (begin + j % each) * TILE;
       if (i >= L::STAGES && !mbar_wait(empty + 8 * st, (i / L::STAGES - 1) & 1, dead)) break;
       if (!(i & 1)) {
-        counted(a, t, first, words);
+        words_of(ahead, words);
+        read_counts(a, t, (begin + (j + 1) % each) * TILE, ahead);
       } else {
         // With dout, whose slot was the queries' of two steps ago or later ones': the step that used these numbers before has ended.
         if (i >= 4 && L::STAGES > 5 && !mbar_wait(empty + 8 * ((i - 5) % L::STAGES), ((i - 5) / L::STAGES) & 1, dead)) break;

@@ -335,10 +335,37 @@ __device__ __forceinline__ void write_rows(const SumArgs& s, long long v0, int r
   for (int r = threadIdx.x / TPR; r < rows; r += SUM_CTA / TPR) {
     const int from = edge[r], to = edge[r + 1];
     if ((from == to && s.leave) || to - from > s.most) continue;
-    for (long long c = part * TPR + threadIdx.x % TPR; c < vecs; c += of * TPR) {
-      float acc[N];
-      sum_rows<T, N, N == 8 ? 4 : 8>(s, places, from - lo, to - lo, c, acc);
-      finish_row<O, N>(s, v0 + r, c, acc);
+    if constexpr (N == 8) {
+      for (long long c = part * TPR + threadIdx.x % TPR; c < vecs; c += of * TPR) {
+        float acc[N];
+        sum_rows<T, N, 4>(s, places, from - lo, to - lo, c, acc);
+        finish_row<O, N>(s, v0 + r, c, acc);
+      }
+    } else {                                        // single elements: eight columns at a time, or a row's latencies add up
+      constexpr int C = 8;
+      for (long long c = part * TPR + threadIdx.x % TPR; c < vecs; c += (long long)C * of * TPR) {
+        float acc[C], base[C];
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+          const long long col = c + (long long)k * of * TPR;
+          acc[k] = base[k] = 0.f;
+          if (s.base && col < vecs) base[k] = to_f(((const O*)s.base)[(v0 + r) * s.base_stride + col]);
+        }
+#pragma unroll 2
+        for (int i = from - lo; i < to - lo; ++i) {
+          const T* const row = (const T*)s.dout + (long long)places[i] * s.dout_stride;
+#pragma unroll
+          for (int k = 0; k < C; ++k) {
+            const long long col = c + (long long)k * of * TPR;
+            if (col < vecs) acc[k] += to_f(row[col]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+          const long long col = c + (long long)k * of * TPR;
+          if (col < vecs) ((O*)s.dtable)[(v0 + r) * s.dtable_stride + col] = from_f<O>(s.base ? fmaf(acc[k], s.scale, base[k]) : acc[k] * s.scale);
+        }
+      }
     }
   }
 }
