@@ -5,10 +5,11 @@ with the training operators between ordinary matrix products, the gradients go a
 compressor (AdaCGD.compress: EF21/3PC difference, level choice, estimator update, server mean), and the server's mean moves
 the parameters.  A second phase lets the workers sample answers and goes on with the clipped policy loss.
 
-    python examples/finetune.py [--steps 60] [--policy-steps 20] [--workers 4]
+    python examples/finetune.py [--steps 60] [--policy-steps 20] [--workers 4] [--heads 0]
 
-The model is a residual network over the current token: s_0 = drop(E[token]), y_0 = norm(s_0), then per block
-s = s + drop(relu(y W1) W2), y = norm(s), and logits y E^T.  Data is synthetic: preferred answers follow
+The model is a residual network: s_0 = drop(E[token]), y_0 = norm(s_0), then per block
+s = s + drop(relu(y W1) W2), y = norm(s), and logits y E^T.  Without heads it sees the current token only; with heads each block has
+a causal attention in front, s = s + drop(attention(q, k, v) Wo) with q, k, v = y Wqkv, queries and keys normed and rotated by head.  Data is synthetic: preferred answers follow
 next = (5 token + 3) mod vocab, rejected ones are random.
 """
 from __future__ import annotations
@@ -26,11 +27,20 @@ import paper_2211_00188_b200 as adacgd  # noqa: E402
 class Model:
     """Parameters as views of one flat vector; `run` fills a flat gradient of the same layout."""
 
-    def __init__(self, vocab, width, hidden, blocks, tokens, dtype=torch.bfloat16, p=0.1, device="cuda"):
-        self.vocab, self.width, self.hidden, self.blocks, self.p, self.dtype = vocab, width, hidden, blocks, p, dtype
+    def __init__(self, vocab, width, hidden, blocks, tokens, dtype=torch.bfloat16, p=0.1, device="cuda", heads=0, key_heads=1):
+        self.vocab, self.width, self.hidden, self.p, self.dtype = vocab, width, hidden, p, dtype
+        self.heads, self.blocks = heads, blocks * (2 if heads else 1)
+        self.attends = lambda k: heads > 0 and k % 2 == 1          # blocks 1, 3, ... where there are heads
         shapes = [("E", (vocab, width)), ("w0", (width,)), ("b0", (width,))]
-        for k in range(1, blocks + 1):
-            shapes += [(f"W1_{k}", (width, hidden)), (f"W2_{k}", (hidden, width)), (f"w{k}", (width,)), (f"b{k}", (width,))]
+        if heads:
+            self.dim, self.keys = width // heads, width // heads * key_heads
+            self.freq = 10000.0 ** (-torch.arange(self.dim // 2, device=device, dtype=torch.float32) / (self.dim // 2))
+        for k in range(1, self.blocks + 1):
+            if self.attends(k):
+                shapes += [(f"Wqkv_{k}", (width, width + 2 * self.keys)), (f"Wo_{k}", (width, width)), (f"wq{k}", (self.dim,)), (f"wk{k}", (self.dim,))]
+            else:
+                shapes += [(f"W1_{k}", (width, hidden)), (f"W2_{k}", (hidden, width))]
+            shapes += [(f"w{k}", (width,)), (f"b{k}", (width,))]
         self.shapes, self.size = shapes, sum(torch.Size(s).numel() for _, s in shapes)
         self.device = device
         self.ops = adacgd.TrainingOps(tokens, width)
@@ -53,29 +63,42 @@ class Model:
                 v.fill_(1.0 if name[0] == "w" else 0.0)
         return flat
 
-    def forward(self, flat, tokens, p, seed):
-        """Logits and what the backward pass needs.  `seed` decides the dropout masks; the block's number is the offset."""
+    def forward(self, flat, tokens, p, seed, sequences=1):
+        """Logits and what the backward pass needs.  `seed` decides the dropout masks; the block's number is the offset.  Tokens are
+        those of `sequences` sequences of one length."""
         P = {k: v.to(self.dtype) for k, v in self.views(flat).items()}
-        n, new = tokens.numel(), lambda: torch.empty(tokens.numel(), self.width, dtype=self.dtype, device=self.device)  # noqa: E731
+        n = tokens.numel()
+        new = lambda cols=self.width: torch.empty(n, cols, dtype=self.dtype, device=self.device)  # noqa: E731
         kept = []
-        branch, s = P["E"][tokens], None
-        a = g = None
+        branch, s = new(), None
+        self.ops.embedding(tokens, P["E"], branch)
+        position = torch.arange(n, device=self.device) % (n // sequences)
         for k in range(self.blocks + 1):
-            if k:
-                a = kept[-1]["y"] @ P[f"W1_{k}"]
-                g = a.relu()
-                branch = g @ P[f"W2_{k}"]
+            c = {}
+            if self.attends(k):
+                w, h = self.width, self.keys
+                c["qkv"] = kept[-1]["y"] @ P[f"Wqkv_{k}"]
+                c["q"], c["k"], c["out"] = new(), new(h), new()
+                c["lse"] = torch.empty(self.heads, n, device=self.device)
+                self.ops.qk_norm(c["qkv"][:, :w], c["qkv"][:, w:w + h], c["q"], c["k"], position, self.freq, head_dim=self.dim, q_weight=P[f"wq{k}"],
+                                 k_weight=P[f"wk{k}"])
+                self.ops.attention(c["q"], c["k"], c["qkv"][:, w + h:], c["out"], heads=self.heads, lse=c["lse"], sequences=sequences)
+                branch = c["out"] @ P[f"Wo_{k}"]
+            elif k:
+                c["a"] = kept[-1]["y"] @ P[f"W1_{k}"]
+                c["g"] = c["a"].relu()
+                branch = c["g"] @ P[f"W2_{k}"]
             y, total = new(), new()
             mean, rstd = torch.empty(n, device=self.device), torch.empty(n, device=self.device)
             self.ops.layer_norm(branch, y, weight=P[f"w{k}"], bias=P[f"b{k}"], residual=s, sum_out=total, mean=mean, rstd=rstd, p=p,
                                 seed=seed, offset=k)
-            kept.append(dict(y=y, s=total, mean=mean, rstd=rstd, a=a, g=g))
+            kept.append(dict(c, y=y, s=total, mean=mean, rstd=rstd))
             s = total
-        return kept[-1]["y"] @ P["E"].t(), (P, kept, tokens, p, seed)
+        return kept[-1]["y"] @ P["E"].t(), (P, kept, tokens, p, seed, sequences, position)
 
     def backward(self, dlogits, state, flat_grad, scale):
         """Gradient of the loss into flat_grad, from scale * dloss/dlogits."""
-        P, kept, tokens, p, seed = state
+        P, kept, tokens, p, seed, sequences, position = state
         G = self.views(flat_grad)
         dy, ds = dlogits @ P["E"], None
         G["E"].copy_(dlogits.t() @ kept[-1]["y"])
@@ -87,14 +110,29 @@ class Model:
                                          dresidual=stream, p=p, seed=seed, offset=k)
             G[f"w{k}"].copy_(dw)
             G[f"b{k}"].copy_(db)
-            if k:
+            if self.attends(k):
+                w, h = self.width, self.keys
+                G[f"Wo_{k}"].copy_(c["out"].t() @ branch)
+                dout, dqkv = branch @ P[f"Wo_{k}"].t(), torch.empty_like(c["qkv"])
+                dq, dk, dot = torch.empty_like(c["q"]), torch.empty_like(c["k"]), torch.empty_like(c["lse"])
+                self.ops.attention_backward(dout, c["q"], c["k"], c["qkv"][:, w + h:], c["out"], c["lse"], dot, dq, dk, dqkv[:, w + h:],
+                                            heads=self.heads, sequences=sequences)
+                dwq, dwk = torch.empty_like(P[f"wq{k}"]), torch.empty_like(P[f"wk{k}"])
+                self.ops.qk_norm_backward(dq, dk, c["qkv"][:, :w], c["qkv"][:, w:w + h], dqkv[:, :w], dqkv[:, w:w + h], position, self.freq,
+                                          head_dim=self.dim, q_weight=P[f"wq{k}"], k_weight=P[f"wk{k}"], dq_weight=dwq, dk_weight=dwk)
+                G[f"wq{k}"].copy_(dwq)
+                G[f"wk{k}"].copy_(dwk)
+                G[f"Wqkv_{k}"].copy_(kept[k - 1]["y"].t() @ dqkv)
+                dy = dqkv @ P[f"Wqkv_{k}"].t()
+                ds = stream
+            elif k:
                 G[f"W2_{k}"].copy_(c["g"].t() @ branch)
                 da = (branch @ P[f"W2_{k}"].t()) * (c["a"] > 0)
                 G[f"W1_{k}"].copy_(kept[k - 1]["y"].t() @ da)
                 dy = da @ P[f"W1_{k}"].t()
                 ds = stream
             else:
-                G["E"].index_add_(0, tokens, branch.float())
+                self.ops.embedding_backward(tokens, branch, G["E"], base=G["E"])
         flat_grad.div_(scale)
 
 
@@ -122,11 +160,11 @@ class Worker:
         self.loss, self.margin = torch.empty(1, device=dev), torch.empty(pairs, device=dev)
 
     def reference(self, model, flat):
-        logits, _ = model.forward(flat, self.inputs, 0.0, 0)
+        logits, _ = model.forward(flat, self.inputs, 0.0, 0, 2 * self.pairs)
         model.ops.token_logp(logits, self.labels, self.ref, mask=self.mask)
 
     def preference_gradient(self, model, flat, row, step, scale=1024.0):
-        logits, state = model.forward(flat, self.inputs, model.p, self.seed * 1000003 + step)
+        logits, state = model.forward(flat, self.inputs, model.p, self.seed * 1000003 + step, 2 * self.pairs)
         model.ops.preference_loss(logits, self.labels, self.ref, self.loss, logits, mask=self.mask, sequences=2 * self.pairs, beta=0.5,
                                   grad_scale=scale, margin=self.margin)          # the gradient takes the logits' place
         model.backward(logits, state, row, scale)
@@ -137,15 +175,17 @@ class Worker:
         tokens = torch.empty(n, self.steps + 1, dtype=torch.long, device=dev)
         tokens[:, 0] = self.inputs.view(n, self.steps)[:, 0]
         for k in range(self.steps):
-            logits, _ = model.forward(flat, tokens[:, k].contiguous(), 0.0, 0)
+            seen = tokens[:, 0 if model.heads else k:k + 1]         # without heads the last token is all that counts
+            logits, _ = model.forward(flat, seen.contiguous().view(-1), 0.0, 0, n)
+            logits = logits.view(n, seen.shape[1], -1)[:, -1]
             tokens[:, k + 1] = torch.multinomial(logits.float().softmax(1), 1, generator=self.gen)[:, 0]
         inputs, labels = tokens[:, :-1].reshape(-1), tokens[:, 1:].reshape(-1)
         reward = (labels == (5 * inputs + 3) % model.vocab).float()
         advantage = (reward - reward.mean()) / (reward.std() + 1e-3)
         old, ref = torch.empty_like(advantage), torch.empty_like(advantage)
-        logits, state = model.forward(flat, inputs, 0.0, 0)
+        logits, state = model.forward(flat, inputs, 0.0, 0, n)
         model.ops.token_logp(logits, labels, old)
-        ref_logits, _ = model.forward(self.start, inputs, 0.0, 0)
+        ref_logits, _ = model.forward(self.start, inputs, 0.0, 0, n)
         model.ops.token_logp(ref_logits, labels, ref)
         model.ops.policy_loss(logits, labels, old, advantage, self.loss, logits, sequences=n, ref_logp=ref, kl_beta=0.01,
                               per_sequence=True, grad_scale=scale)
@@ -154,8 +194,8 @@ class Worker:
 
 
 def train(steps=60, policy_steps=20, workers=4, vocab=96, width=64, hidden=128, blocks=2, pairs=16, length=24, gamma=0.1, policy_gamma=0.4, zeta=1.0,
-          seed=0, dtype=torch.bfloat16, log=print):
-    model = Model(vocab, width, hidden, blocks, 2 * pairs * length, dtype)
+          seed=0, dtype=torch.bfloat16, log=print, heads=0):
+    model = Model(vocab, width, hidden, blocks, 2 * pairs * length, dtype, heads=heads)
     crew = [Worker(model, pairs, length, 100 * seed + i) for i in range(workers)]
     flat = model.initial(seed)
     d = model.size
@@ -210,5 +250,6 @@ if __name__ == "__main__":
     p.add_argument("--steps", type=int, default=60)
     p.add_argument("--policy-steps", type=int, default=20)
     p.add_argument("--workers", type=int, default=4)
+    p.add_argument("--heads", type=int, default=0, help="attention heads of a block (0: the model sees the current token only)")
     a = p.parse_args()
-    train(a.steps, a.policy_steps, a.workers)
+    train(a.steps, a.policy_steps, a.workers, heads=a.heads)

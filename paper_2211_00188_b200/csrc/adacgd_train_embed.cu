@@ -255,7 +255,7 @@ __device__ __forceinline__ int lower_bound_lane(const u32* keys, int lo, int hi,
   return lo;
 }
 
-constexpr int SUM_CTA = 256, SUM_ROWS = 32, SUM_MIN = 64, SUM_STAGE = 512;   // most rows of the table a CTA takes; tokens staged
+constexpr int SUM_CTA = 256, SUM_ROWS = 32, SUM_MIN = 16, SUM_STAGE = 512;   // most rows of the table a CTA takes; tokens staged
 constexpr int MAX_WINDOWS = NORM_PARTS;   // two partial sums a window
 
 struct SumArgs {
@@ -272,6 +272,7 @@ struct SumArgs {
   int rows;         // of the table, that a CTA takes
   float scale;
   bool leave;       // rows without tokens stay as they are
+  bool few;         // the tokens are not sorted
 };
 
 // Sum of the rows places[lo .. hi) (a global or a shared array) in vector c of a row, AHEAD loads in flight.
@@ -335,13 +336,13 @@ __device__ __forceinline__ void write_rows(const SumArgs& s, long long v0, int r
   for (int r = threadIdx.x / TPR; r < rows; r += SUM_CTA / TPR) {
     const int from = edge[r], to = edge[r + 1];
     if ((from == to && s.leave) || to - from > s.most) continue;
-    if constexpr (N == 8) {
+    if (N == 8 || vecs <= 2 * of * TPR) {
       for (long long c = part * TPR + threadIdx.x % TPR; c < vecs; c += of * TPR) {
         float acc[N];
-        sum_rows<T, N, 4>(s, places, from - lo, to - lo, c, acc);
+        sum_rows<T, N, N == 8 ? 4 : 8>(s, places, from - lo, to - lo, c, acc);
         finish_row<O, N>(s, v0 + r, c, acc);
       }
-    } else {                                        // single elements: eight columns at a time, or a row's latencies add up
+    } else if constexpr (N == 1) {                  // single elements of a long row: eight columns at a time, or their latencies add up
       constexpr int C = 8;
       for (long long c = part * TPR + threadIdx.x % TPR; c < vecs; c += (long long)C * of * TPR) {
         float acc[C], base[C];
@@ -429,7 +430,7 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
 
 // Few tokens: no sort, no search.  Every CTA looks at all of them, in order, keeps those of its rows, and puts them in the rows' order; one kernel
 // instead of two, 24 -> 9 us for 1023 tokens and 1001 rows.
-constexpr int FEW_TOKENS = 1024, FEW_EACH = FEW_TOKENS / SUM_CTA;
+constexpr int FEW_TOKENS = 1024, FEW_EACH = FEW_TOKENS / SUM_CTA, FEW_COLS = 1024;   // an id's tokens are one CTA's work there
 
 template <typename T, typename O, int N, int TPR>
 __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum_few(SumArgs s, const void* ids, int id_bytes, const uint8_t* mask) {
@@ -531,11 +532,13 @@ bool launch_dependent(K kern, dim3 grid, int threads, const Where& at, A... args
 
 template <typename T, typename O, int N, int TPR>
 int sum_launch(SumArgs s, const adacgd_embedding_backward_args& a, const Where& at) {
+  const long long slices = (s.cols / N + SUM_CTA - 1) / SUM_CTA;
+  s.slices = (int)(slices < 16 ? slices : 16);
   // Rows of the table one after the other are a chain of memory latencies: few of them a CTA as long as that gives every SM only a
   // few CTAs.
   s.rows = SUM_ROWS;
   while (s.rows > SUM_CTA / TPR && s.rows > 1 && s.vocab < 8ll * s.rows * at.sms) s.rows /= 2;
-  if (s.n <= FEW_TOKENS) {
+  if (s.few) {
     const long long ctas = (s.vocab + s.rows - 1) / s.rows;
     long long parts = (s.cols / N + TPR - 1) / TPR, most = 16ll * at.sms / ctas;   // of the columns, where that does not make too many CTAs
     if (parts > most) parts = most;
@@ -569,8 +572,6 @@ bool sort_tokens(const TrainScratch& ws, const adacgd_embedding_backward_args& a
   int bits = 1;
   while ((1ll << bits) <= a.vocab) ++bits;           // keys up to `vocab` itself
   const int passes = (bits + DIGIT_BITS - 1) / DIGIT_BITS;
-  const long long slices = (a.cols / 8 + SUM_CTA - 1) / SUM_CTA;
-  s->slices = (int)(slices < 1 ? 1 : (slices < 16 ? slices : 16));
   // A warp takes at least 128 tokens and then up to 256 in its registers; more CTAs cost a little in the counts they exchange.
   int ctas = 1, warps = 1;
   while (ctas < SORT_CTAS && s->n > 2048 * ctas) ctas *= 2;
@@ -618,15 +619,16 @@ int launch_embedding_backward(const TrainScratch& ws, const adacgd_embedding_bac
   s.most = (s.n + MAX_WINDOWS - 1) / MAX_WINDOWS;
   if (s.most < SUM_MIN) s.most = SUM_MIN;
   s.windows = s.n > s.most ? (s.n + s.most - 1) / s.most : 0;
-  if (s.n > FEW_TOKENS && !sort_tokens(ws, a, at, &s)) return -1;
-  if (s.n <= FEW_TOKENS) s.most = FEW_TOKENS;
+  s.few = s.n <= FEW_TOKENS && s.cols <= FEW_COLS;
+  if (s.few) s.most = FEW_TOKENS;
+  else if (!sort_tokens(ws, a, at, &s)) return -1;
   int n = -1;
   if (a.table_dtype == ADACGD_F32 && a.dtype == ADACGD_F16) n = sum_t<__half, float>(s, a, at);
   else if (a.table_dtype == ADACGD_F32 && a.dtype == ADACGD_BF16) n = sum_t<__nv_bfloat16, float>(s, a, at);
   else if (a.dtype == ADACGD_F32) n = sum_t<float, float>(s, a, at);
   else if (a.dtype == ADACGD_F16) n = sum_t<__half, __half>(s, a, at);
   else n = sum_t<__nv_bfloat16, __nv_bfloat16>(s, a, at);
-  return n < 0 ? -1 : (s.n > FEW_TOKENS ? n + 1 : n);
+  return n < 0 || s.few ? n : n + 1;
 }
 
 }  // namespace adacgd

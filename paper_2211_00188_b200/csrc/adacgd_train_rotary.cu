@@ -52,7 +52,7 @@ enum Reach { NEAR, LANE, ROW };
 // The lane's eight elements turned.  cs, sn: the lane's entries of the token's tables.
 template <int LPH, int REACH>
 __device__ __forceinline__ void rotate(const adacgd_qk_norm_args& a, const float* cs, const float* sn, int e0, float* row, float (&x)[8]) {
-  float c[8], s[8], y[8];
+  __align__(16) float c[8], s[8], y[8];
 #pragma unroll
   for (int j = 0; j < 8; j += 4) {
     *reinterpret_cast<float4*>(c + j) = *reinterpret_cast<const float4*>(cs + e0 + j);
@@ -69,10 +69,16 @@ __device__ __forceinline__ void rotate(const adacgd_qk_norm_args& a, const float
   } else {
     __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) row[e0 + j] = x[j];
+    for (int j = 0; j < 8; j += 4) *reinterpret_cast<float4*>(row + e0 + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
     __syncwarp();
+    if (a.pairs % 4 == 0) {                           // four elements have their partners side by side
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = e0 + j < a.head_dim ? row[partner(a, e0 + j)] : 0.f;
+      for (int j = 0; j < 8; j += 4)
+        *reinterpret_cast<float4*>(y + j) = *reinterpret_cast<const float4*>(row + (e0 + j < a.head_dim ? partner(a, e0 + j) : 0));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = e0 + j < a.head_dim ? row[partner(a, e0 + j)] : 0.f;
+    }
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) x[j] = fmaf(y[j], s[j], x[j] * c[j]);
@@ -286,9 +292,11 @@ __global__ void __launch_bounds__(ROT_CTA) k_qk_norm_bwd(adacgd_qk_norm_backward
 // there are few tokens, makes the token's cosines and sines once and keeps its lanes' in registers, as it does the weights.
 constexpr int TWO_CTA = 128, TWO_WARPS = TWO_CTA / 32, MAX_PAIRS = 128;
 
-// Cosines and sines of the lane's pairs, packed in twos.  HALVES: pair 8 l + j couples the runs' j-th elements.  Otherwise pair 4 l + i is
-// elements 2 i and 2 i + 1 of the first run, and those of the second follow.
-template <bool HALVES>
+// Cosines and sines of the lane's pairs, packed in twos.  HALVES: pair 8 l + j couples the runs' j-th elements.  NEIGHBOURS: pair 4 l + i is
+// elements 2 i and 2 i + 1 of the first run, and those of the second follow.  FRONT: halves of at most the head's first half, by whole
+// runs: pair 8 (l mod pairs / 8) + j is the first run's j-th element here and pairs / 8 lanes further; the sine has the element's sign.
+enum Turn { HALVES, NEIGHBOURS, FRONT };
+template <int TURN>
 __device__ __forceinline__ void lane_turns(const adacgd_qk_norm_args& a, long long t, int l, bool in, float* table, bool back, F2 (&c)[4], F2 (&s)[4]) {
   float* const sines = table + MAX_PAIRS;
   __syncwarp();
@@ -302,9 +310,14 @@ __device__ __forceinline__ void lane_turns(const adacgd_qk_norm_args& a, long lo
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const int i = HALVES ? 8 * l + 2 * j : (j < 2 ? 4 * l + 2 * j : 4 * (l + a.head_dim / 16) + 2 * (j - 2));
-    c[j] = in ? *reinterpret_cast<const F2*>(table + i) : f2(1.f, 1.f);
-    s[j] = in ? *reinterpret_cast<const F2*>(sines + i) : f2(0.f, 0.f);
+    const int d = a.pairs / 8;
+    const int i = TURN == HALVES ? 8 * l + 2 * j
+                : TURN == FRONT  ? 8 * (l < d ? l : l - d) + 2 * j
+                                 : (j < 2 ? 4 * l + 2 * j : 4 * (l + a.head_dim / 16) + 2 * (j - 2));
+    const bool has = in && (TURN != FRONT || l < 2 * d);
+    c[j] = has ? *reinterpret_cast<const F2*>(table + i) : f2(1.f, 1.f);
+    s[j] = has ? *reinterpret_cast<const F2*>(sines + i) : f2(0.f, 0.f);
+    if (TURN == FRONT && l < d) s[j].v ^= 0x8000000080000000ull;
   }
 }
 __device__ __forceinline__ F2 minus(F2 a) {
@@ -313,8 +326,16 @@ __device__ __forceinline__ F2 minus(F2 a) {
   return r;
 }
 // Turns the lane's sixteen elements: four packed pairs a run.
-template <bool HALVES> __device__ __forceinline__ void turn_two(F2 (&x)[8], const F2 (&c)[4], const F2 (&s)[4]) {
-  if (HALVES) {
+template <int TURN, int LPH> __device__ __forceinline__ void turn_two(F2 (&x)[8], const F2 (&c)[4], const F2 (&s)[4], int l, int d) {
+  if (TURN == FRONT) {
+    const int from = l < d ? l + d : (l < 2 * d ? l - d : l);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      F2 y;
+      y.v = __shfl_sync(0xffffffffu, x[j].v, from, LPH);
+      x[j] = fma2(y, s[j], mul2(x[j], c[j]));
+    }
+  } else if (TURN == HALVES) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const F2 a = x[j], b = x[4 + j];
@@ -371,8 +392,8 @@ __device__ __forceinline__ float dot16(const F2 (&x)[8], const F2 (&y)[8]) {
 }
 
 // Heads [lo, hi) of one matrix row, LPH lanes a head and BATCH rounds of loads ahead.  `ready` makes w, c and s, behind the first loads.
-template <typename T, int LPH, bool HALVES, int BATCH, typename R>
-__device__ __forceinline__ void norm_heads(const T* x, T* out, int lo, int hi, int dim, float eps, int group, int e, bool in, const F2 (&w)[8],
+template <typename T, int LPH, int TURN, int BATCH, typename R>
+__device__ __forceinline__ void norm_heads(const T* x, T* out, int lo, int hi, int dim, float eps, int group, int e, int d, bool in, const F2 (&w)[8],
                                            const F2 (&c)[4], const F2 (&s)[4], R ready) {
   constexpr int G = 32 / LPH;
   const int half = dim / 2;
@@ -401,14 +422,14 @@ __device__ __forceinline__ void norm_heads(const T* x, T* out, int lo, int hi, i
       const F2 r2 = f2(r, r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = mul2(mul2(v[j], r2), w[j]);
-      turn_two<HALVES>(v, c, s);
+      turn_two<TURN, LPH>(v, c, s, e / 8, d);
       if (h < hi && in) store_two(out + (long long)h * dim + e, out + (long long)h * dim + e + half, v);
     }
   }
 }
 
 // parts: warps a token.
-template <typename T, typename P, int LPH, bool HALVES>
+template <typename T, typename P, int LPH, int TURN>
 __global__ void __launch_bounds__(TWO_CTA) k_qk_norm_two(adacgd_qk_norm_args a, int parts) {
   constexpr int BATCH = sizeof(T) == 4 ? 1 : 2;
   __shared__ __align__(16) float tables[TWO_WARPS][2 * MAX_PAIRS];
@@ -420,22 +441,22 @@ __global__ void __launch_bounds__(TWO_CTA) k_qk_norm_two(adacgd_qk_norm_args a, 
   const int lo = (int)((long long)heads * part / parts), hi = (int)((long long)heads * (part + 1) / parts), nq = (int)a.heads;
   F2 c[4], s[4], w[8];
   if (lo < nq) {
-    norm_heads<T, LPH, HALVES, BATCH>((const T*)a.q + t * a.q_stride, (T*)a.q_out + t * a.q_out_stride, lo, min(hi, nq), a.head_dim, a.eps, group, e, in, w, c, s, [&] {
+    norm_heads<T, LPH, TURN, BATCH>((const T*)a.q + t * a.q_stride, (T*)a.q_out + t * a.q_out_stride, lo, min(hi, nq), a.head_dim, a.eps, group, e, a.pairs / 8, in, w, c, s, [&] {
       lane_weights<P>(a.q_weight, e, a.head_dim / 2, in, w);
-      lane_turns<HALVES>(a, t, l, in, tables[warp], false, c, s);
+      lane_turns<TURN>(a, t, l, in, tables[warp], false, c, s);
     });
   }
   if (hi > nq) {
-    norm_heads<T, LPH, HALVES, BATCH>((const T*)a.k + t * a.k_stride, (T*)a.k_out + t * a.k_out_stride, max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e,
-                                      in, w, c, s, [&] {
+    norm_heads<T, LPH, TURN, BATCH>((const T*)a.k + t * a.k_stride, (T*)a.k_out + t * a.k_out_stride, max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e,
+                                      a.pairs / 8, in, w, c, s, [&] {
       lane_weights<P>(a.k_weight, e, a.head_dim / 2, in, w);
-      if (lo >= nq) lane_turns<HALVES>(a, t, l, in, tables[warp], false, c, s);
+      if (lo >= nq) lane_turns<TURN>(a, t, l, in, tables[warp], false, c, s);
     });
   }
 }
 
-template <typename T, int LPH, bool HALVES, int BATCH, typename R>
-__device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, int lo, int hi, int dim, float eps, int group, int e, bool in,
+template <typename T, int LPH, int TURN, int BATCH, typename R>
+__device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, int lo, int hi, int dim, float eps, int group, int e, int shift, bool in,
                                                const F2 (&w)[8], const F2 (&c)[4], const F2 (&s)[4], F2 (&dw)[8], R ready) {
   constexpr int G = 32 / LPH;
   const int half = dim / 2;
@@ -464,7 +485,7 @@ __device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, i
       runs_of(a[k], b[k], v);
       runs_of(p[k], q[k], d);
       fetch(k, h + BATCH * G);
-      turn_two<HALVES>(d, c, s);
+      turn_two<TURN, LPH>(d, c, s, e / 8, shift);
       const float r = rsqrtf(fmaf(head_sum<LPH>(dot16(v, v)), inv, eps));
       const F2 r2 = f2(r, r);
       const bool live = h < hi && in;
@@ -483,7 +504,7 @@ __device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, i
   }
 }
 
-template <typename T, typename P, int LPH, bool HALVES>
+template <typename T, typename P, int LPH, int TURN>
 __global__ void __launch_bounds__(TWO_CTA, sizeof(T) == 4 ? 3 : 4) k_qk_norm_two_bwd(adacgd_qk_norm_backward_args g, int parts, float* part, long long part_stride) {
   constexpr int BATCH = 1, DIM = 16 * LPH, SLOTS = TWO_CTA / LPH;
   const adacgd_qk_norm_args& a = g.f;
@@ -500,17 +521,17 @@ __global__ void __launch_bounds__(TWO_CTA, sizeof(T) == 4 ? 3 : 4) k_qk_norm_two
     const int mine = (int)(item % parts), lo = (int)((long long)heads * mine / parts), hi = (int)((long long)heads * (mine + 1) / parts);
     F2 c[4], s[4], w[8];
     if (lo < nq) {
-      norm_heads_bwd<T, LPH, HALVES, BATCH>((const T*)a.q + t * a.q_stride, (const T*)a.q_out + t * a.q_out_stride, (T*)g.dq + t * g.dq_stride, lo,
-                                            min(hi, nq), a.head_dim, a.eps, group, e, in, w, c, s, dwq, [&] {
+      norm_heads_bwd<T, LPH, TURN, BATCH>((const T*)a.q + t * a.q_stride, (const T*)a.q_out + t * a.q_out_stride, (T*)g.dq + t * g.dq_stride, lo,
+                                            min(hi, nq), a.head_dim, a.eps, group, e, a.pairs / 8, in, w, c, s, dwq, [&] {
         lane_weights<P>(a.q_weight, e, half, in, w);
-        lane_turns<HALVES>(a, t, l, in, tables[warp], true, c, s);
+        lane_turns<TURN>(a, t, l, in, tables[warp], true, c, s);
       });
     }
     if (hi > nq) {
-      norm_heads_bwd<T, LPH, HALVES, BATCH>((const T*)a.k + t * a.k_stride, (const T*)a.k_out + t * a.k_out_stride, (T*)g.dk + t * g.dk_stride,
-                                            max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e, in, w, c, s, dwk, [&] {
+      norm_heads_bwd<T, LPH, TURN, BATCH>((const T*)a.k + t * a.k_stride, (const T*)a.k_out + t * a.k_out_stride, (T*)g.dk + t * g.dk_stride,
+                                            max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e, a.pairs / 8, in, w, c, s, dwk, [&] {
         lane_weights<P>(a.k_weight, e, half, in, w);
-        if (lo >= nq) lane_turns<HALVES>(a, t, l, in, tables[warp], true, c, s);
+        if (lo >= nq) lane_turns<TURN>(a, t, l, in, tables[warp], true, c, s);
       });
     }
   }
@@ -553,7 +574,22 @@ __global__ void __launch_bounds__(256) k_qk_norm_dw(const float* part, long long
 // A warp a head, element by element; the row waits in shared memory for the rotation.
 constexpr int ANY_CTA = 256, ANY_WARPS = ANY_CTA / 32;
 
-template <typename T, typename P>
+// K elements a lane: heads of up to 32 K.  The next head's are loaded ahead.
+template <typename T, int K> struct Lane {
+  float v[K];
+  __device__ __forceinline__ void load(const T* p, int dim, bool on) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int e = (threadIdx.x & 31) + 32 * k;
+      v[k] = on && e < dim ? to_f(p[e]) : 0.f;
+    }
+  }
+};
+template <typename T> __device__ __forceinline__ T* head_at(const adacgd_qk_norm_args& a, const void* q, long long qs, const void* k, long long ks, long long t, int h) {
+  return h < a.heads ? (T*)q + place(qs, t, h, a.head_dim) : (T*)k + place(ks, t, h - (int)a.heads, a.head_dim);
+}
+
+template <typename T, typename P, int K>
 __global__ void __launch_bounds__(ANY_CTA) k_qk_norm_any(adacgd_qk_norm_args a) {
   extern __shared__ float any_smem[];
   const int dim = a.head_dim, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -561,33 +597,42 @@ __global__ void __launch_bounds__(ANY_CTA) k_qk_norm_any(adacgd_qk_norm_args a) 
   float* const sn = cs + dim;
   float* const row = sn + dim + warp * dim;
   const long long t = blockIdx.x;
+  const int heads = (int)(a.heads + a.key_heads);
+  auto at = [&](int h) { return head_at<const T>(a, a.q, a.q_stride, a.k, a.k_stride, t, h); };
+  Lane<T, K> x;
+  if (warp < heads) x.load(at(warp), dim, true);
   for (int i = 2 * a.pairs + threadIdx.x; i < dim; i += ANY_CTA) {
     cs[i] = 1.f;
     sn[i] = 0.f;
   }
   for (int i = threadIdx.x; i < a.pairs; i += ANY_CTA) fill_turns(a, t, i, cs, sn, false);
   __syncthreads();
-  const int heads = (int)(a.heads + a.key_heads);
   for (int h = warp; h < heads; h += ANY_WARPS) {
+    const Lane<T, K> now = x;
+    if (h + ANY_WARPS < heads) x.load(at(h + ANY_WARPS), dim, true);
     const bool query = h < a.heads;
-    const T* const x = query ? (const T*)a.q + place(a.q_stride, t, h, dim) : (const T*)a.k + place(a.k_stride, t, h - (int)a.heads, dim);
-    T* const out = query ? (T*)a.q_out + place(a.q_out_stride, t, h, dim) : (T*)a.k_out + place(a.k_out_stride, t, h - (int)a.heads, dim);
+    T* const out = head_at<T>(a, a.q_out, a.q_out_stride, a.k_out, a.k_out_stride, t, h);
     const void* const w = query ? a.q_weight : a.k_weight;
     float q = 0.f;
     __syncwarp();
-    for (int e = lane; e < dim; e += 32) {
-      const float v = to_f(x[e]);
-      q = fmaf(v, v, q);
-      row[e] = v * param<P>(w, e);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int e = lane + 32 * k;
+      q = fmaf(now.v[k], now.v[k], q);
+      if (e < dim) row[e] = now.v[k] * param<P>(w, e);
     }
     const float r = rsqrtf(fmaf(head_sum<32>(q), 1.f / (float)dim, a.eps));
     __syncwarp();
-    for (int e = lane; e < dim; e += 32) out[e] = from_f<T>(r * fmaf(row[partner(a, e)], sn[e], row[e] * cs[e]));
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int e = lane + 32 * k;
+      if (e < dim) out[e] = from_f<T>(r * fmaf(row[partner(a, e)], sn[e], row[e] * cs[e]));
+    }
   }
 }
 
-// The weights' gradients are added up in the warp's own row of shared memory, the warps' rows at the end.
-template <typename T, typename P>
+// The weights' gradients stay with the lane, and are added up in shared memory at the end.
+template <typename T, typename P, int K>
 __global__ void __launch_bounds__(ANY_CTA) k_qk_norm_bwd_any(adacgd_qk_norm_backward_args g, float* part, long long part_stride) {
   extern __shared__ float any_smem[];
   const adacgd_qk_norm_args& a = g.f;
@@ -596,10 +641,18 @@ __global__ void __launch_bounds__(ANY_CTA) k_qk_norm_bwd_any(adacgd_qk_norm_back
   float* const sn = cs + dim;
   float* const sums = sn + dim;                        // [warps][2][dim]
   float* const row = sums + 2 * ANY_WARPS * dim + warp * dim;
-  float* const mine = sums + 2 * warp * dim;
-  for (int i = lane; i < 2 * dim; i += 32) mine[i] = 0.f;
   const int heads = (int)(a.heads + a.key_heads);
+  float dwq[K], dwk[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) dwq[k] = dwk[k] = 0.f;
   for (long long t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+    auto x_at = [&](int h) { return head_at<const T>(a, a.q, a.q_stride, a.k, a.k_stride, t, h); };
+    auto y_at = [&](int h) { return head_at<const T>(a, a.q_out, a.q_out_stride, a.k_out, a.k_out_stride, t, h); };
+    Lane<T, K> x, y;
+    if (warp < heads) {
+      x.load(x_at(warp), dim, true);
+      y.load(y_at(warp), dim, true);
+    }
     __syncthreads();
     for (int i = 2 * a.pairs + threadIdx.x; i < dim; i += ANY_CTA) {
       cs[i] = 1.f;
@@ -608,43 +661,54 @@ __global__ void __launch_bounds__(ANY_CTA) k_qk_norm_bwd_any(adacgd_qk_norm_back
     for (int i = threadIdx.x; i < a.pairs; i += ANY_CTA) fill_turns(a, t, i, cs, sn, true);
     __syncthreads();
     for (int h = warp; h < heads; h += ANY_WARPS) {
+      const Lane<T, K> v = x, u = y;
+      if (h + ANY_WARPS < heads) {
+        x.load(x_at(h + ANY_WARPS), dim, true);
+        y.load(y_at(h + ANY_WARPS), dim, true);
+      }
       const bool query = h < a.heads;
-      const int kh = h - (int)a.heads;
-      const T* const x = query ? (const T*)a.q + place(a.q_stride, t, h, dim) : (const T*)a.k + place(a.k_stride, t, kh, dim);
-      const T* const y = query ? (const T*)a.q_out + place(a.q_out_stride, t, h, dim) : (const T*)a.k_out + place(a.k_out_stride, t, kh, dim);
-      T* const out = query ? (T*)g.dq + place(g.dq_stride, t, h, dim) : (T*)g.dk + place(g.dk_stride, t, kh, dim);
+      T* const out = head_at<T>(a, g.dq, g.dq_stride, g.dk, g.dk_stride, t, h);
       const void* const w = query ? a.q_weight : a.k_weight;
       float q = 0.f;
       __syncwarp();
-      for (int e = lane; e < dim; e += 32) {
-        const float v = to_f(x[e]);
-        q = fmaf(v, v, q);
-        row[e] = to_f(y[e]);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int e = lane + 32 * k;
+        q = fmaf(v.v[k], v.v[k], q);
+        if (e < dim) row[e] = u.v[k];
       }
       const float r = rsqrtf(fmaf(head_sum<32>(q), 1.f / (float)dim, a.eps));
       __syncwarp();
-      float dot = 0.f;
-      float dn[ADACGD_TRAIN_MAX_HEAD / 32];            // the lane's elements
+      float dot = 0.f, dn[K];
 #pragma unroll
-      for (int k = 0; k < ADACGD_TRAIN_MAX_HEAD / 32; ++k) {
+      for (int k = 0; k < K; ++k) {
         const int e = lane + 32 * k;
+        dn[k] = 0.f;
         if (e < dim) {
-          const float d = fmaf(row[partner(a, e)], sn[e], row[e] * cs[e]), v = to_f(x[e]) * r;
-          mine[(query ? 0 : dim) + e] += d * v;
+          const float d = fmaf(row[partner(a, e)], sn[e], u.v[k] * cs[e]), xr = v.v[k] * r;
+          if (query) dwq[k] = fmaf(d, xr, dwq[k]); else dwk[k] = fmaf(d, xr, dwk[k]);
           dn[k] = d * param<P>(w, e);
-          dot = fmaf(dn[k], v, dot);
+          dot = fmaf(dn[k], xr, dot);
         }
       }
       const float m = head_sum<32>(dot) * (1.f / (float)dim);
 #pragma unroll
-      for (int k = 0; k < ADACGD_TRAIN_MAX_HEAD / 32; ++k) {
+      for (int k = 0; k < K; ++k) {
         const int e = lane + 32 * k;
-        if (e < dim) out[e] = from_f<T>(r * fmaf(-m, to_f(x[e]) * r, dn[k]));
+        if (e < dim) out[e] = from_f<T>(r * fmaf(-m, v.v[k] * r, dn[k]));
       }
     }
   }
-  __syncthreads();
   if (!part) return;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int e = lane + 32 * k;
+    if (e < dim) {
+      sums[2 * warp * dim + e] = dwq[k];
+      sums[(2 * warp + 1) * dim + e] = dwk[k];
+    }
+  }
+  __syncthreads();
   for (int i = threadIdx.x; i < 2 * dim; i += ANY_CTA) {
     float sum = 0.f;
     for (int w = 0; w < ANY_WARPS; ++w) sum += sums[2 * w * dim + i];
@@ -727,8 +791,21 @@ int norm_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g
   return grads ? join_weights<P>(g, s, (int)ctas, at) : 1;
 }
 
-// Heads of two runs a lane: lengths by 16, whole heads turned in halves, or neighbours, or none.
-bool two_runs(const adacgd_qk_norm_args& a) { return a.head_dim % 16 == 0 && (a.interleaved || a.pairs == 0 || 2 * a.pairs == a.head_dim); }
+template <typename T, typename P, int K>
+int any_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g, const Where& at) {
+  static std::atomic<int> table[TRAIN_DEVICES];
+  constexpr int MOST = (2 + 3 * ANY_WARPS) * 32 * K * 4;
+  if (resident_ctas(k_qk_norm_bwd_any<T, P, K>, table, at.device, ANY_CTA, MOST) < 1) return -1;
+  const bool grads = g.dq_weight || g.dk_weight;
+  const int ctas = (int)(g.f.tokens < NORM_PARTS ? g.f.tokens : NORM_PARTS);
+  k_qk_norm_bwd_any<T, P, K><<<ctas, ANY_CTA, (2 + 3 * ANY_WARPS) * g.f.head_dim * 4, at.stream>>>(g, grads ? s.norm_part : (float*)nullptr, s.max_cols);
+  if (cudaGetLastError() != cudaSuccess) return -1;
+  return grads ? join_weights<P>(g, s, ctas, at) : 1;
+}
+
+// Heads of two runs a lane: lengths by 16, turned in neighbours, or in halves of the whole head or of whole runs of its first half.
+bool in_front(const adacgd_qk_norm_args& a) { return a.pairs % 8 == 0 && 4 * a.pairs <= a.head_dim; }
+bool two_runs(const adacgd_qk_norm_args& a) { return a.head_dim % 16 == 0 && (a.interleaved || 2 * a.pairs == a.head_dim || in_front(a)); }
 // Warps a token: one where that gives every SM sixteen of them.
 int parts_of(const adacgd_qk_norm_args& a, int lph, const Where& at) {
   const long long heads = a.heads + a.key_heads, most = (heads + 32 / lph - 1) / (32 / lph);
@@ -737,21 +814,21 @@ int parts_of(const adacgd_qk_norm_args& a, int lph, const Where& at) {
   return (int)(parts < 1 ? 1 : parts);
 }
 
-template <typename T, typename P, int LPH, bool HALVES>
+template <typename T, typename P, int LPH, int TURN>
 int two_launch(const adacgd_qk_norm_args& a, const Where& at) {
   const int parts = parts_of(a, LPH, at);
   const long long ctas = (a.tokens * parts + TWO_WARPS - 1) / TWO_WARPS;
-  k_qk_norm_two<T, P, LPH, HALVES><<<(unsigned)ctas, TWO_CTA, 0, at.stream>>>(a, parts);
+  k_qk_norm_two<T, P, LPH, TURN><<<(unsigned)ctas, TWO_CTA, 0, at.stream>>>(a, parts);
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
-template <typename T, typename P, int LPH, bool HALVES>
+template <typename T, typename P, int LPH, int TURN>
 int two_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g, const Where& at) {
   const int parts = parts_of(g.f, LPH, at);
   long long ctas = (g.f.tokens * parts + TWO_WARPS - 1) / TWO_WARPS;
   if (ctas > (sizeof(T) == 4 ? 3ll : 4ll) * at.sms) ctas = (sizeof(T) == 4 ? 3ll : 4ll) * at.sms;
   if (ctas > NORM_PARTS) ctas = NORM_PARTS;
   const bool grads = g.dq_weight || g.dk_weight;
-  k_qk_norm_two_bwd<T, P, LPH, HALVES><<<(unsigned)ctas, TWO_CTA, 0, at.stream>>>(g, parts, grads ? s.norm_part : (float*)nullptr, s.max_cols);
+  k_qk_norm_two_bwd<T, P, LPH, TURN><<<(unsigned)ctas, TWO_CTA, 0, at.stream>>>(g, parts, grads ? s.norm_part : (float*)nullptr, s.max_cols);
   if (cudaGetLastError() != cudaSuccess) return -1;
   return grads ? join_weights<P>(g, s, (int)ctas, at) : 1;
 }
@@ -762,8 +839,9 @@ int two_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g,
   if (a.head_dim <= 128) { constexpr int LPH = 8; BY_TURN(call) }                                      \
   { constexpr int LPH = 16; BY_TURN(call) }
 #define BY_TURN(call)                                                                                  \
-  if (!a.interleaved && a.pairs) { constexpr bool HALVES = true; return call; }                        \
-  { constexpr bool HALVES = false; return call; }
+  if (a.interleaved || a.pairs == 0) { constexpr int TURN = NEIGHBOURS; return call; }                 \
+  if (2 * a.pairs == a.head_dim) { constexpr int TURN = HALVES; return call; }                         \
+  { constexpr int TURN = FRONT; return call; }
 
 #define BY_HEAD(call)                                                                                  \
   const Reach reach = reach_of(a);                                                                     \
@@ -778,10 +856,13 @@ int two_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g,
 template <typename T, typename P>
 int norm_t(const adacgd_qk_norm_args& a, const Where& at) {
   if (!head_runs<T>(a)) {
-    k_qk_norm_any<T, P><<<(unsigned)a.tokens, ANY_CTA, (2 + ANY_WARPS) * a.head_dim * 4, at.stream>>>(a);
+    const int smem = (2 + ANY_WARPS) * a.head_dim * 4;
+    if (a.head_dim <= 64) k_qk_norm_any<T, P, 2><<<(unsigned)a.tokens, ANY_CTA, smem, at.stream>>>(a);
+    else if (a.head_dim <= 128) k_qk_norm_any<T, P, 4><<<(unsigned)a.tokens, ANY_CTA, smem, at.stream>>>(a);
+    else k_qk_norm_any<T, P, 16><<<(unsigned)a.tokens, ANY_CTA, smem, at.stream>>>(a);
     return cudaGetLastError() == cudaSuccess ? 1 : -1;
   }
-  if (two_runs(a)) { BY_LANES((two_launch<T, P, LPH, HALVES>(a, at))) }
+  if (two_runs(a)) { BY_LANES((two_launch<T, P, LPH, TURN>(a, at))) }
   BY_HEAD((norm_launch<T, P, LPH, REACH>(a, at)))
 }
 
@@ -789,16 +870,11 @@ template <typename T, typename P>
 int norm_bwd_t(const TrainScratch& s, const adacgd_qk_norm_backward_args& g, const Where& at) {
   const adacgd_qk_norm_args& a = g.f;
   if (!head_runs<T>(a) || !on_runs<T>(g.dq, g.dq_stride, a.tokens) || !on_runs<T>(g.dk, g.dk_stride, a.tokens)) {
-    static std::atomic<int> table[TRAIN_DEVICES];
-    constexpr int MOST = (2 + 3 * ANY_WARPS) * ADACGD_TRAIN_MAX_HEAD * 4;
-    if (resident_ctas(k_qk_norm_bwd_any<T, P>, table, at.device, ANY_CTA, MOST) < 1) return -1;
-    const bool grads = g.dq_weight || g.dk_weight;
-    const int ctas = (int)(a.tokens < NORM_PARTS ? a.tokens : NORM_PARTS);
-    k_qk_norm_bwd_any<T, P><<<ctas, ANY_CTA, (2 + 3 * ANY_WARPS) * a.head_dim * 4, at.stream>>>(g, grads ? s.norm_part : (float*)nullptr, s.max_cols);
-    if (cudaGetLastError() != cudaSuccess) return -1;
-    return grads ? join_weights<P>(g, s, ctas, at) : 1;
+    if (a.head_dim <= 64) return any_bwd_launch<T, P, 2>(s, g, at);
+    if (a.head_dim <= 128) return any_bwd_launch<T, P, 4>(s, g, at);
+    return any_bwd_launch<T, P, 16>(s, g, at);
   }
-  if (two_runs(a)) { BY_LANES((two_bwd_launch<T, P, LPH, HALVES>(s, g, at))) }
+  if (two_runs(a)) { BY_LANES((two_bwd_launch<T, P, LPH, TURN>(s, g, at))) }
   BY_HEAD((norm_bwd_launch<T, P, LPH, REACH>(s, g, at)))
 }
 
