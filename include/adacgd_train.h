@@ -212,8 +212,8 @@ typedef struct {
 adacgd_status adacgd_embedding(adacgd_train* t, const adacgd_embedding_args* a);
 
 /* Gradient of the lookup: dtable[v] = [base[v] +] scale * sum of dout[t] over the tokens t that count and have ids[t] = v.
- * Tokens are sorted by id, those of one id in the order of the batch, and summed in that order in pieces: binary32 chains
- * of at most max(64, tokens / 592) rows, joined in binary32 in order.  Ids outside [0, vocab) add to nothing.  Every row of dtable is written,
+ * The tokens of one id are summed in the order of the batch, in pieces: binary32 chains of at most max(16, tokens / 592) rows (1024 where
+ * tokens <= 1024 and cols <= 1024), joined in binary32 in order.  Ids outside [0, vocab) add to nothing.  Every row of dtable is written,
  * unless base is the very same matrix: then rows without tokens stay as they are.  tokens <= max_tokens, cols <= max_cols. */
 typedef struct {
   int64_t tokens, vocab, cols;
@@ -277,7 +277,9 @@ adacgd_status adacgd_qk_norm_backward(adacgd_train* t, const adacgd_qk_norm_back
  * tokens that do not count have out = 0 and lse = -inf.  Products and sums are kept in binary32; for the 16-bit types
  * exp(s_ij - c) is rounded to that type as an operand of the second product, with a power of two c near the row's largest s that keeps it in range.
  * What is stored in rows of tokens that do not count, or of other sequences, reaches no result; Inf or NaN in a token that counts may reach
- * every row of its sequence.  No output may overlap anything. */
+ * every row of its sequence.  No output may overlap anything.
+ * The tensor cores take the 16-bit types where head_dim is a multiple of 8 up to 128 and every matrix has rows on 16 bytes (pointer and
+ * stride); everything else goes to the general cores, at a thirtieth to a hundredth of the rate. */
 typedef struct {
   int64_t tokens, sequences;
   const int32_t* seq_start; /* [sequences + 1] or NULL */

@@ -488,23 +488,23 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_join(SumArgs s) {
   __shared__ int ends[2];
   const u32 key = __ldcg(s.keys + hi - 1);
   if (hi == s.n || __ldcg(s.keys + hi) != key) return;   // the run ends here, so it is short
-  if (threadIdx.x < 32) {
-    const int a = lower_bound_warp(s.keys, 0, hi, key), b = lower_bound_warp(s.keys, hi - 1, s.n, key + 1);
-    if (threadIdx.x == 0) {
-      ends[0] = a;
-      ends[1] = b;
-    }
+  if (threadIdx.x < 64) {
+    const bool behind = threadIdx.x >= 32;                // the run's beginning, its end
+    const int e = behind ? lower_bound_warp(s.keys, hi - 1, s.n, key + 1) : lower_bound_warp(s.keys, lo, hi, key);
+    if ((threadIdx.x & 31) == 0) ends[behind] = e;
   }
   __syncthreads();
   const int a = ends[0], b = ends[1];
-  if (b - a <= s.most || a < lo || (long long)key >= s.vocab) return;
+  // a run that begins in front of the window is another window's
+  if (a == lo && lo > 0 && __ldcg(s.keys + lo - 1) == key) return;
+  if (b - a <= s.most || (long long)key >= s.vocab) return;
   const int last = (b - 1) / s.most;
   const long long vecs = s.cols / N;
   for (long long c = (long long)blockIdx.y * SUM_CTA + threadIdx.x; c < vecs; c += (long long)gridDim.y * SUM_CTA) {
     float acc[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = w; i <= last; ++i) {
       // the run is its window's first one unless it begins behind the window's first token
       float v[N];
