@@ -304,10 +304,10 @@ __device__ __forceinline__ void sum_rows(const SumArgs& s, const u32* places, in
 // Partial sums: N numbers at a multiple of N.
 template <int N> __device__ __forceinline__ void store_part(float* p, const float (&v)[N]) {
   if constexpr (N == 8) {
-    __stcg(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-    __stcg(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
   } else {
-    __stcg(p, v[0]);
+    p[0] = v[0];
   }
 }
 template <int N> __device__ __forceinline__ void load_part(const float* p, float (&v)[N]) {
@@ -328,44 +328,64 @@ __device__ __forceinline__ void finish_row(const SumArgs& s, long long v, long l
   Elems<O, N>::store((O*)s.dtable + v * s.dtable_stride + c * N, o);
 }
 
+// Columns c0 .. c1 - 1 of a row without tokens: zeros, or the base's numbers.  Sixteen bytes at a time but for the ends; element by element such
+// rows, most of a large table, took more instructions than the rest (118 us for 50257 rows of 1001).
+template <typename O>
+__device__ __forceinline__ void plain_row(const SumArgs& s, long long v, int c0, int c1, int t, int threads) {
+  constexpr int V = 16 / sizeof(O);
+  O* const to = (O*)s.dtable + v * s.dtable_stride;
+  const O* const from = s.base ? (const O*)s.base + v * s.base_stride : nullptr;
+  const int skew = (int)(((uintptr_t)(to + c0) & 15) / sizeof(O));
+  const int head = min(c1, c0 + (skew ? V - skew : 0));
+  const bool wide = !from || (((uintptr_t)from ^ (uintptr_t)to) & 15) == 0;
+  const int tail = wide ? head + (c1 - head) / V * V : head;   // behind the whole groups of sixteen bytes
+  for (int c = head + V * t; c < tail; c += V * threads)
+    *reinterpret_cast<uint4*>(to + c) = from ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0, 0, 0, 0);
+  for (int c = c0 + t; c < head; c += threads) to[c] = from ? from[c] : from_f<O>(0.f);
+  for (int c = tail + t; c < c1; c += threads) to[c] = from ? from[c] : from_f<O>(0.f);
+}
+
 // Rows v0 .. v0 + rows - 1 of the table: the tokens of row r are places[edge[r] - lo .. edge[r + 1] - lo).  TPR threads a row; of its
 // columns, every `of`-th part from `part` on.
 template <typename T, typename O, int N, int TPR>
 __device__ __forceinline__ void write_rows(const SumArgs& s, long long v0, int rows, const int* edge, const u32* places, int lo, int part, int of) {
   const long long vecs = s.cols / N;
+  const int t = threadIdx.x % TPR;
   for (int r = threadIdx.x / TPR; r < rows; r += SUM_CTA / TPR) {
     const int from = edge[r], to = edge[r + 1];
     if ((from == to && s.leave) || to - from > s.most) continue;
+    if (N == 1 && from == to) {
+      plain_row<O>(s, v0 + r, (int)(s.cols * part / of), (int)(s.cols * (part + 1) / of), t, TPR);
+      continue;
+    }
     if (N == 8 || vecs <= 2 * of * TPR) {
-      for (long long c = part * TPR + threadIdx.x % TPR; c < vecs; c += of * TPR) {
+      for (long long c = part * TPR + t; c < vecs; c += of * TPR) {
         float acc[N];
-        sum_rows<T, N, N == 8 ? 4 : 8>(s, places, from - lo, to - lo, c, acc);
+        sum_rows<T, N, N == 8 && sizeof(T) == 4 ? 4 : 8>(s, places, from - lo, to - lo, c, acc);
         finish_row<O, N>(s, v0 + r, c, acc);
       }
     } else if constexpr (N == 1) {                  // single elements of a long row: eight columns at a time, or their latencies add up
       constexpr int C = 8;
-      for (long long c = part * TPR + threadIdx.x % TPR; c < vecs; c += (long long)C * of * TPR) {
+      const int cols = (int)s.cols, step = of * TPR;
+      const O* const from_row = s.base ? (const O*)s.base + (v0 + r) * s.base_stride : nullptr;
+      O* const to_row = (O*)s.dtable + (v0 + r) * s.dtable_stride;
+      for (int c = part * TPR + t; c < cols; c += C * step) {
         float acc[C], base[C];
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-          const long long col = c + (long long)k * of * TPR;
           acc[k] = base[k] = 0.f;
-          if (s.base && col < vecs) base[k] = to_f(((const O*)s.base)[(v0 + r) * s.base_stride + col]);
+          if (from_row && c + k * step < cols) base[k] = to_f(from_row[c + k * step]);
         }
 #pragma unroll 2
         for (int i = from - lo; i < to - lo; ++i) {
           const T* const row = (const T*)s.dout + (long long)places[i] * s.dout_stride;
 #pragma unroll
-          for (int k = 0; k < C; ++k) {
-            const long long col = c + (long long)k * of * TPR;
-            if (col < vecs) acc[k] += to_f(row[col]);
-          }
+          for (int k = 0; k < C; ++k)
+            if (c + k * step < cols) acc[k] += to_f(row[c + k * step]);
         }
 #pragma unroll
-        for (int k = 0; k < C; ++k) {
-          const long long col = c + (long long)k * of * TPR;
-          if (col < vecs) ((O*)s.dtable)[(v0 + r) * s.dtable_stride + col] = from_f<O>(s.base ? fmaf(acc[k], s.scale, base[k]) : acc[k] * s.scale);
-        }
+        for (int k = 0; k < C; ++k)
+          if (c + k * step < cols) to_row[c + k * step] = from_f<O>(from_row ? fmaf(acc[k], s.scale, base[k]) : acc[k] * s.scale);
       }
     }
   }
@@ -380,32 +400,58 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __shared__ int edge[SUM_ROWS + 1];
   __shared__ u32 staged[SUM_STAGE];
+  __shared__ __align__(16) float shared[SUM_CTA * N];
   const unsigned long_ctas = (unsigned)s.windows * s.slices;
   if (blockIdx.x < long_ctas) {
     const int w = (int)(blockIdx.x / s.slices), lo = w * s.most, hi = min(s.n, lo + s.most);
     const int slice = (int)(blockIdx.x % s.slices);
-    // at most two long runs reach into a window: the one its first token belongs to and the one its last belongs to
-    // (none where no run crosses the window's ends)
-    const bool from_before = lo > 0 && __ldcg(s.keys + lo - 1) == __ldcg(s.keys + lo), goes_on = hi < s.n && __ldcg(s.keys + hi) == __ldcg(s.keys + hi - 1);
-    if (!from_before && !goes_on) return;
-    if (warp < 2) {
-      const u32 key = __ldcg(s.keys + (warp ? hi - 1 : lo));
-      const int a = lower_bound_warp(s.keys, 0, warp ? hi : lo + 1, key);
-      const int b = lower_bound_warp(s.keys, warp ? hi - 1 : lo, s.n, key + 1);
-      const bool longer = b - a > s.most && (long long)key < s.vocab;
+    // Two runs at most are long and reach into a window: the one its first token belongs to and, another one or the same, the one that goes on
+    // behind it.  A run is longer than `most` where the key `most` places before its end, or behind its start, is the same.
+    const u32 key = __ldcg(s.keys + (warp ? hi - 1 : lo));
+    const bool goes_on = hi < s.n && __ldcg(s.keys + hi) == __ldcg(s.keys + hi - 1);
+    if (warp == 0) {
+      const int end = lower_bound_warp(s.keys, lo, hi, key + 1);
+      bool longer = end == hi && goes_on;
+      if (!longer && end - s.most - 1 >= 0) longer = __ldcg(s.keys + end - s.most - 1) == key;
       if (lane == 0) {
-        edge[2 * warp] = longer ? a : 0;
-        edge[2 * warp + 1] = longer ? b : 0;
+        edge[0] = lo;
+        edge[1] = longer && (long long)key < s.vocab ? end : lo;
+        edge[4] = end == hi;
+      }
+    } else if (warp == 1) {
+      const int start = lower_bound_warp(s.keys, lo, hi, key);
+      const bool longer = goes_on && start + s.most < s.n && __ldcg(s.keys + start + s.most) == key;
+      if (lane == 0) {
+        edge[2] = start;
+        edge[3] = longer && (long long)key < s.vocab ? hi : start;
       }
     }
     __syncthreads();
     for (int k = 0; k < 2; ++k) {
-      const int a = edge[2 * k], b = edge[2 * k + 1];
-      if (b <= a || (k && edge[0] == a)) continue;                       // one run over the whole window: once
+      const int from = edge[2 * k], to = edge[2 * k + 1];
+      if (to <= from || (k && edge[4])) continue;                        // one run over the whole window: once
       float* const part = s.part + (2ll * w + k) * s.part_stride;
+      if (vecs <= SUM_CTA / 2) {                      // groups of threads take parts of the tokens, in order
+        int wide = 8;
+        while (wide < vecs) wide *= 2;
+        const int groups = SUM_CTA / wide, group = threadIdx.x / wide, c = threadIdx.x % wide;
+        float acc[N];
+        if (c < vecs) {
+          sum_rows<T, N, 4>(s, s.places, from + (int)((long long)(to - from) * group / groups), from + (int)((long long)(to - from) * (group + 1) / groups), c, acc);
+          store_part(shared + (group * wide + c) * N, acc);
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < (int)vecs * N; e += SUM_CTA) {
+          float sum = 0.f;
+          for (int i = 0; i < groups; ++i) sum += shared[i * wide * N + e];
+          __stcg(part + e, sum);
+        }
+        __syncthreads();
+        continue;
+      }
       for (long long c = (long long)slice * SUM_CTA + threadIdx.x; c < vecs; c += (long long)s.slices * SUM_CTA) {
         float acc[N];
-        sum_rows<T, N, 4>(s, s.places, max(a, lo), min(b, hi), c, acc);
+        sum_rows<T, N, 4>(s, s.places, from, to, c, acc);
         store_part(part + c * N, acc);
       }
     }
@@ -429,7 +475,7 @@ __global__ void __launch_bounds__(SUM_CTA) k_embedding_sum(SumArgs s) {
 }
 
 // Few tokens: no sort, no search.  Every CTA looks at all of them, in order, keeps those of its rows, and puts them in the rows' order; one kernel
-// instead of two, 24 -> 9 us for 1023 tokens and 1001 rows.
+// instead of three, 24 -> 13 us for 1023 tokens and 1001 rows of 333.
 constexpr int FEW_TOKENS = 1024, FEW_EACH = FEW_TOKENS / SUM_CTA, FEW_COLS = 1024;   // an id's tokens are one CTA's work there
 
 template <typename T, typename O, int N, int TPR>
@@ -553,8 +599,9 @@ int sum_launch(SumArgs s, const adacgd_embedding_backward_args& a, const Where& 
 template <typename T, typename O, int N>
 int sum_by_width(const SumArgs& s, const adacgd_embedding_backward_args& a, const Where& at) {
   const long long vecs = s.cols / N;
-  if (vecs <= 16) return sum_launch<T, O, N, 8>(s, a, at);
-  if (vecs <= 64) return sum_launch<T, O, N, 32>(s, a, at);
+  if (vecs <= 8) return sum_launch<T, O, N, 8>(s, a, at);
+  if (vecs <= 32) return sum_launch<T, O, N, 32>(s, a, at);
+  if (vecs <= 64) return sum_launch<T, O, N, 64>(s, a, at);
   return sum_launch<T, O, N, 256>(s, a, at);
 }
 template <typename T, typename O>
