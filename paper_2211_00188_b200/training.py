@@ -228,7 +228,8 @@ class TrainingOps:
     def qk_norm(self, q, k, q_out, k_out, positions=None, freq=None, *, head_dim: int, q_weight=None, k_weight=None, eps: float = 1e-6,
                 interleaved: bool = False):
         """adacgd_qk_norm: every head of q and k divided by its root mean square, times the weight, its first 2 len(freq) elements
-        turned by the angles position * freq (float32), in halves or, interleaved, in neighbours.  k and k_out may be None."""
+        turned by the angles position * freq (float32), in halves or, interleaved, in neighbours.  positions are int64 or int32; without
+        freq there is no rotation.  k and k_out may be None."""
         call = self.native.qk_norm
         args = (self.handle, q, k, q_out, k_out, positions, freq, head_dim, q_weight, k_weight, eps, interleaved)
         status = call(*args)
@@ -250,7 +251,7 @@ class TrainingOps:
                   scale: Optional[float] = None, mask=None):
         """adacgd_attention over each sequence's tokens; scale defaults to head_dim ** -0.5.  k and v hold the key heads, whose number
         divides heads.  lse, float32 [heads, tokens], is what the backward pass needs.  Tokens where the mask is false are neither
-        queries nor keys; their out is 0."""
+        queries nor keys; their out is 0.  Rows of no sequence stay as they are.  No output may overlap anything."""
         if sequences is None and seq_start is None:
             raise ValueError("attention needs sequences or seq_start")
         call = self.native.attention

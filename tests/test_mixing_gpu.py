@@ -598,3 +598,56 @@ def test_no_tokens(ops):
     lse = torch.empty(2, 0, device="cuda")
     ops.attention(e(16), e(8), e(8), e(16), heads=2, lse=lse, sequences=1)
     ops.attention_backward(e(16), e(16), e(8), e(8), e(16), lse, torch.empty(2, 0, device="cuda"), e(16), e(8), e(8), heads=2, sequences=1)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("count", [31, 32, 40, 1000])
+def test_attention_of_many_sequences(ops, dtype, count):
+    """More sequences than a warp looks at in one round, empty ones among them."""
+    rng = np.random.default_rng(count)
+    lengths = rng.integers(0, 4, count)
+    lengths[rng.integers(0, count)] = 150
+    dt, n = TYPES[dtype], int(lengths.sum())
+    _, make, q, k, v = attention_case(n, 2, 1, 64, dt, count)
+    kw = dict(seq_start=ints(np.concatenate([[0], np.cumsum(lengths)]), torch.int32))
+    out, lse, d = check_attention(ops, q, k, v, 2, dt, make, True, None, kw)
+    check_attention_backward(ops, q, k, v, out, lse, 2, dt, make, True, None, kw, d)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("counted", [(300, 420), (0, 130), (560, 700), (128, 256), (699, 700)])
+def test_attention_of_tiles_without_a_counted_token(ops, dtype, causal, counted):
+    """Whole tiles of padding in front of and behind the tokens, and a hole among them; the padding holds NaN."""
+    dt, n, heads, kv, dim = TYPES[dtype], 700, 2, 1, 64
+    rng, make, q, k, v = attention_case(n, heads, kv, dim, dt, counted[0])
+    mask = np.zeros(n, bool)
+    mask[counted[0]:counted[1]] = True
+    if counted[1] - counted[0] > 50:
+        mask[counted[0] + 20:counted[0] + 30] = False
+    off = torch.from_numpy(~mask).cuda()
+    for t in (q, k, v):
+        t[off] = float("nan")
+    kw = dict(sequences=1)
+    out, lse, d = check_attention(ops, q, k, v, heads, dt, make, causal, mask, kw)
+    dout = make(heads * dim, 0.5)
+    dout[off] = float("nan")
+    check_attention_backward(ops, q, k, v, out, lse, heads, dt, make, causal, mask, kw, d, dout=dout)
+
+
+@pytest.mark.parametrize("size", [1e-4, 1.0, 200.0])
+def test_small_and_large_gradients_in_float16(ops, size):
+    """ds is brought into the type's range before it is rounded: gradients of 1e-4 keep its eleven bits, gradients of 200 do not overflow."""
+    dt, n, heads, kv, dim = torch.float16, 1000, 2, 1, 64
+    _, make, q, k, v = attention_case(n, heads, kv, dim, dt, 12)
+    out, lse = make(heads * dim), torch.empty(heads, n, device="cuda")
+    ops.attention(q, k, v, out, heads=heads, lse=lse, sequences=1, causal=False)
+    dout = make(heads * dim, size)
+    dq, dk, dv, dot = make(heads * dim), make(kv * dim), make(kv * dim), torch.empty(heads, n, device="cuda")
+    ops.attention_backward(dout, q, k, v, out, lse, dot, dq, dk, dv, heads=heads, sequences=1, causal=False)
+    r = O.attention_backward(host(dout), host(q), host(k), host(v), host(out), host(lse), heads, sequences=1, causal=False)
+    for name, got in (("dq", dq), ("dk", dk), ("dv", dv)):
+        # p or ds and the result are each off by at most 2^-11 of themselves, by chance in a sum: less than 2^-10 of the whole; the results' own
+        # smallest step, 2^-24, adds half of itself an element
+        lim = 2.0 ** -10 * np.linalg.norm(r[name]) + 2.0 ** -25 * np.sqrt(r[name].size)
+        assert np.linalg.norm(host(got) - r[name]) < lim, name
