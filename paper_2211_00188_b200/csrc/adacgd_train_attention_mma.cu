@@ -572,7 +572,10 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
   const int head = (int)(blockIdx.x % a.heads);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Tile t;
-  if (!tile_of(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, TILE, &t)) return;
+  if (!tile_of(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, TILE, &t)) {
+    if (!BF16) asm volatile("griddepcontrol.wait;" ::: "memory");   // this kernel ends after the one before it, whatever there is to do
+    return;
+  }
   int begin, end;                                              // tiles of keys
   trim(a, t, reinterpret_cast<int*>(mma_smem), &begin, &end);
   if (t.first / TILE < begin || t.first / TILE >= end) {        // no row that counts
@@ -581,7 +584,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
       zero_row(g.dq, g.dq_stride, t.row + i, head, a.head_dim);
       if (BF16) g.row_dot[(long long)head * a.tokens + t.row + i] = 0.f;
     }
-    if (!BF16) asm volatile("griddepcontrol.wait;" ::: "memory");   // this kernel ends after the one before it, whatever there is to do
+    if (!BF16) asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
   }
   const int last = a.causal ? t.first / TILE + 1 : end, n = last - begin;
