@@ -22,6 +22,7 @@ namespace {
 constexpr int TILE = 128, HALF = TILE * 128;       // rows of a tile; bytes of 64 of its columns
 constexpr int FWD_CTA = 384, FWD_ROWS = 8;         // threads; warps that hold rows, before the product and the copying warp
 constexpr int BWD_CTA = 576, BWD_ROWS = 16;
+constexpr int MOST_SMEM = 227 * 1024;              // a CTA's shared memory
 
 struct Maps {
   CUtensorMap q, k, v, dout;
@@ -79,7 +80,8 @@ __device__ __forceinline__ bool bring(u32 dst, const CUtensorMap* map, int head,
 __device__ __forceinline__ void settle(u32 bar, u32 parity) { mbar_wait(bar, parity, nullptr); }
 
 // The tiles of the item's sequence between its first and its last token that counts: [begin, end), none if nothing counts.  A padded
-// batch has nothing but padding in the others.  By the whole CTA, whose shared memory is not in use yet.
+// batch has nothing but padding in the others.  By the whole CTA.  The scratch lies where no tensor copy arrives: nothing orders these accesses
+// before a copy's writes.
 __device__ __forceinline__ void trim(const adacgd_attention_inputs& a, const Tile& t, int* scratch, int* begin, int* end) {
   *begin = 0;
   *end = (t.length + TILE - 1) / TILE;
@@ -204,7 +206,8 @@ __device__ __forceinline__ u32 low_bits(int n) { return n <= 0 ? 0u : (n >= 32 ?
 // division by the sum at the end takes it out.  binary16 has few numbers below 1: there p is taken 2^7 times larger, at most 2^15.
 template <int DP> struct FwdLayout {
   static constexpr int BYTES = DP * 256, STAGES = DP == 128 ? 5 : 8, RING = 2 * BYTES, BARS = RING + STAGES * BYTES;
-  static constexpr int TOTAL = BARS + 256;
+  static constexpr int TOTAL = BARS + 256, SCRATCH = TOTAL - 8;
+  static_assert(64 + 16 * STAGES + 8 <= SCRATCH - BARS && TOTAL <= MOST_SMEM, "barriers, trim's scratch, the CTA's shared memory");
 };
 
 template <bool BF16, int DP>
@@ -222,7 +225,7 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int kh = head / (a.heads / a.key_heads);
   int begin, end, count[2];                                    // tiles of keys; how many of them A and B meet
-  trim(a, t, reinterpret_cast<int*>(mma_smem), &begin, &end);
+  trim(a, t, reinterpret_cast<int*>(mma_smem + L::SCRATCH), &begin, &end);
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const int mine = t.first / TILE + x;                       // without a row that counts: none
@@ -561,7 +564,8 @@ __device__ __forceinline__ float range_of(const float* most) {
 // conversions and exponentials nothing filled (4600 clocks a step; 1536 of products).
 template <int DP> struct DqLayout {
   static constexpr int BYTES = DP * 256, KS = DP == 128 ? 3 : 4, VS = DP == 128 ? 2 : 4, RING = 2 * BYTES;
-  static constexpr int PART = RING + (KS + VS) * BYTES, BARS = PART + 4 * TILE * 4, TOTAL = BARS + 256;
+  static constexpr int PART = RING + (KS + VS) * BYTES, BARS = PART + 4 * TILE * 4, TOTAL = BARS + 256, SCRATCH = TOTAL - 8;
+  static_assert(64 + 16 * (KS + VS) + 8 <= SCRATCH - BARS && TOTAL <= MOST_SMEM, "barriers, trim's scratch, the CTA's shared memory");
 };
 
 template <bool BF16, int DP>
@@ -577,7 +581,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
     return;
   }
   int begin, end;                                              // tiles of keys
-  trim(a, t, reinterpret_cast<int*>(mma_smem), &begin, &end);
+  trim(a, t, reinterpret_cast<int*>(mma_smem + L::SCRATCH), &begin, &end);
   if (t.first / TILE < begin || t.first / TILE >= end) {        // no row that counts
     const int i = t.first + (int)threadIdx.x;
     if (threadIdx.x < TILE && i < t.length) {
@@ -780,7 +784,8 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
 // a step, of which the products take 2048.)
 template <int DP> struct DkvLayout {
   static constexpr int BYTES = DP * 256, STAGES = DP == 128 ? 5 : 8, RING = 2 * BYTES, STATS = RING + STAGES * BYTES;
-  static constexpr int BARS = STATS + 2 * 2 * TILE * 4, TOTAL = BARS + 256;
+  static constexpr int BARS = STATS + 2 * 2 * TILE * 4, TOTAL = BARS + 256, SCRATCH = TOTAL - 8;
+  static_assert(56 + 16 * STAGES + 8 <= SCRATCH - BARS && TOTAL <= MOST_SMEM, "barriers, trim's scratch, the CTA's shared memory");
 };
 
 template <bool BF16, int DP>
@@ -795,7 +800,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
     return;
   }
   int low_tile, high_tile;                                     // of queries
-  trim(a, t, reinterpret_cast<int*>(mma_smem), &low_tile, &high_tile);
+  trim(a, t, reinterpret_cast<int*>(mma_smem + L::SCRATCH), &low_tile, &high_tile);
   if (t.first / TILE < low_tile || t.first / TILE >= high_tile) {   // no key that counts
     const int i = t.first + (int)threadIdx.x;
     if (threadIdx.x < TILE && i < t.length) {

@@ -41,3 +41,36 @@ def test_dependent_kernels_wait_before_each_return(unit):
     for name, _, body in kernels(source(unit)):
         if WAIT.search(body):
             assert not returns_before_the_wait(body), name
+
+
+def layouts():
+    """{kernel: (names and byte offsets of its shared memory for heads of up to 64, of up to 128)}: the constants as the source computes them."""
+    text = source("adacgd_train_attention_mma.cu")
+    out = {}
+    for name, kernel in (("FwdLayout", "k_attention_mma"), ("DqLayout", "k_attention_dq_mma"), ("DkvLayout", "k_attention_dkv_mma")):
+        body = re.search(r"struct " + name + r" \{(.*?)\};", text, re.S).group(1)
+        sizes = []
+        for dp in (64, 128):
+            at = {"DP": dp, "TILE": 128}
+            for line in re.findall(r"static constexpr int ([^;]*);", body):
+                for part in line.split(","):
+                    left, right = (x.strip() for x in part.split("=", 1))
+                    right = re.sub(r"(.+?)\s*\?\s*(.+?)\s*:\s*(.+)", r"(\2) if (\1) else (\3)", right)
+                    at[left] = eval(right, {}, at)
+            sizes.append(at)
+        out[kernel] = sizes
+    return out
+
+
+def test_no_tensor_copy_arrives_where_plain_accesses_came_before():
+    """Plain writes to shared memory are not ordered before a copy's writes to the same bytes by a barrier alone.  So the two words in which a CTA
+    joins the ends of its mask lie behind the tiles and behind the barriers, inside what the CTA has."""
+    text = source("adacgd_train_attention_mma.cu")
+    bodies = {name: body for name, _, body in kernels(text)}
+    for kernel, sizes in layouts().items():
+        scratch = re.findall(r"\btrim\(a, t, ([^;]*?), &", bodies[kernel])
+        assert scratch == ["reinterpret_cast<int*>(mma_smem + L::SCRATCH)"], kernel
+        for at in sizes:
+            stages = at["STAGES"] if "STAGES" in at else at["KS"] + at["VS"]
+            tiles = at["RING"] + stages * at["BYTES"]                       # all that copies write
+            assert tiles <= at["BARS"] and at["BARS"] + 64 + 16 * stages + 8 <= at["SCRATCH"] and at["SCRATCH"] + 8 <= at["TOTAL"] <= 227 * 1024, kernel
