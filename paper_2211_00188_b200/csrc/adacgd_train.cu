@@ -576,7 +576,7 @@ adacgd_status adacgd_attention_backward(adacgd_train* t, const adacgd_attention_
   const adacgd_status st = check_device(t, entry);
   if (st != ADACGD_OK) return st;
   if (n == 0) return ADACGD_OK;
-  return launched(t, entry, launch_attention_backward(t->s, *g, t->at));
+  return launched(t, entry, launch_attention_backward(*g, t->at));
 }
 
 }  // extern "C"

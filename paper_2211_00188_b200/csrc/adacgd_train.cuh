@@ -27,7 +27,6 @@ struct TrainScratch {
   long long max_tokens, max_cols;
 };
 constexpr int NTRAIN_TICKETS = 64;
-constexpr int ATTENTION_TICKET = 63;   // the losses count from the front
 constexpr int MAX_SMALL_CTAS = 2048;   // of a small policy loss: a row each at most
 
 // Where a call runs.
@@ -65,7 +64,7 @@ int launch_embedding_backward(const TrainScratch& s, const adacgd_embedding_back
 int launch_qk_norm(const adacgd_qk_norm_args& a, const Where& at);
 int launch_qk_norm_backward(const TrainScratch& s, const adacgd_qk_norm_backward_args& a, const Where& at);
 int launch_attention(const adacgd_attention_args& a, const Where& at);
-int launch_attention_backward(const TrainScratch& s, const adacgd_attention_backward_args& a, const Where& at);
+int launch_attention_backward(const adacgd_attention_backward_args& a, const Where& at);
 
 // ---- element types ----
 __device__ __forceinline__ float to_f(float v) { return v; }

@@ -387,8 +387,8 @@ int launch_attention(const adacgd_attention_args& a, const Where& at) {
   BY_TYPE(a.in.dtype, (fwd_t<T>(a, at)))
 }
 
-int launch_attention_backward(const TrainScratch& s, const adacgd_attention_backward_args& a, const Where& at) {
-  const int n = launch_attention_backward_mma(s, a, at);
+int launch_attention_backward(const adacgd_attention_backward_args& a, const Where& at) {
+  const int n = launch_attention_backward_mma(a, at);
   if (n) return n;
   BY_TYPE(a.in.dtype, (bwd_t<T>(a, at)))
 }

@@ -8,7 +8,7 @@ namespace adacgd {
 
 // Each returns the number of kernels launched, -1 after a failed launch, or 0 where it does not take the call.
 int launch_attention_mma(const adacgd_attention_args& a, const Where& at);
-int launch_attention_backward_mma(const TrainScratch& ws, const adacgd_attention_backward_args& a, const Where& at);
+int launch_attention_backward_mma(const adacgd_attention_backward_args& a, const Where& at);
 
 // Sequences are cut into tiles of B rows.  With seq_start the host does not know their lengths: sequence q gets the tile numbers
 // from floor(start / B) + q on, which leaves room for ceil(length / B) of them, and the numbers behind a sequence's last tile do nothing.

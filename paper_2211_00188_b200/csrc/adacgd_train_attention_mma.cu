@@ -429,130 +429,93 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
 // backward: the range of ds
 // --------------------------------------------------------------------------
 // bfloat16 holds ds as it is.  binary16 would lose what is below 2^-14, and gradients are often that small, so there ds is multiplied by a power
-// of two that brings the largest one possible, |dout_i| (|v_j| + |out_i|) <= 2 max|dout_i| max|v_j|, below 2^14.  This kernel takes those two
-// maxima, a pair a CTA, and the rows' products dout.out; LPR lanes take a head's row, four rows at a time.
-constexpr int DOT_CTA = 256, DOT_CTAS = NORM_PARTS - 1, DOT_ROWS = 4;
+// of two that brings the largest one possible, |dout_i| (|v_j| + |out_i|) <= 2 |dout_i| max|v|, below 2^14.  For dq that is a factor a row: the
+// row's own |dout_i| and the largest |v| of its sequence and key head.  dk sums over the rows, so there it is the largest |dout| of the sequence and of the
+// heads that share the key head.  What other sequences and key heads hold has no part in it.
+// This kernel takes the maxima of a tile, squared, a CTA one tile, key head and part of the heads that share it; LPR lanes take a head's row, four
+// rows at a time.  They wait in the rows of dv, which are written last: in the tile's first row and the key head's columns, the parts' maxima of |dout|, then that
+// of |v|.  The kernel of dq joins those of its sequence, and the first of a group's heads leaves what dk needs in its tile's own first row of dk: there it is read
+// and overwritten by one CTA.
+constexpr int RANGE_CTA = 256, RANGE_ROWS = 4;
 
-// Row number i as a token (behind the first one) and a head.
-__device__ __forceinline__ void row_of(long long i, int heads, long long* t, int* h) {
-  if (i >> 32) {
-    *t = i / heads;
-    *h = (int)(i % heads);
-  } else {
-    *t = (u32)i / (u32)heads;
-    *h = (int)((u32)i % (u32)heads);
-  }
+// Parts of a group of heads: as many as there are heads, and room for their maxima.
+__host__ __device__ __forceinline__ int range_parts(const adacgd_attention_inputs& a) {
+  const int group = a.heads / a.key_heads, room = a.head_dim / 2 - 1;
+  return group < room ? group : room;
+}
+__device__ __forceinline__ float* range_at(void* base, long long stride, long long row, int kh, int dim) {
+  return reinterpret_cast<float*>((char*)base + (row * stride + (long long)kh * dim) * 2);
 }
 
 template <int LPR>
-__global__ void __launch_bounds__(DOT_CTA) k_attention_dot(adacgd_attention_backward_args g, float* most, u32* ticket) {
+__global__ void __launch_bounds__(RANGE_CTA) k_attention_range(adacgd_attention_backward_args g) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const adacgd_attention_inputs& a = g.in;
-  const int lane = threadIdx.x % LPR, d = lane * 8;
+  constexpr int GROUPS = RANGE_CTA / LPR;
+  Tile t;
+  if (!tile_of(a, blockIdx.x, TILE, &t)) return;
+  const int lane = threadIdx.x % LPR, mine = threadIdx.x / LPR, d = lane * 8, kh = (int)blockIdx.y, part = (int)blockIdx.z, parts = (int)gridDim.z;
   const bool in = d < a.head_dim;
-  constexpr int GROUPS = DOT_CTA / LPR;
-  long long lo = 0, hi = a.tokens, unused;
-  if (a.seq_start) {                                  // rows of no sequence keep their row_dot and do not count
-    seq_bounds(a.seq_start, 0, a.tokens, 0, &lo, &unused);
-    seq_bounds(a.seq_start, a.sequences - 1, a.tokens, 0, &unused, &hi);
-  }
-  auto sum = [](float v) {
-#pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-  };
-  float mo = 0.f, mv = 0.f;
-  const long long queries = (hi - lo) * a.heads, keys = (hi - lo) * a.key_heads;
-  // a CTA's rows of a round lie side by side
-  for (long long i0 = (long long)blockIdx.x * GROUPS * DOT_ROWS; i0 < queries; i0 += (long long)gridDim.x * GROUPS * DOT_ROWS) {
-    Run<__half> x[DOT_ROWS], y[DOT_ROWS];
-    long long t[DOT_ROWS];
-    int h[DOT_ROWS];
-    bool on[DOT_ROWS];
-#pragma unroll
-    for (int u = 0; u < DOT_ROWS; ++u) {
-      const long long i = i0 + u * GROUPS + threadIdx.x / LPR;
-      row_of(i < queries ? i : 0, a.heads, &t[u], &h[u]);
-      t[u] += lo;
-      on[u] = i < queries && (!a.mask || a.mask[t[u]]);
-      if (on[u] && in) {
-        x[u] = load_run((const __half*)g.dout + t[u] * g.dout_stride + (long long)h[u] * a.head_dim + d);
-        y[u] = load_run((const __half*)g.out + t[u] * g.out_stride + (long long)h[u] * a.head_dim + d);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < DOT_ROWS; ++u) {
-      float p[8], q[8], dot = 0.f, sq = 0.f;
-      if (on[u] && in) {
-        unpack(x[u], p);
-        unpack(y[u], q);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          dot = fmaf(p[k], q[k], dot);
-          sq = fmaf(p[k], p[k], sq);
-        }
-      }
-      dot = sum(dot);
-      mo = fmaxf(mo, sum(sq));
-      if (lane == 0 && i0 + u * GROUPS + threadIdx.x / LPR < queries) g.row_dot[(long long)h[u] * a.tokens + t[u]] = dot;
-    }
-  }
-  for (long long i0 = (long long)blockIdx.x * GROUPS; i0 < keys; i0 += (long long)gridDim.x * GROUPS) {
-    const long long i = i0 + threadIdx.x / LPR;
-    long long t;
-    int h;
-    row_of(i < keys ? i : 0, a.key_heads, &t, &h);
-    t += lo;
-    float x[8], sq = 0.f;
-    if (i < keys && in && (!a.mask || a.mask[t])) {
-      unpack(load_run((const __half*)a.v + t * a.v_stride + (long long)h * a.head_dim + d), x);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) sq = fmaf(x[k], x[k], sq);
-    }
-    mv = fmaxf(mv, sum(sq));
-  }
-  __shared__ float part[2][GROUPS];
-  if (lane == 0) {
-    part[0][threadIdx.x / LPR] = mo;
-    part[1][threadIdx.x / LPR] = mv;
-  }
-  __syncthreads();
-  __shared__ bool last;
-  if (threadIdx.x < 2) {
+  const int group = a.heads / a.key_heads, h0 = (int)((long long)group * part / parts), heads = (int)((long long)group * (part + 1) / parts) - h0;
+  const int rows = min(TILE, t.length - t.first);
+  const long long row = t.row + t.first;
+  auto largest = [&](const void* base, long long stride, int head, int count) {   // of |x|^2 over the tile's rows and `count` heads
     float m = 0.f;
-    for (int i = 0; i < GROUPS; ++i) m = fmaxf(m, part[threadIdx.x][i]);
-    __stcg(most + 2 + 2 * blockIdx.x + threadIdx.x, m);
-    __threadfence();
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(ticket, 1u) + 1 == gridDim.x;
-  __syncthreads();
-  if (!last || threadIdx.x >= 32) return;                     // the last CTA to finish joins them
-  __threadfence();
-  float a0 = 0.f, a1 = 0.f;
-  for (int i = threadIdx.x; i < (int)gridDim.x; i += 32) {
-    const float2 m = __ldcg(reinterpret_cast<const float2*>(most) + 1 + i);
-    a0 = fmaxf(a0, m.x);
-    a1 = fmaxf(a1, m.y);
-  }
+    for (int i0 = 0; i0 < rows * count; i0 += GROUPS * RANGE_ROWS) {             // heads of a row lie side by side
+      Run<__half> x[RANGE_ROWS];
+      bool on[RANGE_ROWS];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    a0 = fmaxf(a0, __shfl_xor_sync(0xffffffffu, a0, o));
-    a1 = fmaxf(a1, __shfl_xor_sync(0xffffffffu, a1, o));
+      for (int u = 0; u < RANGE_ROWS; ++u) {
+        const int i = i0 + u * GROUPS + mine, r = i / count;
+        on[u] = in && r < rows && (!a.mask || a.mask[row + r]);
+        if (on[u]) x[u] = load_run((const __half*)base + (row + r) * stride + (long long)(head + i - r * count) * a.head_dim + d);
+      }
+#pragma unroll
+      for (int u = 0; u < RANGE_ROWS; ++u) {
+        float v[8], sq = 0.f;
+        if (on[u]) {
+          unpack(x[u], v);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) sq = fmaf(v[k], v[k], sq);
+        }
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+        m = fmaxf(m, sq);
+      }
+    }
+    return m;
+  };
+  __shared__ float most[2][GROUPS];
+  const float mo = largest(g.dout, g.dout_stride, kh * group + h0, heads), mv = part == 0 ? largest(a.v, a.v_stride, kh, 1) : 0.f;
+  if (lane == 0) {
+    most[0][mine] = mo;
+    most[1][mine] = mv;
   }
-  if (threadIdx.x == 0) {
-    most[0] = a0;
-    most[1] = a1;
-    *ticket = 0;
+  __syncthreads();
+  if (threadIdx.x < (part == 0 ? 2 : 1)) {
+    float m = 0.f;
+    for (int i = 0; i < GROUPS; ++i) m = fmaxf(m, most[threadIdx.x][i]);
+    __stcg(range_at(g.dv, g.dv_stride, row, kh, a.head_dim) + (threadIdx.x ? parts : part), m);
   }
 }
 
-// The power of two.
-__device__ __forceinline__ float range_of(const float* most) {
-  const float2 m = __ldcg(reinterpret_cast<const float2*>(most));
-  const float bound = 2.002f * sqrtf(m.x) * sqrtf(m.y);
+// The power of two, of the squares of the largest |dout| and |v|.
+__device__ __forceinline__ float range_of(float dout2, float v2) {
+  const float bound = 2.002f * sqrtf(dout2) * sqrtf(v2);
   if (!(bound > 0.f) || isinf(bound)) return 1.f;
   return __int_as_float(((int)fminf(fmaxf(13.f - floorf(log2f(bound)), -60.f), 60.f) + 127) << 23);
+}
+// The largest of numbers [from, to) of the sequence's tiles begin .. end - 1: by a warp.
+__device__ __forceinline__ float join_range(const adacgd_attention_backward_args& g, const Tile& t, int kh, int begin, int end, int from, int to) {
+  const int each = to - from;
+  float m = 0.f;
+  for (long long i = threadIdx.x & 31; i < (long long)(end - begin) * each; i += 32) {
+    const long long k = i / each;
+    m = fmaxf(m, __ldcg(range_at(g.dv, g.dv_stride, t.row + (begin + k) * TILE, kh, g.in.head_dim) + from + (i - k * each)));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  return m;
 }
 
 // --------------------------------------------------------------------------
@@ -569,7 +532,7 @@ template <int DP> struct DqLayout {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most) {
+__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g) {
   typedef DqLayout<DP> L;
   extern __shared__ __align__(1024) unsigned char mma_smem[];
   const adacgd_attention_inputs& a = g.in;
@@ -586,7 +549,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
     const int i = t.first + (int)threadIdx.x;
     if (threadIdx.x < TILE && i < t.length) {
       zero_row(g.dq, g.dq_stride, t.row + i, head, a.head_dim);
-      if (BF16) g.row_dot[(long long)head * a.tokens + t.row + i] = 0.f;
+      g.row_dot[(long long)head * a.tokens + t.row + i] = 0.f;
     }
     if (!BF16) asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
@@ -689,28 +652,41 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
     const u32 lanes = (u32)(warp & 3) << 21;
     const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
     const long long at = (long long)head * a.tokens + t.row + i;
-    float dot = 0.f, range = 1.f;
-    if (BF16) {
-      if (on) {                                                // each quarter of the warps takes 32 of the head's elements
-        const __nv_bfloat16* const x = (const __nv_bfloat16*)g.dout + (t.row + i) * g.dout_stride + (long long)head * a.head_dim;
-        const __nv_bfloat16* const y = (const __nv_bfloat16*)g.out + (t.row + i) * g.out_stride + (long long)head * a.head_dim;
-        for (int d = 32 * part_of; d < min(a.head_dim, 32 * part_of + 32); d += 8) {
-          float u[8], v[8];
-          unpack(load_run(x + d), u);
-          unpack(load_run(y + d), v);
+    typedef typename std::conditional<BF16, __nv_bfloat16, __half>::type T;
+    float dot = 0.f, sq = 0.f, range = 1.f;
+    if (on) {                                                  // each quarter of the warps takes 32 of the head's elements
+      const T* const x = (const T*)g.dout + (t.row + i) * g.dout_stride + (long long)head * a.head_dim;
+      const T* const y = (const T*)g.out + (t.row + i) * g.out_stride + (long long)head * a.head_dim;
+      for (int d = 32 * part_of; d < min(a.head_dim, 32 * part_of + 32); d += 8) {
+        float u[8], v[8];
+        unpack(load_run(x + d), u);
+        unpack(load_run(y + d), v);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) dot = fmaf(u[k], v[k], dot);
+        for (int k = 0; k < 8; ++k) {
+          dot = fmaf(u[k], v[k], dot);
+          if (!BF16) sq = fmaf(u[k], u[k], sq);
         }
       }
-      part[part_of * TILE + r] = dot;
+    }
+    auto row_sum = [&](float v) {                              // of the row's four threads
+      part[part_of * TILE + r] = v;
       asm volatile("bar.sync 1, 512;" ::: "memory");
-      dot = (part[r] + part[TILE + r]) + (part[2 * TILE + r] + part[3 * TILE + r]);
-      if (part_of == 0 && inside) g.row_dot[at] = dot;
-    } else {
+      return (part[r] + part[TILE + r]) + (part[2 * TILE + r] + part[3 * TILE + r]);
+    };
+    dot = row_sum(dot);
+    if (part_of == 0 && inside) g.row_dot[at] = dot;
+    if (!BF16) {
+      asm volatile("bar.sync 1, 512;" ::: "memory");           // the sums before have been read
+      sq = row_sum(sq);
       asm volatile("griddepcontrol.wait;" ::: "memory");
-      if (on) dot = __ldcg(g.row_dot + at);
-      range = range_of(most);
+      const int parts = range_parts(a);
+      const float most = join_range(g, t, kh, begin, end, parts, parts + 1);
+      range = range_of(sq, most);
       dot *= range;
+      if (warp == 0 && head == kh * (a.heads / a.key_heads)) {
+        const float all = join_range(g, t, kh, begin, end, 0, parts);
+        if (lane == 0) __stcg(reinterpret_cast<float2*>(range_at(g.dk, g.dk_stride, t.row + t.first, kh, a.head_dim)), make_float2(all, most));
+      }
     }
     const float low = on ? -g.lse[at] * LOG2E : -INFINITY, c = a.scale * LOG2E;
     const F2 c2 = f2(c, c), low2 = f2(low, low), dot2 = f2(-dot, -dot), range2 = f2(range, range);
@@ -789,7 +765,7 @@ template <int DP> struct DkvLayout {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g, const float* most) {
+__global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_constant__ Maps maps, adacgd_attention_backward_args g) {
   typedef DkvLayout<DP> L;
   extern __shared__ __align__(1024) unsigned char mma_smem[];
   const adacgd_attention_inputs& a = g.in;
@@ -803,11 +779,11 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   trim(a, t, reinterpret_cast<int*>(mma_smem + L::SCRATCH), &low_tile, &high_tile);
   if (t.first / TILE < low_tile || t.first / TILE >= high_tile) {   // no key that counts
     const int i = t.first + (int)threadIdx.x;
+    asm volatile("griddepcontrol.wait;" ::: "memory");           // dv still holds what the kernel before reads
     if (threadIdx.x < TILE && i < t.length) {
       zero_row(g.dk, g.dk_stride, t.row + i, kh, a.head_dim);
       zero_row(g.dv, g.dv_stride, t.row + i, kh, a.head_dim);
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
   }
   const u32 base = smem_addr(mma_smem), bars = base + L::BARS;
@@ -843,6 +819,10 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   const u32 k_tile = base, v_tile = base + L::BYTES, ring = base + L::RING;
   // binary16: p is taken 2^14 times larger, ds by its range (see above)
   const float shift = BF16 ? 0.f : 14.f, back = BF16 ? 1.f : 6.103515625e-05f;
+  auto own_range = [&] {
+    const float2 m = __ldcg(reinterpret_cast<const float2*>(range_at(g.dk, g.dk_stride, t.row + t.first, kh, a.head_dim)));
+    return range_of(m.x, m.y);
+  };
   const int begin = a.causal ? t.first / TILE : low_tile, each = high_tile - begin, n = each * group;
   if (warp == BWD_ROWS + 1) {
     u32 side = 0, words[4];
@@ -862,7 +842,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
         if (i >= 4 && L::STAGES > 5 && !mbar_wait(empty + 8 * ((i - 5) % L::STAGES), ((i - 5) / L::STAGES) & 1, dead)) break;
         if (i == 1) {                                          // row_dot comes from the kernel before this one
           asm volatile("griddepcontrol.wait;" ::: "memory");
-          if (!BF16) range = range_of(most);
+          if (!BF16) range = own_range();
         }
         float* const to = stats + (j & 1) * 2 * TILE;
         const long long at = (long long)head * a.tokens + t.row + first;
@@ -921,7 +901,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
     float range = 1.f;
     if (!BF16) {
       asm volatile("griddepcontrol.wait;" ::: "memory");
-      range = range_of(most);
+      range = own_range();
     }
     const float c = a.scale * LOG2E;
     const F2 c2 = f2(c, c), range2 = f2(range * back, range * back);
@@ -1063,18 +1043,15 @@ template <bool BF16, int DP> int fwd_mma(const Maps& m, const adacgd_attention_a
   static std::atomic<int> table[TRAIN_DEVICES];
   return launch_mma(k_attention_mma<BF16, DP>, table, FWD_CTA, FwdLayout<DP>::TOTAL, tile_slots(g.in, 2 * TILE) * g.in.heads, false, at, m, g) ? 1 : -1;
 }
-template <bool BF16, int DP> int bwd_mma(const TrainScratch& ws, const Maps& m, const adacgd_attention_backward_args& g, const Where& at) {
+template <bool BF16, int DP> int bwd_mma(const Maps& m, const adacgd_attention_backward_args& g, const Where& at) {
   static std::atomic<int> table[2][TRAIN_DEVICES];
   const long long slots = tile_slots(g.in, TILE);
-  const float* const most = ws.norm_part;                      // of at least 2 * NORM_PARTS numbers
   if (!BF16) {
-    constexpr int LPR = DP / 8;
-    const long long rows = DOT_CTA / LPR * DOT_ROWS, want = (g.in.tokens * g.in.heads + rows - 1) / rows;
-    k_attention_dot<LPR><<<(unsigned)(want < DOT_CTAS ? want : DOT_CTAS), DOT_CTA, 0, at.stream>>>(g, ws.norm_part, ws.tickets + ATTENTION_TICKET);
+    k_attention_range<DP / 8><<<dim3((unsigned)slots, (unsigned)g.in.key_heads, (unsigned)range_parts(g.in)), RANGE_CTA, 0, at.stream>>>(g);
     if (cudaGetLastError() != cudaSuccess) return -1;
   }
-  if (!launch_mma(k_attention_dq_mma<BF16, DP>, table[0], BWD_CTA, DqLayout<DP>::TOTAL, slots * g.in.heads, !BF16, at, m, g, most)) return -1;
-  if (!launch_mma(k_attention_dkv_mma<BF16, DP>, table[1], BWD_CTA, DkvLayout<DP>::TOTAL, slots * g.in.key_heads, true, at, m, g, most)) return -1;
+  if (!launch_mma(k_attention_dq_mma<BF16, DP>, table[0], BWD_CTA, DqLayout<DP>::TOTAL, slots * g.in.heads, !BF16, at, m, g)) return -1;
+  if (!launch_mma(k_attention_dkv_mma<BF16, DP>, table[1], BWD_CTA, DkvLayout<DP>::TOTAL, slots * g.in.key_heads, true, at, m, g)) return -1;
   return BF16 ? 2 : 3;
 }
 
@@ -1095,7 +1072,7 @@ int launch_attention_mma(const adacgd_attention_args& g, const Where& at) {
   BY_KIND((fwd_mma<BF16, DP>(m, g, at)))
 }
 
-int launch_attention_backward_mma(const TrainScratch& ws, const adacgd_attention_backward_args& g, const Where& at) {
+int launch_attention_backward_mma(const adacgd_attention_backward_args& g, const Where& at) {
   const adacgd_attention_inputs& a = g.in;
   if (!takes(a) || !rows_on_16(g.out, g.out_stride, a.tokens) || !rows_on_16(g.dout, g.dout_stride, a.tokens) ||
       !rows_on_16(g.dq, g.dq_stride, a.tokens) || !rows_on_16(g.dk, g.dk_stride, a.tokens) || !rows_on_16(g.dv, g.dv_stride, a.tokens))
@@ -1104,7 +1081,7 @@ int launch_attention_backward_mma(const TrainScratch& ws, const adacgd_attention
   if (!map_of(&m.q, a.q, a.q_stride, a, a.heads) || !map_of(&m.k, a.k, a.k_stride, a, a.key_heads) || !map_of(&m.v, a.v, a.v_stride, a, a.key_heads) ||
       !map_of(&m.dout, g.dout, g.dout_stride, a, a.heads))
     return 0;
-  BY_KIND((bwd_mma<BF16, DP>(ws, m, g, at)))
+  BY_KIND((bwd_mma<BF16, DP>(m, g, at)))
 }
 
 }  // namespace adacgd

@@ -5,7 +5,7 @@ import torch
 
 import paper_2211_00188_b200 as pkg
 from oracle import training_oracle as O
-from test_mixing_gpu import attention_case, ints
+from test_mixing_gpu import attention_case, ints, score_tol
 from test_training_gpu import TYPES, close, dev, host, strided
 
 pytestmark = pytest.mark.gpu
@@ -87,3 +87,100 @@ def test_only_empty_sequences(ops, dtype, dim):
         assert torch.equal(a, b)
     del graph
     mine.close()
+
+
+def float16_case(ops, lengths, heads, kv, dim, seed, causal):
+    start = ints(np.cumsum([0] + list(lengths)), torch.int32)
+    b = Both(ops, sum(lengths), heads, kv, dim, torch.float16, seed, seq_start=start, causal=causal)
+    b.q *= 1.2
+    b.dout *= 0.01
+    return b
+
+
+def part(b, rows):
+    """The same tensors cut to the rows of one sequence, which then stands alone."""
+    n = rows.stop - rows.start
+    alone = Both(b.ops, n, b.heads, b.k.shape[1] * b.heads // b.q.shape[1], b.q.shape[1] // b.heads, b.q.dtype, 0, sequences=1, causal=b.kw["causal"])
+    for name in ("q", "k", "v", "dout"):
+        getattr(alone, name).copy_(getattr(b, name)[rows])
+    return alone
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dim,heads,kv", [(64, 2, 2), (128, 4, 2), (8, 9, 1), (80, 3, 1)])
+@pytest.mark.parametrize("other", ["large", "infinite dout", "infinite v", "nothing"])
+def test_float16_gradients_of_a_sequence_do_not_depend_on_another(ops, causal, dim, heads, kv, other):
+    """ds is brought into the type's range by a power of two; what decides it is the row's or the sequence's own.  A neighbour 10^5 times larger, or
+    infinite, changes no bit."""
+    lengths = [200, 333, 140]
+    b = float16_case(ops, lengths, heads, kv, dim, dim + heads, causal)
+    if other == "nothing":
+        b.dout[200:533] = 0.0
+    elif other == "large":
+        b.dout[200:533] *= 1e5
+        b.v[200:533] *= 10
+    elif other == "infinite v":
+        b.v[300, 0] = float("inf")
+    else:
+        b.dout[300, 1] = float("-inf")
+    b()
+    for rows in (slice(0, 200), slice(533, 673)):
+        alone = part(b, rows)
+        alone()
+        for name in ("out", "dq", "dk", "dv"):
+            assert torch.equal(getattr(b, name)[rows], getattr(alone, name)), name
+        assert torch.equal(b.lse[:, rows], alone.lse) and torch.equal(b.dot[:, rows], alone.dot)
+
+
+def test_float16_gradients_of_a_key_head_do_not_depend_on_another(ops):
+    b = float16_case(ops, [300, 90], 4, 2, 64, 3, True)
+    b()
+    want = [t.clone() for t in (b.dq, b.dk, b.dv)]
+    b.dout[:, 128:] *= 1e5
+    b.v[:, 64:] = float("inf")
+    b()
+    for got, w, cols in zip((b.dq, b.dk, b.dv), want, (128, 64, 64)):
+        assert torch.equal(got[:, :cols], w[:, :cols])
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("value", [5e4, float("inf"), float("nan")])
+def test_float16_gradients_of_a_query_do_not_depend_on_another(ops, causal, value):
+    """One row of dout far above the others: their dq keeps its bits, which are those of the formula.  dq_i adds n terms scale ds_ij k_j; ds is rounded in
+    binary16 (2^-11 of itself, or 2^-25 of its smallest step), multiplied so that 2 |dout_i| max|v| is at least 2^13."""
+    n, heads, dim = 500, 2, 64
+    b = float16_case(ops, [n], heads, 1, dim, 5, causal)
+    b()
+    want = b.dq.clone()
+    b.dout[123] = value
+    b()
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[123] = False
+    assert torch.equal(b.dq[keep], want[keep])
+    b.dout[123] = 0.0
+    r = O.attention_backward(host(b.dout), host(b.q), host(b.k), host(b.v), host(b.out), host(b.lse), heads, sequences=1, causal=causal)
+    s, E = dim ** -0.5, 2.0 ** -24
+    d = score_tol(host(b.q), host(b.k), heads, s)
+    wl = np.abs(host(b.lse)).max()
+    size = np.linalg.norm(host(b.dout).reshape(n, heads, dim), axis=2).repeat(dim, 1)
+    top = np.linalg.norm(host(b.v), axis=1).max()
+    tol = 2.0 ** -11 * np.abs(r["dq"]) + (2.0 ** -11 + 2 * d + 8 * E * (1 + wl) + 2 * (dim + 16) * E + (n + 32) * E) * r["aq"]
+    tol = tol + s * n * np.abs(host(b.k)).max() * 2.0 ** -25 * 2.002 * size * top / 2.0 ** 13 + 2.0 ** -25
+    k = host(keep).astype(bool)
+    close(want[keep], r["dq"][k], tol[k], "dq")
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_float16_gradients_with_rows_far_apart(ops, causal):
+    """Rows of dout over nine powers of ten, the largest in the middle: every row of dq has the accuracy of its own size."""
+    n, heads, dim = 400, 2, 128
+    b = float16_case(ops, [n], heads, 2, dim, 6, causal)
+    b.forward()
+    b.dout[:] = torch.randn_like(b.dout.float()).mul_(10.0 ** torch.linspace(-4, 2.5, n, device="cuda")[:, None]).half()
+    b.backward()
+    r = O.attention_backward(host(b.dout), host(b.q), host(b.k), host(b.v), host(b.out), host(b.lse), heads, sequences=1, causal=causal)
+    got = host(b.dq).reshape(n, heads, dim)
+    err = np.linalg.norm(got - r["dq"].reshape(n, heads, dim), axis=2)
+    # as in test_small_and_large_gradients_in_float16, for each row; the terms of a row may cancel, so against the norm of their sizes
+    lim = 2.0 ** -10 * np.linalg.norm(r["aq"].reshape(n, heads, dim), axis=2) + 2.0 ** -25 * np.sqrt(dim)
+    assert (err < lim).all(), (err / lim).max()
