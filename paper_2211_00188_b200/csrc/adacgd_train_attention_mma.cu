@@ -159,7 +159,8 @@ __device__ __forceinline__ void poison_row(void* base, long long stride, long lo
 }
 
 // 2^x of a pair on the multiplying units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 with the least relative error on
-// [-1/2, 1/2] (2.7e-6, computed by exchange; its mean is 4e-8), 2^n as a factor so that NaN stays NaN.  Below 2^-126 the result is 2^-126.
+// [-1/2, 1/2] (2.7e-6, computed by exchange; its mean is 4e-8), 2^n as a factor so that NaN stays NaN.  x is held at -127, where the factor's bits
+// come out as those of 0: what is below 2^-126.5 is exactly 0, as the hardware's function has it below 2^-126.
 __device__ __forceinline__ float at_least(float x, float low) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(low));
@@ -167,7 +168,7 @@ __device__ __forceinline__ float at_least(float x, float low) {
 }
 __device__ __forceinline__ F2 exp2_by_products(float x0, float x1) {
   const float big = 12582912.f;                                // 1.5 2^23: adding it rounds to an integer, in the low bits of the sum
-  const F2 x = f2(at_least(x0, -126.f), at_least(x1, -126.f)), t = add2(x, f2(big, big)), n = add2(t, f2(-big, -big));
+  const F2 x = f2(at_least(x0, -127.f), at_least(x1, -127.f)), t = add2(x, f2(big, big)), n = add2(t, f2(-big, -big));
   const F2 f = fma2(n, f2(-1.f, -1.f), x);
   F2 y = fma2(f2(0x1.3997d6p-7f, 0x1.3997d6p-7f), f, f2(0x1.ca1440p-5f, 0x1.ca1440p-5f));
   y = fma2(y, f, f2(0x1.ec06dap-3f, 0x1.ec06dap-3f));

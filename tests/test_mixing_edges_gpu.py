@@ -6,7 +6,7 @@ import torch
 import paper_2211_00188_b200 as pkg
 from oracle import training_oracle as O
 from test_mixing_gpu import attention_case, ints, score_tol
-from test_training_gpu import TYPES, close, dev, host, strided
+from test_training_gpu import TYPES, U, close, dev, host, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -184,3 +184,24 @@ def test_float16_gradients_with_rows_far_apart(ops, causal):
     # as in test_small_and_large_gradients_in_float16, for each row; the terms of a row may cancel, so against the norm of their sizes
     lim = 2.0 ** -10 * np.linalg.norm(r["aq"].reshape(n, heads, dim), axis=2) + 2.0 ** -25 * np.sqrt(dim)
     assert (err < lim).all(), (err / lim).max()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n,dim", [(128, 64), (384, 128)])
+def test_keys_of_no_weight_have_none(ops, dtype, n, dim):
+    """exp(-2000) is 0 in 64 bits too: values near the type's largest behind such scores reach nothing."""
+    dt = TYPES[dtype]
+    q, k, v = (torch.zeros(n, dim, device="cuda", dtype=dt) for _ in range(3))
+    q[:, 0] = 1.0
+    idle = torch.rand(n, generator=torch.Generator().manual_seed(n)).cuda() < 0.8
+    idle[0] = False
+    k[idle, 0] = -2000.0
+    v[idle] = 6e4 if dtype == "f16" else 1e38
+    v[~idle, 1] = 1.0
+    out, lse = torch.empty_like(q), torch.empty(1, n, device="cuda")
+    ops.attention(q, k, v, out, heads=1, lse=lse, sequences=1, causal=False, scale=1.0)
+    want = torch.zeros_like(out)
+    want[:, 1] = 1.0
+    assert torch.equal(out[:, :1], want[:, :1]) and torch.equal(out[:, 2:], want[:, 2:])
+    # the exponentials of the others are all 1, some by a polynomial that is off by 2.7e-6; the sum and the result add their roundings
+    close(out, host(want), 2.7e-6 + (n + 32) * 2.0 ** -24 + U[dt] + np.zeros((n, dim)), "out")
