@@ -28,8 +28,8 @@ __device__ __forceinline__ void fill_turns(const adacgd_qk_norm_args& a, long lo
   sn[p] = -s;
   sn[q] = s;
 }
+// The other element of e's pair; e < 2 pairs.
 __device__ __forceinline__ int partner(const adacgd_qk_norm_args& a, int e) {
-  if (e >= 2 * a.pairs) return e;
   if (a.interleaved) return e ^ 1;
   return e < a.pairs ? e + a.pairs : e - a.pairs;
 }
@@ -46,7 +46,8 @@ constexpr int ROT_CTA = 256;
 constexpr int ROT_MAX_TOKENS = 8;
 
 // How the partner of a pair is reached: NEAR within the lane (neighbours), LANE in another lane at the same place, ROW through shared
-// memory (halves whose distance is no whole number of runs).
+// memory (halves whose distance is no whole number of runs).  Behind the rotated front a partner counts as 0, so that an infinity there
+// stays where it is: its product with a sine of 0 would be NaN.
 enum Reach { NEAR, LANE, ROW };
 
 // The lane's eight elements turned.  cs, sn: the lane's entries of the token's tables.
@@ -60,12 +61,15 @@ __device__ __forceinline__ void rotate(const adacgd_qk_norm_args& a, const float
   }
   if (REACH == NEAR) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = x[j ^ 1];
+    for (int j = 0; j < 8; ++j) y[j] = e0 + j < 2 * a.pairs ? x[j ^ 1] : 0.f;
   } else if (REACH == LANE) {
     const int d = a.pairs / 8, me = e0 / 8;
     const int from = me < d ? me + d : (me < 2 * d ? me - d : me);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = __shfl_sync(0xffffffffu, x[j], from, LPH);
+    for (int j = 0; j < 8; ++j) {
+      y[j] = __shfl_sync(0xffffffffu, x[j], from, LPH);
+      if (me >= 2 * d) y[j] = 0.f;
+    }
   } else {
     __syncwarp();
 #pragma unroll
@@ -74,10 +78,10 @@ __device__ __forceinline__ void rotate(const adacgd_qk_norm_args& a, const float
     if (a.pairs % 4 == 0) {                           // four elements have their partners side by side
 #pragma unroll
       for (int j = 0; j < 8; j += 4)
-        *reinterpret_cast<float4*>(y + j) = *reinterpret_cast<const float4*>(row + (e0 + j < a.head_dim ? partner(a, e0 + j) : 0));
+        *reinterpret_cast<float4*>(y + j) = e0 + j < 2 * a.pairs ? *reinterpret_cast<const float4*>(row + partner(a, e0 + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = e0 + j < a.head_dim ? row[partner(a, e0 + j)] : 0.f;
+      for (int j = 0; j < 8; ++j) y[j] = e0 + j < 2 * a.pairs ? row[partner(a, e0 + j)] : 0.f;
     }
   }
 #pragma unroll
@@ -325,14 +329,16 @@ __device__ __forceinline__ F2 minus(F2 a) {
   r.v = a.v ^ 0x8000000080000000ull;
   return r;
 }
-// Turns the lane's sixteen elements: four packed pairs a run.
-template <int TURN, int LPH> __device__ __forceinline__ void turn_two(F2 (&x)[8], const F2 (&c)[4], const F2 (&s)[4], int l, int d) {
+// Turns the lane's sixteen elements, of a head of `dim`: four packed pairs a run.  See Reach for what lies behind the rotated front.
+template <int TURN, int LPH> __device__ __forceinline__ void turn_two(F2 (&x)[8], const F2 (&c)[4], const F2 (&s)[4], int l, int pairs, int dim) {
   if (TURN == FRONT) {
+    const int d = pairs / 8;
     const int from = l < d ? l + d : (l < 2 * d ? l - d : l);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       F2 y;
       y.v = __shfl_sync(0xffffffffu, x[j].v, from, LPH);
+      if (l >= 2 * d) y.v = 0;
       x[j] = fma2(y, s[j], mul2(x[j], c[j]));
     }
   } else if (TURN == HALVES) {
@@ -350,7 +356,8 @@ template <int TURN, int LPH> __device__ __forceinline__ void turn_two(F2 (&x)[8]
       split(c[j / 2], cx, cy);
       split(s[j / 2], sx, sy);
       const float u = j & 1 ? cy : cx, v = j & 1 ? sy : sx;
-      x[j] = f2(fmaf(a, u, -(b * v)), fmaf(b, u, a * v));
+      const bool on = 4 * l + (j < 4 ? j : dim / 4 + j - 4) < pairs;
+      x[j] = f2(fmaf(a, u, -((on ? b : 0.f) * v)), fmaf(b, u, (on ? a : 0.f) * v));
     }
   }
 }
@@ -393,7 +400,7 @@ __device__ __forceinline__ float dot16(const F2 (&x)[8], const F2 (&y)[8]) {
 
 // Heads [lo, hi) of one matrix row, LPH lanes a head and BATCH rounds of loads ahead.  `ready` makes w, c and s, behind the first loads.
 template <typename T, int LPH, int TURN, int BATCH, typename R>
-__device__ __forceinline__ void norm_heads(const T* x, T* out, int lo, int hi, int dim, float eps, int group, int e, int d, bool in, const F2 (&w)[8],
+__device__ __forceinline__ void norm_heads(const T* x, T* out, int lo, int hi, int dim, float eps, int group, int e, int pairs, bool in, const F2 (&w)[8],
                                            const F2 (&c)[4], const F2 (&s)[4], R ready) {
   constexpr int G = 32 / LPH;
   const int half = dim / 2;
@@ -422,7 +429,7 @@ __device__ __forceinline__ void norm_heads(const T* x, T* out, int lo, int hi, i
       const F2 r2 = f2(r, r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = mul2(mul2(v[j], r2), w[j]);
-      turn_two<TURN, LPH>(v, c, s, e / 8, d);
+      turn_two<TURN, LPH>(v, c, s, e / 8, pairs, dim);
       if (h < hi && in) store_two(out + (long long)h * dim + e, out + (long long)h * dim + e + half, v);
     }
   }
@@ -441,14 +448,14 @@ __global__ void __launch_bounds__(TWO_CTA) k_qk_norm_two(adacgd_qk_norm_args a, 
   const int lo = (int)((long long)heads * part / parts), hi = (int)((long long)heads * (part + 1) / parts), nq = (int)a.heads;
   F2 c[4], s[4], w[8];
   if (lo < nq) {
-    norm_heads<T, LPH, TURN, BATCH>((const T*)a.q + t * a.q_stride, (T*)a.q_out + t * a.q_out_stride, lo, min(hi, nq), a.head_dim, a.eps, group, e, a.pairs / 8, in, w, c, s, [&] {
+    norm_heads<T, LPH, TURN, BATCH>((const T*)a.q + t * a.q_stride, (T*)a.q_out + t * a.q_out_stride, lo, min(hi, nq), a.head_dim, a.eps, group, e, a.pairs, in, w, c, s, [&] {
       lane_weights<P>(a.q_weight, e, a.head_dim / 2, in, w);
       lane_turns<TURN>(a, t, l, in, tables[warp], false, c, s);
     });
   }
   if (hi > nq) {
     norm_heads<T, LPH, TURN, BATCH>((const T*)a.k + t * a.k_stride, (T*)a.k_out + t * a.k_out_stride, max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e,
-                                      a.pairs / 8, in, w, c, s, [&] {
+                                      a.pairs, in, w, c, s, [&] {
       lane_weights<P>(a.k_weight, e, a.head_dim / 2, in, w);
       if (lo >= nq) lane_turns<TURN>(a, t, l, in, tables[warp], false, c, s);
     });
@@ -456,7 +463,7 @@ __global__ void __launch_bounds__(TWO_CTA) k_qk_norm_two(adacgd_qk_norm_args a, 
 }
 
 template <typename T, int LPH, int TURN, int BATCH, typename R>
-__device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, int lo, int hi, int dim, float eps, int group, int e, int shift, bool in,
+__device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, int lo, int hi, int dim, float eps, int group, int e, int pairs, bool in,
                                                const F2 (&w)[8], const F2 (&c)[4], const F2 (&s)[4], F2 (&dw)[8], R ready) {
   constexpr int G = 32 / LPH;
   const int half = dim / 2;
@@ -485,7 +492,7 @@ __device__ __forceinline__ void norm_heads_bwd(const T* x, const T* y, T* out, i
       runs_of(a[k], b[k], v);
       runs_of(p[k], q[k], d);
       fetch(k, h + BATCH * G);
-      turn_two<TURN, LPH>(d, c, s, e / 8, shift);
+      turn_two<TURN, LPH>(d, c, s, e / 8, pairs, dim);
       const float r = rsqrtf(fmaf(head_sum<LPH>(dot16(v, v)), inv, eps));
       const F2 r2 = f2(r, r);
       const bool live = h < hi && in;
@@ -522,14 +529,14 @@ __global__ void __launch_bounds__(TWO_CTA, sizeof(T) == 4 ? 3 : 4) k_qk_norm_two
     F2 c[4], s[4], w[8];
     if (lo < nq) {
       norm_heads_bwd<T, LPH, TURN, BATCH>((const T*)a.q + t * a.q_stride, (const T*)a.q_out + t * a.q_out_stride, (T*)g.dq + t * g.dq_stride, lo,
-                                            min(hi, nq), a.head_dim, a.eps, group, e, a.pairs / 8, in, w, c, s, dwq, [&] {
+                                            min(hi, nq), a.head_dim, a.eps, group, e, a.pairs, in, w, c, s, dwq, [&] {
         lane_weights<P>(a.q_weight, e, half, in, w);
         lane_turns<TURN>(a, t, l, in, tables[warp], true, c, s);
       });
     }
     if (hi > nq) {
       norm_heads_bwd<T, LPH, TURN, BATCH>((const T*)a.k + t * a.k_stride, (const T*)a.k_out + t * a.k_out_stride, (T*)g.dk + t * g.dk_stride,
-                                            max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e, a.pairs / 8, in, w, c, s, dwk, [&] {
+                                            max(lo, nq) - nq, hi - nq, a.head_dim, a.eps, group, e, a.pairs, in, w, c, s, dwk, [&] {
         lane_weights<P>(a.k_weight, e, half, in, w);
         if (lo >= nq) lane_turns<TURN>(a, t, l, in, tables[warp], true, c, s);
       });
@@ -626,7 +633,7 @@ __global__ void __launch_bounds__(ANY_CTA) k_qk_norm_any(adacgd_qk_norm_args a) 
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int e = lane + 32 * k;
-      if (e < dim) out[e] = from_f<T>(r * fmaf(row[partner(a, e)], sn[e], row[e] * cs[e]));
+      if (e < dim) out[e] = from_f<T>(r * fmaf(e < 2 * a.pairs ? row[partner(a, e)] : 0.f, sn[e], row[e] * cs[e]));
     }
   }
 }
@@ -685,7 +692,7 @@ __global__ void __launch_bounds__(ANY_CTA) k_qk_norm_bwd_any(adacgd_qk_norm_back
         const int e = lane + 32 * k;
         dn[k] = 0.f;
         if (e < dim) {
-          const float d = fmaf(row[partner(a, e)], sn[e], u.v[k] * cs[e]), xr = v.v[k] * r;
+          const float d = fmaf(e < 2 * a.pairs ? row[partner(a, e)] : 0.f, sn[e], u.v[k] * cs[e]), xr = v.v[k] * r;
           if (query) dwq[k] = fmaf(d, xr, dwq[k]); else dwk[k] = fmaf(d, xr, dwk[k]);
           dn[k] = d * param<P>(w, e);
           dot = fmaf(dn[k], xr, dot);

@@ -205,3 +205,50 @@ def test_keys_of_no_weight_have_none(ops, dtype, n, dim):
     assert torch.equal(out[:, :1], want[:, :1]) and torch.equal(out[:, 2:], want[:, 2:])
     # the exponentials of the others are all 1, some by a polynomial that is off by 2.7e-6; the sum and the result add their roundings
     close(out, host(want), 2.7e-6 + (n + 32) * 2.0 ** -24 + U[dt] + np.zeros((n, dim)), "out")
+
+
+# ----------------------------------------------------------------------------- norm and rotation
+
+# head length, pairs, neighbours, extra columns, first element: each of the kernels' ways to a pair; heads longer than their rotated front
+FRONTS = [(64, 16, True, 0, 0), (64, 0, False, 0, 0), (128, 16, False, 0, 0), (256, 24, False, 0, 0), (72, 8, False, 0, 0), (72, 12, False, 0, 0),
+          (72, 10, False, 0, 0), (40, 8, True, 0, 0), (40, 0, True, 0, 0), (50, 12, True, 0, 0), (50, 12, False, 0, 0), (64, 16, True, 3, 1),
+          (130, 0, False, 0, 0), (272, 60, True, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("dim,pairs,interleaved,extra,shift", FRONTS)
+@pytest.mark.parametrize("where", ["x", "weight", "dout"])
+def test_infinities_outside_the_rotated_front(ops, dtype, dim, pairs, interleaved, extra, shift, where):
+    """An element that is not turned takes nothing from another one: an infinity there reaches what the formulas say, and no neighbour, in its own place or
+    in a weight's gradient."""
+    dt, rng, n, heads, kv, E = TYPES[dtype], np.random.default_rng(dim + pairs), 9, 3, 2, 2.0 ** -24
+    make = lambda c, s=1.0: strided(dev(rng.normal(size=(n, c)) * s, dt), extra, shift)  # noqa: E731
+    x, dout, w = [make(heads * dim), make(kv * dim)], [make(heads * dim, 0.1), make(kv * dim, 0.1)], [dev(rng.normal(size=dim) * 0.3 + 1) for _ in range(2)]
+    places = {2 * pairs + 1, (2 * pairs + dim) // 2, dim - 1}
+    for j, e in enumerate(places):
+        for c in (0, 1):
+            if where == "weight":
+                w[c][e] = float("inf")
+            else:
+                (x if where == "x" else dout)[c][2 + 2 * j, (j % 2) * dim + e] = float("inf")
+    pos, freq = rng.integers(1, 5000, n), torch.rand(pairs, device="cuda")
+    rot = dict(positions=ints(pos), freq=freq) if pairs else {}
+    out, dx, dw = [make(heads * dim), make(kv * dim)], [make(heads * dim), make(kv * dim)], [torch.empty(dim, device="cuda") for _ in range(2)]
+    common = dict(head_dim=dim, q_weight=w[0], k_weight=w[1], eps=1e-5, interleaved=interleaved, **rot)
+    ops.qk_norm(*x, *out, **common)
+    ops.qk_norm_backward(*dout, *x, *dx, dq_weight=dw[0], dk_weight=dw[1], **common)
+    K, eps, f = dim / 8 + 24, float(np.float32(1e-5)), host(freq)
+    size = lambda t: np.abs(np.nan_to_num(t, nan=0.0, posinf=0.0, neginf=0.0))  # noqa: E731
+    with np.errstate(all="ignore"):
+        for c in (0, 1):
+            wh, h, up = host(w[c]), host(x[c]).reshape(n, -1, dim), host(dout[c])
+            want = O.qk_norm(host(x[c]), dim, wh, eps, pos, f, interleaved)
+            r = 1 / np.sqrt((size(h) ** 2).mean(2, keepdims=True) + eps)
+            hr, one, amp = size(h) * r, size(wh), size(up).reshape(h.shape).max(2, keepdims=True)
+            top = (hr * one).max(2, keepdims=True) + 0 * hr
+            close(out[c], want, U[dt] * np.abs(want) + 2 * K * E * top.reshape(want.shape) + 2.0 ** -25, "out")
+            wdx, wdw = O.qk_norm_backward(up, host(x[c]), dim, wh, eps, pos, f, interleaved)
+            g = 2 * amp * one.max()
+            lim = r * (g + hr.max(2, keepdims=True) * (g * hr).mean(2, keepdims=True)) + 0 * hr
+            close(dx[c], wdx, U[dt] * np.abs(wdx) + 2 * K * E * lim.reshape(wdx.shape) + 2.0 ** -25, "dx")
+            close(dw[c], wdw, 2.0 ** -24 * np.abs(wdw) + ((n * h.shape[1] + 8) + 4 * K) * E * (2 * amp * hr).sum((0, 1)), "dweight")
