@@ -42,6 +42,7 @@ typedef struct adacgd_train adacgd_train; /* opaque; created by adacgd_train_ini
 #define ADACGD_BF16 2
 
 #define ADACGD_TRAIN_MAX_COLS 32768 /* widest row of adacgd_layer_norm and its backward pass */
+#define ADACGD_TRAIN_MAX_RUN (2147483648ll - 16777216ll) /* most tokens of a lookup's gradient, of attention and its backward pass: 2^31 - 2^24 */
 
 /* Bytes of device workspace for calls of at most max_tokens rows (of a norm's backward pass, or of logits; sequences
  * count as rows too) and norms of at most max_cols columns. */
@@ -214,7 +215,7 @@ adacgd_status adacgd_embedding(adacgd_train* t, const adacgd_embedding_args* a);
 /* Gradient of the lookup: dtable[v] = [base[v] +] scale * sum of dout[t] over the tokens t that count and have ids[t] = v.
  * The tokens of one id are summed in the order of the batch, in pieces: binary32 chains of at most max(16, tokens / 592) rows (1024 where
  * tokens <= 1024 and cols <= 1024), joined in binary32 in order.  Ids outside [0, vocab) add to nothing.  Every row of dtable is written,
- * unless base is the very same matrix: then rows without tokens stay as they are.  tokens <= max_tokens, cols <= max_cols. */
+ * unless base is the very same matrix: then rows without tokens stay as they are.  tokens <= max_tokens and ADACGD_TRAIN_MAX_RUN, cols <= max_cols. */
 typedef struct {
   int64_t tokens, vocab, cols;
   const void* ids;
@@ -281,7 +282,7 @@ adacgd_status adacgd_qk_norm_backward(adacgd_train* t, const adacgd_qk_norm_back
  * The tensor cores take the 16-bit types where head_dim is a multiple of 8 up to 128 and every matrix has rows on 16 bytes (pointer and
  * stride); everything else goes to the general cores, at a thirtieth to a hundredth of the rate. */
 typedef struct {
-  int64_t tokens, sequences;
+  int64_t tokens, sequences; /* tokens <= ADACGD_TRAIN_MAX_RUN */
   const int32_t* seq_start; /* [sequences + 1] or NULL */
   const uint8_t* mask;      /* [tokens] or NULL */
   const void* q;            int64_t q_stride;     /* [tokens, heads * head_dim] */

@@ -150,7 +150,7 @@ const char* check_qk(const adacgd_qk_norm_args& a) {
 }
 
 const char* check_attention(const adacgd_attention_inputs& a) {
-  if (a.tokens < 0 || a.tokens >= (1ll << 31)) return "tokens must be in [0, 2^31)";
+  if (a.tokens < 0 || a.tokens > ADACGD_TRAIN_MAX_RUN) return "tokens must be in [0, ADACGD_TRAIN_MAX_RUN = 2^31 - 2^24]";
   if (a.sequences < 1 || a.sequences >= (1ll << 31)) return "sequences must be in [1, 2^31)";
   if (((uintptr_t)a.seq_start) & 3) return "seq_start is not aligned";
   if (!a.seq_start && a.tokens % a.sequences) return "without seq_start, sequences must divide tokens";
@@ -454,7 +454,8 @@ adacgd_status adacgd_embedding(adacgd_train* t, const adacgd_embedding_args* a) 
 adacgd_status adacgd_embedding_backward(adacgd_train* t, const adacgd_embedding_backward_args* a) {
   const char* entry = "adacgd_embedding_backward";
   if (!t || !a) return invalid(t, entry, "context or arguments are NULL");
-  if (a->tokens < 0 || a->tokens > t->s.max_tokens) return invalid(t, entry, "tokens must be in [0, max_tokens]");
+  if (a->tokens < 0 || a->tokens > t->s.max_tokens || a->tokens > ADACGD_TRAIN_MAX_RUN)
+    return invalid(t, entry, "tokens must be in [0, max_tokens], at most ADACGD_TRAIN_MAX_RUN = 2^31 - 2^24");
   if (a->vocab < 1 || a->vocab >= (1ll << 31)) return invalid(t, entry, "vocab must be in [1, 2^31)");
   if (a->cols < 1 || a->cols > t->s.max_cols) return invalid(t, entry, "cols must be in [1, max_cols]");
   if (!good_type(a->dtype)) return invalid(t, entry, "unknown dtype");

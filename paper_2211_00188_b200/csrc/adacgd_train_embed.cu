@@ -257,6 +257,8 @@ __device__ __forceinline__ int lower_bound_lane(const u32* keys, int lo, int hi,
 
 constexpr int SUM_CTA = 256, SUM_ROWS = 32, SUM_MIN = 16, SUM_STAGE = 512;   // most rows of the table a CTA takes; tokens staged
 constexpr int MAX_WINDOWS = NORM_PARTS;   // two partial sums a window
+// Places among the sorted tokens are 32-bit: none that is formed, a window or a CTA's stride behind the last token, may pass 2^31.
+static_assert(ADACGD_TRAIN_MAX_RUN + (ADACGD_TRAIN_MAX_RUN + MAX_WINDOWS - 1) / MAX_WINDOWS + 32 * SORT_KEEP + SORT_CTA < (1ll << 31), "places fit in an int");
 
 struct SumArgs {
   const void* dout; long long dout_stride;

@@ -1,4 +1,6 @@
 """Calls of the operators that mix tokens which the formulas allow and an ordinary batch does not make.  Tolerances: see test_mixing_gpu.py."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -252,3 +254,42 @@ def test_infinities_outside_the_rotated_front(ops, dtype, dim, pairs, interleave
             lim = r * (g + hr.max(2, keepdims=True) * (g * hr).mean(2, keepdims=True)) + 0 * hr
             close(dx[c], wdx, U[dt] * np.abs(wdx) + 2 * K * E * lim.reshape(wdx.shape) + 2.0 ** -25, "dx")
             close(dw[c], wdw, 2.0 ** -24 * np.abs(wdw) + ((n * h.shape[1] + 8) + 4 * K) * E * (2 * amp * hr).sum((0, 1)), "dweight")
+
+
+# ----------------------------------------------------------------------------- the most tokens
+
+class Inputs(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("sequences", C.c_int64), ("seq_start", C.c_void_p), ("mask", C.c_void_p)] + \
+        [f for n in "qkv" for f in ((n, C.c_void_p), (n + "_stride", C.c_int64))] + \
+        [("heads", C.c_int32), ("key_heads", C.c_int32), ("head_dim", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float), ("dtype", C.c_int32)]
+
+
+class Forward(C.Structure):
+    _fields_ = [("in_", Inputs), ("out", C.c_void_p), ("out_stride", C.c_int64), ("lse", C.c_void_p)]
+
+
+class Gradient(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("vocab", C.c_int64), ("cols", C.c_int64), ("ids", C.c_void_p), ("mask", C.c_void_p)] + \
+        [f for n in ("dout", "base", "dtable") for f in ((n, C.c_void_p), (n + "_stride", C.c_int64))] + \
+        [("scale", C.c_float), ("dtype", C.c_int32), ("table_dtype", C.c_int32), ("id_bytes", C.c_int32)]
+
+
+def test_more_tokens_than_32_bit_places_are_refused():
+    """The checks alone: a context for 2^31 - 1 tokens, whose workspace would take 51 GB and is never touched, and matrices that are not there."""
+    lib = pkg.load_training_library()
+    need, ctx, small = C.c_size_t(), C.c_void_p(), torch.zeros(4096, dtype=torch.uint8, device="cuda")
+    most = 2 ** 31 - 2 ** 24
+    assert lib.adacgd_train_workspace_bytes(2 ** 31 - 1, 8, C.byref(need)) == 0
+    assert small.data_ptr() % 256 == 0
+    assert lib.adacgd_train_init(C.byref(ctx), 2 ** 31 - 1, 8, small.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == 0
+    at = small.data_ptr()
+    for tokens in (2 ** 31 - 1, most + 1):
+        g = Gradient(tokens=tokens, vocab=5, cols=8, ids=at, dout=at, dout_stride=8, dtable=at, dtable_stride=8, scale=1.0, id_bytes=4)
+        a = Forward(in_=Inputs(tokens=tokens, sequences=1, q=at, q_stride=8, k=at, k_stride=8, v=at, v_stride=8, heads=1, key_heads=1, head_dim=8, scale=1.0),
+                    out=at, out_stride=8)
+        for call, args in ((lib.adacgd_embedding_backward, g), (lib.adacgd_attention, a)):
+            assert call(ctx, C.byref(args)) == 1
+            assert b"MAX_RUN" in lib.adacgd_train_last_error(ctx)
+    assert lib.adacgd_train_launch_count(ctx) == 0
+    torch.cuda.synchronize()
+    lib.adacgd_train_destroy(ctx)

@@ -74,3 +74,20 @@ def test_no_tensor_copy_arrives_where_plain_accesses_came_before():
             stages = at["STAGES"] if "STAGES" in at else at["KS"] + at["VS"]
             tiles = at["RING"] + stages * at["BYTES"]                       # all that copies write
             assert tiles <= at["BARS"] and at["BARS"] + 64 + 16 * stages + 8 <= at["SCRATCH"] and at["SCRATCH"] + 8 <= at["TOTAL"] <= 227 * 1024, kernel
+
+
+def test_places_among_the_most_tokens_fit_in_32_bits():
+    """The numbers that the lookup's gradient and attention form in int, for the most tokens that they take: the end of a window or tile, one step behind the last
+    token.  (For 2^31 - 1 tokens each of them would be negative.)"""
+    header = open(os.path.join(os.path.dirname(os.path.dirname(CSRC)), "include", "adacgd_train.h")).read()
+    most = eval(re.search(r"#define ADACGD_TRAIN_MAX_RUN (\([^)]*\))", header).group(1).replace("ll", ""))
+    embed, shared, mma = source("adacgd_train_embed.cu"), source("adacgd_train.cuh"), source("adacgd_train_attention_mma.cu")
+    number = lambda text, name: int(re.search(r"\b" + name + r" = (\d+)", text).group(1))  # noqa: E731
+    windows = number(shared, "NORM_PARTS")
+    assert re.search(r"MAX_WINDOWS = NORM_PARTS;", embed)
+    window = -(-most // windows)
+    for text, name in ((embed, "SORT_CTA"), (embed, "SUM_CTA"), (mma, "FWD_CTA"), (mma, "BWD_CTA"), (mma, "TILE")):
+        assert most + window + 2 * number(text, name) < 2 ** 31
+    checks = source("adacgd_train.cu")
+    for entry in (r"const char\* check_attention\(.*?\n}", r"adacgd_status adacgd_embedding_backward\(.*?\n}"):
+        assert "tokens > ADACGD_TRAIN_MAX_RUN" in re.search(entry, checks, re.S).group()
