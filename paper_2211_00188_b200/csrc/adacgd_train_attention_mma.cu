@@ -5,7 +5,7 @@
 // Common to the three kernels.  A CTA holds one tile of rows and walks over the tiles it meets; tiles are 128 rows of 64 or
 // 128 columns in shared memory, rows of 128 bytes, swizzled, brought by one warp's tensor copies, which fill columns behind a
 // head's end with zeros.  One thread issues the products; their operands are tiles and, for probabilities and ds, tensor memory, where
-// the eight other warps, a thread a row, put them in place of the scores they were made from.
+// the row warps put them in place of the scores they were made from: forward eight of them, a thread a row, backward sixteen, four threads a row.
 // A row that does not count, or belongs to another sequence, must not reach a sum over rows even as 0 x NaN: where a tile that is summed over has
 // such rows, the copying warp sets them to zero before it hands the tile on.
 //

@@ -1,5 +1,6 @@
-// Norm and rotation of queries and keys, and its backward pass (adacgd_train.h).  Bound by memory: every element is read once and
-// written once.  A head is held by the lanes of a part of a warp, eight elements each, so its mean of squares is a few
+// Norm and rotation of queries and keys, and its backward pass (adacgd_train.h).  Every element is read once and written once.  Heads of a multiple of
+// 16 elements are bound by memory; the kernels for other lengths by a token's chain of latencies: position, angles, tables, barrier, heads.
+// A head is held by the lanes of a part of a warp, eight elements each, so its mean of squares is a few
 // shuffles; the cosines and sines of a token are made once (in binary64: position times frequency, reduced to a turn) and used by all its heads.
 #include "adacgd_train.cuh"
 
@@ -10,8 +11,9 @@ __device__ __forceinline__ long long position_at(const adacgd_qk_norm_args& a, l
   return a.position_bytes == 8 ? reinterpret_cast<const long long*>(a.positions)[t] : (long long)reinterpret_cast<const int32_t*>(a.positions)[t];
 }
 
-// Cosine and sine of position * freq.  The product of a 53-bit and a 24-bit number is rounded once in binary64; as turns it is reduced exactly, so the
-// angle is off by 2^-52 of itself: 1e-9 rad at ten million rad.
+// Cosine and sine of position * freq.  Position times frequency and that in turns are each rounded to binary64, as 1 / (2 pi) is; the reduction is
+// exact: the angle is off by 2^-51 of itself at most, 5e-9 rad at ten million rad.  Rounding what is left of the turn to binary32 adds up to 2^-26 of a
+// turn, 9.4e-8 rad, at any position.
 __device__ __forceinline__ void turn(long long position, float freq, float* c, float* s) {
   const double turns = (double)position * (double)freq * 0.15915494309189535;   // 1 / (2 pi)
   sincospif(2.f * (float)(turns - rint(turns)), s, c);

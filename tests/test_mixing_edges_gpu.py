@@ -293,3 +293,24 @@ def test_more_tokens_than_32_bit_places_are_refused():
     assert lib.adacgd_train_launch_count(ctx) == 0
     torch.cuda.synchronize()
     lib.adacgd_train_destroy(ctx)
+
+
+# ----------------------------------------------------------------------------- lookup
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n", [0, 40])
+@pytest.mark.parametrize("cols", [24, 1001, 2056])
+def test_a_gradient_of_no_token_that_counts(ops, dtype, n, cols):
+    """Every row is written all the same: 0, or the base's; in place nothing is."""
+    dt, vocab = TYPES[dtype], 77
+    tok = torch.arange(n, device="cuda") % vocab
+    dout = torch.full((n, cols), float("nan"), device="cuda", dtype=dt)
+    mask = torch.zeros(n, dtype=torch.bool, device="cuda")
+    base = torch.randn(vocab, cols, device="cuda").to(dt)
+    g = torch.full_like(base, 5.0)
+    ops.embedding_backward(tok, dout, g, mask=mask)
+    assert not g.any()
+    ops.embedding_backward(tok, dout, g, mask=mask, base=base)
+    assert torch.equal(g, base)
+    ops.embedding_backward(tok, dout, g, mask=mask, base=g)
+    assert torch.equal(g, base)
