@@ -433,10 +433,11 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
 // of two that brings the largest one possible, |dout_i| (|v_j| + |out_i|) <= 2 |dout_i| max|v|, below 2^14.  For dq that is a factor a row: the
 // row's own |dout_i| and the largest |v| of its sequence and key head.  dk sums over the rows, so there it is the largest |dout| of the sequence and of the
 // heads that share the key head.  What other sequences and key heads hold has no part in it.
-// This kernel takes the maxima of a tile, squared, a CTA one tile, key head and part of the heads that share it; LPR lanes take a head's row, four
-// rows at a time.  They wait in the rows of dv, which are written last: in the tile's first row and the key head's columns, the parts' maxima of |dout|, then that
-// of |v|.  The kernel of dq joins those of its sequence, and the first of a group's heads leaves what dk needs in its tile's own first row of dk: there it is read
-// and overwritten by one CTA.
+// This kernel takes the rows' products dout.out, their |dout|^2 and the maxima of a tile, a CTA one tile, key head and part of the heads that share it;
+// LPR lanes take a head's row, four rows at a time.  What the others need waits where it is overwritten last:
+//   |dout_i|^2 in the row's own columns of dq, read and overwritten by one CTA;
+//   the maxima in dv, in the tile's first row and the key head's columns: the parts' ones of |dout|^2, then that of |v|^2.  The kernel of dq joins those of
+//   its sequence, and where it has a group's first head it leaves dk's factor in its tile's own first row of dk, read and overwritten by one CTA.
 constexpr int RANGE_CTA = 256, RANGE_ROWS = 4;
 
 // Parts of a group of heads: as many as there are heads, and room for their maxima.
@@ -460,34 +461,59 @@ __global__ void __launch_bounds__(RANGE_CTA) k_attention_range(adacgd_attention_
   const int group = a.heads / a.key_heads, h0 = (int)((long long)group * part / parts), heads = (int)((long long)group * (part + 1) / parts) - h0;
   const int rows = min(TILE, t.length - t.first);
   const long long row = t.row + t.first;
-  auto largest = [&](const void* base, long long stride, int head, int count) {   // of |x|^2 over the tile's rows and `count` heads
-    float m = 0.f;
-    for (int i0 = 0; i0 < rows * count; i0 += GROUPS * RANGE_ROWS) {             // heads of a row lie side by side
-      Run<__half> x[RANGE_ROWS];
-      bool on[RANGE_ROWS];
+  float mo = 0.f, mv = 0.f;
+  auto sum = [](float v) {
 #pragma unroll
-      for (int u = 0; u < RANGE_ROWS; ++u) {
-        const int i = i0 + u * GROUPS + mine, r = i / count;
-        on[u] = in && r < rows && (!a.mask || a.mask[row + r]);
-        if (on[u]) x[u] = load_run((const __half*)base + (row + r) * stride + (long long)(head + i - r * count) * a.head_dim + d);
-      }
+    for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  };
+  for (int i0 = 0; i0 < rows * heads; i0 += GROUPS * RANGE_ROWS) {               // heads of a row lie side by side
+    Run<__half> x[RANGE_ROWS], y[RANGE_ROWS];
+    int r[RANGE_ROWS], head[RANGE_ROWS];
+    bool on[RANGE_ROWS];
 #pragma unroll
-      for (int u = 0; u < RANGE_ROWS; ++u) {
-        float v[8], sq = 0.f;
-        if (on[u]) {
-          unpack(x[u], v);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) sq = fmaf(v[k], v[k], sq);
-        }
-#pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-        m = fmaxf(m, sq);
+    for (int u = 0; u < RANGE_ROWS; ++u) {
+      const int i = i0 + u * GROUPS + mine;
+      r[u] = i / heads;
+      head[u] = kh * group + h0 + i - r[u] * heads;
+      on[u] = r[u] < rows && (!a.mask || a.mask[row + r[u]]);
+      if (on[u] && in) {
+        x[u] = load_run((const __half*)g.dout + (row + r[u]) * g.dout_stride + (long long)head[u] * a.head_dim + d);
+        y[u] = load_run((const __half*)g.out + (row + r[u]) * g.out_stride + (long long)head[u] * a.head_dim + d);
       }
     }
-    return m;
-  };
+#pragma unroll
+    for (int u = 0; u < RANGE_ROWS; ++u) {
+      float p[8], q[8], dot = 0.f, sq = 0.f;
+      if (on[u] && in) {
+        unpack(x[u], p);
+        unpack(y[u], q);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          dot = fmaf(p[k], q[k], dot);
+          sq = fmaf(p[k], p[k], sq);
+        }
+      }
+      dot = sum(dot);
+      sq = sum(sq);
+      mo = fmaxf(mo, sq);
+      if (lane == 0 && r[u] < rows) g.row_dot[(long long)head[u] * a.tokens + row + r[u]] = dot;
+      if (lane == 0 && on[u]) *range_at(g.dq, g.dq_stride, row + r[u], head[u], a.head_dim) = sq;
+    }
+  }
+  if (part == 0) {
+#pragma unroll 4
+    for (int r = mine; r < (rows + GROUPS - 1) / GROUPS * GROUPS; r += GROUPS) {
+      float v[8], sq = 0.f;
+      if (in && r < rows && (!a.mask || a.mask[row + r])) {
+        unpack(load_run((const __half*)a.v + (row + r) * a.v_stride + (long long)kh * a.head_dim + d), v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sq = fmaf(v[k], v[k], sq);
+      }
+      mv = fmaxf(mv, sum(sq));
+    }
+  }
   __shared__ float most[2][GROUPS];
-  const float mo = largest(g.dout, g.dout_stride, kh * group + h0, heads), mv = part == 0 ? largest(a.v, a.v_stride, kh, 1) : 0.f;
   if (lane == 0) {
     most[0][mine] = mo;
     most[1][mine] = mv;
@@ -500,19 +526,22 @@ __global__ void __launch_bounds__(RANGE_CTA) k_attention_range(adacgd_attention_
   }
 }
 
-// The power of two, of the squares of the largest |dout| and |v|.
+// The power of two, of the squares of the largest |dout| and |v|: 2 |dout| |v| is at least 2^(half the exponent of 4 dout2 v2, rounded down).  The squares
+// are in [2^-48, 2^40] or 0; 4.01 makes up for the roundings.
 __device__ __forceinline__ float range_of(float dout2, float v2) {
-  const float bound = 2.002f * sqrtf(dout2) * sqrtf(v2);
-  if (!(bound > 0.f) || isinf(bound)) return 1.f;
-  return __int_as_float(((int)fminf(fmaxf(13.f - floorf(log2f(bound)), -60.f), 60.f) + 127) << 23);
+  const float square = 4.01f * dout2 * v2;
+  if (!(square > 0.f) || isinf(square)) return 1.f;
+  const int half = ((__float_as_int(square) >> 23) - 127) >> 1;
+  return __int_as_float((127 + min(13 - half, 60)) << 23);
 }
 // The largest of numbers [from, to) of the sequence's tiles begin .. end - 1: by a warp.
 __device__ __forceinline__ float join_range(const adacgd_attention_backward_args& g, const Tile& t, int kh, int begin, int end, int from, int to) {
-  const int each = to - from;
   float m = 0.f;
-  for (long long i = threadIdx.x & 31; i < (long long)(end - begin) * each; i += 32) {
-    const long long k = i / each;
-    m = fmaxf(m, __ldcg(range_at(g.dv, g.dv_stride, t.row + (begin + k) * TILE, kh, g.in.head_dim) + from + (i - k * each)));
+#pragma unroll 2
+  for (int k = begin + (int)(threadIdx.x & 31); k < end; k += 32) {
+    const float* const at = range_at(g.dv, g.dv_stride, t.row + (long long)k * TILE, kh, g.in.head_dim);
+#pragma unroll 4
+    for (int i = from; i < to; ++i) m = fmaxf(m, __ldcg(at + i));
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -550,7 +579,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
     const int i = t.first + (int)threadIdx.x;
     if (threadIdx.x < TILE && i < t.length) {
       zero_row(g.dq, g.dq_stride, t.row + i, head, a.head_dim);
-      g.row_dot[(long long)head * a.tokens + t.row + i] = 0.f;
+      if (BF16) g.row_dot[(long long)head * a.tokens + t.row + i] = 0.f;
     }
     if (!BF16) asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
@@ -608,6 +637,12 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
       ++nv;
       bring<DP>(v_tiles + sv * L::BYTES, &maps.v, kh, t.row + first, words, false, v_full + 8 * sv, aside, side, dead);
     }
+    if (!BF16 && head == kh * (a.heads / a.key_heads)) {         // for dk, under the last products
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      const int parts = range_parts(a);
+      const float all = join_range(g, t, kh, begin, end, 0, parts), v = join_range(g, t, kh, begin, end, parts, parts + 1);
+      if (lane == 0) __stcg(range_at(g.dk, g.dk_stride, t.row + t.first, kh, a.head_dim), range_of(all, v));
+    }
     if (*dead) {
       settle(q_full, 0);
       for (int b = max(0, nk - L::KS); b < nk; ++b) settle(k_full + 8 * (b % L::KS), (b / L::KS) & 1);
@@ -653,41 +688,32 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dq_mma(const __grid_co
     const u32 lanes = (u32)(warp & 3) << 21;
     const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
     const long long at = (long long)head * a.tokens + t.row + i;
-    typedef typename std::conditional<BF16, __nv_bfloat16, __half>::type T;
-    float dot = 0.f, sq = 0.f, range = 1.f;
-    if (on) {                                                  // each quarter of the warps takes 32 of the head's elements
-      const T* const x = (const T*)g.dout + (t.row + i) * g.dout_stride + (long long)head * a.head_dim;
-      const T* const y = (const T*)g.out + (t.row + i) * g.out_stride + (long long)head * a.head_dim;
-      for (int d = 32 * part_of; d < min(a.head_dim, 32 * part_of + 32); d += 8) {
-        float u[8], v[8];
-        unpack(load_run(x + d), u);
-        unpack(load_run(y + d), v);
+    float dot = 0.f, range = 1.f;
+    if (BF16) {
+      if (on) {                                                // each quarter of the warps takes 32 of the head's elements
+        const __nv_bfloat16* const x = (const __nv_bfloat16*)g.dout + (t.row + i) * g.dout_stride + (long long)head * a.head_dim;
+        const __nv_bfloat16* const y = (const __nv_bfloat16*)g.out + (t.row + i) * g.out_stride + (long long)head * a.head_dim;
+        for (int d = 32 * part_of; d < min(a.head_dim, 32 * part_of + 32); d += 8) {
+          float u[8], v[8];
+          unpack(load_run(x + d), u);
+          unpack(load_run(y + d), v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          dot = fmaf(u[k], v[k], dot);
-          if (!BF16) sq = fmaf(u[k], u[k], sq);
+          for (int k = 0; k < 8; ++k) dot = fmaf(u[k], v[k], dot);
         }
       }
-    }
-    auto row_sum = [&](float v) {                              // of the row's four threads
-      part[part_of * TILE + r] = v;
+      part[part_of * TILE + r] = dot;
       asm volatile("bar.sync 1, 512;" ::: "memory");
-      return (part[r] + part[TILE + r]) + (part[2 * TILE + r] + part[3 * TILE + r]);
-    };
-    dot = row_sum(dot);
-    if (part_of == 0 && inside) g.row_dot[at] = dot;
-    if (!BF16) {
-      asm volatile("bar.sync 1, 512;" ::: "memory");           // the sums before have been read
-      sq = row_sum(sq);
+      dot = (part[r] + part[TILE + r]) + (part[2 * TILE + r] + part[3 * TILE + r]);
+      if (part_of == 0 && inside) g.row_dot[at] = dot;
+    } else {
       asm volatile("griddepcontrol.wait;" ::: "memory");
-      const int parts = range_parts(a);
-      const float most = join_range(g, t, kh, begin, end, parts, parts + 1);
-      range = range_of(sq, most);
+      // each number is fetched once a CTA: their addresses lie a row of the matrix apart (by every thread that needs them: 644 against 615 us at 8192 tokens)
+      if (on) dot = __ldcg(g.row_dot + at);
+      if (part_of == 0) part[r] = on ? __ldcg(range_at(g.dq, g.dq_stride, t.row + i, head, a.head_dim)) : 0.f;
+      if (warp == 4) part[TILE + lane] = join_range(g, t, kh, begin, end, range_parts(a), range_parts(a) + 1);
+      asm volatile("bar.sync 1, 512;" ::: "memory");
+      range = range_of(part[r], part[TILE]);
       dot *= range;
-      if (warp == 0 && head == kh * (a.heads / a.key_heads)) {
-        const float all = join_range(g, t, kh, begin, end, 0, parts);
-        if (lane == 0) __stcg(reinterpret_cast<float2*>(range_at(g.dk, g.dk_stride, t.row + t.first, kh, a.head_dim)), make_float2(all, most));
-      }
     }
     const float low = on ? -g.lse[at] * LOG2E : -INFINITY, c = a.scale * LOG2E;
     const F2 c2 = f2(c, c), low2 = f2(low, low), dot2 = f2(-dot, -dot), range2 = f2(range, range);
@@ -820,10 +846,6 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
   const u32 k_tile = base, v_tile = base + L::BYTES, ring = base + L::RING;
   // binary16: p is taken 2^14 times larger, ds by its range (see above)
   const float shift = BF16 ? 0.f : 14.f, back = BF16 ? 1.f : 6.103515625e-05f;
-  auto own_range = [&] {
-    const float2 m = __ldcg(reinterpret_cast<const float2*>(range_at(g.dk, g.dk_stride, t.row + t.first, kh, a.head_dim)));
-    return range_of(m.x, m.y);
-  };
   const int begin = a.causal ? t.first / TILE : low_tile, each = high_tile - begin, n = each * group;
   if (warp == BWD_ROWS + 1) {
     u32 side = 0, words[4];
@@ -843,7 +865,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
         if (i >= 4 && L::STAGES > 5 && !mbar_wait(empty + 8 * ((i - 5) % L::STAGES), ((i - 5) / L::STAGES) & 1, dead)) break;
         if (i == 1) {                                          // row_dot comes from the kernel before this one
           asm volatile("griddepcontrol.wait;" ::: "memory");
-          if (!BF16) range = own_range();
+          if (!BF16) range = __ldcg(range_at(g.dk, g.dk_stride, t.row + t.first, kh, a.head_dim));
         }
         float* const to = stats + (j & 1) * 2 * TILE;
         const long long at = (long long)head * a.tokens + t.row + first;
@@ -902,7 +924,7 @@ __global__ void __launch_bounds__(BWD_CTA, 1) k_attention_dkv_mma(const __grid_c
     float range = 1.f;
     if (!BF16) {
       asm volatile("griddepcontrol.wait;" ::: "memory");
-      range = own_range();
+      range = __ldcg(range_at(g.dk, g.dk_stride, t.row + t.first, kh, a.head_dim));
     }
     const float c = a.scale * LOG2E;
     const F2 c2 = f2(c, c), range2 = f2(range * back, range * back);
