@@ -47,10 +47,11 @@ __device__ __forceinline__ long long place(long long stride, long long t, int h,
 constexpr int ROT_CTA = 256;
 constexpr int ROT_MAX_TOKENS = 8;
 
-// How the partner of a pair is reached: NEAR within the lane (neighbours), LANE in another lane at the same place, ROW through shared
-// memory (halves whose distance is no whole number of runs).  Behind the rotated front a partner counts as 0, so that an infinity there
-// stays where it is: its product with a sine of 0 would be NaN.
-enum Reach { NEAR, LANE, ROW };
+// How the partner of a pair is reached: NEAR within the lane (neighbours, whole heads), PART the same of a front of the head or none of it, LANE in
+// another lane at the same place, ROW through shared memory (halves whose distance is no whole number of runs).  Behind the rotated front a
+// partner counts as 0, so that an infinity there stays where it is: its product with a sine of 0 would be NaN.  (PART for whole heads too took 79 registers
+// instead of 64, 51.5 instead of 45.4 us for 16384 x 16 heads of 72.)
+enum Reach { NEAR, LANE, ROW, PART };
 
 // The lane's eight elements turned.  cs, sn: the lane's entries of the token's tables.
 template <int LPH, int REACH>
@@ -61,9 +62,9 @@ __device__ __forceinline__ void rotate(const adacgd_qk_norm_args& a, const float
     *reinterpret_cast<float4*>(c + j) = *reinterpret_cast<const float4*>(cs + e0 + j);
     *reinterpret_cast<float4*>(s + j) = *reinterpret_cast<const float4*>(sn + e0 + j);
   }
-  if (REACH == NEAR) {
+  if (REACH == NEAR || REACH == PART) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = e0 + j < 2 * a.pairs ? x[j ^ 1] : 0.f;
+    for (int j = 0; j < 8; ++j) y[j] = REACH == NEAR || e0 + j < 2 * a.pairs ? x[j ^ 1] : 0.f;
   } else if (REACH == LANE) {
     const int d = a.pairs / 8, me = e0 / 8;
     const int from = me < d ? me + d : (me < 2 * d ? me - d : me);
@@ -300,13 +301,15 @@ constexpr int TWO_CTA = 128, TWO_WARPS = TWO_CTA / 32, MAX_PAIRS = 128;
 
 // Cosines and sines of the lane's pairs, packed in twos.  HALVES: pair 8 l + j couples the runs' j-th elements.  NEIGHBOURS: pair 4 l + i is
 // elements 2 i and 2 i + 1 of the first run, and those of the second follow.  FRONT: halves of at most the head's first half, by whole
-// runs: pair 8 (l mod pairs / 8) + j is the first run's j-th element here and pairs / 8 lanes further; the sine has the element's sign.
-enum Turn { HALVES, NEIGHBOURS, FRONT };
+// runs: pair 8 (l mod pairs / 8) + j is the first run's j-th element here and pairs / 8 lanes further; the sine has the element's sign.  PARTLY:
+// neighbours in a front of the head.  NONE: no pairs.  (One kernel for the last two and NEIGHBOURS: 131 instead of 127 us for 32768 x 40 heads of 128.)
+enum Turn { HALVES, NEIGHBOURS, FRONT, PARTLY, NONE };
 template <int TURN>
 __device__ __forceinline__ void lane_turns(const adacgd_qk_norm_args& a, long long t, int l, bool in, float* table, bool back, F2 (&c)[4], F2 (&s)[4]) {
+  if (TURN == NONE) return;
   float* const sines = table + MAX_PAIRS;
   __syncwarp();
-  const long long position = a.pairs ? position_at(a, t) : 0;
+  const long long position = position_at(a, t);
   for (int i = threadIdx.x & 31; i < a.head_dim / 2; i += 32) {
     float x = 1.f, y = 0.f;
     if (i < a.pairs) turn(position, a.freq[i], &x, &y);
@@ -333,6 +336,7 @@ __device__ __forceinline__ F2 minus(F2 a) {
 }
 // Turns the lane's sixteen elements, of a head of `dim`: four packed pairs a run.  See Reach for what lies behind the rotated front.
 template <int TURN, int LPH> __device__ __forceinline__ void turn_two(F2 (&x)[8], const F2 (&c)[4], const F2 (&s)[4], int l, int pairs, int dim) {
+  if (TURN == NONE) return;
   if (TURN == FRONT) {
     const int d = pairs / 8;
     const int from = l < d ? l + d : (l < 2 * d ? l - d : l);
@@ -358,7 +362,7 @@ template <int TURN, int LPH> __device__ __forceinline__ void turn_two(F2 (&x)[8]
       split(c[j / 2], cx, cy);
       split(s[j / 2], sx, sy);
       const float u = j & 1 ? cy : cx, v = j & 1 ? sy : sx;
-      const bool on = 4 * l + (j < 4 ? j : dim / 4 + j - 4) < pairs;
+      const bool on = TURN == NEIGHBOURS || 4 * l + (j < 4 ? j : dim / 4 + j - 4) < pairs;
       x[j] = f2(fmaf(a, u, -((on ? b : 0.f) * v)), fmaf(b, u, (on ? a : 0.f) * v));
     }
   }
@@ -738,7 +742,8 @@ template <typename T> bool head_runs(const adacgd_qk_norm_args& a) {
          on_runs<T>(a.q_out, a.q_out_stride, a.tokens) && on_runs<T>(a.k_out, a.k_out_stride, a.tokens);
 }
 Reach reach_of(const adacgd_qk_norm_args& a) {
-  if (a.interleaved || a.pairs == 0) return NEAR;
+  if (a.interleaved && 2 * a.pairs == a.head_dim) return NEAR;
+  if (a.interleaved || a.pairs == 0) return PART;
   return a.pairs % 8 == 0 ? LANE : ROW;
 }
 
@@ -848,7 +853,9 @@ int two_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g,
   if (a.head_dim <= 128) { constexpr int LPH = 8; BY_TURN(call) }                                      \
   { constexpr int LPH = 16; BY_TURN(call) }
 #define BY_TURN(call)                                                                                  \
-  if (a.interleaved || a.pairs == 0) { constexpr int TURN = NEIGHBOURS; return call; }                 \
+  if (a.pairs == 0) { constexpr int TURN = NONE; return call; }                                        \
+  if (a.interleaved && 2 * a.pairs < a.head_dim) { constexpr int TURN = PARTLY; return call; }         \
+  if (a.interleaved) { constexpr int TURN = NEIGHBOURS; return call; }                                 \
   if (2 * a.pairs == a.head_dim) { constexpr int TURN = HALVES; return call; }                         \
   { constexpr int TURN = FRONT; return call; }
 
@@ -859,6 +866,7 @@ int two_bwd_launch(const TrainScratch& s, const adacgd_qk_norm_backward_args& g,
   { constexpr int LPH = 32; BY_REACH(call) }
 #define BY_REACH(call)                                                                                 \
   if (reach == NEAR) { constexpr int REACH = NEAR; return call; }                                      \
+  if (reach == PART) { constexpr int REACH = PART; return call; }                                      \
   if (reach == LANE) { constexpr int REACH = LANE; return call; }                                      \
   { constexpr int REACH = ROW; return call; }
 
