@@ -12,7 +12,8 @@
  * Conventions, where they differ from or add to those of adacgd.h
  *   - A context (adacgd_train) owns nothing on the device: the caller gives it a workspace, which it must not share
  *     with another context.  All work is enqueued on the stream given to adacgd_train_init; no call synchronises.
- *     Inputs have to be ready, and outputs are ready, in that stream's order.  One call at a time per context.
+ *     Inputs have to be ready, and outputs are ready, in that stream's order.  One call at a time per context, captured
+ *     ones too: graphs with calls of one context are replayed one after the other.
  *   - A context is bound to the device that was current at adacgd_train_init, as adacgd_ctx is.
  *   - Matrices are row-major with a row stride in elements and unit column stride; vectors are contiguous.  No
  *     alignment beyond the element's own is needed; rows aligned to 16 bytes
@@ -235,7 +236,7 @@ adacgd_status adacgd_embedding_backward(adacgd_train* t, const adacgd_embedding_
  * and the first 2 pairs elements of n are turned in pairs (a, b), by the angle position * freq[i] for pair i:
  *   a' = a cos - b sin,  b' = b cos + a sin;   (a, b) = elements (i, pairs + i), or with interleaved (2 i, 2 i + 1).
  * The angle is the product of the position and the binary32 number freq[i], formed and reduced in binary64.  k may be NULL
- * with key_heads = 0; pairs = 0 is the norm alone. */
+ * with key_heads = 0; pairs = 0 is the norm alone.  The mean of the squares is a binary32 number: it is infinite for elements beyond 1.8e19, and 0 below 1e-23. */
 typedef struct {
   int64_t tokens, heads, key_heads;
   int32_t head_dim;        /* in [1, ADACGD_TRAIN_MAX_HEAD] */
@@ -315,7 +316,7 @@ typedef struct {
   float* row_dot;           /* [heads][tokens] */
   void* dq;                 int64_t dq_stride;
   void* dk;                 int64_t dk_stride;
-  void* dv;                 int64_t dv_stride;
+  void* dv;                 int64_t dv_stride;     /* dq, dk and dv hold other numbers while the call runs */
 } adacgd_attention_backward_args;
 adacgd_status adacgd_attention_backward(adacgd_train* t, const adacgd_attention_backward_args* a);
 

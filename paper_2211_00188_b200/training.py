@@ -73,7 +73,8 @@ class TrainingOps:
 
     max_tokens bounds the rows of a norm's or lookup's backward pass and of logits, max_cols the columns of those backward passes.
     Work runs on `stream` (default: the stream that is current now).  A call made while another stream is current is
-    ordered behind that stream's work, and that stream waits for it.  One thread at a time per context.
+    ordered behind that stream's work, and that stream waits for it.  One thread at a time per context; graphs captured from
+    one context are replayed one after the other.
 
     Matrices are 2-D with unit column stride and any row stride, of type float32, float16 or bfloat16; vectors are
     contiguous.  Rows must not overlap: an expanded row is refused.  Outputs may be the very same tensor as an input matrix
