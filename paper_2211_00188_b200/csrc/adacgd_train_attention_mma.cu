@@ -8,6 +8,8 @@
 // the row warps put them in place of the scores they were made from: forward eight of them, a thread a row, backward sixteen, four threads a row.
 // A row that does not count, or belongs to another sequence, must not reach a sum over rows even as 0 x NaN: where a tile that is summed over has
 // such rows, the copying warp sets them to zero before it hands the tile on.
+// p and ds are rounded to the matrices' type, as an operand of a product is of the other one's type; the errors of the results are 1.2 to 1.45 times
+// those of a computation in 32 bits that rounds them alone.
 //
 // The backward pass is two kernels that each compute the scores again, seven products for the five that are needed: every sum stays in one
 // CTA's tensor memory, without atomics, and dq needs no binary32 array.
@@ -204,7 +206,7 @@ __device__ __forceinline__ u32 low_bits(int n) { return n <= 0 ? 0u : (n >= 32 ?
 // A CTA takes two tiles of queries of a head, A and B.  While the products of one run, four warps turn the scores of the other into
 // probabilities: S = Q K^T, the row's maximum, p = 2^(c s - c max) in S's place, O += p V.  The maximum that p is taken against is
 // moved only when it has grown by more than 2^8, so O, which stays in tensor memory, is hardly ever rescaled; p is at most 256 then, and the
-// division by the sum at the end takes it out.  binary16 has few numbers below 1: there p is taken 2^7 times larger, at most 2^15.
+// division by the sum at the end takes it out.  (Rows of other sequences and rows that do not count have no say in that: a rescaling changes roundings.)  binary16 has few numbers below 1: there p is taken 2^7 times larger, at most 2^15.
 template <int DP> struct FwdLayout {
   static constexpr int BYTES = DP * 256, STAGES = DP == 128 ? 5 : 8, RING = 2 * BYTES, BARS = RING + STAGES * BYTES;
   static constexpr int TOTAL = BARS + 256, SCRATCH = TOTAL - 8;
@@ -326,6 +328,7 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
     const int x = warp >> 2, i = t.first + x * TILE + (warp & 3) * 32 + lane;
     const u32 lanes = (u32)(warp & 3) << 21, s_at = tmem + x * TILE + lanes, o_at = tmem + 2 * TILE + x * DP + lanes;
     const float c = a.scale * LOG2E;
+    const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
     float top = -INFINITY, sum = 0.f;
     bool ok = true;
     // A and B end with the same tile; where causal, A's walk begins a tile later
@@ -364,7 +367,7 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
       const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
       if (u == 0) {
         top = most;
-      } else if (__any_sync(0xffffffffu, (most - top) * c > 8.f)) {   // -inf - -inf is NaN: no
+      } else if (__any_sync(0xffffffffu, on && (most - top) * c > 8.f)) {   // only rows that count decide; -inf - -inf is NaN: no
         const float now = fmaxf(top, most), f = now == -INFINITY ? 1.f : ex2((top - now) * c);
         sum *= f;
         top = now;
@@ -412,7 +415,6 @@ __global__ void __launch_bounds__(FWD_CTA, 1) k_attention_mma(const __grid_const
     }
     if (count[x] && ok && mbar_wait(o_full + 8 * x, 0, dead)) {
       tc_fence_after();
-      const bool inside = i < t.length, on = inside && (!a.mask || a.mask[t.row + i]);
 #pragma unroll
       for (int d = 0; d < DP; d += 32) store_cols<BF16>(g.out, g.out_stride, t.row + i, head, a.head_dim, d, o_at, 1.f / sum, inside, !on);
       if (inside && g.lse) g.lse[(long long)head * a.tokens + t.row + i] = on ? fmaf(top, a.scale, logf(BF16 ? sum : sum * 0.0078125f)) : -INFINITY;

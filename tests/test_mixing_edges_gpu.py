@@ -209,6 +209,41 @@ def test_keys_of_no_weight_have_none(ops, dtype, n, dim):
     close(out, host(want), 2.7e-6 + (n + 32) * 2.0 ** -24 + U[dt] + np.zeros((n, dim)), "out")
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("masked", [False, True])
+def test_large_scores_of_other_rows_change_no_bit(ops, dtype, dim, causal, masked):
+    """Rows of the next sequence, or that do not count, lie in the same tile of queries.  Their scores rise far from one tile of keys to the next, while
+    those of the rows that count hardly do: the results are the bits of the sequence that stands alone, or of a batch whose masked rows hold zeros."""
+    dt, n, heads = TYPES[dtype], 400, 2
+    b = Both(ops, n, heads, 1, dim, dt, dim, causal=causal)
+    start = ints([0, 200, 400], torch.int32)
+    mask = torch.ones(n, dtype=torch.bool, device="cuda")
+    if masked:
+        mask[170:200:3] = False
+        mask[360::2] = False
+    b.kw.update(seq_start=start, mask=mask if masked else None)
+    b.q.mul_(0.5)
+    b.k[:, 5], b.k[0:128, 5], b.k[200:328, 5] = 0.0, 1.0, 1.0
+    b.q[:, 5] = 0.0
+    b.q[:, dim + 5] = 0.0
+    plain = b.q.clone()
+    b()
+    want = [t.clone() for t in b.results()]
+    for name, rows in (("next", slice(200, 400)), ("masked", ~mask)):
+        b.q.copy_(plain)
+        b.q[rows, 5] = 300.0
+        b.q[rows, dim + 5] = 200.0
+        b()
+        keep = torch.zeros(n, dtype=torch.bool, device="cuda")
+        keep[:200] = True
+        if name == "masked":
+            keep[:] = True
+        for got, w, by_row in zip(b.results(), want, (True, False, False, True, True, True)):
+            assert torch.equal(got[keep], w[keep]) if by_row else torch.equal(got[:, keep], w[:, keep]), name
+
+
 # ----------------------------------------------------------------------------- norm and rotation
 
 # head length, pairs, neighbours, extra columns, first element: each of the kernels' ways to a pair; heads longer than their rotated front
